@@ -8,13 +8,16 @@ from pathlib import Path
 
 HERE = Path(__file__).resolve().parent
 ROOT = HERE.parent
-SRC = HERE / "csrc" / "tula_ags.cu"
+CSRC = HERE / "csrc"
+SRC = CSRC / "tula_ags.cu"
+SRCS = [SRC, CSRC / "tula_train.cu", CSRC / "tula_mx.cu"]
 HEADER = ROOT / "include" / "tula_ags.h"
+TRAIN_HEADER = ROOT / "include" / "tula_train.h"
 LIB = HERE / "libtula_ags.so"
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC,-O2", "-shared",
-              "-cudart", "shared", "-fmad=false"]
+              "-cudart", "shared", "-fmad=false", "--threads", "0"]
 
 
 def cuda_lib_dir(nvcc: str) -> str:
@@ -36,7 +39,7 @@ def _stale() -> bool:
     if not LIB.exists():
         return True
     t = LIB.stat().st_mtime
-    return any(p.stat().st_mtime > t for p in (SRC, HEADER))
+    return any(p.stat().st_mtime > t for p in (*SRCS, CSRC / "tula_common.h", HEADER, TRAIN_HEADER))
 
 
 def build(force: bool = False, verbose: bool = False) -> Path:
@@ -46,7 +49,7 @@ def build(force: bool = False, verbose: bool = False) -> Path:
     tmp = LIB.with_name(f"{LIB.name}.{os.getpid()}.tmp")
     nvcc = nvcc_path()
     cmd = [nvcc, *ARCH, *NVCC_FLAGS, "-Xlinker", f"-rpath={cuda_lib_dir(nvcc)}",
-           "-I", str(ROOT / "include"), str(SRC), "-o", str(tmp)]
+           "-I", str(ROOT / "include"), *map(str, SRCS), "-o", str(tmp)]
     if verbose:
         cmd.insert(1, "-Xptxas=-v")
     subprocess.run(cmd, check=True)

@@ -40,6 +40,7 @@
 // the order in which tiles land, so results are bitwise reproducible and
 // independent of the grid and of which CTA took which tile.
 #include "tula_ags.h"
+#include "tula_common.h"
 
 #include <cuda_runtime.h>
 
@@ -2702,6 +2703,11 @@ int check_ws(void *ws, size_t bytes, int n, const Plan &pl) {
 
 
 }  // namespace
+
+namespace tula {
+void note_launch() { g_launches.fetch_add(1, std::memory_order_relaxed); }
+void note_cuda_error(int e) { g_last_cuda = e; }
+}  // namespace tula
 
 // ============================================================================
 // C ABI

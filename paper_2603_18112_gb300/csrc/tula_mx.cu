@@ -1,0 +1,745 @@
+// Microscaled 4-bit matrices (MXFP4) for sm_103a: quantisation, reading back, products.
+#include "tula_common.h"
+#include "tula_train.h"
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <cstring>
+#include <type_traits>
+
+namespace {
+
+constexpr unsigned kFull = 0xffffffffu;
+constexpr int kTile = 128;          // rows and columns of a scale tile
+constexpr int kScaleTile = 512;     // its bytes: 128 rows by 4 blocks of 32 columns
+constexpr int kBlock = 32;          // elements that share a scale
+
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_start() {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+// ----------------------------------------------------------------------------
+// Elements
+// ----------------------------------------------------------------------------
+
+// Word of two elements of a 16-bit type as two floats.
+template <typename T>
+__device__ __forceinline__ float2 pair_of(unsigned u) {
+    if (std::is_same<T, __half>::value) {
+        __half2 h;
+        memcpy(&h, &u, 4);
+        return __half22float2(h);
+    }
+    return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+}
+
+// The block's scale byte from the bits of its largest magnitude (as fp32; infinities and NaN have
+// larger bits than any number).
+__device__ __forceinline__ unsigned scale_byte(unsigned top) {
+    const unsigned e = top >> 23;
+    return e == 255u ? 255u : e > 2u ? e - 2u : 0u;
+}
+// What its elements are multiplied by: 2^(127 - s), exact; 0 for a block that is NaN, whose codes
+// are 0.
+__device__ __forceinline__ float inverse_scale(unsigned s) {
+    return s == 255u ? 0.f : __uint_as_float((254u - s) << 23);
+}
+
+// Eight elements' codes, the first in the lowest bits.  A magnitude of 6 or more gives 6.
+__device__ __forceinline__ unsigned codes8(const float (&x)[8]) {
+    unsigned r;
+    asm("{\n"
+        ".reg .b8 b0, b1, b2, b3;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n"
+        "mov.b32 %0, {b0, b1, b2, b3};\n"
+        "}\n"
+        : "=r"(r)
+        : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]));
+    return r;
+}
+
+// ----------------------------------------------------------------------------
+// Quantisation
+// ----------------------------------------------------------------------------
+//
+// One CTA per 128 x 128 tile of x, which is one scale tile of x and one of its transpose.  Along
+// the rows four lanes share a block, eight elements each; the transpose reads the tile again from
+// shared memory, a thread per two columns by 32 rows.  HBM bounds it: 2 or 4 bytes in and 17/32
+// out per element and form, against some ten operations.
+
+struct QuantArgs {
+    const void *x;
+    long long rows, cols, stride;
+    unsigned char *codes, *scales, *codes_t, *scales_t;
+    int tiles_c;  // tiles along the columns
+    int tiles_r;
+};
+
+// Eight elements of a row from column c on, as they are: 16-bit types in 4 words, fp32 in 8.  Zero
+// beyond `left` elements.  VB: bytes that a load may take (the row's alignment).
+template <typename T, int VB>
+__device__ __forceinline__ void load_row8(unsigned (&w)[sizeof(T) * 2], const T *p, long long left) {
+    constexpr int kWords = sizeof(T) * 2;
+    if (left >= 8 && VB >= 4) {
+        if (VB == 16) {
+#pragma unroll
+            for (int k = 0; k < kWords / 4; ++k) {
+                const uint4 q = __ldcs(reinterpret_cast<const uint4 *>(p) + k);
+                w[4 * k] = q.x, w[4 * k + 1] = q.y, w[4 * k + 2] = q.z, w[4 * k + 3] = q.w;
+            }
+        } else if (VB == 8) {
+#pragma unroll
+            for (int k = 0; k < kWords / 2; ++k) {
+                const uint2 q = __ldcs(reinterpret_cast<const uint2 *>(p) + k);
+                w[2 * k] = q.x, w[2 * k + 1] = q.y;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kWords; ++k) w[k] = __ldcs(reinterpret_cast<const unsigned *>(p) + k);
+        }
+        return;
+    }
+    if (sizeof(T) == 4) {
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) w[k] = k < left ? __ldcs(reinterpret_cast<const unsigned *>(p) + k) : 0u;
+    } else {
+        const unsigned short *h = reinterpret_cast<const unsigned short *>(p);
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) {
+            const unsigned lo = 2 * k < left ? __ldcs(h + 2 * k) : 0, hi = 2 * k + 1 < left ? __ldcs(h + 2 * k + 1) : 0;
+            w[k] = lo | hi << 16;
+        }
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void floats8(float (&x)[8], const unsigned (&w)[sizeof(T) * 2]) {
+    if (sizeof(T) == 4) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = __uint_as_float(w[k]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 f = pair_of<T>(w[k]);
+            x[2 * k] = f.x;
+            x[2 * k + 1] = f.y;
+        }
+    }
+}
+
+template <typename T, int VB, bool Rows, bool Cols>
+__global__ void __launch_bounds__(256) k_quantize(const QuantArgs a) {
+    constexpr int kWords = sizeof(T) * 2;   // of eight elements
+    constexpr int kPitch = kTile * sizeof(T) / 4;  // words of a tile's row
+    extern __shared__ __align__(16) unsigned tile[];  // Cols: kTile * kPitch
+    __shared__ __align__(16) unsigned scale_words[2][kTile];
+    let_next_start();
+    wait_for_previous();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tr = blockIdx.x / a.tiles_c, tc = blockIdx.x % a.tiles_c;
+    const long long r0 = (long long)tr * kTile, c0 = (long long)tc * kTile;
+    const int sub = lane & 15;  // eight columns of the tile
+    const long long left = a.cols - c0 - 8 * sub;
+    const size_t pitch = (size_t)a.tiles_c * (kTile / 2);
+    unsigned w[8][kWords];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const long long r = r0 + warp * 16 + 2 * i + (lane >> 4);
+        const T *p = static_cast<const T *>(a.x) + r * a.stride + c0 + 8 * sub;
+        load_row8<T, VB>(w[i], p, r < a.rows ? left : 0);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int row = warp * 16 + 2 * i + (lane >> 4);
+        if (Rows) {
+            float x[8];
+            floats8<T>(x, w[i]);
+            unsigned top = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(x[k]) & 0x7fffffffu);
+            top = max(top, __shfl_xor_sync(kFull, top, 1));
+            top = max(top, __shfl_xor_sync(kFull, top, 2));
+            const unsigned s = scale_byte(top);
+            const float f = inverse_scale(s);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = __fmul_rn(x[k], f);
+            const unsigned q = s == 255u ? 0u : codes8(x);
+            unsigned word = s << (8 * (sub >> 2));
+            word |= __shfl_xor_sync(kFull, word, 4);
+            word |= __shfl_xor_sync(kFull, word, 8);
+            if (r0 + row < a.rows)
+                *reinterpret_cast<unsigned *>(a.codes + (size_t)(r0 + row) * pitch + c0 / 2 + 4 * sub) = q;
+            if (sub == 0) scale_words[0][(row & 31) * 4 + (row >> 5)] = word;
+        }
+        if (Cols) {
+#pragma unroll
+            for (int k = 0; k < kWords / 4; ++k)
+                *reinterpret_cast<uint4 *>(&tile[row * kPitch + sub * kWords + 4 * k]) =
+                    make_uint4(w[i][4 * k], w[i][4 * k + 1], w[i][4 * k + 2], w[i][4 * k + 3]);
+        }
+    }
+    __syncthreads();
+    if (Rows && tid < 32)
+        *reinterpret_cast<uint4 *>(a.scales + ((size_t)tr * a.tiles_c + tc) * kScaleTile + 16 * tid) =
+            *reinterpret_cast<const uint4 *>(&scale_words[0][4 * tid]);
+    if (!Cols) return;
+    // columns 2 * (tid % 64) and the next, rows 32 * (tid / 64) on
+    const int pair = tid & 63, rb = tid >> 6;
+    unsigned q[2][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        unsigned top = 0;
+        float x[32];
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+            const unsigned *p = &tile[(32 * rb + k) * kPitch + pair * (int)(sizeof(T) / 2)];
+            if (sizeof(T) == 4) {
+                x[k] = __uint_as_float(p[h]);
+            } else {
+                const float2 f = pair_of<T>(p[0]);
+                x[k] = h ? f.y : f.x;
+            }
+            top = max(top, __float_as_uint(x[k]) & 0x7fffffffu);
+        }
+        const unsigned s = scale_byte(top);
+        const float f = inverse_scale(s);
+#pragma unroll
+        for (int k = 0; k < 32; k += 8) {
+            float y[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = __fmul_rn(x[k + j], f);
+            q[h][k / 8] = s == 255u ? 0u : codes8(y);
+        }
+        const int c = 2 * pair + h;
+        reinterpret_cast<unsigned char *>(scale_words[1])[(c & 31) * 16 + (c >> 5) * 4 + rb] = (unsigned char)s;
+    }
+    __syncthreads();  // the tile's values are all read: their place takes the codes
+    constexpr int kOut = 20;  // words of a column's 64 bytes of codes, and 16 bytes to spread the banks
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        *reinterpret_cast<uint4 *>(&tile[(2 * pair + h) * kOut + 4 * rb]) = make_uint4(q[h][0], q[h][1], q[h][2], q[h][3]);
+    __syncthreads();
+    const size_t pitch_t = (size_t)a.tiles_r * (kTile / 2);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int c = k * 64 + (tid >> 2), part = tid & 3;
+        if (c0 + c < a.cols)
+            *reinterpret_cast<uint4 *>(a.codes_t + (size_t)(c0 + c) * pitch_t + r0 / 2 + 16 * part) =
+                *reinterpret_cast<const uint4 *>(&tile[c * kOut + 4 * part]);
+    }
+    if (tid < 32)
+        *reinterpret_cast<uint4 *>(a.scales_t + ((size_t)tc * a.tiles_r + tr) * kScaleTile + 16 * tid) =
+            *reinterpret_cast<const uint4 *>(&scale_words[1][4 * tid]);
+}
+
+// ----------------------------------------------------------------------------
+// Reading back
+// ----------------------------------------------------------------------------
+
+__device__ __forceinline__ float scale_value(unsigned s) {
+    return s == 255u ? __uint_as_float(0x7fffffffu) : __uint_as_float(s ? s << 23 : 0x00400000u);
+}
+// Two codes' values.
+__device__ __forceinline__ float2 code_pair(unsigned byte) {
+    unsigned h;
+    asm("{\n.reg .b8 b, u1, u2, u3;\nmov.b32 {b, u1, u2, u3}, %1;\ncvt.rn.f16x2.e2m1x2 %0, b;\n}\n" : "=r"(h) : "r"(byte));
+    __half2 v;
+    memcpy(&v, &h, 4);
+    return __half22float2(v);
+}
+
+__device__ __forceinline__ void put(float *p, float v) { *p = v; }
+__device__ __forceinline__ void put(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
+__device__ __forceinline__ void put(__half *p, float v) { *p = __float2half_rn(v); }
+
+// Eight values from column 8 * (index % row_groups) of a row, a thread each.
+template <typename T, bool Vec>
+__global__ void __launch_bounds__(256) k_dequantize(const unsigned char *codes, const unsigned char *scales,
+                                                    long long rows, long long cols, long long groups, T *out) {
+    let_next_start();
+    wait_for_previous();
+    const long long n = rows * groups, tiles_c = (cols + kTile - 1) / kTile;
+    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
+        const long long r = i / groups, c = 8 * (i % groups);
+        const unsigned q = __ldcs(reinterpret_cast<const unsigned *>(codes + (size_t)r * tiles_c * (kTile / 2) + c / 2));
+        const unsigned s = scales[((size_t)(r / kTile) * tiles_c + c / kTile) * kScaleTile + (r & 31) * 16 +
+                                  (r & 127) / 32 * 4 + (c & 127) / kBlock];
+        const float f = scale_value(s);
+        __align__(16) T y[8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 v = code_pair(q >> (8 * k) & 0xffu);
+            put(&y[2 * k], __fmul_rn(v.x, f));
+            put(&y[2 * k + 1], __fmul_rn(v.y, f));
+        }
+        T *p = out + r * cols + c;
+        if (Vec) {
+#pragma unroll
+            for (int k = 0; k < (int)sizeof(T) / 2; ++k)
+                __stcs(reinterpret_cast<uint4 *>(p) + k, reinterpret_cast<const uint4 *>(y)[k]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (c + k < cols) p[k] = y[k];
+        }
+    }
+}
+
+// ----------------------------------------------------------------------------
+// Products: tcgen05 with block scales
+// ----------------------------------------------------------------------------
+//
+// out = A B^T by tiles of 128 rows of one operand (P, the instruction's M) by NT rows of the other
+// (Q, its N).  Codes come by TMA, 256 columns (128 bytes a row) a stage, scales by bulk copies;
+// one thread moves a stage's scales to tensor memory and issues its instructions (64 columns each,
+// two scales a row); accumulators lie in tensor memory and four warps read them back.
+
+constexpr int kStageK = 256;
+constexpr uint32_t kSpinLimit = 1u << 19;  // bound on every wait (~2 s)
+constexpr int kMmaThreads = 192;           // a copying warp, an issuing warp, four that read back
+
+static __device__ unsigned g_mx_error;
+
+__device__ __forceinline__ uint32_t smem_addr(const void *p) {
+    return (uint32_t)__cvta_generic_to_shared(p);
+}
+__device__ __forceinline__ void mbar_init(uint32_t bar, unsigned count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint32_t bar, unsigned bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint32_t bar, unsigned parity) {
+    unsigned ok;
+    asm volatile("{\n.reg .pred p;\n"
+                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+                 "selp.u32 %0, 1, 0, p;\n}\n"
+                 : "=r"(ok)
+                 : "r"(bar), "r"(parity)
+                 : "memory");
+    return ok != 0;
+}
+// False if the wait ran out, here or before in another warp (`dead`).
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, unsigned parity, volatile int *dead) {
+    for (uint32_t i = 0; i < kSpinLimit; ++i) {
+        if (mbar_try(bar, parity)) return true;
+        if (*dead) return false;
+    }
+    *dead = 1;
+    atomicOr(&g_mx_error, 1u);
+    return false;
+}
+
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+                 "l"(map), "r"(x), "r"(y), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, unsigned bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+                 "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
+}
+
+// Shared-memory matrix descriptors: addresses in units of 16 bytes; bit 46: their version.
+// Codes: rows of 128 bytes with the 128-byte swizzle, groups of eight rows 1024 bytes apart.
+__device__ __forceinline__ uint64_t codes_desc(uint32_t addr) {
+    return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
+           (uint64_t)2 << 61;
+}
+// A scale tile: 32 rows of 16 bytes, no swizzle, groups of eight rows 128 bytes apart.
+__device__ __forceinline__ uint64_t scales_desc(uint32_t addr) {
+    return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+}
+// The instruction's descriptor: E2M1 operands, E8M0 scales, M = 128, N.
+__host__ __device__ constexpr uint32_t mma_desc(int n) {
+    return 1u << 7 | 1u << 10 | (uint32_t)(n >> 3) << 17 | 1u << 23 | (128u >> 7) << 27;
+}
+// Which two of a word's four scales the instruction takes: id 0 or 2, of both operands.
+__device__ __forceinline__ uint32_t with_scale_id(uint32_t desc, uint32_t id) {
+    return desc | id << 4 | id << 29;
+}
+
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, bool add) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %6, 0;\n"
+                 "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}\n" ::"r"(d),
+                 "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"((unsigned)add)
+                 : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_alloc(uint32_t where, unsigned cols) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(where), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+}
+__device__ __forceinline__ void tmem_free(uint32_t tmem, unsigned cols) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols));
+}
+// 16 columns of this warp's 32 lanes.
+__device__ __forceinline__ void tmem_load16(float (&v)[16], uint32_t tmem) {
+    unsigned r[16];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+                   "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(tmem));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int k = 0; k < 16; ++k) v[k] = __uint_as_float(r[k]);
+}
+
+struct MatmulArgs {
+    const unsigned char *p_scales, *q_scales;
+    void *out;
+    long long P, Q;       // rows of each operand
+    long long ld_p, ld_q; // elements of out from one row of P (Q) to the next
+    int tiles_k;          // of 128 columns
+    int p_tiles, q_tiles; // tiles of each operand's scales along its rows
+    int grid_q;           // CTAs along Q
+};
+
+template <int NT>
+struct MmaShape {
+    static constexpr int kScaleTilesQ = NT > 128 ? NT / 128 : 1;
+    static constexpr int kP = 128 * 128, kQ = NT * 128;                     // bytes of codes a stage
+    static constexpr int kSP = 2 * kScaleTile, kSQ = 2 * kScaleTilesQ * kScaleTile;
+    static constexpr int kStage = kP + kQ + kSP + kSQ;
+    static constexpr int kStages = NT >= 256 ? 4 : NT >= 128 ? 3 : 5;
+    static constexpr int kSmem = kStages * kStage + 1024;                   // aligned to 1024 at run time
+    static constexpr int kScaleP = NT < 32 ? 32 : NT;                       // tensor memory columns
+    static constexpr int kScaleQ = kScaleP + 8;
+    static constexpr int kUsed = kScaleQ + 8 * kScaleTilesQ;
+    static constexpr int kCols = kUsed <= 64 ? 64 : kUsed <= 128 ? 128 : kUsed <= 256 ? 256 : 512;
+};
+
+template <int NT, typename T>
+__global__ void __launch_bounds__(kMmaThreads) k_matmul(const __grid_constant__ CUtensorMap map_p,
+                                                        const __grid_constant__ CUtensorMap map_q, const MatmulArgs a) {
+    using S = MmaShape<NT>;
+    extern __shared__ __align__(16) unsigned tile[];
+    __shared__ __align__(8) unsigned long long bars[2 * S::kStages + 1];
+    __shared__ uint32_t tmem_at;
+    __shared__ volatile int dead;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t stages = (smem_addr(tile) + 1023) & ~1023u;
+    const uint32_t full = smem_addr(bars), empty = full + 8 * S::kStages, done = empty + 8 * S::kStages;
+    const int tp = blockIdx.x / a.grid_q, tq = blockIdx.x % a.grid_q;
+    const int stages_k = (a.tiles_k + 1) / 2;
+    if (tid == 0) {
+        for (int s = 0; s < S::kStages; ++s) {
+            mbar_init(full + 8 * s, 1);
+            mbar_init(empty + 8 * s, 1);
+        }
+        mbar_init(done, 1);
+        dead = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc(smem_addr(&tmem_at), S::kCols);
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = tmem_at;
+    let_next_start();
+    wait_for_previous();
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int issued = 0;
+            for (int k = 0; k < stages_k; ++k) {
+                const int s = k % S::kStages;
+                if (k >= S::kStages && !mbar_wait(empty + 8 * s, (k / S::kStages - 1) & 1, &dead)) break;
+                const uint32_t at = stages + s * S::kStage, bar = full + 8 * s;
+                const int tiles = min(2, a.tiles_k - 2 * k);  // scale tiles along the columns
+                mbar_expect(bar, S::kP + S::kQ + (1 + S::kScaleTilesQ) * tiles * kScaleTile);
+                tma_load_2d(at, &map_p, k * (kStageK / 2), tp * 128, bar);
+                tma_load_2d(at + S::kP, &map_q, k * (kStageK / 2), tq * NT, bar);
+                bulk_load(at + S::kP + S::kQ, a.p_scales + ((size_t)tp * a.tiles_k + 2 * k) * kScaleTile, tiles * kScaleTile, bar);
+                for (int j = 0; j < S::kScaleTilesQ; ++j) {
+                    // rows beyond Q: any scales will do, their results are not stored
+                    const int row = min(tq * S::kScaleTilesQ + j, a.q_tiles - 1);
+                    bulk_load(at + S::kP + S::kQ + S::kSP + j * 2 * kScaleTile,
+                              a.q_scales + ((size_t)row * a.tiles_k + 2 * k) * kScaleTile, tiles * kScaleTile, bar);
+                }
+                issued = k + 1;
+            }
+            // no copy may be in flight when the CTA ends
+            if (dead)
+                for (int k = max(0, issued - S::kStages); k < issued; ++k) {
+                    const int s = k % S::kStages;
+                    for (uint32_t i = 0; i < kSpinLimit && !mbar_try(full + 8 * s, (k / S::kStages) & 1); ++i) {}
+                }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (lane == 0) {
+            for (int k = 0; k < stages_k; ++k) {
+                const int s = k % S::kStages;
+                if (!mbar_wait(full + 8 * s, (k / S::kStages) & 1, &dead)) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t at = stages + s * S::kStage, sc = at + S::kP + S::kQ;
+                const int tiles = min(2, a.tiles_k - 2 * k);
+                for (int t = 0; t < tiles; ++t) {
+                    copy_scales(tmem + S::kScaleP + 4 * t, scales_desc(sc + t * kScaleTile));
+                    for (int j = 0; j < S::kScaleTilesQ; ++j)
+                        copy_scales(tmem + S::kScaleQ + 4 * (t * S::kScaleTilesQ + j),
+                                    scales_desc(sc + S::kSP + (j * 2 + t) * kScaleTile));
+                }
+                const uint64_t da = codes_desc(at), db = codes_desc(at + S::kP);
+                for (int t = 0; t < tiles; ++t)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        mma(tmem, da + 2 * (2 * t + h), db + 2 * (2 * t + h), with_scale_id(mma_desc(NT), 2 * h),
+                            tmem + S::kScaleP + 4 * t, tmem + S::kScaleQ + 4 * t * S::kScaleTilesQ, k > 0 || t > 0 || h > 0);
+                commit(empty + 8 * s);
+            }
+            commit(done);
+        }
+        __syncwarp();
+    } else {
+        const bool ok = stages_k == 0 || mbar_wait(done, 0, &dead);
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const int quad = warp & 3;  // the quarter of tensor memory's lanes that this warp may read
+        const long long p = (long long)tp * 128 + quad * 32 + lane;
+        T *out = static_cast<T *>(a.out) + p * a.ld_p;
+        const bool vec = a.ld_q == 1 && ((a.ld_p * sizeof(T)) & 15) == 0 && (reinterpret_cast<uintptr_t>(a.out) & 15) == 0;
+        if (ok) {
+            for (int c = 0; c < NT; c += 16) {
+                const long long q0 = (long long)tq * NT + c;
+                if (q0 >= a.Q) break;
+                float v[16];
+                __syncwarp();
+                if (stages_k) {
+                    tmem_load16(v, tmem + ((unsigned)(quad * 32) << 16) + c);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) v[k] = 0.f;
+                }
+                if (p >= a.P) continue;
+                if (vec && q0 + 16 <= a.Q) {
+                    __align__(16) T y[16];
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) put(&y[k], v[k]);
+#pragma unroll
+                    for (int k = 0; k < (int)sizeof(T); ++k)
+                        reinterpret_cast<uint4 *>(out + q0)[k] = reinterpret_cast<const uint4 *>(y)[k];
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k)
+                        if (q0 + k < a.Q) put(out + (q0 + k) * a.ld_q, v[k]);
+                }
+            }
+        }
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    }
+    __syncthreads();
+    if (warp == 1) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        tmem_free(tmem, S::kCols);
+    }
+}
+
+// ----------------------------------------------------------------------------
+// Host side
+// ----------------------------------------------------------------------------
+
+int cuda_failed(cudaError_t e) {
+    tula::note_cuda_error((int)e);
+    return TULA_ERR_CUDA;
+}
+
+inline long long up(long long n, long long m) { return (n + m - 1) / m; }
+inline int type_size(int type) { return type == TULA_TYPE_F32 ? 4 : 2; }
+inline bool good_type(int type) { return type >= TULA_TYPE_F32 && type <= TULA_TYPE_F16; }
+inline bool aligned(const void *p, unsigned n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+// Tiles of 128 x 128; -1 beyond what one grid and 32-bit coordinates hold.
+long long tiles_of(long long rows, long long cols) {
+    if (rows < 0 || cols < 0 || rows > (1LL << 38) || cols > (1LL << 31) || rows > (1LL << 31)) return -1;
+    const long long t = up(rows, kTile) * up(cols, kTile);
+    return t < (1LL << 31) ? t : -1;
+}
+
+template <typename T, int VB>
+int launch_quantize(const QuantArgs &a, unsigned grid, cudaStream_t s) {
+    void (*k)(const QuantArgs) = a.codes && a.codes_t ? k_quantize<T, VB, true, true>
+                                 : a.codes            ? k_quantize<T, VB, true, false>
+                                                      : k_quantize<T, VB, false, true>;
+    const int smem = a.codes_t ? kTile * kTile * (int)sizeof(T) : 0;
+    if (smem > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute((const void *)k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return cuda_failed(e);
+    }
+    return tula::launch(k, dim3(grid), 256, smem, s, 1, a);
+}
+template <typename T>
+int quantize_typed(const QuantArgs &a, unsigned grid, cudaStream_t s) {
+    const size_t both = reinterpret_cast<uintptr_t>(a.x) | (a.rows > 1 ? (size_t)a.stride * sizeof(T) : 0);
+    if (both % 16 == 0) return launch_quantize<T, 16>(a, grid, s);
+    if (both % 8 == 0) return launch_quantize<T, 8>(a, grid, s);
+    if (both % 4 == 0) return launch_quantize<T, 4>(a, grid, s);
+    return launch_quantize<T, 2>(a, grid, s);
+}
+
+template <typename T>
+int dequantize_typed(const void *codes, const void *scales, long long rows, long long cols, void *out, cudaStream_t s) {
+    const long long groups = up(cols, 8);
+    const bool vec = aligned(out, 16) && cols * (long long)sizeof(T) % 16 == 0 && cols % 8 == 0;
+    const long long blocks = std::min<long long>(up(rows * groups, 256), 152 * 64);
+    return tula::launch(vec ? k_dequantize<T, true> : k_dequantize<T, false>, dim3((unsigned)blocks), 256, 0, s, 1,
+                        static_cast<const unsigned char *>(codes), static_cast<const unsigned char *>(scales), rows, cols,
+                        groups, static_cast<T *>(out));
+}
+
+typedef CUresult (*EncodeFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                             const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                             CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeFn encode_fn() {
+    static EncodeFn fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q);
+        return e == cudaSuccess && q == cudaDriverEntryPointSuccess ? reinterpret_cast<EncodeFn>(p) : nullptr;
+    }();
+    return fn;
+}
+
+// Codes as a matrix of bytes, boxes of 128 bytes by `rows` rows.
+bool codes_map(CUtensorMap *m, const void *codes, long long rows, long long pitch, int box_rows) {
+    const EncodeFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)pitch, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch};
+    const cuuint32_t box[2] = {128, (cuuint32_t)box_rows}, steps[2] = {1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(codes), dims, strides, box, steps,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int NT, typename T>
+int launch_matmul(const CUtensorMap &mp, const CUtensorMap &mq, const MatmulArgs &a, unsigned grid, cudaStream_t s) {
+    using S = MmaShape<NT>;
+    static_assert(S::kSmem <= 227 * 1024 - 1024, "shared memory");
+    const cudaError_t e = cudaFuncSetAttribute((const void *)k_matmul<NT, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+    if (e != cudaSuccess) return cuda_failed(e);
+    return tula::launch(k_matmul<NT, T>, dim3(grid), kMmaThreads, S::kSmem, s, 1, mp, mq, a);
+}
+
+}  // namespace
+
+extern "C" {
+
+int tula_mx_size(int64_t rows, int64_t cols, size_t *code_bytes, size_t *scale_bytes) {
+    if (!code_bytes || !scale_bytes || tiles_of(rows, cols) < 0) return TULA_ERR_ARG;
+    *code_bytes = (size_t)rows * (size_t)up(cols, kTile) * (kTile / 2);
+    *scale_bytes = (size_t)tiles_of(rows, cols) * kScaleTile;
+    return TULA_OK;
+}
+
+int tula_mx_quantize(const void *x, int type, int64_t rows, int64_t cols, int64_t stride, void *codes, void *scales,
+                     void *codes_t, void *scales_t, void *stream) {
+    const long long tiles = tiles_of(rows, cols);
+    if (!good_type(type) || tiles < 0 || stride < cols) return TULA_ERR_ARG;
+    if (tiles == 0) return TULA_OK;
+    if (!codes != !scales || !codes_t != !scales_t || (!codes && !codes_t)) return TULA_ERR_ARG;
+    if (!x || !aligned(x, type_size(type)) || !aligned(codes, 16) || !aligned(scales, 16) || !aligned(codes_t, 16) ||
+        !aligned(scales_t, 16))
+        return TULA_ERR_ARG;
+    QuantArgs a;
+    a.x = x;
+    a.rows = rows;
+    a.cols = cols;
+    a.stride = stride;
+    a.codes = static_cast<unsigned char *>(codes);
+    a.scales = static_cast<unsigned char *>(scales);
+    a.codes_t = static_cast<unsigned char *>(codes_t);
+    a.scales_t = static_cast<unsigned char *>(scales_t);
+    a.tiles_c = (int)up(cols, kTile);
+    a.tiles_r = (int)up(rows, kTile);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (type == TULA_TYPE_F32) return quantize_typed<float>(a, (unsigned)tiles, s);
+    if (type == TULA_TYPE_BF16) return quantize_typed<__nv_bfloat16>(a, (unsigned)tiles, s);
+    return quantize_typed<__half>(a, (unsigned)tiles, s);
+}
+
+int tula_mx_dequantize(const void *codes, const void *scales, int64_t rows, int64_t cols, void *out, int type, void *stream) {
+    const long long tiles = tiles_of(rows, cols);
+    if (!good_type(type) || tiles < 0) return TULA_ERR_ARG;
+    if (tiles == 0) return TULA_OK;
+    if (!codes || !scales || !out || !aligned(codes, 16) || !aligned(scales, 16) || !aligned(out, type_size(type)))
+        return TULA_ERR_ARG;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (type == TULA_TYPE_F32) return dequantize_typed<float>(codes, scales, rows, cols, out, s);
+    if (type == TULA_TYPE_BF16) return dequantize_typed<__nv_bfloat16>(codes, scales, rows, cols, out, s);
+    return dequantize_typed<__half>(codes, scales, rows, cols, out, s);
+}
+
+int tula_mx_matmul(const void *a_codes, const void *a_scales, const void *b_codes, const void *b_scales, int64_t M, int64_t N,
+                   int64_t K, void *out, int out_type, void *stream) {
+    if (!good_type(out_type) || tiles_of(M, K) < 0 || tiles_of(N, K) < 0 || tiles_of(M, N) < 0) return TULA_ERR_ARG;
+    if (M == 0 || N == 0) return TULA_OK;
+    if (!out || !aligned(out, type_size(out_type))) return TULA_ERR_ARG;
+    if (K && (!a_codes || !a_scales || !b_codes || !b_scales || !aligned(a_codes, 16) || !aligned(a_scales, 16) ||
+              !aligned(b_codes, 16) || !aligned(b_scales, 16)))
+        return TULA_ERR_ARG;
+    // The operand with few rows is the instruction's N, so that its 128 rows are not padding.
+    const bool swap = M <= 128;
+    MatmulArgs a;
+    a.p_scales = static_cast<const unsigned char *>(swap ? b_scales : a_scales);
+    a.q_scales = static_cast<const unsigned char *>(swap ? a_scales : b_scales);
+    a.P = swap ? N : M;
+    a.Q = swap ? M : N;
+    a.ld_p = swap ? 1 : N;
+    a.ld_q = swap ? N : 1;
+    a.out = out;
+    a.tiles_k = (int)up(K, kTile);
+    a.p_tiles = (int)up(a.P, kTile);
+    a.q_tiles = (int)up(a.Q, kTile);
+    const int NT = a.Q <= 32 ? 32 : a.Q <= 64 ? 64 : 128;
+    a.grid_q = (int)up(a.Q, NT);
+    const long long grid = (long long)a.p_tiles * a.grid_q;
+    if (grid >= (1LL << 31)) return TULA_ERR_ARG;
+    CUtensorMap mp, mq;
+    std::memset(&mp, 0, sizeof(mp));
+    std::memset(&mq, 0, sizeof(mq));
+    if (K) {
+        const long long pitch = (long long)a.tiles_k * (kTile / 2);
+        if (!codes_map(&mp, swap ? b_codes : a_codes, a.P, pitch, 128) || !codes_map(&mq, swap ? a_codes : b_codes, a.Q, pitch, NT))
+            return cuda_failed(cudaErrorInvalidValue);
+    }
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    auto typed = [&](auto t) {
+        using T = decltype(t);
+        return NT == 32 ? launch_matmul<32, T>(mp, mq, a, (unsigned)grid, s)
+               : NT == 64 ? launch_matmul<64, T>(mp, mq, a, (unsigned)grid, s)
+                          : launch_matmul<128, T>(mp, mq, a, (unsigned)grid, s);
+    };
+    if (out_type == TULA_TYPE_F32) return typed(float());
+    if (out_type == TULA_TYPE_BF16) return typed(__nv_bfloat16());
+    return typed(__half());
+}
+
+int tula_mx_error(void *stream, int *error_out) {
+    if (!error_out) return TULA_ERR_ARG;
+    void *p = nullptr;
+    unsigned v = 0;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    cudaError_t e = cudaGetSymbolAddress(&p, g_mx_error);
+    if (e == cudaSuccess) e = cudaMemcpyAsync(&v, p, sizeof(v), cudaMemcpyDeviceToHost, s);
+    if (e == cudaSuccess) e = cudaMemsetAsync(p, 0, sizeof(v), s);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    if (e != cudaSuccess) return cuda_failed(e);
+    *error_out = (int)v;
+    return TULA_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,741 @@
+// The global gradient norm, clipping and AdamW over a list of tensors, for sm_103a.
+//
+//   k_norm   sum of squares of every gradient; the last CTA to finish turns it into the norm, the
+//            clipping coefficient and the step's scalars
+//   k_clip   g = coef * g
+//   k_adamw  the update of w, m, v and the weights' copies
+//
+// All three stream: a few operations for 2 to 30 bytes, so HBM bounds them, or, for lists of a few
+// hundred thousand elements, the launches.  The plan's device tables (a row per tensor, an entry
+// per tile) make each pass one launch with a few bytes of parameters whatever the number of
+// tensors, and a tile's tensor one load away.
+#include "tula_common.h"
+#include "tula_train.h"
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <cmath>
+#include <cstring>
+#include <memory>
+#include <new>
+#include <vector>
+
+namespace {
+
+constexpr unsigned kFull = 0xffffffffu;
+constexpr int kThreads = 256;
+constexpr int kVec = 8;             // elements a thread moves at once: 16 bytes of a 16-bit type
+constexpr int kSmallTile = 2048;    // elements per tile: one vector a thread
+constexpr int kLargeTile = 8192;    // four
+constexpr int kFan = 64;            // partial sums that one CTA adds up at each level
+constexpr float kNormEps = 1e-6f;
+
+// One tensor.  Pointers are moved back by `lead` elements: element i of the tensor is index
+// lead + i, and a vector of kVec at an index that is a multiple of kVec lies on 16-byte boundaries
+// in every buffer.  lead < 0: there is no such index, the pointers are as given.
+struct Row {
+    unsigned long long g, w, m, v, copy;
+    long long n;
+    int lead;
+    short gtype, ctype;
+    unsigned long long spare;
+};
+static_assert(sizeof(Row) == 64, "a row is half an L2 line");
+struct Tile {
+    int tensor;
+    int index;  // of the tensor's tiles
+};
+
+// The scalars one step's update needs, written by the norm's last CTA.
+struct StepScalars {
+    float mult, step_size, rbc2;
+    int go;
+};
+
+struct Tables {
+    const Row *rows;
+    const Tile *tiles;
+    int n_tiles, tile;  // elements per tile
+    int group, n_groups;  // tiles per CTA of the norm and of clipping
+    double *part;       // [n_groups]
+    double *part2;      // [ceil(n_groups / kFan)]
+    unsigned *tickets;  // [1 + ceil(n_groups / kFan)], zero between launches
+    StepScalars *scal;
+};
+
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_start() {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+// ----------------------------------------------------------------------------
+// Elements
+// ----------------------------------------------------------------------------
+
+__device__ __forceinline__ float2 unpack_bf16(unsigned u) {
+    return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+}
+__device__ __forceinline__ float2 unpack_f16(unsigned u) {
+    __half2 h;
+    memcpy(&h, &u, 4);
+    return __half22float2(h);
+}
+__device__ __forceinline__ unsigned pack_bf16(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    unsigned u;
+    memcpy(&u, &h, 4);
+    return u;
+}
+__device__ __forceinline__ unsigned pack_f16(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    unsigned u;
+    memcpy(&u, &h, 4);
+    return u;
+}
+
+// kVec elements at index i (a multiple of kVec) of a buffer of type `type`.
+template <bool Stream>
+__device__ __forceinline__ void load8(float (&x)[kVec], unsigned long long base, int type, long long i) {
+    if (type == TULA_TYPE_F32) {
+        const float4 *p = reinterpret_cast<const float4 *>(base) + i / 4;
+        const float4 a = Stream ? __ldcs(p) : __ldcg(p), b = Stream ? __ldcs(p + 1) : __ldcg(p + 1);
+        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
+        x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+        return;
+    }
+    const uint4 *p = reinterpret_cast<const uint4 *>(base) + i / 8;
+    const uint4 q = Stream ? __ldcs(p) : __ldcg(p);
+    const unsigned u[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float2 f = type == TULA_TYPE_BF16 ? unpack_bf16(u[k]) : unpack_f16(u[k]);
+        x[2 * k] = f.x;
+        x[2 * k + 1] = f.y;
+    }
+}
+__device__ __forceinline__ void store8(const float (&x)[kVec], unsigned long long base, int type, long long i) {
+    if (type == TULA_TYPE_F32) {
+        float4 *p = reinterpret_cast<float4 *>(base) + i / 4;
+        __stcs(p, make_float4(x[0], x[1], x[2], x[3]));
+        __stcs(p + 1, make_float4(x[4], x[5], x[6], x[7]));
+        return;
+    }
+    unsigned u[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        u[k] = type == TULA_TYPE_BF16 ? pack_bf16(x[2 * k], x[2 * k + 1]) : pack_f16(x[2 * k], x[2 * k + 1]);
+    __stcs(reinterpret_cast<uint4 *>(base) + i / 8, make_uint4(u[0], u[1], u[2], u[3]));
+}
+__device__ __forceinline__ float load1(unsigned long long base, int type, long long i) {
+    if (type == TULA_TYPE_F32) return __ldcg(reinterpret_cast<const float *>(base) + i);
+    const unsigned short u = __ldcg(reinterpret_cast<const unsigned short *>(base) + i);
+    return type == TULA_TYPE_BF16 ? __uint_as_float((unsigned)u << 16) : __half2float(__ushort_as_half(u));
+}
+__device__ __forceinline__ void store1(float x, unsigned long long base, int type, long long i) {
+    if (type == TULA_TYPE_F32)
+        reinterpret_cast<float *>(base)[i] = x;
+    else if (type == TULA_TYPE_BF16)
+        reinterpret_cast<__nv_bfloat16 *>(base)[i] = __float2bfloat16_rn(x);
+    else
+        reinterpret_cast<__half *>(base)[i] = __float2half_rn(x);
+}
+
+// ----------------------------------------------------------------------------
+// The norm
+// ----------------------------------------------------------------------------
+
+// A thread's sum of squares as it stands where every square and sum is safe in fp32; else 0 with
+// the sum in `d`, its elements scaled by an exact power of two first.  A sum in [2^-100, 2^120]
+// is safe: nothing overflowed, and what underflowed is below 2^-40 of it.  Below, every element is
+// under 2^-50 and is squared times 2^100; above (inf and NaN too), times 2^-72.
+template <int N>
+__device__ __forceinline__ float safe_square_sum(const float (&x)[N], double &d) {
+    float c[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < N; ++k) c[k & 3] = __fmaf_rn(x[k], x[k], c[k & 3]);
+    const float s = __fadd_rn(__fadd_rn(c[0], c[1]), __fadd_rn(c[2], c[3]));
+    d = 0.0;
+    if (s >= 0x1p-100f && s <= 0x1p120f) return s;
+    const float f = s < 0x1p-100f ? 0x1p100f : 0x1p-72f;
+    float r = 0.f;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const float y = __fmul_rn(x[k], f);
+        r = __fmaf_rn(y, y, r);
+    }
+    if (r != 0.f) d = (double)r * (s < 0x1p-100f ? 0x1p-200 : 0x1p144);
+    return 0.f;
+}
+
+// A warp's sum, in lane 0.  fp32 lane sums of at most 2^120 add to at most 2^125; the
+// fp64 part is there in the rare warps that have one.
+__device__ __forceinline__ double warp_sum(float s, double d) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) s = __fadd_rn(s, __shfl_xor_sync(kFull, s, o));
+    if (__any_sync(kFull, d != 0.0)) {  // NaN too
+#pragma unroll
+        for (int o = 16; o; o >>= 1) d += __shfl_xor_sync(kFull, d, o);
+        return d + (double)s;
+    }
+    return (double)s;
+}
+
+struct NormArgs {
+    double grad_scale, max_norm;
+    float *record;
+    // the step's scalars (steps NULL: a norm alone)
+    long long *steps;
+    double log_beta1, log_beta2, lr;
+    int skip;
+};
+
+// -(beta^t - 1) to fp32's precision.
+__device__ __forceinline__ float one_minus_pow(double log_beta, long long t) {
+    return -expm1f((float)((double)t * log_beta));
+}
+__device__ __forceinline__ StepScalars step_scalars(float mult, const NormArgs &a, long long t) {
+    StepScalars s;
+    s.mult = mult;
+    s.step_size = __fdiv_rn((float)a.lr, one_minus_pow(a.log_beta1, t));
+    s.rbc2 = __fdiv_rn(1.f, __fsqrt_rn(one_minus_pow(a.log_beta2, t)));
+    s.go = 1;
+    return s;
+}
+
+__device__ void finish_norm(double total, const Tables &tb, const NormArgs &a) {
+    const double norm = sqrt(total) / a.grad_scale;
+    const bool finite = norm <= 1.7e308;
+    double coef = 1.0;
+    if (a.max_norm > 0.0) {
+        coef = a.max_norm / (norm + (double)kNormEps);
+        if (coef > 1.0) coef = 1.0;
+    }
+    if (a.record) {
+        a.record[TULA_RECORD_NORM] = (float)norm;
+        a.record[TULA_RECORD_COEF] = (float)coef;
+        a.record[TULA_RECORD_FINITE] = finite ? 1.f : 0.f;
+    }
+    if (a.steps) {
+        const bool go = finite || !a.skip;
+        const long long t = a.steps[0] + 1;
+        StepScalars s = step_scalars((float)(coef / a.grad_scale), a, t);
+        s.go = go;
+        *tb.scal = s;
+        if (go)
+            a.steps[0] = t;
+        else
+            a.steps[1] += 1;
+    } else {
+        tb.scal->mult = (float)coef;
+    }
+}
+
+// Sum of n doubles, 64 at most, by one warp in a fixed order; in every lane.
+__device__ __forceinline__ double sum64(const double *p, int n) {
+    const int lane = threadIdx.x & 31;
+    double v = lane < n ? __ldcg(p + lane) : 0.0;
+    if (lane + 32 < n) v += __ldcg(p + lane + 32);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
+    return v;
+}
+
+template <int VPT>
+__global__ void __launch_bounds__(kThreads) k_norm(const Tables tb, const NormArgs a) {
+    __shared__ double sums[kThreads / 32];
+    let_next_start();
+    wait_for_previous();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int first = blockIdx.x * tb.group, last = min(first + tb.group, tb.n_tiles);
+    double acc = 0.0;  // lane 0: the warp's
+    for (int t = first; t < last; ++t) {
+        const Tile tile = tb.tiles[t];
+        const Row &row = tb.rows[tile.tensor];
+        const int type = row.gtype, lead = row.lead;
+        const long long n = row.n, i0 = (long long)tile.index * (VPT * kThreads * kVec);
+        const unsigned long long g = row.g;
+        float x[VPT * kVec];
+        if (lead >= 0 && i0 >= lead && i0 + VPT * kThreads * kVec <= lead + n) {
+#pragma unroll
+            for (int j = 0; j < VPT; ++j)
+                load8<false>(*reinterpret_cast<float(*)[kVec]>(&x[j * kVec]), g, type,
+                             i0 + (j * kThreads + tid) * kVec);
+        } else if (lead >= 0) {
+#pragma unroll
+            for (int j = 0; j < VPT; ++j) {
+                const long long i = i0 + (j * kThreads + tid) * kVec;
+                if (i >= lead && i + kVec <= lead + n) {
+                    load8<false>(*reinterpret_cast<float(*)[kVec]>(&x[j * kVec]), g, type, i);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < kVec; ++k)
+                        x[j * kVec + k] = i + k >= lead && i + k < lead + n ? load1(g, type, i + k) : 0.f;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < VPT * kVec; ++k) {
+                const long long i = i0 + k * kThreads + tid;
+                x[k] = i < n ? load1(g, type, i) : 0.f;
+            }
+        }
+        double d;
+        const float s = safe_square_sum(x, d);
+        acc += warp_sum(s, d);
+    }
+    if (lane == 0) sums[warp] = acc;
+    __syncthreads();
+    if (warp != 0) return;
+    // The CTA's partial sum; the last of kFan CTAs adds up theirs, and the last of those all.
+    const int node = blockIdx.x / kFan, n_nodes = (tb.n_groups + kFan - 1) / kFan;
+    const int in_node = min(kFan, tb.n_groups - node * kFan);
+    bool last_here = false;
+    if (lane == 0) {
+        double s = 0.0;
+        for (int k = 0; k < kThreads / 32; ++k) s += sums[k];
+        __stcg(tb.part + blockIdx.x, s);
+        __threadfence();
+        last_here = atomicAdd(tb.tickets + 1 + node, 1u) == (unsigned)in_node - 1;
+    }
+    if (!__shfl_sync(kFull, last_here, 0)) return;
+    __threadfence();
+    double s = sum64(tb.part + (size_t)node * kFan, in_node);
+    if (lane == 0) {
+        tb.tickets[1 + node] = 0;
+        __stcg(tb.part2 + node, s);
+        __threadfence();
+        last_here = atomicAdd(tb.tickets, 1u) == (unsigned)n_nodes - 1;
+    }
+    if (!__shfl_sync(kFull, last_here, 0)) return;
+    __threadfence();
+    double total = 0.0;
+    for (int k = 0; k < n_nodes; k += kFan) total += sum64(tb.part2 + k, min(kFan, n_nodes - k));
+    if (lane == 0) {
+        tb.tickets[0] = 0;
+        finish_norm(total, tb, a);
+    }
+}
+
+// ----------------------------------------------------------------------------
+// Clipping
+// ----------------------------------------------------------------------------
+
+__device__ __forceinline__ void scale_at(unsigned long long g, int type, long long i, float c) {
+    store1(__fmul_rn(load1(g, type, i), c), g, type, i);
+}
+
+// Tiles from the last to the first: what the norm read last is still in L2.
+template <int VPT>
+__global__ void __launch_bounds__(kThreads) k_clip(const Tables tb) {
+    let_next_start();
+    wait_for_previous();
+    const float c = tb.scal->mult;
+    if (c == 1.f) return;
+    const int tid = threadIdx.x;
+    const int first = (tb.n_groups - 1 - (int)blockIdx.x) * tb.group;
+    for (int t = min(first + tb.group, tb.n_tiles) - 1; t >= first; --t) {
+        const Tile tile = tb.tiles[t];
+        const Row &row = tb.rows[tile.tensor];
+        const int type = row.gtype, lead = row.lead;
+        const long long n = row.n, i0 = (long long)tile.index * (VPT * kThreads * kVec);
+        const unsigned long long g = row.g;
+        if (lead >= 0 && i0 >= lead && i0 + VPT * kThreads * kVec <= lead + n) {
+            float x[VPT][kVec];
+#pragma unroll
+            for (int j = 0; j < VPT; ++j) load8<true>(x[j], g, type, i0 + (j * kThreads + tid) * kVec);
+#pragma unroll
+            for (int j = 0; j < VPT; ++j) {
+#pragma unroll
+                for (int k = 0; k < kVec; ++k) x[j][k] = __fmul_rn(x[j][k], c);
+                store8(x[j], g, type, i0 + (j * kThreads + tid) * kVec);
+            }
+        } else if (lead >= 0) {
+            for (int j = 0; j < VPT; ++j) {
+                const long long i = i0 + (j * kThreads + tid) * kVec;
+                if (i >= lead && i + kVec <= lead + n) {
+                    float x[kVec];
+                    load8<true>(x, g, type, i);
+#pragma unroll
+                    for (int k = 0; k < kVec; ++k) x[k] = __fmul_rn(x[k], c);
+                    store8(x, g, type, i);
+                } else {
+                    for (int k = 0; k < kVec; ++k)
+                        if (i + k >= lead && i + k < lead + n) scale_at(g, type, i + k, c);
+                }
+            }
+        } else {
+#pragma unroll 4
+            for (int k = 0; k < VPT * kVec; ++k) {
+                const long long i = i0 + k * kThreads + tid;
+                if (i < n) scale_at(g, type, i, c);
+            }
+        }
+    }
+}
+
+// ----------------------------------------------------------------------------
+// AdamW
+// ----------------------------------------------------------------------------
+
+struct Adam {
+    float beta1, beta2, ob1, ob2, decay, eps;  // ob: 1 - beta; decay: 1 - lr * weight_decay
+};
+
+__device__ __forceinline__ void adamw1(float g, float &w, float &m, float &v, const Adam &h,
+                                       const StepScalars &s) {
+    const float d = __fmul_rn(g, s.mult);
+    m = __fmaf_rn(h.beta1, m, __fmul_rn(h.ob1, d));
+    v = __fmaf_rn(h.beta2, v, __fmul_rn(__fmul_rn(h.ob2, d), d));
+    const float den = __fmaf_rn(__fsqrt_rn(v), s.rbc2, h.eps);
+    w = __fmaf_rn(-s.step_size, __fdiv_rn(m, den), __fmul_rn(w, h.decay));
+}
+
+__device__ __forceinline__ void adamw_vec(const Row &r, int gtype, int ctype, bool copy, long long i,
+                                          const Adam &h, const StepScalars &s) {
+    float g[kVec], w[kVec], m[kVec], v[kVec];
+    load8<true>(w, r.w, TULA_TYPE_F32, i);
+    load8<true>(m, r.m, TULA_TYPE_F32, i);
+    load8<true>(v, r.v, TULA_TYPE_F32, i);
+    load8<true>(g, r.g, gtype, i);
+#pragma unroll
+    for (int k = 0; k < kVec; ++k) adamw1(g[k], w[k], m[k], v[k], h, s);
+    store8(w, r.w, TULA_TYPE_F32, i);
+    store8(m, r.m, TULA_TYPE_F32, i);
+    store8(v, r.v, TULA_TYPE_F32, i);
+    if (copy) store8(w, r.copy, ctype, i);
+}
+__device__ __forceinline__ void adamw_one(const Row &r, bool copy, long long i, const Adam &h,
+                                          const StepScalars &s) {
+    float w = load1(r.w, TULA_TYPE_F32, i), m = load1(r.m, TULA_TYPE_F32, i);
+    float v = load1(r.v, TULA_TYPE_F32, i);
+    adamw1(load1(r.g, r.gtype, i), w, m, v, h, s);
+    store1(w, r.w, TULA_TYPE_F32, i);
+    store1(m, r.m, TULA_TYPE_F32, i);
+    store1(v, r.v, TULA_TYPE_F32, i);
+    if (copy) store1(w, r.copy, r.ctype, i);
+}
+
+// Normed: the norm's last CTA has left the step's scalars.  Else each CTA takes them from the step
+// count, which the last CTA to have read it moves on.
+template <int VPT, bool Normed>
+__global__ void __launch_bounds__(kThreads) k_adamw(const Tables tb, const Adam h, const NormArgs a,
+                                                    float mult) {
+    let_next_start();
+    wait_for_previous();
+    const int tid = threadIdx.x;
+    StepScalars s;
+    if (Normed) {
+        s = *tb.scal;
+        if (!s.go) return;
+    } else {
+        __shared__ StepScalars shared;
+        if (tid == 0) {
+            const long long t = *(volatile long long *)a.steps + 1;
+            shared = step_scalars(mult, a, t);
+            __threadfence();
+            if (atomicAdd(tb.tickets, 1u) == gridDim.x - 1) {
+                tb.tickets[0] = 0;
+                a.steps[0] = t;
+            }
+        }
+        __syncthreads();
+        s = shared;
+    }
+    const Tile tile = tb.tiles[tb.n_tiles - 1 - (int)blockIdx.x];
+    const Row row = tb.rows[tile.tensor];
+    const bool copy = row.copy != 0;
+    const long long n = row.n, i0 = (long long)tile.index * (VPT * kThreads * kVec);
+    const int lead = row.lead;
+    if (lead >= 0) {
+#pragma unroll 1
+        for (int j = 0; j < VPT; ++j) {
+            const long long i = i0 + (j * kThreads + tid) * kVec;
+            if (i >= lead && i + kVec <= lead + n) {
+                adamw_vec(row, row.gtype, row.ctype, copy, i, h, s);
+            } else {
+                for (int k = 0; k < kVec; ++k)
+                    if (i + k >= lead && i + k < lead + n) adamw_one(row, copy, i + k, h, s);
+            }
+        }
+    } else {
+#pragma unroll 4
+        for (int k = 0; k < VPT * kVec; ++k) {
+            const long long i = i0 + k * kThreads + tid;
+            if (i < n) adamw_one(row, copy, i, h, s);
+        }
+    }
+}
+
+// A list without elements: the norm is 0, the step counts.
+__global__ void k_empty(const Tables tb, const NormArgs a) {
+    wait_for_previous();
+    finish_norm(0.0, tb, a);
+}
+
+// ----------------------------------------------------------------------------
+// Host side
+// ----------------------------------------------------------------------------
+
+struct Layout {
+    size_t scal, tickets, part2, part, rows, tiles, total;
+    int tile, group, n_groups;
+};
+
+// Tiles of the whole list at `tile` elements each, at any alignment.
+bool count_tiles(const int64_t *numels, int n, int tile, long long *out) {
+    long long t = 0;
+    for (int i = 0; i < n; ++i) {
+        if (numels[i] < 0) return false;
+        if (numels[i]) t += numels[i] / tile + (numels[i] % tile + kVec - 1 + tile - 1) / tile;
+        if (t >= (1LL << 31) - 1) return false;
+    }
+    *out = t;
+    return true;
+}
+
+bool layout(const int64_t *numels, int n, Layout *L) {
+    if (!numels || n < 1) return false;
+    long long t;
+    // Up to eight CTAs an SM small tiles spread a list over more SMs; beyond, large ones have
+    // more bytes in flight and fewer partial sums.
+    L->tile = kSmallTile;
+    if (!count_tiles(numels, n, kSmallTile, &t) || t > 8 * 152) {
+        L->tile = kLargeTile;
+        if (!count_tiles(numels, n, kLargeTile, &t)) return false;
+    }
+    // The norm's CTAs take one tile up to 16 CTAs an SM, then up to four.
+    const long long per = t / (16 * 152);
+    L->group = per < 1 ? 1 : per > 4 ? 4 : (int)per;
+    L->n_groups = (int)((t + L->group - 1) / L->group);
+    const size_t nodes = ((size_t)L->n_groups + kFan - 1) / kFan;
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        const size_t o = off;
+        off = (off + bytes + 255) & ~size_t(255);
+        return o;
+    };
+    L->scal = take(sizeof(StepScalars));
+    L->tickets = take(4 * (1 + nodes));
+    L->part2 = take(8 * nodes);
+    L->part = take(8 * (size_t)L->n_groups);
+    L->rows = take(sizeof(Row) * (size_t)n);
+    L->tiles = take(sizeof(Tile) * (size_t)t);
+    L->total = off;
+    return true;
+}
+
+inline int size_of(int type) { return type == TULA_TYPE_F32 ? 4 : 2; }
+
+int cuda_failed(cudaError_t e) {
+    tula::note_cuda_error((int)e);
+    return TULA_ERR_CUDA;
+}
+
+}  // namespace
+
+struct tula_train_plan {
+    int dev;
+    bool weights;
+    Tables tb;
+};
+
+namespace {
+
+// The index at which the tensor starts so that vectors lie on 16-byte boundaries in all of its
+// buffers, or -1.
+int lead_of(const unsigned long long *ptrs, const int *sizes, int count) {
+    for (int lead = 0; lead < kVec; ++lead) {
+        bool ok = true;
+        for (int k = 0; k < count; ++k) ok = ok && ((ptrs[k] - (unsigned long long)(lead * sizes[k])) & 15) == 0;
+        if (ok) return lead;
+    }
+    return -1;
+}
+
+int check_plan(tula_train_plan *plan) {
+    if (!plan) return TULA_ERR_ARG;
+    int dev = 0;
+    const cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return cuda_failed(e);
+    return dev == plan->dev ? TULA_OK : TULA_ERR_ARG;
+}
+
+int run_norm(const Tables &tb, const NormArgs &a, cudaStream_t s) {
+    if (tb.n_tiles == 0) return tula::launch(k_empty, dim3(1), 1, 0, s, 1, tb, a);
+    return tula::launch(tb.tile == kSmallTile ? k_norm<1> : k_norm<4>, dim3((unsigned)tb.n_groups),
+                        kThreads, 0, s, 1, tb, a);
+}
+
+}  // namespace
+
+extern "C" {
+
+int tula_train_workspace_size(const int64_t *numels, int n_tensors, size_t *bytes) {
+    Layout L;
+    if (!bytes || !layout(numels, n_tensors, &L)) return TULA_ERR_ARG;
+    *bytes = L.total;
+    return TULA_OK;
+}
+
+int tula_train_plan_create(const tula_train_tensors *t, void *workspace, size_t workspace_bytes,
+                           void *stream, tula_train_plan **plan_out) {
+    if (!plan_out) return TULA_ERR_ARG;
+    *plan_out = nullptr;
+    Layout L;
+    if (!t || !t->grad_ptrs || !layout(t->numels, t->n_tensors, &L)) return TULA_ERR_ARG;
+    const bool weights = t->param_ptrs != nullptr;
+    if ((t->exp_avg_ptrs != nullptr) != weights || (t->exp_avg_sq_ptrs != nullptr) != weights ||
+        (t->copy_ptrs && !weights))
+        return TULA_ERR_ARG;
+    const int n = t->n_tensors;
+    std::unique_ptr<tula_train_plan> plan(new (std::nothrow) tula_train_plan());
+    std::vector<Row> rows;
+    std::vector<Tile> tiles;
+    if (!plan) return TULA_ERR_NO_MEMORY;
+    try {
+        rows.resize((size_t)n);
+        tiles.reserve((L.total - L.tiles) / sizeof(Tile));
+        for (int i = 0; i < n; ++i) {
+            Row &r = rows[(size_t)i];
+            std::memset(&r, 0, sizeof(r));
+            r.n = t->numels[i];
+            r.gtype = (short)(t->grad_types ? t->grad_types[i] : TULA_TYPE_F32);
+            r.ctype = (short)(t->copy_types ? t->copy_types[i] : TULA_TYPE_BF16);
+            if (r.gtype < TULA_TYPE_F32 || r.gtype > TULA_TYPE_F16) return TULA_ERR_ARG;
+            if (t->copy_ptrs && r.ctype != TULA_TYPE_BF16 && r.ctype != TULA_TYPE_F16) return TULA_ERR_ARG;
+            if (r.n == 0) continue;
+            unsigned long long *dst[5] = {&r.g, &r.w, &r.m, &r.v, &r.copy};
+            unsigned long long p[5];
+            int size[5], count = 0;
+            auto add = [&](const void *q, int bytes) {
+                p[count] = reinterpret_cast<unsigned long long>(q);
+                size[count++] = bytes;
+            };
+            add(t->grad_ptrs[i], size_of(r.gtype));
+            if (weights) {
+                add(t->param_ptrs[i], 4);
+                add(t->exp_avg_ptrs[i], 4);
+                add(t->exp_avg_sq_ptrs[i], 4);
+                if (t->copy_ptrs) add(t->copy_ptrs[i], 2);
+            }
+            for (int k = 0; k < count; ++k)
+                if (!p[k] || p[k] % (unsigned)size[k]) return TULA_ERR_ARG;
+            r.lead = lead_of(p, size, count);
+            const int lead = r.lead < 0 ? 0 : r.lead;
+            for (int k = 0; k < count; ++k) *dst[k] = p[k] - (unsigned long long)(lead * size[k]);
+            const long long nt = (r.n + lead + L.tile - 1) / L.tile;
+            for (long long k = 0; k < nt; ++k) tiles.push_back({i, (int)k});
+        }
+    } catch (const std::bad_alloc &) {
+        return TULA_ERR_NO_MEMORY;
+    }
+    if (!workspace || workspace_bytes < L.total || (reinterpret_cast<uintptr_t>(workspace) & 255u))
+        return TULA_ERR_WORKSPACE;
+    cudaError_t e = cudaGetDevice(&plan->dev);
+    if (e != cudaSuccess) return cuda_failed(e);
+    char *ws = static_cast<char *>(workspace);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    Tables &tb = plan->tb;
+    tb.rows = reinterpret_cast<const Row *>(ws + L.rows);
+    tb.tiles = reinterpret_cast<const Tile *>(ws + L.tiles);
+    tb.n_tiles = (int)tiles.size();
+    tb.tile = L.tile;
+    tb.group = L.group;
+    tb.n_groups = (tb.n_tiles + L.group - 1) / L.group;
+    tb.part = reinterpret_cast<double *>(ws + L.part);
+    tb.part2 = reinterpret_cast<double *>(ws + L.part2);
+    tb.tickets = reinterpret_cast<unsigned *>(ws + L.tickets);
+    tb.scal = reinterpret_cast<StepScalars *>(ws + L.scal);
+    plan->weights = weights;
+    e = cudaMemsetAsync(ws, 0, L.part2, s);
+    if (e == cudaSuccess)
+        e = cudaMemcpyAsync(ws + L.rows, rows.data(), sizeof(Row) * (size_t)n, cudaMemcpyHostToDevice, s);
+    if (e == cudaSuccess && !tiles.empty())
+        e = cudaMemcpyAsync(ws + L.tiles, tiles.data(), sizeof(Tile) * tiles.size(), cudaMemcpyHostToDevice, s);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    if (e != cudaSuccess) return cuda_failed(e);
+    *plan_out = plan.release();
+    return TULA_OK;
+}
+
+int tula_train_plan_destroy(tula_train_plan *plan) {
+    delete plan;
+    return TULA_OK;
+}
+
+int tula_grad_norm(tula_train_plan *plan, float grad_scale, float max_norm, float *record, void *stream) {
+    if (!plan || !record || !(grad_scale > 0.f) || !(max_norm >= 0.f)) return TULA_ERR_ARG;
+    const int rc = check_plan(plan);
+    if (rc) return rc;
+    NormArgs a = {};
+    a.grad_scale = grad_scale;
+    a.max_norm = max_norm;
+    a.record = record;
+    return run_norm(plan->tb, a, static_cast<cudaStream_t>(stream));
+}
+
+int tula_grad_clip(tula_train_plan *plan, float max_norm, float *record, void *stream) {
+    if (!(max_norm > 0.f)) return TULA_ERR_ARG;
+    const int rc = tula_grad_norm(plan, 1.f, max_norm, record, stream);
+    if (rc || plan->tb.n_tiles == 0) return rc;
+    const Tables &tb = plan->tb;
+    return tula::launch(tb.tile == kSmallTile ? k_clip<1> : k_clip<4>, dim3((unsigned)tb.n_groups), kThreads,
+                        0, static_cast<cudaStream_t>(stream), 1, tb);
+}
+
+void tula_adamw_default_hparams(tula_adamw_hparams *hp) {
+    if (!hp) return;
+    std::memset(hp, 0, sizeof(*hp));
+    hp->lr = 1e-3;
+    hp->beta1 = 0.9;
+    hp->beta2 = 0.999;
+    hp->eps = 1e-8;
+    hp->weight_decay = 0.01;
+    hp->grad_scale = 1.0;
+}
+
+int tula_adamw_step(tula_train_plan *plan, const tula_adamw_hparams *hp, void *stream) {
+    if (!plan || !hp || !plan->weights || !hp->steps) return TULA_ERR_ARG;
+    auto at_least_0 = [](double v) { return v >= 0.0 && v <= 1.7e308; };
+    if (!at_least_0(hp->lr) || !at_least_0(hp->eps) || !at_least_0(hp->weight_decay) ||
+        !(hp->max_norm >= 0.0) || !(hp->grad_scale > 0.0) || !(hp->grad_scale <= 1.7e308) ||
+        !(hp->beta1 >= 0.0 && hp->beta1 < 1.0) || !(hp->beta2 >= 0.0 && hp->beta2 < 1.0) ||
+        (hp->skip_nonfinite != 0 && hp->skip_nonfinite != 1))
+        return TULA_ERR_ARG;
+    const bool normed = hp->max_norm > 0.0 || hp->skip_nonfinite;
+    if (normed && !hp->record) return TULA_ERR_ARG;
+    if ((reinterpret_cast<uintptr_t>(hp->steps) & 7u) || (reinterpret_cast<uintptr_t>(hp->record) & 3u))
+        return TULA_ERR_ARG;
+    int rc = check_plan(plan);
+    if (rc) return rc;
+    const Tables &tb = plan->tb;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    NormArgs a = {};
+    a.grad_scale = hp->grad_scale;
+    a.max_norm = hp->max_norm;
+    a.record = normed ? hp->record : nullptr;
+    a.steps = reinterpret_cast<long long *>(hp->steps);
+    a.log_beta1 = std::log(hp->beta1);
+    a.log_beta2 = std::log(hp->beta2);
+    a.lr = hp->lr;
+    a.skip = hp->skip_nonfinite;
+    Adam h;
+    h.beta1 = (float)hp->beta1;
+    h.beta2 = (float)hp->beta2;
+    h.ob1 = (float)(1.0 - hp->beta1);
+    h.ob2 = (float)(1.0 - hp->beta2);
+    h.decay = (float)(1.0 - hp->lr * hp->weight_decay);
+    h.eps = (float)hp->eps;
+    const float mult = (float)(1.0 / hp->grad_scale);
+    if (normed || tb.n_tiles == 0) {
+        rc = run_norm(tb, a, s);
+        if (rc || tb.n_tiles == 0) return rc;
+    }
+    const bool small = tb.tile == kSmallTile;
+    return tula::launch(normed ? (small ? k_adamw<1, true> : k_adamw<4, true>)
+                               : (small ? k_adamw<1, false> : k_adamw<4, false>),
+                        dim3((unsigned)tb.n_tiles), kThreads, 0, s, 1, tb, h, a, mult);
+}
+
+}  // extern "C"

@@ -1,0 +1,176 @@
+"""Binding of the MXFP4 matrices of libtula_ags (include/tula_train.h).
+
+    q = quantize(x)                       # blocks of 32 along the rows of x
+    q, qt = quantize(x, cols=True)        # and x's transpose, blocks along x's columns
+    x4 = dequantize(q, torch.bfloat16)
+    y = matmul(a, b)                      # A B^T
+    y = linear(x, w)                      # x w^T, differentiable: both gradients are MXFP4 products
+
+Everything runs in the CUDA library, asynchronously on the current stream.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import NamedTuple
+
+import torch
+
+from .optim import TYPES
+from .tula_ags import _check, _stream_ptr, c_int, c_size_t, c_void_p, lib
+
+_i64 = ctypes.c_int64
+_typed = None
+
+
+def _lib():
+    global _typed
+    if _typed is None:
+        L = lib()
+        L.tula_mx_size.argtypes = [_i64, _i64, ctypes.POINTER(c_size_t), ctypes.POINTER(c_size_t)]
+        L.tula_mx_quantize.argtypes = [c_void_p, c_int, _i64, _i64, _i64] + [c_void_p] * 5
+        L.tula_mx_dequantize.argtypes = [c_void_p, c_void_p, _i64, _i64, c_void_p, c_int, c_void_p]
+        L.tula_mx_matmul.argtypes = [c_void_p] * 4 + [_i64] * 3 + [c_void_p, c_int, c_void_p]
+        L.tula_mx_error.argtypes = [c_void_p, ctypes.POINTER(c_int)]
+        _typed = L
+    return _typed
+
+
+class MXMatrix(NamedTuple):
+    """A rows x cols matrix in MXFP4: codes uint8 [rows, P / 2] and scales uint8
+    [ceil(rows / 128), P / 128, 32, 4, 4], P = cols rounded up to a multiple of 128."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    rows: int
+    cols: int
+
+
+def tula_mx_size(rows: int, cols: int) -> tuple[int, int]:
+    """Bytes of the codes and of the scales."""
+    a, b = c_size_t(0), c_size_t(0)
+    _check(_lib().tula_mx_size(rows, cols, ctypes.byref(a), ctypes.byref(b)), "tula_mx_size")
+    return a.value, b.value
+
+
+def empty(rows: int, cols: int, device) -> MXMatrix:
+    """An MXMatrix to quantise into."""
+    tiles = -(-cols // 128)
+    return MXMatrix(torch.empty(rows, tiles * 64, dtype=torch.uint8, device=device),
+                    torch.empty(-(-rows // 128), tiles, 32, 4, 4, dtype=torch.uint8, device=device),
+                    rows, cols)
+
+
+def _on_gpu(*tensors):
+    for t in tensors:
+        if t.device.type != "cuda" or t.device != tensors[0].device:
+            raise TypeError(f"tensors on one GPU are wanted, got {[str(t.device) for t in tensors]}")
+
+
+def _good(q: MXMatrix, what: str):
+    tiles, r = -(-q.cols // 128), -(-q.rows // 128)
+    if (q.codes.dtype != torch.uint8 or q.scales.dtype != torch.uint8 or not q.codes.is_contiguous()
+            or not q.scales.is_contiguous() or q.codes.numel() != q.rows * tiles * 64
+            or q.scales.numel() != r * tiles * 512):
+        raise ValueError(f"{what}: not the codes and scales of a {q.rows} x {q.cols} matrix")
+
+
+def _type(dtype, what):
+    if dtype not in TYPES:
+        raise TypeError(f"{what}: float32, bfloat16 or float16 is wanted, got {dtype}")
+    return TYPES[dtype]
+
+
+def quantize(x: torch.Tensor, rows: bool = True, cols: bool = False, stream=None):
+    """x (2-D; its rows may lie apart) as an MXMatrix (rows), its transpose as one (cols), or both
+    as a pair from one reading of x."""
+    _on_gpu(x)
+    kind = _type(x.dtype, "quantize")
+    if x.dim() != 2 or not (rows or cols):
+        raise ValueError("quantize: a matrix, and at least one of rows and cols, are wanted")
+    r, c = x.shape
+    # a row of one element, or the only row, may have any stride
+    if c > 1 and x.stride(1) != 1 or r > 1 and x.stride(0) < c:
+        x = x.contiguous()
+    stride = x.stride(0) if r > 1 else c
+    q = empty(r, c, x.device) if rows else None
+    t = empty(c, r, x.device) if cols else None
+    with torch.cuda.device(x.device):
+        _check(_lib().tula_mx_quantize(
+            x.data_ptr(), kind, r, c, stride, q.codes.data_ptr() if rows else None,
+            q.scales.data_ptr() if rows else None, t.codes.data_ptr() if cols else None,
+            t.scales.data_ptr() if cols else None, _stream_ptr(stream)), "tula_mx_quantize")
+    return (q, t) if rows and cols else q if rows else t
+
+
+def dequantize(q: MXMatrix, dtype=torch.bfloat16, stream=None) -> torch.Tensor:
+    """The values that q stands for."""
+    _good(q, "dequantize")
+    _on_gpu(q.codes, q.scales)
+    kind = _type(dtype, "dequantize")
+    out = torch.empty(q.rows, q.cols, dtype=dtype, device=q.codes.device)
+    with torch.cuda.device(out.device):
+        _check(_lib().tula_mx_dequantize(q.codes.data_ptr(), q.scales.data_ptr(), q.rows, q.cols,
+                                         out.data_ptr(), kind, _stream_ptr(stream)), "tula_mx_dequantize")
+    return out
+
+
+def matmul(a: MXMatrix, b: MXMatrix, dtype=torch.bfloat16, stream=None) -> torch.Tensor:
+    """A B^T for a of M x K and b of N x K, as an M x N tensor of dtype."""
+    _good(a, "matmul")
+    _good(b, "matmul")
+    _on_gpu(a.codes, a.scales, b.codes, b.scales)
+    if a.cols != b.cols:
+        raise ValueError(f"matmul: {a.cols} columns and {b.cols}")
+    kind = _type(dtype, "matmul")
+    out = torch.empty(a.rows, b.rows, dtype=dtype, device=a.codes.device)
+    with torch.cuda.device(out.device):
+        _check(_lib().tula_mx_matmul(a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(),
+                                     b.scales.data_ptr(), a.rows, b.rows, a.cols, out.data_ptr(), kind,
+                                     _stream_ptr(stream)), "tula_mx_matmul")
+    return out
+
+
+def tula_mx_error(stream=None) -> int:
+    """Reads and clears the products' error word after the work on `stream` (synchronous): 0 =
+    every wait inside the kernels completed."""
+    out = c_int(0)
+    _check(_lib().tula_mx_error(_stream_ptr(stream), ctypes.byref(out)), "tula_mx_error")
+    return out.value
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w):
+        need_x, need_w = ctx.needs_input_grad
+        # what the backward pass multiplies by is kept in 4 bits: x^T for dw, w^T for dx
+        qx = quantize(x, cols=need_w)
+        qw = quantize(w, cols=need_x)
+        qx, xt = qx if need_w else (qx, None)
+        qw, wt = qw if need_x else (qw, None)
+        ctx.types = (x.dtype, w.dtype)
+        ctx.sides = (xt, wt)
+        return matmul(qx, qw, x.dtype)
+
+    @staticmethod
+    def backward(ctx, dy):
+        xt, wt = ctx.sides
+        need_x, need_w = ctx.needs_input_grad
+        dx = dw = None
+        q = quantize(dy, rows=need_x, cols=need_w)
+        rows, cols = q if need_x and need_w else (q, q)
+        if need_x:
+            dx = matmul(rows, wt, ctx.types[0])   # dy [M, N] (w^T [K, N])^T
+        if need_w:
+            dw = matmul(cols, xt, ctx.types[1])   # dy^T [N, M] (x^T [K, M])^T
+        return dx, dw
+
+
+def linear(x: torch.Tensor, w: torch.Tensor) -> torch.Tensor:
+    """y = x w^T with x [..., K] and w [N, K] quantised to MXFP4 along K, in x's type.  Its
+    gradients are products of MXFP4 matrices too, quantised along the dimension that each sums
+    over: dx = dy w in x's type (blocks along N), dw = dy^T x in w's type (blocks along the rows
+    of x)."""
+    if x.shape[-1] != w.shape[-1] or w.dim() != 2:
+        raise ValueError(f"linear: x {tuple(x.shape)} and w {tuple(w.shape)}")
+    if x.dim() == 2:
+        return _Linear.apply(x, w)
+    return _Linear.apply(x.reshape(-1, x.shape[-1]), w).view(*x.shape[:-1], w.shape[0])
