@@ -367,6 +367,16 @@ __device__ __forceinline__ uint32_t with_scale_id(uint32_t desc, uint32_t id) {
     return desc | id << 4 | id << 29;
 }
 
+// True in one lane of a converged warp.  The tensor core's and the copies' instructions take their
+// operands from uniform registers: issued from warps that run whole, with one lane elected for the
+// instruction alone, they cost a few cycles each; from a branch of lane 0 a stage's ten took some
+// 900 cycles, and a product of 8192^3 300 us.
+__device__ __forceinline__ bool elect_one() {
+    unsigned p;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
+    return p != 0;
+}
+
 __device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
     asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
@@ -403,27 +413,46 @@ struct MatmulArgs {
     const unsigned char *p_scales, *q_scales;
     void *out;
     long long P, Q;       // rows of each operand
-    long long ld_p, ld_q; // elements of out from one row of P (Q) to the next
+    long long ld;         // elements of out from row to row
     int tiles_k;          // of 128 columns
-    int p_tiles, q_tiles; // tiles of each operand's scales along its rows
-    int grid_q;           // CTAs along Q
+    int q_tiles;          // tiles of Q's scales along its rows
+    int grid_q;           // tiles of the product along Q
+    int split;            // CTAs of a cluster that share a tile's columns
 };
+
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t in_cta(uint32_t addr, unsigned rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float load_cluster(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
 
 template <int NT>
 struct MmaShape {
-    static constexpr int kScaleTilesQ = NT > 128 ? NT / 128 : 1;
     static constexpr int kP = 128 * 128, kQ = NT * 128;                     // bytes of codes a stage
-    static constexpr int kSP = 2 * kScaleTile, kSQ = 2 * kScaleTilesQ * kScaleTile;
+    static constexpr int kSP = 2 * kScaleTile, kSQ = 2 * kScaleTile;
     static constexpr int kStage = kP + kQ + kSP + kSQ;
-    static constexpr int kStages = NT >= 256 ? 4 : NT >= 128 ? 3 : 5;
+    static constexpr int kStages = NT >= 128 ? 3 : NT >= 64 ? 4 : 5;        // two CTAs an SM
+    static constexpr int kPitch = 129;                                      // floats of a column of partial sums
     static constexpr int kSmem = kStages * kStage + 1024;                   // aligned to 1024 at run time
-    static constexpr int kScaleP = NT < 32 ? 32 : NT;                       // tensor memory columns
+    static constexpr int kScaleP = NT;                                      // tensor memory columns
     static constexpr int kScaleQ = kScaleP + 8;
-    static constexpr int kUsed = kScaleQ + 8 * kScaleTilesQ;
-    static constexpr int kCols = kUsed <= 64 ? 64 : kUsed <= 128 ? 128 : kUsed <= 256 ? 256 : 512;
+    static constexpr int kUsed = kScaleQ + 8;
+    static constexpr int kCols = kUsed <= 64 ? 64 : kUsed <= 128 ? 128 : 256;
+    static_assert(NT * kPitch * 4 <= kStages * kStage && 2 * kSmem <= 226 * 1024, "shared memory");
 };
 
-template <int NT, typename T>
+// One tile of 128 rows of P by NT of Q a cluster; its CTAs share the columns, and add up their
+// partial sums through distributed shared memory in the order of their ranks.  Swap: out is
+// [Q][P], its rows run along P.
+template <int NT, bool Swap, typename T>
 __global__ void __launch_bounds__(kMmaThreads) k_matmul(const __grid_constant__ CUtensorMap map_p,
                                                         const __grid_constant__ CUtensorMap map_q, const MatmulArgs a) {
     using S = MmaShape<NT>;
@@ -431,11 +460,13 @@ __global__ void __launch_bounds__(kMmaThreads) k_matmul(const __grid_constant__ 
     __shared__ __align__(8) unsigned long long bars[2 * S::kStages + 1];
     __shared__ uint32_t tmem_at;
     __shared__ volatile int dead;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(kFull, tid >> 5, 0);
     const uint32_t stages = (smem_addr(tile) + 1023) & ~1023u;
     const uint32_t full = smem_addr(bars), empty = full + 8 * S::kStages, done = empty + 8 * S::kStages;
-    const int tp = blockIdx.x / a.grid_q, tq = blockIdx.x % a.grid_q;
-    const int stages_k = (a.tiles_k + 1) / 2;
+    const int rank = blockIdx.x % a.split, t = blockIdx.x / a.split;
+    const int tp = t / a.grid_q, tq = t % a.grid_q;
+    const int all_k = (a.tiles_k + 1) / 2, per = (all_k + a.split - 1) / a.split;
+    const int k_begin = min(rank * per, all_k), n_k = min(per, all_k - k_begin);  // stages of this CTA
     if (tid == 0) {
         for (int s = 0; s < S::kStages; ++s) {
             mbar_init(full + 8 * s, 1);
@@ -449,94 +480,105 @@ __global__ void __launch_bounds__(kMmaThreads) k_matmul(const __grid_constant__ 
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    const uint32_t tmem = tmem_at;
+    const uint32_t tmem = __shfl_sync(kFull, tmem_at, 0);
     let_next_start();
     wait_for_previous();
 
     if (warp == 0) {
-        if (lane == 0) {
-            int issued = 0;
-            for (int k = 0; k < stages_k; ++k) {
-                const int s = k % S::kStages;
-                if (k >= S::kStages && !mbar_wait(empty + 8 * s, (k / S::kStages - 1) & 1, &dead)) break;
-                const uint32_t at = stages + s * S::kStage, bar = full + 8 * s;
-                const int tiles = min(2, a.tiles_k - 2 * k);  // scale tiles along the columns
-                mbar_expect(bar, S::kP + S::kQ + (1 + S::kScaleTilesQ) * tiles * kScaleTile);
+        int issued = 0;
+        bool ok = true;
+        for (int i = 0; i < n_k; ++i) {
+            const int s = i % S::kStages, k = k_begin + i;
+            if (i >= S::kStages) ok = __all_sync(kFull, mbar_wait(empty + 8 * s, (i / S::kStages - 1) & 1, &dead));
+            if (!ok) break;
+            const uint32_t at = stages + s * S::kStage, bar = full + 8 * s;
+            const int tiles = min(2, a.tiles_k - 2 * k);  // scale tiles along the columns
+            if (elect_one()) {
+                mbar_expect(bar, S::kP + S::kQ + 2 * tiles * kScaleTile);
                 tma_load_2d(at, &map_p, k * (kStageK / 2), tp * 128, bar);
                 tma_load_2d(at + S::kP, &map_q, k * (kStageK / 2), tq * NT, bar);
                 bulk_load(at + S::kP + S::kQ, a.p_scales + ((size_t)tp * a.tiles_k + 2 * k) * kScaleTile, tiles * kScaleTile, bar);
-                for (int j = 0; j < S::kScaleTilesQ; ++j) {
-                    // rows beyond Q: any scales will do, their results are not stored
-                    const int row = min(tq * S::kScaleTilesQ + j, a.q_tiles - 1);
-                    bulk_load(at + S::kP + S::kQ + S::kSP + j * 2 * kScaleTile,
-                              a.q_scales + ((size_t)row * a.tiles_k + 2 * k) * kScaleTile, tiles * kScaleTile, bar);
-                }
-                issued = k + 1;
+                // the scale tile that these rows of Q are in
+                bulk_load(at + S::kP + S::kQ + S::kSP, a.q_scales + ((size_t)tq * a.tiles_k + 2 * k) * kScaleTile,
+                          tiles * kScaleTile, bar);
             }
-            // no copy may be in flight when the CTA ends
-            if (dead)
-                for (int k = max(0, issued - S::kStages); k < issued; ++k) {
-                    const int s = k % S::kStages;
-                    for (uint32_t i = 0; i < kSpinLimit && !mbar_try(full + 8 * s, (k / S::kStages) & 1); ++i) {}
-                }
+            __syncwarp();
+            issued = i + 1;
         }
+        // no copy may be in flight when the CTA ends
+        if (dead)
+            for (int i = max(0, issued - S::kStages); i < issued; ++i) {
+                const int s = i % S::kStages;
+                for (uint32_t w = 0; w < kSpinLimit && !mbar_try(full + 8 * s, (i / S::kStages) & 1); ++w) {}
+            }
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0) {
-            for (int k = 0; k < stages_k; ++k) {
-                const int s = k % S::kStages;
-                if (!mbar_wait(full + 8 * s, (k / S::kStages) & 1, &dead)) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t at = stages + s * S::kStage, sc = at + S::kP + S::kQ;
-                const int tiles = min(2, a.tiles_k - 2 * k);
-                for (int t = 0; t < tiles; ++t) {
-                    copy_scales(tmem + S::kScaleP + 4 * t, scales_desc(sc + t * kScaleTile));
-                    for (int j = 0; j < S::kScaleTilesQ; ++j)
-                        copy_scales(tmem + S::kScaleQ + 4 * (t * S::kScaleTilesQ + j),
-                                    scales_desc(sc + S::kSP + (j * 2 + t) * kScaleTile));
+        bool ok = true;
+        for (int i = 0; i < n_k; ++i) {
+            const int s = i % S::kStages;
+            ok = __all_sync(kFull, mbar_wait(full + 8 * s, (i / S::kStages) & 1, &dead));
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t at = stages + s * S::kStage, sc = at + S::kP + S::kQ;
+            const int tiles = min(2, a.tiles_k - 2 * (k_begin + i));
+            const uint64_t da = codes_desc(at), db = codes_desc(at + S::kP);
+            if (elect_one()) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    if (j == tiles) break;
+                    copy_scales(tmem + S::kScaleP + 4 * j, scales_desc(sc + j * kScaleTile));
+                    copy_scales(tmem + S::kScaleQ + 4 * j, scales_desc(sc + S::kSP + j * kScaleTile));
                 }
-                const uint64_t da = codes_desc(at), db = codes_desc(at + S::kP);
-                for (int t = 0; t < tiles; ++t)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    if (j == tiles) break;
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
-                        mma(tmem, da + 2 * (2 * t + h), db + 2 * (2 * t + h), with_scale_id(mma_desc(NT), 2 * h),
-                            tmem + S::kScaleP + 4 * t, tmem + S::kScaleQ + 4 * t * S::kScaleTilesQ, k > 0 || t > 0 || h > 0);
+                        mma(tmem, da + 2 * (2 * j + h), db + 2 * (2 * j + h), with_scale_id(mma_desc(NT), 2 * h),
+                            tmem + S::kScaleP + 4 * j, tmem + S::kScaleQ + 4 * j, i > 0 || j > 0 || h > 0);
+                }
                 commit(empty + 8 * s);
             }
-            commit(done);
+            __syncwarp();
         }
+        if (ok && elect_one()) commit(done);
         __syncwarp();
     } else {
-        const bool ok = stages_k == 0 || mbar_wait(done, 0, &dead);
+        const bool ok = __all_sync(kFull, n_k == 0 || mbar_wait(done, 0, &dead));
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const int quad = warp & 3;  // the quarter of tensor memory's lanes that this warp may read
-        const long long p = (long long)tp * 128 + quad * 32 + lane;
-        T *out = static_cast<T *>(a.out) + p * a.ld_p;
-        const bool vec = a.ld_q == 1 && ((a.ld_p * sizeof(T)) & 15) == 0 && (reinterpret_cast<uintptr_t>(a.out) & 15) == 0;
-        if (ok) {
-            for (int c = 0; c < NT; c += 16) {
-                const long long q0 = (long long)tq * NT + c;
-                if (q0 >= a.Q) break;
-                float v[16];
-                __syncwarp();
-                if (stages_k) {
-                    tmem_load16(v, tmem + ((unsigned)(quad * 32) << 16) + c);
-                } else {
+        const int row = quad * 32 + lane;
+        const long long p = (long long)tp * 128 + row;
+        T *out = static_cast<T *>(a.out);
+        const bool vec = !Swap && a.split == 1 && ((a.ld * sizeof(T)) & 15) == 0 && (reinterpret_cast<uintptr_t>(a.out) & 15) == 0;
+        for (int c = 0; ok && c < NT; c += 16) {
+            const long long q0 = (long long)tq * NT + c;
+            if (q0 >= a.Q) break;
+            float v[16];
+            __syncwarp();
+            if (n_k) {
+                tmem_load16(v, tmem + ((unsigned)(quad * 32) << 16) + c);
+            } else {
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) v[k] = 0.f;
-                }
-                if (p >= a.P) continue;
+                for (int k = 0; k < 16; ++k) v[k] = 0.f;
+            }
+            if (a.split > 1) {
+                // the stages' place: every copy has landed and every instruction has read it
+#pragma unroll
+                for (int k = 0; k < 16; ++k)
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(stages + 4 * ((c + k) * S::kPitch + row)), "f"(v[k]) : "memory");
+            } else if (p < a.P) {
                 if (vec && q0 + 16 <= a.Q) {
                     __align__(16) T y[16];
 #pragma unroll
                     for (int k = 0; k < 16; ++k) put(&y[k], v[k]);
 #pragma unroll
                     for (int k = 0; k < (int)sizeof(T); ++k)
-                        reinterpret_cast<uint4 *>(out + q0)[k] = reinterpret_cast<const uint4 *>(y)[k];
+                        reinterpret_cast<uint4 *>(out + p * a.ld + q0)[k] = reinterpret_cast<const uint4 *>(y)[k];
                 } else {
 #pragma unroll
                     for (int k = 0; k < 16; ++k)
-                        if (q0 + k < a.Q) put(out + (q0 + k) * a.ld_q, v[k]);
+                        if (q0 + k < a.Q) put(out + (Swap ? (q0 + k) * a.ld + p : p * a.ld + q0 + k), v[k]);
                 }
             }
         }
@@ -546,6 +588,294 @@ __global__ void __launch_bounds__(kMmaThreads) k_matmul(const __grid_constant__ 
     if (warp == 1) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         tmem_free(tmem, S::kCols);
+    }
+    if (a.split == 1) return;
+    cluster_sync();
+    // This CTA's share of the tile: columns of it where out runs along P, else rows.
+    T *out = static_cast<T *>(a.out);
+    const int q_here = (int)min((long long)NT, a.Q - (long long)tq * NT);
+    const int p_here = (int)min(128ll, a.P - (long long)tp * 128);
+    const int share = ((Swap ? q_here : p_here) + a.split - 1) / a.split;
+    const int inner = Swap ? p_here : q_here, first = rank * share;
+    const int outer = min(share, (Swap ? q_here : p_here) - first);
+    for (int i = tid; i < outer * inner; i += kMmaThreads) {
+        const int o = first + i / inner, n = i % inner;
+        const uint32_t at = stages + 4 * (Swap ? o * S::kPitch + n : n * S::kPitch + o);
+        float sum = 0.f;
+#pragma unroll 8
+        for (int r = 0; r < a.split; ++r) sum = __fadd_rn(sum, load_cluster(in_cta(at, r)));
+        const long long p = (long long)tp * 128 + (Swap ? n : o), q = (long long)tq * NT + (Swap ? o : n);
+        put(out + (Swap ? q * a.ld + p : p * a.ld + q), sum);
+    }
+    cluster_sync();  // the others have read this CTA's sums
+}
+
+// ----------------------------------------------------------------------------
+// Large products: pairs of CTAs
+// ----------------------------------------------------------------------------
+//
+// Two CTAs of a cluster compute a tile of 256 rows of A by 256 of B with one instruction stream
+// (cta_group::2): each holds its 128 rows of A, 128 of the 256 rows of B, and its 128 rows of
+// accumulators.  A stage of 256 columns is 35 KB a CTA for 2 x 128 x 256 x 256 operations, twice
+// the operations a byte of 128 x 128 tiles, whose traffic from L2 (15 TB/s) bounded them.
+// Persistent: a pair takes every n-th tile.  Tensor memory has 512 columns: two accumulators of
+// 256 that overlap in 32, and the scales' 24.  Four warps read an accumulator back, the columns that
+// the other one needs first, while the next tile's instructions run.
+
+constexpr int kPairThreads = 192;
+struct Pair {
+    static constexpr int kStages = 5;
+    static constexpr int kA = 128 * 128, kB = 128 * 128;
+    static constexpr int kSA = 2 * kScaleTile, kSB = 4 * kScaleTile;  // the scales of all 256 rows of B
+    static constexpr int kStage = kA + kB + kSA + kSB;
+    static constexpr int kOut = 4 * 2 * 4096;  // two buffers a warp, 32 rows of 128 bytes each
+    static constexpr int kSmem = kStages * kStage + kOut + 1024;
+    static constexpr int kAcc1 = 224, kScaleA = 480, kScaleB = 488;  // tensor memory columns
+    static_assert(kStage % 1024 == 0 && kSmem <= 226 * 1024, "shared memory");
+};
+
+struct PairArgs {
+    void *out;
+    long long M, N;
+    int tiles_k;
+    int tiles_m, tiles_n;  // of 256
+    int vec;               // out's rows at 16-byte boundaries: stored by TMA
+};
+
+__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], "
+                 "[%4];" ::"r"(dst),
+                 "l"(map), "r"(x), "r"(y), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void copy_scales_pair(uint32_t tmem, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, bool add) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %6, 0;\n"
+                 "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}\n" ::"r"(d),
+                 "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"((unsigned)add)
+                 : "memory");
+}
+// Arrives on the barrier of both CTAs once every instruction before has completed.
+__device__ __forceinline__ void commit_pair(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+                 "h"((unsigned short)3)
+                 : "memory");
+}
+__device__ __forceinline__ void arrive_cluster(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__host__ __device__ constexpr uint32_t pair_desc() {
+    return 1u << 7 | 1u << 10 | (uint32_t)(256 >> 3) << 17 | 1u << 23 | (256u >> 7) << 27;
+}
+
+// Tiles in the order in which the pairs take them: columns of `kBand` tiles of A, so that those in
+// work at a time share rows of both operands in L2.
+constexpr int kBand = 8;
+__device__ __forceinline__ void tile_at(int t, const PairArgs &a, int &tm, int &tn) {
+    const int band = t / (kBand * a.tiles_n), in = t - band * kBand * a.tiles_n;
+    const int rows = min(kBand, a.tiles_m - band * kBand);
+    tm = band * kBand + in % rows;
+    tn = in / rows;
+}
+
+template <typename T>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+    k_matmul_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                  const __grid_constant__ CUtensorMap map_sa, const __grid_constant__ CUtensorMap map_sb,
+                  const __grid_constant__ CUtensorMap map_out, const PairArgs a) {
+    extern __shared__ __align__(16) unsigned tile[];
+    __shared__ __align__(8) unsigned long long bars[2 * Pair::kStages + 2];
+    __shared__ uint32_t tmem_at;
+    __shared__ volatile int dead;
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(kFull, tid >> 5, 0);
+    const unsigned rank = blockIdx.x & 1;
+    const int pairs = gridDim.x / 2, pair = blockIdx.x / 2, n_tiles = a.tiles_m * a.tiles_n;
+    const uint32_t stages = (smem_addr(tile) + 1023) & ~1023u;
+    const uint32_t outs = stages + Pair::kStages * Pair::kStage;
+    const uint32_t full = smem_addr(bars), empty = full + 8 * Pair::kStages;
+    const uint32_t acc_full = empty + 8 * Pair::kStages, acc_free = acc_full + 8;
+    const int n_k = (a.tiles_k + 1) / 2;
+    if (tid == 0) {
+        for (int s = 0; s < Pair::kStages; ++s) {
+            mbar_init(full + 8 * s, 1);
+            mbar_init(empty + 8 * s, 1);
+        }
+        mbar_init(acc_full, 1);
+        mbar_init(acc_free, 8);  // four warps of each CTA
+        dead = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_at)), "r"(512)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    cluster_sync();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = 0;  // all 512 columns were asked for
+    let_next_start();
+    wait_for_previous();
+
+    if (warp == 0) {
+        int i = 0;  // stages filled
+        bool ok = true;
+        for (int t = pair; ok && t < n_tiles; t += pairs) {
+            int tm, tn;
+            tile_at(t, a, tm, tn);
+            for (int k = 0; k < n_k; ++k, ++i) {
+                const int s = i % Pair::kStages;
+                if (i >= Pair::kStages) ok = __all_sync(kFull, mbar_wait(empty + 8 * s, (i / Pair::kStages - 1) & 1, &dead));
+                if (!ok) break;
+                const uint32_t at = stages + s * Pair::kStage, bar = in_cta(full + 8 * s, 0);
+                if (elect_one()) {
+                    if (rank == 0) mbar_expect(full + 8 * s, 2 * Pair::kStage);  // both CTAs' copies
+                    tma_load_pair(at, &map_a, k * (kStageK / 2), tm * 256 + rank * 128, bar);
+                    tma_load_pair(at + Pair::kA, &map_b, k * (kStageK / 2), tn * 256 + rank * 128, bar);
+                    tma_load_pair(at + Pair::kA + Pair::kB, &map_sa, k * 256, tm * 2 + rank, bar);
+                    tma_load_pair(at + Pair::kA + Pair::kB + Pair::kSA, &map_sb, k * 256, tn * 2, bar);
+                }
+                __syncwarp();
+            }
+        }
+        // The other CTA's arrivals on this one's barriers have all landed before it ends.
+        for (int j = max(0, i - Pair::kStages); ok && j < i; ++j)
+            ok = __all_sync(kFull, mbar_wait(empty + 8 * (j % Pair::kStages), (j / Pair::kStages) & 1, &dead));
+        // No copy may be in flight when the CTA ends.  On the way out of a wait that ran out
+        // the copies' barrier may be the other CTA's: a millisecond is far more than they take.
+        if (!ok)
+            for (int w = 0; w < 1000; ++w) __nanosleep(1000);
+        __syncwarp();
+    } else if (warp == 1) {
+        if (rank == 0) {
+            int i = 0, n = 0;
+            bool ok = true;
+            for (int t = pair; ok && t < n_tiles; t += pairs, ++n) {
+                if (n > 0) ok = __all_sync(kFull, mbar_wait(acc_free, (n - 1) & 1, &dead));
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t acc = tmem + (n & 1 ? Pair::kAcc1 : 0);
+                for (int k = 0; ok && k < n_k; ++k, ++i) {
+                    const int s = i % Pair::kStages;
+                    ok = __all_sync(kFull, mbar_wait(full + 8 * s, (i / Pair::kStages) & 1, &dead));
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t at = stages + s * Pair::kStage, sc = at + Pair::kA + Pair::kB;
+                    const int tiles = min(2, a.tiles_k - 2 * k);
+                    const uint64_t da = codes_desc(at), db = codes_desc(at + Pair::kA);
+                    if (elect_one()) {
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            if (j == tiles) break;
+                            copy_scales_pair(tmem + Pair::kScaleA + 4 * j, scales_desc(sc + j * kScaleTile));
+#pragma unroll
+                            for (int h = 0; h < 2; ++h)
+                                copy_scales_pair(tmem + Pair::kScaleB + 8 * j + 4 * h,
+                                                 scales_desc(sc + Pair::kSA + (2 * h + j) * kScaleTile));
+                        }
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            if (j == tiles) break;
+#pragma unroll
+                            for (int h = 0; h < 2; ++h)
+                                mma_pair(acc, da + 2 * (2 * j + h), db + 2 * (2 * j + h), with_scale_id(pair_desc(), 2 * h),
+                                         tmem + Pair::kScaleA + 4 * j, tmem + Pair::kScaleB + 8 * j, k > 0 || j > 0 || h > 0);
+                        }
+                        commit_pair(empty + 8 * s);
+                        if (k == n_k - 1) commit_pair(acc_full);
+                    }
+                    __syncwarp();
+                }
+            }
+        }
+        __syncwarp();
+    } else {
+        const int quad = warp & 3;
+        constexpr int kChunk = 128 / (int)sizeof(T);  // columns of 128 bytes of out
+        T *out = static_cast<T *>(a.out);
+        int n = 0, buf = 0;
+        for (int t = pair; t < n_tiles; t += pairs, ++n) {
+            int tm, tn;
+            tile_at(t, a, tm, tn);
+            if (!__all_sync(kFull, mbar_wait(acc_full, n & 1, &dead))) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t acc = tmem + (n & 1 ? Pair::kAcc1 : 0) + ((unsigned)(quad * 32) << 16);
+            const long long row0 = (long long)tm * 256 + rank * 128 + quad * 32;
+#pragma unroll 1
+            for (int c = 0; c < 256 / kChunk; ++c) {
+                // the columns that the two accumulators share come first
+                const int chunk = n & 1 ? c : 256 / kChunk - 1 - c, col = chunk * kChunk;
+                const uint32_t at = outs + quad * 8192 + buf * 4096;
+                // the store before last has read this buffer
+                if (a.vec) {
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                    __syncwarp();
+                }
+                __align__(16) T y[kChunk];
+#pragma unroll
+                for (int k = 0; k < kChunk; k += 16) {
+                    float v[16];
+                    tmem_load16(v, acc + col + k);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) put(&y[k + j], v[j]);
+                }
+                if (c == 0) {
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) arrive_cluster(in_cta(acc_free, 0));
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint4 q = reinterpret_cast<const uint4 *>(y)[j];
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + lane * 128 + ((j ^ (lane & 7)) << 4)),
+                                 "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w)
+                                 : "memory");
+                }
+                const long long c0 = (long long)tn * 256 + col;
+                if (a.vec) {
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (row0 < a.M && c0 < a.N)
+                            asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(&map_out),
+                                         "r"((int)c0), "r"((int)row0), "r"(at)
+                                         : "memory");
+                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    }
+                    buf ^= 1;
+                } else {
+                    __syncwarp();
+                    for (int r = 0; r < 32 && row0 + r < a.M; ++r)
+#pragma unroll
+                        for (int k = lane; k < kChunk; k += 32) {
+                            const uint32_t from = at + r * 128 + ((((k * (int)sizeof(T)) >> 4) ^ (r & 7)) << 4) + ((k * (int)sizeof(T)) & 15);
+                            if (c0 + k >= a.N) continue;
+                            T *to = out + (row0 + r) * a.N + c0 + k;
+                            if (sizeof(T) == 4) {
+                                unsigned u;
+                                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(u) : "r"(from) : "memory");
+                                *reinterpret_cast<unsigned *>(to) = u;
+                            } else {
+                                unsigned short u;
+                                asm volatile("ld.shared.b16 %0, [%1];" : "=h"(u) : "r"(from) : "memory");
+                                *reinterpret_cast<unsigned short *>(to) = u;
+                            }
+                        }
+                    __syncwarp();
+                }
+            }
+        }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        __syncwarp();
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    }
+    __syncthreads();
+    cluster_sync();
+    if (warp == 1) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
     }
 }
 
@@ -614,24 +944,111 @@ EncodeFn encode_fn() {
     return fn;
 }
 
-// Codes as a matrix of bytes, boxes of 128 bytes by `rows` rows.
-bool codes_map(CUtensorMap *m, const void *codes, long long rows, long long pitch, int box_rows) {
+// A matrix of `rows` rows of `cols` elements, `pitch` bytes apart, in boxes.
+bool make_map(CUtensorMap *m, CUtensorMapDataType type, const void *base, long long rows, long long cols, long long pitch,
+              int box_rows, int box_cols, CUtensorMapSwizzle swizzle) {
     const EncodeFn fn = encode_fn();
     if (!fn) return false;
-    const cuuint64_t dims[2] = {(cuuint64_t)pitch, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch};
-    const cuuint32_t box[2] = {128, (cuuint32_t)box_rows}, steps[2] = {1, 1};
-    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(codes), dims, strides, box, steps,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch};
+    const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, steps[2] = {1, 1};
+    return fn(m, type, 2, const_cast<void *>(base), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// Codes in boxes of 128 bytes by box_rows rows.
+bool codes_map(CUtensorMap *m, const void *codes, long long rows, int tiles_k, int box_rows) {
+    const long long pitch = (long long)tiles_k * (kTile / 2);
+    return make_map(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, rows, pitch, pitch, box_rows, 128, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+// Scales, a row per 128 of the matrix, in boxes of two tiles (256 words) by box_rows.
+bool scales_map(CUtensorMap *m, const void *scales, long long rows, int tiles_k, int box_rows) {
+    return make_map(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, scales, up(rows, kTile), (long long)tiles_k * (kScaleTile / 4),
+                    (long long)tiles_k * kScaleTile, box_rows, 256, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
-template <int NT, typename T>
+int sm_count() {
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    return n;
+}
+
+template <int NT, bool Swap, typename T>
 int launch_matmul(const CUtensorMap &mp, const CUtensorMap &mq, const MatmulArgs &a, unsigned grid, cudaStream_t s) {
     using S = MmaShape<NT>;
-    static_assert(S::kSmem <= 227 * 1024 - 1024, "shared memory");
-    const cudaError_t e = cudaFuncSetAttribute((const void *)k_matmul<NT, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+    const cudaError_t e = cudaFuncSetAttribute((const void *)k_matmul<NT, Swap, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
     if (e != cudaSuccess) return cuda_failed(e);
-    return tula::launch(k_matmul<NT, T>, dim3(grid), kMmaThreads, S::kSmem, s, 1, mp, mq, a);
+    return tula::launch(k_matmul<NT, Swap, T>, dim3(grid), kMmaThreads, S::kSmem, s, a.split, mp, mq, a);
+}
+
+template <typename T>
+int matmul_small(const void *a_codes, const void *a_scales, const void *b_codes, const void *b_scales, long long M, long long N,
+                 long long K, void *out, cudaStream_t s) {
+    // The operand with few rows is the instruction's N, so that its 128 rows are not padding.
+    const bool swap = M <= 128;
+    MatmulArgs a;
+    a.p_scales = static_cast<const unsigned char *>(swap ? b_scales : a_scales);
+    a.q_scales = static_cast<const unsigned char *>(swap ? a_scales : b_scales);
+    a.P = swap ? N : M;
+    a.Q = swap ? M : N;
+    a.ld = N;
+    a.out = out;
+    a.tiles_k = (int)up(K, kTile);
+    a.q_tiles = (int)up(a.Q, kTile);
+    const int nt = a.Q <= 32 ? 32 : a.Q <= 64 ? 64 : 128;
+    a.grid_q = (int)up(a.Q, nt);
+    const long long tiles = up(a.P, 128) * a.grid_q;
+    // Few tiles: up to eight CTAs share one's columns, two stages at least for each, while all
+    // are resident (two an SM).
+    a.split = 1;
+    while (a.split < 8 && tiles * a.split * 2 <= 2 * 152 && up(a.tiles_k, 2) >= 4 * a.split) a.split *= 2;
+    if (tiles * a.split >= (1LL << 31)) return TULA_ERR_ARG;
+    CUtensorMap mp, mq;
+    std::memset(&mp, 0, sizeof(mp));
+    std::memset(&mq, 0, sizeof(mq));
+    if (K && (!codes_map(&mp, swap ? b_codes : a_codes, a.P, a.tiles_k, 128) ||
+              !codes_map(&mq, swap ? a_codes : b_codes, a.Q, a.tiles_k, nt)))
+        return cuda_failed(cudaErrorInvalidValue);
+    const unsigned grid = (unsigned)(tiles * a.split);
+    if (swap)
+        return nt == 32 ? launch_matmul<32, true, T>(mp, mq, a, grid, s)
+               : nt == 64 ? launch_matmul<64, true, T>(mp, mq, a, grid, s)
+                          : launch_matmul<128, true, T>(mp, mq, a, grid, s);
+    return nt == 32 ? launch_matmul<32, false, T>(mp, mq, a, grid, s)
+           : nt == 64 ? launch_matmul<64, false, T>(mp, mq, a, grid, s)
+                      : launch_matmul<128, false, T>(mp, mq, a, grid, s);
+}
+
+template <typename T>
+int matmul_large(const void *a_codes, const void *a_scales, const void *b_codes, const void *b_scales, long long M, long long N,
+                 long long K, void *out, cudaStream_t s) {
+    PairArgs a;
+    a.out = out;
+    a.M = M;
+    a.N = N;
+    a.tiles_k = (int)up(K, kTile);
+    a.tiles_m = (int)up(M, 256);
+    a.tiles_n = (int)up(N, 256);
+    a.vec = aligned(out, 16) && N * (long long)sizeof(T) % 16 == 0;
+    CUtensorMap ma, mb, sa, sb, mo;
+    std::memset(&mo, 0, sizeof(mo));
+    const CUtensorMapDataType type = sizeof(T) == 4 ? CU_TENSOR_MAP_DATA_TYPE_UINT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16;
+    if (!codes_map(&ma, a_codes, M, a.tiles_k, 128) || !codes_map(&mb, b_codes, N, a.tiles_k, 128) ||
+        !scales_map(&sa, a_scales, M, a.tiles_k, 1) || !scales_map(&sb, b_scales, N, a.tiles_k, 2) ||
+        (a.vec && !make_map(&mo, type, out, M, N, N * (long long)sizeof(T), 32, 128 / (int)sizeof(T), CU_TENSOR_MAP_SWIZZLE_128B)))
+        return cuda_failed(cudaErrorInvalidValue);
+    const cudaError_t e = cudaFuncSetAttribute((const void *)k_matmul_pair<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, Pair::kSmem);
+    if (e != cudaSuccess) return cuda_failed(e);
+    const long long tiles = (long long)a.tiles_m * a.tiles_n, pairs = std::max(1, sm_count() / 2);
+    return tula::launch(k_matmul_pair<T>, dim3((unsigned)(2 * std::min(tiles, pairs))), kPairThreads, Pair::kSmem, s, 1, ma, mb, sa,
+                        sb, mo, a);
+}
+
+template <typename T>
+int matmul_typed(const void *a_codes, const void *a_scales, const void *b_codes, const void *b_scales, long long M, long long N,
+                 long long K, void *out, cudaStream_t s) {
+    // Pairs of CTAs from half as many tiles of 256 x 256 as there are pairs on.
+    if (K > 0 && M > 128 && N > 128 && up(M, 256) * up(N, 256) >= 38)
+        return matmul_large<T>(a_codes, a_scales, b_codes, b_scales, M, N, K, out, s);
+    return matmul_small<T>(a_codes, a_scales, b_codes, b_scales, M, N, K, out, s);
 }
 
 }  // namespace
@@ -691,41 +1108,10 @@ int tula_mx_matmul(const void *a_codes, const void *a_scales, const void *b_code
     if (K && (!a_codes || !a_scales || !b_codes || !b_scales || !aligned(a_codes, 16) || !aligned(a_scales, 16) ||
               !aligned(b_codes, 16) || !aligned(b_scales, 16)))
         return TULA_ERR_ARG;
-    // The operand with few rows is the instruction's N, so that its 128 rows are not padding.
-    const bool swap = M <= 128;
-    MatmulArgs a;
-    a.p_scales = static_cast<const unsigned char *>(swap ? b_scales : a_scales);
-    a.q_scales = static_cast<const unsigned char *>(swap ? a_scales : b_scales);
-    a.P = swap ? N : M;
-    a.Q = swap ? M : N;
-    a.ld_p = swap ? 1 : N;
-    a.ld_q = swap ? N : 1;
-    a.out = out;
-    a.tiles_k = (int)up(K, kTile);
-    a.p_tiles = (int)up(a.P, kTile);
-    a.q_tiles = (int)up(a.Q, kTile);
-    const int NT = a.Q <= 32 ? 32 : a.Q <= 64 ? 64 : 128;
-    a.grid_q = (int)up(a.Q, NT);
-    const long long grid = (long long)a.p_tiles * a.grid_q;
-    if (grid >= (1LL << 31)) return TULA_ERR_ARG;
-    CUtensorMap mp, mq;
-    std::memset(&mp, 0, sizeof(mp));
-    std::memset(&mq, 0, sizeof(mq));
-    if (K) {
-        const long long pitch = (long long)a.tiles_k * (kTile / 2);
-        if (!codes_map(&mp, swap ? b_codes : a_codes, a.P, pitch, 128) || !codes_map(&mq, swap ? a_codes : b_codes, a.Q, pitch, NT))
-            return cuda_failed(cudaErrorInvalidValue);
-    }
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    auto typed = [&](auto t) {
-        using T = decltype(t);
-        return NT == 32 ? launch_matmul<32, T>(mp, mq, a, (unsigned)grid, s)
-               : NT == 64 ? launch_matmul<64, T>(mp, mq, a, (unsigned)grid, s)
-                          : launch_matmul<128, T>(mp, mq, a, (unsigned)grid, s);
-    };
-    if (out_type == TULA_TYPE_F32) return typed(float());
-    if (out_type == TULA_TYPE_BF16) return typed(__nv_bfloat16());
-    return typed(__half());
+    if (out_type == TULA_TYPE_F32) return matmul_typed<float>(a_codes, a_scales, b_codes, b_scales, M, N, K, out, s);
+    if (out_type == TULA_TYPE_BF16) return matmul_typed<__nv_bfloat16>(a_codes, a_scales, b_codes, b_scales, M, N, K, out, s);
+    return matmul_typed<__half>(a_codes, a_scales, b_codes, b_scales, M, N, K, out, s);
 }
 
 int tula_mx_error(void *stream, int *error_out) {
