@@ -7,6 +7,7 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cstring>
 #include <type_traits>
 
@@ -428,25 +429,29 @@ __device__ __forceinline__ uint32_t in_cta(uint32_t addr, unsigned rank) {
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
-__device__ __forceinline__ float load_cluster(uint32_t addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+__device__ __forceinline__ float4 load_cluster4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                 : "r"(addr)
+                 : "memory");
     return v;
 }
 
-template <int NT>
+template <int NT, bool Swap>
 struct MmaShape {
     static constexpr int kP = 128 * 128, kQ = NT * 128;                     // bytes of codes a stage
     static constexpr int kSP = 2 * kScaleTile, kSQ = 2 * kScaleTile;
     static constexpr int kStage = kP + kQ + kSP + kSQ;
     static constexpr int kStages = NT >= 128 ? 3 : NT >= 64 ? 4 : 5;        // two CTAs an SM
-    static constexpr int kPitch = 129;                                      // floats of a column of partial sums
+    // partial sums: lines along out's rows, four floats apart to spread the banks
+    static constexpr int kLines = Swap ? NT : 128, kLine = Swap ? 128 : NT, kPitch = kLine + 4;
     static constexpr int kSmem = kStages * kStage + 1024;                   // aligned to 1024 at run time
     static constexpr int kScaleP = NT;                                      // tensor memory columns
     static constexpr int kScaleQ = kScaleP + 8;
     static constexpr int kUsed = kScaleQ + 8;
     static constexpr int kCols = kUsed <= 64 ? 64 : kUsed <= 128 ? 128 : 256;
-    static_assert(NT * kPitch * 4 <= kStages * kStage && 2 * kSmem <= 226 * 1024, "shared memory");
+    static_assert(kLines * kPitch * 4 <= kStages * kStage && 2 * kSmem <= 226 * 1024, "shared memory");
 };
 
 // One tile of 128 rows of P by NT of Q a cluster; its CTAs share the columns, and add up their
@@ -455,7 +460,7 @@ struct MmaShape {
 template <int NT, bool Swap, typename T>
 __global__ void __launch_bounds__(kMmaThreads) k_matmul(const __grid_constant__ CUtensorMap map_p,
                                                         const __grid_constant__ CUtensorMap map_q, const MatmulArgs a) {
-    using S = MmaShape<NT>;
+    using S = MmaShape<NT, Swap>;
     extern __shared__ __align__(16) unsigned tile[];
     __shared__ __align__(8) unsigned long long bars[2 * S::kStages + 1];
     __shared__ uint32_t tmem_at;
@@ -564,9 +569,17 @@ __global__ void __launch_bounds__(kMmaThreads) k_matmul(const __grid_constant__ 
             }
             if (a.split > 1) {
                 // the stages' place: every copy has landed and every instruction has read it
+                if (Swap) {
 #pragma unroll
-                for (int k = 0; k < 16; ++k)
-                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(stages + 4 * ((c + k) * S::kPitch + row)), "f"(v[k]) : "memory");
+                    for (int k = 0; k < 16; ++k)
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(stages + 4 * ((c + k) * S::kPitch + row)), "f"(v[k]) : "memory");
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 16; k += 4)
+                        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(stages + 4 * (row * S::kPitch + c + k)),
+                                     "f"(v[k]), "f"(v[k + 1]), "f"(v[k + 2]), "f"(v[k + 3])
+                                     : "memory");
+                }
             } else if (p < a.P) {
                 if (vec && q0 + 16 <= a.Q) {
                     __align__(16) T y[16];
@@ -591,21 +604,42 @@ __global__ void __launch_bounds__(kMmaThreads) k_matmul(const __grid_constant__ 
     }
     if (a.split == 1) return;
     cluster_sync();
-    // This CTA's share of the tile: columns of it where out runs along P, else rows.
+    // This CTA's share of the tile's lines, four elements a thread.
     T *out = static_cast<T *>(a.out);
     const int q_here = (int)min((long long)NT, a.Q - (long long)tq * NT);
     const int p_here = (int)min(128ll, a.P - (long long)tp * 128);
-    const int share = ((Swap ? q_here : p_here) + a.split - 1) / a.split;
-    const int inner = Swap ? p_here : q_here, first = rank * share;
-    const int outer = min(share, (Swap ? q_here : p_here) - first);
-    for (int i = tid; i < outer * inner; i += kMmaThreads) {
-        const int o = first + i / inner, n = i % inner;
-        const uint32_t at = stages + 4 * (Swap ? o * S::kPitch + n : n * S::kPitch + o);
-        float sum = 0.f;
-#pragma unroll 8
-        for (int r = 0; r < a.split; ++r) sum = __fadd_rn(sum, load_cluster(in_cta(at, r)));
-        const long long p = (long long)tp * 128 + (Swap ? n : o), q = (long long)tq * NT + (Swap ? o : n);
-        put(out + (Swap ? q * a.ld + p : p * a.ld + q), sum);
+    const int lines = Swap ? q_here : p_here, line = Swap ? p_here : q_here;
+    const int share = (lines + a.split - 1) / a.split, first = rank * share;
+    const long long line0 = Swap ? (long long)tq * NT : (long long)tp * 128, col0 = Swap ? (long long)tp * 128 : (long long)tq * NT;
+    const bool vec = a.ld % 4 == 0 && (reinterpret_cast<uintptr_t>(a.out) & (4 * sizeof(T) - 1)) == 0;
+    constexpr int kQuads = S::kLine / 4;
+    for (int i = tid; i < min(share, lines - first) * kQuads; i += kMmaThreads) {
+        const int o = first + i / kQuads, n = i % kQuads * 4;
+        if (n >= line) continue;
+        const uint32_t at = stages + 4 * (o * S::kPitch + n);
+        float4 part[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+            if (r < a.split) part[r] = load_cluster4(in_cta(at, r));
+        float4 sum = part[0];
+#pragma unroll
+        for (int r = 1; r < 8; ++r)
+            if (r < a.split)
+                sum = make_float4(__fadd_rn(sum.x, part[r].x), __fadd_rn(sum.y, part[r].y), __fadd_rn(sum.z, part[r].z),
+                                  __fadd_rn(sum.w, part[r].w));
+        T *to = out + (line0 + o) * a.ld + col0 + n;
+        __align__(16) T y[4];
+        put(&y[0], sum.x), put(&y[1], sum.y), put(&y[2], sum.z), put(&y[3], sum.w);
+        if (vec && n + 4 <= line) {
+            if (sizeof(T) == 4)
+                *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(y);
+            else
+                *reinterpret_cast<uint2 *>(to) = *reinterpret_cast<const uint2 *>(y);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (n + k < line) to[k] = y[k];
+        }
     }
     cluster_sync();  // the others have read this CTA's sums
 }
@@ -900,16 +934,29 @@ long long tiles_of(long long rows, long long cols) {
     return t < (1LL << 31) ? t : -1;
 }
 
+// Lets a kernel have `smem` bytes of dynamic shared memory, once per kernel and device.
+int allow_smem(const void *kernel, int smem, std::atomic<uint64_t> *done) {
+    if (smem <= 48 * 1024) return TULA_OK;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    const uint64_t bit = 1ull << (dev & 63);
+    if (e == cudaSuccess && (dev > 63 || !(done->load(std::memory_order_acquire) & bit))) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e == cudaSuccess) done->fetch_or(bit, std::memory_order_release);
+    }
+    return e == cudaSuccess ? TULA_OK : cuda_failed(e);
+}
+
 template <typename T, int VB>
 int launch_quantize(const QuantArgs &a, unsigned grid, cudaStream_t s) {
-    void (*k)(const QuantArgs) = a.codes && a.codes_t ? k_quantize<T, VB, true, true>
-                                 : a.codes            ? k_quantize<T, VB, true, false>
-                                                      : k_quantize<T, VB, false, true>;
+    static std::atomic<uint64_t> done[3];
+    const int which = a.codes && a.codes_t ? 0 : a.codes ? 1 : 2;
+    void (*k)(const QuantArgs) = which == 0   ? k_quantize<T, VB, true, true>
+                                 : which == 1 ? k_quantize<T, VB, true, false>
+                                              : k_quantize<T, VB, false, true>;
     const int smem = a.codes_t ? kTile * kTile * (int)sizeof(T) : 0;
-    if (smem > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute((const void *)k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-        if (e != cudaSuccess) return cuda_failed(e);
-    }
+    const int rc = allow_smem((const void *)k, smem, &done[which]);
+    if (rc) return rc;
     return tula::launch(k, dim3(grid), 256, smem, s, 1, a);
 }
 template <typename T>
@@ -965,6 +1012,7 @@ bool scales_map(CUtensorMap *m, const void *scales, long long rows, int tiles_k,
                     (long long)tiles_k * kScaleTile, box_rows, 256, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
+// (cudaDeviceGetAttribute is a table lookup, some 30 ns)
 int sm_count() {
     int dev = 0, n = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
@@ -973,9 +1021,10 @@ int sm_count() {
 
 template <int NT, bool Swap, typename T>
 int launch_matmul(const CUtensorMap &mp, const CUtensorMap &mq, const MatmulArgs &a, unsigned grid, cudaStream_t s) {
-    using S = MmaShape<NT>;
-    const cudaError_t e = cudaFuncSetAttribute((const void *)k_matmul<NT, Swap, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
-    if (e != cudaSuccess) return cuda_failed(e);
+    using S = MmaShape<NT, Swap>;
+    static std::atomic<uint64_t> done;
+    const int rc = allow_smem((const void *)k_matmul<NT, Swap, T>, S::kSmem, &done);
+    if (rc) return rc;
     return tula::launch(k_matmul<NT, Swap, T>, dim3(grid), kMmaThreads, S::kSmem, s, a.split, mp, mq, a);
 }
 
@@ -1035,8 +1084,9 @@ int matmul_large(const void *a_codes, const void *a_scales, const void *b_codes,
         !scales_map(&sa, a_scales, M, a.tiles_k, 1) || !scales_map(&sb, b_scales, N, a.tiles_k, 2) ||
         (a.vec && !make_map(&mo, type, out, M, N, N * (long long)sizeof(T), 32, 128 / (int)sizeof(T), CU_TENSOR_MAP_SWIZZLE_128B)))
         return cuda_failed(cudaErrorInvalidValue);
-    const cudaError_t e = cudaFuncSetAttribute((const void *)k_matmul_pair<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, Pair::kSmem);
-    if (e != cudaSuccess) return cuda_failed(e);
+    static std::atomic<uint64_t> done;
+    const int rc = allow_smem((const void *)k_matmul_pair<T>, Pair::kSmem, &done);
+    if (rc) return rc;
     const long long tiles = (long long)a.tiles_m * a.tiles_n, pairs = std::max(1, sm_count() / 2);
     return tula::launch(k_matmul_pair<T>, dim3((unsigned)(2 * std::min(tiles, pairs))), kPairThreads, Pair::kSmem, s, 1, ma, mb, sa,
                         sb, mo, a);

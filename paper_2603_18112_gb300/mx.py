@@ -11,7 +11,6 @@ Everything runs in the CUDA library, asynchronously on the current stream.
 from __future__ import annotations
 
 import ctypes
-from typing import NamedTuple
 
 import torch
 
@@ -35,13 +34,52 @@ def _lib():
     return _typed
 
 
-class MXMatrix(NamedTuple):
-    """A rows x cols matrix in MXFP4: codes uint8 [rows, P / 2] and scales uint8
-    [ceil(rows / 128), P / 128, 32, 4, 4], P = cols rounded up to a multiple of 128."""
-    codes: torch.Tensor
-    scales: torch.Tensor
-    rows: int
-    cols: int
+class MXMatrix:
+    """A rows x cols matrix in MXFP4: ``codes`` uint8 [rows, P / 2] and ``scales`` uint8
+    [ceil(rows / 128), P / 128, 32, 4, 4], P = cols rounded up to a multiple of 128; of any shapes
+    of those sizes, contiguous, on one GPU.  Not to be changed once made."""
+
+    __slots__ = ("rows", "cols", "dev", "code_ptr", "scale_ptr", "_codes", "_scales", "_buffer")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int):
+        tiles = (cols + 127) // 128
+        if (codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or not codes.is_contiguous()
+                or not scales.is_contiguous() or rows < 0 or cols < 0 or codes.numel() != rows * tiles * 64
+                or scales.numel() != (rows + 127) // 128 * tiles * 512):
+            raise ValueError(f"not the codes and scales of a {rows} x {cols} matrix")
+        self.rows, self.cols, self._codes, self._scales = rows, cols, codes, scales
+        self.dev = _on_gpu(codes, scales)
+        self.code_ptr, self.scale_ptr = codes.data_ptr(), scales.data_ptr()
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, device) -> "MXMatrix":
+        """One to quantise into, in one allocation."""
+        self = cls.__new__(cls)
+        tiles = (cols + 127) // 128
+        n = (rows + 127) // 128 * tiles * 512
+        buf = torch.empty(n + rows * tiles * 64, dtype=torch.uint8, device=device)
+        self.rows, self.cols, self._buffer, self._codes, self._scales = rows, cols, buf, None, None
+        self.dev, self.scale_ptr = buf.get_device(), buf.data_ptr()
+        self.code_ptr = self.scale_ptr + n
+        return self
+
+    def _split(self):
+        n = self.code_ptr - self.scale_ptr
+        tiles = (self.cols + 127) // 128
+        self._scales = self._buffer[:n].view(-1, tiles, 32, 4, 4) if tiles else self._buffer[:n]
+        self._codes = self._buffer[n:].view(self.rows, tiles * 64)
+
+    @property
+    def codes(self) -> torch.Tensor:
+        if self._codes is None:
+            self._split()
+        return self._codes
+
+    @property
+    def scales(self) -> torch.Tensor:
+        if self._scales is None:
+            self._split()
+        return self._scales
 
 
 def tula_mx_size(rows: int, cols: int) -> tuple[int, int]:
@@ -51,38 +89,41 @@ def tula_mx_size(rows: int, cols: int) -> tuple[int, int]:
     return a.value, b.value
 
 
-def empty(rows: int, cols: int, device) -> MXMatrix:
-    """An MXMatrix to quantise into."""
-    tiles = -(-cols // 128)
-    return MXMatrix(torch.empty(rows, tiles * 64, dtype=torch.uint8, device=device),
-                    torch.empty(-(-rows // 128), tiles, 32, 4, 4, dtype=torch.uint8, device=device),
-                    rows, cols)
+_raw_stream, _get_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
 def _on_gpu(*tensors):
+    """The index of the one GPU that the tensors are on."""
+    dev = tensors[0].get_device()
     for t in tensors:
-        if t.device.type != "cuda" or t.device != tensors[0].device:
+        if not t.is_cuda or t.get_device() != dev:
             raise TypeError(f"tensors on one GPU are wanted, got {[str(t.device) for t in tensors]}")
+    return dev
 
 
-def _good(q: MXMatrix, what: str):
-    tiles, r = -(-q.cols // 128), -(-q.rows // 128)
-    if (q.codes.dtype != torch.uint8 or q.scales.dtype != torch.uint8 or not q.codes.is_contiguous()
-            or not q.scales.is_contiguous() or q.codes.numel() != q.rows * tiles * 64
-            or q.scales.numel() != r * tiles * 512):
-        raise ValueError(f"{what}: not the codes and scales of a {q.rows} x {q.cols} matrix")
+def _call(where, dev, fn, *args):
+    """fn(*args, current stream) with the tensors' GPU current; switching to it costs some
+    microseconds, so only where it is not."""
+    if dev == _get_device():
+        rc = fn(*args, _raw_stream(dev))
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, _raw_stream(dev))
+    if rc:
+        _check(rc, where)
 
 
 def _type(dtype, what):
-    if dtype not in TYPES:
+    kind = TYPES.get(dtype)
+    if kind is None:
         raise TypeError(f"{what}: float32, bfloat16 or float16 is wanted, got {dtype}")
-    return TYPES[dtype]
+    return kind
 
 
-def quantize(x: torch.Tensor, rows: bool = True, cols: bool = False, stream=None):
+def quantize(x: torch.Tensor, rows: bool = True, cols: bool = False):
     """x (2-D; its rows may lie apart) as an MXMatrix (rows), its transpose as one (cols), or both
     as a pair from one reading of x."""
-    _on_gpu(x)
+    dev = _on_gpu(x)
     kind = _type(x.dtype, "quantize")
     if x.dim() != 2 or not (rows or cols):
         raise ValueError("quantize: a matrix, and at least one of rows and cols, are wanted")
@@ -91,41 +132,31 @@ def quantize(x: torch.Tensor, rows: bool = True, cols: bool = False, stream=None
     if c > 1 and x.stride(1) != 1 or r > 1 and x.stride(0) < c:
         x = x.contiguous()
     stride = x.stride(0) if r > 1 else c
-    q = empty(r, c, x.device) if rows else None
-    t = empty(c, r, x.device) if cols else None
-    with torch.cuda.device(x.device):
-        _check(_lib().tula_mx_quantize(
-            x.data_ptr(), kind, r, c, stride, q.codes.data_ptr() if rows else None,
-            q.scales.data_ptr() if rows else None, t.codes.data_ptr() if cols else None,
-            t.scales.data_ptr() if cols else None, _stream_ptr(stream)), "tula_mx_quantize")
+    q = MXMatrix.empty(r, c, x.device) if rows else None
+    t = MXMatrix.empty(c, r, x.device) if cols else None
+    _call("tula_mx_quantize", dev, _lib().tula_mx_quantize, x.data_ptr(), kind, r, c, stride,
+          q.code_ptr if rows else None, q.scale_ptr if rows else None,
+          t.code_ptr if cols else None, t.scale_ptr if cols else None)
     return (q, t) if rows and cols else q if rows else t
 
 
-def dequantize(q: MXMatrix, dtype=torch.bfloat16, stream=None) -> torch.Tensor:
+def dequantize(q: MXMatrix, dtype=torch.bfloat16) -> torch.Tensor:
     """The values that q stands for."""
-    _good(q, "dequantize")
-    _on_gpu(q.codes, q.scales)
     kind = _type(dtype, "dequantize")
-    out = torch.empty(q.rows, q.cols, dtype=dtype, device=q.codes.device)
-    with torch.cuda.device(out.device):
-        _check(_lib().tula_mx_dequantize(q.codes.data_ptr(), q.scales.data_ptr(), q.rows, q.cols,
-                                         out.data_ptr(), kind, _stream_ptr(stream)), "tula_mx_dequantize")
+    out = torch.empty(q.rows, q.cols, dtype=dtype, device=q.dev)
+    _call("tula_mx_dequantize", q.dev, _lib().tula_mx_dequantize, q.code_ptr, q.scale_ptr, q.rows,
+          q.cols, out.data_ptr(), kind)
     return out
 
 
-def matmul(a: MXMatrix, b: MXMatrix, dtype=torch.bfloat16, stream=None) -> torch.Tensor:
+def matmul(a: MXMatrix, b: MXMatrix, dtype=torch.bfloat16) -> torch.Tensor:
     """A B^T for a of M x K and b of N x K, as an M x N tensor of dtype."""
-    _good(a, "matmul")
-    _good(b, "matmul")
-    _on_gpu(a.codes, a.scales, b.codes, b.scales)
-    if a.cols != b.cols:
-        raise ValueError(f"matmul: {a.cols} columns and {b.cols}")
+    if a.cols != b.cols or a.dev != b.dev:
+        raise ValueError(f"matmul: {a.cols} columns on GPU {a.dev} and {b.cols} on GPU {b.dev}")
     kind = _type(dtype, "matmul")
-    out = torch.empty(a.rows, b.rows, dtype=dtype, device=a.codes.device)
-    with torch.cuda.device(out.device):
-        _check(_lib().tula_mx_matmul(a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(),
-                                     b.scales.data_ptr(), a.rows, b.rows, a.cols, out.data_ptr(), kind,
-                                     _stream_ptr(stream)), "tula_mx_matmul")
+    out = torch.empty(a.rows, b.rows, dtype=dtype, device=a.dev)
+    _call("tula_mx_matmul", a.dev, _lib().tula_mx_matmul, a.code_ptr, a.scale_ptr, b.code_ptr,
+          b.scale_ptr, a.rows, b.rows, a.cols, out.data_ptr(), kind)
     return out
 
 

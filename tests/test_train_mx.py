@@ -65,7 +65,9 @@ def test_binding_refusals():
     with pytest.raises(TypeError):
         mx.quantize(torch.zeros(4, 4))
     with pytest.raises(ValueError):
-        mx.dequantize(mx.MXMatrix(torch.zeros(4, 64, dtype=torch.uint8), torch.zeros(512, dtype=torch.uint8), 5, 4))
+        mx.MXMatrix(torch.zeros(4, 64, dtype=torch.uint8), torch.zeros(512, dtype=torch.uint8), 5, 4)
+    with pytest.raises(TypeError):
+        mx.MXMatrix(torch.zeros(4, 64, dtype=torch.uint8), torch.zeros(512, dtype=torch.uint8), 4, 4)
     with pytest.raises(ValueError):
         mx.linear(torch.zeros(3, 4), torch.zeros(5, 6))
 
@@ -300,7 +302,9 @@ def test_matmul_refusals():
     with pytest.raises(TypeError):
         mx.matmul(a, a, torch.float64)
     with pytest.raises(ValueError):
-        mx.matmul(a._replace(rows=5), a)
+        mx.MXMatrix(a.codes, a.scales, 5, 64)
+    same = mx.MXMatrix(a.codes, a.scales, 4, 64)
+    assert torch.equal(mx.matmul(same, a), mx.matmul(a, a))
 
 
 # ---------------------------------------------------------------------------------------------
