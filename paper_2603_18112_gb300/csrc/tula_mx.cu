@@ -24,6 +24,54 @@ __device__ __forceinline__ void let_next_start() {
 }
 
 // ----------------------------------------------------------------------------
+// Barriers and copies
+// ----------------------------------------------------------------------------
+
+constexpr uint32_t kSpinLimit = 1u << 19;  // bound on every wait (~2 s)
+static __device__ unsigned g_mx_error;
+
+__device__ __forceinline__ uint32_t smem_addr(const void *p) {
+    return (uint32_t)__cvta_generic_to_shared(p);
+}
+__device__ __forceinline__ void mbar_init(uint32_t bar, unsigned count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint32_t bar, unsigned bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint32_t bar, unsigned parity) {
+    unsigned ok;
+    asm volatile("{\n.reg .pred p;\n"
+                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+                 "selp.u32 %0, 1, 0, p;\n}\n"
+                 : "=r"(ok)
+                 : "r"(bar), "r"(parity)
+                 : "memory");
+    return ok != 0;
+}
+// False if the wait ran out, here or before in another warp (`dead`).
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, unsigned parity, volatile int *dead) {
+    for (uint32_t i = 0; i < kSpinLimit; ++i) {
+        if (mbar_try(bar, parity)) return true;
+        if (*dead) return false;
+    }
+    *dead = 1;
+    atomicOr(&g_mx_error, 1u);
+    return false;
+}
+
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+                 "l"(map), "r"(x), "r"(y), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, unsigned bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+                 "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
+}
+
+// ----------------------------------------------------------------------------
 // Elements
 // ----------------------------------------------------------------------------
 
@@ -83,40 +131,69 @@ struct QuantArgs {
     int tiles_r;
 };
 
-// Eight elements of a row from column c on, as they are: 16-bit types in 4 words, fp32 in 8.  Zero
-// beyond `left` elements.  VB: bytes that a load may take (the row's alignment).
-template <typename T, int VB>
-__device__ __forceinline__ void load_row8(unsigned (&w)[sizeof(T) * 2], const T *p, long long left) {
-    constexpr int kWords = sizeof(T) * 2;
-    if (left >= 8 && VB >= 4) {
-        if (VB == 16) {
+// Eight elements of a row as they are, 16-bit types in 4 words, fp32 in 8; zero beyond `left` of
+// them.  Aligned: they start at a 16-byte boundary.  Else the 16-byte granules that hold them are
+// loaded, the last also by the next lane, and shifted; inner: all of them lie within the matrix
+// ([begin, end)) and all eight within the row, else granules that reach out of it are loaded element
+// by element.
+template <typename T>
+__device__ __forceinline__ uint4 load_granule(unsigned long long at, unsigned long long begin, unsigned long long end) {
+    if (at >= begin && at + 16 <= end) return __ldg(reinterpret_cast<const uint4 *>(at));
+    unsigned w[4];
 #pragma unroll
-            for (int k = 0; k < kWords / 4; ++k) {
-                const uint4 q = __ldcs(reinterpret_cast<const uint4 *>(p) + k);
-                w[4 * k] = q.x, w[4 * k + 1] = q.y, w[4 * k + 2] = q.z, w[4 * k + 3] = q.w;
-            }
-        } else if (VB == 8) {
-#pragma unroll
-            for (int k = 0; k < kWords / 2; ++k) {
-                const uint2 q = __ldcs(reinterpret_cast<const uint2 *>(p) + k);
-                w[2 * k] = q.x, w[2 * k + 1] = q.y;
-            }
+    for (int k = 0; k < 4; ++k) {
+        const unsigned long long p = at + 4 * k;
+        w[k] = 0;
+        if (sizeof(T) == 4) {
+            if (p >= begin && p < end) w[k] = *reinterpret_cast<const unsigned *>(p);
         } else {
+            if (p >= begin && p < end) w[k] = *reinterpret_cast<const unsigned short *>(p);
+            if (p + 2 >= begin && p + 2 < end) w[k] |= (unsigned)*reinterpret_cast<const unsigned short *>(p + 2) << 16;
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <typename T, bool Aligned>
+__device__ __forceinline__ void load_row8(unsigned (&w)[sizeof(T) * 2], const T *p, bool inner, long long left,
+                                          unsigned long long begin, unsigned long long end) {
+    constexpr int kWords = sizeof(T) * 2;
+    if (!inner && left <= 0) {
 #pragma unroll
-            for (int k = 0; k < kWords; ++k) w[k] = __ldcs(reinterpret_cast<const unsigned *>(p) + k);
+        for (int k = 0; k < kWords; ++k) w[k] = 0;
+        return;
+    }
+    if (Aligned && (inner || left >= 8)) {
+#pragma unroll
+        for (int k = 0; k < kWords / 4; ++k) {
+            const uint4 q = __ldcs(reinterpret_cast<const uint4 *>(p) + k);
+            w[4 * k] = q.x, w[4 * k + 1] = q.y, w[4 * k + 2] = q.z, w[4 * k + 3] = q.w;
         }
         return;
     }
-    if (sizeof(T) == 4) {
+    const unsigned long long at = reinterpret_cast<unsigned long long>(p);
+    const int off = (int)(at & 15);
+    unsigned v[kWords + 4];
 #pragma unroll
-        for (int k = 0; k < kWords; ++k) w[k] = k < left ? __ldcs(reinterpret_cast<const unsigned *>(p) + k) : 0u;
-    } else {
-        const unsigned short *h = reinterpret_cast<const unsigned short *>(p);
+    for (int k = 0; k <= kWords / 4; ++k) {
+        uint4 q = make_uint4(0, 0, 0, 0);
+        if (inner)
+            q = __ldg(reinterpret_cast<const uint4 *>(at - off) + k);
+        else if (k < kWords / 4 || off)
+            q = load_granule<T>(at - off + 16 * k, begin, end);
+        v[4 * k] = q.x, v[4 * k + 1] = q.y, v[4 * k + 2] = q.z, v[4 * k + 3] = q.w;
+    }
 #pragma unroll
-        for (int k = 0; k < kWords; ++k) {
-            const unsigned lo = 2 * k < left ? __ldcs(h + 2 * k) : 0, hi = 2 * k + 1 < left ? __ldcs(h + 2 * k + 1) : 0;
-            w[k] = lo | hi << 16;
-        }
+    for (int k = 0; k < kWords + 2; ++k) v[k] = off & 8 ? v[k + 2] : v[k];
+#pragma unroll
+    for (int k = 0; k < kWords + 1; ++k) v[k] = off & 4 ? v[k + 1] : v[k];
+#pragma unroll
+    for (int k = 0; k < kWords; ++k) {
+        w[k] = sizeof(T) == 2 && off & 2 ? __funnelshift_r(v[k], v[k + 1], 16) : v[k];
+        if (inner) continue;
+        if (sizeof(T) == 4)
+            w[k] = k < left ? w[k] : 0u;
+        else
+            w[k] = 2 * k + 1 < left ? w[k] : 2 * k < left ? w[k] & 0xffffu : 0u;
     }
 }
 
@@ -135,55 +212,134 @@ __device__ __forceinline__ void floats8(float (&x)[8], const unsigned (&w)[sizeo
     }
 }
 
-template <typename T, int VB, bool Rows, bool Cols>
-__global__ void __launch_bounds__(256) k_quantize(const QuantArgs a) {
-    constexpr int kWords = sizeof(T) * 2;   // of eight elements
+// The largest magnitude of 16-bit elements, from their own bits to fp32's.
+template <typename T>
+__device__ __forceinline__ unsigned top_bits(unsigned half) {
+    return std::is_same<T, __half>::value ? __float_as_uint(__half2float(__ushort_as_half((unsigned short)half))) : half << 16;
+}
+// The larger magnitudes of a word and those so far; 16-bit elements by halves, in their own bits.
+template <typename T>
+__device__ __forceinline__ unsigned larger(unsigned top, unsigned w) {
+    return sizeof(T) == 4 ? max(top, w & 0x7fffffffu) : __vmaxu2(top, w & 0x7fff7fffu);
+}
+
+// Eight elements of a row, four lanes to a block, sixteen to the tile's row: their codes; scales:
+// the row's four scale bytes.
+template <typename T>
+__device__ __forceinline__ unsigned quantize_row8(const unsigned (&w)[sizeof(T) * 2], int sub, unsigned &scales) {
+    unsigned top = 0;
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(T) * 2; ++j) top = larger<T>(top, w[j]);
+    if (sizeof(T) == 2) top = max(top & 0xffffu, top >> 16);
+    top = max(top, __shfl_xor_sync(kFull, top, 1));
+    top = max(top, __shfl_xor_sync(kFull, top, 2));
+    if (sizeof(T) == 2) top = top_bits<T>(top);
+    const unsigned s = scale_byte(top);
+    const float f = inverse_scale(s);
+    float x[8];
+    floats8<T>(x, w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = __fmul_rn(x[j], f);
+    scales = s << (8 * (sub >> 2));
+    scales |= __shfl_xor_sync(kFull, scales, 4);
+    scales |= __shfl_xor_sync(kFull, scales, 8);
+    return s == 255u ? 0u : codes8(x);
+}
+
+// 32 rows (block rb) of word c of a tile in shared memory, that is of one column (fp32) or two:
+// codes to out, `pitch` bytes a column, scale bytes to scales.
+template <typename T>
+__device__ __forceinline__ void quantize_cols(const unsigned *tile, int c, int rb, unsigned char *out, int pitch,
+                                              unsigned char *scales) {
+    unsigned w[32], top = 0;
+#pragma unroll
+    for (int k = 0; k < 32; ++k) {
+        w[k] = tile[(32 * rb + k) * (kTile * (int)sizeof(T) / 4) + c];
+        top = larger<T>(top, w[k]);
+    }
+#pragma unroll
+    for (int h = 0; h < 4 / (int)sizeof(T); ++h) {
+        const int col = sizeof(T) == 4 ? c : 2 * c + h;
+        const unsigned s = scale_byte(sizeof(T) == 4 ? top : top_bits<T>(h ? top >> 16 : top & 0xffffu));
+        const float f = inverse_scale(s);
+        unsigned q[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float v;
+                if (sizeof(T) == 4) {
+                    v = __uint_as_float(w[8 * k + j]);
+                } else {
+                    const float2 p = pair_of<T>(w[8 * k + j]);
+                    v = h ? p.y : p.x;
+                }
+                x[j] = __fmul_rn(v, f);
+            }
+            q[k] = s == 255u ? 0u : codes8(x);
+        }
+        *reinterpret_cast<uint4 *>(out + col * pitch + 16 * rb) = make_uint4(q[0], q[1], q[2], q[3]);
+        scales[(col & 31) * 16 + (col >> 5) * 4 + rb] = (unsigned char)s;
+    }
+}
+
+constexpr int kOutPitch = 80;  // bytes of a column's 64 of codes, and 16 to spread the banks
+
+// fp32: twice the threads, so that a column block is one thread's in either type's tile.
+template <typename T>
+struct QuantShape {
+    static constexpr int kThreads = sizeof(T) == 4 ? 512 : 256;
+    static constexpr int kCtas = sizeof(T) == 4 ? 2 : 4;  // an SM, that registers are left for
+    static constexpr int kSmem = kTile * kTile * (int)sizeof(T) + kTile * kOutPitch;
+};
+
+template <typename T, bool Aligned, bool Rows, bool Cols>
+__global__ void __launch_bounds__(QuantShape<T>::kThreads, QuantShape<T>::kCtas) k_quantize(const QuantArgs a) {
+    constexpr int kThreads = QuantShape<T>::kThreads;
+    constexpr int kWords = sizeof(T) * 2;          // of eight elements
     constexpr int kPitch = kTile * sizeof(T) / 4;  // words of a tile's row
-    extern __shared__ __align__(16) unsigned tile[];  // Cols: kTile * kPitch
+    constexpr int kLoads = kTile * 16 / kThreads;  // of eight elements a thread
+    extern __shared__ __align__(16) unsigned tile[];  // Cols
     __shared__ __align__(16) unsigned scale_words[2][kTile];
     let_next_start();
     wait_for_previous();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x;
     const int tr = blockIdx.x / a.tiles_c, tc = blockIdx.x % a.tiles_c;
     const long long r0 = (long long)tr * kTile, c0 = (long long)tc * kTile;
-    const int sub = lane & 15;  // eight columns of the tile
+    const int sub = tid & 15;  // eight columns of the tile
     const long long left = a.cols - c0 - 8 * sub;
-    const size_t pitch = (size_t)a.tiles_c * (kTile / 2);
-    unsigned w[8][kWords];
+    const size_t pitch = (size_t)a.tiles_c * (kTile / 2), pitch_t = (size_t)a.tiles_r * (kTile / 2);
+    const unsigned long long begin = reinterpret_cast<unsigned long long>(a.x);
+    const unsigned long long end = begin + ((unsigned long long)(a.rows - 1) * a.stride + a.cols) * sizeof(T);
+    unsigned w[kLoads][kWords];
+    const T *p0 = static_cast<const T *>(a.x) + (r0 + (tid >> 4)) * a.stride + c0 + 8 * sub;
+    if (c0 + kTile <= a.cols && (Aligned ? r0 + kTile <= a.rows : tr > 0 && r0 + kTile < a.rows)) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const long long r = r0 + warp * 16 + 2 * i + (lane >> 4);
-        const T *p = static_cast<const T *>(a.x) + r * a.stride + c0 + 8 * sub;
-        load_row8<T, VB>(w[i], p, r < a.rows ? left : 0);
+        for (int i = 0; i < kLoads; ++i)
+            load_row8<T, Aligned>(w[i], p0 + i * (kThreads / 16) * a.stride, true, 8, begin, end);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const long long r = r0 + i * (kThreads / 16) + (tid >> 4);
+            load_row8<T, Aligned>(w[i], p0 + i * (kThreads / 16) * a.stride, false, r < a.rows ? left : 0, begin, end);
+        }
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int row = warp * 16 + 2 * i + (lane >> 4);
-        if (Rows) {
-            float x[8];
-            floats8<T>(x, w[i]);
-            unsigned top = 0;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(x[k]) & 0x7fffffffu);
-            top = max(top, __shfl_xor_sync(kFull, top, 1));
-            top = max(top, __shfl_xor_sync(kFull, top, 2));
-            const unsigned s = scale_byte(top);
-            const float f = inverse_scale(s);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] = __fmul_rn(x[k], f);
-            const unsigned q = s == 255u ? 0u : codes8(x);
-            unsigned word = s << (8 * (sub >> 2));
-            word |= __shfl_xor_sync(kFull, word, 4);
-            word |= __shfl_xor_sync(kFull, word, 8);
-            if (r0 + row < a.rows)
-                *reinterpret_cast<unsigned *>(a.codes + (size_t)(r0 + row) * pitch + c0 / 2 + 4 * sub) = q;
-            if (sub == 0) scale_words[0][(row & 31) * 4 + (row >> 5)] = word;
-        }
+    for (int i = 0; i < kLoads; ++i) {
+        const int row = i * (kThreads / 16) + (tid >> 4);
         if (Cols) {
 #pragma unroll
             for (int k = 0; k < kWords / 4; ++k)
                 *reinterpret_cast<uint4 *>(&tile[row * kPitch + sub * kWords + 4 * k]) =
                     make_uint4(w[i][4 * k], w[i][4 * k + 1], w[i][4 * k + 2], w[i][4 * k + 3]);
+        }
+        if (Rows) {
+            unsigned scales;
+            const unsigned q = quantize_row8<T>(w[i], sub, scales);
+            if (r0 + row < a.rows)
+                *reinterpret_cast<unsigned *>(a.codes + (size_t)(r0 + row) * pitch + c0 / 2 + 4 * sub) = q;
+            if (sub == 0) scale_words[0][(row & 31) * 4 + (row >> 5)] = scales;
         }
     }
     __syncthreads();
@@ -191,53 +347,121 @@ __global__ void __launch_bounds__(256) k_quantize(const QuantArgs a) {
         *reinterpret_cast<uint4 *>(a.scales + ((size_t)tr * a.tiles_c + tc) * kScaleTile + 16 * tid) =
             *reinterpret_cast<const uint4 *>(&scale_words[0][4 * tid]);
     if (!Cols) return;
-    // columns 2 * (tid % 64) and the next, rows 32 * (tid / 64) on
-    const int pair = tid & 63, rb = tid >> 6;
-    unsigned q[2][4];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        unsigned top = 0;
-        float x[32];
-#pragma unroll
-        for (int k = 0; k < 32; ++k) {
-            const unsigned *p = &tile[(32 * rb + k) * kPitch + pair * (int)(sizeof(T) / 2)];
-            if (sizeof(T) == 4) {
-                x[k] = __uint_as_float(p[h]);
-            } else {
-                const float2 f = pair_of<T>(p[0]);
-                x[k] = h ? f.y : f.x;
-            }
-            top = max(top, __float_as_uint(x[k]) & 0x7fffffffu);
-        }
-        const unsigned s = scale_byte(top);
-        const float f = inverse_scale(s);
-#pragma unroll
-        for (int k = 0; k < 32; k += 8) {
-            float y[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = __fmul_rn(x[k + j], f);
-            q[h][k / 8] = s == 255u ? 0u : codes8(y);
-        }
-        const int c = 2 * pair + h;
-        reinterpret_cast<unsigned char *>(scale_words[1])[(c & 31) * 16 + (c >> 5) * 4 + rb] = (unsigned char)s;
-    }
-    __syncthreads();  // the tile's values are all read: their place takes the codes
-    constexpr int kOut = 20;  // words of a column's 64 bytes of codes, and 16 bytes to spread the banks
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-        *reinterpret_cast<uint4 *>(&tile[(2 * pair + h) * kOut + 4 * rb]) = make_uint4(q[h][0], q[h][1], q[h][2], q[h][3]);
+    unsigned char *out = reinterpret_cast<unsigned char *>(tile + kTile * kPitch);
+    constexpr int kSide = kPitch;  // words of a row
+    quantize_cols<T>(tile, tid % kSide, tid / kSide, out, kOutPitch, reinterpret_cast<unsigned char *>(scale_words[1]));
     __syncthreads();
-    const size_t pitch_t = (size_t)a.tiles_r * (kTile / 2);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int c = k * 64 + (tid >> 2), part = tid & 3;
+    for (int k = 0; k < 4 * kTile / kThreads; ++k) {
+        const int c = (k * kThreads + tid) >> 2, part = tid & 3;
         if (c0 + c < a.cols)
             *reinterpret_cast<uint4 *>(a.codes_t + (size_t)(c0 + c) * pitch_t + r0 / 2 + 16 * part) =
-                *reinterpret_cast<const uint4 *>(&tile[c * kOut + 4 * part]);
+                *reinterpret_cast<const uint4 *>(out + c * kOutPitch + 16 * part);
     }
     if (tid < 32)
         *reinterpret_cast<uint4 *>(a.scales_t + ((size_t)tc * a.tiles_r + tr) * kScaleTile + 16 * tid) =
             *reinterpret_cast<const uint4 *>(&scale_words[1][4 * tid]);
+}
+
+// The same with whole tiles brought by TMA (rows at 16-byte boundaries), persistent: while a tile
+// is quantised the next ones are on their way, so that HBM does not wait for arithmetic.  Both
+// forms are taken from shared memory.
+template <typename T>
+struct QuantRing {
+    static constexpr int kThreads = sizeof(T) == 4 ? 512 : 256;
+    static constexpr int kCtas = sizeof(T) == 4 ? 1 : 2;  // an SM
+    static constexpr int kStages = 3;
+    static constexpr int kTileBytes = kTile * kTile * (int)sizeof(T);
+    static constexpr int kOut = kOutPitch;
+    static constexpr int kSmem = kStages * kTileBytes + kTile * kOut + 2 * kScaleTile + 128;
+    static_assert(kCtas * (kSmem + 1024) <= 228 * 1024, "shared memory");
+};
+
+template <typename T, bool Rows, bool Cols>
+__global__ void __launch_bounds__(QuantRing<T>::kThreads, QuantRing<T>::kCtas)
+    k_quantize_tiles(const __grid_constant__ CUtensorMap map, const QuantArgs a) {
+    using R = QuantRing<T>;
+    constexpr int kWords = sizeof(T) * 2;          // of eight elements
+    constexpr int kPitch = kTile * sizeof(T) / 4;  // words of a tile's row
+    extern __shared__ __align__(16) unsigned tile[];
+    __shared__ __align__(8) unsigned long long bars[R::kStages];
+    __shared__ volatile int dead;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    unsigned char *base = reinterpret_cast<unsigned char *>(tile) + (-smem_addr(tile) & 127u);
+    unsigned char *out = base + R::kStages * R::kTileBytes;
+    unsigned *scale_r = reinterpret_cast<unsigned *>(out + kTile * R::kOut);
+    unsigned char *scale_c = reinterpret_cast<unsigned char *>(scale_r + kTile);
+    const uint32_t full = smem_addr(bars);
+    const int n_tiles = a.tiles_r * a.tiles_c;
+    if (tid == 0) {
+        for (int s = 0; s < R::kStages; ++s) mbar_init(full + 8 * s, 1);
+        dead = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    let_next_start();
+    wait_for_previous();
+    auto fetch = [&](int t, int s) {
+        mbar_expect(full + 8 * s, R::kTileBytes);
+        tma_load_2d(smem_addr(base) + s * R::kTileBytes, &map, t % a.tiles_c * kTile, t / a.tiles_c * kTile, full + 8 * s);
+    };
+    int fetched = 0;  // thread 0
+    if (tid == 0)
+        for (; fetched < R::kStages && blockIdx.x + fetched * gridDim.x < n_tiles; ++fetched)
+            fetch(blockIdx.x + fetched * gridDim.x, fetched);
+    const size_t pitch = (size_t)a.tiles_c * (kTile / 2), pitch_t = (size_t)a.tiles_r * (kTile / 2);
+    int i = 0;
+    for (int t = blockIdx.x; t < n_tiles; t += gridDim.x, ++i) {
+        const int s = i % R::kStages;
+        const bool ok = mbar_wait(full + 8 * s, (i / R::kStages) & 1, &dead);
+        if (!__syncthreads_and(ok)) break;  // and the last tile's codes have been read
+        const unsigned *x_tile = reinterpret_cast<const unsigned *>(base + s * R::kTileBytes);
+        const int tr = t / a.tiles_c, tc = t % a.tiles_c;
+        const long long r0 = (long long)tr * kTile, c0 = (long long)tc * kTile;
+        if (Rows) {
+            const int sub = lane & 15;
+            constexpr int kRows = kTile / (R::kThreads / 32);  // of a warp
+#pragma unroll
+            for (int k = 0; k < kRows / 2; ++k) {
+                const int row = warp * kRows + 2 * k + (lane >> 4);
+                unsigned w[kWords], scales;
+#pragma unroll
+                for (int j = 0; j < kWords / 4; ++j) {
+                    const uint4 q = *reinterpret_cast<const uint4 *>(&x_tile[row * kPitch + sub * kWords + 4 * j]);
+                    w[4 * j] = q.x, w[4 * j + 1] = q.y, w[4 * j + 2] = q.z, w[4 * j + 3] = q.w;
+                }
+                const unsigned q = quantize_row8<T>(w, sub, scales);
+                if (r0 + row < a.rows)
+                    *reinterpret_cast<unsigned *>(a.codes + (size_t)(r0 + row) * pitch + c0 / 2 + 4 * sub) = q;
+                if (sub == 0) scale_r[(row & 31) * 4 + (row >> 5)] = scales;
+            }
+        }
+        if (Cols) quantize_cols<T>(x_tile, tid % kPitch, tid / kPitch, out, R::kOut, scale_c);
+        __syncthreads();  // the tile has been read, its codes and scales are there
+        if (tid == 0 && blockIdx.x + fetched * gridDim.x < n_tiles) {
+            fetch(blockIdx.x + fetched * gridDim.x, s);
+            ++fetched;
+        }
+        if (Cols) {
+#pragma unroll
+            for (int k = 0; k < 4 * kTile / R::kThreads; ++k) {
+                const int c = (k * R::kThreads + tid) >> 2, part = tid & 3;
+                if (c0 + c < a.cols)
+                    *reinterpret_cast<uint4 *>(a.codes_t + (size_t)(c0 + c) * pitch_t + r0 / 2 + 16 * part) =
+                        *reinterpret_cast<const uint4 *>(out + c * R::kOut + 16 * part);
+            }
+            if (tid < 32)
+                *reinterpret_cast<uint4 *>(a.scales_t + ((size_t)tc * a.tiles_r + tr) * kScaleTile + 16 * tid) =
+                    *reinterpret_cast<const uint4 *>(scale_c + 16 * tid);
+        }
+        if (Rows && tid >= 32 && tid < 64)
+            *reinterpret_cast<uint4 *>(a.scales + ((size_t)tr * a.tiles_c + tc) * kScaleTile + 16 * lane) =
+                *reinterpret_cast<const uint4 *>(&scale_r[4 * lane]);
+    }
+    // no copy may be in flight when the CTA ends
+    if (tid == 0)
+        for (; i < fetched; ++i)
+            for (uint32_t w = 0; w < kSpinLimit && !mbar_try(full + 8 * (i % R::kStages), (i / R::kStages) & 1); ++w) {}
 }
 
 // ----------------------------------------------------------------------------
@@ -260,35 +484,81 @@ __device__ __forceinline__ void put(float *p, float v) { *p = v; }
 __device__ __forceinline__ void put(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void put(__half *p, float v) { *p = __float2half_rn(v); }
 
-// Eight values from column 8 * (index % row_groups) of a row, a thread each.
-template <typename T, bool Vec>
-__global__ void __launch_bounds__(256) k_dequantize(const unsigned char *codes, const unsigned char *scales,
-                                                    long long rows, long long cols, long long groups, T *out) {
+// Eight elements to a boundary of as many bytes.
+template <typename T>
+__device__ __forceinline__ void store_run(T *to, const T (&y)[8]) {
+    const unsigned *q = reinterpret_cast<const unsigned *>(y);
+    constexpr int kHalf = sizeof(T) == 4 ? 4 : 0;  // words of four elements
+    if (sizeof(T) == 2)
+        __stcs(reinterpret_cast<uint4 *>(to), make_uint4(q[0], q[1], q[2], q[3]));
+    else
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(q[0]), "r"(q[1]), "r"(q[2]),
+                     "r"(q[3]), "r"(q[kHalf]), "r"(q[kHalf + 1]), "r"(q[kHalf + 2]), "r"(q[kHalf + 3])
+                     : "memory");
+}
+
+struct DequantArgs {
+    const unsigned char *codes, *scales;
+    long long n, cols;  // elements, columns
+    int tiles_c, lead;  // lead: elements from the boundary below out to out
+    unsigned long long magic;  // ceil(2^64 / cols), or 0 where the division by it would not be exact
+};
+__device__ __forceinline__ unsigned scale_at(const DequantArgs &a, long long r, long long c) {
+    return a.scales[((size_t)(r / kTile) * a.tiles_c + c / kTile) * kScaleTile + (r & 31) * 16 + (r & 127) / 32 * 4 +
+                    (c & 127) / kBlock];
+}
+
+// Out is one run of elements: a thread writes the eight between two boundaries of as many bytes,
+// whatever rows they belong to, and takes their codes from where they lie.  Easy: rows start at
+// multiples of eight; then four such groups a thread for 16-bit types (17 us for 8192 x 4096 to
+// bf16, 20 with one), elsewhere one (fp32: 31 us, 33 with four; odd sizes: 30 and 39).
+template <typename T, bool Easy>
+constexpr int kGroupsOf = Easy && sizeof(T) == 2 ? 4 : 1;
+template <typename T, bool Easy>
+__global__ void __launch_bounds__(256) k_dequantize(const DequantArgs a, T *out) {
+    constexpr int kGroups = kGroupsOf<T, Easy>;
     let_next_start();
     wait_for_previous();
-    const long long n = rows * groups, tiles_c = (cols + kTile - 1) / kTile;
-    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
-        const long long r = i / groups, c = 8 * (i % groups);
-        const unsigned q = __ldcs(reinterpret_cast<const unsigned *>(codes + (size_t)r * tiles_c * (kTile / 2) + c / 2));
-        const unsigned s = scales[((size_t)(r / kTile) * tiles_c + c / kTile) * kScaleTile + (r & 31) * 16 +
-                                  (r & 127) / 32 * 4 + (c & 127) / kBlock];
-        const float f = scale_value(s);
-        __align__(16) T y[8];
+    long long f[kGroups], r[kGroups], c[kGroups];
+    unsigned q[kGroups], s0[kGroups], s1[kGroups];
+    bool whole[kGroups];  // eight elements of one row
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float2 v = code_pair(q >> (8 * k) & 0xffu);
-            put(&y[2 * k], __fmul_rn(v.x, f));
-            put(&y[2 * k + 1], __fmul_rn(v.y, f));
+    for (int j = 0; j < kGroups; ++j) {
+        f[j] = 8 * ((long long)blockIdx.x * (256 * kGroups) + 256 * j + threadIdx.x) - (Easy ? 0 : a.lead);
+        const long long at = max(f[j], 0ll);
+        r[j] = a.magic ? (long long)__umul64hi((unsigned long long)at, a.magic) : at / a.cols;
+        c[j] = at - r[j] * a.cols;
+        whole[j] = f[j] >= 0 && f[j] + 8 <= a.n && c[j] + 8 <= a.cols;
+        if (!whole[j]) continue;
+        const unsigned *w = reinterpret_cast<const unsigned *>(a.codes + (size_t)r[j] * a.tiles_c * (kTile / 2)) + c[j] / 8;
+        q[j] = __ldcs(w);
+        s0[j] = scale_at(a, r[j], c[j]);
+        if (!Easy) {
+            const int in = (int)(c[j] & 7);
+            if (in) q[j] = __funnelshift_r(q[j], __ldcs(w + 1), 4 * in);
+            s1[j] = scale_at(a, r[j], c[j] + 7);
         }
-        T *p = out + r * cols + c;
-        if (Vec) {
+    }
 #pragma unroll
-            for (int k = 0; k < (int)sizeof(T) / 2; ++k)
-                __stcs(reinterpret_cast<uint4 *>(p) + k, reinterpret_cast<const uint4 *>(y)[k]);
-        } else {
+    for (int j = 0; j < kGroups; ++j) {
+        if (whole[j]) {
+            const float f0 = scale_value(s0[j]), f1 = Easy ? f0 : scale_value(s1[j]);
+            const int in = (int)(c[j] & 31);
+            __align__(16) T y[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (c + k < cols) p[k] = y[k];
+            for (int k = 0; k < 4; ++k) {
+                const float2 v = code_pair(q[j] >> (8 * k) & 0xffu);
+                put(&y[2 * k], __fmul_rn(v.x, Easy || in + 2 * k < 32 ? f0 : f1));
+                put(&y[2 * k + 1], __fmul_rn(v.y, Easy || in + 2 * k + 1 < 32 ? f0 : f1));
+            }
+            store_run(out + f[j], y);
+        } else if (!Easy) {
+            long long row = r[j], col = c[j];
+            for (long long e = max(f[j], 0ll); e < min(f[j] + 8, a.n); ++e) {
+                const unsigned byte = a.codes[(size_t)row * a.tiles_c * (kTile / 2) + col / 2];
+                put(out + e, __fmul_rn(code_pair(col & 1 ? byte >> 4 : byte & 15u).x, scale_value(scale_at(a, row, col))));
+                if (++col == a.cols) ++row, col = 0;
+            }
         }
     }
 }
@@ -303,51 +573,7 @@ __global__ void __launch_bounds__(256) k_dequantize(const unsigned char *codes, 
 // two scales a row); accumulators lie in tensor memory and four warps read them back.
 
 constexpr int kStageK = 256;
-constexpr uint32_t kSpinLimit = 1u << 19;  // bound on every wait (~2 s)
-constexpr int kMmaThreads = 192;           // a copying warp, an issuing warp, four that read back
-
-static __device__ unsigned g_mx_error;
-
-__device__ __forceinline__ uint32_t smem_addr(const void *p) {
-    return (uint32_t)__cvta_generic_to_shared(p);
-}
-__device__ __forceinline__ void mbar_init(uint32_t bar, unsigned count) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_expect(uint32_t bar, unsigned bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool mbar_try(uint32_t bar, unsigned parity) {
-    unsigned ok;
-    asm volatile("{\n.reg .pred p;\n"
-                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
-                 "selp.u32 %0, 1, 0, p;\n}\n"
-                 : "=r"(ok)
-                 : "r"(bar), "r"(parity)
-                 : "memory");
-    return ok != 0;
-}
-// False if the wait ran out, here or before in another warp (`dead`).
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, unsigned parity, volatile int *dead) {
-    for (uint32_t i = 0; i < kSpinLimit; ++i) {
-        if (mbar_try(bar, parity)) return true;
-        if (*dead) return false;
-    }
-    *dead = 1;
-    atomicOr(&g_mx_error, 1u);
-    return false;
-}
-
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-                 "l"(map), "r"(x), "r"(y), "r"(bar)
-                 : "memory");
-}
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, unsigned bytes, uint32_t bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
-                 "l"(src), "r"(bytes), "r"(bar)
-                 : "memory");
-}
+constexpr int kMmaThreads = 192;  // a copying warp, an issuing warp, four that read back
 
 // Shared-memory matrix descriptors: addresses in units of 16 bytes; bit 46: their version.
 // Codes: rows of 128 bytes with the 128-byte swizzle, groups of eight rows 1024 bytes apart.
@@ -947,37 +1173,6 @@ int allow_smem(const void *kernel, int smem, std::atomic<uint64_t> *done) {
     return e == cudaSuccess ? TULA_OK : cuda_failed(e);
 }
 
-template <typename T, int VB>
-int launch_quantize(const QuantArgs &a, unsigned grid, cudaStream_t s) {
-    static std::atomic<uint64_t> done[3];
-    const int which = a.codes && a.codes_t ? 0 : a.codes ? 1 : 2;
-    void (*k)(const QuantArgs) = which == 0   ? k_quantize<T, VB, true, true>
-                                 : which == 1 ? k_quantize<T, VB, true, false>
-                                              : k_quantize<T, VB, false, true>;
-    const int smem = a.codes_t ? kTile * kTile * (int)sizeof(T) : 0;
-    const int rc = allow_smem((const void *)k, smem, &done[which]);
-    if (rc) return rc;
-    return tula::launch(k, dim3(grid), 256, smem, s, 1, a);
-}
-template <typename T>
-int quantize_typed(const QuantArgs &a, unsigned grid, cudaStream_t s) {
-    const size_t both = reinterpret_cast<uintptr_t>(a.x) | (a.rows > 1 ? (size_t)a.stride * sizeof(T) : 0);
-    if (both % 16 == 0) return launch_quantize<T, 16>(a, grid, s);
-    if (both % 8 == 0) return launch_quantize<T, 8>(a, grid, s);
-    if (both % 4 == 0) return launch_quantize<T, 4>(a, grid, s);
-    return launch_quantize<T, 2>(a, grid, s);
-}
-
-template <typename T>
-int dequantize_typed(const void *codes, const void *scales, long long rows, long long cols, void *out, cudaStream_t s) {
-    const long long groups = up(cols, 8);
-    const bool vec = aligned(out, 16) && cols * (long long)sizeof(T) % 16 == 0 && cols % 8 == 0;
-    const long long blocks = std::min<long long>(up(rows * groups, 256), 152 * 64);
-    return tula::launch(vec ? k_dequantize<T, true> : k_dequantize<T, false>, dim3((unsigned)blocks), 256, 0, s, 1,
-                        static_cast<const unsigned char *>(codes), static_cast<const unsigned char *>(scales), rows, cols,
-                        groups, static_cast<T *>(out));
-}
-
 typedef CUresult (*EncodeFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                              const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -1017,6 +1212,70 @@ int sm_count() {
     int dev = 0, n = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
     return n;
+}
+
+template <typename T, bool Aligned>
+int launch_quantize(const QuantArgs &a, unsigned grid, cudaStream_t s) {
+    static std::atomic<uint64_t> done[3];
+    const int which = a.codes && a.codes_t ? 0 : a.codes ? 1 : 2;
+    void (*k)(const QuantArgs) = which == 0   ? k_quantize<T, Aligned, true, true>
+                                 : which == 1 ? k_quantize<T, Aligned, true, false>
+                                              : k_quantize<T, Aligned, false, true>;
+    const int smem = a.codes_t ? QuantShape<T>::kSmem : 0;
+    const int rc = allow_smem((const void *)k, smem, &done[which]);
+    if (rc) return rc;
+    return tula::launch(k, dim3(grid), QuantShape<T>::kThreads, smem, s, 1, a);
+}
+template <typename T>
+int launch_quantize_tiles(const QuantArgs &a, unsigned tiles, cudaStream_t s) {
+    using R = QuantRing<T>;
+    static std::atomic<uint64_t> done[3];
+    const int which = a.codes && a.codes_t ? 0 : a.codes ? 1 : 2;
+    void (*k)(const CUtensorMap, const QuantArgs) = which == 0   ? k_quantize_tiles<T, true, true>
+                                                    : which == 1 ? k_quantize_tiles<T, true, false>
+                                                                 : k_quantize_tiles<T, false, true>;
+    const int rc = allow_smem((const void *)k, R::kSmem, &done[which]);
+    if (rc) return rc;
+    CUtensorMap map;
+    const CUtensorMapDataType type = sizeof(T) == 4 ? CU_TENSOR_MAP_DATA_TYPE_UINT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16;
+    // (an only row's stride is any number)
+    const long long row_bytes = (a.rows > 1 ? a.stride : up(a.cols, 8) * 8) * (long long)sizeof(T);
+    if (!make_map(&map, type, a.x, a.rows, a.cols, row_bytes, kTile, kTile, CU_TENSOR_MAP_SWIZZLE_NONE))
+        return cuda_failed(cudaErrorInvalidValue);
+    const unsigned ctas = (unsigned)std::max(1, R::kCtas * sm_count());
+    return tula::launch(k, dim3(std::min(tiles, ctas)), R::kThreads, R::kSmem, s, 1, map, a);
+}
+
+template <typename T>
+int quantize_typed(const QuantArgs &a, unsigned grid, cudaStream_t s) {
+    const size_t both = reinterpret_cast<uintptr_t>(a.x) | (a.rows > 1 ? (size_t)a.stride * sizeof(T) : 0);
+    // Tiles by TMA once every CTA that fits takes two at least (with fewer, one tile a CTA has all of
+    // them in flight at once), for fp32's transpose and the transpose of 16-bit types alone: 8192 x
+    // 4096 fp32 takes 32 us in both forms (36 without), bf16 15 us transposed (17).  Forms along the
+    // rows want the warps that the rings leave no room for: bf16 24 us in both forms, 28 by TMA.
+    const bool by_tma = a.codes_t && (sizeof(T) == 4 || !a.codes);
+    if (both % 16 == 0 && by_tma && (long long)grid >= 2ll * QuantRing<T>::kCtas * sm_count() && a.cols <= 0x7fffff00ll &&
+        a.rows <= 0x7fffff00ll)
+        return launch_quantize_tiles<T>(a, grid, s);
+    return both % 16 == 0 ? launch_quantize<T, true>(a, grid, s) : launch_quantize<T, false>(a, grid, s);
+}
+
+template <typename T>
+int dequantize_typed(const void *codes, const void *scales, long long rows, long long cols, void *out, cudaStream_t s) {
+    DequantArgs a;
+    a.codes = static_cast<const unsigned char *>(codes);
+    a.scales = static_cast<const unsigned char *>(scales);
+    a.n = rows * cols;
+    a.cols = cols;
+    a.tiles_c = (int)up(cols, kTile);
+    a.lead = (int)(reinterpret_cast<uintptr_t>(out) % (8 * sizeof(T)) / sizeof(T));
+    // floor(f / cols) = floor(f m / 2^64) while f (m cols - 2^64) < 2^64, that is f < 2^64 / cols
+    a.magic = cols > 1 && (unsigned long long)a.n < ~0ull / (unsigned long long)cols ? ~0ull / (unsigned long long)cols + 1 : 0;
+    const bool easy = cols % 8 == 0 && a.lead == 0;
+    const long long blocks = up(a.n + a.lead, 8 * 256 * (easy ? kGroupsOf<T, true> : kGroupsOf<T, false>));
+    if (blocks >= (1LL << 31)) return TULA_ERR_ARG;
+    return tula::launch(easy ? k_dequantize<T, true> : k_dequantize<T, false>, dim3((unsigned)blocks), 256,
+                        0, s, 1, a, static_cast<T *>(out));
 }
 
 template <int NT, bool Swap, typename T>

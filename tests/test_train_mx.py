@@ -201,6 +201,47 @@ def test_zeros_denormals_infinities_and_nans():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols,stride", [(3000, 4101, 4104), (5000, 2500, 2504), (1, 100000, 100000), (129, 80000, 80000)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_large_matrices_equal_their_slabs(rows, cols, stride, dtype):
+    """Large matrices go another way than small ones: each slab of 128 rows has to come out as by
+    itself, and is checked against the definition in one place."""
+    x = _matrix(rows, cols, dtype, 50, stride)
+    x[rows // 2, cols // 3] = math.nan
+    q, t = mx.quantize(x, cols=True)
+    only_q, only_t = mx.quantize(x), mx.quantize(x, rows=False, cols=True)
+    assert torch.equal(q.codes, only_q.codes) and torch.equal(q.scales, only_q.scales)
+    assert torch.equal(t.codes, only_t.codes) and torch.equal(t.scales, only_t.scales)
+    for k in range(-(-rows // 128)):
+        a, b = 128 * k, min(rows, 128 * k + 128)
+        sq, st = mx.quantize(x[a:b], cols=True)
+        assert torch.equal(sq.codes, q.codes[a:b]) and torch.equal(sq.scales[0], q.scales[k])
+        assert torch.equal(st.codes, t.codes[:, 64 * k:64 * k + 64]) and torch.equal(st.scales[:, 0], t.scales[:, k])
+    a = 128 * (rows // 256)
+    part = x[a:a + 128, :3000]
+    code, s = quantised64(part)
+    c, r = unpacked(mx.quantize(part))
+    assert torch.equal(c, code) and torch.equal(r, s)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols", [(3, 5), (40, 33), (300, 1001), (7, 4096), (1000, 130)])
+@pytest.mark.parametrize("kind", [0, 1, 2])
+@pytest.mark.parametrize("off", [0, 1, 3])
+def test_dequantize_into_any_alignment(rows, cols, kind, off):
+    """The C call writes the matrix and nothing beside it, wherever out starts."""
+    dtype = [torch.float32, torch.bfloat16, torch.float16][kind]
+    q = mx.quantize(_matrix(rows, cols, torch.float32, 51))
+    room = torch.full((rows * cols + 64,), 7.0, dtype=dtype, device="cuda")
+    out = room[16 + off:16 + off + rows * cols]
+    rc = mx._lib().tula_mx_dequantize(q.codes.data_ptr(), q.scales.data_ptr(), rows, cols, out.data_ptr(), kind,
+                                      torch.cuda.current_stream().cuda_stream)
+    assert rc == 0
+    assert torch.equal(out.view(rows, cols).cpu(), values64(*unpacked(q)).to(dtype))
+    assert bool((room[:16 + off] == 7).all()) and bool((room[16 + off + rows * cols:] == 7).all())
+
+
+@pytest.mark.gpu
 def test_empty_matrices_and_odd_layouts():
     for shape in ((0, 5), (5, 0), (0, 0)):
         q, t = mx.quantize(torch.zeros(shape, device="cuda"), cols=True)
