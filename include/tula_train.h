@@ -29,9 +29,9 @@ extern "C" {
 
 /* A list of tensors.  The arrays are HOST arrays of n_tensors entries, read by
  * tula_train_plan_create only; what they point to is device memory, aligned to its element.
- * Tensors whose buffers lie alike within 16 bytes (all at a 16-byte boundary, or views at one
- * element offset into flat buffers that start at such boundaries) move in 16-byte accesses, others
- * element by element. */
+ * Tensors whose buffers start alike within eight elements (all at a boundary of eight, or views at
+ * one element offset into flat buffers that start at such boundaries) move eight elements at a
+ * time, others one by one. */
 typedef struct tula_train_tensors {
     int n_tensors;
     const int64_t *numels;             /* >= 0 (0 = skipped) */
@@ -44,8 +44,8 @@ typedef struct tula_train_tensors {
     const int *copy_types;             /* TULA_TYPE_BF16 or TULA_TYPE_F16; NULL: all bf16 */
 } tula_train_tensors;
 
-/* Bytes of device workspace a plan over these sizes needs (host only): 64 per tensor, and 8 to 16
- * per 2048 elements (small lists) or 8192. */
+/* Bytes of device workspace a plan over these sizes needs (host only): 64 to 72 per tile of 2048
+ * elements (up to about 2.5 M elements in all) or 8192, and for what is left of each tensor. */
 int tula_train_workspace_size(const int64_t *numels, int n_tensors, size_t *bytes);
 
 /*
