@@ -123,6 +123,20 @@ struct Raw {
             w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
         }
     }
+    __device__ __forceinline__ unsigned bits() const {  // or'd, with a 16-bit type's in the upper half
+        unsigned b = (w[0] | w[1]) | (w[2] | w[3]);
+        if (kWide) b |= (w[kWide ? 4 : 0] | w[kWide ? 5 : 0]) | (w[kWide ? 6 : 0] | w[kWide ? 7 : 0]);
+        return kWide ? b : b | b << 16;
+    }
+    // element k from index i, or 0
+    __device__ __forceinline__ void set(int k, unsigned long long base, int i, bool there) {
+        if (kWide) {
+            w[k & (kWide ? 7 : 3)] = there ? __ldcg(reinterpret_cast<const unsigned *>(base) + i) : 0u;
+        } else {
+            const unsigned u = there ? __ldcg(reinterpret_cast<const unsigned short *>(base) + i) : 0u;
+            w[k / 2 & 3] = k & 1 ? w[k / 2 & 3] | u << 16 : u;
+        }
+    }
     __device__ __forceinline__ void floats(float (&x)[kVec]) const {
         if (kWide) {
 #pragma unroll
@@ -184,30 +198,41 @@ __device__ __forceinline__ void store1(float x, unsigned long long base, int typ
 // The norm
 // ----------------------------------------------------------------------------
 
-// A thread's sum of squares as it stands where every square and sum is safe in fp32; else 0 with
-// the sum in `d`, its elements scaled by an exact power of two first.  A sum in [2^-100, 2^120]
-// is safe: nothing overflowed, and what underflowed is below 2^-40 of it.  Below, every element is
-// under 2^-50 and is squared times 2^100; above (inf and NaN too), times 2^-72.
-template <int N>
-__device__ __forceinline__ float safe_square_sum(const float (&x)[N], double &d) {
+// A thread's sum of squares of N vectors; `bits`: the elements' bits, or'd.
+template <int N, int Type>
+__device__ __forceinline__ float square_sum(const Raw<Type> (&raw)[N], unsigned &bits) {
     float c[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int k = 0; k < N; ++k) c[k & 3] = __fmaf_rn(x[k], x[k], c[k & 3]);
-    const float s = __fadd_rn(__fadd_rn(c[0], c[1]), __fadd_rn(c[2], c[3]));
-    d = 0.0;
-    if (s >= 0x1p-100f && s <= 0x1p120f) return s;
-    const float f = s < 0x1p-100f ? 0x1p100f : 0x1p-72f;
-    float r = 0.f;
+    for (int j = 0; j < N; ++j) {
+        float x[kVec];
+        raw[j].floats(x);
+        bits |= raw[j].bits();
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
+        for (int k = 0; k < kVec; ++k) c[k & 3] = __fmaf_rn(x[k], x[k], c[k & 3]);
+    }
+    return __fadd_rn(__fadd_rn(c[0], c[1]), __fadd_rn(c[2], c[3]));
+}
+// Whether it is safe as it stands: in [2^-100, 2^120] nothing overflowed, and what underflowed is
+// below 2^-40 of it; so is a sum of zeros.
+__device__ __forceinline__ bool safe(float s, unsigned bits) {
+    return (s >= 0x1p-100f && s <= 0x1p120f) || (bits << 1) == 0;
+}
+// Else the elements are squared again, scaled by an exact power of two: below, every element is under
+// 2^-50 and is taken times 2^100; above (inf and NaN too), times 2^-72.
+template <int Type>
+__device__ double scaled_sum(const Raw<Type> &raw, float s) {
+    const float f = s < 0x1p-100f ? 0x1p100f : 0x1p-72f;
+    float x[kVec], r = 0.f;
+    raw.floats(x);
+#pragma unroll
+    for (int k = 0; k < kVec; ++k) {
         const float y = __fmul_rn(x[k], f);
         r = __fmaf_rn(y, y, r);
     }
-    if (r != 0.f) d = (double)r * (s < 0x1p-100f ? 0x1p-200 : 0x1p144);
-    return 0.f;
+    return (double)r * (s < 0x1p-100f ? 0x1p-200 : 0x1p144);
 }
 
-// A warp's sum, in lane 0.  fp32 lane sums of at most 2^122 add to at most 2^127; the
+// A warp's sum, in lane 0.  fp32 lane sums of at most 2^120 add to at most 2^125; the
 // fp64 part is there in the rare warps that have one.
 __device__ __forceinline__ double warp_sum(float s, double d) {
 #pragma unroll
@@ -283,46 +308,50 @@ __device__ __forceinline__ double sum_fan(const double *p, int n) {
     return v[0];
 }
 
-// One warp's sum over a tile, in lane 0.
+// Vector j of a thread's of a tile, elements that are not the tensor's as 0.
+template <int Type>
+__device__ __forceinline__ void load_part(Raw<Type> &raw, const Row &row, int j) {
+    const int tid = threadIdx.x, i = (j * kThreads + tid) * kVec;
+    if (row.vec && i >= row.lo && i + kVec <= row.hi) {
+        raw.template load<false>(row.g, i);
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < kVec; ++k) {
+        const int e = row.vec ? i + k : (j * kVec + k) * kThreads + tid;
+        raw.set(k, row.g, e, e >= row.lo && e < row.hi);
+    }
+}
+
+// One warp's sum over a tile, in lane 0.  Nothing but a sum stays of the elements, so that registers
+// leave room for eight CTAs an SM; where it is not safe they are loaded again.
 template <int VPT, int Type>
 __device__ __forceinline__ double tile_sum(const Row &row) {
     const int tid = threadIdx.x;
-    const unsigned long long g = row.g;
+    float s = 0.f;
+    unsigned bits = 0;
     if (row.vec && row.lo == 0 && row.hi == VPT * kThreads * kVec) {
-        float x[VPT * kVec];
         Raw<Type> raw[VPT];
 #pragma unroll
-        for (int j = 0; j < VPT; ++j) raw[j].template load<false>(g, (j * kThreads + tid) * kVec);
-#pragma unroll
-        for (int j = 0; j < VPT; ++j) raw[j].floats(*reinterpret_cast<float(*)[kVec]>(&x[j * kVec]));
-        double d;
-        const float s = safe_square_sum(x, d);
-        return warp_sum(s, d);
-    }
-    // (rolled: unrolled, its registers left room for two CTAs an SM, and whole tiles took twice as long)
-    float s = 0.f;
-    double d = 0.0;
+        for (int j = 0; j < VPT; ++j) raw[j].template load<false>(row.g, (j * kThreads + tid) * kVec);
+        s = square_sum(raw, bits);
+    } else {
 #pragma unroll 1
-    for (int j = 0; j < VPT; ++j) {
-        const int i = (j * kThreads + tid) * kVec;
-        float x[kVec];
-        if (row.vec && i >= row.lo && i + kVec <= row.hi) {
-            Raw<Type> raw;
-            raw.template load<false>(g, i);
-            raw.floats(x);
-        } else if (row.vec) {
-#pragma unroll
-            for (int k = 0; k < kVec; ++k) x[k] = i + k >= row.lo && i + k < row.hi ? load1(g, Type, i + k) : 0.f;
-        } else {
-#pragma unroll
-            for (int k = 0; k < kVec; ++k) {
-                const int e = (j * kVec + k) * kThreads + tid;
-                x[k] = e < row.hi ? load1(g, Type, e) : 0.f;
-            }
+        for (int j = 0; j < VPT; ++j) {
+            Raw<Type> raw[1];
+            load_part(raw[0], row, j);
+            s = __fadd_rn(s, square_sum(raw, bits));
         }
-        double more;
-        s = __fadd_rn(s, safe_square_sum(x, more));
-        d += more;
+    }
+    double d = 0.0;
+    if (!safe(s, bits)) {
+#pragma unroll 1
+        for (int j = 0; j < VPT; ++j) {
+            Raw<Type> raw;
+            load_part(raw, row, j);
+            d += scaled_sum(raw, s);
+        }
+        s = 0.f;
     }
     return warp_sum(s, d);
 }
@@ -337,7 +366,7 @@ __device__ __forceinline__ void fetch_rows(Row (&rows)[kMaxGroup], const Tables 
 }
 
 template <int VPT>
-__global__ void __launch_bounds__(kThreads) k_norm(const Tables tb, const NormArgs a) {
+__global__ void __launch_bounds__(kThreads, 8) k_norm(const Tables tb, const NormArgs a) {
     __shared__ double sums[kThreads / 32];
     __shared__ __align__(16) Row rows[kMaxGroup];
     let_next_start();
