@@ -18,20 +18,20 @@ from .optim import TYPES
 from .tula_ags import _check, _stream_ptr, c_int, c_size_t, c_void_p, lib
 
 _i64 = ctypes.c_int64
-_typed = None
+_fns = None  # the library's functions, their types declared
 
 
 def _lib():
-    global _typed
-    if _typed is None:
+    global _fns
+    if _fns is None:
         L = lib()
         L.tula_mx_size.argtypes = [_i64, _i64, ctypes.POINTER(c_size_t), ctypes.POINTER(c_size_t)]
         L.tula_mx_quantize.argtypes = [c_void_p, c_int, _i64, _i64, _i64] + [c_void_p] * 5
         L.tula_mx_dequantize.argtypes = [c_void_p, c_void_p, _i64, _i64, c_void_p, c_int, c_void_p]
         L.tula_mx_matmul.argtypes = [c_void_p] * 4 + [_i64] * 3 + [c_void_p, c_int, c_void_p]
         L.tula_mx_error.argtypes = [c_void_p, ctypes.POINTER(c_int)]
-        _typed = L
-    return _typed
+        _fns = L
+    return _fns
 
 
 class MXMatrix:
@@ -39,7 +39,7 @@ class MXMatrix:
     [ceil(rows / 128), P / 128, 32, 4, 4], P = cols rounded up to a multiple of 128; of any shapes
     of those sizes, contiguous, on one GPU.  Not to be changed once made."""
 
-    __slots__ = ("rows", "cols", "dev", "code_ptr", "scale_ptr", "_codes", "_scales", "_buffer")
+    __slots__ = ("rows", "cols", "device", "dev", "code_ptr", "scale_ptr", "_codes", "_scales", "_buffer")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int):
         tiles = (cols + 127) // 128
@@ -48,18 +48,18 @@ class MXMatrix:
                 or scales.numel() != (rows + 127) // 128 * tiles * 512):
             raise ValueError(f"not the codes and scales of a {rows} x {cols} matrix")
         self.rows, self.cols, self._codes, self._scales = rows, cols, codes, scales
-        self.dev = _on_gpu(codes, scales)
+        self.dev, self.device = _on_gpu(codes, scales), codes.device
         self.code_ptr, self.scale_ptr = codes.data_ptr(), scales.data_ptr()
 
     @classmethod
-    def empty(cls, rows: int, cols: int, device) -> "MXMatrix":
+    def empty(cls, rows: int, cols: int, device: torch.device) -> "MXMatrix":
         """One to quantise into, in one allocation."""
         self = cls.__new__(cls)
         tiles = (cols + 127) // 128
         n = (rows + 127) // 128 * tiles * 512
         buf = torch.empty(n + rows * tiles * 64, dtype=torch.uint8, device=device)
         self.rows, self.cols, self._buffer, self._codes, self._scales = rows, cols, buf, None, None
-        self.dev, self.scale_ptr = buf.get_device(), buf.data_ptr()
+        self.dev, self.device, self.scale_ptr = device.index, device, buf.data_ptr()
         self.code_ptr = self.scale_ptr + n
         return self
 
@@ -96,21 +96,22 @@ def _on_gpu(*tensors):
     """The index of the one GPU that the tensors are on."""
     dev = tensors[0].get_device()
     for t in tensors:
-        if not t.is_cuda or t.get_device() != dev:
+        if t.get_device() != dev or dev < 0:
             raise TypeError(f"tensors on one GPU are wanted, got {[str(t.device) for t in tensors]}")
     return dev
 
 
-def _call(where, dev, fn, *args):
-    """fn(*args, current stream) with the tensors' GPU current; switching to it costs some
-    microseconds, so only where it is not."""
+def _call(name, dev, *args):
+    """The library's `name` with these arguments and the current stream, with the tensors' GPU
+    current; switching to it costs some microseconds, so only where it is not."""
+    fn = getattr(_fns or _lib(), name)
     if dev == _get_device():
         rc = fn(*args, _raw_stream(dev))
     else:
         with torch.cuda.device(dev):
             rc = fn(*args, _raw_stream(dev))
     if rc:
-        _check(rc, where)
+        _check(rc, name)
 
 
 def _type(dtype, what):
@@ -123,29 +124,40 @@ def _type(dtype, what):
 def quantize(x: torch.Tensor, rows: bool = True, cols: bool = False):
     """x (2-D; its rows may lie apart) as an MXMatrix (rows), its transpose as one (cols), or both
     as a pair from one reading of x."""
-    dev = _on_gpu(x)
+    dev = x.get_device()
+    if dev < 0:
+        raise TypeError(f"quantize: a tensor on a GPU is wanted, got {x.device}")
     kind = _type(x.dtype, "quantize")
-    if x.dim() != 2 or not (rows or cols):
+    shape, device = x.shape, x.device
+    if len(shape) != 2 or not (rows or cols):
         raise ValueError("quantize: a matrix, and at least one of rows and cols, are wanted")
-    r, c = x.shape
+    r, c = shape
+    stride, step = x.stride()
     # a row of one element, or the only row, may have any stride
-    if c > 1 and x.stride(1) != 1 or r > 1 and x.stride(0) < c:
+    if c > 1 and step != 1 or r > 1 and stride < c:
         x = x.contiguous()
-    stride = x.stride(0) if r > 1 else c
-    q = MXMatrix.empty(r, c, x.device) if rows else None
-    t = MXMatrix.empty(c, r, x.device) if cols else None
-    _call("tula_mx_quantize", dev, _lib().tula_mx_quantize, x.data_ptr(), kind, r, c, stride,
-          q.code_ptr if rows else None, q.scale_ptr if rows else None,
-          t.code_ptr if cols else None, t.scale_ptr if cols else None)
-    return (q, t) if rows and cols else q if rows else t
+        stride = c
+    if r <= 1:
+        stride = c
+    if not cols:
+        q = MXMatrix.empty(r, c, device)
+        _call("tula_mx_quantize", dev, x.data_ptr(), kind, r, c, stride, q.code_ptr, q.scale_ptr, None, None)
+        return q
+    t = MXMatrix.empty(c, r, device)
+    if not rows:
+        _call("tula_mx_quantize", dev, x.data_ptr(), kind, r, c, stride, None, None, t.code_ptr, t.scale_ptr)
+        return t
+    q = MXMatrix.empty(r, c, device)
+    _call("tula_mx_quantize", dev, x.data_ptr(), kind, r, c, stride, q.code_ptr, q.scale_ptr, t.code_ptr,
+          t.scale_ptr)
+    return q, t
 
 
 def dequantize(q: MXMatrix, dtype=torch.bfloat16) -> torch.Tensor:
     """The values that q stands for."""
     kind = _type(dtype, "dequantize")
-    out = torch.empty(q.rows, q.cols, dtype=dtype, device=q.dev)
-    _call("tula_mx_dequantize", q.dev, _lib().tula_mx_dequantize, q.code_ptr, q.scale_ptr, q.rows,
-          q.cols, out.data_ptr(), kind)
+    out = torch.empty((q.rows, q.cols), dtype=dtype, device=q.device)
+    _call("tula_mx_dequantize", q.dev, q.code_ptr, q.scale_ptr, q.rows, q.cols, out.data_ptr(), kind)
     return out
 
 
@@ -154,9 +166,9 @@ def matmul(a: MXMatrix, b: MXMatrix, dtype=torch.bfloat16) -> torch.Tensor:
     if a.cols != b.cols or a.dev != b.dev:
         raise ValueError(f"matmul: {a.cols} columns on GPU {a.dev} and {b.cols} on GPU {b.dev}")
     kind = _type(dtype, "matmul")
-    out = torch.empty(a.rows, b.rows, dtype=dtype, device=a.dev)
-    _call("tula_mx_matmul", a.dev, _lib().tula_mx_matmul, a.code_ptr, a.scale_ptr, b.code_ptr,
-          b.scale_ptr, a.rows, b.rows, a.cols, out.data_ptr(), kind)
+    out = torch.empty((a.rows, b.rows), dtype=dtype, device=a.device)
+    _call("tula_mx_matmul", a.dev, a.code_ptr, a.scale_ptr, b.code_ptr, b.scale_ptr, a.rows, b.rows, a.cols,
+          out.data_ptr(), kind)
     return out
 
 
