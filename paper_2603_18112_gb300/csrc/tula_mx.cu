@@ -884,14 +884,15 @@ __global__ void __launch_bounds__(kMmaThreads) k_matmul(const __grid_constant__ 
 
 constexpr int kPairThreads = 192;
 struct Pair {
-    static constexpr int kStages = 5;
+    static constexpr int kStages = 6;
     static constexpr int kA = 128 * 128, kB = 128 * 128;
     static constexpr int kSA = 2 * kScaleTile, kSB = 4 * kScaleTile;  // the scales of all 256 rows of B
     static constexpr int kStage = kA + kB + kSA + kSB;
-    static constexpr int kOut = 4 * 2 * 4096;  // two buffers a warp, 32 rows of 128 bytes each
-    static constexpr int kSmem = kStages * kStage + kOut + 1024;
+    static constexpr int kOut = 4 * 4096;  // a buffer a warp, 32 rows of 128 bytes
+    static constexpr int kBars = 2 * kStages + 2;
+    static constexpr int kSmem = kStages * kStage + kOut + 8 * kBars + 16;
     static constexpr int kAcc1 = 224, kScaleA = 480, kScaleB = 488;  // tensor memory columns
-    static_assert(kStage % 1024 == 0 && kSmem <= 226 * 1024, "shared memory");
+    static_assert(kStage % 1024 == 0 && kSmem <= 227 * 1024, "shared memory");
 };
 
 struct PairArgs {
@@ -945,18 +946,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     k_matmul_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                   const __grid_constant__ CUtensorMap map_sa, const __grid_constant__ CUtensorMap map_sb,
                   const __grid_constant__ CUtensorMap map_out, const PairArgs a) {
-    extern __shared__ __align__(16) unsigned tile[];
-    __shared__ __align__(8) unsigned long long bars[2 * Pair::kStages + 2];
-    __shared__ uint32_t tmem_at;
-    __shared__ volatile int dead;
+    // All of the 227 KB but some: nothing in static shared memory, so that the stages start at a
+    // multiple of 1024 bytes without room to move them there (checked below).
+    extern __shared__ __align__(1024) unsigned char all[];
+    unsigned long long *bars = reinterpret_cast<unsigned long long *>(all + Pair::kStages * Pair::kStage + Pair::kOut);
+    uint32_t *tmem_at = reinterpret_cast<uint32_t *>(bars + Pair::kBars);
+    volatile int &dead = *reinterpret_cast<volatile int *>(tmem_at + 1);
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(kFull, tid >> 5, 0);
     const unsigned rank = blockIdx.x & 1;
     const int pairs = gridDim.x / 2, pair = blockIdx.x / 2, n_tiles = a.tiles_m * a.tiles_n;
-    const uint32_t stages = (smem_addr(tile) + 1023) & ~1023u;
+    const uint32_t stages = smem_addr(all);
     const uint32_t outs = stages + Pair::kStages * Pair::kStage;
     const uint32_t full = smem_addr(bars), empty = full + 8 * Pair::kStages;
     const uint32_t acc_full = empty + 8 * Pair::kStages, acc_free = acc_full + 8;
     const int n_k = (a.tiles_k + 1) / 2;
+    if (stages & 1023u) {  // no kernel that this may happen to has been seen
+        if (tid == 0) atomicOr(&g_mx_error, 2u);
+        return;
+    }
     if (tid == 0) {
         for (int s = 0; s < Pair::kStages; ++s) {
             mbar_init(full + 8 * s, 1);
@@ -968,7 +975,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_at)), "r"(512)
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_at)), "r"(512)
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
     }
@@ -1055,7 +1062,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         const int quad = warp & 3;
         constexpr int kChunk = 128 / (int)sizeof(T);  // columns of 128 bytes of out
         T *out = static_cast<T *>(a.out);
-        int n = 0, buf = 0;
+        int n = 0;
         for (int t = pair; t < n_tiles; t += pairs, ++n) {
             int tm, tn;
             tile_at(t, a, tm, tn);
@@ -1067,12 +1074,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
             for (int c = 0; c < 256 / kChunk; ++c) {
                 // the columns that the two accumulators share come first
                 const int chunk = n & 1 ? c : 256 / kChunk - 1 - c, col = chunk * kChunk;
-                const uint32_t at = outs + quad * 8192 + buf * 4096;
-                // the store before last has read this buffer
-                if (a.vec) {
-                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-                    __syncwarp();
-                }
+                const uint32_t at = outs + quad * 4096;
                 __align__(16) T y[kChunk];
 #pragma unroll
                 for (int k = 0; k < kChunk; k += 16) {
@@ -1085,6 +1087,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     __syncwarp();
                     if (lane == 0) arrive_cluster(in_cta(acc_free, 0));
+                }
+                if (a.vec) {  // the last store has read the buffer
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                    __syncwarp();
                 }
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -1104,7 +1110,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
                                          : "memory");
                         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     }
-                    buf ^= 1;
                 } else {
                     __syncwarp();
                     for (int r = 0; r < 32 && row0 + r < a.M; ++r)
