@@ -636,6 +636,24 @@ __device__ __forceinline__ void tmem_load16(float (&v)[16], uint32_t tmem) {
     for (int k = 0; k < 16; ++k) v[k] = __uint_as_float(r[k]);
 }
 
+// 32 columns, not waited for; tmem_wait makes the registers good.
+__device__ __forceinline__ void tmem_load32(unsigned *r, uint32_t tmem) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+                   "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+                   "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+                   "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(tmem));
+}
+template <int N>
+__device__ __forceinline__ void tmem_wait(unsigned (&r)[N]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int k = 0; k < N; ++k) asm volatile("" : "+r"(r[k]));  // no use of them moves up
+}
+
 struct MatmulArgs {
     const unsigned char *p_scales, *q_scales;
     void *out;
@@ -1076,18 +1094,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
                 const int chunk = n & 1 ? c : 256 / kChunk - 1 - c, col = chunk * kChunk;
                 const uint32_t at = outs + quad * 4096;
                 __align__(16) T y[kChunk];
+                unsigned v[kChunk];
 #pragma unroll
-                for (int k = 0; k < kChunk; k += 16) {
-                    float v[16];
-                    tmem_load16(v, acc + col + k);
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) put(&y[k + j], v[j]);
-                }
+                for (int k = 0; k < kChunk; k += 32) tmem_load32(v + k, acc + col + k);
+                tmem_wait(v);
                 if (c == 0) {
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     __syncwarp();
                     if (lane == 0) arrive_cluster(in_cta(acc_free, 0));
                 }
+#pragma unroll
+                for (int k = 0; k < kChunk; ++k) put(&y[k], __uint_as_float(v[k]));
                 if (a.vec) {  // the last store has read the buffer
                     if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                     __syncwarp();
