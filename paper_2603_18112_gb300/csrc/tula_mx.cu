@@ -673,6 +673,11 @@ __device__ __forceinline__ uint32_t in_cta(uint32_t addr, unsigned rank) {
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
+__device__ __forceinline__ float load_cluster(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
 __device__ __forceinline__ float4 load_cluster4(uint32_t addr) {
     float4 v;
     asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
@@ -716,6 +721,9 @@ __global__ void __launch_bounds__(kMmaThreads) k_matmul(const __grid_constant__ 
     const int tp = t / a.grid_q, tq = t % a.grid_q;
     const int all_k = (a.tiles_k + 1) / 2, per = (all_k + a.split - 1) / a.split;
     const int k_begin = min(rank * per, all_k), n_k = min(per, all_k - k_begin);  // stages of this CTA
+    // A thread of those that read back has a row of P: out's rows along Q are stored from there if
+    // they lie at 16-byte boundaries, and else, as partial sums are, by way of shared memory.
+    const bool shared = a.split > 1 || (!Swap && (((a.ld * sizeof(T)) | reinterpret_cast<uintptr_t>(a.out)) & 15));
     if (tid == 0) {
         for (int s = 0; s < S::kStages; ++s) {
             mbar_init(full + 8 * s, 1);
@@ -799,7 +807,6 @@ __global__ void __launch_bounds__(kMmaThreads) k_matmul(const __grid_constant__ 
         const int row = quad * 32 + lane;
         const long long p = (long long)tp * 128 + row;
         T *out = static_cast<T *>(a.out);
-        const bool vec = !Swap && a.split == 1 && ((a.ld * sizeof(T)) & 15) == 0 && (reinterpret_cast<uintptr_t>(a.out) & 15) == 0;
         for (int c = 0; ok && c < NT; c += 16) {
             const long long q0 = (long long)tq * NT + c;
             if (q0 >= a.Q) break;
@@ -811,7 +818,7 @@ __global__ void __launch_bounds__(kMmaThreads) k_matmul(const __grid_constant__ 
 #pragma unroll
                 for (int k = 0; k < 16; ++k) v[k] = 0.f;
             }
-            if (a.split > 1) {
+            if (shared) {
                 // the stages' place: every copy has landed and every instruction has read it
                 if (Swap) {
 #pragma unroll
@@ -825,7 +832,7 @@ __global__ void __launch_bounds__(kMmaThreads) k_matmul(const __grid_constant__ 
                                      : "memory");
                 }
             } else if (p < a.P) {
-                if (vec && q0 + 16 <= a.Q) {
+                if (!Swap && q0 + 16 <= a.Q) {
                     __align__(16) T y[16];
 #pragma unroll
                     for (int k = 0; k < 16; ++k) put(&y[k], v[k]);
@@ -846,9 +853,10 @@ __global__ void __launch_bounds__(kMmaThreads) k_matmul(const __grid_constant__ 
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         tmem_free(tmem, S::kCols);
     }
-    if (a.split == 1) return;
-    cluster_sync();
-    // This CTA's share of the tile's lines, four elements a thread.
+    if (!shared) return;
+    if (a.split > 1) cluster_sync();
+    // This CTA's share of the tile's lines, four elements a thread where they lie at a boundary of four,
+    // else a warp to a line.
     T *out = static_cast<T *>(a.out);
     const int q_here = (int)min((long long)NT, a.Q - (long long)tq * NT);
     const int p_here = (int)min(128ll, a.P - (long long)tp * 128);
@@ -856,8 +864,18 @@ __global__ void __launch_bounds__(kMmaThreads) k_matmul(const __grid_constant__ 
     const int share = (lines + a.split - 1) / a.split, first = rank * share;
     const long long line0 = Swap ? (long long)tq * NT : (long long)tp * 128, col0 = Swap ? (long long)tp * 128 : (long long)tq * NT;
     const bool vec = a.ld % 4 == 0 && (reinterpret_cast<uintptr_t>(a.out) & (4 * sizeof(T) - 1)) == 0;
+    const int n_lines = min(share, lines - first);
+    if (!vec) {
+        for (int o = first + warp; o < first + n_lines; o += kMmaThreads / 32)
+            for (int n = lane; n < line; n += 32) {
+                const uint32_t at = stages + 4 * (o * S::kPitch + n);
+                float sum = load_cluster(in_cta(at, 0));
+                for (int r = 1; r < a.split; ++r) sum = __fadd_rn(sum, load_cluster(in_cta(at, r)));
+                put(out + (line0 + o) * a.ld + col0 + n, sum);
+            }
+    }
     constexpr int kQuads = S::kLine / 4;
-    for (int i = tid; i < min(share, lines - first) * kQuads; i += kMmaThreads) {
+    for (int i = tid; vec && i < n_lines * kQuads; i += kMmaThreads) {
         const int o = first + i / kQuads, n = i % kQuads * 4;
         if (n >= line) continue;
         const uint32_t at = stages + 4 * (o * S::kPitch + n);
@@ -885,7 +903,7 @@ __global__ void __launch_bounds__(kMmaThreads) k_matmul(const __grid_constant__ 
                 if (n + k < line) to[k] = y[k];
         }
     }
-    cluster_sync();  // the others have read this CTA's sums
+    if (a.split > 1) cluster_sync();  // the others have read this CTA's sums
 }
 
 // ----------------------------------------------------------------------------
@@ -1129,22 +1147,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
                     }
                 } else {
                     __syncwarp();
-                    for (int r = 0; r < 32 && row0 + r < a.M; ++r)
+                    const int here = (int)max(0ll, min((long long)kChunk, a.N - c0));
+                    // Element by element along the rows (in pairs, at 4-byte boundaries where there are
+                    // any, it took twice the time: lanes at the ends part ways); eight rows are read
+                    // before any is stored.
+                    constexpr int kPer = kChunk / 32;
+                    const unsigned char *mine = all + (at - stages);
+                    for (int r0 = 0; r0 < 32; r0 += 8) {
+                        T u[8][kPer];
 #pragma unroll
-                        for (int k = lane; k < kChunk; k += 32) {
-                            const uint32_t from = at + r * 128 + ((((k * (int)sizeof(T)) >> 4) ^ (r & 7)) << 4) + ((k * (int)sizeof(T)) & 15);
-                            if (c0 + k >= a.N) continue;
-                            T *to = out + (row0 + r) * a.N + c0 + k;
-                            if (sizeof(T) == 4) {
-                                unsigned u;
-                                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(u) : "r"(from) : "memory");
-                                *reinterpret_cast<unsigned *>(to) = u;
-                            } else {
-                                unsigned short u;
-                                asm volatile("ld.shared.b16 %0, [%1];" : "=h"(u) : "r"(from) : "memory");
-                                *reinterpret_cast<unsigned short *>(to) = u;
-                            }
+                        for (int j = 0; j < 8; ++j)
+#pragma unroll
+                            for (int k = 0; k < kPer; ++k)
+                                u[j][k] = *reinterpret_cast<const T *>(
+                                    mine + (r0 + j) * 128 + (((lane + 32 * k) * (int)sizeof(T)) ^ ((r0 + j & 7) << 4)));
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            T *to = out + (row0 + r0 + j) * a.N + c0 + lane;
+#pragma unroll
+                            for (int k = 0; k < kPer; ++k)
+                                if (lane + 32 * k < here && row0 + r0 + j < a.M) to[32 * k] = u[j][k];
                         }
+                    }
                     __syncwarp();
                 }
             }
@@ -1326,10 +1350,12 @@ int matmul_small(const void *a_codes, const void *a_scales, const void *b_codes,
     const int nt = a.Q <= 32 ? 32 : a.Q <= 64 ? 64 : 128;
     a.grid_q = (int)up(a.Q, nt);
     const long long tiles = up(a.P, 128) * a.grid_q;
-    // Few tiles: up to eight CTAs share one's columns, two stages at least for each, while all
-    // are resident (two an SM).
+    // Few tiles: up to eight CTAs share one's columns while all are resident (two an SM), two stages at
+    // least for each, or four where the sums that they exchange are as long (128 x 4096 x 4096: 8.3
+    // us with four CTAs, 9.2 with eight; 1 x 4096 x 4096: 4.0 us with eight).
+    const int least = nt >= 64 ? 8 : 4;
     a.split = 1;
-    while (a.split < 8 && tiles * a.split * 2 <= 2 * 152 && up(a.tiles_k, 2) >= 4 * a.split) a.split *= 2;
+    while (a.split < 8 && tiles * a.split * 2 <= 2 * 152 && up(a.tiles_k, 2) >= least * a.split) a.split *= 2;
     if (tiles * a.split >= (1LL << 31)) return TULA_ERR_ARG;
     CUtensorMap mp, mq;
     std::memset(&mp, 0, sizeof(mp));
