@@ -217,11 +217,26 @@ template <typename T>
 __device__ __forceinline__ unsigned top_bits(unsigned half) {
     return std::is_same<T, __half>::value ? __float_as_uint(__half2float(__ushort_as_half((unsigned short)half))) : half << 16;
 }
-// The larger magnitudes of a word and those so far; 16-bit elements by halves, in their own bits.
+// The larger magnitudes of a word and those so far, the signs of no meaning, a NaN kept; 16-bit
+// elements by halves.  One instruction, where integer ones take a mask and a maximum.
 template <typename T>
 __device__ __forceinline__ unsigned larger(unsigned top, unsigned w) {
-    return sizeof(T) == 4 ? max(top, w & 0x7fffffffu) : __vmaxu2(top, w & 0x7fff7fffu);
+    unsigned r;
+    if (sizeof(T) == 4)
+        asm("max.NaN.xorsign.abs.f32 %0, %1, %2;" : "=r"(r) : "r"(top), "r"(w));
+    else if (std::is_same<T, __half>::value)
+        asm("max.NaN.xorsign.abs.f16x2 %0, %1, %2;" : "=r"(r) : "r"(top), "r"(w));
+    else
+        asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(top), "r"(w));
+    return r;
 }
+__device__ __forceinline__ unsigned mul_bf16x2(unsigned a, unsigned b) {
+    unsigned r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// inverse_scale as bf16 bits.
+__device__ __forceinline__ unsigned inverse_scale_bf16(unsigned s) { return s == 255u ? 0u : (254u - s) << 7; }
 
 // Eight elements of a row, four lanes to a block, sixteen to the tile's row: their codes; scales:
 // the row's four scale bytes.
@@ -230,16 +245,26 @@ __device__ __forceinline__ unsigned quantize_row8(const unsigned (&w)[sizeof(T) 
     unsigned top = 0;
 #pragma unroll
     for (int j = 0; j < (int)sizeof(T) * 2; ++j) top = larger<T>(top, w[j]);
+    top &= sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu;
     if (sizeof(T) == 2) top = max(top & 0xffffu, top >> 16);
     top = max(top, __shfl_xor_sync(kFull, top, 1));
     top = max(top, __shfl_xor_sync(kFull, top, 2));
     if (sizeof(T) == 2) top = top_bits<T>(top);
     const unsigned s = scale_byte(top);
-    const float f = inverse_scale(s);
     float x[8];
-    floats8<T>(x, w);
+    if (std::is_same<T, __nv_bfloat16>::value) {
+        // exact in bf16 too (what falls below its range is far below the smallest code)
+        const unsigned f = inverse_scale_bf16(s) * 0x10001u;
+        unsigned v[sizeof(T) * 2];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = __fmul_rn(x[j], f);
+        for (int j = 0; j < (int)sizeof(T) * 2; ++j) v[j] = mul_bf16x2(w[j], f);
+        floats8<T>(x, v);
+    } else {
+        const float f = inverse_scale(s);
+        floats8<T>(x, w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = __fmul_rn(x[j], f);
+    }
     scales = s << (8 * (sub >> 2));
     scales |= __shfl_xor_sync(kFull, scales, 4);
     scales |= __shfl_xor_sync(kFull, scales, 8);
@@ -257,11 +282,22 @@ __device__ __forceinline__ void quantize_cols(const unsigned *tile, int c, int r
         w[k] = tile[(32 * rb + k) * (kTile * (int)sizeof(T) / 4) + c];
         top = larger<T>(top, w[k]);
     }
+    constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
+    constexpr int kCols = 4 / (int)sizeof(T);
+    top &= sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu;
+    unsigned s[kCols];
 #pragma unroll
-    for (int h = 0; h < 4 / (int)sizeof(T); ++h) {
-        const int col = sizeof(T) == 4 ? c : 2 * c + h;
-        const unsigned s = scale_byte(sizeof(T) == 4 ? top : top_bits<T>(h ? top >> 16 : top & 0xffffu));
-        const float f = inverse_scale(s);
+    for (int h = 0; h < kCols; ++h)
+        s[h] = scale_byte(sizeof(T) == 4 ? top : top_bits<T>(h ? top >> 16 : top & 0xffffu));
+    if (kBf16) {
+        const unsigned f = inverse_scale_bf16(s[0]) | inverse_scale_bf16(s[kCols - 1]) << 16;
+#pragma unroll
+        for (int k = 0; k < 32; ++k) w[k] = mul_bf16x2(w[k], f);
+    }
+#pragma unroll
+    for (int h = 0; h < kCols; ++h) {
+        const int col = kCols * c + h;
+        const float f = inverse_scale(s[h]);
         unsigned q[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -275,12 +311,12 @@ __device__ __forceinline__ void quantize_cols(const unsigned *tile, int c, int r
                     const float2 p = pair_of<T>(w[8 * k + j]);
                     v = h ? p.y : p.x;
                 }
-                x[j] = __fmul_rn(v, f);
+                x[j] = kBf16 ? v : __fmul_rn(v, f);
             }
-            q[k] = s == 255u ? 0u : codes8(x);
+            q[k] = s[h] == 255u ? 0u : codes8(x);
         }
         *reinterpret_cast<uint4 *>(out + col * pitch + 16 * rb) = make_uint4(q[0], q[1], q[2], q[3]);
-        scales[(col & 31) * 16 + (col >> 5) * 4 + rb] = (unsigned char)s;
+        scales[(col & 31) * 16 + (col >> 5) * 4 + rb] = (unsigned char)s[h];
     }
 }
 
@@ -501,63 +537,119 @@ struct DequantArgs {
     const unsigned char *codes, *scales;
     long long n, cols;  // elements, columns
     int tiles_c, lead;  // lead: elements from the boundary below out to out
-    unsigned long long magic;  // ceil(2^64 / cols), or 0 where the division by it would not be exact
+    unsigned long long magic;  // ceil(2^64 / cols) (Easy: / (cols / 8)), or 0: see divide
 };
-__device__ __forceinline__ unsigned scale_at(const DequantArgs &a, long long r, long long c) {
+// x / d with magic = ceil(2^64 / d): for a 32-bit x the quotient is exact; for others where
+// x d < 2^64, and the host has left magic 0 where that does not hold.
+__device__ __forceinline__ unsigned divide(unsigned x, unsigned long long magic, long long) {
+    const unsigned long long lo = (unsigned long long)x * (unsigned)magic;
+    return (unsigned)(((unsigned long long)x * (unsigned)(magic >> 32) + (lo >> 32)) >> 32);
+}
+__device__ __forceinline__ long long divide(long long x, unsigned long long magic, long long d) {
+    return magic ? (long long)__umul64hi((unsigned long long)x, magic) : x / d;
+}
+template <typename I>
+__device__ __forceinline__ unsigned scale_at(const DequantArgs &a, I r, I c) {
     return a.scales[((size_t)(r / kTile) * a.tiles_c + c / kTile) * kScaleTile + (r & 31) * 16 + (r & 127) / 32 * 4 +
                     (c & 127) / kBlock];
 }
 
+// The values of eight codes as pairs of bf16, but for the scale.  A value's two bytes are looked up by
+// byte permutations whose selectors are four codes' magnitudes at a time; then the signs are put in.
+// (By conversions to fp16 and fp32 the kernel issued in 83 % of all cycles and HBM waited for it.)
+__device__ __forceinline__ void code_values(unsigned (&v)[4], unsigned q) {
+    const unsigned m = q & 0x77777777u, up = q << 4;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        // 0, 0.5, 1, 1.5 and 2, 3, 4, 6: high bytes 00 3f 3f 3f and 40 each, low ones 00 00 80 c0 and 00 40 80 c0
+        const unsigned hi = __byte_perm(0x3f3f3f00u, 0x40404040u, m >> (16 * k));
+        const unsigned lo = __byte_perm(0xc0800000u, 0xc0804000u, m >> (16 * k));
+        v[2 * k] = __byte_perm(lo, hi, 0x5140);
+        v[2 * k + 1] = __byte_perm(lo, hi, 0x7362);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] |= __byte_perm(up, q, (4 + k) << 12 | k << 4) & 0x80008000u;
+}
+// Eight elements from their codes, the first `first` with scale s0, the others with s1.
+template <typename T>
+__device__ __forceinline__ void scaled_values(T (&y)[8], unsigned q, unsigned s0, unsigned s1, int first) {
+    unsigned v[4];
+    code_values(v, q);
+    if (std::is_same<T, __nv_bfloat16>::value) {
+        auto bf16_scale = [](unsigned s) { return s == 255u ? 0x7fffu : s ? s << 7 : 0x0040u; };
+        const unsigned b0 = bf16_scale(s0), b1 = bf16_scale(s1);
+        unsigned *out = reinterpret_cast<unsigned *>(y);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            out[k * (int)sizeof(T) / 2] = mul_bf16x2(v[k], (2 * k < first ? b0 : b1) | (2 * k + 1 < first ? b0 : b1) << 16);
+    } else {
+        const float f0 = scale_value(s0), f1 = scale_value(s1);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            put(&y[2 * k], __fmul_rn(__uint_as_float(v[k] << 16), 2 * k < first ? f0 : f1));
+            put(&y[2 * k + 1], __fmul_rn(__uint_as_float(v[k] & 0xffff0000u), 2 * k + 1 < first ? f0 : f1));
+        }
+    }
+}
+
 // Out is one run of elements: a thread writes the eight between two boundaries of as many bytes,
 // whatever rows they belong to, and takes their codes from where they lie.  Easy: rows start at
-// multiples of eight; then four such groups a thread for 16-bit types (17 us for 8192 x 4096 to
-// bf16, 20 with one), elsewhere one (fp32: 31 us, 33 with four; odd sizes: 30 and 39).
+// multiples of eight.  Four such groups a thread for 16-bit types then, elsewhere one (measured
+// at 8192 x 4096).  I: an unsigned where all indexes fit.
 template <typename T, bool Easy>
 constexpr int kGroupsOf = Easy && sizeof(T) == 2 ? 4 : 1;
-template <typename T, bool Easy>
+template <typename T, bool Easy, typename I>
 __global__ void __launch_bounds__(256) k_dequantize(const DequantArgs a, T *out) {
     constexpr int kGroups = kGroupsOf<T, Easy>;
     let_next_start();
     wait_for_previous();
-    long long f[kGroups], r[kGroups], c[kGroups];
+    I f[kGroups], r[kGroups], c[kGroups];
     unsigned q[kGroups], s0[kGroups], s1[kGroups];
     bool whole[kGroups];  // eight elements of one row
+    const I n = (I)a.n, cols = (I)a.cols;
 #pragma unroll
     for (int j = 0; j < kGroups; ++j) {
-        f[j] = 8 * ((long long)blockIdx.x * (256 * kGroups) + 256 * j + threadIdx.x) - (Easy ? 0 : a.lead);
-        const long long at = max(f[j], 0ll);
-        r[j] = a.magic ? (long long)__umul64hi((unsigned long long)at, a.magic) : at / a.cols;
-        c[j] = at - r[j] * a.cols;
-        whole[j] = f[j] >= 0 && f[j] + 8 <= a.n && c[j] + 8 <= a.cols;
+        const I g = (I)blockIdx.x * (256 * kGroups) + 256 * j + threadIdx.x;
+        if (Easy) {
+            f[j] = 8 * g;
+            r[j] = divide(g, a.magic, a.cols / 8);
+            c[j] = f[j] - r[j] * cols;
+            whole[j] = f[j] < n;
+        } else {
+            f[j] = 8 * g - (I)a.lead;  // (the first group: below 0, or beyond n for unsigned ones)
+            const I at = g == 0 ? 0 : f[j];
+            r[j] = divide(at, a.magic, a.cols);
+            c[j] = at - r[j] * cols;
+            whole[j] = (g > 0 || a.lead == 0) && f[j] < n && n - f[j] >= 8 && cols - c[j] >= 8;
+        }
         if (!whole[j]) continue;
         const unsigned *w = reinterpret_cast<const unsigned *>(a.codes + (size_t)r[j] * a.tiles_c * (kTile / 2)) + c[j] / 8;
         q[j] = __ldcs(w);
-        s0[j] = scale_at(a, r[j], c[j]);
+        s1[j] = s0[j] = scale_at(a, r[j], c[j]);
         if (!Easy) {
             const int in = (int)(c[j] & 7);
             if (in) q[j] = __funnelshift_r(q[j], __ldcs(w + 1), 4 * in);
-            s1[j] = scale_at(a, r[j], c[j] + 7);
+            s1[j] = scale_at<I>(a, r[j], c[j] + 7);
         }
     }
 #pragma unroll
     for (int j = 0; j < kGroups; ++j) {
         if (whole[j]) {
-            const float f0 = scale_value(s0[j]), f1 = Easy ? f0 : scale_value(s1[j]);
-            const int in = (int)(c[j] & 31);
-            __align__(16) T y[8];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float2 v = code_pair(q[j] >> (8 * k) & 0xffu);
-                put(&y[2 * k], __fmul_rn(v.x, Easy || in + 2 * k < 32 ? f0 : f1));
-                put(&y[2 * k + 1], __fmul_rn(v.y, Easy || in + 2 * k + 1 < 32 ? f0 : f1));
-            }
+            __align__(32) T y[8];
+            scaled_values(y, q[j], s0[j], s1[j], Easy ? 8 : 32 - (int)(c[j] & 31));
             store_run(out + f[j], y);
         } else if (!Easy) {
-            long long row = r[j], col = c[j];
-            for (long long e = max(f[j], 0ll); e < min(f[j] + 8, a.n); ++e) {
+            I row = r[j], col = c[j];
+            const I g = (I)blockIdx.x * (256 * kGroups) + 256 * j + threadIdx.x;
+            const int skip = g == 0 ? a.lead : 0;  // elements before out
+            if (g > 0 && f[j] >= n) continue;
+            const I left = g == 0 ? n : n - f[j];
+            const int here = left < (I)(8 - skip) ? (int)left : 8 - skip;
+            T *to = g == 0 ? out : out + f[j];
+            for (int k = 0; k < here; ++k) {
                 const unsigned byte = a.codes[(size_t)row * a.tiles_c * (kTile / 2) + col / 2];
-                put(out + e, __fmul_rn(code_pair(col & 1 ? byte >> 4 : byte & 15u).x, scale_value(scale_at(a, row, col))));
-                if (++col == a.cols) ++row, col = 0;
+                put(to + k, __fmul_rn(code_pair(col & 1 ? byte >> 4 : byte & 15u).x, scale_value(scale_at(a, row, col))));
+                if (++col == cols) ++row, col = 0;
             }
         }
     }
@@ -1315,13 +1407,16 @@ int dequantize_typed(const void *codes, const void *scales, long long rows, long
     a.cols = cols;
     a.tiles_c = (int)up(cols, kTile);
     a.lead = (int)(reinterpret_cast<uintptr_t>(out) % (8 * sizeof(T)) / sizeof(T));
-    // floor(f / cols) = floor(f m / 2^64) while f (m cols - 2^64) < 2^64, that is f < 2^64 / cols
-    a.magic = cols > 1 && (unsigned long long)a.n < ~0ull / (unsigned long long)cols ? ~0ull / (unsigned long long)cols + 1 : 0;
     const bool easy = cols % 8 == 0 && a.lead == 0;
     const long long blocks = up(a.n + a.lead, 8 * 256 * (easy ? kGroupsOf<T, true> : kGroupsOf<T, false>));
     if (blocks >= (1LL << 31)) return TULA_ERR_ARG;
-    return tula::launch(easy ? k_dequantize<T, true> : k_dequantize<T, false>, dim3((unsigned)blocks), 256,
-                        0, s, 1, a, static_cast<T *>(out));
+    // 32-bit indexes where the last group's, beyond n, still fits
+    const bool small = (easy ? blocks * 256 * kGroupsOf<T, true> * 8 : a.n + 8 * 256 * 2) < (1LL << 32);
+    const unsigned long long d = (unsigned long long)(easy ? cols / 8 : cols);
+    a.magic = d > 1 && (small || (unsigned long long)a.n < ~0ull / d) ? ~0ull / d + 1 : 0;
+    void (*k)(const DequantArgs, T *) = easy ? (small && d > 1 ? k_dequantize<T, true, unsigned> : k_dequantize<T, true, long long>)
+                                             : (small && d > 1 ? k_dequantize<T, false, unsigned> : k_dequantize<T, false, long long>);
+    return tula::launch(k, dim3((unsigned)blocks), 256, 0, s, 1, a, static_cast<T *>(out));
 }
 
 template <int NT, bool Swap, typename T>
