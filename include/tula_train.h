@@ -127,6 +127,7 @@ int tula_adamw_step(tula_train_plan *plan, const tula_adamw_hparams *hp, void *s
  *           cores take them; zero beyond the matrix
  * Both 16-byte aligned.
  */
+/* Bytes of a matrix; rows and cols below 2^31 - 1023, at most 2^31 tiles (TULA_ERR_ARG). */
 int tula_mx_size(int64_t rows, int64_t cols, size_t *code_bytes, size_t *scale_bytes);
 
 /*
@@ -158,8 +159,8 @@ int tula_mx_matmul(const void *a_codes, const void *a_scales, const void *b_code
 /*
  * The error word of the products on the current device, read after the work already enqueued on
  * `stream` (the call waits for that stream), then cleared: 0 when every bounded wait inside a
- * product's kernel completed; bit 0 set when one ran out, and the products since the last read
- * are then not valid.
+ * product's kernel completed; bit 0 set when one ran out, bit 1 when shared memory did not start where
+ * the kernel needs it, and the products since the last read are then not valid.
  */
 int tula_mx_error(void *stream, int *error_out);
 

@@ -131,6 +131,9 @@ struct QuantArgs {
     int tiles_r;
 };
 
+// (A kernel may start while the one before it still writes x: nothing of x is read before the wait,
+// which makes it visible, and nothing by the read-only path, which takes it for constant.)
+//
 // Eight elements of a row as they are, 16-bit types in 4 words, fp32 in 8; zero beyond `left` of
 // them.  Aligned: they start at a 16-byte boundary.  Else the 16-byte granules that hold them are
 // loaded, the last also by the next lane, and shifted; inner: all of them lie within the matrix
@@ -138,7 +141,7 @@ struct QuantArgs {
 // by element.
 template <typename T>
 __device__ __forceinline__ uint4 load_granule(unsigned long long at, unsigned long long begin, unsigned long long end) {
-    if (at >= begin && at + 16 <= end) return __ldg(reinterpret_cast<const uint4 *>(at));
+    if (at >= begin && at + 16 <= end) return *reinterpret_cast<const uint4 *>(at);
     unsigned w[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -177,7 +180,7 @@ __device__ __forceinline__ void load_row8(unsigned (&w)[sizeof(T) * 2], const T 
     for (int k = 0; k <= kWords / 4; ++k) {
         uint4 q = make_uint4(0, 0, 0, 0);
         if (inner)
-            q = __ldg(reinterpret_cast<const uint4 *>(at - off) + k);
+            q = reinterpret_cast<const uint4 *>(at - off)[k];
         else if (k < kWords / 4 || off)
             q = load_granule<T>(at - off + 16 * k, begin, end);
         v[4 * k] = q.x, v[4 * k + 1] = q.y, v[4 * k + 2] = q.z, v[4 * k + 3] = q.w;
@@ -550,8 +553,8 @@ __device__ __forceinline__ long long divide(long long x, unsigned long long magi
 }
 template <typename I>
 __device__ __forceinline__ unsigned scale_at(const DequantArgs &a, I r, I c) {
-    return a.scales[((size_t)(r / kTile) * a.tiles_c + c / kTile) * kScaleTile + (r & 31) * 16 + (r & 127) / 32 * 4 +
-                    (c & 127) / kBlock];
+    return __ldcg(a.scales + ((size_t)(r / kTile) * a.tiles_c + c / kTile) * kScaleTile + (r & 31) * 16 + (r & 127) / 32 * 4 +
+                  (c & 127) / kBlock);
 }
 
 // The values of eight codes as pairs of bf16, but for the scale.  A value's two bytes are looked up by
@@ -624,11 +627,11 @@ __global__ void __launch_bounds__(256) k_dequantize(const DequantArgs a, T *out)
         }
         if (!whole[j]) continue;
         const unsigned *w = reinterpret_cast<const unsigned *>(a.codes + (size_t)r[j] * a.tiles_c * (kTile / 2)) + c[j] / 8;
-        q[j] = __ldcs(w);
+        q[j] = __ldcg(w);
         s1[j] = s0[j] = scale_at(a, r[j], c[j]);
         if (!Easy) {
             const int in = (int)(c[j] & 7);
-            if (in) q[j] = __funnelshift_r(q[j], __ldcs(w + 1), 4 * in);
+            if (in) q[j] = __funnelshift_r(q[j], __ldcg(w + 1), 4 * in);
             s1[j] = scale_at<I>(a, r[j], c[j] + 7);
         }
     }
@@ -647,7 +650,7 @@ __global__ void __launch_bounds__(256) k_dequantize(const DequantArgs a, T *out)
             const int here = left < (I)(8 - skip) ? (int)left : 8 - skip;
             T *to = g == 0 ? out : out + f[j];
             for (int k = 0; k < here; ++k) {
-                const unsigned byte = a.codes[(size_t)row * a.tiles_c * (kTile / 2) + col / 2];
+                const unsigned byte = __ldcg(a.codes + (size_t)row * a.tiles_c * (kTile / 2) + col / 2);
                 put(to + k, __fmul_rn(code_pair(col & 1 ? byte >> 4 : byte & 15u).x, scale_value(scale_at(a, row, col))));
                 if (++col == cols) ++row, col = 0;
             }
@@ -752,7 +755,6 @@ struct MatmulArgs {
     long long P, Q;       // rows of each operand
     long long ld;         // elements of out from row to row
     int tiles_k;          // of 128 columns
-    int q_tiles;          // tiles of Q's scales along its rows
     int grid_q;           // tiles of the product along Q
     int split;            // CTAs of a cluster that share a tile's columns
 };
@@ -1291,9 +1293,11 @@ inline int type_size(int type) { return type == TULA_TYPE_F32 ? 4 : 2; }
 inline bool good_type(int type) { return type >= TULA_TYPE_F32 && type <= TULA_TYPE_F16; }
 inline bool aligned(const void *p, unsigned n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
+constexpr long long kMostRows = (1LL << 31) - 1024;  // coordinates of tiles that reach beyond them fit an int
+
 // Tiles of 128 x 128; -1 beyond what one grid and 32-bit coordinates hold.
 long long tiles_of(long long rows, long long cols) {
-    if (rows < 0 || cols < 0 || rows > (1LL << 38) || cols > (1LL << 31) || rows > (1LL << 31)) return -1;
+    if (rows < 0 || cols < 0 || rows > kMostRows || cols > kMostRows) return -1;
     const long long t = up(rows, kTile) * up(cols, kTile);
     return t < (1LL << 31) ? t : -1;
 }
@@ -1367,12 +1371,11 @@ int launch_quantize(const QuantArgs &a, unsigned grid, cudaStream_t s) {
 template <typename T>
 int launch_quantize_tiles(const QuantArgs &a, unsigned tiles, cudaStream_t s) {
     using R = QuantRing<T>;
-    static std::atomic<uint64_t> done[3];
-    const int which = a.codes && a.codes_t ? 0 : a.codes ? 1 : 2;
-    void (*k)(const CUtensorMap, const QuantArgs) = which == 0   ? k_quantize_tiles<T, true, true>
-                                                    : which == 1 ? k_quantize_tiles<T, true, false>
-                                                                 : k_quantize_tiles<T, false, true>;
-    const int rc = allow_smem((const void *)k, R::kSmem, &done[which]);
+    static std::atomic<uint64_t> done[2];
+    void (*k)(const CUtensorMap, const QuantArgs) = k_quantize_tiles<T, false, true>;
+    if constexpr (sizeof(T) == 4)  // (16-bit types come here for the transpose alone)
+        if (a.codes) k = k_quantize_tiles<T, true, true>;
+    const int rc = allow_smem((const void *)k, R::kSmem, &done[a.codes != nullptr]);
     if (rc) return rc;
     CUtensorMap map;
     const CUtensorMapDataType type = sizeof(T) == 4 ? CU_TENSOR_MAP_DATA_TYPE_UINT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16;
@@ -1441,7 +1444,6 @@ int matmul_small(const void *a_codes, const void *a_scales, const void *b_codes,
     a.ld = N;
     a.out = out;
     a.tiles_k = (int)up(K, kTile);
-    a.q_tiles = (int)up(a.Q, kTile);
     const int nt = a.Q <= 32 ? 32 : a.Q <= 64 ? 64 : 128;
     a.grid_q = (int)up(a.Q, nt);
     const long long tiles = up(a.P, 128) * a.grid_q;

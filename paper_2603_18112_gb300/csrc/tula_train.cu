@@ -49,7 +49,7 @@ struct Row {
 static_assert(sizeof(Row) == 64, "half an L2 line");
 
 // The scalars one step's update needs, written by the norm's last CTA.
-struct StepScalars {
+struct alignas(16) StepScalars {
     float mult, step_size, rbc2;
     int go;
 };
@@ -94,32 +94,22 @@ __device__ __forceinline__ unsigned pack_f16(float a, float b) {
     return u;
 }
 
-// kVec elements of a type as they lie in memory, at index i (a multiple of kVec).  Stream: not to be
-// kept in the caches.
+// kVec elements of a type as they lie in memory, at index i (a multiple of kVec).  Past L1: nothing is
+// read twice, and AdamW over 184 M elements takes 744 us, 749 with streaming loads through it.
 template <int Type>
 struct Raw {
     static constexpr bool kWide = Type == TULA_TYPE_F32;
     unsigned w[kWide ? 8 : 4];
-    template <bool Stream>
     __device__ __forceinline__ void load(unsigned long long base, int i) {
         if (kWide) {
-            const unsigned long long p = base + 4ull * i;
             constexpr int kHalf = kWide ? 4 : 0;
-            if (Stream)
-                asm volatile("ld.global.cs.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                             : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[kHalf]), "=r"(w[kHalf + 1]),
-                               "=r"(w[kHalf + 2]), "=r"(w[kHalf + 3])
-                             : "l"(p)
-                             : "memory");
-            else
-                asm volatile("ld.global.cg.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                             : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[kHalf]), "=r"(w[kHalf + 1]),
-                               "=r"(w[kHalf + 2]), "=r"(w[kHalf + 3])
-                             : "l"(p)
-                             : "memory");
+            asm volatile("ld.global.cg.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[kHalf]), "=r"(w[kHalf + 1]),
+                           "=r"(w[kHalf + 2]), "=r"(w[kHalf + 3])
+                         : "l"(base + 4ull * i)
+                         : "memory");
         } else {
-            const uint4 *p = reinterpret_cast<const uint4 *>(base + 2ull * i);
-            const uint4 q = Stream ? __ldcs(p) : __ldcg(p);
+            const uint4 q = __ldcg(reinterpret_cast<const uint4 *>(base + 2ull * i));
             w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
         }
     }
@@ -151,19 +141,18 @@ struct Raw {
         }
     }
 };
-template <bool Stream>
 __device__ __forceinline__ void load8(float (&x)[kVec], unsigned long long base, int type, int i) {
     if (type == TULA_TYPE_F32) {
         Raw<TULA_TYPE_F32> r;
-        r.load<Stream>(base, i);
+        r.load(base, i);
         r.floats(x);
     } else if (type == TULA_TYPE_BF16) {
         Raw<TULA_TYPE_BF16> r;
-        r.load<Stream>(base, i);
+        r.load(base, i);
         r.floats(x);
     } else {
         Raw<TULA_TYPE_F16> r;
-        r.load<Stream>(base, i);
+        r.load(base, i);
         r.floats(x);
     }
 }
@@ -327,7 +316,7 @@ template <int Type>
 __device__ __forceinline__ void load_part(Raw<Type> &raw, const Row &row, int j) {
     const int tid = threadIdx.x, i = (j * kThreads + tid) * kVec;
     if (row.vec && i >= row.lo && i + kVec <= row.hi) {
-        raw.template load<false>(row.g, i);
+        raw.load(row.g, i);
         return;
     }
 #pragma unroll
@@ -347,7 +336,7 @@ __device__ __forceinline__ double tile_sum(const Row &row) {
     if (row.vec && row.lo == 0 && row.hi == VPT * kThreads * kVec) {
         Raw<Type> raw[VPT];
 #pragma unroll
-        for (int j = 0; j < VPT; ++j) raw[j].template load<false>(row.g, (j * kThreads + tid) * kVec);
+        for (int j = 0; j < VPT; ++j) raw[j].load(row.g, (j * kThreads + tid) * kVec);
         s = square_sum(raw, bits);
     } else {
 #pragma unroll 1
@@ -444,7 +433,7 @@ __device__ __forceinline__ void tile_scale(const Row &row, float c) {
     if (row.vec && row.lo == 0 && row.hi == VPT * kThreads * kVec) {
         Raw<Type> raw[VPT];
 #pragma unroll
-        for (int j = 0; j < VPT; ++j) raw[j].template load<true>(g, (j * kThreads + tid) * kVec);
+        for (int j = 0; j < VPT; ++j) raw[j].load(g, (j * kThreads + tid) * kVec);
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
             float x[kVec];
@@ -458,7 +447,7 @@ __device__ __forceinline__ void tile_scale(const Row &row, float c) {
             const int i = (j * kThreads + tid) * kVec;
             if (i >= row.lo && i + kVec <= row.hi) {
                 float x[kVec];
-                load8<true>(x, g, Type, i);
+                load8(x, g, Type, i);
 #pragma unroll
                 for (int k = 0; k < kVec; ++k) x[k] = __fmul_rn(x[k], c);
                 store8(x, g, Type, i);
@@ -484,7 +473,7 @@ __global__ void __launch_bounds__(kThreads) k_clip(const Tables tb) {
     const int first = (tb.n_groups - 1 - (int)blockIdx.x) * tb.group, n = min(tb.group, tb.n_tiles - first);
     fetch_rows(rows, tb, first, n);
     wait_for_previous();
-    const float c = tb.scal->mult;
+    const float c = __ldcg(&tb.scal->mult);
     if (c == 1.f) return;
     for (int t = n - 1; t >= 0; --t) {
         const Row &row = rows[t];
@@ -527,10 +516,10 @@ __device__ __forceinline__ void adamw1(float g, float &w, float &m, float &v, co
 struct AdamVec {
     float g[kVec], w[kVec], m[kVec], v[kVec];
     __device__ __forceinline__ void load(const Row &r, int i) {
-        load8<true>(w, r.w, TULA_TYPE_F32, i);
-        load8<true>(m, r.m, TULA_TYPE_F32, i);
-        load8<true>(v, r.v, TULA_TYPE_F32, i);
-        load8<true>(g, r.g, r.gtype, i);
+        load8(w, r.w, TULA_TYPE_F32, i);
+        load8(m, r.m, TULA_TYPE_F32, i);
+        load8(v, r.v, TULA_TYPE_F32, i);
+        load8(g, r.g, r.gtype, i);
     }
     __device__ __forceinline__ void update(const Row &r, int i, const Adam &h, const StepScalars &s) {
 #pragma unroll
@@ -567,7 +556,8 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const Tables tb, const Adam 
     if (fits(tid * kVec)) x.load(row, tid * kVec);
     StepScalars s;
     if (Normed) {
-        s = *tb.scal;
+        const float4 q = __ldcg(reinterpret_cast<const float4 *>(tb.scal));
+        s.mult = q.x, s.step_size = q.y, s.rbc2 = q.z, s.go = __float_as_int(q.w);
         if (!s.go) return;
     } else {
         __shared__ float scalars[2];
