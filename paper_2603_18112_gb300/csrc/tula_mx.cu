@@ -118,10 +118,20 @@ __device__ __forceinline__ unsigned codes8(const float (&x)[8]) {
 // Quantisation
 // ----------------------------------------------------------------------------
 //
-// One CTA per 128 x 128 tile of x, which is one scale tile of x and one of its transpose.  Along
-// the rows four lanes share a block, eight elements each; the transpose reads the tile again from
-// shared memory, a thread per two columns by 32 rows.  HBM bounds it: 2 or 4 bytes in and 17/32
-// out per element and form, against some ten operations.
+// One CTA per 128 x 128 tile of x, which is one scale tile of x and one of its transpose.  Along the
+// rows a thread takes a block whole (16-bit types), so that what there is to do once a block is done
+// once: with four threads to a block the kernel issued in two thirds of all cycles, and 8192 x 8192
+// bf16 took 43 us in both forms instead of 39.  Four threads share a block of fp32, whose 128 bytes a
+// lane would spread each load over 32 lines (39 us for 8192 x 4096, 32 so).  The transpose reads the
+// tile again from shared memory, a thread per 32 rows of one column (fp32) or of two.  HBM bounds it:
+// 2 or 4 bytes in and 17/32 out per element and form, against four to seven operations.
+template <typename T>
+struct Part {
+    static constexpr int kElems = sizeof(T) == 4 ? 8 : 32;  // of a row, that a thread takes at a time
+    static constexpr int kLanes = kBlock / kElems;          // to a block
+    static constexpr int kWords = kElems * (int)sizeof(T) / 4;
+    static constexpr int kSubs = 4 * kLanes;                // to a tile's row
+};
 
 struct QuantArgs {
     const void *x;
@@ -134,11 +144,10 @@ struct QuantArgs {
 // (A kernel may start while the one before it still writes x: nothing of x is read before the wait,
 // which makes it visible, and nothing by the read-only path, which takes it for constant.)
 //
-// Eight elements of a row as they are, 16-bit types in 4 words, fp32 in 8; zero beyond `left` of
-// them.  Aligned: they start at a 16-byte boundary.  Else the 16-byte granules that hold them are
-// loaded, the last also by the next lane, and shifted; inner: all of them lie within the matrix
-// ([begin, end)) and all eight within the row, else granules that reach out of it are loaded element
-// by element.
+// A part's elements as they are, zero beyond `left` of them.  Aligned: they start at a 32-byte
+// boundary.  Else the 16-byte granules that hold them are loaded, an end one also by its neighbour, and
+// shifted; inner: all of them lie within the matrix ([begin, end)) and the part within the row, else
+// granules that reach out of it are loaded element by element.
 template <typename T>
 __device__ __forceinline__ uint4 load_granule(unsigned long long at, unsigned long long begin, unsigned long long end) {
     if (at >= begin && at + 16 <= end) return *reinterpret_cast<const uint4 *>(at);
@@ -157,20 +166,21 @@ __device__ __forceinline__ uint4 load_granule(unsigned long long at, unsigned lo
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 template <typename T, bool Aligned>
-__device__ __forceinline__ void load_row8(unsigned (&w)[sizeof(T) * 2], const T *p, bool inner, long long left,
+__device__ __forceinline__ void load_part(unsigned (&w)[Part<T>::kWords], const T *p, bool inner, long long left,
                                           unsigned long long begin, unsigned long long end) {
-    constexpr int kWords = sizeof(T) * 2;
+    constexpr int kWords = Part<T>::kWords;
     if (!inner && left <= 0) {
 #pragma unroll
         for (int k = 0; k < kWords; ++k) w[k] = 0;
         return;
     }
-    if (Aligned && (inner || left >= 8)) {
+    if (Aligned && (inner || left >= Part<T>::kElems)) {
 #pragma unroll
-        for (int k = 0; k < kWords / 4; ++k) {
-            const uint4 q = __ldcs(reinterpret_cast<const uint4 *>(p) + k);
-            w[4 * k] = q.x, w[4 * k + 1] = q.y, w[4 * k + 2] = q.z, w[4 * k + 3] = q.w;
-        }
+        for (int k = 0; k < kWords; k += 8)
+            asm volatile("ld.global.cs.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=r"(w[k]), "=r"(w[k + 1]), "=r"(w[k + 2]), "=r"(w[k + 3]), "=r"(w[k + 4]), "=r"(w[k + 5]),
+                           "=r"(w[k + 6]), "=r"(w[k + 7])
+                         : "l"(reinterpret_cast<const unsigned *>(p) + k));
         return;
     }
     const unsigned long long at = reinterpret_cast<unsigned long long>(p);
@@ -201,7 +211,7 @@ __device__ __forceinline__ void load_row8(unsigned (&w)[sizeof(T) * 2], const T 
 }
 
 template <typename T>
-__device__ __forceinline__ void floats8(float (&x)[8], const unsigned (&w)[sizeof(T) * 2]) {
+__device__ __forceinline__ void floats8(float (&x)[8], const unsigned *w) {
     if (sizeof(T) == 4) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) x[k] = __uint_as_float(w[k]);
@@ -241,48 +251,69 @@ __device__ __forceinline__ unsigned mul_bf16x2(unsigned a, unsigned b) {
 // inverse_scale as bf16 bits.
 __device__ __forceinline__ unsigned inverse_scale_bf16(unsigned s) { return s == 255u ? 0u : (254u - s) << 7; }
 
-// Eight elements of a row, four lanes to a block, sixteen to the tile's row: their codes; scales:
-// the row's four scale bytes.
+// A part's codes; returns its block's scale byte.
 template <typename T>
-__device__ __forceinline__ unsigned quantize_row8(const unsigned (&w)[sizeof(T) * 2], int sub, unsigned &scales) {
-    unsigned top = 0;
+__device__ __forceinline__ unsigned quantize_part(const unsigned (&w)[Part<T>::kWords], unsigned (&q)[Part<T>::kElems / 8]) {
+    constexpr int kWords = Part<T>::kWords, kEight = kWords / (Part<T>::kElems / 8);
+    constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
+    unsigned tops[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int j = 0; j < (int)sizeof(T) * 2; ++j) top = larger<T>(top, w[j]);
+    for (int j = 0; j < kWords; ++j) tops[j & 3] = larger<T>(tops[j & 3], w[j]);
+    unsigned top = larger<T>(larger<T>(tops[0], tops[1]), larger<T>(tops[2], tops[3]));
     top &= sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu;
-    if (sizeof(T) == 2) top = max(top & 0xffffu, top >> 16);
-    top = max(top, __shfl_xor_sync(kFull, top, 1));
-    top = max(top, __shfl_xor_sync(kFull, top, 2));
-    if (sizeof(T) == 2) top = top_bits<T>(top);
+    if (sizeof(T) == 2) top = top_bits<T>(max(top & 0xffffu, top >> 16));
+#pragma unroll
+    for (int o = 1; o < Part<T>::kLanes; o *= 2) top = max(top, __shfl_xor_sync(kFull, top, o));
     const unsigned s = scale_byte(top);
-    float x[8];
-    if (std::is_same<T, __nv_bfloat16>::value) {
-        // exact in bf16 too (what falls below its range is far below the smallest code)
-        const unsigned f = inverse_scale_bf16(s) * 0x10001u;
-        unsigned v[sizeof(T) * 2];
+    const float f = inverse_scale(s);
+    // exact in bf16 too (what falls below its range is far below the smallest code)
+    const unsigned f2 = inverse_scale_bf16(s) * 0x10001u;
 #pragma unroll
-        for (int j = 0; j < (int)sizeof(T) * 2; ++j) v[j] = mul_bf16x2(w[j], f);
+    for (int k = 0; k < Part<T>::kElems / 8; ++k) {
+        unsigned v[kEight];
+#pragma unroll
+        for (int j = 0; j < kEight; ++j) v[j] = kBf16 ? mul_bf16x2(w[k * kEight + j], f2) : w[k * kEight + j];
+        float x[8];
         floats8<T>(x, v);
-    } else {
-        const float f = inverse_scale(s);
-        floats8<T>(x, w);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = __fmul_rn(x[j], f);
+        for (int j = 0; j < 8; ++j)
+            if (!kBf16) x[j] = __fmul_rn(x[j], f);
+        q[k] = s == 255u ? 0u : codes8(x);
     }
-    scales = s << (8 * (sub >> 2));
-    scales |= __shfl_xor_sync(kFull, scales, 4);
-    scales |= __shfl_xor_sync(kFull, scales, 8);
-    return s == 255u ? 0u : codes8(x);
+    return s;
+}
+// Its codes and, by the block's first lane, its scale byte to where they go: part `sub` of a tile's row.
+template <typename T>
+__device__ __forceinline__ void put_part(const unsigned (&w)[Part<T>::kWords], int row, int sub, bool there, unsigned char *codes,
+                                         unsigned char *scales) {
+    unsigned q[Part<T>::kElems / 8];
+    const unsigned s = quantize_part<T>(w, q);
+    if (sub % Part<T>::kLanes == 0) scales[(row & 31) * 16 + (row >> 5) * 4 + sub / Part<T>::kLanes] = (unsigned char)s;
+    if (!there) return;
+    if constexpr (Part<T>::kElems == 32)
+        *reinterpret_cast<uint4 *>(codes + 16 * sub) = make_uint4(q[0], q[1], q[2], q[3]);
+    else
+        *reinterpret_cast<unsigned *>(codes + 4 * sub) = q[0];
+}
+
+// The tile in shared memory: rows of 128 elements in 16-byte chunks, whose places within 128 bytes are
+// exchanged so that neither the stores of parts nor the column reads (a word a lane, all of one row)
+// meet in a bank.
+template <typename T>
+__device__ __forceinline__ int chunk_place(int row, int chunk) {
+    return sizeof(T) == 4 ? chunk ^ (chunk >> 3 & 3) ^ (row & 1) << 2 : chunk ^ (chunk >> 3) ^ (row & 1) << 1;
 }
 
 // 32 rows (block rb) of word c of a tile in shared memory, that is of one column (fp32) or two:
 // codes to out, `pitch` bytes a column, scale bytes to scales.
-template <typename T>
+template <typename T, bool Swizzled>
 __device__ __forceinline__ void quantize_cols(const unsigned *tile, int c, int rb, unsigned char *out, int pitch,
                                               unsigned char *scales) {
     unsigned w[32], top = 0;
+    const int at[2] = {4 * chunk_place<T>(0, c >> 2) + (c & 3), 4 * chunk_place<T>(1, c >> 2) + (c & 3)};
 #pragma unroll
     for (int k = 0; k < 32; ++k) {
-        w[k] = tile[(32 * rb + k) * (kTile * (int)sizeof(T) / 4) + c];
+        w[k] = tile[(32 * rb + k) * (kTile * (int)sizeof(T) / 4) + (Swizzled ? at[k & 1] : c)];
         top = larger<T>(top, w[k]);
     }
     constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
@@ -336,59 +367,55 @@ struct QuantShape {
 template <typename T, bool Aligned, bool Rows, bool Cols>
 __global__ void __launch_bounds__(QuantShape<T>::kThreads, QuantShape<T>::kCtas) k_quantize(const QuantArgs a) {
     constexpr int kThreads = QuantShape<T>::kThreads;
-    constexpr int kWords = sizeof(T) * 2;          // of eight elements
-    constexpr int kPitch = kTile * sizeof(T) / 4;  // words of a tile's row
-    constexpr int kLoads = kTile * 16 / kThreads;  // of eight elements a thread
+    constexpr int kWords = Part<T>::kWords, kSubs = Part<T>::kSubs;
+    constexpr int kPitch = kTile * sizeof(T) / 4;       // words of a tile's row
+    constexpr int kLoads = kTile * kSubs / kThreads;    // parts a thread
     extern __shared__ __align__(16) unsigned tile[];  // Cols
-    __shared__ __align__(16) unsigned scale_words[2][kTile];
+    __shared__ __align__(16) unsigned char scale_bytes[2][kScaleTile];
     let_next_start();
     wait_for_previous();
     const int tid = threadIdx.x;
     const int tr = blockIdx.x / a.tiles_c, tc = blockIdx.x % a.tiles_c;
     const long long r0 = (long long)tr * kTile, c0 = (long long)tc * kTile;
-    const int sub = tid & 15;  // eight columns of the tile
-    const long long left = a.cols - c0 - 8 * sub;
+    const int sub = tid % kSubs;
     const size_t pitch = (size_t)a.tiles_c * (kTile / 2), pitch_t = (size_t)a.tiles_r * (kTile / 2);
     const unsigned long long begin = reinterpret_cast<unsigned long long>(a.x);
     const unsigned long long end = begin + ((unsigned long long)(a.rows - 1) * a.stride + a.cols) * sizeof(T);
     unsigned w[kLoads][kWords];
-    const T *p0 = static_cast<const T *>(a.x) + (r0 + (tid >> 4)) * a.stride + c0 + 8 * sub;
-    if (c0 + kTile <= a.cols && (Aligned ? r0 + kTile <= a.rows : tr > 0 && r0 + kTile < a.rows)) {
+    const T *p0 = static_cast<const T *>(a.x) + (r0 + tid / kSubs) * a.stride + c0 + Part<T>::kElems * sub;
+    const bool inner = c0 + kTile <= a.cols && (Aligned ? r0 + kTile <= a.rows : tr > 0 && r0 + kTile < a.rows);
+    if (inner) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
-            load_row8<T, Aligned>(w[i], p0 + i * (kThreads / 16) * a.stride, true, 8, begin, end);
+            load_part<T, Aligned>(w[i], p0 + i * (kThreads / kSubs) * a.stride, true, Part<T>::kElems, begin, end);
     } else {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const long long r = r0 + i * (kThreads / 16) + (tid >> 4);
-            load_row8<T, Aligned>(w[i], p0 + i * (kThreads / 16) * a.stride, false, r < a.rows ? left : 0, begin, end);
+            const long long r = r0 + i * (kThreads / kSubs) + tid / kSubs;
+            load_part<T, Aligned>(w[i], p0 + i * (kThreads / kSubs) * a.stride, false,
+                                  r < a.rows ? a.cols - c0 - Part<T>::kElems * sub : 0, begin, end);
         }
     }
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-        const int row = i * (kThreads / 16) + (tid >> 4);
+        const int row = i * (kThreads / kSubs) + tid / kSubs;
         if (Cols) {
 #pragma unroll
             for (int k = 0; k < kWords / 4; ++k)
-                *reinterpret_cast<uint4 *>(&tile[row * kPitch + sub * kWords + 4 * k]) =
+                *reinterpret_cast<uint4 *>(&tile[row * kPitch + 4 * chunk_place<T>(row, sub * (kWords / 4) + k)]) =
                     make_uint4(w[i][4 * k], w[i][4 * k + 1], w[i][4 * k + 2], w[i][4 * k + 3]);
         }
-        if (Rows) {
-            unsigned scales;
-            const unsigned q = quantize_row8<T>(w[i], sub, scales);
-            if (r0 + row < a.rows)
-                *reinterpret_cast<unsigned *>(a.codes + (size_t)(r0 + row) * pitch + c0 / 2 + 4 * sub) = q;
-            if (sub == 0) scale_words[0][(row & 31) * 4 + (row >> 5)] = scales;
-        }
+        if (Rows)
+            put_part<T>(w[i], row, sub, inner || r0 + row < a.rows, a.codes + (size_t)(r0 + row) * pitch + c0 / 2, scale_bytes[0]);
     }
     __syncthreads();
     if (Rows && tid < 32)
         *reinterpret_cast<uint4 *>(a.scales + ((size_t)tr * a.tiles_c + tc) * kScaleTile + 16 * tid) =
-            *reinterpret_cast<const uint4 *>(&scale_words[0][4 * tid]);
+            *reinterpret_cast<const uint4 *>(&scale_bytes[0][16 * tid]);
     if (!Cols) return;
     unsigned char *out = reinterpret_cast<unsigned char *>(tile + kTile * kPitch);
     constexpr int kSide = kPitch;  // words of a row
-    quantize_cols<T>(tile, tid % kSide, tid / kSide, out, kOutPitch, reinterpret_cast<unsigned char *>(scale_words[1]));
+    quantize_cols<T, true>(tile, tid % kSide, tid / kSide, out, kOutPitch, scale_bytes[1]);
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < 4 * kTile / kThreads; ++k) {
@@ -399,12 +426,12 @@ __global__ void __launch_bounds__(QuantShape<T>::kThreads, QuantShape<T>::kCtas)
     }
     if (tid < 32)
         *reinterpret_cast<uint4 *>(a.scales_t + ((size_t)tc * a.tiles_r + tr) * kScaleTile + 16 * tid) =
-            *reinterpret_cast<const uint4 *>(&scale_words[1][4 * tid]);
+            *reinterpret_cast<const uint4 *>(&scale_bytes[1][16 * tid]);
 }
 
 // The same with whole tiles brought by TMA (rows at 16-byte boundaries), persistent: while a tile
-// is quantised the next ones are on their way, so that HBM does not wait for arithmetic.  Both
-// forms are taken from shared memory.
+// is quantised the next ones are on their way, so that HBM does not wait for arithmetic.  For the
+// transpose of any type, and for both forms of fp32 (Rows).
 template <typename T>
 struct QuantRing {
     static constexpr int kThreads = sizeof(T) == 4 ? 512 : 256;
@@ -416,20 +443,18 @@ struct QuantRing {
     static_assert(kCtas * (kSmem + 1024) <= 228 * 1024, "shared memory");
 };
 
-template <typename T, bool Rows, bool Cols>
+template <typename T, bool Rows>
 __global__ void __launch_bounds__(QuantRing<T>::kThreads, QuantRing<T>::kCtas)
     k_quantize_tiles(const __grid_constant__ CUtensorMap map, const QuantArgs a) {
     using R = QuantRing<T>;
-    constexpr int kWords = sizeof(T) * 2;          // of eight elements
     constexpr int kPitch = kTile * sizeof(T) / 4;  // words of a tile's row
     extern __shared__ __align__(16) unsigned tile[];
     __shared__ __align__(8) unsigned long long bars[R::kStages];
     __shared__ volatile int dead;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x;
     unsigned char *base = reinterpret_cast<unsigned char *>(tile) + (-smem_addr(tile) & 127u);
     unsigned char *out = base + R::kStages * R::kTileBytes;
-    unsigned *scale_r = reinterpret_cast<unsigned *>(out + kTile * R::kOut);
-    unsigned char *scale_c = reinterpret_cast<unsigned char *>(scale_r + kTile);
+    unsigned char *scale_c = out + kTile * R::kOut, *scale_r = scale_c + kScaleTile;
     const uint32_t full = smem_addr(bars);
     const int n_tiles = a.tiles_r * a.tiles_c;
     if (tid == 0) {
@@ -448,7 +473,7 @@ __global__ void __launch_bounds__(QuantRing<T>::kThreads, QuantRing<T>::kCtas)
     if (tid == 0)
         for (; fetched < R::kStages && blockIdx.x + fetched * gridDim.x < n_tiles; ++fetched)
             fetch(blockIdx.x + fetched * gridDim.x, fetched);
-    const size_t pitch = (size_t)a.tiles_c * (kTile / 2), pitch_t = (size_t)a.tiles_r * (kTile / 2);
+    const size_t pitch_t = (size_t)a.tiles_r * (kTile / 2);
     int i = 0;
     for (int t = blockIdx.x; t < n_tiles; t += gridDim.x, ++i) {
         const int s = i % R::kStages;
@@ -458,44 +483,39 @@ __global__ void __launch_bounds__(QuantRing<T>::kThreads, QuantRing<T>::kCtas)
         const int tr = t / a.tiles_c, tc = t % a.tiles_c;
         const long long r0 = (long long)tr * kTile, c0 = (long long)tc * kTile;
         if (Rows) {
-            const int sub = lane & 15;
-            constexpr int kRows = kTile / (R::kThreads / 32);  // of a warp
+            constexpr int kSubs = Part<T>::kSubs, kWords = Part<T>::kWords;
+            const int sub = tid % kSubs;
 #pragma unroll
-            for (int k = 0; k < kRows / 2; ++k) {
-                const int row = warp * kRows + 2 * k + (lane >> 4);
-                unsigned w[kWords], scales;
+            for (int k = 0; k < kTile * kSubs / R::kThreads; ++k) {
+                const int row = k * (R::kThreads / kSubs) + tid / kSubs;
+                unsigned w[kWords];
 #pragma unroll
                 for (int j = 0; j < kWords / 4; ++j) {
                     const uint4 q = *reinterpret_cast<const uint4 *>(&x_tile[row * kPitch + sub * kWords + 4 * j]);
                     w[4 * j] = q.x, w[4 * j + 1] = q.y, w[4 * j + 2] = q.z, w[4 * j + 3] = q.w;
                 }
-                const unsigned q = quantize_row8<T>(w, sub, scales);
-                if (r0 + row < a.rows)
-                    *reinterpret_cast<unsigned *>(a.codes + (size_t)(r0 + row) * pitch + c0 / 2 + 4 * sub) = q;
-                if (sub == 0) scale_r[(row & 31) * 4 + (row >> 5)] = scales;
+                put_part<T>(w, row, sub, r0 + row < a.rows, a.codes + (size_t)(r0 + row) * a.tiles_c * (kTile / 2) + c0 / 2, scale_r);
             }
         }
-        if (Cols) quantize_cols<T>(x_tile, tid % kPitch, tid / kPitch, out, R::kOut, scale_c);
+        quantize_cols<T, false>(x_tile, tid % kPitch, tid / kPitch, out, R::kOut, scale_c);
         __syncthreads();  // the tile has been read, its codes and scales are there
         if (tid == 0 && blockIdx.x + fetched * gridDim.x < n_tiles) {
             fetch(blockIdx.x + fetched * gridDim.x, s);
             ++fetched;
         }
-        if (Cols) {
 #pragma unroll
-            for (int k = 0; k < 4 * kTile / R::kThreads; ++k) {
-                const int c = (k * R::kThreads + tid) >> 2, part = tid & 3;
-                if (c0 + c < a.cols)
-                    *reinterpret_cast<uint4 *>(a.codes_t + (size_t)(c0 + c) * pitch_t + r0 / 2 + 16 * part) =
-                        *reinterpret_cast<const uint4 *>(out + c * R::kOut + 16 * part);
-            }
-            if (tid < 32)
-                *reinterpret_cast<uint4 *>(a.scales_t + ((size_t)tc * a.tiles_r + tr) * kScaleTile + 16 * tid) =
-                    *reinterpret_cast<const uint4 *>(scale_c + 16 * tid);
+        for (int k = 0; k < 4 * kTile / R::kThreads; ++k) {
+            const int c = (k * R::kThreads + tid) >> 2, part = tid & 3;
+            if (c0 + c < a.cols)
+                *reinterpret_cast<uint4 *>(a.codes_t + (size_t)(c0 + c) * pitch_t + r0 / 2 + 16 * part) =
+                    *reinterpret_cast<const uint4 *>(out + c * R::kOut + 16 * part);
         }
+        if (tid < 32)
+            *reinterpret_cast<uint4 *>(a.scales_t + ((size_t)tc * a.tiles_r + tr) * kScaleTile + 16 * tid) =
+                *reinterpret_cast<const uint4 *>(scale_c + 16 * tid);
         if (Rows && tid >= 32 && tid < 64)
-            *reinterpret_cast<uint4 *>(a.scales + ((size_t)tr * a.tiles_c + tc) * kScaleTile + 16 * lane) =
-                *reinterpret_cast<const uint4 *>(&scale_r[4 * lane]);
+            *reinterpret_cast<uint4 *>(a.scales + ((size_t)tr * a.tiles_c + tc) * kScaleTile + 16 * (tid - 32)) =
+                *reinterpret_cast<const uint4 *>(scale_r + 16 * (tid - 32));
     }
     // no copy may be in flight when the CTA ends
     if (tid == 0)
@@ -1372,9 +1392,9 @@ template <typename T>
 int launch_quantize_tiles(const QuantArgs &a, unsigned tiles, cudaStream_t s) {
     using R = QuantRing<T>;
     static std::atomic<uint64_t> done[2];
-    void (*k)(const CUtensorMap, const QuantArgs) = k_quantize_tiles<T, false, true>;
+    void (*k)(const CUtensorMap, const QuantArgs) = k_quantize_tiles<T, false>;
     if constexpr (sizeof(T) == 4)  // (16-bit types come here for the transpose alone)
-        if (a.codes) k = k_quantize_tiles<T, true, true>;
+        if (a.codes) k = k_quantize_tiles<T, true>;
     const int rc = allow_smem((const void *)k, R::kSmem, &done[a.codes != nullptr]);
     if (rc) return rc;
     CUtensorMap map;
@@ -1392,13 +1412,13 @@ int quantize_typed(const QuantArgs &a, unsigned grid, cudaStream_t s) {
     const size_t both = reinterpret_cast<uintptr_t>(a.x) | (a.rows > 1 ? (size_t)a.stride * sizeof(T) : 0);
     // Tiles by TMA once every CTA that fits takes two at least (with fewer, one tile a CTA has all of
     // them in flight at once), for fp32's transpose and the transpose of 16-bit types alone: 8192 x
-    // 4096 fp32 takes 32 us in both forms (36 without), bf16 15 us transposed (17).  Forms along the
-    // rows want the warps that the rings leave no room for: bf16 24 us in both forms, 28 by TMA.
+    // 4096 fp32 takes 31 us in both forms (36 without), bf16 15 us transposed (18).  16-bit types' rows
+    // want the warps that the rings leave no room for: 22 us in both forms, 28 by TMA.
     const bool by_tma = a.codes_t && (sizeof(T) == 4 || !a.codes);
     if (both % 16 == 0 && by_tma && (long long)grid >= 2ll * QuantRing<T>::kCtas * sm_count() && a.cols <= 0x7fffff00ll &&
         a.rows <= 0x7fffff00ll)
         return launch_quantize_tiles<T>(a, grid, s);
-    return both % 16 == 0 ? launch_quantize<T, true>(a, grid, s) : launch_quantize<T, false>(a, grid, s);
+    return both % 32 == 0 ? launch_quantize<T, true>(a, grid, s) : launch_quantize<T, false>(a, grid, s);
 }
 
 template <typename T>
