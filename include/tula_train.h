@@ -157,12 +157,17 @@ int tula_mx_matmul(const void *a_codes, const void *a_scales, const void *b_code
                    void *stream);
 
 /*
- * The error word of the products on the current device, read after the work already enqueued on
- * `stream` (the call waits for that stream), then cleared: 0 when every bounded wait inside a
- * product's kernel completed; bit 0 set when one ran out, bit 1 when shared memory did not start where
- * the kernel needs it, and the products since the last read are then not valid.
+ * The error word of these kernels on the current device, read after the work already enqueued on
+ * `stream` (the call waits for that stream), then cleared: 0 when every bounded wait inside the
+ * kernels completed; bit 0 set when one ran out, bit 1 when shared memory did not start where a
+ * product's kernel needs it, and the results since the last read are then not valid.
  */
 int tula_mx_error(void *stream, int *error_out);
+
+/* Failure-detection check: launches, on `stream`, one warp that waits, with the kernels' bound, on a
+ * barrier that nothing arrives on (about two seconds) and records it as they do: tula_mx_error then
+ * reports bit 0.  The CUDA context stays usable. */
+int tula_mx_check_wait_timeout(void *stream);
 
 #ifdef __cplusplus
 }

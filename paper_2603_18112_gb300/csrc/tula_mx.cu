@@ -1299,6 +1299,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     }
 }
 
+// Failure detection: a wait on a barrier that nothing arrives on.
+__global__ void k_mx_wait_check() {
+    __shared__ __align__(8) unsigned long long bar;
+    __shared__ volatile int dead;
+    wait_for_previous();
+    if (threadIdx.x == 0) {
+        mbar_init(smem_addr(&bar), 1);
+        dead = 0;
+    }
+    __syncwarp();
+    mbar_wait(smem_addr(&bar), 0, &dead);
+}
+
 // ----------------------------------------------------------------------------
 // Host side
 // ----------------------------------------------------------------------------
@@ -1586,6 +1599,10 @@ int tula_mx_matmul(const void *a_codes, const void *a_scales, const void *b_code
     if (out_type == TULA_TYPE_F32) return matmul_typed<float>(a_codes, a_scales, b_codes, b_scales, M, N, K, out, s);
     if (out_type == TULA_TYPE_BF16) return matmul_typed<__nv_bfloat16>(a_codes, a_scales, b_codes, b_scales, M, N, K, out, s);
     return matmul_typed<__half>(a_codes, a_scales, b_codes, b_scales, M, N, K, out, s);
+}
+
+int tula_mx_check_wait_timeout(void *stream) {
+    return tula::launch(k_mx_wait_check, dim3(1), 32, 0, static_cast<cudaStream_t>(stream), 1);
 }
 
 int tula_mx_error(void *stream, int *error_out) {

@@ -795,7 +795,8 @@ int tula_train_plan_destroy(tula_train_plan *plan) {
 }
 
 int tula_grad_norm(tula_train_plan *plan, float grad_scale, float max_norm, float *record, void *stream) {
-    if (!plan || !record || !(grad_scale > 0.f) || !(max_norm >= 0.f)) return TULA_ERR_ARG;
+    if (!plan || !record || (reinterpret_cast<uintptr_t>(record) & 3u) || !(grad_scale > 0.f) || !(max_norm >= 0.f))
+        return TULA_ERR_ARG;
     const int rc = check_plan(plan);
     if (rc) return rc;
     NormArgs a = {};

@@ -13,6 +13,7 @@ from __future__ import annotations
 import ctypes
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from .optim import TYPES
 from .tula_ags import _check, _stream_ptr, c_int, c_size_t, c_void_p, lib
@@ -30,6 +31,7 @@ def _lib():
         L.tula_mx_dequantize.argtypes = [c_void_p, c_void_p, _i64, _i64, c_void_p, c_int, c_void_p]
         L.tula_mx_matmul.argtypes = [c_void_p] * 4 + [_i64] * 3 + [c_void_p, c_int, c_void_p]
         L.tula_mx_error.argtypes = [c_void_p, ctypes.POINTER(c_int)]
+        L.tula_mx_check_wait_timeout.argtypes = [c_void_p]
         _fns = L
     return _fns
 
@@ -133,6 +135,10 @@ def quantize(x: torch.Tensor, rows: bool = True, cols: bool = False):
         raise ValueError("quantize: a matrix, and at least one of rows and cols, are wanted")
     r, c = shape
     stride, step = x.stride()
+    if step != 1 and stride == 1 and r > 1 and step >= r:
+        # a transposed matrix lies in memory as its transpose does: each form is the other's of that
+        got = quantize(x.t(), rows=cols, cols=rows)
+        return got[::-1] if rows and cols else got
     # a row of one element, or the only row, may have any stride
     if c > 1 and step != 1 or r > 1 and stride < c:
         x = x.contiguous()
@@ -172,6 +178,12 @@ def matmul(a: MXMatrix, b: MXMatrix, dtype=torch.bfloat16) -> torch.Tensor:
     return out
 
 
+def tula_mx_check_wait_timeout(stream=None) -> None:
+    """Makes a bounded wait of the kernels run out (about two seconds on the GPU): afterwards
+    tula_mx_error reports bit 0."""
+    _check(_lib().tula_mx_check_wait_timeout(_stream_ptr(stream)), "tula_mx_check_wait_timeout")
+
+
 def tula_mx_error(stream=None) -> int:
     """Reads and clears the products' error word after the work on `stream` (synchronous): 0 =
     every wait inside the kernels completed."""
@@ -194,6 +206,7 @@ class _Linear(torch.autograd.Function):
         return matmul(qx, qw, x.dtype)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         xt, wt = ctx.sides
         need_x, need_w = ctx.needs_input_grad

@@ -411,6 +411,32 @@ def test_linear_gradients_against_differences():
 
 
 @pytest.mark.gpu
+def test_linear_of_broadcast_gradients_and_views():
+    """A gradient that is one value broadcast (that of a sum), a weight that is a transposed view, and
+    a second differentiation, which is refused."""
+    x, v = _matrix(70, 96, torch.bfloat16, 42).requires_grad_(), _matrix(96, 50, torch.float32, 43).requires_grad_()
+    mx.linear(x, v.t()).sum().backward()
+    ones = torch.ones(70, 50, dtype=torch.bfloat16, device="cuda")
+    dx, dw = torch.autograd.grad(mx.linear(x, v.t().contiguous()), (x, v), ones)
+    assert torch.equal(x.grad, dx) and torch.equal(v.grad, dw)
+    dx = torch.autograd.grad(mx.linear(x, v.t()).square().sum(), x, create_graph=True)[0]
+    with pytest.raises(RuntimeError):
+        dx.sum().backward()
+
+
+@pytest.mark.gpu
+def test_a_wait_that_runs_out_is_reported():
+    """Failure detection without a fault: the check's wait runs out (about two seconds), the word
+    reports it once, and products go on."""
+    assert mx.tula_mx_error() == 0
+    mx.tula_mx_check_wait_timeout()
+    a = mx.quantize(_matrix(5, 64, torch.float32, 44))
+    out = mx.matmul(a, a, torch.float32)
+    assert mx.tula_mx_error() == 1 and mx.tula_mx_error() == 0
+    assert torch.equal(out, mx.matmul(a, a, torch.float32))
+
+
+@pytest.mark.gpu
 def test_linear_of_more_dimensions_and_on_another_stream():
     x, w = _matrix(6 * 35, 96, torch.bfloat16, 40).view(6, 35, 96), _matrix(50, 96, torch.float32, 41)
     want = mx.linear(x.view(-1, 96), w)

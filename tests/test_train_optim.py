@@ -284,6 +284,44 @@ def test_adamw(name, layout, gdtype, copies, max_norm, scale):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("offsets", [(0, 1, 0, 0, 0), (1, 2, 3, 4, 5), (0, 0, 0, 0, 1), (4, 0, 4, 4, 4)])
+@pytest.mark.parametrize("max_norm", [0.0, 0.5])
+@pytest.mark.parametrize("sizes", [[1, 7, 3000], [2_600_000, 5, 20_001]])
+def test_adamw_of_buffers_at_offsets_of_their_own(offsets, max_norm, sizes):
+    """Weights, gradients, moments and copies that start at different elements of eight: the results are
+    those of buffers that lie alike, up to the norm's order of addition."""
+    def at(off, xs):
+        flat = torch.zeros(sum(sizes) + 8, dtype=xs[0].dtype, device="cuda")
+        out, i = [], off
+        for x in xs:
+            flat[i:i + x.numel()] = x
+            out.append(flat[i:i + x.numel()])
+            i += x.numel()
+        return out
+
+    base = _adam_state(sizes, torch.bfloat16, "padded", torch.bfloat16, 16)
+    moved = [at(o, xs) for o, xs in zip(offsets, base)]
+    steps = []
+    for w, g, m, v, c in (base, moved):
+        step = O.AdamWStep(w, g, m, v, copies=c, max_norm=max_norm)
+        step(1e-2, (0.9, 0.98), 1e-8, 0.1)
+        steps.append(step)
+    if max_norm:
+        a, b = (s.record.tolist() for s in steps)
+        assert a[0] == pytest.approx(b[0], rel=2 * NORM_TOL)
+    for i in range(len(sizes)):
+        (w, g, m, v, c), (w2, g2, m2, v2, c2) = ([r[i] for r in s] for s in (base, moved))
+        if max_norm == 0.0:
+            assert torch.equal(w, w2) and torch.equal(m, m2) and torch.equal(v, v2) and torch.equal(c, c2)
+        else:
+            for x, y in ((w, w2), (m, m2), (v, v2)):
+                # coefficients 4 NORM_TOL apart, of which a moment's square takes twice as much
+                assert bool(((x - y).abs() <= (8 * NORM_TOL + 8 * U) * (x.abs() + 0.05)).all())
+            assert torch.equal(c2, w2.bfloat16())
+        assert torch.equal(g, g2)
+
+
+@pytest.mark.gpu
 def test_adamw_matches_torch_from_the_first_step():
     """Zero moments, steps from 1 on, the defaults of torch.optim.AdamW."""
     gen = torch.Generator(device="cuda").manual_seed(3)
