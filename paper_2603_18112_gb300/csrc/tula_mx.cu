@@ -789,7 +789,7 @@ __device__ __forceinline__ uint32_t in_cta(uint32_t addr, unsigned rank) {
 }
 __device__ __forceinline__ float load_cluster(uint32_t addr) {
     float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr));  // (no fence for the others)
     return v;
 }
 __device__ __forceinline__ float4 load_cluster4(uint32_t addr) {
@@ -980,13 +980,25 @@ __global__ void __launch_bounds__(kMmaThreads) k_matmul(const __grid_constant__ 
     const bool vec = a.ld % 4 == 0 && (reinterpret_cast<uintptr_t>(a.out) & (4 * sizeof(T) - 1)) == 0;
     const int n_lines = min(share, lines - first);
     if (!vec) {
-        for (int o = first + warp; o < first + n_lines; o += kMmaThreads / 32)
-            for (int n = lane; n < line; n += 32) {
-                const uint32_t at = stages + 4 * (o * S::kPitch + n);
-                float sum = load_cluster(in_cta(at, 0));
-                for (int r = 1; r < a.split; ++r) sum = __fadd_rn(sum, load_cluster(in_cta(at, r)));
-                put(out + (line0 + o) * a.ld + col0 + n, sum);
+        constexpr int kPer = S::kLine / 32;
+        for (int o = first + warp; o < first + n_lines; o += kMmaThreads / 32) {
+            float sum[kPer];
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) sum[k] = 0.f;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                if (r >= a.split) break;
+                const uint32_t at = in_cta(stages + 4 * (o * S::kPitch + lane), r);
+#pragma unroll
+                for (int k = 0; k < kPer; ++k) {
+                    const float v = load_cluster(at + 128 * k);
+                    sum[k] = r ? __fadd_rn(sum[k], v) : v;
+                }
             }
+#pragma unroll
+            for (int k = 0; k < kPer; ++k)
+                if (lane + 32 * k < line) put(out + (line0 + o) * a.ld + col0 + lane + 32 * k, sum[k]);
+        }
     }
     constexpr int kQuads = S::kLine / 4;
     for (int i = tid; vec && i < n_lines * kQuads; i += kMmaThreads) {
@@ -1050,7 +1062,7 @@ struct PairArgs {
     long long M, N;
     int tiles_k;
     int tiles_m, tiles_n;  // of 256
-    int vec;               // out's rows at 16-byte boundaries: stored by TMA
+    int word;              // bytes that divide out's address and rows: 16 (stored by TMA), 8, 4 or 2
 };
 
 __device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
@@ -1089,6 +1101,36 @@ __device__ __forceinline__ void tile_at(int t, const PairArgs &a, int &tm, int &
     const int rows = min(kBand, a.tiles_m - band * kBand);
     tm = band * kBand + in % rows;
     tn = in / rows;
+}
+
+// 32 rows of 128 bytes from a warp's buffer to out, W bytes a lane; `here` bytes of each row, `rows` of
+// them.  Eight rows are read before any is stored.  (16-bit elements in pairs from odd places took twice
+// the time: lanes at the ends part ways.)
+template <int W>
+__device__ __forceinline__ void store_rows(const unsigned char *buffer, unsigned char *to, long long pitch, int here, int rows) {
+    using Word = std::conditional_t<W == 8, uint2, std::conditional_t<W == 4, unsigned, unsigned short>>;
+    constexpr int kLanes = W == 8 ? 16 : 32;           // to a row
+    constexpr int kPer = 128 / (kLanes * W);           // words a lane takes of it
+    constexpr int kAtOnce = 32 / kLanes, kStep = 8 / kAtOnce;
+    const int lane = threadIdx.x & 31, byte = lane % kLanes * W;
+    for (int r0 = 0; r0 < 32; r0 += 8) {
+        Word u[kStep][kPer];
+#pragma unroll
+        for (int j = 0; j < kStep; ++j)
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) {
+                const int r = r0 + j * kAtOnce + (kAtOnce > 1 ? lane / kLanes : 0);
+                u[j][k] = *reinterpret_cast<const Word *>(buffer + r * 128 + ((byte + 32 * W * k) ^ ((r & 7) << 4)));
+            }
+#pragma unroll
+        for (int j = 0; j < kStep; ++j) {
+            const int r = r0 + j * kAtOnce + (kAtOnce > 1 ? lane / kLanes : 0);
+            unsigned char *p = to + r * pitch + byte;
+#pragma unroll
+            for (int k = 0; k < kPer; ++k)
+                if (byte + 32 * W * k < here && r < rows) *reinterpret_cast<Word *>(p + 32 * W * k) = u[j][k];
+        }
+    }
 }
 
 template <typename T>
@@ -1211,7 +1253,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     } else {
         const int quad = warp & 3;
         constexpr int kChunk = 128 / (int)sizeof(T);  // columns of 128 bytes of out
-        T *out = static_cast<T *>(a.out);
         int n = 0;
         for (int t = pair; t < n_tiles; t += pairs, ++n) {
             int tm, tn;
@@ -1237,7 +1278,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
                 }
 #pragma unroll
                 for (int k = 0; k < kChunk; ++k) put(&y[k], __uint_as_float(v[k]));
-                if (a.vec) {  // the last store has read the buffer
+                if (a.word == 16) {  // the last store has read the buffer
                     if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                     __syncwarp();
                 }
@@ -1249,7 +1290,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
                                  : "memory");
                 }
                 const long long c0 = (long long)tn * 256 + col;
-                if (a.vec) {
+                if (a.word == 16) {
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                     if (lane == 0) {
@@ -1261,28 +1302,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
                     }
                 } else {
                     __syncwarp();
-                    const int here = (int)max(0ll, min((long long)kChunk, a.N - c0));
-                    // Element by element along the rows (in pairs, at 4-byte boundaries where there are
-                    // any, it took twice the time: lanes at the ends part ways); eight rows are read
-                    // before any is stored.
-                    constexpr int kPer = kChunk / 32;
-                    const unsigned char *mine = all + (at - stages);
-                    for (int r0 = 0; r0 < 32; r0 += 8) {
-                        T u[8][kPer];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
-#pragma unroll
-                            for (int k = 0; k < kPer; ++k)
-                                u[j][k] = *reinterpret_cast<const T *>(
-                                    mine + (r0 + j) * 128 + (((lane + 32 * k) * (int)sizeof(T)) ^ ((r0 + j & 7) << 4)));
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            T *to = out + (row0 + r0 + j) * a.N + c0 + lane;
-#pragma unroll
-                            for (int k = 0; k < kPer; ++k)
-                                if (lane + 32 * k < here && row0 + r0 + j < a.M) to[32 * k] = u[j][k];
-                        }
-                    }
+                    const int here = (int)max(0ll, min((long long)kChunk, a.N - c0)) * (int)sizeof(T);
+                    const int rows = (int)max(0ll, min(32ll, a.M - row0));
+                    const long long pitch = a.N * (long long)sizeof(T);
+                    unsigned char *to = static_cast<unsigned char *>(a.out) + row0 * pitch + c0 * (long long)sizeof(T);
+                    const unsigned char *buffer = all + (at - stages);
+                    if (a.word == 8)
+                        store_rows<8>(buffer, to, pitch, here, rows);
+                    else if (a.word == 4)
+                        store_rows<4>(buffer, to, pitch, here, rows);
+                    else if (sizeof(T) == 2)
+                        store_rows<2>(buffer, to, pitch, here, rows);
                     __syncwarp();
                 }
             }
@@ -1513,13 +1543,14 @@ int matmul_large(const void *a_codes, const void *a_scales, const void *b_codes,
     a.tiles_k = (int)up(K, kTile);
     a.tiles_m = (int)up(M, 256);
     a.tiles_n = (int)up(N, 256);
-    a.vec = aligned(out, 16) && N * (long long)sizeof(T) % 16 == 0;
+    const unsigned long long both = reinterpret_cast<unsigned long long>(out) | (unsigned long long)(N * (long long)sizeof(T));
+    a.word = both % 16 == 0 ? 16 : both % 8 == 0 ? 8 : both % 4 == 0 ? 4 : 2;
     CUtensorMap ma, mb, sa, sb, mo;
     std::memset(&mo, 0, sizeof(mo));
     const CUtensorMapDataType type = sizeof(T) == 4 ? CU_TENSOR_MAP_DATA_TYPE_UINT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16;
     if (!codes_map(&ma, a_codes, M, a.tiles_k, 128) || !codes_map(&mb, b_codes, N, a.tiles_k, 128) ||
         !scales_map(&sa, a_scales, M, a.tiles_k, 1) || !scales_map(&sb, b_scales, N, a.tiles_k, 2) ||
-        (a.vec && !make_map(&mo, type, out, M, N, N * (long long)sizeof(T), 32, 128 / (int)sizeof(T), CU_TENSOR_MAP_SWIZZLE_128B)))
+        (a.word == 16 && !make_map(&mo, type, out, M, N, N * (long long)sizeof(T), 32, 128 / (int)sizeof(T), CU_TENSOR_MAP_SWIZZLE_128B)))
         return cuda_failed(cudaErrorInvalidValue);
     static std::atomic<uint64_t> done;
     const int rc = allow_smem((const void *)k_matmul_pair<T>, Pair::kSmem, &done);
