@@ -285,7 +285,10 @@ def _check_product(a, b, dtype):
 MNK = [(1, 1, 1), (1, 16, 32), (1, 4096, 4096), (3, 5, 7), (16, 128, 256), (17, 100, 300), (33, 130, 128),
        (64, 257, 512), (65, 300, 384), (128, 128, 128), (128, 1000, 2048), (129, 128, 640), (200, 1, 1000),
        (300, 70, 96), (256, 256, 256), (257, 511, 1025), (1000, 999, 4097), (2048, 1024, 512), (4096, 2, 64),
-       (130, 8200, 160), (513, 1536, 8192)]
+       (130, 8200, 160), (513, 1536, 8192),
+       # pairs of CTAs, for short and for long sums, rows at every alignment
+       (2100, 2304, 100), (2049, 2561, 1024), (3000, 2500, 640), (2048, 2504, 1152), (1100, 3001, 2050),
+       (2500, 2306, 1500), (5000, 136, 4100)]
 
 
 @pytest.mark.gpu
@@ -298,7 +301,7 @@ def test_matmul(M, N, K):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("M,N,K", [(5, 40, 96), (128, 384, 256), (300, 260, 1100)])
+@pytest.mark.parametrize("M,N,K", [(5, 40, 96), (128, 384, 256), (300, 260, 1100), (2050, 2400, 512), (2050, 2400, 2000)])
 def test_matmul_exact(M, N, K):
     """Small integers: every sum is exact, so the product has to be, in every place."""
     gen = torch.Generator(device="cuda").manual_seed(9)
