@@ -45,7 +45,7 @@ typedef struct tula_train_tensors {
 } tula_train_tensors;
 
 /* Bytes of device workspace a plan over these sizes needs (host only): 64 to 72 per tile of 2048
- * elements (up to about 2.5 M elements in all) or 8192, and for what is left of each tensor. */
+ * elements (up to about 2.5 M elements in all) or 4096, and for what is left of each tensor. */
 int tula_train_workspace_size(const int64_t *numels, int n_tensors, size_t *bytes);
 
 /*
@@ -74,7 +74,8 @@ int tula_train_plan_destroy(tula_train_plan *plan);
  * are read only.  Squares are summed in fp32 within 32 elements of a thread and its warp (with an
  * exact power of two taken out where they would overflow or underflow, so that the norm holds over
  * the whole range of the types) and in fp64 beyond, in an order that depends on the sizes and
- * alignments only.  An infinity in the gradients gives inf, a NaN gives NaN.
+ * alignments only.  An infinity in the gradients gives inf, a NaN gives NaN.  grad_scale lies in
+ * [2^-100, 2^100].
  */
 int tula_grad_norm(tula_train_plan *plan, float grad_scale, float max_norm, float *record,
                    void *stream);
@@ -107,8 +108,8 @@ void tula_adamw_default_hparams(tula_adamw_hparams *hp);
  *   w = w (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
  * and the copies w rounded to their type.  Gradients are read only (clipping does not write them).
  * The norm is taken, and the record written, only with a max_norm or skip_nonfinite.
- * 0 <= beta < 1; TULA_ERR_ARG for other values, for NaN, for grad_scale <= 0, lr, eps, weight_decay or
- * max_norm < 0, and for a plan without weights.
+ * 0 <= beta < 1; TULA_ERR_ARG for other values, for NaN, for grad_scale outside [2^-100, 2^100], lr, eps,
+ * weight_decay or max_norm < 0, and for a plan without weights.
  */
 int tula_adamw_step(tula_train_plan *plan, const tula_adamw_hparams *hp, void *stream);
 
