@@ -123,6 +123,10 @@ struct Raw {
         if (kWide) b |= (w[kWide ? 4 : 0] | w[kWide ? 5 : 0]) | (w[kWide ? 6 : 0] | w[kWide ? 7 : 0]);
         return kWide ? b : b | b << 16;
     }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (unsigned &u : w) u = 0;
+    }
     // element k from index i, or 0
     __device__ __forceinline__ void set(int k, unsigned long long base, int i, bool there) {
         if (kWide) {
@@ -316,18 +320,32 @@ __device__ __forceinline__ double sum_fan(const double *p, int n) {
     return v[0];
 }
 
-// Vector j of a thread's of a tile, elements that are not the tensor's as 0.
+// Of a tile whose tensor begins or ends within a vector, the one vector at each end that is the tensor's
+// in part: whether vector j of this thread is one.  The others are whole or not the tensor's at all.
+template <int VPT>
+__device__ __forceinline__ bool in_part(const Row &row, int j) {
+    const int i = (j * kThreadsOf<VPT> + (int)threadIdx.x) * kVec;
+    return row.vec && !(i >= row.lo && i + kVec <= row.hi) && i + kVec > row.lo && i < row.hi;
+}
+// Vector j of a thread's of a tile; 0 unless it is whole.
 template <int VPT, int Type>
-__device__ __forceinline__ void load_part(Raw<Type> &raw, const Row &row, int j) {
-    constexpr int kThreads = kThreadsOf<VPT>;
-    const int tid = threadIdx.x, i = (j * kThreads + tid) * kVec;
-    if (row.vec && i >= row.lo && i + kVec <= row.hi) {
+__device__ __forceinline__ bool load_whole(Raw<Type> &raw, const Row &row, int j) {
+    const int i = (j * kThreadsOf<VPT> + (int)threadIdx.x) * kVec;
+    const bool whole = row.vec && i >= row.lo && i + kVec <= row.hi;
+    if (whole)
         raw.load(row.g, i);
-        return;
-    }
+    else
+        raw.clear();
+    return whole;
+}
+// Vector j element by element, those that are not the tensor's as 0.
+template <int VPT, int Type>
+__device__ __forceinline__ void load_elements(Raw<Type> &raw, const Row &row, int j) {
+    constexpr int kThreads = kThreadsOf<VPT>;
+    const int tid = threadIdx.x;
 #pragma unroll
     for (int k = 0; k < kVec; ++k) {
-        const int e = row.vec ? i + k : (j * kVec + k) * kThreads + tid;
+        const int e = row.vec ? (j * kThreads + tid) * kVec + k : (j * kVec + k) * kThreads + tid;
         raw.set(k, row.g, e, e >= row.lo && e < row.hi);
     }
 }
@@ -337,28 +355,37 @@ __device__ __forceinline__ void load_part(Raw<Type> &raw, const Row &row, int j)
 template <int VPT, int Type>
 __device__ __forceinline__ double tile_sum(const Row &row) {
     constexpr int kThreads = kThreadsOf<VPT>;
-    const int tid = threadIdx.x;
+    // vectors at a time: 64 bytes a thread (the registers of 128 would spill)
+    constexpr int kAtOnce = Raw<Type>::kWide && VPT > 1 ? VPT / 2 : VPT;
+    const bool full = row.vec && row.lo == 0 && row.hi == VPT * kThreads * kVec;
     float s = 0.f;
     unsigned bits = 0;
-    if (row.vec && row.lo == 0 && row.hi == VPT * kThreads * kVec) {
-        Raw<Type> raw[VPT];
-#pragma unroll
-        for (int j = 0; j < VPT; ++j) raw[j].load(row.g, (j * kThreads + tid) * kVec);
-        s = square_sum(raw, bits);
-    } else {
 #pragma unroll 1
-        for (int j = 0; j < VPT; ++j) {
-            Raw<Type> raw[1];
-            load_part<VPT>(raw[0], row, j);
-            s = __fadd_rn(s, square_sum(raw, bits));
+    for (int j0 = 0; j0 < VPT; j0 += kAtOnce) {
+        Raw<Type> raw[kAtOnce];
+        if (full) {
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) raw[j].load(row.g, ((j0 + j) * kThreads + (int)threadIdx.x) * kVec);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) load_whole<VPT>(raw[j], row, j0 + j);
         }
+        s = __fadd_rn(s, square_sum(raw, bits));
     }
+    if (!row.vec || row.lo % kVec || row.hi % kVec)
+#pragma unroll 1
+        for (int j = 0; j < VPT; ++j)
+            if (!row.vec || in_part<VPT>(row, j)) {
+                Raw<Type> one[1];
+                load_elements<VPT>(one[0], row, j);
+                s = __fadd_rn(s, square_sum(one, bits));
+            }
     double d = 0.0;
     if (!safe(s, bits)) {
 #pragma unroll 1
         for (int j = 0; j < VPT; ++j) {
             Raw<Type> raw;
-            load_part<VPT>(raw, row, j);
+            if (!load_whole<VPT>(raw, row, j)) load_elements<VPT>(raw, row, j);
             d += scaled_sum(raw, s);
         }
         s = 0.f;
@@ -438,38 +465,25 @@ template <int VPT, int Type>
 __device__ __forceinline__ void tile_scale(const Row &row, float c) {
     constexpr int kThreads = kThreadsOf<VPT>;
     const int tid = threadIdx.x;
-    const unsigned long long g = row.g;
-    if (row.vec && row.lo == 0 && row.hi == VPT * kThreads * kVec) {
-        Raw<Type> raw[VPT];
+    Raw<Type> raw[VPT];
+    bool whole[VPT];
 #pragma unroll
-        for (int j = 0; j < VPT; ++j) raw[j].load(g, (j * kThreads + tid) * kVec);
+    for (int j = 0; j < VPT; ++j) whole[j] = load_whole<VPT>(raw[j], row, j);
 #pragma unroll
-        for (int j = 0; j < VPT; ++j) {
-            float x[kVec];
-            raw[j].floats(x);
+    for (int j = 0; j < VPT; ++j) {
+        float x[kVec];
+        raw[j].floats(x);
 #pragma unroll
-            for (int k = 0; k < kVec; ++k) x[k] = __fmul_rn(x[k], c);
-            store8(x, g, Type, (j * kThreads + tid) * kVec);
-        }
-    } else if (row.vec) {
-        for (int j = 0; j < VPT; ++j) {
-            const int i = (j * kThreads + tid) * kVec;
-            if (i >= row.lo && i + kVec <= row.hi) {
-                float x[kVec];
-                load8(x, g, Type, i);
-#pragma unroll
-                for (int k = 0; k < kVec; ++k) x[k] = __fmul_rn(x[k], c);
-                store8(x, g, Type, i);
-            } else {
-                for (int k = 0; k < kVec; ++k)
-                    if (i + k >= row.lo && i + k < row.hi) scale1(g, Type, i + k, c);
-            }
-        }
-    } else {
-#pragma unroll 8
-        for (int k = 0; k < VPT * kVec; ++k) {
-            const int i = k * kThreads + tid;
-            if (i < row.hi) scale1(g, Type, i, c);
+        for (int k = 0; k < kVec; ++k) x[k] = __fmul_rn(x[k], c);
+        if (whole[j]) store8(x, row.g, Type, (j * kThreads + tid) * kVec);
+    }
+    if (row.vec && row.lo % kVec == 0 && row.hi % kVec == 0) return;
+#pragma unroll 1
+    for (int j = 0; j < VPT; ++j) {
+        if (row.vec && !in_part<VPT>(row, j)) continue;
+        for (int k = 0; k < kVec; ++k) {
+            const int e = row.vec ? (j * kThreads + tid) * kVec + k : (j * kVec + k) * kThreads + tid;
+            if (e >= row.lo && e < row.hi) scale1(row.g, Type, e, c);
         }
     }
 }
