@@ -1038,9 +1038,10 @@ __global__ void __launch_bounds__(kMmaThreads) k_matmul(const __grid_constant__ 
 //
 // Two CTAs of a cluster compute a tile of 256 rows of A by 256 of B with one instruction stream
 // (cta_group::2): each holds its 128 rows of A, 128 of the 256 rows of B, and its 128 rows of
-// accumulators.  A stage of 256 columns is 35 KB a CTA for 2 x 128 x 256 x 256 operations, twice
-// the operations a byte of 128 x 128 tiles, whose traffic from L2 (15 TB/s) bounded them.
-// Persistent: a pair takes every n-th tile.  Tensor memory has 512 columns: two accumulators of
+// accumulators.  A stage of 256 columns is 35.8 KB a CTA for 2 x 128 x 256 x 256 operations, twice
+// the operations a byte of 128 x 128 tiles; an SM takes in 64 bytes a clock, which bounds 8192^3 at
+// 135 us (149 measured, the tensor pipe active 78 % of it).  Products with short sums are bound by
+// writing (16384 x 16384 x 512: 143 us, fill_ of as much 136).  Persistent: a pair takes every n-th tile.  Tensor memory has 512 columns: two accumulators of
 // 256 that overlap in 32, and the scales' 24.  Four warps read an accumulator back, the columns that
 // the other one needs first, while the next tile's instructions run.
 
@@ -1398,8 +1399,15 @@ bool make_map(CUtensorMap *m, CUtensorMapDataType type, const void *base, long l
     if (!fn) return false;
     const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch};
     const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, steps[2] = {1, 1};
-    return fn(m, type, 2, const_cast<void *>(base), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
-              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    auto encode = [&] {
+        return fn(m, type, 2, const_cast<void *>(base), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    };
+    if (encode()) return true;
+    // The driver's call wants a current context, which a thread whose first call this is (autograd's, for
+    // a backward pass) has only once the runtime is told of its device.
+    int dev = 0;
+    return cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess && encode();
 }
 // Codes in boxes of 128 bytes by box_rows rows.
 bool codes_map(CUtensorMap *m, const void *codes, long long rows, int tiles_k, int box_rows) {
@@ -1453,13 +1461,14 @@ int launch_quantize_tiles(const QuantArgs &a, unsigned tiles, cudaStream_t s) {
 template <typename T>
 int quantize_typed(const QuantArgs &a, unsigned grid, cudaStream_t s) {
     const size_t both = reinterpret_cast<uintptr_t>(a.x) | (a.rows > 1 ? (size_t)a.stride * sizeof(T) : 0);
-    // Tiles by TMA once every CTA that fits takes two at least (with fewer, one tile a CTA has all of
-    // them in flight at once), for fp32's transpose and the transpose of 16-bit types alone: 8192 x
-    // 4096 fp32 takes 31 us in both forms (36 without), bf16 15 us transposed (18).  16-bit types' rows
-    // want the warps that the rings leave no room for: 22 us in both forms, 28 by TMA.
-    const bool by_tma = a.codes_t && (sizeof(T) == 4 || !a.codes);
-    if (both % 16 == 0 && by_tma && (long long)grid >= 2ll * QuantRing<T>::kCtas * sm_count() && a.cols <= 0x7fffff00ll &&
-        a.rows <= 0x7fffff00ll)
+    // Tiles by TMA for the transpose alone (us: 2048 x 1024 fp32 2.5, 3.6 without; 4096 x 4096 8.1 and 10.9;
+    // 8192 x 4096 bf16 10.9 and 14.9), and for both forms of fp32 up to a tile an SM (2048 x 1024 3.3
+    // and 4.5) and from eight on (8192 x 4096 29 and 32); between them what comes from L2 needs no
+    // ring (4096 x 2048 8.6 and 8.0).  16-bit types' rows want the warps that the rings leave no room for:
+    // 8192 x 4096 takes 22 us in both forms, 28 by TMA.
+    const int sms = sm_count();
+    const bool by_tma = a.codes_t && (!a.codes || (sizeof(T) == 4 && ((int)grid <= sms || (long long)grid >= 8ll * sms)));
+    if (both % 16 == 0 && by_tma)
         return launch_quantize_tiles<T>(a, grid, s);
     return both % 32 == 0 ? launch_quantize<T, true>(a, grid, s) : launch_quantize<T, false>(a, grid, s);
 }
@@ -1497,7 +1506,8 @@ int launch_matmul(const CUtensorMap &mp, const CUtensorMap &mq, const MatmulArgs
 template <typename T>
 int matmul_small(const void *a_codes, const void *a_scales, const void *b_codes, const void *b_scales, long long M, long long N,
                  long long K, void *out, cudaStream_t s) {
-    // The operand with few rows is the instruction's N, so that its 128 rows are not padding.
+    // The operand with few rows is the instruction's N, so that its 128 rows are not padding; N as small as
+    // they are (16 x 4096 x 4096: 4.4 us with 32, 6.1 with 128; 48 x 4096 x 25088: 9.3 with 64, 10.0).
     const bool swap = M <= 128;
     MatmulArgs a;
     a.p_scales = static_cast<const unsigned char *>(swap ? b_scales : a_scales);
@@ -1563,8 +1573,9 @@ int matmul_large(const void *a_codes, const void *a_scales, const void *b_codes,
 template <typename T>
 int matmul_typed(const void *a_codes, const void *a_scales, const void *b_codes, const void *b_scales, long long M, long long N,
                  long long K, void *out, cudaStream_t s) {
-    // Pairs of CTAs from half as many tiles of 256 x 256 as there are pairs on.
-    if (K > 0 && M > 128 && N > 128 && up(M, 256) * up(N, 256) >= 38)
+    // Pairs of CTAs from 32 tiles of 256 x 256 on: 1024 x 2048 x 4096 takes 9.5 us (10.3 by tiles of 128),
+    // 2048 x 4096 x 512 8.5 (10.6); 1024 x 1024 x 4096, 16 tiles, 9.4 (9.1).
+    if (K > 0 && M > 128 && N > 128 && up(M, 256) * up(N, 256) >= 32)
         return matmul_large<T>(a_codes, a_scales, b_codes, b_scales, M, N, K, out, s);
     return matmul_small<T>(a_codes, a_scales, b_codes, b_scales, M, N, K, out, s);
 }

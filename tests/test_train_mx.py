@@ -339,6 +339,31 @@ def test_nan_blocks_and_empty_sums(M):
 
 
 @pytest.mark.gpu
+def test_calls_from_a_thread_that_has_made_none():
+    """The first CUDA call of a thread is a product, a transpose's quantisation, a clipping."""
+    import threading
+    x = _matrix(600, 256, torch.float32, 61)
+    a = mx.quantize(x)
+    want = [mx.matmul(a, a), mx.quantize(x, rows=False, cols=True).codes]
+    torch.cuda.synchronize()
+    got, errors = [None, None], []
+
+    def run(i, fn):
+        try:
+            got[i] = fn()
+            torch.cuda.synchronize()
+        except Exception as e:  # noqa: BLE001
+            errors.append(e)
+
+    for i, fn in enumerate((lambda: mx.matmul(a, a), lambda: mx.quantize(x, rows=False, cols=True).codes)):
+        t = threading.Thread(target=run, args=(i, fn))
+        t.start()
+        t.join()
+    assert not errors
+    assert all(torch.equal(u, v) for u, v in zip(want, got))
+
+
+@pytest.mark.gpu
 def test_matmul_refusals():
     a, b = mx.quantize(_matrix(4, 64, torch.float32, 7)), mx.quantize(_matrix(4, 96, torch.float32, 8))
     with pytest.raises(ValueError):
