@@ -39,24 +39,58 @@ def _lib():
 _raw_stream, _get_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
+_unfreed: list = []  # blocks that were dropped while another stream may read them
+
+
+def _free_after_readers(delete):
+    """Gives such blocks back once their own streams, whose next allocations may get them, wait for the
+    readers.  Streams under capture cannot wait so; their blocks stay for the next call."""
+    for block in list(_unfreed):
+        ptr, device, own, readers = block
+        own, *readers = [torch.cuda.ExternalStream(s, device) if s else torch.cuda.default_stream(device)
+                         for s in (own, *readers)]
+        capturing = False
+        for s in (own, *readers):
+            with torch.cuda.stream(s):
+                capturing = capturing or torch.cuda.is_current_stream_capturing()
+        if capturing:
+            continue
+        for s in readers:
+            own.wait_stream(s)
+        _unfreed.remove(block)
+        delete(ptr)
+
+
 class _Block:
     """Device memory from torch's allocator, for the current device and stream, without a tensor around
     it: with torch.empty ahead of it a launch takes the host 7.5 us on a GB300 machine, with this 3.5."""
 
-    __slots__ = ("ptr", "size")
+    __slots__ = ("ptr", "size", "device", "stream", "readers")
 
     def __init__(self, size: int, device: int, _alloc=torch._C._cuda_cudaCachingAllocator_raw_alloc):
-        self.ptr = 0
+        self.ptr, self.size, self.device, self.readers = 0, size, device, None
+        self.stream = stream = _raw_stream(device)
         if size and device == _get_device():
-            self.ptr = _alloc(size, _raw_stream(device))
+            self.ptr = _alloc(size, stream)
         elif size:
             with torch.cuda.device(device):
-                self.ptr = _alloc(size, _raw_stream(device))
-        self.size = size
+                self.ptr = _alloc(size, stream)
+
+    def read_elsewhere(self, stream: int):
+        """The device's current stream, which is not the block's own, is about to read the block.  (What a
+        graph reads has to live as long as the graph: its streams hold no work to wait for.)"""
+        with torch.cuda.device(self.device):
+            if not torch.cuda.is_current_stream_capturing():
+                self.readers = (self.readers or set()) | {stream}
 
     def __del__(self, _delete=torch._C._cuda_cudaCachingAllocator_raw_delete):
-        if self.ptr:
+        if not self.ptr:
+            return
+        if self.readers is None:
             _delete(self.ptr)
+        else:
+            _unfreed.append((self.ptr, self.device, self.stream, self.readers))
+            _free_after_readers(_delete)
 
     @property
     def __cuda_array_interface__(self):
@@ -67,7 +101,9 @@ class MXMatrix:
     """A rows x cols matrix in MXFP4: ``codes`` uint8 [rows, P / 2] and ``scales`` uint8
     [ceil(rows / 128), P / 128, 32, 4, 4], P = cols rounded up to a multiple of 128; of any shapes
     of those sizes, contiguous, on one GPU.  Not to be changed once made.  Its memory belongs to the
-    stream it was made on, as a tensor's does."""
+    stream it was made on, as a tensor's does; products and readings on other streams are waited for
+    before it is used again, once they are ordered after its making.  (Tensors taken from ``codes`` and
+    ``scales`` keep it alive, but what other operations read of them on other streams is not noted.)"""
 
     __slots__ = ("rows", "cols", "device", "dev", "code_ptr", "scale_ptr", "_codes", "_scales", "_block")
 
@@ -77,7 +113,7 @@ class MXMatrix:
                 or not scales.is_contiguous() or rows < 0 or cols < 0 or codes.numel() != rows * tiles * 64
                 or scales.numel() != (rows + 127) // 128 * tiles * 512):
             raise ValueError(f"not the codes and scales of a {rows} x {cols} matrix")
-        self.rows, self.cols, self._codes, self._scales = rows, cols, codes, scales
+        self.rows, self.cols, self._codes, self._scales, self._block = rows, cols, codes, scales, None
         self.dev, self.device = _on_gpu(codes, scales), codes.device
         self.code_ptr, self.scale_ptr = codes.data_ptr(), scales.data_ptr()
 
@@ -93,6 +129,12 @@ class MXMatrix:
         self.scale_ptr = block.ptr
         self.code_ptr = block.ptr + n
         return self
+
+    def _reads(self):
+        """The current stream is about to read it."""
+        block = self._block
+        if block is not None and block.stream != _raw_stream(self.dev):  # (a caller's tensors are the caller's)
+            block.read_elsewhere(_raw_stream(self.dev))
 
     def _split(self):
         n, tiles = self.code_ptr - self.scale_ptr, (self.cols + 127) // 128
@@ -189,6 +231,7 @@ def quantize(x: torch.Tensor, rows: bool = True, cols: bool = False):
 def dequantize(q: MXMatrix, dtype=torch.bfloat16) -> torch.Tensor:
     """The values that q stands for."""
     kind = _type(dtype, "dequantize")
+    q._reads()
     out = torch.empty((q.rows, q.cols), dtype=dtype, device=q.device)
     _call("tula_mx_dequantize", q.dev, q.code_ptr, q.scale_ptr, q.rows, q.cols, out.data_ptr(), kind)
     return out
@@ -199,6 +242,8 @@ def matmul(a: MXMatrix, b: MXMatrix, dtype=torch.bfloat16) -> torch.Tensor:
     if a.cols != b.cols or a.dev != b.dev:
         raise ValueError(f"matmul: {a.cols} columns on GPU {a.dev} and {b.cols} on GPU {b.dev}")
     kind = _type(dtype, "matmul")
+    a._reads()
+    b._reads()
     out = torch.empty((a.rows, b.rows), dtype=dtype, device=a.device)
     _call("tula_mx_matmul", a.dev, a.code_ptr, a.scale_ptr, b.code_ptr, b.scale_ptr, a.rows, b.rows, a.cols,
           out.data_ptr(), kind)

@@ -474,3 +474,43 @@ def test_linear_of_more_dimensions_and_on_another_stream():
         got = mx.linear(x, w)
     side.synchronize()
     assert torch.equal(got.view(-1, 50), want)
+
+
+@pytest.mark.gpu
+def test_memory_waits_for_readers_on_other_streams():
+    x = torch.randn(512, 512, device="cuda", generator=torch.Generator("cuda").manual_seed(31)).bfloat16()
+    expect, ones = mx.dequantize(mx.quantize(x)), torch.ones_like(x)
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()  # no holes of other tests in the streams' pools
+    own, other = torch.cuda.Stream(), torch.cuda.Stream()
+    for stream in (own, other):
+        stream.wait_stream(torch.cuda.current_stream())
+    for read in (lambda q: mx.dequantize(q), lambda q: mx.matmul(q, q, torch.float32)):
+        with torch.cuda.stream(own):
+            q = mx.quantize(x)
+            right = read(q)
+        other.wait_stream(own)
+        with torch.cuda.stream(other):
+            torch.cuda._sleep(20_000_000)  # some 10 ms, in which q is dropped
+            got = read(q)
+        at = q.scale_ptr
+        del q
+        with torch.cuda.stream(own):  # takes the same memory
+            again = [mx.quantize(ones)]
+            while len(again) < 64 and not abs(again[-1].scale_ptr - at) < 512 * 256:
+                again.append(mx.quantize(ones))
+            assert len(again) < 64
+        torch.cuda.synchronize()
+        assert torch.equal(got, right)
+        del again
+    assert torch.equal(expect, mx.dequantize(mx.quantize(x)))
+    assert mx.tula_mx_error() == 0 and not mx._unfreed
+    # read in a graph, on the stream that captures it: nothing is noted, and dropping it there is harmless
+    q = mx.quantize(x)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = mx.dequantize(q)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert q._block.readers is None and torch.equal(out, expect)
