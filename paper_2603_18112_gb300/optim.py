@@ -128,6 +128,15 @@ class _Plan:
                                                  self.workspace.numel(), _stream_ptr(None),
                                                  ctypes.byref(self.handle)), "tula_train_plan_create")
         self._destroy = _lib().tula_train_plan_destroy  # kept for __del__ at shutdown
+        self.memory, self.last = [self.workspace], ()
+
+    def ran_on(self, stream):
+        """A call went to this stream, not the one of the call before.  Kernels read the tiles' rows from the
+        workspace, so what is the plan's own goes back to the allocator only after its work."""
+        self.last, index = stream.value, self.device.index
+        s = torch.cuda.ExternalStream(stream.value, index) if stream.value else torch.cuda.default_stream(index)
+        for t in self.memory:
+            t.record_stream(s)
 
     def __del__(self):
         if getattr(self, "handle", None):
@@ -143,21 +152,26 @@ class GradClipper:
         self._plan = _Plan(grads)
         self.record = torch.zeros(TULA_RECORD_LEN, dtype=torch.float32, device=self._plan.device)
         self._record = c_void_p(self.record.data_ptr())
+        self._plan.memory.append(self.record)
         # The fill above ran on the current stream; calls may be issued on any other.
         torch.cuda.synchronize(self._plan.device)
 
     def norm(self, grad_scale=1.0, max_norm=0.0, stream=None) -> torch.Tensor:
         """|G| / grad_scale, and the coefficient that max_norm would ask for; gradients are read
         only.  Returns the record."""
-        _check(_lib().tula_grad_norm(self._plan.handle, grad_scale, max_norm, self._record,
-                                     _stream_ptr(stream)), "tula_grad_norm")
+        s, plan = _stream_ptr(stream), self._plan
+        _check(_lib().tula_grad_norm(plan.handle, grad_scale, max_norm, self._record, s), "tula_grad_norm")
+        if s.value != plan.last:
+            plan.ran_on(s)
         return self.record
 
     def clip_(self, max_norm, stream=None) -> torch.Tensor:
         """Scales the gradients in place to a norm of at most max_norm.  Returns the record, whose
         norm is that before clipping."""
-        _check(_lib().tula_grad_clip(self._plan.handle, max_norm, self._record, _stream_ptr(stream)),
-               "tula_grad_clip")
+        s, plan = _stream_ptr(stream), self._plan
+        _check(_lib().tula_grad_clip(plan.handle, max_norm, self._record, s), "tula_grad_clip")
+        if s.value != plan.last:
+            plan.ran_on(s)
         return self.record
 
 
@@ -179,6 +193,7 @@ class AdamWStep:
             raise TypeError(f"steps: two int64 on {dev} are wanted")
         self.steps = steps
         self.record = torch.zeros(TULA_RECORD_LEN, dtype=torch.float32, device=dev)
+        self._plan.memory += [steps, self.record]
         self.hp = tula_adamw_hparams()
         _lib().tula_adamw_default_hparams(ctypes.byref(self.hp))
         self.hp.max_norm = max_norm
@@ -192,6 +207,9 @@ class AdamWStep:
         hp = self.hp
         hp.lr, hp.eps, hp.weight_decay, hp.grad_scale = lr, eps, weight_decay, grad_scale
         hp.beta1, hp.beta2 = betas
-        _check(_lib().tula_adamw_step(self._plan.handle, self._hp, _stream_ptr(stream)), "tula_adamw_step")
+        s, plan = _stream_ptr(stream), self._plan
+        _check(_lib().tula_adamw_step(plan.handle, self._hp, s), "tula_adamw_step")
+        if s.value != plan.last:
+            plan.ran_on(s)
 
     __call__ = step

@@ -423,3 +423,27 @@ def test_graph_and_another_stream():
     assert b[-1].steps.tolist() == [3, 0] == a[-1].steps.tolist()
     for r in range(5):
         assert all(torch.equal(x, y) for x, y in zip(a[r], b[r]))
+
+
+@pytest.mark.gpu
+def test_a_plans_memory_waits_for_calls_on_other_streams():
+    """A plan that is dropped right after a call on another stream: its workspace does not go to the
+    next allocation while that call may be running."""
+    g = [torch.full((5000,), 0.5, device="cuda") for _ in range(40)]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    clip = O.GradClipper(g)
+    at, size = clip._plan.workspace.data_ptr(), clip._plan.workspace.numel()
+    at_record = clip.record.data_ptr()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)
+    clip.clip_(1.0, side)
+    del clip
+    taken = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(32)]
+    taken += [torch.empty(4, device="cuda") for _ in range(32)]
+    assert not side.query()
+    assert all(not at <= t.data_ptr() < at + size and t.data_ptr() != at_record for t in taken)
+    torch.cuda.synchronize()
+    norm = 0.5 * (40 * 5000) ** 0.5
+    for t in g:
+        torch.testing.assert_close(t, torch.full_like(t, 0.5 / norm), rtol=1e-5, atol=0)
