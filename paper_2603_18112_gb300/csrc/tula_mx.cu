@@ -876,7 +876,11 @@ __global__ void __launch_bounds__(kMmaThreads) k_matmul(const __grid_constant__ 
             __syncwarp();
             issued = i + 1;
         }
-        // no copy may be in flight when the CTA ends
+        // The issuing warp's arrivals have all landed before the CTA ends, also those on stages that nothing
+        // is copied to any more.
+        for (int i = max(0, issued - S::kStages); ok && i < issued; ++i)
+            ok = __all_sync(kFull, mbar_wait(empty + 8 * (i % S::kStages), (i / S::kStages) & 1, &dead));
+        // Nor may a copy be in flight then.
         if (dead)
             for (int i = max(0, issued - S::kStages); i < issued; ++i) {
                 const int s = i % S::kStages;
@@ -912,7 +916,7 @@ __global__ void __launch_bounds__(kMmaThreads) k_matmul(const __grid_constant__ 
             }
             __syncwarp();
         }
-        if (ok && elect_one()) commit(done);
+        if (ok && n_k && elect_one()) commit(done);  // (without stages nothing waits for it)
         __syncwarp();
     } else {
         const bool ok = __all_sync(kFull, n_k == 0 || mbar_wait(done, 0, &dead));

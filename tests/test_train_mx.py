@@ -339,6 +339,22 @@ def test_nan_blocks_and_empty_sums(M):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("M,N", [(1, 128), (20, 300), (60, 128), (100, 200), (200, 100)])
+@pytest.mark.parametrize("stages", [9, 17, 18, 33, 34, 35, 41])
+def test_shares_of_a_sum_that_some_ctas_have_nothing_of(M, N, stages):
+    """Sums whose stages of 256 columns do not divide among the CTAs of a cluster: the last ones have
+    fewer or none.  Again and again, so that a CTA's barriers lie where another's did before."""
+    K = 256 * stages - 100
+    a, b = mx.quantize(_matrix(M, K, torch.float32, 70)), mx.quantize(_matrix(N, K, torch.float32, 71))
+    want = _check_product(a, b, torch.float32)
+    empty = mx.quantize(torch.zeros(M, 0, device="cuda")), mx.quantize(torch.zeros(N, 0, device="cuda"))
+    for _ in range(20):
+        zero = mx.matmul(*empty, torch.float32)
+        assert torch.equal(mx.matmul(a, b, torch.float32), want) and not zero.any()
+    assert mx.tula_mx_error() == 0
+
+
+@pytest.mark.gpu
 def test_calls_from_a_thread_that_has_made_none():
     """The first CUDA call of a thread is a product, a transpose's quantisation, a clipping."""
     import threading
