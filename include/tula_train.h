@@ -63,8 +63,9 @@ int tula_train_plan_create(const tula_train_tensors *tensors, void *workspace,
 int tula_train_plan_destroy(tula_train_plan *plan);
 
 /* What a norm leaves in a record, device fp32 [TULA_RECORD_LEN]. */
-#define TULA_RECORD_NORM 0   /* |G| over all gradients, each divided by grad_scale (held in fp64 for
-                                what follows from it; inf here above fp32's range) */
+#define TULA_RECORD_NORM 0   /* |G| over all gradients, each divided by grad_scale (inf here above fp32's
+                                range; what follows from it then is computed in fp64, as it is wherever
+                                fp32 would leave its normal range on the way) */
 #define TULA_RECORD_COEF 1   /* min(1, max_norm / (|G| + 1e-6)); 1 without a max_norm */
 #define TULA_RECORD_FINITE 2 /* 1 if |G| is finite, else 0 */
 #define TULA_RECORD_LEN 4    /* the last word is left as it is */

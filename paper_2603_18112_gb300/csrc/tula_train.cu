@@ -246,6 +246,7 @@ __device__ __forceinline__ double warp_sum(float s, double d) {
 struct NormArgs {
     double grad_scale, max_norm;
     float inv_scale;  // 1 / grad_scale
+    bool in_fp32;     // what follows from an ordinary sum of squares stays in fp32's normal range
     float *record;
     // the step's scalars (steps NULL: a norm alone)
     long long *steps;
@@ -267,7 +268,7 @@ __device__ __forceinline__ float root_correction(const NormArgs &a, long long t)
 __device__ void finish_norm(double total, const Tables &tb, const NormArgs &a) {
     float norm, coef = 1.f, mult;
     bool finite = true;
-    if (total >= 0x1p-100 && total <= 0x1p100) {
+    if (a.in_fp32 && total >= 0x1p-100 && total <= 0x1p100) {
         // in fp32 (its root and quotients take a tenth of the time that fp64's take on this part)
         norm = __fmul_rn(__fsqrt_rn((float)total), a.inv_scale);
         if (a.max_norm > 0.0) coef = fminf(__fdiv_rn((float)a.max_norm, __fadd_rn(norm, kNormEps)), 1.f);
@@ -712,6 +713,14 @@ int check_plan(tula_train_plan *plan) {
     return dev == plan->dev ? TULA_OK : TULA_ERR_ARG;
 }
 
+// Whether finish_norm may go on from a root in [2^-50, 2^50] in fp32.  With 1 / grad_scale within 2^+-32 the
+// norm is within 2^+-82, and with a threshold of 2^-32 or more the coefficient is 2^-114 or more (above fp32's
+// range the threshold is inf, and the coefficient 1 all the same); the two factors' product is what an
+// element is multiplied by, threshold / root or 1 / grad_scale.
+bool stays_in_fp32(const NormArgs &a) {
+    return a.inv_scale >= 0x1p-32f && a.inv_scale <= 0x1p32f && (a.max_norm == 0.0 || a.max_norm >= 0x1p-32);
+}
+
 int run_norm(const Tables &tb, const NormArgs &a, cudaStream_t s) {
     if (tb.n_tiles == 0) return tula::launch(k_empty, dim3(1), 1, 0, s, 1, tb, a);
     return tula::launch(tb.tile == kSmallTile ? k_norm<1> : k_norm<4>, dim3((unsigned)tb.n_groups),
@@ -826,6 +835,7 @@ int tula_grad_norm(tula_train_plan *plan, float grad_scale, float max_norm, floa
     a.grad_scale = grad_scale;
     a.inv_scale = 1.f / grad_scale;
     a.max_norm = max_norm;
+    a.in_fp32 = stays_in_fp32(a);
     a.record = record;
     return run_norm(plan->tb, a, static_cast<cudaStream_t>(stream));
 }
@@ -872,6 +882,7 @@ int tula_adamw_step(tula_train_plan *plan, const tula_adamw_hparams *hp, void *s
     a.grad_scale = hp->grad_scale;
     a.inv_scale = (float)(1.0 / hp->grad_scale);
     a.max_norm = hp->max_norm;
+    a.in_fp32 = stays_in_fp32(a);
     a.record = normed ? hp->record : nullptr;
     a.steps = reinterpret_cast<long long *>(hp->steps);
     a.log_beta1 = std::log(hp->beta1);

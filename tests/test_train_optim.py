@@ -321,6 +321,41 @@ def test_adamw_of_buffers_at_offsets_of_their_own(offsets, max_norm, sizes):
         assert torch.equal(g, g2)
 
 
+# exponents (grad_scale, |G| before it) at which the norm, the coefficient or their product with
+# 1 / grad_scale leaves fp32's normal range on the way, though what an element is multiplied by does not
+ENDS = [(-100, 30), (-99, 30), (-90, 49), (-76, 20), (-60, -20), (-33, 49), (-32, 49), (-31, 49), (0, 49),
+        (31, -20), (33, -20), (60, 40), (99, 45), (100, 50)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("scale2,norm2", ENDS)
+@pytest.mark.parametrize("max_norm", [0.0, 2.0 ** -40, 1.0, 2.0 ** 60])
+def test_norm_and_adamw_over_the_range_of_grad_scale(scale2, norm2, max_norm):
+    w, g, m, v, _ = _adam_state([5000, 33], torch.float32, "padded", None, 17)
+    scale = 2.0 ** scale2
+    by = 2.0 ** norm2 / _norm64(g)
+    for x in g:
+        x.mul_(by)
+    for x in m + v:
+        x.zero_()
+    norm = _norm64(g) / scale
+    coef = min(1.0, max_norm / (norm + 1e-6)) if max_norm else 1.0
+    rec = O.GradClipper(g).norm(grad_scale=scale, max_norm=max_norm).tolist()
+    # on fp32's grid, also below its normal range
+    assert rec[0] == pytest.approx(_f32(norm), rel=NORM_TOL, abs=2.0 ** -149) and rec[2] == 1.0
+    assert rec[1] == pytest.approx(coef, rel=2 * NORM_TOL, abs=2.0 ** -149)
+    if not max_norm and norm2 - scale2 > 60:
+        return  # squares beyond fp32's range
+    lr, b1, b2, eps, wd = 3e-3, 0.9, 0.98, 1e-8, 0.1
+    steps = torch.tensor([999, 0], dtype=torch.int64, device="cuda")
+    step = O.AdamWStep(w, g, m, v, max_norm=max_norm, steps=steps)
+    want = [_adam64(*x, 1000, coef / scale, lr, b1, b2, eps, wd) for x in zip(w, g, m, v)]
+    step(lr, (b1, b2), eps, wd, grad_scale=scale)
+    for i, (ref, tol) in enumerate(want):
+        for role, x, r, e in zip("wmv", (w[i], m[i], v[i]), ref, tol):
+            assert bool(((x.double() - r).abs() <= e).all()), (i, role)
+
+
 @pytest.mark.gpu
 def test_adamw_matches_torch_from_the_first_step():
     """Zero moments, steps from 1 on, the defaults of torch.optim.AdamW."""
