@@ -84,7 +84,7 @@ int tula_grad_norm(tula_train_plan *plan, float grad_scale, float max_norm, floa
 /*
  * The norm as above (grad_scale 1), then g = coef * g for every gradient, in fp32, rounded once to
  * its type.  max_norm > 0.  With coef = 1 the gradients are left as they are; an infinite norm has
- * coef 0 and a NaN norm the coef NaN.
+ * coef 0, whatever max_norm, and a NaN norm the coef NaN.
  */
 int tula_grad_clip(tula_train_plan *plan, float max_norm, float *record, void *stream);
 

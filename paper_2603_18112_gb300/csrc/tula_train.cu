@@ -279,7 +279,8 @@ __device__ void finish_norm(double total, const Tables &tb, const NormArgs &a) {
         double c = 1.0;
         if (a.max_norm > 0.0) {
             c = a.max_norm / (n + (double)kNormEps);
-            if (c > 1.0) c = 1.0;  // a NaN stays
+            if (c > 1.0) c = 1.0;      // a NaN stays
+            if (n > 1.7e308) c = 0.0;  // also below an infinite threshold
         }
         norm = (float)n;
         coef = (float)c;

@@ -216,6 +216,27 @@ def test_norm_of_infinities_and_nans(dtype, bad):
             assert norm == math.inf and coef == 0.0
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_clipping_of_infinities_and_nans(dtype):
+    """An infinite norm has coef 0, whatever the threshold, so that finite gradients become zeros and
+    infinite ones NaN; a NaN makes them all NaN."""
+    for bad, max_norm in ((math.inf, 1.0), (math.inf, math.inf), (-math.inf, 3.0), (math.nan, 1.0), (math.nan, math.inf)):
+        for where in (0, 4321, 19999):
+            grads = _grads([100, 20000, 3], dtype, "padded", 7)
+            grads[1][where] = bad
+            norm, coef, finite, _ = O.GradClipper(grads).clip_(max_norm).tolist()
+            assert finite == 0.0
+            if math.isnan(bad):
+                assert math.isnan(norm) and math.isnan(coef)
+                assert all(bool(torch.isnan(g).all()) for g in grads)
+                continue
+            assert norm == math.inf and coef == 0.0
+            nans = torch.isnan(grads[1])
+            assert bool(nans[where]) and int(nans.sum()) == 1
+            assert not grads[0].any() and not grads[2].any() and not grads[1][~nans].any()
+
+
 def _adam_state(sizes, gdtype, layout, copies, seed):
     gen = torch.Generator(device="cuda").manual_seed(seed)
     packed, shift = {"padded": (False, 0), "packed": (True, 0), "shifted": (True, 3)}[layout]
