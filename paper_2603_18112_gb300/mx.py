@@ -65,10 +65,10 @@ class _Block:
     """Device memory from torch's allocator, for the current device and stream, without a tensor around
     it: with torch.empty ahead of it a launch takes the host 7.5 us on a GB300 machine, with this 3.5."""
 
-    __slots__ = ("ptr", "size", "device", "stream", "readers")
+    __slots__ = ("ptr", "size", "device", "stream", "_noted")
 
     def __init__(self, size: int, device: int, _alloc=torch._C._cuda_cudaCachingAllocator_raw_alloc):
-        self.ptr, self.size, self.device, self.readers = 0, size, device, None
+        self.ptr, self.size, self.device, self._noted = 0, size, device, set()
         self.stream = stream = _raw_stream(device)
         if size and device == _get_device():
             self.ptr = _alloc(size, stream)
@@ -81,15 +81,20 @@ class _Block:
         graph reads has to live as long as the graph: its streams hold no work to wait for.)"""
         with torch.cuda.device(self.device):
             if not torch.cuda.is_current_stream_capturing():
-                self.readers = (self.readers or set()) | {stream}
+                self._noted.add(stream)  # (one step: other threads may be noting theirs)
+
+    @property
+    def readers(self):
+        """The other streams that have read it, or None."""
+        return self._noted or None
 
     def __del__(self, _delete=torch._C._cuda_cudaCachingAllocator_raw_delete):
         if not self.ptr:
             return
-        if self.readers is None:
+        if not self._noted:
             _delete(self.ptr)
         else:
-            _unfreed.append((self.ptr, self.device, self.stream, self.readers))
+            _unfreed.append((self.ptr, self.device, self.stream, self._noted))
             _free_after_readers(_delete)
 
     @property

@@ -1,0 +1,117 @@
+"""Memory of quantised matrices that other streams read: noting the readers, and giving it back once they
+are waited for.  On the CPU, with streams and an allocator that only keep books."""
+import threading
+
+import pytest
+
+from paper_2603_18112_gb300 import mx
+
+
+class Streams:
+    """Streams by their handles, 0 the default one: which are under capture, who waited for whom, what
+    was given back."""
+
+    def __init__(self):
+        self.here = threading.local()
+        self.capturing, self.waits, self.freed, self.on_wait = set(), [], [], None
+        self.next = 0x1000
+
+    @property
+    def current(self):
+        return getattr(self.here, "stream", 0)
+
+    def handle(self, stream):
+        outer = self
+
+        class Stream:
+            cuda_stream = stream
+
+            def wait_stream(self, other):
+                outer.waits.append((stream, other.cuda_stream))
+                if outer.on_wait:
+                    outer.on_wait(stream, other.cuda_stream)
+
+        return Stream()
+
+    def on(self, stream):
+        outer = self
+
+        class On:
+            def __enter__(self):
+                self.before, outer.here.stream = outer.current, stream.cuda_stream
+
+            def __exit__(self, *_):
+                outer.here.stream = self.before
+
+        return On()
+
+    def alloc(self, size, stream):
+        self.next += 0x1000
+        return self.next
+
+    def block(self, stream, readers=()):
+        """One made on `stream` and read on `readers`."""
+        with self.on(self.handle(stream)):
+            block = mx._Block(256, 0, self.alloc)
+        for r in readers:
+            self.read(block, r)
+        return block
+
+    def read(self, block, stream):
+        with self.on(self.handle(int(stream))):
+            block.read_elsewhere(stream)
+
+
+@pytest.fixture
+def streams(monkeypatch):
+    s = Streams()
+
+    class Device:
+        def __init__(self, _):
+            pass
+
+        def __enter__(self):
+            pass
+
+        def __exit__(self, *_):
+            pass
+
+    monkeypatch.setattr(mx, "_raw_stream", lambda device: s.current)
+    monkeypatch.setattr(mx, "_get_device", lambda: 0)
+    monkeypatch.setattr(mx, "_unfreed", [])
+    monkeypatch.setattr(mx._Block.__del__, "__defaults__", (s.freed.append,))
+    monkeypatch.setattr(mx.torch.cuda, "device", Device)
+    monkeypatch.setattr(mx.torch.cuda, "stream", s.on)
+    monkeypatch.setattr(mx.torch.cuda, "ExternalStream", lambda handle, device: s.handle(handle))
+    monkeypatch.setattr(mx.torch.cuda, "default_stream", lambda device: s.handle(0))
+    monkeypatch.setattr(mx.torch.cuda, "is_current_stream_capturing", lambda: s.current in s.capturing)
+    return s
+
+
+def test_readers_are_waited_for(streams):
+    block = streams.block(7, [8, 9, 8])
+    ptr = block.ptr
+    del block
+    assert sorted(streams.waits) == [(7, 8), (7, 9)] and streams.freed == [ptr]
+    block = streams.block(7)
+    ptr = block.ptr
+    del block
+    assert len(streams.waits) == 2 and streams.freed[1:] == [ptr]
+
+
+def test_readers_noted_at_the_same_time_are_all_kept(streams):
+    """A thread notes its stream in the middle of another thread's note."""
+    block = streams.block(7)
+
+    class Slow(int):
+        between = None
+
+        def __hash__(self):
+            if Slow.between:
+                between, Slow.between = Slow.between, None
+                between()
+            return int.__hash__(self)
+
+    Slow.between = lambda: streams.read(block, 9)
+    streams.read(block, Slow(8))
+    assert block.readers == {8, 9}

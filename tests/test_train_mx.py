@@ -530,3 +530,35 @@ def test_memory_waits_for_readers_on_other_streams():
     graph.replay()
     torch.cuda.synchronize()
     assert q._block.readers is None and torch.equal(out, expect)
+
+
+@pytest.mark.gpu
+def test_threads_on_streams_of_their_own_read_one_matrix():
+    """All of their streams are noted, and none of their products sees other contents."""
+    import threading
+    a = mx.quantize(_matrix(40, 512, torch.float32, 90))
+    for _ in range(5):
+        q = mx.quantize(_matrix(300, 512, torch.float32, 91))
+        want = mx.matmul(a, q)
+        streams = [torch.cuda.Stream() for _ in range(6)]
+        torch.cuda.synchronize()
+        start, got, errors = threading.Barrier(len(streams)), [], []
+
+        def serve(stream, q=q, want=want):
+            try:
+                with torch.cuda.stream(stream):
+                    start.wait(60)
+                    outs = [mx.matmul(a, q) for _ in range(10)]
+                    same = torch.stack([(o == want).all() for o in outs]).all()
+                    stream.synchronize()
+                    got.append(bool(same))
+            except Exception as e:  # noqa: BLE001
+                errors.append(e)
+
+        threads = [threading.Thread(target=serve, args=(s,)) for s in streams]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+        assert not errors and got == [True] * len(streams)
+        assert q._block.readers == {s.cuda_stream for s in streams}
