@@ -79,6 +79,8 @@ class _Block:
     def read_elsewhere(self, stream: int):
         """The device's current stream, which is not the block's own, is about to read the block.  (What a
         graph reads has to live as long as the graph: its streams hold no work to wait for.)"""
+        if stream in self._noted:
+            return
         with torch.cuda.device(self.device):
             if not torch.cuda.is_current_stream_capturing():
                 self._noted.add(stream)  # (one step: other threads may be noting theirs)

@@ -115,3 +115,17 @@ def test_readers_noted_at_the_same_time_are_all_kept(streams):
     Slow.between = lambda: streams.read(block, 9)
     streams.read(block, Slow(8))
     assert block.readers == {8, 9}
+
+
+def test_a_reader_that_is_noted_costs_no_more(streams, monkeypatch):
+    """Weights that are read on one stream again and again: from the second time on nothing is asked."""
+    block = streams.block(7, [8])
+
+    def none(*_):
+        raise AssertionError
+
+    with monkeypatch.context() as m:
+        m.setattr(mx.torch.cuda, "device", none)
+        m.setattr(mx.torch.cuda, "is_current_stream_capturing", none)
+        streams.read(block, 8)
+    assert block.readers == {8}
