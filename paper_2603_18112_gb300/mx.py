@@ -42,23 +42,38 @@ _raw_stream, _get_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_ge
 _unfreed: list = []  # blocks that were dropped while another stream may read them
 
 
+def _wait_for_readers(device, own, readers):
+    """Has the stream that a block's memory goes back to wait for those that read it; False under capture."""
+    own, *readers = [torch.cuda.ExternalStream(s, device) if s else torch.cuda.default_stream(device)
+                     for s in (own, *readers)]
+    for s in (own, *readers):
+        with torch.cuda.stream(s):
+            if torch.cuda.is_current_stream_capturing():
+                return False
+    for s in readers:
+        own.wait_stream(s)
+    return True
+
+
 def _free_after_readers(delete):
     """Gives such blocks back once their own streams, whose next allocations may get them, wait for the
-    readers.  Streams under capture cannot wait so; their blocks stay for the next call."""
-    for block in list(_unfreed):
-        ptr, device, own, readers = block
-        own, *readers = [torch.cuda.ExternalStream(s, device) if s else torch.cuda.default_stream(device)
-                         for s in (own, *readers)]
-        capturing = False
-        for s in (own, *readers):
-            with torch.cuda.stream(s):
-                capturing = capturing or torch.cuda.is_current_stream_capturing()
-        if capturing:
-            continue
-        for s in readers:
-            own.wait_stream(s)
-        _unfreed.remove(block)
-        delete(ptr)
+    readers.  Streams under capture cannot wait so; their blocks stay for the next call.  A block is the
+    caller's alone from the moment it is taken out of the list: other threads, and the collector in the
+    middle of this, may be here too."""
+    held = []
+    try:
+        while _unfreed:
+            try:
+                block = _unfreed.pop()
+            except IndexError:  # another took the last
+                break
+            ptr, *where = block
+            if _wait_for_readers(*where):
+                delete(ptr)
+            else:
+                held.append(block)
+    finally:
+        _unfreed.extend(held)
 
 
 class _Block:

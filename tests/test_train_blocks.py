@@ -1,6 +1,9 @@
 """Memory of quantised matrices that other streams read: noting the readers, and giving it back once they
 are waited for.  On the CPU, with streams and an allocator that only keep books."""
+import itertools
+import sys
 import threading
+import time
 
 import pytest
 
@@ -14,7 +17,7 @@ class Streams:
     def __init__(self):
         self.here = threading.local()
         self.capturing, self.waits, self.freed, self.on_wait = set(), [], [], None
-        self.next = 0x1000
+        self.addresses = itertools.count(0x1000, 0x1000)
 
     @property
     def current(self):
@@ -46,8 +49,7 @@ class Streams:
         return On()
 
     def alloc(self, size, stream):
-        self.next += 0x1000
-        return self.next
+        return next(self.addresses)
 
     def block(self, stream, readers=()):
         """One made on `stream` and read on `readers`."""
@@ -129,3 +131,57 @@ def test_a_reader_that_is_noted_costs_no_more(streams, monkeypatch):
         m.setattr(mx.torch.cuda, "is_current_stream_capturing", none)
         streams.read(block, 8)
     assert block.readers == {8}
+
+
+def _held(streams, blocks):
+    """Drops blocks while their streams are under capture, so that they wait for a later call."""
+    ptrs = [b.ptr for b in blocks]
+    streams.capturing |= {b.stream for b in blocks}
+    blocks.clear()
+    assert not streams.freed and len(mx._unfreed) == len(ptrs)
+    streams.capturing.clear()
+    return ptrs
+
+
+def test_each_block_is_given_back_once(streams):
+    """Two give blocks back at the same time: one begins in the middle of the other's waits, as another
+    thread's or the collector's may."""
+    blocks = [streams.block(7, [8]), streams.block(7, [9]), streams.block(6, [8])]
+    ptrs = _held(streams, blocks)
+
+    def again(*_):
+        streams.on_wait = None
+        mx._free_after_readers(streams.freed.append)
+
+    streams.on_wait = again
+    mx._free_after_readers(streams.freed.append)
+    assert sorted(streams.freed) == ptrs and not mx._unfreed
+
+
+def test_each_block_is_given_back_once_by_threads(streams):
+    errors = []
+
+    def hook(unraisable):
+        errors.append(unraisable)
+
+    before, sys.unraisablehook = sys.unraisablehook, hook
+    streams.on_wait = lambda *_: time.sleep(1e-5)
+    ptrs = []
+
+    def drop(stream):
+        for _ in range(200):
+            block = streams.block(stream, [8, 9])
+            ptrs.append(block.ptr)
+            del block
+
+    try:
+        threads = [threading.Thread(target=drop, args=(s,)) for s in (4, 5, 6, 7)]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+        mx._free_after_readers(streams.freed.append)
+    finally:
+        sys.unraisablehook = before
+    assert not errors and not mx._unfreed
+    assert len(streams.freed) == 800 and sorted(streams.freed) == sorted(ptrs)
