@@ -68,7 +68,13 @@ def _free_after_readers(delete):
             except IndexError:  # another took the last
                 break
             ptr, *where = block
-            if _wait_for_readers(*where):
+            try:
+                waits = _wait_for_readers(*where)
+            except RuntimeError:
+                # a stream that is no more, as one of another library may be: nothing says when its work
+                # ends, so the memory stays taken, and the blocks after it are not held up
+                continue
+            if waits:
                 delete(ptr)
             else:
                 held.append(block)

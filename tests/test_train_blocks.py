@@ -185,3 +185,17 @@ def test_each_block_is_given_back_once_by_threads(streams):
         sys.unraisablehook = before
     assert not errors and not mx._unfreed
     assert len(streams.freed) == 800 and sorted(streams.freed) == sorted(ptrs)
+
+
+def test_a_stream_that_cannot_be_waited_for(streams):
+    """Its block stays where it is, and the others are given back."""
+    blocks = [streams.block(7, [8]), streams.block(7, [9]), streams.block(6, [8])]
+    ptrs = _held(streams, blocks)
+
+    def gone(own, reader):
+        if reader == 9:
+            raise RuntimeError("no such stream")
+
+    streams.on_wait = gone
+    mx._free_after_readers(streams.freed.append)
+    assert sorted(streams.freed) == [ptrs[0], ptrs[2]] and not mx._unfreed
