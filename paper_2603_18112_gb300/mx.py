@@ -39,6 +39,7 @@ def _lib():
 _raw_stream, _get_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
+_raw_delete = torch._C._cuda_cudaCachingAllocator_raw_delete
 _unfreed: list = []  # blocks that were dropped while another stream may read them
 
 
@@ -57,9 +58,9 @@ def _wait_for_readers(device, own, readers):
 
 def _free_after_readers(delete):
     """Gives such blocks back once their own streams, whose next allocations may get them, wait for the
-    readers.  Streams under capture cannot wait so; their blocks stay for the next call.  A block is the
-    caller's alone from the moment it is taken out of the list: other threads, and the collector in the
-    middle of this, may be here too."""
+    readers.  Streams under capture cannot wait so; their blocks stay for the next call, which the next
+    block's making is at the latest.  A block is the caller's alone from the moment it is taken out of the
+    list: other threads, and the collector in the middle of this, may be here too."""
     held = []
     try:
         while _unfreed:
@@ -91,6 +92,8 @@ class _Block:
     def __init__(self, size: int, device: int, _alloc=torch._C._cuda_cudaCachingAllocator_raw_alloc):
         self.ptr, self.size, self.device, self._noted = 0, size, device, set()
         self.stream = stream = _raw_stream(device)
+        if _unfreed and not torch.cuda.is_current_stream_capturing():
+            _free_after_readers(_raw_delete)
         if size and device == _get_device():
             self.ptr = _alloc(size, stream)
         elif size:
@@ -111,7 +114,7 @@ class _Block:
         """The other streams that have read it, or None."""
         return self._noted or None
 
-    def __del__(self, _delete=torch._C._cuda_cudaCachingAllocator_raw_delete):
+    def __del__(self, _delete=_raw_delete):
         if not self.ptr:
             return
         if not self._noted:

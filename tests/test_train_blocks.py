@@ -82,6 +82,7 @@ def streams(monkeypatch):
     monkeypatch.setattr(mx, "_get_device", lambda: 0)
     monkeypatch.setattr(mx, "_unfreed", [])
     monkeypatch.setattr(mx._Block.__del__, "__defaults__", (s.freed.append,))
+    monkeypatch.setattr(mx, "_raw_delete", s.freed.append, raising=False)
     monkeypatch.setattr(mx.torch.cuda, "device", Device)
     monkeypatch.setattr(mx.torch.cuda, "stream", s.on)
     monkeypatch.setattr(mx.torch.cuda, "ExternalStream", lambda handle, device: s.handle(handle))
@@ -199,3 +200,21 @@ def test_a_stream_that_cannot_be_waited_for(streams):
     streams.on_wait = gone
     mx._free_after_readers(streams.freed.append)
     assert sorted(streams.freed) == [ptrs[0], ptrs[2]] and not mx._unfreed
+
+
+def test_a_block_dropped_under_capture_goes_back_after_it(streams):
+    """With the next block that is made, also where no other one is ever read elsewhere; not while the
+    stream that one is made on is under capture itself."""
+    block = streams.block(7, [8])
+    ptr = block.ptr
+    streams.capturing.add(8)
+    del block
+    streams.block(6)
+    assert ptr not in streams.freed
+    streams.capturing.add(6)
+    streams.capturing.remove(8)
+    streams.block(6)
+    assert ptr not in streams.freed and not streams.waits
+    streams.capturing.clear()
+    streams.block(6)
+    assert ptr in streams.freed and streams.waits == [(7, 8)] and not mx._unfreed

@@ -562,3 +562,25 @@ def test_threads_on_streams_of_their_own_read_one_matrix():
             t.join()
         assert not errors and got == [True] * len(streams)
         assert q._block.readers == {s.cuda_stream for s in streams}
+
+
+@pytest.mark.gpu
+def test_a_matrix_dropped_under_capture_goes_back_after_it():
+    x = _matrix(512, 512, torch.bfloat16, 92)
+    own, other = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(own):
+        q = mx.quantize(x)
+    other.wait_stream(own)
+    with torch.cuda.stream(other):
+        out = mx.dequantize(q)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=other):
+        twice = out + out
+        del q
+    assert len(mx._unfreed) == 1
+    again = mx.dequantize(mx.quantize(x))
+    graph.replay()
+    torch.cuda.synchronize()
+    assert not mx._unfreed and torch.equal(again, out) and torch.equal(twice, out + out)
