@@ -43,14 +43,20 @@ _raw_delete = torch._C._cuda_cudaCachingAllocator_raw_delete
 _unfreed: list = []  # blocks that were dropped while another stream may read them
 
 
+def _stream(handle, device):
+    return torch.cuda.ExternalStream(handle, device) if handle else torch.cuda.default_stream(device)
+
+
+def _under_capture(stream):
+    with torch.cuda.stream(stream):
+        return torch.cuda.is_current_stream_capturing()
+
+
 def _wait_for_readers(device, own, readers):
     """Has the stream that a block's memory goes back to wait for those that read it; False under capture."""
-    own, *readers = [torch.cuda.ExternalStream(s, device) if s else torch.cuda.default_stream(device)
-                     for s in (own, *readers)]
-    for s in (own, *readers):
-        with torch.cuda.stream(s):
-            if torch.cuda.is_current_stream_capturing():
-                return False
+    own, *readers = [_stream(s, device) for s in (own, *readers)]
+    if any(map(_under_capture, (own, *readers))):
+        return False
     for s in readers:
         own.wait_stream(s)
     return True
@@ -101,13 +107,17 @@ class _Block:
                 self.ptr = _alloc(size, stream)
 
     def read_elsewhere(self, stream: int):
-        """The device's current stream, which is not the block's own, is about to read the block.  (What a
-        graph reads has to live as long as the graph: its streams hold no work to wait for.)"""
+        """The device's current stream, which is not the block's own, is about to read the block.  Under
+        capture that is noted where the block may be of the same capture, so that its memory is not handed
+        out again within it.  (What a graph reads of before it has to live as long as the graph: its
+        streams hold no work to wait for.)"""
         if stream in self._noted:
             return
         with torch.cuda.device(self.device):
-            if not torch.cuda.is_current_stream_capturing():
-                self._noted.add(stream)  # (one step: other threads may be noting theirs)
+            if torch.cuda.is_current_stream_capturing() and not (
+                    self.stream and _under_capture(_stream(self.stream, self.device))):
+                return
+        self._noted.add(stream)  # (one step: other threads may be noting theirs)
 
     @property
     def readers(self):

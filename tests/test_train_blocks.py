@@ -218,3 +218,23 @@ def test_a_block_dropped_under_capture_goes_back_after_it(streams):
     streams.capturing.clear()
     streams.block(6)
     assert ptr in streams.freed and streams.waits == [(7, 8)] and not mx._unfreed
+
+
+def test_a_block_made_under_capture_is_not_handed_out_within_it(streams):
+    """Read on a second stream of the capture: its memory would go to the capture's next block, which the
+    graph may fill while the reader's branch still runs.  A block from before the capture is the caller's
+    to keep, and no reader is noted."""
+    before = streams.block(5)
+    streams.capturing |= {7, 8}
+    block = streams.block(7, [8])
+    ptr = block.ptr
+    assert block.readers == {8}
+    streams.read(before, 8)
+    streams.read(before, 7)
+    assert before.readers is None
+    del block
+    streams.block(7)
+    assert ptr not in streams.freed
+    streams.capturing.clear()
+    streams.block(6)
+    assert ptr in streams.freed and not mx._unfreed

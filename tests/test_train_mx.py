@@ -584,3 +584,31 @@ def test_a_matrix_dropped_under_capture_goes_back_after_it():
     graph.replay()
     torch.cuda.synchronize()
     assert not mx._unfreed and torch.equal(again, out) and torch.equal(twice, out + out)
+
+
+@pytest.mark.gpu
+def test_matrices_of_a_capture_read_on_its_second_stream():
+    """A branch of a graph reads a matrix that the capture made and dropped: what the other branch makes
+    after it lies elsewhere."""
+    x = _matrix(512, 512, torch.bfloat16, 93)
+    ones, want = torch.ones_like(x), mx.dequantize(mx.quantize(x))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        q = mx.quantize(x)
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            out = mx.dequantize(q)
+        at = q.scale_ptr
+        del q
+        later = [mx.quantize(ones) for _ in range(4)]
+        assert all(abs(m.scale_ptr - at) >= 512 * 256 for m in later)
+        torch.cuda.current_stream().wait_stream(side)
+    for _ in range(5):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    del later
+    mx.quantize(x)
+    assert not mx._unfreed
