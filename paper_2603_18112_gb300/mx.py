@@ -138,6 +138,11 @@ class _Block:
         return {"shape": (self.size,), "typestr": "|u1", "data": (self.ptr, False), "version": 3}
 
 
+def _bytes(rows, cols):
+    """Of a matrix's scales and codes, which follow them."""
+    return (rows + 127) // 128 * ((cols + 127) // 128) * 512 + rows * ((cols + 127) // 128) * 64
+
+
 class MXMatrix:
     """A rows x cols matrix in MXFP4: ``codes`` uint8 [rows, P / 2] and ``scales`` uint8
     [ceil(rows / 128), P / 128, 32, 4, 4], P = cols rounded up to a multiple of 128; of any shapes
@@ -169,6 +174,16 @@ class MXMatrix:
         self._codes = self._scales = None
         self.scale_ptr = block.ptr
         self.code_ptr = block.ptr + n
+        return self
+
+    @classmethod
+    def _within(cls, memory: torch.Tensor, at: int, rows: int, cols: int) -> "MXMatrix":
+        """One to quantise into, or quantised there before, `at` bytes into a uint8 tensor that outlives it."""
+        self = cls.__new__(cls)
+        self.rows, self.cols, self.dev, self.device = rows, cols, memory.get_device(), memory.device
+        self._codes = self._scales = self._block = None
+        self.scale_ptr = memory.data_ptr() + at
+        self.code_ptr = self.scale_ptr + (rows + 127) // 128 * ((cols + 127) // 128) * 512
         return self
 
     def _reads(self):
@@ -233,6 +248,24 @@ def _type(dtype, what):
     return kind
 
 
+def _quantize_into(x, dev, kind, q, t):
+    """A matrix into q, its transpose into t; either may be None."""
+    r, c = x.shape
+    stride, step = x.stride()
+    if step != 1 and stride == 1 and r > 1 and step >= r:
+        # a transposed matrix lies in memory as its transpose does: each form is the other's of that
+        return _quantize_into(x.t(), dev, kind, t, q)
+    # a row of one element, or the only row, may have any stride
+    if c > 1 and step != 1 or r > 1 and stride < c:
+        x = x.contiguous()
+        stride = c
+    if r <= 1:
+        stride = c
+    a, b = (q.code_ptr, q.scale_ptr) if q else (None, None)
+    a_t, b_t = (t.code_ptr, t.scale_ptr) if t else (None, None)
+    _call("tula_mx_quantize", dev, x.data_ptr(), kind, r, c, stride, a, b, a_t, b_t)
+
+
 def quantize(x: torch.Tensor, rows: bool = True, cols: bool = False):
     """x (2-D; its rows may lie apart) as an MXMatrix (rows), its transpose as one (cols), or both
     as a pair from one reading of x."""
@@ -244,29 +277,13 @@ def quantize(x: torch.Tensor, rows: bool = True, cols: bool = False):
     if len(shape) != 2 or not (rows or cols):
         raise ValueError("quantize: a matrix, and at least one of rows and cols, are wanted")
     r, c = shape
-    stride, step = x.stride()
-    if step != 1 and stride == 1 and r > 1 and step >= r:
-        # a transposed matrix lies in memory as its transpose does: each form is the other's of that
-        got = quantize(x.t(), rows=cols, cols=rows)
-        return got[::-1] if rows and cols else got
-    # a row of one element, or the only row, may have any stride
-    if c > 1 and step != 1 or r > 1 and stride < c:
-        x = x.contiguous()
-        stride = c
-    if r <= 1:
-        stride = c
+    q = MXMatrix.empty(r, c, device) if rows else None
     if not cols:
-        q = MXMatrix.empty(r, c, device)
-        _call("tula_mx_quantize", dev, x.data_ptr(), kind, r, c, stride, q.code_ptr, q.scale_ptr, None, None)
+        _quantize_into(x, dev, kind, q, None)
         return q
     t = MXMatrix.empty(c, r, device)
-    if not rows:
-        _call("tula_mx_quantize", dev, x.data_ptr(), kind, r, c, stride, None, None, t.code_ptr, t.scale_ptr)
-        return t
-    q = MXMatrix.empty(r, c, device)
-    _call("tula_mx_quantize", dev, x.data_ptr(), kind, r, c, stride, q.code_ptr, q.scale_ptr, t.code_ptr,
-          t.scale_ptr)
-    return q, t
+    _quantize_into(x, dev, kind, q, t)
+    return (q, t) if rows else t
 
 
 def dequantize(q: MXMatrix, dtype=torch.bfloat16) -> torch.Tensor:
@@ -309,27 +326,38 @@ class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w):
         need_x, need_w = ctx.needs_input_grad
-        # what the backward pass multiplies by is kept in 4 bits: x^T for dw, w^T for dx
-        qx = quantize(x, cols=need_w)
-        qw = quantize(w, cols=need_x)
-        qx, xt = qx if need_w else (qx, None)
-        qw, wt = qw if need_x else (qw, None)
-        ctx.types = (x.dtype, w.dtype)
-        ctx.sides = (xt, wt)
+        (m, k), n = x.shape, w.shape[0]
+        dev, x_kind, w_kind = _on_gpu(x, w), _type(x.dtype, "linear"), _type(w.dtype, "linear")
+        # what the backward pass multiplies by is kept in 4 bits: x^T for dw, then w^T for dx
+        ctx.types, ctx.sizes, ctx.device = (x.dtype, w.dtype), (m, n, k), x.device
+        ctx.at = at = _bytes(k, m) if need_w else 0
+        ctx.end = end = at + (_bytes(k, n) if need_x else 0)
+        xt = wt = None
+        if need_x or need_w:
+            kept = torch.empty(end, dtype=torch.uint8, device=x.device)
+            xt = MXMatrix._within(kept, 0, k, m) if need_w else None
+            wt = MXMatrix._within(kept, at, k, n) if need_x else None
+        qx, qw = MXMatrix.empty(m, k, x.device), MXMatrix.empty(n, k, w.device)
+        _quantize_into(x, dev, x_kind, qx, xt)
+        _quantize_into(w, dev, w_kind, qw, wt)
+        if need_x or need_w:
+            ctx.save_for_backward(kept)
         return matmul(qx, qw, x.dtype)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
-        xt, wt = ctx.sides
-        need_x, need_w = ctx.needs_input_grad
+        kept, = ctx.saved_tensors
+        if kept.dtype != torch.uint8 or kept.numel() != ctx.end or kept.device != ctx.device or not kept.is_contiguous():
+            raise RuntimeError("linear: a hook on saved tensors gave back another tensor than it was given")
+        (m, n, k), (need_x, need_w) = ctx.sizes, ctx.needs_input_grad
         dx = dw = None
         q = quantize(dy, rows=need_x, cols=need_w)
         rows, cols = q if need_x and need_w else (q, q)
-        if need_x:
-            dx = matmul(rows, wt, ctx.types[0])   # dy [M, N] (w^T [K, N])^T
-        if need_w:
-            dw = matmul(cols, xt, ctx.types[1])   # dy^T [N, M] (x^T [K, M])^T
+        if need_x:  # dy [M, N] (w^T [K, N])^T
+            dx = matmul(rows, MXMatrix._within(kept, ctx.at, k, n), ctx.types[0])
+        if need_w:  # dy^T [N, M] (x^T [K, M])^T
+            dw = matmul(cols, MXMatrix._within(kept, 0, k, m), ctx.types[1])
         return dx, dw
 
 

@@ -612,3 +612,58 @@ def test_matrices_of_a_capture_read_on_its_second_stream():
     del later
     mx.quantize(x)
     assert not mx._unfreed
+
+
+def _layer(M, N, K, xtype=torch.bfloat16, seed=80):
+    x = _matrix(M, K, xtype, seed).requires_grad_()
+    w = _matrix(N, K, torch.float32, seed + 1).requires_grad_()
+    return x, w, _matrix(M, N, xtype, seed + 2)
+
+
+@pytest.mark.gpu
+def test_what_the_backward_pass_reads_goes_with_it():
+    """The 4-bit operands are freed by the backward pass, not with y; a second one is refused, unless
+    they were asked to stay."""
+    x, w, dy = _layer(2048, 1024, 4096)
+    torch.autograd.grad(mx.linear(x, w), (x, w), dy)
+    before = torch.cuda.memory_allocated()
+    y = mx.linear(x, w)
+    dx, dw = torch.autograd.grad(y, (x, w), dy)
+    results = sum(t.numel() * t.element_size() for t in (y, dx, dw))
+    # (the allocator hands out multiples of 512 bytes)
+    assert torch.cuda.memory_allocated() - before <= results + 4 * 512
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(y, (x, w), dy)
+    y = mx.linear(x, w)
+    for keep in (True, False):
+        again = torch.autograd.grad(y, (x, w), dy, retain_graph=keep)
+        assert torch.equal(again[0], dx) and torch.equal(again[1], dw)
+
+
+@pytest.mark.gpu
+def test_hooks_on_saved_tensors_and_checkpoints():
+    """What is kept for the backward pass goes through saved-tensor hooks (here to the host and back), and
+    a checkpointed layer keeps nothing."""
+    from torch.utils.checkpoint import checkpoint
+    x, w, dy = _layer(300, 260, 520)
+    want = torch.autograd.grad(mx.linear(x, w), (x, w), dy)
+    packed = []
+
+    def pack(t):
+        packed.append(t.numel() * t.element_size())
+        return t.cpu()
+
+    with torch.autograd.graph.saved_tensors_hooks(pack, lambda t: t.cuda()):
+        y = mx.linear(x, w)
+    got = torch.autograd.grad(y, (x, w), dy)
+    assert sum(packed) == sum(sum(mx.tula_mx_size(r, c)) for r, c in ((520, 300), (520, 260)))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    y = checkpoint(mx.linear, x, w, use_reentrant=False)
+    assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(y, (x, w), dy), want))
+    checkpoint(mx.linear, x, w, use_reentrant=True).backward(dy)
+    assert torch.equal(x.grad, want[0]) and torch.equal(w.grad, want[1])
+    for wrong in (lambda t: t.cpu(), lambda t: t[:-16], lambda t: t.int()):
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: t, wrong):
+            y = mx.linear(x, w)
+        with pytest.raises(RuntimeError):
+            torch.autograd.grad(y, (x, w), dy)
