@@ -324,8 +324,9 @@ def tula_mx_error(stream=None) -> int:
 
 class _Linear(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w):
-        need_x, need_w = ctx.needs_input_grad
+    def forward(ctx, x, w, recorded):
+        # (needs_input_grad follows requires_grad, also where no gradient is recorded)
+        need_x, need_w = (n and recorded for n in ctx.needs_input_grad[:2])
         (m, k), n = x.shape, w.shape[0]
         dev, x_kind, w_kind = _on_gpu(x, w), _type(x.dtype, "linear"), _type(w.dtype, "linear")
         # what the backward pass multiplies by is kept in 4 bits: x^T for dw, then w^T for dx
@@ -350,7 +351,7 @@ class _Linear(torch.autograd.Function):
         kept, = ctx.saved_tensors
         if kept.dtype != torch.uint8 or kept.numel() != ctx.end or kept.device != ctx.device or not kept.is_contiguous():
             raise RuntimeError("linear: a hook on saved tensors gave back another tensor than it was given")
-        (m, n, k), (need_x, need_w) = ctx.sizes, ctx.needs_input_grad
+        (m, n, k), (need_x, need_w, _) = ctx.sizes, ctx.needs_input_grad
         dx = dw = None
         q = quantize(dy, rows=need_x, cols=need_w)
         rows, cols = q if need_x and need_w else (q, q)
@@ -358,7 +359,7 @@ class _Linear(torch.autograd.Function):
             dx = matmul(rows, MXMatrix._within(kept, ctx.at, k, n), ctx.types[0])
         if need_w:  # dy^T [N, M] (x^T [K, M])^T
             dw = matmul(cols, MXMatrix._within(kept, 0, k, m), ctx.types[1])
-        return dx, dw
+        return dx, dw, None
 
 
 def linear(x: torch.Tensor, w: torch.Tensor) -> torch.Tensor:
@@ -368,6 +369,7 @@ def linear(x: torch.Tensor, w: torch.Tensor) -> torch.Tensor:
     of x)."""
     if x.shape[-1] != w.shape[-1] or w.dim() != 2:
         raise ValueError(f"linear: x {tuple(x.shape)} and w {tuple(w.shape)}")
+    recorded = torch.is_grad_enabled()
     if x.dim() == 2:
-        return _Linear.apply(x, w)
-    return _Linear.apply(x.reshape(-1, x.shape[-1]), w).view(*x.shape[:-1], w.shape[0])
+        return _Linear.apply(x, w, recorded)
+    return _Linear.apply(x.reshape(-1, x.shape[-1]), w, recorded).view(*x.shape[:-1], w.shape[0])

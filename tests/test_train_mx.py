@@ -667,3 +667,29 @@ def test_hooks_on_saved_tensors_and_checkpoints():
             y = mx.linear(x, w)
         with pytest.raises(RuntimeError):
             torch.autograd.grad(y, (x, w), dy)
+
+
+@pytest.mark.gpu
+def test_linear_without_gradients_quantises_one_form(monkeypatch):
+    """Where no gradient is recorded, or none is asked for, no transpose is quantised."""
+    x, w, dy = _layer(70, 50, 96)
+    want = mx.linear(x, w).detach()
+    forms, call = [], mx._call
+
+    def noted(name, dev, *args):
+        if name == "tula_mx_quantize":
+            forms.append((args[5] is not None, args[7] is not None))
+        return call(name, dev, *args)
+
+    monkeypatch.setattr(mx, "_call", noted)
+    for mode in (torch.no_grad, torch.inference_mode):
+        with mode():
+            y = mx.linear(x, w)
+        assert torch.equal(y, want) and not y.requires_grad
+        assert forms == [(True, False)] * 2
+        forms.clear()
+    mx.linear(x.detach(), w.detach())
+    assert forms == [(True, False)] * 2
+    forms.clear()
+    dw = torch.autograd.grad(mx.linear(x.detach(), w), w, dy)[0]        # dw reads x^T and dy^T alone
+    assert forms == [(True, True), (True, False), (False, True)] and dw.shape == w.shape
