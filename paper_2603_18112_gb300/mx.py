@@ -372,4 +372,6 @@ def linear(x: torch.Tensor, w: torch.Tensor) -> torch.Tensor:
     recorded = torch.is_grad_enabled()
     if x.dim() == 2:
         return _Linear.apply(x, w, recorded)
-    return _Linear.apply(x.reshape(-1, x.shape[-1]), w, recorded).view(*x.shape[:-1], w.shape[0])
+    # (the rows are counted here: reshape cannot infer them where x has no columns)
+    rows = x.reshape(x.shape[:-1].numel(), x.shape[-1])
+    return _Linear.apply(rows, w, recorded).view(*x.shape[:-1], w.shape[0])

@@ -693,3 +693,15 @@ def test_linear_without_gradients_quantises_one_form(monkeypatch):
     forms.clear()
     dw = torch.autograd.grad(mx.linear(x.detach(), w), w, dy)[0]        # dw reads x^T and dy^T alone
     assert forms == [(True, True), (True, False), (False, True)] and dw.shape == w.shape
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape,N", [((2, 3, 0), 5), ((0,), 4), ((0, 3, 8), 5), ((2, 0, 0), 3), ((2, 3, 8), 0)])
+def test_linear_of_empty_dimensions(shape, N):
+    """Ones and a sum over nothing among them: each sum counts its terms."""
+    x = torch.ones(shape, device="cuda", requires_grad=True)
+    w = torch.ones(N, shape[-1], device="cuda", requires_grad=True)
+    y = mx.linear(x, w)
+    assert y.shape == (*shape[:-1], N) and bool((y == shape[-1]).all())
+    dx, dw = torch.autograd.grad(y, (x, w), torch.ones_like(y))
+    assert dx.shape == x.shape and dw.shape == w.shape and bool((dw == x.shape[:-1].numel()).all())
