@@ -432,6 +432,24 @@ def test_adamw_at_the_ends_of_its_hyperparameters(beta1, beta2, eps, wd):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("eps", [0.0, 1e-8, 1.0])
+@pytest.mark.parametrize("sizes", [[40_001], [2_600_000, 33]])
+def test_adamw_rounds_as_fp32_does(eps, sizes):
+    """Zero weights and moments and betas of 0, as of a bias before its first step: v = d^2,
+    w = -lr m / (sqrt(v) + eps), a rounding for each operation, bit for bit."""
+    _, g, _, _, _ = _adam_state(sizes, torch.float32, "padded", None, 18)
+    w, m, v = ([torch.zeros_like(x) for x in g] for _ in range(3))
+    O.AdamWStep(w, g, m, v)(3e-3, (0.0, 0.0), eps, 0.0)
+    for i, x in enumerate(g):
+        d = x.cpu().numpy()
+        square = d * d
+        with np.errstate(invalid="ignore"):
+            quotient = d / (np.sqrt(square) + np.float32(eps))
+        assert np.array_equal(m[i].cpu().numpy(), d) and np.array_equal(v[i].cpu().numpy(), square)
+        assert np.array_equal(w[i].cpu().numpy(), -(np.float32(3e-3) * quotient), equal_nan=True)
+
+
+@pytest.mark.gpu
 def test_refusals_of_a_plan_in_use():
     w, g, m, v, _ = _adam_state([300], torch.float32, "padded", None, 14)
     clip, step = O.GradClipper(g), O.AdamWStep(w, g, m, v)
