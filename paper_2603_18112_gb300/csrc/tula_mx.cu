@@ -1435,9 +1435,9 @@ template <typename T, bool Aligned>
 int launch_quantize(const QuantArgs &a, unsigned grid, cudaStream_t s) {
     static std::atomic<uint64_t> done[3];
     const int which = a.codes && a.codes_t ? 0 : a.codes ? 1 : 2;
-    void (*k)(const QuantArgs) = which == 0   ? k_quantize<T, Aligned, true, true>
-                                 : which == 1 ? k_quantize<T, Aligned, true, false>
-                                              : k_quantize<T, Aligned, false, true>;
+    void (*k)(const QuantArgs) = which == 0 ? k_quantize<T, Aligned, true, true> : k_quantize<T, Aligned, true, false>;
+    if constexpr (!Aligned)  // (aligned rows' transpose alone goes by TMA)
+        if (which == 2) k = k_quantize<T, Aligned, false, true>;
     const int smem = a.codes_t ? QuantShape<T>::kSmem : 0;
     const int rc = allow_smem((const void *)k, smem, &done[which]);
     if (rc) return rc;
