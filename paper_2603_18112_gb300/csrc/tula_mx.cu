@@ -1044,10 +1044,11 @@ __global__ void __launch_bounds__(kMmaThreads) k_matmul(const __grid_constant__ 
 // (cta_group::2): each holds its 128 rows of A, 128 of the 256 rows of B, and its 128 rows of
 // accumulators.  A stage of 256 columns is 35.8 KB a CTA for 2 x 128 x 256 x 256 operations, twice
 // the operations a byte of 128 x 128 tiles; an SM takes in 64 bytes a clock, which bounds 8192^3 at
-// 135 us (149 measured, the tensor pipe active 78 % of it).  Products with short sums are bound by
-// writing (16384 x 16384 x 512: 143 us, fill_ of as much 136).  Persistent: a pair takes every n-th tile.  Tensor memory has 512 columns: two accumulators of
-// 256 that overlap in 32, and the scales' 24.  Four warps read an accumulator back, the columns that
-// the other one needs first, while the next tile's instructions run.
+// 135 us (150 measured a few at a time, 160 over seconds; the tensor pipe active 78 % of it).  Products
+// with short sums are bound by writing (16384 x 16384 x 512: 143 to 147 us, fill_ of as much 136).
+// Persistent: a pair takes every n-th tile.  Tensor memory has 512 columns: two accumulators of 256 that
+// overlap in 32, and the scales' 24.  Four warps read an accumulator back, the columns that the other
+// one needs first, while the next tile's instructions run.
 
 constexpr int kPairThreads = 192;
 struct Pair {

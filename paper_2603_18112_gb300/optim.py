@@ -146,7 +146,8 @@ class _Plan:
 
 class GradClipper:
     """The global norm over a fixed list of gradients, and clipping by it.  ``record`` holds what
-    the last call left (TULA_RECORD_*), on the GPU."""
+    the last call left (TULA_RECORD_*), on the GPU.  The tensors are those it was made with: a gradient
+    that is replaced, as by zero_grad's default, is not seen."""
 
     def __init__(self, grads):
         self._plan = _Plan(grads)
@@ -181,7 +182,8 @@ class AdamWStep:
 
     max_norm > 0 clips by the global norm (the gradients stay as they are); skip_nonfinite leaves a
     step out whose norm is not finite.  ``steps`` is int64 [taken, left out] and ``record`` as in
-    GradClipper, both on the GPU; exp_avgs and exp_avg_sqs are zero-filled before the first step."""
+    GradClipper, both on the GPU; exp_avgs and exp_avg_sqs are zero-filled before the first step.  The
+    tensors, gradients among them, are those it was made with, as in GradClipper."""
 
     def __init__(self, params, grads, exp_avgs, exp_avg_sqs, copies=None, *, max_norm=0.0,
                  skip_nonfinite=False, steps=None):
