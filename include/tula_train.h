@@ -1,7 +1,7 @@
 /*
  * Training in reduced precision next to the optimizer step of tula_ags.h: the global gradient norm
- * and clipping, AdamW on fp32 master weights, and microscaled 4-bit matrices (MXFP4).  Part of
- * libtula_ags.
+ * and clipping, AdamW on fp32 master weights, microscaled 4-bit matrices (MXFP4) and 8-bit
+ * floating-point ones.  Part of libtula_ags.
  *
  * Conventions are those of tula_ags.h: caller-owned device memory; calls are asynchronous on
  * `stream` (a cudaStream_t; NULL = the legacy default stream), allocate nothing, never synchronize
@@ -159,7 +159,7 @@ int tula_mx_matmul(const void *a_codes, const void *a_scales, const void *b_code
                    void *stream);
 
 /*
- * The error word of these kernels on the current device, read after the work already enqueued on
+ * The error word of the MXFP4 kernels on the current device, read after the work already enqueued on
  * `stream` (the call waits for that stream), then cleared: 0 when every bounded wait inside the
  * kernels completed; bit 0 set when one ran out, bit 1 when shared memory did not start where a
  * product's kernel needs it, and the results since the last read are then not valid.
@@ -170,6 +170,58 @@ int tula_mx_error(void *stream, int *error_out);
  * barrier that nothing arrives on (about two seconds) and records it as they do: tula_mx_error then
  * reports bit 0.  The CUDA context stays usable. */
 int tula_mx_check_wait_timeout(void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * 8-bit floating-point matrices with a scale for each block of 128
+ * ------------------------------------------------------------------------------------------ */
+
+/* Codes: E4M3 (largest 448) and E5M2 (largest 57344). */
+#define TULA_FP8_E4M3 0
+#define TULA_FP8_E5M2 1
+
+/*
+ * A rows x cols matrix of 8-bit codes: blocks of 128 elements along a row (the last one of a row may
+ * be shorter), or of 128 rows by 128 columns, share a scale 2^(s - 127), s an E8M0 byte (255: NaN).
+ * With P = cols rounded up to a multiple of 128:
+ *   codes   [rows][P] bytes; zero beyond the matrix
+ *   scales  [ceil(rows / 128)][ceil(P / 512)] tiles of 512 bytes, each of 128 rows by 4 blocks of
+ *           columns: byte (row % 32) * 16 + (row % 128) / 32 * 4 + block % 4; zero beyond the matrix.
+ *           (A block of 128 rows has its scale in each of them: what reads the matrix need not know.)
+ * Both 16-byte aligned.
+ */
+/* Bytes of a matrix; sizes as for tula_mx_size. */
+int tula_fp8_size(int64_t rows, int64_t cols, size_t *code_bytes, size_t *scale_bytes);
+
+/*
+ * Quantises x, device [rows][stride] of `type` (stride >= cols, in elements), to `code`: the scale is
+ * the least power of two (2^-127 at least) that brings the block's largest magnitude to the code's
+ * largest value or below, elements are x / 2^(s - 127) to the nearest code, ties to the even one; the
+ * division is exact.  A block with an infinity or NaN gets s = 255 and codes 0.
+ *   square             blocks of 128 x 128 (1) or of 1 x 128 (0)
+ *   codes, scales      x itself; both or neither
+ *   codes_t, scales_t  its transpose (cols x rows), blocks along x's columns (square: the same blocks);
+ *                      both or neither
+ * One pair at least; with both, x is read once.  rows, cols >= 0 (0: nothing is done).
+ */
+int tula_fp8_quantize(const void *x, int type, int64_t rows, int64_t cols, int64_t stride, int code,
+                      int square, void *codes, void *scales, void *codes_t, void *scales_t,
+                      void *stream);
+
+/* The values a matrix stands for, rounded to `type`, into out, device [rows][cols]. */
+int tula_fp8_dequantize(const void *codes, const void *scales, int64_t rows, int64_t cols, int code,
+                        void *out, int type, void *stream);
+
+/*
+ * out = A B^T, A an M x K and B an N x K matrix of 8-bit codes (each of its own kind of code); out
+ * device [M][N] of `out_type`.  As tula_mx_matmul: products of codes and scales are exact and added in
+ * fp32 by the tensor cores in an order that depends on M, N and K only; the sum is rounded once.
+ */
+int tula_fp8_matmul(const void *a_codes, const void *a_scales, int a_code, const void *b_codes,
+                    const void *b_scales, int b_code, int64_t M, int64_t N, int64_t K, void *out,
+                    int out_type, void *stream);
+
+/* The error word of the 8-bit products, as tula_mx_error. */
+int tula_fp8_error(void *stream, int *error_out);
 
 #ifdef __cplusplus
 }

@@ -10,7 +10,7 @@ HERE = Path(__file__).resolve().parent
 ROOT = HERE.parent
 CSRC = HERE / "csrc"
 SRC = CSRC / "tula_ags.cu"
-SRCS = [SRC, CSRC / "tula_train.cu", CSRC / "tula_mx.cu"]
+SRCS = [SRC, CSRC / "tula_train.cu", CSRC / "tula_mx.cu", CSRC / "tula_fp8.cu"]
 HEADER = ROOT / "include" / "tula_ags.h"
 TRAIN_HEADER = ROOT / "include" / "tula_train.h"
 LIB = HERE / "libtula_ags.so"
@@ -39,7 +39,7 @@ def _stale() -> bool:
     if not LIB.exists():
         return True
     t = LIB.stat().st_mtime
-    return any(p.stat().st_mtime > t for p in (*SRCS, CSRC / "tula_common.h", HEADER, TRAIN_HEADER))
+    return any(p.stat().st_mtime > t for p in (*CSRC.iterdir(), HEADER, TRAIN_HEADER))
 
 
 def build(force: bool = False, verbose: bool = False) -> Path:

@@ -138,53 +138,48 @@ class _Block:
         return {"shape": (self.size,), "typestr": "|u1", "data": (self.ptr, False), "version": 3}
 
 
-def _bytes(rows, cols):
-    """Of a matrix's scales and codes, which follow them."""
-    return (rows + 127) // 128 * ((cols + 127) // 128) * 512 + rows * ((cols + 127) // 128) * 64
-
-
-class MXMatrix:
-    """A rows x cols matrix in MXFP4: ``codes`` uint8 [rows, P / 2] and ``scales`` uint8
-    [ceil(rows / 128), P / 128, 32, 4, 4], P = cols rounded up to a multiple of 128; of any shapes
-    of those sizes, contiguous, on one GPU.  Not to be changed once made.  Its memory belongs to the
-    stream it was made on, as a tensor's does; products and readings on other streams are waited for
-    before it is used again, once they are ordered after its making.  (Tensors taken from ``codes`` and
-    ``scales`` keep it alive, but what other operations read of them on other streams is not noted.)"""
+class _Quantised:
+    """A quantised matrix: codes and scales on one GPU, in one allocation of this module's or a caller's
+    tensors.  A class gives the sizes and shapes of its format."""
 
     __slots__ = ("rows", "cols", "device", "dev", "code_ptr", "scale_ptr", "_codes", "_scales", "_block")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int):
-        tiles = (cols + 127) // 128
         if (codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or not codes.is_contiguous()
-                or not scales.is_contiguous() or rows < 0 or cols < 0 or codes.numel() != rows * tiles * 64
-                or scales.numel() != (rows + 127) // 128 * tiles * 512):
+                or not scales.is_contiguous() or rows < 0 or cols < 0
+                or (scales.numel(), codes.numel()) != self._sizes(rows, cols)):
             raise ValueError(f"not the codes and scales of a {rows} x {cols} matrix")
         self.rows, self.cols, self._codes, self._scales, self._block = rows, cols, codes, scales, None
         self.dev, self.device = _on_gpu(codes, scales), codes.device
         self.code_ptr, self.scale_ptr = codes.data_ptr(), scales.data_ptr()
 
     @classmethod
-    def empty(cls, rows: int, cols: int, device: torch.device) -> "MXMatrix":
+    def empty(cls, rows: int, cols: int, device: torch.device):
         """One to quantise into, in one allocation."""
         self = cls.__new__(cls)
-        tiles = (cols + 127) // 128
-        n = (rows + 127) // 128 * tiles * 512
+        n, codes = cls._sizes(rows, cols)
         self.rows, self.cols, self.dev, self.device = rows, cols, device.index, device
-        self._block = block = _Block(n + rows * tiles * 64, device.index)
+        self._block = block = _Block(n + codes, device.index)
         self._codes = self._scales = None
         self.scale_ptr = block.ptr
         self.code_ptr = block.ptr + n
         return self
 
     @classmethod
-    def _within(cls, memory: torch.Tensor, at: int, rows: int, cols: int) -> "MXMatrix":
+    def _within(cls, memory: torch.Tensor, at: int, rows: int, cols: int):
         """One to quantise into, or quantised there before, `at` bytes into a uint8 tensor that outlives it."""
         self = cls.__new__(cls)
         self.rows, self.cols, self.dev, self.device = rows, cols, memory.get_device(), memory.device
         self._codes = self._scales = self._block = None
         self.scale_ptr = memory.data_ptr() + at
-        self.code_ptr = self.scale_ptr + (rows + 127) // 128 * ((cols + 127) // 128) * 512
+        self.code_ptr = self.scale_ptr + cls._sizes(rows, cols)[0]
         return self
+
+    @classmethod
+    def _bytes(cls, rows, cols):
+        """Of the scales and the codes, which follow them."""
+        n, codes = cls._sizes(rows, cols)
+        return n + codes
 
     def _reads(self):
         """The current stream is about to read it."""
@@ -193,11 +188,12 @@ class MXMatrix:
             block.read_elsewhere(_raw_stream(self.dev))
 
     def _split(self):
-        n, tiles = self.code_ptr - self.scale_ptr, (self.cols + 127) // 128
+        n = self.code_ptr - self.scale_ptr
         all_ = (torch.as_tensor(self._block, device=self.device) if self._block.size
                 else torch.empty(0, dtype=torch.uint8, device=self.device))
-        self._scales = all_[:n].view((self.rows + 127) // 128, tiles, 32, 4, 4)
-        self._codes = all_[n:].view(self.rows, tiles * 64)
+        scales, codes = self._shapes(self.rows, self.cols)
+        self._scales = all_[:n].view(scales)
+        self._codes = all_[n:].view(codes)
 
     @property
     def codes(self) -> torch.Tensor:
@@ -210,6 +206,28 @@ class MXMatrix:
         if self._scales is None:
             self._split()
         return self._scales
+
+
+class MXMatrix(_Quantised):
+    """A rows x cols matrix in MXFP4: ``codes`` uint8 [rows, P / 2] and ``scales`` uint8
+    [ceil(rows / 128), P / 128, 32, 4, 4], P = cols rounded up to a multiple of 128; of any shapes
+    of those sizes, contiguous, on one GPU.  Not to be changed once made.  Its memory belongs to the
+    stream it was made on, as a tensor's does; products and readings on other streams are waited for
+    before it is used again, once they are ordered after its making.  (Tensors taken from ``codes`` and
+    ``scales`` keep it alive, but what other operations read of them on other streams is not noted.)"""
+
+    __slots__ = ()
+
+    @staticmethod
+    def _sizes(rows, cols):
+        """Bytes of the scales and of the codes."""
+        tiles = (cols + 127) // 128
+        return (rows + 127) // 128 * tiles * 512, rows * tiles * 64
+
+    @staticmethod
+    def _shapes(rows, cols):
+        tiles = (cols + 127) // 128
+        return ((rows + 127) // 128, tiles, 32, 4, 4), (rows, tiles * 64)
 
 
 def tula_mx_size(rows: int, cols: int) -> tuple[int, int]:
@@ -331,8 +349,8 @@ class _Linear(torch.autograd.Function):
         dev, x_kind, w_kind = _on_gpu(x, w), _type(x.dtype, "linear"), _type(w.dtype, "linear")
         # what the backward pass multiplies by is kept in 4 bits: x^T for dw, then w^T for dx
         ctx.types, ctx.sizes, ctx.device = (x.dtype, w.dtype), (m, n, k), x.device
-        ctx.at = at = _bytes(k, m) if need_w else 0
-        ctx.end = end = at + (_bytes(k, n) if need_x else 0)
+        ctx.at = at = MXMatrix._bytes(k, m) if need_w else 0
+        ctx.end = end = at + (MXMatrix._bytes(k, n) if need_x else 0)
         xt = wt = None
         if need_x or need_w:
             kept = torch.empty(end, dtype=torch.uint8, device=x.device)
