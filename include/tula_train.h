@@ -1,7 +1,7 @@
 /*
  * Training in reduced precision next to the optimizer step of tula_ags.h: the global gradient norm
- * and clipping, AdamW on fp32 master weights, microscaled 4-bit matrices (MXFP4) and 8-bit
- * floating-point ones.  Part of libtula_ags.
+ * and clipping, AdamW on fp32 master weights, microscaled 4-bit matrices (MXFP4), 8-bit
+ * floating-point ones, and layer norm.  Part of libtula_ags.
  *
  * Conventions are those of tula_ags.h: caller-owned device memory; calls are asynchronous on
  * `stream` (a cudaStream_t; NULL = the legacy default stream), allocate nothing, never synchronize
@@ -222,6 +222,37 @@ int tula_fp8_matmul(const void *a_codes, const void *a_scales, int a_code, const
 
 /* The error word of the 8-bit products, as tula_mx_error. */
 int tula_fp8_error(void *stream, int *error_out);
+
+/* ---------------------------------------------------------------------------------------------
+ * Layer norm
+ * ------------------------------------------------------------------------------------------ */
+
+/*
+ * y = (x - mean) r w + b for each row of x, device [rows][stride] of `type` (stride >= cols, in
+ * elements), mean and var (the mean of (x - mean)^2) over its cols elements, r = 1 / sqrt(var + eps);
+ * y device [rows][cols] of `type`.  weight and bias: device [cols] of param_type, or NULL (1 and 0).
+ * stats: device fp32 [rows][2], mean and r for the backward pass, or NULL.  In fp32, rounded once (the
+ * squares of x - mean have to lie in its range).  A row with an infinity or NaN gives NaN.  rows below
+ * 2^40, cols up to 2^24, eps >= 0 (TULA_ERR_ARG).
+ */
+int tula_layer_norm(const void *x, int type, int64_t rows, int64_t cols, int64_t stride,
+                    const void *weight, const void *bias, int param_type, float eps, void *y,
+                    float *stats, void *stream);
+
+/*
+ * Its gradients.  With n = (x - mean) r and g = dy w:
+ *   dx = r (g - mean(g) - n mean(g n)),  dweight = sum of dy n,  dbias = sum of dy  (over the rows)
+ * dy device [rows][dy_stride], x and stats of the forward pass; dx device [rows][cols] of `type`,
+ * dweight and dbias device [cols] of param_type; each of the three may be NULL.  The sums over the rows
+ * are taken in fp32 in an order that depends on the sizes and the device, rounded once.  The
+ * workspace, of tula_layer_norm_workspace_size bytes (16-byte aligned, any contents), is needed for
+ * dweight and dbias and may be used again by what is enqueued after.
+ */
+int tula_layer_norm_workspace_size(int64_t rows, int64_t cols, size_t *bytes);
+int tula_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, int64_t stride, int type,
+                             int64_t rows, int64_t cols, const void *weight, int param_type,
+                             const float *stats, void *dx, void *dweight, void *dbias,
+                             void *workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -10,7 +10,8 @@ HERE = Path(__file__).resolve().parent
 ROOT = HERE.parent
 CSRC = HERE / "csrc"
 SRC = CSRC / "tula_ags.cu"
-SRCS = [SRC, CSRC / "tula_train.cu", CSRC / "tula_mx.cu", CSRC / "tula_fp8.cu"]
+SRCS = [SRC, CSRC / "tula_train.cu", CSRC / "tula_mx.cu", CSRC / "tula_fp8.cu",
+        CSRC / "tula_norm.cu"]
 HEADER = ROOT / "include" / "tula_ags.h"
 TRAIN_HEADER = ROOT / "include" / "tula_train.h"
 LIB = HERE / "libtula_ags.so"
