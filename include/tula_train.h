@@ -1,11 +1,11 @@
 /*
  * Training in reduced precision next to the optimizer step of tula_ags.h: the global gradient norm
- * and clipping, AdamW on fp32 master weights, microscaled 4-bit matrices (MXFP4), 8-bit
+ * and clipping, AdamW on fp32 master weights, Muon, microscaled 4-bit matrices (MXFP4), 8-bit
  * floating-point ones, and layer norm.  Part of libtula_ags.
  *
  * Conventions are those of tula_ags.h: caller-owned device memory; calls are asynchronous on
  * `stream` (a cudaStream_t; NULL = the legacy default stream), allocate nothing, never synchronize
- * the host and can be captured into a CUDA graph (tula_train_plan_create is the exception, see
+ * the host and can be captured into a CUDA graph (the plans' creation is the exception, see
  * there); the return value is TULA_OK or a TULA_ERR_* code, and argument errors are detected on
  * the host before anything is enqueued; results are bitwise reproducible run to run.
  */
@@ -253,6 +253,86 @@ int tula_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, i
                              int64_t rows, int64_t cols, const void *weight, int param_type,
                              const float *stats, void *dx, void *dweight, void *dbias,
                              void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Orthogonalised updates (Muon)
+ * ------------------------------------------------------------------------------------------ */
+
+/*
+ * O(u): u / |u| (the Frobenius norm; a matrix of zeros stays) and then ns_steps of
+ *   X <- a X + b A X + c A^2 X,  A = X X^T,  (a, b, c) = (3.4445, -4.7750, 2.0315)
+ * which bring the singular values near 1 (to 0.7 to 1.2 in five steps) and leave the singular vectors.
+ * Operands are held in fp16 and summed in fp32, so that values are within about 2e-3 of the formula's
+ * relative to the matrix's norm (more where singular values lie far below the largest one: a rounding of
+ * 2^-12 of that grows with them).  A matrix with an infinity or NaN gives NaN.
+ */
+
+/*
+ * O of each of `batch` matrices x, device [rows][stride] of `type`, batch_stride elements apart
+ * (stride >= cols, batch_stride >= 0), into out, device [batch][rows][cols] of out_type, bf16 or fp16.
+ * ns_steps in [0, 100], rows and cols up to 2^20 (TULA_ERR_ARG).  The workspace (256-byte aligned, any
+ * contents; some 6 to 8 bytes an element, TULA_ERR_ARG beyond 256 GB) may be used again by what is
+ * enqueued after; calls that share one must be ordered.  Sums depend on sizes and alignments only.
+ */
+int tula_orthogonalize_workspace_size(int64_t batch, int64_t rows, int64_t cols, size_t *bytes);
+int tula_orthogonalize(const void *x, int type, int64_t batch, int64_t rows, int64_t cols,
+                       int64_t stride, int64_t batch_stride, int ns_steps, void *out, int out_type,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
+/* A list of matrices.  HOST arrays of n_matrices entries, read by tula_muon_plan_create only; what
+ * they point to is device memory, contiguous [rows][cols], aligned to its element (matrices whose
+ * columns are a multiple of eight and whose buffers all start at 16 bytes move eight at a time). */
+typedef struct tula_muon_matrices {
+    int n_matrices;
+    const int64_t *rows, *cols;        /* >= 0 (0: skipped), up to 2^20 */
+    void *const *grad_ptrs;
+    const int *grad_types;             /* TULA_TYPE_*; NULL: all fp32 */
+    float *const *param_ptrs;          /* fp32 weights */
+    float *const *momentum_ptrs;       /* fp32, zero before the first step */
+    void *const *copy_ptrs;            /* copies of the weights for the model, or NULL */
+    const int *copy_types;             /* TULA_TYPE_BF16 or TULA_TYPE_F16; NULL: all bf16 */
+} tula_muon_matrices;
+
+/* Bytes of device workspace a plan over these sizes needs (host only): some 6 to 8 an element.
+ * TULA_ERR_ARG for sizes beyond the limits and for more than 256 GB. */
+int tula_muon_workspace_size(const int64_t *rows, const int64_t *cols, int n_matrices, size_t *bytes);
+
+/* A plan, as tula_train_plan_create's: the same contract, errors and lifetime. */
+typedef struct tula_muon_plan tula_muon_plan;
+int tula_muon_plan_create(const tula_muon_matrices *matrices, void *workspace, size_t workspace_bytes,
+                          void *stream, tula_muon_plan **plan_out);
+int tula_muon_plan_destroy(tula_muon_plan *plan);
+
+#define TULA_MUON_SCALE_RMS 0    /* 0.2 sqrt(max(rows, cols)): updates as large as AdamW's */
+#define TULA_MUON_SCALE_ASPECT 1 /* sqrt(max(1, rows / cols)) */
+
+typedef struct tula_muon_hparams {
+    double lr, momentum, weight_decay;
+    double grad_scale;    /* the loss scale: a factor the gradients hold (1: none) */
+    int nesterov;         /* what is orthogonalised: d + momentum m (1) or m (0) */
+    int ns_steps;         /* 0 to 100 */
+    int scale;            /* TULA_MUON_SCALE_* */
+    const float *record;  /* device fp32 [TULA_RECORD_LEN] as tula_grad_norm leaves it, or NULL: gradients
+                             are clipped by its coefficient, and with a norm that is not finite the step
+                             changes nothing */
+} tula_muon_hparams;
+
+/* lr 1e-3, momentum 0.95, no weight decay, grad_scale 1, nesterov, five steps, SCALE_RMS, no record. */
+void tula_muon_default_hparams(tula_muon_hparams *hp);
+
+/*
+ * One step of Muon (Jordan et al., 2024: momentum orthogonalised by Newton-Schulz steps).  With c the
+ * record's coefficient (1 without one) and s the shape's scale, for each matrix:
+ *   d = g * (c / grad_scale),  m = momentum m + d,  u = d + momentum m or m
+ *   w = w (1 - lr weight_decay) - lr s O(u)
+ * in fp32 but for O, and the copies w rounded to their type.  Gradients are read only.  0 <= momentum < 1;
+ * TULA_ERR_ARG for other values, for NaN, for grad_scale outside [2^-100, 2^100], for lr or weight_decay
+ * outside [0, 1e30], and for an unknown scale.
+ */
+int tula_muon_step(tula_muon_plan *plan, const tula_muon_hparams *hp, void *stream);
+
+/* The error word of these products, as tula_mx_error. */
+int tula_muon_error(void *stream, int *error_out);
 
 #ifdef __cplusplus
 }

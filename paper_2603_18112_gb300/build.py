@@ -11,7 +11,7 @@ ROOT = HERE.parent
 CSRC = HERE / "csrc"
 SRC = CSRC / "tula_ags.cu"
 SRCS = [SRC, CSRC / "tula_train.cu", CSRC / "tula_mx.cu", CSRC / "tula_fp8.cu",
-        CSRC / "tula_norm.cu"]
+        CSRC / "tula_norm.cu", CSRC / "tula_muon.cu"]
 HEADER = ROOT / "include" / "tula_ags.h"
 TRAIN_HEADER = ROOT / "include" / "tula_train.h"
 LIB = HERE / "libtula_ags.so"

@@ -1,0 +1,1024 @@
+// Orthogonalised updates (Muon) for sm_103a: momentum, Newton-Schulz steps, the weights' update.
+//
+// A Newton-Schulz step takes a matrix X, n its smaller side, to p(A) X with A = X X^T and
+// p(t) = a + b t + c t^2 (a tall X: to X p(X^T X)): every singular value s goes to s p(s^2), which with
+// Muon's coefficients brings it near 1 from anywhere in (0, 1] in about five steps.  With X scaled to
+// Frobenius norm 1 first,
+//
+//   k_muon_first   m = mu m + d, and the sum of squares of what is orthogonalised, a part a tile
+//   k_muon_scale   X = u / |u|, in fp16
+//   k_product      A = X X^T;  B = a I + b A + c A^2;  X' = B X: three launches a step
+//   k_muon_last    the weights and their copies, or the values themselves
+//
+// One launch covers all matrices of a list.  The products are nearly all of the work: per step 2 n^2 m and
+// 2 n^3 operations of which symmetry leaves half, and 2 n^2 m.  They run on the tensor cores from fp16
+// operands with fp32 sums.  Why fp16: all values are bounded (singular values of at most about 1.2, so
+// elements too), and its 11 bits leave the result 1 to 2e-3 off, where bf16's 8 leave it 1e-2 off; the first
+// step's X, whose elements are about 1 / sqrt(n m), is kept larger by a power of two.  B takes in a I before
+// it is rounded: then its diagonal is near 0.7 instead of -2.7, and X need not be added afterwards.
+//
+// Matrices lie in the workspace as tiles of 128 rows by 64 columns, 16 KB each, zero beyond the matrix, and
+// the whole workspace is one array of 128-byte rows to the copies: a tile is 128 of them.  Brought to shared
+// memory with the 128-byte swizzle, its rows serve as an operand with the sum along the tile's columns or
+// along its rows (the instruction's K- or MN-major forms have the same image), so nothing is ever transposed
+// in memory: X is read both ways, and tall matrices stay as they are.
+#include "tula_tc.cuh"
+
+#include <cmath>
+#include <memory>
+#include <new>
+#include <vector>
+
+namespace {
+
+constexpr double kA = 3.4445, kB = -4.7750, kC = 2.0315;
+constexpr int kTileCols = 64, kTileBytes = kTile * 128;
+constexpr int kMostGroups = 32;    // shapes of one launch
+constexpr int kMostSteps = 100;
+constexpr long long kMostSide = 1LL << 20;
+constexpr long long kMostTiles = 1LL << 24;  // of a workspace: rows of 128 bytes fit an int
+
+// ----------------------------------------------------------------------------
+// Products
+// ----------------------------------------------------------------------------
+
+// An operand of 128 (or 256, by pairs) rows of the product's side: in tiles of `pitch` to a row of them.
+// along: the sum runs along the tiles' columns (K-major); else along their rows.
+struct Side {
+    int base, step;   // the first matrix's first tile, tiles from matrix to matrix
+    int pitch, rows;  // tiles
+    int along;
+};
+struct ProductGroup {
+    Side p, q;
+    int out, out_step, out_pitch, out_rows;
+    int first, per;   // the group's first block of work, blocks to a matrix
+    int blocks_m, blocks_n;
+    int n_k;          // stages of 64
+    int n;            // where the identity ends
+    float alpha;
+};
+struct ProductArgs {
+    const unsigned char *tiles;
+    const float *record;
+    int n_groups, n_blocks;
+    int none;         // a row beyond the workspace
+    ProductGroup g[kMostGroups];
+};
+static_assert(sizeof(ProductArgs) <= 4096 - 3 * 128 - 64, "kernel parameters");
+
+// What is made of the sums: alpha times them, of a symmetric product (its blocks on and above the diagonal are
+// taken, and stored twice); the polynomial, symmetric too; alpha times them.
+enum Kind { kGram, kPoly, kApply };
+
+template <bool Pair>
+struct Shape {
+    static constexpr int kSide = Pair ? 256 : 128;  // of a block of the output
+    static constexpr int kStages = 6;
+    static constexpr int kOperand = 128 * 128;      // bytes of a stage, a CTA
+    static constexpr int kStage = 2 * kOperand;
+    static constexpr int kOuts = 4 * 2 * 4096;      // two buffers a warp
+    static constexpr int kBars = 2 * kStages + 4;
+    static constexpr int kSmem = kStages * kStage + kOuts + 8 * kBars + 16 + 1024;
+    static constexpr int kCols = 2 * kSide;         // two accumulators
+    static_assert(kSmem <= 227 * 1024, "shared memory");
+};
+constexpr int kThreads = 192;  // a copying warp, an issuing warp, four that read back
+
+// Shared-memory matrix descriptors of an operand (bit 46: their version; the 128-byte swizzle).  Along: rows of
+// 64 elements of the sum, groups of eight 1024 bytes apart.  Else: rows of 64 of the side, one for each element
+// of the sum, groups of eight 1024 bytes apart, the next 64 of the side 8192 bytes on.
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr, bool along) {
+    return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(along ? 1 : 8192 >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
+           (uint64_t)2 << 61;
+}
+// fp16 operands, fp32 sums.
+__device__ __forceinline__ uint32_t product_desc(int m, int n, bool p_along, bool q_along) {
+    return 1u << 4 | (p_along ? 0u : 1u << 15) | (q_along ? 0u : 1u << 16) | (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;
+}
+template <bool Pair>
+__device__ __forceinline__ void mma16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+    if (Pair)
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+                     "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((unsigned)add)
+                     : "memory");
+    else
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+                     "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((unsigned)add)
+                     : "memory");
+}
+
+// A block of work: its group, matrix and place.
+struct Block {
+    int matrix, m, n;
+};
+template <Kind K>
+__device__ __forceinline__ Block block_at(const ProductArgs &a, int t, const ProductGroup *&g) {
+    int i = 0;
+    while (i + 1 < a.n_groups && t >= a.g[i + 1].first) ++i;
+    g = &a.g[i];
+    const int in = t - g->first;
+    Block b;
+    b.matrix = in / g->per;
+    int k = in - b.matrix * g->per;
+    if (K == kApply) {
+        b.m = k % g->blocks_m;
+        b.n = k / g->blocks_m;
+    } else {  // columns of the upper triangle
+        b.n = 0;
+        while (k > b.n) k -= ++b.n;
+        b.m = k;
+    }
+    return b;
+}
+
+// Rows of the workspace of half h of an operand's stage.
+__device__ __forceinline__ int stage_row(const Side &s, int matrix, int i, int k, int h, int none) {
+    if (s.along) return i < s.rows ? (s.base + matrix * s.step + i * s.pitch + k) * kTile + 64 * h : none;
+    return 2 * i + h < s.pitch ? (s.base + matrix * s.step + (k >> 1) * s.pitch + 2 * i + h) * kTile + 64 * (k & 1) : none;
+}
+
+template <bool Pair, Kind K>
+__global__ void __launch_bounds__(kThreads, 1)
+    k_product(const __grid_constant__ CUtensorMap map_in, const __grid_constant__ CUtensorMap map_out,
+              const __grid_constant__ CUtensorMap map_mirror, const __grid_constant__ ProductArgs a) {
+    using S = Shape<Pair>;
+    extern __shared__ __align__(16) unsigned char raw[];
+    unsigned char *all = raw + (-smem_addr(raw) & 1023u);
+    unsigned long long *bars = reinterpret_cast<unsigned long long *>(all + S::kStages * S::kStage + S::kOuts);
+    uint32_t *tmem_at = reinterpret_cast<uint32_t *>(bars + S::kBars);
+    volatile int &dead = *reinterpret_cast<volatile int *>(tmem_at + 1);
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(kFull, tid >> 5, 0);
+    const unsigned rank = Pair ? blockIdx.x & 1 : 0;
+    const int workers = Pair ? gridDim.x / 2 : gridDim.x, worker = Pair ? blockIdx.x / 2 : blockIdx.x;
+    const uint32_t stages = smem_addr(all), outs = stages + S::kStages * S::kStage;
+    const uint32_t full = smem_addr(bars), empty = full + 8 * S::kStages, acc_full = empty + 8 * S::kStages, acc_free = acc_full + 16;
+    if (tid == 0) {
+        for (int s = 0; s < S::kStages; ++s) {
+            mbar_init(full + 8 * s, 1);
+            mbar_init(empty + 8 * s, 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(acc_full + 8 * s, 1);
+            mbar_init(acc_free + 8 * s, Pair ? 8 : 4);  // the reading warps, of both CTAs
+        }
+        dead = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        if (Pair) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_at)), "r"(S::kCols)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+        } else {
+            tmem_alloc(smem_addr(tmem_at), S::kCols);
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (Pair) cluster_sync();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = __shfl_sync(kFull, *tmem_at, 0);
+    let_next_start();
+    wait_for_previous();
+    const bool go = !a.record || a.record[TULA_RECORD_FINITE] != 0.f;
+    const int n_blocks = go ? a.n_blocks : 0;
+
+    if (warp == 0) {
+        int i = 0;  // stages filled
+        bool ok = true;
+        for (int t = worker; ok && t < n_blocks; t += workers) {
+            const ProductGroup *g;
+            const Block b = block_at<K>(a, t, g);
+            const int im = Pair ? 2 * b.m + rank : b.m, in = Pair ? 2 * b.n + rank : b.n;
+            for (int k = 0; k < g->n_k; ++k, ++i) {
+                const int s = i % S::kStages;
+                if (i >= S::kStages) ok = __all_sync(kFull, mbar_wait(empty + 8 * s, (i / S::kStages - 1) & 1, &dead));
+                if (!ok) break;
+                const uint32_t at = stages + s * S::kStage, bar = Pair ? in_cta(full + 8 * s, 0) : full + 8 * s;
+                if (elect_one()) {
+                    if (rank == 0) mbar_expect(full + 8 * s, (Pair ? 2 : 1) * S::kStage);  // both CTAs' copies
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int yp = stage_row(g->p, b.matrix, im, k, h, a.none), yq = stage_row(g->q, b.matrix, in, k, h, a.none);
+                        if (Pair) {
+                            tma_load_pair(at + 8192 * h, &map_in, 0, yp, bar);
+                            tma_load_pair(at + S::kOperand + 8192 * h, &map_in, 0, yq, bar);
+                        } else {
+                            tma_load_2d(at + 8192 * h, &map_in, 0, yp, bar);
+                            tma_load_2d(at + S::kOperand + 8192 * h, &map_in, 0, yq, bar);
+                        }
+                    }
+                }
+                __syncwarp();
+            }
+        }
+        // The issuing warp's arrivals (of the other CTA too) have all landed before the CTA ends.
+        for (int j = max(0, i - S::kStages); ok && j < i; ++j)
+            ok = __all_sync(kFull, mbar_wait(empty + 8 * (j % S::kStages), (j / S::kStages) & 1, &dead));
+        // No copy may be in flight when the CTA ends.  On the way out of a wait that ran out
+        // the copies' barrier may be the other CTA's: a millisecond is far more than they take.
+        if (!ok)
+            for (int w = 0; w < 1000; ++w) __nanosleep(1000);
+        __syncwarp();
+    } else if (warp == 1) {
+        if (rank == 0) {
+            int i = 0, n = 0;
+            bool ok = true;
+            for (int t = worker; ok && t < n_blocks; t += workers, ++n) {
+                const ProductGroup *g;
+                block_at<K>(a, t, g);
+                const bool pa = g->p.along, qa = g->q.along;
+                const uint32_t idesc = product_desc(S::kSide, S::kSide, pa, qa);
+                // from one instruction's 16 of the sum to the next: 32 bytes of a row, or 16 rows
+                const uint32_t p_next = pa ? 2 : 128, q_next = qa ? 2 : 128;
+                if (n > 1) ok = __all_sync(kFull, mbar_wait(acc_free + 8 * (n & 1), (n / 2 - 1) & 1, &dead));
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t acc = tmem + (n & 1) * S::kSide;
+                for (int k = 0; ok && k < g->n_k; ++k, ++i) {
+                    const int s = i % S::kStages;
+                    ok = __all_sync(kFull, mbar_wait(full + 8 * s, (i / S::kStages) & 1, &dead));
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t at = stages + s * S::kStage;
+                    const uint64_t dp = operand_desc(at, pa), dq = operand_desc(at + S::kOperand, qa);
+                    if (elect_one()) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) mma16<Pair>(acc, dp + j * p_next, dq + j * q_next, idesc, k > 0 || j > 0);
+                        if (Pair) {
+                            commit_pair(empty + 8 * s);
+                            if (k == g->n_k - 1) commit_pair(acc_full + 8 * (n & 1));
+                        } else {
+                            commit(empty + 8 * s);
+                            if (k == g->n_k - 1) commit(acc_full + 8 * (n & 1));
+                        }
+                    }
+                    __syncwarp();
+                }
+            }
+        }
+        __syncwarp();
+    } else {
+        const int quad = warp & 3, row = quad * 32 + lane;
+        const uint32_t buffer = outs + quad * 8192, mirror = buffer + 4096;
+        int n = 0;
+        for (int t = worker; t < n_blocks; t += workers, ++n) {
+            const ProductGroup *g;
+            const Block b = block_at<K>(a, t, g);
+            const int im = Pair ? 2 * b.m + rank : b.m;
+            if (!__all_sync(kFull, mbar_wait(acc_full + 8 * (n & 1), (n / 2) & 1, &dead))) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t acc = tmem + (n & 1) * S::kSide + ((unsigned)(quad * 32) << 16);
+            const int out = g->out + b.matrix * g->out_step;
+#pragma unroll 1
+            for (int c = 0; c < S::kSide / kTileCols; ++c) {
+                const int j = b.n * (S::kSide / kTileCols) + c;  // column of tiles
+                unsigned v[64];
+                tmem_load32(v, acc + c * kTileCols);
+                tmem_load32(v + 32, acc + c * kTileCols + 32);
+                const bool there = j < g->out_pitch && im < g->out_rows;
+                unsigned add[32];
+                if (K == kPoly && there) {
+                    const uint4 *from = reinterpret_cast<const uint4 *>(
+                        a.tiles + (size_t)(g->p.base + b.matrix * g->p.step + im * g->p.pitch + j) * kTileBytes + row * 128);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const uint4 q = from[k];
+                        add[4 * k] = q.x, add[4 * k + 1] = q.y, add[4 * k + 2] = q.z, add[4 * k + 3] = q.w;
+                    }
+                }
+                tmem_wait(v);
+                if (c == S::kSide / kTileCols - 1) {
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) arrive_cluster(Pair ? in_cta(acc_free + 8 * (n & 1), 0) : acc_free + 8 * (n & 1));
+                }
+                if (!there) continue;
+                unsigned y[32];
+#pragma unroll
+                for (int k = 0; k < 32; ++k) {
+                    float lo = __uint_as_float(v[2 * k]), hi = __uint_as_float(v[2 * k + 1]);
+                    if (K == kPoly) {
+                        __half2 h;
+                        memcpy(&h, &add[k], 4);
+                        const float2 f = __half22float2(h);
+                        const int i = im * kTile + row, col = j * kTileCols + 2 * k;
+                        lo = fmaf((float)kC, lo, fmaf((float)kB, f.x, i == col && i < g->n ? (float)kA : 0.f));
+                        hi = fmaf((float)kC, hi, fmaf((float)kB, f.y, i == col + 1 && i < g->n ? (float)kA : 0.f));
+                    } else {
+                        lo *= g->alpha;
+                        hi *= g->alpha;
+                    }
+                    const __half2 h = __floats2half2_rn(lo, hi);
+                    memcpy(&y[k], &h, 4);
+                }
+                const bool twice = K != kApply && b.m != b.n;
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // the last stores have read the buffers
+                __syncwarp();
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buffer + lane * 128 + ((k ^ (lane & 7)) << 4)),
+                                 "r"(y[4 * k]), "r"(y[4 * k + 1]), "r"(y[4 * k + 2]), "r"(y[4 * k + 3])
+                                 : "memory");
+                if (twice) {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) {
+                        asm volatile("st.shared.b16 [%0], %1;" ::"r"(mirror + 128 * k + 2 * lane), "h"((unsigned short)y[k]) : "memory");
+                        asm volatile("st.shared.b16 [%0], %1;" ::"r"(mirror + 128 * k + 64 + 2 * lane), "h"((unsigned short)(y[k] >> 16))
+                                     : "memory");
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) {
+                    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(&map_out), "r"(0),
+                                 "r"((out + im * g->out_pitch + j) * kTile + quad * 32), "r"(buffer)
+                                 : "memory");
+                    if (twice)
+                        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(&map_mirror),
+                                     "r"(32 * (quad & 1)),
+                                     "r"((out + (j >> 1) * g->out_pitch + 2 * im + (quad >> 1)) * kTile + 64 * (j & 1)), "r"(mirror)
+                                     : "memory");
+                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                }
+            }
+        }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        __syncwarp();
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    }
+    __syncthreads();
+    if (Pair) cluster_sync();
+    if (warp == 1) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (Pair)
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kCols));
+        else
+            tmem_free(tmem, S::kCols);
+    }
+}
+
+// ----------------------------------------------------------------------------
+// Before and after the products
+// ----------------------------------------------------------------------------
+//
+// One CTA a tile of 128 x 64, 32 elements a thread: eight of a row at a time where all buffers allow it (Vec:
+// rows of a multiple of eight elements at 16-byte boundaries), else one.  These stream: 8 to 22 bytes an
+// element.
+
+struct Matrix {  // of a plan
+    const void *g;
+    float *m, *w;
+    void *copy;
+    int gtype, ctype, vec, spare;
+};
+struct Group {
+    int first, per;       // the group's first tile of all, tiles to a matrix
+    int matrix;           // its first matrix
+    int rows, cols, pitch;  // pitch: tiles to a row of tiles
+    int x, x_last;        // X's first tile, and the last step's
+    float scale;          // the power of two that X is larger by at first
+    float step;           // lr times the shape's factor
+};
+struct StreamArgs {
+    const Matrix *matrices;  // a plan's, or NULL: one group,
+    const void *x;           // read from here
+    long long stride, batch_stride;
+    void *y;                 // and written there, contiguous
+    int xtype, ytype, vec;
+    unsigned char *tiles;
+    double *parts;           // sums of squares, one a tile
+    const float *record;
+    float grad_scale, mu, decay;
+    int nesterov, n_groups;
+    Group g[kMostGroups];
+};
+static_assert(sizeof(StreamArgs) <= 4096 - 64, "kernel parameters");
+
+constexpr int kStreamThreads = 256;
+
+struct Place {
+    const Group *g;
+    int matrix, tile;      // of the group, of the matrix
+    int row0, col0;
+};
+__device__ __forceinline__ Place place_of(const StreamArgs &a, int t) {
+    int i = 0;
+    while (i + 1 < a.n_groups && t >= a.g[i + 1].first) ++i;
+    Place p;
+    p.g = &a.g[i];
+    p.matrix = (t - p.g->first) / p.g->per;
+    p.tile = t - p.g->first - p.matrix * p.g->per;
+    p.row0 = p.tile / p.g->pitch * kTile;
+    p.col0 = p.tile % p.g->pitch * kTileCols;
+    return p;
+}
+// Element k of a thread's 32, within the tile.
+template <bool Vec>
+__device__ __forceinline__ int row_of(int k) { return Vec ? (k >> 3) * 32 + (threadIdx.x >> 3) : k * 4 + (threadIdx.x >> 6); }
+template <bool Vec>
+__device__ __forceinline__ int col_of(int k) { return Vec ? (threadIdx.x & 7) * 8 + (k & 7) : threadIdx.x & 63; }
+
+__device__ __forceinline__ float value(float v) { return v; }
+__device__ __forceinline__ float value(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float value(__half v) { return __half2float(v); }
+
+template <typename T, int N>
+struct alignas(sizeof(T) * N < 16 ? sizeof(T) * N : 16) Run {
+    T v[N];
+};
+// A thread's elements of a matrix whose rows lie `stride` apart; zero beyond it.
+template <typename T, bool Vec>
+__device__ __forceinline__ void load_tile(float (&f)[32], const T *base, long long stride, const Place &p) {
+    constexpr int kN = Vec ? 8 : 1;
+    Run<T, kN> r[32 / kN];
+#pragma unroll
+    for (int k = 0; k < 32; k += kN) {
+        const int i = p.row0 + row_of<Vec>(k), j = p.col0 + col_of<Vec>(k);
+        if (i < p.g->rows && j < p.g->cols)
+            r[k / kN] = *reinterpret_cast<const Run<T, kN> *>(base + i * stride + j);
+        else
+#pragma unroll
+            for (int e = 0; e < kN; ++e) r[k / kN].v[e] = T(0.f);
+    }
+#pragma unroll
+    for (int k = 0; k < 32; ++k) f[k] = value(r[k / kN].v[k % kN]);
+}
+template <typename T, bool Vec>
+__device__ __forceinline__ void store_tile(T *base, long long stride, const Place &p, const float (&f)[32]) {
+    constexpr int kN = Vec ? 8 : 1;
+#pragma unroll
+    for (int k = 0; k < 32; k += kN) {
+        const int i = p.row0 + row_of<Vec>(k), j = p.col0 + col_of<Vec>(k);
+        if (i >= p.g->rows || j >= p.g->cols) continue;
+        Run<T, kN> r;
+#pragma unroll
+        for (int e = 0; e < kN; ++e) put(&r.v[e], f[k + e]);
+        *reinterpret_cast<Run<T, kN> *>(base + i * stride + j) = r;
+    }
+}
+template <bool Vec>
+__device__ __forceinline__ void load_typed(float (&f)[32], const void *base, int type, long long stride, const Place &p) {
+    if (type == TULA_TYPE_F32)
+        load_tile<float, Vec>(f, static_cast<const float *>(base), stride, p);
+    else if (type == TULA_TYPE_BF16)
+        load_tile<__nv_bfloat16, Vec>(f, static_cast<const __nv_bfloat16 *>(base), stride, p);
+    else
+        load_tile<__half, Vec>(f, static_cast<const __half *>(base), stride, p);
+}
+template <bool Vec>
+__device__ __forceinline__ void store_typed(void *base, int type, long long stride, const Place &p, const float (&f)[32]) {
+    if (type == TULA_TYPE_BF16)
+        store_tile<__nv_bfloat16, Vec>(static_cast<__nv_bfloat16 *>(base), stride, p, f);
+    else
+        store_tile<__half, Vec>(static_cast<__half *>(base), stride, p, f);
+}
+// A plan's element type starts at the matrix; another's matrices lie batch_stride apart.
+__device__ __forceinline__ const void *batch_at(const StreamArgs &a, int matrix) {
+    return static_cast<const unsigned char *>(a.x) + (size_t)matrix * a.batch_stride * (a.xtype == TULA_TYPE_F32 ? 4 : 2);
+}
+
+// What is orthogonalised.  First: the momentum moves on.
+template <bool First, bool Vec>
+__device__ __forceinline__ void load_update(float (&u)[32], const StreamArgs &a, const Place &p, const Matrix &q) {
+    if (!a.matrices) {
+        load_typed<Vec>(u, batch_at(a, p.matrix), a.xtype, a.stride, p);
+        return;
+    }
+    const float mult = a.record ? __fdiv_rn(a.record[TULA_RECORD_COEF], a.grad_scale) : __fdiv_rn(1.f, a.grad_scale);
+    float m[32];
+    load_typed<Vec>(u, q.g, q.gtype, p.g->cols, p);
+    load_tile<float, Vec>(m, q.m, p.g->cols, p);
+#pragma unroll
+    for (int k = 0; k < 32; ++k) {
+        const float d = __fmul_rn(u[k], mult);
+        if (First) m[k] = fmaf(a.mu, m[k], d);
+        u[k] = a.nesterov ? fmaf(a.mu, m[k], d) : m[k];
+    }
+    if (First) store_tile<float, Vec>(q.m, p.g->cols, p, m);
+}
+
+// The sum of squares of a warp's elements: in fp32 with an exact power of two taken out, so that no square
+// leaves its range.
+__device__ __forceinline__ double warp_squares(const float (&u)[32]) {
+    unsigned top = 0;
+#pragma unroll
+    for (int k = 0; k < 32; ++k) top = max(top, __float_as_uint(u[k]) & 0x7fffffffu);
+    top = __reduce_max_sync(kFull, top) >> 23;
+    const unsigned e = min(top, 253u);
+    const float f = __uint_as_float((254u - e) << 23);  // 2^(127 - e)
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < 32; ++k) {
+        const float v = __fmul_rn(u[k], f);
+        s = fmaf(v, v, s);
+    }
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
+    return (double)s * __hiloint2double((1023 + 2 * ((int)e - 127)) << 20, 0);
+}
+
+template <bool Vec>
+__device__ __forceinline__ void first_tile(const StreamArgs &a, const Place &p, const Matrix &q, double *sums) {
+    float u[32];
+    load_update<true, Vec>(u, a, p, q);
+    const double s = warp_squares(u);
+    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = s;
+}
+__device__ __forceinline__ bool left_out(const StreamArgs &a) { return a.record && a.record[TULA_RECORD_FINITE] == 0.f; }
+
+__global__ void __launch_bounds__(kStreamThreads) k_muon_first(const __grid_constant__ StreamArgs a) {
+    __shared__ double sums[kStreamThreads / 32];
+    let_next_start();
+    wait_for_previous();
+    if (left_out(a)) return;
+    const Place p = place_of(a, blockIdx.x);
+    Matrix q = {};
+    if (a.matrices) q = a.matrices[p.g->matrix + p.matrix];
+    if (a.matrices ? q.vec : a.vec)
+        first_tile<true>(a, p, q, sums);
+    else
+        first_tile<false>(a, p, q, sums);
+    __syncthreads();
+    if (threadIdx.x) return;
+    double s = 0.0;
+    for (int k = 0; k < kStreamThreads / 32; ++k) s += sums[k];
+    a.parts[blockIdx.x] = s;
+}
+
+template <bool Vec>
+__device__ __forceinline__ void scale_tile(const StreamArgs &a, const Place &p, const Matrix &q, float f1, float f2) {
+    float u[32];
+    load_update<false, Vec>(u, a, p, q);
+    __half *x = reinterpret_cast<__half *>(a.tiles + (size_t)(p.g->x + p.matrix * p.g->per + p.tile) * kTileBytes);
+    constexpr int kN = Vec ? 8 : 1;
+#pragma unroll
+    for (int k = 0; k < 32; k += kN) {
+        Run<__half, kN> r;
+#pragma unroll
+        for (int e = 0; e < kN; ++e) {
+            // (a NaN factor leaves the zeros beyond the matrix alone)
+            const bool in = p.row0 + row_of<Vec>(k + e) < p.g->rows && p.col0 + col_of<Vec>(k + e) < p.g->cols;
+            r.v[e] = __float2half_rn(in ? __fmul_rn(__fmul_rn(u[k + e], f1), f2) : 0.f);
+        }
+        *reinterpret_cast<Run<__half, kN> *>(x + row_of<Vec>(k) * kTileCols + col_of<Vec>(k)) = r;
+    }
+}
+__global__ void __launch_bounds__(kStreamThreads) k_muon_scale(const __grid_constant__ StreamArgs a) {
+    __shared__ double sums[kStreamThreads / 32];
+    let_next_start();
+    wait_for_previous();
+    if (left_out(a)) return;
+    const Place p = place_of(a, blockIdx.x);
+    // the matrix's norm, by every CTA for itself: its tiles' parts come from L2
+    const double *parts = a.parts + p.g->first + p.matrix * p.g->per;
+    double s = 0.0;
+    for (int i = threadIdx.x; i < p.g->per; i += kStreamThreads) s += __ldcg(parts + i);
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
+    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = s;
+    __syncthreads();
+    s = 0.0;
+    for (int k = 0; k < kStreamThreads / 32; ++k) s += sums[k];
+    // u / |u| as u f1 f2: f1 a power of two that brings u near 1, exactly, wherever in fp32's range it is.  A
+    // matrix of zeros stays, one with an infinity or NaN becomes NaN.
+    const double norm = sqrt(s);
+    float f1 = 0.f, f2 = 0.f;
+    if (!(norm < 1e300)) {
+        f1 = f2 = __uint_as_float(0x7fffffffu);
+    } else if (norm > 0.0) {
+        const int k = max(-126, min(126, (int)((unsigned)__double2hiint(norm) >> 20) - 1023));
+        f1 = __uint_as_float((unsigned)(127 - k) << 23);
+        f2 = (float)((double)p.g->scale / norm * __hiloint2double((1023 + k) << 20, 0));
+    }
+    Matrix q = {};
+    if (a.matrices) q = a.matrices[p.g->matrix + p.matrix];
+    if (a.matrices ? q.vec : a.vec)
+        scale_tile<true>(a, p, q, f1, f2);
+    else
+        scale_tile<false>(a, p, q, f1, f2);
+}
+
+template <bool Vec>
+__device__ __forceinline__ void last_tile(const StreamArgs &a, const Place &p, const Matrix &q) {
+    float x[32];
+    const __half *from = reinterpret_cast<const __half *>(a.tiles + (size_t)(p.g->x_last + p.matrix * p.g->per + p.tile) * kTileBytes);
+    constexpr int kN = Vec ? 8 : 1;
+#pragma unroll
+    for (int k = 0; k < 32; k += kN) {
+        const Run<__half, kN> r = *reinterpret_cast<const Run<__half, kN> *>(from + row_of<Vec>(k) * kTileCols + col_of<Vec>(k));
+#pragma unroll
+        for (int e = 0; e < kN; ++e) x[k + e] = __half2float(r.v[e]);
+    }
+    if (!a.matrices) {
+        const size_t at = (size_t)p.matrix * p.g->rows * p.g->cols * 2;
+        store_typed<Vec>(static_cast<unsigned char *>(a.y) + at, a.ytype, p.g->cols, p, x);
+        return;
+    }
+    float w[32];
+    load_tile<float, Vec>(w, q.w, p.g->cols, p);
+#pragma unroll
+    for (int k = 0; k < 32; ++k) w[k] = fmaf(-p.g->step, x[k], __fmul_rn(w[k], a.decay));
+    store_tile<float, Vec>(q.w, p.g->cols, p, w);
+    if (q.copy) store_typed<Vec>(q.copy, q.ctype, p.g->cols, p, w);
+}
+__global__ void __launch_bounds__(kStreamThreads) k_muon_last(const __grid_constant__ StreamArgs a) {
+    let_next_start();
+    wait_for_previous();
+    if (left_out(a)) return;
+    const Place p = place_of(a, blockIdx.x);
+    Matrix q = {};
+    if (a.matrices) q = a.matrices[p.g->matrix + p.matrix];
+    if (a.matrices ? q.vec : a.vec)
+        last_tile<true>(a, p, q);
+    else
+        last_tile<false>(a, p, q);
+}
+
+// ----------------------------------------------------------------------------
+// Host side
+// ----------------------------------------------------------------------------
+
+// Matrices of one shape.
+struct Kin {
+    long long rows, cols;
+    int count, matrix;  // how many, the first one's place in the table
+    int x0, x1, gram, poly;  // first tiles
+    int tile_rows() const { return (int)up(rows, kTile); }
+    int tile_cols() const { return (int)up(cols, kTileCols); }
+    int tiles() const { return tile_rows() * tile_cols(); }
+    bool wide() const { return rows <= cols; }
+    long long n() const { return std::min(rows, cols); }
+    int gram_rows() const { return (int)up(n(), kTile); }
+    int gram_cols() const { return (int)up(n(), kTileCols); }
+    int gram_tiles() const { return gram_rows() * gram_cols(); }
+    // 2^s, s the whole part of log2(sqrt(rows cols)), at most 15: no element of X, 1 at most, leaves fp16's range
+    int shift() const { return std::min(15, (int)std::floor(0.5 * std::log2((double)rows * (double)cols))); }
+};
+
+bool good_shape(long long rows, long long cols) { return rows >= 0 && cols >= 0 && rows <= kMostSide && cols <= kMostSide; }
+
+// Gives every shape its tiles; returns how many there are, -1 beyond the limit.
+long long place(std::vector<Kin> &kin) {
+    long long at = 0;
+    for (Kin &k : kin) {
+        const long long x = (long long)k.tile_rows() * k.tile_cols() * k.count, a = (long long)k.gram_rows() * k.gram_cols() * k.count;
+        if (at + 2 * x + 2 * a >= kMostTiles) return -1;
+        k.x0 = (int)at;
+        k.x1 = (int)(at + x);
+        k.gram = (int)(at + 2 * x);
+        k.poly = (int)(at + 2 * x + a);
+        at += 2 * x + 2 * a;
+    }
+    return at;
+}
+long long stream_tiles(const Kin *kin, int n) {
+    long long t = 0;
+    for (int i = 0; i < n; ++i) t += (long long)kin[i].tiles() * kin[i].count;
+    return t;
+}
+
+struct Maps {
+    CUtensorMap in, out, mirror;
+};
+bool make_maps(Maps &m, const void *tiles, long long n) {
+    const CUtensorMapDataType f16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    return make_map(&m.in, f16, tiles, n * kTile, kTileCols, 128, 64, kTileCols, CU_TENSOR_MAP_SWIZZLE_128B) &&
+           make_map(&m.out, f16, tiles, n * kTile, kTileCols, 128, 32, kTileCols, CU_TENSOR_MAP_SWIZZLE_128B) &&
+           make_map(&m.mirror, f16, tiles, n * kTile, kTileCols, 128, 64, 32, CU_TENSOR_MAP_SWIZZLE_NONE);
+}
+
+template <bool Pair, Kind K>
+int launch_product(const Maps &maps, const ProductArgs &a, int sms, cudaStream_t s) {
+    using S = Shape<Pair>;
+    static std::atomic<uint64_t> done;
+    const int rc = allow_smem((const void *)k_product<Pair, K>, S::kSmem, &done);
+    if (rc) return rc;
+    const int workers = std::min(a.n_blocks, Pair ? std::max(1, sms / 2) : sms);
+    return tula::launch(k_product<Pair, K>, dim3((unsigned)(workers * (Pair ? 2 : 1))), kThreads, S::kSmem, s, Pair ? 2 : 1, maps.in,
+                        maps.out, maps.mirror, a);
+}
+
+// One product of all shapes.  x: X's first tiles are x0 (0) or x1 (1); first: of the first step.
+template <bool Pair>
+int fill(ProductArgs &a, const Kin *kin, int n, Kind kind, int x, bool first) {
+    constexpr int kSide = Shape<Pair>::kSide;
+    long long blocks = 0;
+    a.n_groups = n;
+    for (int i = 0; i < n; ++i) {
+        const Kin &k = kin[i];
+        ProductGroup &g = a.g[i];
+        const Side sx = {x ? k.x1 : k.x0, k.tiles(), k.tile_cols(), k.tile_rows(), 1};
+        const Side sa = {k.gram, k.gram_tiles(), k.gram_cols(), k.gram_rows(), 1};
+        const Side sb = {k.poly, k.gram_tiles(), k.gram_cols(), k.gram_rows(), 1};
+        Side across = sx;
+        across.along = 0;
+        g.n = (int)k.n();
+        g.alpha = 1.f;
+        if (kind == kApply) {
+            g.p = k.wide() ? sb : sx;
+            g.q = k.wide() ? across : sb;
+            g.out = x ? k.x0 : k.x1;
+            g.out_step = k.tiles();
+            g.out_pitch = k.tile_cols();
+            g.out_rows = k.tile_rows();
+            g.blocks_m = (int)up(k.rows, kSide);
+            g.blocks_n = (int)up(k.cols, kSide);
+            g.per = g.blocks_m * g.blocks_n;
+            g.n_k = (int)up(k.n(), 64);
+            if (first) g.alpha = (float)std::ldexp(1.0, -k.shift());
+        } else {
+            g.p = g.q = kind == kPoly ? sa : k.wide() ? sx : across;
+            g.out = kind == kPoly ? k.poly : k.gram;
+            g.out_step = k.gram_tiles();
+            g.out_pitch = k.gram_cols();
+            g.out_rows = k.gram_rows();
+            g.blocks_m = g.blocks_n = (int)up(k.n(), kSide);
+            g.per = (int)((long long)g.blocks_m * (g.blocks_m + 1) / 2);
+            g.n_k = (int)up(kind == kPoly ? k.n() : std::max(k.rows, k.cols), 64);
+            if (first && kind == kGram) g.alpha = (float)std::ldexp(1.0, -2 * k.shift());
+        }
+        g.first = (int)blocks;
+        blocks += (long long)g.per * k.count;
+        if (blocks >= (1LL << 30)) return -1;
+    }
+    a.n_blocks = (int)blocks;
+    return (int)blocks;
+}
+template <Kind K>
+int product(const Maps &maps, ProductArgs &a, const Kin *kin, int n, int x, bool first, int sms, cudaStream_t s) {
+    const int pairs = fill<true>(a, kin, n, K, x, first);
+    const int singles = fill<false>(a, kin, n, K, x, first);
+    if (pairs < 0 || singles < 0) return TULA_ERR_ARG;
+    if (up(pairs, std::max(1, sms / 2)) <= up(singles, sms)) {
+        fill<true>(a, kin, n, K, x, first);
+        return launch_product<true, K>(maps, a, sms, s);
+    }
+    return launch_product<false, K>(maps, a, sms, s);
+}
+
+// All of it for shapes whose tiles are placed.  `stream`: its groups are filled here.
+int run(const Maps &maps, long long n_tiles, const Kin *kin, int n, StreamArgs &st, int steps, cudaStream_t s) {
+    const int sms = std::max(1, sm_count());
+    ProductArgs a;
+    a.tiles = st.tiles;
+    a.record = st.record;
+    a.none = (int)(n_tiles * kTile);
+    long long tiles = 0;
+    st.n_groups = n;
+    for (int i = 0; i < n; ++i) {
+        const Kin &k = kin[i];
+        Group &g = st.g[i];
+        g.first = (int)tiles;
+        g.per = k.tiles();
+        g.matrix = k.matrix;
+        g.rows = (int)k.rows;
+        g.cols = (int)k.cols;
+        g.pitch = k.tile_cols();
+        g.x = k.x0;
+        g.x_last = steps % 2 ? k.x1 : k.x0;
+        g.scale = steps ? (float)std::ldexp(1.0, k.shift()) : 1.f;
+        tiles += (long long)g.per * k.count;
+    }
+    if (tiles == 0) return TULA_OK;
+    int rc = tula::launch(k_muon_first, dim3((unsigned)tiles), kStreamThreads, 0, s, 1, st);
+    if (!rc) rc = tula::launch(k_muon_scale, dim3((unsigned)tiles), kStreamThreads, 0, s, 1, st);
+    for (int i = 0; !rc && i < steps; ++i) {
+        rc = product<kGram>(maps, a, kin, n, i & 1, i == 0, sms, s);
+        if (!rc) rc = product<kPoly>(maps, a, kin, n, i & 1, i == 0, sms, s);
+        if (!rc) rc = product<kApply>(maps, a, kin, n, i & 1, i == 0, sms, s);
+    }
+    if (!rc) rc = tula::launch(k_muon_last, dim3((unsigned)tiles), kStreamThreads, 0, s, 1, st);
+    return rc;
+}
+
+inline size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
+
+}  // namespace
+
+struct tula_muon_plan {
+    std::vector<Kin> kin;
+    Maps maps;
+    long long n_tiles;
+    const Matrix *matrices;
+    double *parts;
+    unsigned char *tiles;
+};
+
+namespace {
+
+// The list's shapes, and which one each matrix is of (-1: empty).
+bool shapes_of(const int64_t *rows, const int64_t *cols, int n, std::vector<Kin> &kin, std::vector<int> &which) {
+    which.assign((size_t)n, -1);
+    for (int i = 0; i < n; ++i) {
+        if (!good_shape(rows[i], cols[i])) return false;
+        if (rows[i] == 0 || cols[i] == 0) continue;
+        size_t k = 0;
+        while (k < kin.size() && (kin[k].rows != rows[i] || kin[k].cols != cols[i])) ++k;
+        if (k == kin.size()) kin.push_back(Kin{rows[i], cols[i], 0, 0, 0, 0, 0, 0});
+        ++kin[k].count;
+        which[i] = (int)k;
+    }
+    // the longest sums first, so that the last blocks to be taken are short ones
+    std::vector<int> order(kin.size()), where(kin.size());
+    for (size_t k = 0; k < kin.size(); ++k) order[k] = (int)k;
+    std::stable_sort(order.begin(), order.end(),
+                     [&](int a, int b) { return std::max(kin[a].rows, kin[a].cols) > std::max(kin[b].rows, kin[b].cols); });
+    std::vector<Kin> sorted;
+    int first = 0;
+    for (size_t k = 0; k < order.size(); ++k) {
+        where[order[k]] = (int)k;
+        sorted.push_back(kin[order[k]]);
+        sorted.back().matrix = first;
+        first += sorted.back().count;
+    }
+    for (int &w : which)
+        if (w >= 0) w = where[w];
+    kin.swap(sorted);
+    return true;
+}
+struct Sizes {
+    size_t table, parts, all;
+    long long n_tiles;
+};
+bool sizes_of(std::vector<Kin> &kin, Sizes &z) {
+    z.n_tiles = place(kin);
+    if (z.n_tiles < 0) return false;
+    size_t n = 0;
+    for (const Kin &k : kin) n += (size_t)k.count;
+    z.table = round_up(n * sizeof(Matrix));
+    z.parts = round_up((size_t)stream_tiles(kin.data(), (int)kin.size()) * sizeof(double));
+    z.all = z.table + z.parts + (size_t)z.n_tiles * kTileBytes;
+    return true;
+}
+
+}  // namespace
+
+extern "C" {
+
+int tula_muon_workspace_size(const int64_t *rows, const int64_t *cols, int n_matrices, size_t *bytes) {
+    if (!bytes || n_matrices < 0 || (n_matrices && (!rows || !cols))) return TULA_ERR_ARG;
+    try {
+        std::vector<Kin> kin;
+        std::vector<int> which;
+        Sizes z;
+        if (!shapes_of(rows, cols, n_matrices, kin, which) || !sizes_of(kin, z)) return TULA_ERR_ARG;
+        *bytes = std::max<size_t>(z.all, 256);
+    } catch (const std::bad_alloc &) {
+        return TULA_ERR_NO_MEMORY;
+    }
+    return TULA_OK;
+}
+
+int tula_muon_plan_create(const tula_muon_matrices *m, void *workspace, size_t workspace_bytes, void *stream, tula_muon_plan **plan_out) {
+    if (!plan_out) return TULA_ERR_ARG;
+    *plan_out = nullptr;
+    if (!m || m->n_matrices < 0) return TULA_ERR_ARG;
+    const int n = m->n_matrices;
+    if (n && (!m->rows || !m->cols || !m->grad_ptrs || !m->param_ptrs || !m->momentum_ptrs)) return TULA_ERR_ARG;
+    try {
+        std::unique_ptr<tula_muon_plan> plan(new tula_muon_plan);
+        std::vector<int> which;
+        Sizes z;
+        if (!shapes_of(m->rows, m->cols, n, plan->kin, which) || !sizes_of(plan->kin, z)) return TULA_ERR_ARG;
+        std::vector<int> next(plan->kin.size(), 0);
+        std::vector<Matrix> table(z.table / sizeof(Matrix));
+        for (int i = 0; i < n; ++i) {
+            if (which[i] < 0) continue;
+            const Kin &k = plan->kin[which[i]];
+            Matrix &q = table[(size_t)(k.matrix + next[which[i]]++)];
+            q = {};
+            q.g = m->grad_ptrs[i];
+            q.m = m->momentum_ptrs[i];
+            q.w = m->param_ptrs[i];
+            q.copy = m->copy_ptrs ? m->copy_ptrs[i] : nullptr;
+            q.gtype = m->grad_types ? m->grad_types[i] : TULA_TYPE_F32;
+            q.ctype = m->copy_types ? m->copy_types[i] : TULA_TYPE_BF16;
+            if (!good_type(q.gtype) || (q.ctype != TULA_TYPE_BF16 && q.ctype != TULA_TYPE_F16) || !q.g || !q.m || !q.w ||
+                (m->copy_ptrs && !q.copy) || !aligned(q.g, type_size(q.gtype)) || !aligned(q.m, 4) || !aligned(q.w, 4) ||
+                !aligned(q.copy, 2))
+                return TULA_ERR_ARG;
+            q.vec = k.cols % 8 == 0 && aligned(q.g, 16) && aligned(q.m, 16) && aligned(q.w, 16) && aligned(q.copy, 16);
+        }
+        if (!workspace || !aligned(workspace, 256) || workspace_bytes < std::max<size_t>(z.all, 256)) return TULA_ERR_WORKSPACE;
+        unsigned char *at = static_cast<unsigned char *>(workspace);
+        plan->n_tiles = z.n_tiles;
+        plan->matrices = reinterpret_cast<const Matrix *>(at);
+        plan->parts = reinterpret_cast<double *>(at + z.table);
+        plan->tiles = at + z.table + z.parts;
+        std::memset(&plan->maps, 0, sizeof(plan->maps));
+        if (z.n_tiles) {
+            cudaStream_t s = static_cast<cudaStream_t>(stream);
+            cudaError_t e = cudaMemcpyAsync(at, table.data(), table.size() * sizeof(Matrix), cudaMemcpyHostToDevice, s);
+            if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+            if (e != cudaSuccess) return cuda_failed(e);
+            if (!make_maps(plan->maps, plan->tiles, z.n_tiles)) return cuda_failed(cudaErrorInvalidValue);
+        }
+        *plan_out = plan.release();
+    } catch (const std::bad_alloc &) {
+        return TULA_ERR_NO_MEMORY;
+    }
+    return TULA_OK;
+}
+
+int tula_muon_plan_destroy(tula_muon_plan *plan) {
+    delete plan;
+    return TULA_OK;
+}
+
+void tula_muon_default_hparams(tula_muon_hparams *hp) {
+    if (!hp) return;
+    *hp = tula_muon_hparams{};
+    hp->lr = 1e-3;
+    hp->momentum = 0.95;
+    hp->grad_scale = 1.0;
+    hp->nesterov = 1;
+    hp->ns_steps = 5;
+    hp->scale = TULA_MUON_SCALE_RMS;
+}
+
+int tula_muon_step(tula_muon_plan *plan, const tula_muon_hparams *hp, void *stream) {
+    if (!plan || !hp) return TULA_ERR_ARG;
+    const bool good = hp->lr >= 0 && hp->lr <= 1e30 && hp->momentum >= 0 && hp->momentum < 1 && hp->weight_decay >= 0 &&
+                      hp->weight_decay <= 1e30 && hp->grad_scale >= 0x1p-100 && hp->grad_scale <= 0x1p100 && hp->ns_steps >= 0 &&
+                      hp->ns_steps <= kMostSteps && (hp->scale == TULA_MUON_SCALE_RMS || hp->scale == TULA_MUON_SCALE_ASPECT) &&
+                      aligned(hp->record, 4);
+    if (!good) return TULA_ERR_ARG;
+    StreamArgs st = {};
+    st.matrices = plan->matrices;
+    st.tiles = plan->tiles;
+    st.record = hp->record;
+    st.grad_scale = (float)hp->grad_scale;
+    st.mu = (float)hp->momentum;
+    st.decay = (float)(1.0 - hp->lr * hp->weight_decay);
+    st.nesterov = hp->nesterov != 0;
+    const int n = (int)plan->kin.size();
+    long long done = 0;
+    for (int i = 0; i < n; i += kMostGroups) {
+        const int here = std::min(kMostGroups, n - i);
+        const Kin *kin = plan->kin.data() + i;
+        for (int k = 0; k < here; ++k) {
+            const double r = (double)kin[k].rows, c = (double)kin[k].cols;
+            const double factor = hp->scale == TULA_MUON_SCALE_RMS ? 0.2 * std::sqrt(std::max(r, c)) : std::sqrt(std::max(1.0, r / c));
+            st.g[k].step = (float)(hp->lr * factor);
+        }
+        st.parts = plan->parts + done;
+        done += stream_tiles(kin, here);
+        const int rc = run(plan->maps, plan->n_tiles, kin, here, st, hp->ns_steps, static_cast<cudaStream_t>(stream));
+        if (rc) return rc;
+    }
+    return TULA_OK;
+}
+
+int tula_orthogonalize_workspace_size(int64_t batch, int64_t rows, int64_t cols, size_t *bytes) {
+    if (!bytes || batch < 0 || !good_shape(rows, cols) || batch >= kMostTiles) return TULA_ERR_ARG;
+    *bytes = 256;
+    if (batch == 0 || rows == 0 || cols == 0) return TULA_OK;
+    try {
+        std::vector<Kin> kin{Kin{rows, cols, (int)batch, 0, 0, 0, 0, 0}};
+        Sizes z;
+        if (!sizes_of(kin, z)) return TULA_ERR_ARG;
+        *bytes = z.parts + (size_t)z.n_tiles * kTileBytes;
+    } catch (const std::bad_alloc &) {
+        return TULA_ERR_NO_MEMORY;
+    }
+    return TULA_OK;
+}
+
+int tula_orthogonalize(const void *x, int type, int64_t batch, int64_t rows, int64_t cols, int64_t stride, int64_t batch_stride, int ns_steps,
+                       void *out, int out_type, void *workspace, size_t workspace_bytes, void *stream) {
+    size_t need = 0;
+    const int rc = tula_orthogonalize_workspace_size(batch, rows, cols, &need);
+    if (rc) return rc;
+    if (!good_type(type) || (out_type != TULA_TYPE_BF16 && out_type != TULA_TYPE_F16) || stride < cols || batch_stride < 0 || ns_steps < 0 ||
+        ns_steps > kMostSteps)
+        return TULA_ERR_ARG;
+    if (batch == 0 || rows == 0 || cols == 0) return TULA_OK;
+    if (!x || !out || !aligned(x, type_size(type)) || !aligned(out, 2)) return TULA_ERR_ARG;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < need) return TULA_ERR_WORKSPACE;
+    try {
+        std::vector<Kin> kin{Kin{rows, cols, (int)batch, 0, 0, 0, 0, 0}};
+        Sizes z;
+        if (!sizes_of(kin, z)) return TULA_ERR_ARG;
+        StreamArgs st = {};
+        st.x = x;
+        st.xtype = type;
+        st.stride = stride;
+        st.batch_stride = batch_stride;
+        st.y = out;
+        st.ytype = out_type;
+        st.parts = static_cast<double *>(workspace);
+        st.tiles = static_cast<unsigned char *>(workspace) + z.parts;
+        st.grad_scale = 1.f;
+        const size_t size = type_size(type), of16 = 16 / size;
+        st.vec = cols % 8 == 0 && aligned(x, 16) && aligned(out, 16) && (rows == 1 || stride % of16 == 0) &&
+                 (batch == 1 || batch_stride % of16 == 0);
+        Maps maps;
+        if (!make_maps(maps, st.tiles, z.n_tiles)) return cuda_failed(cudaErrorInvalidValue);
+        return run(maps, z.n_tiles, kin.data(), 1, st, ns_steps, static_cast<cudaStream_t>(stream));
+    } catch (const std::bad_alloc &) {
+        return TULA_ERR_NO_MEMORY;
+    }
+}
+
+int tula_muon_error(void *stream, int *error_out) { return read_error(stream, error_out); }
+
+}  // extern "C"

@@ -1,4 +1,4 @@
-"""Binding of the gradient norm, clipping and AdamW of libtula_ags (include/tula_train.h).
+"""Binding of the gradient norm, clipping, AdamW and Muon of libtula_ags (include/tula_train.h).
 
     clip = GradClipper(grads)                 # a list of fp32, bf16 or fp16 CUDA tensors
     record = clip.clip_(1.0)                  # [|G|, coefficient, finite, -] on the GPU
@@ -6,7 +6,11 @@
     step = AdamWStep(params, grads, exp_avgs, exp_avg_sqs, copies=bf16_weights, max_norm=1.0)
     step(1e-3, (0.9, 0.95), 1e-8, 0.1)        # asynchronous on the current stream
 
-Both lay their tensors out in a plan once; a call then passes scalars only.  The tensors must stay
+    step = MuonStep(matrices, grads, momenta, copies=bf16_weights)
+    step(2e-4, 0.95, 0.1, record=record)
+    o = orthogonalize(u)                      # a matrix, or a batch of them
+
+The first three lay their tensors out in a plan once; a call then passes scalars only.  The tensors must stay
 where they are (zero gradients in place).  As in ``tula_ags``, everything runs in the CUDA library.
 """
 from __future__ import annotations
@@ -39,6 +43,22 @@ class tula_adamw_hparams(ctypes.Structure):
                 ("skip_nonfinite", c_int), ("record", c_void_p), ("steps", c_void_p)]
 
 
+class tula_muon_matrices(ctypes.Structure):
+    """Mirror of the C struct tula_muon_matrices."""
+    _fields_ = [("n_matrices", c_int), ("rows", c_void_p), ("cols", c_void_p), ("grad_ptrs", c_void_p),
+                ("grad_types", c_void_p), ("param_ptrs", c_void_p), ("momentum_ptrs", c_void_p),
+                ("copy_ptrs", c_void_p), ("copy_types", c_void_p)]
+
+
+class tula_muon_hparams(ctypes.Structure):
+    """Mirror of the C struct tula_muon_hparams."""
+    _fields_ = [("lr", ctypes.c_double), ("momentum", ctypes.c_double), ("weight_decay", ctypes.c_double),
+                ("grad_scale", ctypes.c_double), ("nesterov", c_int), ("ns_steps", c_int), ("scale", c_int),
+                ("record", c_void_p)]
+
+
+MUON_SCALES = {"rms": 0, "aspect": 1}  # TULA_MUON_SCALE_*
+
 _typed = False
 
 
@@ -56,6 +76,18 @@ def _lib():
         L.tula_adamw_default_hparams.argtypes = [ctypes.POINTER(tula_adamw_hparams)]
         L.tula_adamw_default_hparams.restype = None
         L.tula_adamw_step.argtypes = [c_void_p, ctypes.POINTER(tula_adamw_hparams), c_void_p]
+        L.tula_muon_workspace_size.argtypes = [i64p, i64p, c_int, ctypes.POINTER(c_size_t)]
+        L.tula_muon_plan_create.argtypes = [ctypes.POINTER(tula_muon_matrices), c_void_p, c_size_t,
+                                            c_void_p, ctypes.POINTER(c_void_p)]
+        L.tula_muon_plan_destroy.argtypes = [c_void_p]
+        L.tula_muon_default_hparams.argtypes = [ctypes.POINTER(tula_muon_hparams)]
+        L.tula_muon_default_hparams.restype = None
+        L.tula_muon_step.argtypes = [c_void_p, ctypes.POINTER(tula_muon_hparams), c_void_p]
+        L.tula_muon_error.argtypes = [c_void_p, ctypes.POINTER(c_int)]
+        i64 = ctypes.c_int64
+        L.tula_orthogonalize_workspace_size.argtypes = [i64, i64, i64, ctypes.POINTER(c_size_t)]
+        L.tula_orthogonalize.argtypes = [c_void_p, c_int, i64, i64, i64, i64, i64, c_int, c_void_p, c_int,
+                                         c_void_p, c_size_t, c_void_p]
         _typed = True
     return L
 
@@ -85,7 +117,24 @@ def _ptrs(tensors, allowed, numels, index, what):
     return _host_array(c_void_p, "Q", map(_data_ptr, tensors))
 
 
-class _Plan:
+class _Planned:
+    """What plans over fixed tensors have in common: a handle, and memory of their own."""
+
+    def ran_on(self, stream):
+        """A call went to this stream, not the one of the call before.  Kernels read the tiles' rows from the
+        workspace, so what is the plan's own goes back to the allocator only after its work."""
+        self.last, index = stream.value, self.device.index
+        s = torch.cuda.ExternalStream(stream.value, index) if stream.value else torch.cuda.default_stream(index)
+        for t in self.memory:
+            t.record_stream(s)
+
+    def __del__(self):
+        if getattr(self, "handle", None):
+            self._destroy(self.handle)
+            self.handle = None
+
+
+class _Plan(_Planned):
     """A tula_train_plan over fixed tensors, with its workspace."""
 
     def __init__(self, grads, params=None, exp_avgs=None, exp_avg_sqs=None, copies=None):
@@ -129,19 +178,6 @@ class _Plan:
                                                  ctypes.byref(self.handle)), "tula_train_plan_create")
         self._destroy = _lib().tula_train_plan_destroy  # kept for __del__ at shutdown
         self.memory, self.last = [self.workspace], ()
-
-    def ran_on(self, stream):
-        """A call went to this stream, not the one of the call before.  Kernels read the tiles' rows from the
-        workspace, so what is the plan's own goes back to the allocator only after its work."""
-        self.last, index = stream.value, self.device.index
-        s = torch.cuda.ExternalStream(stream.value, index) if stream.value else torch.cuda.default_stream(index)
-        for t in self.memory:
-            t.record_stream(s)
-
-    def __del__(self):
-        if getattr(self, "handle", None):
-            self._destroy(self.handle)
-            self.handle = None
 
 
 class GradClipper:
@@ -215,3 +251,127 @@ class AdamWStep:
             plan.ran_on(s)
 
     __call__ = step
+
+
+class _MuonPlan(_Planned):
+    """A tula_muon_plan over fixed matrices, with its workspace."""
+
+    def __init__(self, params, grads, momenta, copies):
+        params = list(params)
+        if not params:
+            raise ValueError("no matrices")
+        self.device = dev = params[0].device
+        if dev.type != "cuda":
+            raise TypeError(f"CUDA tensors are wanted, got {dev}")
+        if any(t.dim() != 2 for t in params):
+            raise ValueError(f"matrices are wanted, got {next(tuple(t.shape) for t in params if t.dim() != 2)}")
+        numels, shapes = list(map(_numel, params)), [t.shape for t in params]
+        self._tensors, ptrs, types = [], [], []
+        for name, ts, allowed in (("grads", grads, set(TYPES)), ("params", params, {torch.float32}),
+                                  ("momenta", momenta, {torch.float32}),
+                                  ("copies", copies, {torch.bfloat16, torch.float16})):
+            if ts is None:
+                ptrs.append(None)
+                types.append(None)
+                continue
+            ts = list(ts)
+            if len(ts) != len(params):
+                raise ValueError(f"{len(ts)} {name} for {len(params)} matrices")
+            if [t.shape for t in ts] != shapes:
+                raise ValueError(f"{name}: other shapes than the matrices have")
+            self._tensors.append(ts)  # must outlive the plan
+            ptrs.append(_ptrs(ts, allowed, numels, dev.index, name))
+            types.append(_host_array(c_int, "i", [TYPES[t.dtype] for t in ts]))
+        rows, cols = (_host_array(ctypes.c_int64, "q", [t.shape[k] for t in params]) for k in (0, 1))
+
+        def at(a):
+            return ctypes.cast(a, c_void_p) if a is not None else None
+
+        desc = tula_muon_matrices(len(params), at(rows), at(cols), at(ptrs[0]), at(types[0]), at(ptrs[1]), at(ptrs[2]),
+                                  at(ptrs[3]), at(types[3]))
+        need = c_size_t(0)
+        _check(_lib().tula_muon_workspace_size(rows, cols, len(params), ctypes.byref(need)), "tula_muon_workspace_size")
+        self.workspace = torch.empty(need.value, dtype=torch.uint8, device=dev)
+        self.handle = c_void_p()
+        with torch.cuda.device(dev):
+            _check(_lib().tula_muon_plan_create(ctypes.byref(desc), c_void_p(self.workspace.data_ptr()),
+                                                self.workspace.numel(), _stream_ptr(None), ctypes.byref(self.handle)),
+                   "tula_muon_plan_create")
+        self._destroy = _lib().tula_muon_plan_destroy  # kept for __del__ at shutdown
+        self.memory, self.last = [self.workspace], ()
+
+
+class MuonStep:
+    """Muon on fp32 matrices and momenta, from gradients of any of the types; copies: bf16 or fp16
+    tensors that receive the weights.
+
+    momenta are zero-filled before the first step.  scale: what an update is multiplied by beside lr,
+    "rms" (0.2 sqrt(max(rows, cols)), updates as large as AdamW's) or "aspect" (sqrt(max(1, rows / cols))).
+    The tensors, gradients among them, are those it was made with, as in GradClipper."""
+
+    def __init__(self, params, grads, momenta, copies=None, *, nesterov=True, ns_steps=5, scale="rms"):
+        if scale not in MUON_SCALES:
+            raise ValueError(f"scale: one of {sorted(MUON_SCALES)} is wanted, got {scale!r}")
+        self._plan = _MuonPlan(params, grads, momenta, copies)
+        self.hp = tula_muon_hparams()
+        _lib().tula_muon_default_hparams(ctypes.byref(self.hp))
+        self.hp.nesterov, self.hp.ns_steps, self.hp.scale = 1 if nesterov else 0, ns_steps, MUON_SCALES[scale]
+        self._hp = ctypes.byref(self.hp)
+        torch.cuda.synchronize(self._plan.device)
+
+    def step(self, lr, momentum=0.95, weight_decay=0.0, grad_scale=1.0, record=None, stream=None) -> None:
+        """record: as GradClipper.norm leaves it (with this grad_scale), for clipping by the norm that it
+        was taken over and for leaving a step out whose norm is not finite."""
+        hp, plan = self.hp, self._plan
+        hp.lr, hp.momentum, hp.weight_decay, hp.grad_scale = lr, momentum, weight_decay, grad_scale
+        if record is None:
+            hp.record = None
+        else:
+            if (record.dtype != torch.float32 or record.numel() != TULA_RECORD_LEN or record.device != plan.device
+                    or not record.is_contiguous()):
+                raise TypeError(f"record: {TULA_RECORD_LEN} float32 on {plan.device} are wanted")
+            hp.record = record.data_ptr()
+        s = _stream_ptr(stream)
+        _check(_lib().tula_muon_step(plan.handle, self._hp, s), "tula_muon_step")
+        if s.value != plan.last:
+            plan.ran_on(s)
+
+    __call__ = step
+
+
+def orthogonalize(x: torch.Tensor, steps: int = 5, dtype=torch.bfloat16) -> torch.Tensor:
+    """The matrix x, or each matrix of a batch [..., rows, cols] (fp32, bf16 or fp16), with its singular
+    values brought near 1 by Muon's Newton-Schulz steps, as bf16 or fp16, on the current stream."""
+    if x.dim() < 2:
+        raise ValueError(f"orthogonalize: a matrix or a batch of them is wanted, got {tuple(x.shape)}")
+    if x.dtype not in TYPES or dtype not in (torch.bfloat16, torch.float16) or not x.is_cuda:
+        raise TypeError(f"orthogonalize: float32, bfloat16 or float16 on a GPU to bfloat16 or float16 is wanted, got {x.dtype} "
+                        f"on {x.device} to {dtype}")
+    x = x.detach()
+    rows, cols = x.shape[-2:]
+    out = torch.empty(x.shape, dtype=dtype, device=x.device)
+    if not out.numel():
+        return out
+    batch = out.numel() // (rows * cols)
+    if x.dim() != 3:
+        x = x.reshape(batch, rows, cols)
+    apart, stride, step = x.stride()
+    if step != 1 and cols > 1 or stride < cols and rows > 1 or apart < 0:
+        x = x.contiguous()
+        apart, stride, step = x.stride()
+    need = c_size_t(0)
+    _check(_lib().tula_orthogonalize_workspace_size(batch, rows, cols, ctypes.byref(need)), "tula_orthogonalize_workspace_size")
+    with torch.cuda.device(x.device):
+        space = torch.empty(need.value, dtype=torch.uint8, device=x.device)
+        _check(_lib().tula_orthogonalize(x.data_ptr(), TYPES[x.dtype], batch, rows, cols, max(stride, cols),
+                                         apart, steps, out.data_ptr(), TYPES[dtype], space.data_ptr(), need.value,
+                                         _stream_ptr(None)), "tula_orthogonalize")
+    return out
+
+
+def tula_muon_error(stream=None) -> int:
+    """Reads and clears the error word of Muon's products after the work on `stream` (synchronous): 0 =
+    every wait inside the kernels completed."""
+    out = c_int(0)
+    _check(_lib().tula_muon_error(_stream_ptr(stream), ctypes.byref(out)), "tula_muon_error")
+    return out.value
