@@ -7,15 +7,20 @@
 //
 // HBM bounds all of it: some ten operations an element of 2 or 4 bytes read and written once.  A group of
 // threads holds a row in registers, so that the mean, the variance about it and the output come from one
-// reading, and keeps its columns' weights, and in the backward pass their sums, in registers from row to row;
-// a row's loads are issued before the one ahead of it is worked on.
+// reading, and keeps its columns' weights, and in the backward pass their sums, in registers from row to row.
+// Rows on 16-byte boundaries come by bulk copies into a ring of shared memory, several rows ahead (with one row
+// ahead in registers instead, 16384 x 4096 bf16 took 254 us forward and backward); others into
+// registers, one row ahead.
 #include "tula_tc.cuh"
 
 namespace {
 
-constexpr int kMostThreads = 1024;
+constexpr int kMostThreads = 512;  // of a CTA, and of an SM
 constexpr int kMostCluster = 8;
-constexpr int kN = 8;  // elements that a thread holds of a row
+// Elements that a thread holds of a row.  What each row costs every warp (exchanges, of which an SM does one a
+// cycle, barriers, addresses) is spread over as many: with eight a thread 16384 x 4096 bf16 took 133 us forward.
+constexpr int kN = 16;
+constexpr int kMostStages = 8;
 
 struct NormArgs {
     const void *x, *dy, *w, *b;
@@ -25,6 +30,8 @@ struct NormArgs {
     long long rows, stride, dy_stride;
     int cols, group;          // threads to a row in a CTA, a power of two: all of it, or at most that
     int cluster;              // CTAs to a row
+    int share;                // columns of a CTA: all, or a multiple of 16 and none without any
+    int stages;               // of the ring
     float eps;
 };
 
@@ -32,8 +39,9 @@ __device__ __forceinline__ float value(float v) { return v; }
 __device__ __forceinline__ float value(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float value(__half v) { return __half2float(v); }
 
-// Part t of a row in `group` parts.  Vec: the row starts on a 16-byte boundary and has whole vectors of 16
-// bytes; the threads' vectors lie next to each other.  Else their elements do, and move one by one.
+// Part t of a row, or of a CTA's share of it, in `group` parts.  Vec: it starts on a 16-byte boundary and has
+// whole vectors of 16 bytes; the threads' vectors lie next to each other.  Else their elements do, and move
+// one by one.
 template <typename T, bool Vec>
 struct Part {
     static constexpr int kElems = 16 / (int)sizeof(T);
@@ -43,16 +51,23 @@ struct Part {
     }
     __device__ __forceinline__ void load(const T *row, int t, int group, int cols) {
 #pragma unroll
-        for (int k = 0; k < kN; k += Vec ? kElems : 1) {
+        for (int k = 0; k < kN; ++k) {
             const int c = column(k, t, group);
-            if (Vec) {
-                uint4 q = make_uint4(0, 0, 0, 0);
-                if (c < cols) q = __ldcs(reinterpret_cast<const uint4 *>(row + c));
-                memcpy(&v[k], &q, 16);
-            } else {
-                v[k] = T(0.f);
-                if (c < cols) v[k] = __ldcs(row + c);
-            }
+            v[k] = T(0.f);
+            if (c < cols) v[k] = __ldcs(row + c);
+        }
+    }
+    __device__ __forceinline__ void load_shared(uint32_t row, int t, int group, int cols) {
+#pragma unroll
+        for (int k = 0; k < kN; k += kElems) {
+            const int c = column(k, t, group);
+            uint4 q = make_uint4(0, 0, 0, 0);
+            if (c < cols)
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                             : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w)
+                             : "r"(row + c * (int)sizeof(T))
+                             : "memory");
+            memcpy(&v[k], &q, 16);
         }
     }
     __device__ __forceinline__ void store(T *row, int t, int group, int cols, const float (&f)[kN]) {
@@ -75,12 +90,12 @@ struct Part {
 
 // The columns' parameters; `none` where there are none.
 template <typename T, bool Vec, typename W>
-__device__ __forceinline__ void load_params(float (&f)[kN], const void *p, float none, int t, int group, int cols) {
+__device__ __forceinline__ void load_params(float (&f)[kN], const void *p, float none, int t, int group, int col0, int cols) {
 #pragma unroll
     for (int k = 0; k < kN; ++k) {
         const int c = Part<T, Vec>::column(k, t, group);
         f[k] = none;
-        if (p && c < cols) f[k] = value(static_cast<const W *>(p)[c]);
+        if (p && c < cols) f[k] = value(static_cast<const W *>(p)[col0 + c]);
     }
 }
 
@@ -89,175 +104,289 @@ __device__ __forceinline__ void load_params(float (&f)[kN], const void *p, float
 // a sum is enough (whoever writes a place again has passed the barrier of the sum between, which all reach
 // after they have read it).
 struct Sums {
-    float2 warps[2][32], ctas[2][kMostCluster];
+    float warps[2][2][kMostThreads / 32];
+    float2 ctas[2][kMostCluster];
 };
 struct GroupSum {
     Sums *place;
     int group, cluster, turn;
-    __device__ __forceinline__ float2 operator()(float a, float b) {
-        for (int o = min(group, 32) / 2; o; o >>= 1) {
-            a += __shfl_xor_sync(kFull, a, o);
-            b += __shfl_xor_sync(kFull, b, o);
-        }
-        if (group <= 32) return make_float2(a, b);
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = group >> 5;
-        float2 *at = place->warps[turn];
-        if (lane == 0) at[warp] = make_float2(a, b);
+    // N sums at a time: one or two.
+    template <int N>
+    __device__ __forceinline__ void operator()(float (&v)[N]) {
+        for (int o = min(group, 32) / 2; o; o >>= 1)
+#pragma unroll
+            for (int m = 0; m < N; ++m) v[m] += __shfl_xor_sync(kFull, v[m], o);
+        if (group <= 32) return;
+        const int warp = threadIdx.x >> 5, n = group >> 5;
+        if ((threadIdx.x & 31) == 0)
+#pragma unroll
+            for (int m = 0; m < N; ++m) place->warps[turn][m][warp] = v[m];
         __syncthreads();
-        const float2 v = lane < n ? at[(warp & ~(n - 1)) + lane] : make_float2(0.f, 0.f);
-        a = v.x, b = v.y;
-        for (int o = n / 2; o; o >>= 1) {
-            a += __shfl_xor_sync(kFull, a, o);
-            b += __shfl_xor_sync(kFull, b, o);
+#pragma unroll
+        for (int m = 0; m < N; ++m) {
+            const float *at = &place->warps[turn][m][warp & ~(n - 1)];  // the group's warps, by all of its threads
+            if (n == 2) {
+                v[m] = at[0] + at[1];
+            } else {
+                v[m] = 0.f;
+                for (int k = 0; k < n; k += 4) {
+                    const float4 q = *reinterpret_cast<const float4 *>(at + k);
+                    v[m] += (q.x + q.y) + (q.z + q.w);
+                }
+            }
         }
-        a = __shfl_sync(kFull, a, 0);  // (lanes from n on hold zeros)
-        b = __shfl_sync(kFull, b, 0);
         if (cluster > 1) {
             float2 *mine = place->ctas[turn];
             if (threadIdx.x < cluster)
                 asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(
                                  in_cta(smem_addr(mine + blockIdx.x % cluster), threadIdx.x)),
-                             "f"(a), "f"(b)
+                             "f"(v[0]), "f"(v[N - 1])
                              : "memory");
             cluster_sync();
-            a = b = 0.f;
+#pragma unroll
+            for (int m = 0; m < N; ++m) v[m] = 0.f;
             for (int k = 0; k < cluster; ++k) {
-                a += mine[k].x;
-                b += mine[k].y;
+                v[0] += mine[k].x;
+                if (N > 1) v[N - 1] += mine[k].y;
             }
         }
         turn ^= 1;
-        return make_float2(a, b);
+    }
+    __device__ __forceinline__ float operator()(float v) {
+        float one[1] = {v};
+        (*this)(one);
+        return one[0];
     }
 };
+
+// The ring: stage s holds the rows of one round of the CTA's groups, of each of N matrices.  A wait that runs
+// out leaves what is there: the others end at once then, and the error word says so.
+template <typename T, int N>
+struct Ring {
+    uint32_t at, bars;  // shared addresses
+    volatile int *dead;
+    int stages, per, bytes, pitch;  // rows to a round; bytes of a row here, and from row to row
+
+    __device__ __forceinline__ uint32_t row(int s, int m, int g) const { return at + ((s * N + m) * per + g) * pitch; }
+    // Of rows r0 to r0 + n; by one warp.
+    __device__ __forceinline__ void fetch(int s, const T *const (&from)[N], const long long (&stride)[N], int n) {
+        const int lane = threadIdx.x & 31;
+        const uint32_t bar = bars + 8 * s;
+        if (lane == 0) mbar_expect(bar, (unsigned)(N * n * bytes));
+        __syncwarp();
+#pragma unroll
+        for (int m = 0; m < N; ++m) {
+            if (stride[m] * (long long)sizeof(T) == bytes && pitch == bytes) {
+                if (lane == 0) bulk_load(row(s, m, 0), from[m], (unsigned)(n * bytes), bar);
+            } else {
+                for (int g = lane; g < n; g += 32) bulk_load(row(s, m, g), from[m] + g * stride[m], (unsigned)bytes, bar);
+            }
+        }
+    }
+    __device__ __forceinline__ void wait(int s, unsigned parity) { mbar_wait(bars + 8 * s, parity, dead); }
+};
+
+template <typename T, int N>
+__device__ __forceinline__ void start_ring(const Ring<T, N> &ring) {
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < ring.stages; ++s) mbar_init(ring.bars + 8 * s, 1);
+        *ring.dead = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+}
 
 template <typename T, typename W, bool Vec>
 __global__ void __launch_bounds__(kMostThreads) k_norm_forward(const NormArgs a) {
     using P = Part<T, Vec>;
-    __shared__ Sums place;
+    extern __shared__ __align__(128) unsigned char memory[];  // Vec: the ring
+    __shared__ __align__(16) Sums place;
+    __shared__ __align__(8) unsigned long long bars[kMostStages];
+    __shared__ volatile int dead;
+    const int per = blockDim.x / a.group, g = threadIdx.x / a.group, t = threadIdx.x & (a.group - 1);
+    const int col0 = blockIdx.x % a.cluster * a.share, cols = min(a.cols - col0, a.share);  // the CTA's share
+    const long long block = blockIdx.x / a.cluster, step = (long long)(gridDim.x / a.cluster) * per;
+    const int bytes = cols * (int)sizeof(T);
+    Ring<T, 1> ring{smem_addr(memory), smem_addr(bars), &dead, a.stages, per, bytes, bytes};
+    if (Vec) start_ring(ring);
     let_next_start();
     if (a.cluster > 1) cluster_sync();  // the other CTAs' shared memory may be written to from here on
     wait_for_previous();
-    const int cols = a.cols, per = blockDim.x / a.group;  // rows at a time
-    const int group = a.group * a.cluster, t = (threadIdx.x & (a.group - 1)) + blockIdx.x % a.cluster * a.group;
-    const long long block = blockIdx.x / a.cluster, step = (long long)(gridDim.x / a.cluster) * per;
     GroupSum sum{&place, a.group, a.cluster, 0};
-    float w[kN], b[kN];
-    load_params<T, Vec, W>(w, a.w, 1.f, t, group, cols);
-    load_params<T, Vec, W>(b, a.b, 0.f, t, group, cols);
-    const float inv = 1.f / (float)cols;
-    long long r = block * per + threadIdx.x / a.group;
-    const T *x = static_cast<const T *>(a.x);
+    const float inv = 1.f / (float)a.cols;
+    const T *const x[1] = {static_cast<const T *>(a.x) + col0};
+    const long long stride[1] = {a.stride};
+    const long long first = block * per;
     P now, next;
-    if (r < a.rows) now.load(x + r * a.stride, t, group, cols);
+    if (Vec) {
+        if (threadIdx.x < 32) {
+            long long r0 = first;
+            for (int s = 0; s < a.stages && r0 < a.rows; ++s, r0 += step) {
+                const T *const from[1] = {x[0] + r0 * a.stride};
+                ring.fetch(s, from, stride, (int)min((long long)per, a.rows - r0));
+            }
+        }
+    } else if (first + g < a.rows) {
+        now.load(x[0] + (first + g) * a.stride, t, a.group, cols);
+    }
+    float w[kN], b[kN];
+    load_params<T, Vec, W>(w, a.w, 1.f, t, a.group, col0, cols);
+    load_params<T, Vec, W>(b, a.b, 0.f, t, a.group, col0, cols);
+    int s = 0;
+    unsigned parity = 0;
     // (all threads of a CTA go round as often: groups beyond the last row take part in the exchanges)
-    for (long long r0 = block * per; r0 < a.rows; r0 += step, r += step) {
+    for (long long r0 = first; r0 < a.rows; r0 += step) {
+        const long long r = r0 + g;
         const bool there = r < a.rows;
-        if (r + step < a.rows) next.load(x + (r + step) * a.stride, t, group, cols);
-        float c[kN], s = 0.f;
+        if (Vec) {
+            ring.wait(s, parity);
+            if (there) now.load_shared(ring.row(s, 0, g), t, a.group, cols);
+        } else if (r + step < a.rows) {
+            next.load(x[0] + (r + step) * a.stride, t, a.group, cols);
+        }
+        float c[kN], total = 0.f;
 #pragma unroll
         for (int k = 0; k < kN; ++k) {
             c[k] = there ? value(now.v[k]) : 0.f;
-            s += c[k];
+            total += c[k];
         }
-        const float mean = sum(s, 0.f).x * inv;
-        s = 0.f;
+        const float mean = sum(total) * inv;
+        if (Vec) {
+            if (a.group <= 32) __syncthreads();
+            if (threadIdx.x < 32 && r0 + a.stages * step < a.rows) {  // all have read the stage
+                const T *const from[1] = {x[0] + (r0 + a.stages * step) * a.stride};
+                ring.fetch(s, from, stride, (int)min((long long)per, a.rows - r0 - a.stages * step));
+            }
+            if (++s == a.stages) s = 0, parity ^= 1;
+        }
+        total = 0.f;
 #pragma unroll
         for (int k = 0; k < kN; ++k) {
-            c[k] = P::column(k, t, group) < cols ? c[k] - mean : 0.f;
-            s = fmaf(c[k], c[k], s);
+            c[k] = P::column(k, t, a.group) < cols ? c[k] - mean : 0.f;
+            total = fmaf(c[k], c[k], total);
         }
-        const float var = sum(s, 0.f).x * inv;
-        const float rstd = 1.f / sqrtf(var + a.eps);
+        const float rstd = rsqrtf(sum(total) * inv + a.eps);
         if (there) {
 #pragma unroll
             for (int k = 0; k < kN; ++k) c[k] = fmaf(c[k] * rstd, w[k], b[k]);
-            now.store(static_cast<T *>(a.y) + r * cols, t, group, cols, c);
-            if (a.stats && t == 0) reinterpret_cast<float2 *>(a.stats)[r] = make_float2(mean, rstd);
+            now.store(static_cast<T *>(a.y) + r * a.cols + col0, t, a.group, cols, c);
+            if (a.stats && t == 0 && col0 == 0) reinterpret_cast<float2 *>(a.stats)[r] = make_float2(mean, rstd);
         }
-        now = next;
+        if (!Vec) now = next;
     }
 }
 
 template <typename T, typename W, bool Vec, bool Params>
 __global__ void __launch_bounds__(kMostThreads) k_norm_backward(const NormArgs a) {
     using P = Part<T, Vec>;
-    __shared__ Sums place;
-    extern __shared__ float sums[];  // Params: [2][kN * threads], groups of less than the CTA
+    extern __shared__ __align__(128) unsigned char memory[];  // Vec: the ring; Params: then the groups' sums
+    __shared__ __align__(16) Sums place;
+    __shared__ __align__(8) unsigned long long bars[kMostStages];
+    __shared__ volatile int dead;
+    const int per = blockDim.x / a.group, g = threadIdx.x / a.group, t = threadIdx.x & (a.group - 1);
+    const int col0 = blockIdx.x % a.cluster * a.share, cols = min(a.cols - col0, a.share);  // the CTA's share
+    const long long block = blockIdx.x / a.cluster, step = (long long)(gridDim.x / a.cluster) * per;
+    const int bytes = cols * (int)sizeof(T);
+    Ring<T, 2> ring{smem_addr(memory), smem_addr(bars), &dead, a.stages, per, bytes, bytes};
+    if (Vec) start_ring(ring);
     let_next_start();
     if (a.cluster > 1) cluster_sync();
     wait_for_previous();
-    const int cols = a.cols, per = blockDim.x / a.group;
-    const int group = a.group * a.cluster, t = (threadIdx.x & (a.group - 1)) + blockIdx.x % a.cluster * a.group;
-    const long long block = blockIdx.x / a.cluster, step = (long long)(gridDim.x / a.cluster) * per;
     GroupSum sum{&place, a.group, a.cluster, 0};
-    float w[kN], dw[kN], db[kN];
-    load_params<T, Vec, W>(w, a.w, 1.f, t, group, cols);
-#pragma unroll
-    for (int k = 0; k < kN; ++k) dw[k] = db[k] = 0.f;
-    const float inv = 1.f / (float)cols;
-    long long r = block * per + threadIdx.x / a.group;
-    const T *x = static_cast<const T *>(a.x), *dy = static_cast<const T *>(a.dy);
+    const float inv = 1.f / (float)a.cols;
+    const T *const x = static_cast<const T *>(a.x) + col0, *const dy = static_cast<const T *>(a.dy) + col0;
+    const long long stride[2] = {a.stride, a.dy_stride};
     const float2 *stats = reinterpret_cast<const float2 *>(a.stats);
+    const long long first = block * per;
     P now_x, now_d, next_x, next_d;
     float2 now_s = make_float2(0.f, 0.f), next_s = now_s;
-    if (r < a.rows) {
-        now_x.load(x + r * a.stride, t, group, cols);
-        now_d.load(dy + r * a.dy_stride, t, group, cols);
-        now_s = __ldcs(stats + r);
+    if (Vec) {
+        if (threadIdx.x < 32) {
+            long long r0 = first;
+            for (int s = 0; s < a.stages && r0 < a.rows; ++s, r0 += step) {
+                const T *const from[2] = {x + r0 * a.stride, dy + r0 * a.dy_stride};
+                ring.fetch(s, from, stride, (int)min((long long)per, a.rows - r0));
+            }
+        }
+    } else if (first + g < a.rows) {
+        now_x.load(x + (first + g) * a.stride, t, a.group, cols);
+        now_d.load(dy + (first + g) * a.dy_stride, t, a.group, cols);
     }
-    for (long long r0 = block * per; r0 < a.rows; r0 += step, r += step) {
+    if (first + g < a.rows) now_s = __ldcs(stats + first + g);
+    float w[kN], dw[kN], db[kN];
+    load_params<T, Vec, W>(w, a.w, 1.f, t, a.group, col0, cols);
+#pragma unroll
+    for (int k = 0; k < kN; ++k) dw[k] = db[k] = 0.f;
+    int s = 0;
+    unsigned parity = 0;
+    for (long long r0 = first; r0 < a.rows; r0 += step) {
+        const long long r = r0 + g;
         const bool there = r < a.rows;
         if (r + step < a.rows) {
-            next_x.load(x + (r + step) * a.stride, t, group, cols);
-            next_d.load(dy + (r + step) * a.dy_stride, t, group, cols);
             next_s = __ldcs(stats + r + step);
-        }
-        float s1 = 0.f, s2 = 0.f;
-        if (there) {
-#pragma unroll
-            for (int k = 0; k < kN; ++k) {
-                const bool in = P::column(k, t, group) < cols;
-                const float n = in ? (value(now_x.v[k]) - now_s.x) * now_s.y : 0.f, d = value(now_d.v[k]);
-                const float g = d * w[k];
-                s1 += g;
-                s2 = fmaf(g, n, s2);
-                if (Params) {
-                    dw[k] = fmaf(d, n, dw[k]);
-                    db[k] += d;
-                }
+            if (!Vec) {
+                next_x.load(x + (r + step) * a.stride, t, a.group, cols);
+                next_d.load(dy + (r + step) * a.dy_stride, t, a.group, cols);
             }
         }
-        if (a.y) {
-            const float2 s = sum(s1, s2);
+        if (Vec) {
+            ring.wait(s, parity);
             if (there) {
-                float f[kN];
-#pragma unroll
-                for (int k = 0; k < kN; ++k) {
-                    const float n = (value(now_x.v[k]) - now_s.x) * now_s.y, g = value(now_d.v[k]) * w[k];
-                    f[k] = now_s.y * (g - fmaf(n, s.y, s.x) * inv);
-                }
-                now_x.store(static_cast<T *>(a.y) + r * cols, t, group, cols, f);
+                now_x.load_shared(ring.row(s, 0, g), t, a.group, cols);
+                now_d.load_shared(ring.row(s, 1, g), t, a.group, cols);
             }
         }
-        now_x = next_x, now_d = next_d, now_s = next_s;
+        float n[kN], d[kN], s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int k = 0; k < kN; ++k) {
+            const bool in = there && P::column(k, t, a.group) < cols;
+            n[k] = in ? (value(now_x.v[k]) - now_s.x) * now_s.y : 0.f;
+            d[k] = in ? value(now_d.v[k]) : 0.f;
+            if (Params) {
+                dw[k] = fmaf(d[k], n[k], dw[k]);
+                db[k] += d[k];
+            }
+            d[k] *= w[k];
+            s1 += d[k];
+            s2 = fmaf(d[k], n[k], s2);
+        }
+        float sums[2] = {s1, s2};
+        if (a.y) sum(sums);
+        if (Vec) {
+            if (!a.y || a.group <= 32) __syncthreads();
+            if (threadIdx.x < 32 && r0 + a.stages * step < a.rows) {  // all have read the stage
+                const T *const from[2] = {x + (r0 + a.stages * step) * a.stride, dy + (r0 + a.stages * step) * a.dy_stride};
+                ring.fetch(s, from, stride, (int)min((long long)per, a.rows - r0 - a.stages * step));
+            }
+            if (++s == a.stages) s = 0, parity ^= 1;
+        }
+        if (a.y && there) {
+            const float m1 = sums[0] * inv, m2 = sums[1] * inv;
+#pragma unroll
+            for (int k = 0; k < kN; ++k) d[k] = now_s.y * (d[k] - fmaf(n[k], m2, m1));
+            now_x.store(static_cast<T *>(a.y) + r * a.cols + col0, t, a.group, cols, d);
+        }
+        if (!Vec) now_x = next_x, now_d = next_d;
+        now_s = next_s;
     }
     if (!Params) return;
-    float *to = a.parts + (size_t)block * 2 * cols;
+    float *to = a.parts + (size_t)block * 2 * a.cols + col0;
+    const int group = a.group;
     if (per == 1) {
 #pragma unroll
         for (int k = 0; k < kN; ++k) {
             const int c = P::column(k, t, group);
-            if (c < cols) to[c] = dw[k], to[cols + c] = db[k];
+            if (c < cols) to[c] = dw[k], to[a.cols + c] = db[k];
         }
         return;
     }
     // the groups' sums, in their order
-    const int g0 = threadIdx.x / group;
+    float *sums = reinterpret_cast<float *>(memory);
+    __syncthreads();  // the ring has been read
 #pragma unroll
     for (int k = 0; k < kN; ++k) {
-        sums[(g0 * kN + k) * group + t] = dw[k];
-        sums[((per + g0) * kN + k) * group + t] = db[k];
+        sums[(g * kN + k) * group + t] = dw[k];
+        sums[((per + g) * kN + k) * group + t] = db[k];
     }
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * kN * group; i += blockDim.x) {
@@ -265,15 +394,15 @@ __global__ void __launch_bounds__(kMostThreads) k_norm_backward(const NormArgs a
         const int c = P::column(j / group, j & (group - 1), group);
         if (c >= cols) continue;
         float v = 0.f;
-        for (int g = 0; g < per; ++g) v += sums[(which * per + g) * kN * group + j];
-        to[which * cols + c] = v;
+        for (int q = 0; q < per; ++q) v += sums[(which * per + q) * kN * group + j];
+        to[which * a.cols + c] = v;
     }
 }
 
 // Rows that registers do not hold: a CTA to a row, which is read three times, or twice, mostly from L2.
 template <typename T, typename W>
 __global__ void __launch_bounds__(kMostThreads) k_norm_forward_wide(const NormArgs a) {
-    __shared__ Sums place;
+    __shared__ __align__(16) Sums place;
     let_next_start();
     wait_for_previous();
     GroupSum sum{&place, (int)blockDim.x, 1, 0};
@@ -282,13 +411,13 @@ __global__ void __launch_bounds__(kMostThreads) k_norm_forward_wide(const NormAr
         const T *x = static_cast<const T *>(a.x) + r * a.stride;
         float s = 0.f;
         for (int c = threadIdx.x; c < cols; c += blockDim.x) s += value(x[c]);
-        const float mean = sum(s, 0.f).x / (float)cols;
+        const float mean = sum(s) / (float)cols;
         s = 0.f;
         for (int c = threadIdx.x; c < cols; c += blockDim.x) {
             const float d = value(x[c]) - mean;
             s = fmaf(d, d, s);
         }
-        const float rstd = 1.f / sqrtf(sum(s, 0.f).x / (float)cols + a.eps);
+        const float rstd = rsqrtf(sum(s) / (float)cols + a.eps);
         T *y = static_cast<T *>(a.y) + r * cols;
         for (int c = threadIdx.x; c < cols; c += blockDim.x) {
             const float w = a.w ? value(static_cast<const W *>(a.w)[c]) : 1.f, b = a.b ? value(static_cast<const W *>(a.b)[c]) : 0.f;
@@ -299,7 +428,7 @@ __global__ void __launch_bounds__(kMostThreads) k_norm_forward_wide(const NormAr
 }
 template <typename T, typename W>
 __global__ void __launch_bounds__(kMostThreads) k_norm_backward_wide(const NormArgs a) {
-    __shared__ Sums place;
+    __shared__ __align__(16) Sums place;
     let_next_start();
     wait_for_previous();
     GroupSum sum{&place, (int)blockDim.x, 1, 0};
@@ -313,11 +442,12 @@ __global__ void __launch_bounds__(kMostThreads) k_norm_backward_wide(const NormA
             s1 += g;
             s2 = fmaf(g, (value(x[c]) - st.x) * st.y, s2);
         }
-        const float2 s = sum(s1, s2);
+        float s[2] = {s1, s2};
+        sum(s);
         T *dx = static_cast<T *>(a.y) + r * cols;
         for (int c = threadIdx.x; c < cols; c += blockDim.x) {
             const float g = value(dy[c]) * (a.w ? value(static_cast<const W *>(a.w)[c]) : 1.f);
-            put(dx + c, st.y * (g - fmaf((value(x[c]) - st.x) * st.y, s.y, s.x) / (float)cols));
+            put(dx + c, st.y * (g - fmaf((value(x[c]) - st.x) * st.y, s[1], s[0]) / (float)cols));
         }
     }
 }
@@ -341,23 +471,26 @@ __global__ void __launch_bounds__(256) k_norm_sums_wide(const NormArgs a) {
     to[a.cols + c] = db;
 }
 
-// The parts' sums in their order, eight threads to a column, in turn and then together.
+// The parts' sums, 32 threads to a column: each those of every 32nd, then together in their order.
 template <typename W>
-__global__ void __launch_bounds__(256) k_norm_params(const float *parts, int n, int cols, W *dw, W *db) {
-    __shared__ float sums[8][33];
+__global__ void __launch_bounds__(1024) k_norm_params(const float *parts, int n, int cols, W *dw, W *db) {
+    __shared__ float sums[32][33];
     let_next_start();
     wait_for_previous();
     const int lane = threadIdx.x & 31, turn = threadIdx.x >> 5;
     const long long c = (long long)blockIdx.x * 32 + lane;  // of both gradients
     float v = 0.f;
     if (c < 2ll * cols)
-        for (int i = turn; i < n; i += 8) v += parts[(size_t)i * 2 * cols + c];
+#pragma unroll 4
+        for (int i = turn; i < n; i += 32) v += __ldcg(parts + (size_t)i * 2 * cols + c);
     sums[turn][lane] = v;
     __syncthreads();
-    if (turn || c >= 2ll * cols) return;
-    for (int k = 1; k < 8; ++k) v += sums[k][lane];
-    W *to = c < cols ? dw : db;
-    if (to) put(to + (c < cols ? c : c - cols), v);
+    v = sums[lane][turn];  // part `lane` of column `turn`
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
+    const long long at = (long long)blockIdx.x * 32 + turn;
+    if (lane || at >= 2ll * cols) return;
+    W *to = at < cols ? dw : db;
+    if (to) put(to + (at < cols ? at : at - cols), v);
 }
 
 // ----------------------------------------------------------------------------
@@ -366,21 +499,20 @@ __global__ void __launch_bounds__(256) k_norm_params(const float *parts, int n, 
 
 // How rows of so many columns are shared out: the threads of a CTA to a row, the CTAs to one.
 struct Layout {
-    int group, threads, cluster;  // cluster 0: rows that registers do not hold
+    int group, threads, cluster, share;  // cluster 0: rows that registers do not hold
     unsigned grid;
     unsigned blocks() const { return grid / (unsigned)std::max(1, cluster); }
 };
 Layout layout_of(long long rows, int cols, int sms) {
     Layout l;
-    const long long parts = up(cols, kN);
+    const long long ctas = up(cols, kMostThreads * kN);
+    l.cluster = ctas <= kMostCluster ? (int)ctas : 0;
+    l.share = ctas == 1 ? cols : (int)up(up(cols, ctas), kN) * kN;
     l.group = 1;
-    while (l.group < kMostThreads && l.group < parts) l.group *= 2;
-    l.cluster = 1;
-    while (l.cluster <= kMostCluster && (long long)l.cluster * l.group < parts) l.cluster *= 2;
+    while (l.group < kMostThreads && l.group * kN < l.share) l.group *= 2;
     l.threads = std::max(l.group, 256);
-    if (l.cluster > kMostCluster) {
-        l.cluster = 0;
-        l.grid = (unsigned)std::min<long long>(rows, 2ll * sms);
+    if (!l.cluster) {
+        l.grid = (unsigned)std::min<long long>(rows, 4ll * sms);
         return l;
     }
     const long long per = l.threads / l.group, blocks = std::max(1, sms * (kMostThreads / l.threads) / l.cluster);
@@ -393,6 +525,14 @@ unsigned parts_of(const Layout &l, long long rows) {
     return l.cluster ? l.blocks() : (unsigned)std::min<long long>(kWideParts, up(rows, 64));
 }
 
+// The ring's memory: 384 bytes a thread, so that all threads of an SM take 192 KB.
+constexpr int kRingThread = 384, kRingMost = kRingThread * kMostThreads;
+inline int ring_bytes(const Layout &l, size_t size, int matrices, int &stages) {
+    const int stage = l.threads * kN * (int)size * matrices;
+    stages = std::min(kMostStages, kRingThread * l.threads / stage);
+    return stages * stage;
+}
+
 inline bool lies(const void *p, long long stride, size_t size) {  // rows on 16-byte boundaries
     return (reinterpret_cast<uintptr_t>(p) | (size_t)stride * size) % 16 == 0;
 }
@@ -403,9 +543,13 @@ int forward_typed(NormArgs &a, cudaStream_t s) {
     if (!l.cluster) return tula::launch(k_norm_forward_wide<T, W>, dim3(l.grid), l.threads, 0, s, 1, a);
     a.group = l.group;
     a.cluster = l.cluster;
+    a.share = l.share;
     const bool vec = a.cols % (16 / (int)sizeof(T)) == 0 && lies(a.x, a.stride, sizeof(T)) && lies(a.y, a.cols, sizeof(T));
     void (*k)(const NormArgs) = vec ? k_norm_forward<T, W, true> : k_norm_forward<T, W, false>;
-    return tula::launch(k, dim3(l.grid), l.threads, 0, s, l.cluster, a);
+    static std::atomic<uint64_t> done;
+    const int smem = vec ? ring_bytes(l, sizeof(T), 1, a.stages) : 0;
+    const int rc = vec ? allow_smem((const void *)k, kRingMost, &done) : TULA_OK;
+    return rc ? rc : tula::launch(k, dim3(l.grid), l.threads, smem, s, l.cluster, a);
 }
 template <typename T, typename W>
 int backward_typed(NormArgs &a, void *dw, void *db, cudaStream_t s) {
@@ -414,19 +558,23 @@ int backward_typed(NormArgs &a, void *dw, void *db, cudaStream_t s) {
     if (l.cluster) {
         a.group = l.group;
         a.cluster = l.cluster;
+        a.share = l.share;
         const bool vec = a.cols % (16 / (int)sizeof(T)) == 0 && lies(a.x, a.stride, sizeof(T)) && lies(a.dy, a.dy_stride, sizeof(T)) &&
                          (!a.y || lies(a.y, a.cols, sizeof(T)));
         void (*k)(const NormArgs) = a.parts ? (vec ? k_norm_backward<T, W, true, true> : k_norm_backward<T, W, false, true>)
                                             : (vec ? k_norm_backward<T, W, true, false> : k_norm_backward<T, W, false, false>);
-        const int smem = a.parts && l.threads > l.group ? 2 * l.threads * kN * 4 : 0;  // 16 KB
-        rc = tula::launch(k, dim3(l.grid), l.threads, smem, s, l.cluster, a);
+        static std::atomic<uint64_t> done[2];
+        int smem = vec ? ring_bytes(l, sizeof(T), 2, a.stages) : 0;
+        if (a.parts && l.threads > l.group) smem = std::max(smem, 2 * l.threads * kN * 4);  // 32 KB
+        if (vec) rc = allow_smem((const void *)k, kRingMost, &done[a.parts != nullptr]);
+        if (!rc) rc = tula::launch(k, dim3(l.grid), l.threads, smem, s, l.cluster, a);
     } else {
         if (a.y) rc = tula::launch(k_norm_backward_wide<T, W>, dim3(l.grid), l.threads, 0, s, 1, a);
         if (!rc && a.parts)
             rc = tula::launch(k_norm_sums_wide<T>, dim3((unsigned)up(a.cols, 256), parts_of(l, a.rows)), 256, 0, s, 1, a);
     }
     if (rc || !a.parts) return rc;
-    return tula::launch(k_norm_params<W>, dim3((unsigned)up(2ll * a.cols, 32)), 256, 0, s, 1, (const float *)a.parts,
+    return tula::launch(k_norm_params<W>, dim3((unsigned)up(2ll * a.cols, 32)), 1024, 0, s, 1, (const float *)a.parts,
                         (int)parts_of(l, a.rows), a.cols, static_cast<W *>(dw), static_cast<W *>(db));
 }
 
@@ -473,8 +621,8 @@ int tula_layer_norm(const void *x, int type, int64_t rows, int64_t cols, int64_t
 
 int tula_layer_norm_workspace_size(int64_t rows, int64_t cols, size_t *bytes) {
     if (!bytes || !good_sizes(rows, cols)) return TULA_ERR_ARG;
-    // as many parts as a GPU of up to 256 SMs has CTAs (of 256 threads, four an SM)
-    const long long parts = std::min<long long>(std::max<long long>(rows, 1), 4 * 256);
+    // as many parts as a GPU of up to 256 SMs has CTAs (of 256 threads, two an SM)
+    const long long parts = std::min<long long>(std::max<long long>(rows, 1), 2 * 256);
     *bytes = (size_t)parts * 2 * (size_t)cols * 4;
     return TULA_OK;
 }
