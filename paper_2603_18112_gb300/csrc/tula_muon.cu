@@ -71,20 +71,24 @@ static_assert(sizeof(ProductArgs) <= 4096 - 3 * 128 - 64, "kernel parameters");
 // taken, and stored twice); the polynomial, symmetric too; alpha times them.
 enum Kind { kGram, kPoly, kApply };
 
+// A copying warp, an issuing warp, and those that read back: two to each quarter of tensor memory's lanes, each
+// with half of the columns.  (With one to a quarter the sums of 1024 columns were read back more slowly than
+// they were made: 72 matrices, three products of n = 1024 each, took 2.19 ms instead of PRODMS.)
+constexpr int kReaders = 8;
+constexpr int kThreads = 64 + 32 * kReaders;
+
 template <bool Pair>
 struct Shape {
     static constexpr int kSide = Pair ? 256 : 128;  // of a block of the output
-    static constexpr int kStages = 6;
+    static constexpr int kStages = 5;
     static constexpr int kOperand = 128 * 128;      // bytes of a stage, a CTA
     static constexpr int kStage = 2 * kOperand;
-    static constexpr int kOuts = 4 * 2 * 4096;      // two buffers a warp
+    static constexpr int kOuts = kReaders * 2 * 4096;  // two buffers a warp
     static constexpr int kBars = 2 * kStages + 4;
     static constexpr int kSmem = kStages * kStage + kOuts + 8 * kBars + 16 + 1024;
     static constexpr int kCols = 2 * kSide;         // two accumulators
     static_assert(kSmem <= 227 * 1024, "shared memory");
 };
-constexpr int kThreads = 192;  // a copying warp, an issuing warp, four that read back
-
 // Shared-memory matrix descriptors of an operand (bit 46: their version; the 128-byte swizzle).  Along: rows of
 // 64 elements of the sum, groups of eight 1024 bytes apart.  Else: rows of 64 of the side, one for each element
 // of the sum, groups of eight 1024 bytes apart, the next 64 of the side 8192 bytes on.
@@ -132,11 +136,32 @@ __device__ __forceinline__ Block block_at(const ProductArgs &a, int t, const Pro
     return b;
 }
 
-// Rows of the workspace of half h of an operand's stage.
-__device__ __forceinline__ int stage_row(const Side &s, int matrix, int i, int k, int h, int none) {
-    if (s.along) return i < s.rows ? (s.base + matrix * s.step + i * s.pitch + k) * kTile + 64 * h : none;
-    return 2 * i + h < s.pitch ? (s.base + matrix * s.step + (k >> 1) * s.pitch + 2 * i + h) * kTile + 64 * (k & 1) : none;
-}
+// Rows of the workspace that an operand's stages start at, in registers: the loops are full of statements that
+// the compiler may not move loads across, and with the group's fields read again for each stage the copying
+// warp took some 800 cycles to one.
+struct Walk {
+    unsigned row0, row1;  // of the two halves of stage 0; none where there are none
+    unsigned odd, even;   // rows from an even stage to the odd one after it, and from there to the next
+    __device__ __forceinline__ Walk(const Side &s, int matrix, int i, unsigned none) {
+        const int first = s.base + matrix * s.step;
+        if (s.along) {
+            row0 = i < s.rows ? (first + i * s.pitch) * kTile : none;
+            row1 = row0 == none ? none : row0 + 64;
+            odd = even = kTile;
+        } else {
+            row0 = 2 * i < s.pitch ? (first + 2 * i) * kTile : none;
+            row1 = 2 * i + 1 < s.pitch ? (first + 2 * i + 1) * kTile : none;
+            odd = 64;
+            even = s.pitch * kTile - 64;
+        }
+        // (none and what comes after it lie beyond the workspace, also as negative coordinates)
+    }
+    __device__ __forceinline__ void next(int k) {
+        const unsigned by = k & 1 ? even : odd;
+        row0 += by;
+        row1 += by;
+    }
+};
 
 template <bool Pair, Kind K>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -160,7 +185,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(acc_full + 8 * s, 1);
-            mbar_init(acc_free + 8 * s, Pair ? 8 : 4);  // the reading warps, of both CTAs
+            mbar_init(acc_free + 8 * s, (Pair ? 2 : 1) * kReaders);  // the reading warps, of both CTAs
         }
         dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -190,27 +215,30 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int t = worker; ok && t < n_blocks; t += workers) {
             const ProductGroup *g;
             const Block b = block_at<K>(a, t, g);
-            const int im = Pair ? 2 * b.m + rank : b.m, in = Pair ? 2 * b.n + rank : b.n;
-            for (int k = 0; k < g->n_k; ++k, ++i) {
+            const int n_k = g->n_k;
+            Walk p(g->p, b.matrix, Pair ? 2 * b.m + rank : b.m, a.none), q(g->q, b.matrix, Pair ? 2 * b.n + rank : b.n, a.none);
+            for (int k = 0; k < n_k; ++k, ++i) {
                 const int s = i % S::kStages;
                 if (i >= S::kStages) ok = __all_sync(kFull, mbar_wait(empty + 8 * s, (i / S::kStages - 1) & 1, &dead));
                 if (!ok) break;
                 const uint32_t at = stages + s * S::kStage, bar = Pair ? in_cta(full + 8 * s, 0) : full + 8 * s;
                 if (elect_one()) {
                     if (rank == 0) mbar_expect(full + 8 * s, (Pair ? 2 : 1) * S::kStage);  // both CTAs' copies
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int yp = stage_row(g->p, b.matrix, im, k, h, a.none), yq = stage_row(g->q, b.matrix, in, k, h, a.none);
-                        if (Pair) {
-                            tma_load_pair(at + 8192 * h, &map_in, 0, yp, bar);
-                            tma_load_pair(at + S::kOperand + 8192 * h, &map_in, 0, yq, bar);
-                        } else {
-                            tma_load_2d(at + 8192 * h, &map_in, 0, yp, bar);
-                            tma_load_2d(at + S::kOperand + 8192 * h, &map_in, 0, yq, bar);
-                        }
+                    if (Pair) {
+                        tma_load_pair(at, &map_in, 0, (int)p.row0, bar);
+                        tma_load_pair(at + 8192, &map_in, 0, (int)p.row1, bar);
+                        tma_load_pair(at + S::kOperand, &map_in, 0, (int)q.row0, bar);
+                        tma_load_pair(at + S::kOperand + 8192, &map_in, 0, (int)q.row1, bar);
+                    } else {
+                        tma_load_2d(at, &map_in, 0, (int)p.row0, bar);
+                        tma_load_2d(at + 8192, &map_in, 0, (int)p.row1, bar);
+                        tma_load_2d(at + S::kOperand, &map_in, 0, (int)q.row0, bar);
+                        tma_load_2d(at + S::kOperand + 8192, &map_in, 0, (int)q.row1, bar);
                     }
                 }
                 __syncwarp();
+                p.next(k);
+                q.next(k);
             }
         }
         // The issuing warp's arrivals (of the other CTA too) have all landed before the CTA ends.
@@ -229,13 +257,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const ProductGroup *g;
                 block_at<K>(a, t, g);
                 const bool pa = g->p.along, qa = g->q.along;
+                const int n_k = g->n_k;
                 const uint32_t idesc = product_desc(S::kSide, S::kSide, pa, qa);
                 // from one instruction's 16 of the sum to the next: 32 bytes of a row, or 16 rows
                 const uint32_t p_next = pa ? 2 : 128, q_next = qa ? 2 : 128;
                 if (n > 1) ok = __all_sync(kFull, mbar_wait(acc_free + 8 * (n & 1), (n / 2 - 1) & 1, &dead));
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t acc = tmem + (n & 1) * S::kSide;
-                for (int k = 0; ok && k < g->n_k; ++k, ++i) {
+                for (int k = 0; ok && k < n_k; ++k, ++i) {
                     const int s = i % S::kStages;
                     ok = __all_sync(kFull, mbar_wait(full + 8 * s, (i / S::kStages) & 1, &dead));
                     if (!ok) break;
@@ -247,10 +276,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                         for (int j = 0; j < 4; ++j) mma16<Pair>(acc, dp + j * p_next, dq + j * q_next, idesc, k > 0 || j > 0);
                         if (Pair) {
                             commit_pair(empty + 8 * s);
-                            if (k == g->n_k - 1) commit_pair(acc_full + 8 * (n & 1));
+                            if (k == n_k - 1) commit_pair(acc_full + 8 * (n & 1));
                         } else {
                             commit(empty + 8 * s);
-                            if (k == g->n_k - 1) commit(acc_full + 8 * (n & 1));
+                            if (k == n_k - 1) commit(acc_full + 8 * (n & 1));
                         }
                     }
                     __syncwarp();
@@ -259,41 +288,51 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         __syncwarp();
     } else {
-        const int quad = warp & 3, row = quad * 32 + lane;
-        const uint32_t buffer = outs + quad * 8192, mirror = buffer + 4096;
+        const int quad = warp & 3, row = quad * 32 + lane, half = (warp - 2) >> 2;
+        constexpr int kChunks = S::kSide / kTileCols / 2;  // of 64 columns, a warp
+        const uint32_t buffers = outs + (warp - 2) * 8192;
+        uint32_t other = 0;  // kApply: the two buffers in turn; else one is for the block's mirror
         int n = 0;
         for (int t = worker; t < n_blocks; t += workers, ++n) {
             const ProductGroup *g;
             const Block b = block_at<K>(a, t, g);
             const int im = Pair ? 2 * b.m + rank : b.m;
+            const int out = g->out + b.matrix * g->out_step;
+            const int j0 = b.n * (S::kSide / kTileCols) + half * kChunks;  // column of tiles
+            const int out_pitch = g->out_pitch;
+            const int chunks = im < g->out_rows ? max(0, min(kChunks, out_pitch - j0)) : 0;  // within the output
+            const bool twice = K != kApply && b.m != b.n;
+            const float alpha = g->alpha;
+            const int diagonal = K == kPoly && row + im * kTile < g->n ? row + im * kTile : -1;
+            const unsigned char *const added =  // kPoly: A's rows
+                a.tiles + (size_t)(g->p.base + b.matrix * g->p.step + im * g->p.pitch + j0) * kTileBytes + row * 128;
+            unsigned add[32];
+            auto fetch = [&](int c) {
+                const unsigned char *from = added + (size_t)c * kTileBytes;
+#pragma unroll
+                for (int k = 0; k < 32; k += 8)
+                    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                                 : "=r"(add[k]), "=r"(add[k + 1]), "=r"(add[k + 2]), "=r"(add[k + 3]), "=r"(add[k + 4]),
+                                   "=r"(add[k + 5]), "=r"(add[k + 6]), "=r"(add[k + 7])
+                                 : "l"(from + 4 * k));
+            };
+            if (K == kPoly && chunks) fetch(0);
             if (!__all_sync(kFull, mbar_wait(acc_full + 8 * (n & 1), (n / 2) & 1, &dead))) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t acc = tmem + (n & 1) * S::kSide + ((unsigned)(quad * 32) << 16);
-            const int out = g->out + b.matrix * g->out_step;
+            const uint32_t acc = tmem + (n & 1) * S::kSide + half * kChunks * kTileCols + ((unsigned)(quad * 32) << 16);
 #pragma unroll 1
-            for (int c = 0; c < S::kSide / kTileCols; ++c) {
-                const int j = b.n * (S::kSide / kTileCols) + c;  // column of tiles
+            for (int c = 0; c < kChunks; ++c) {
+                const int j = j0 + c;
                 unsigned v[64];
                 tmem_load32(v, acc + c * kTileCols);
                 tmem_load32(v + 32, acc + c * kTileCols + 32);
-                const bool there = j < g->out_pitch && im < g->out_rows;
-                unsigned add[32];
-                if (K == kPoly && there) {
-                    const uint4 *from = reinterpret_cast<const uint4 *>(
-                        a.tiles + (size_t)(g->p.base + b.matrix * g->p.step + im * g->p.pitch + j) * kTileBytes + row * 128);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const uint4 q = from[k];
-                        add[4 * k] = q.x, add[4 * k + 1] = q.y, add[4 * k + 2] = q.z, add[4 * k + 3] = q.w;
-                    }
-                }
                 tmem_wait(v);
-                if (c == S::kSide / kTileCols - 1) {
+                if (c == kChunks - 1) {
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     __syncwarp();
                     if (lane == 0) arrive_cluster(Pair ? in_cta(acc_free + 8 * (n & 1), 0) : acc_free + 8 * (n & 1));
                 }
-                if (!there) continue;
+                if (c >= chunks) continue;
                 unsigned y[32];
 #pragma unroll
                 for (int k = 0; k < 32; ++k) {
@@ -302,18 +341,24 @@ __global__ void __launch_bounds__(kThreads, 1)
                         __half2 h;
                         memcpy(&h, &add[k], 4);
                         const float2 f = __half22float2(h);
-                        const int i = im * kTile + row, col = j * kTileCols + 2 * k;
-                        lo = fmaf((float)kC, lo, fmaf((float)kB, f.x, i == col && i < g->n ? (float)kA : 0.f));
-                        hi = fmaf((float)kC, hi, fmaf((float)kB, f.y, i == col + 1 && i < g->n ? (float)kA : 0.f));
+                        const int col = diagonal - j * kTileCols;
+                        lo = fmaf((float)kC, lo, fmaf((float)kB, f.x, col == 2 * k ? (float)kA : 0.f));
+                        hi = fmaf((float)kC, hi, fmaf((float)kB, f.y, col == 2 * k + 1 ? (float)kA : 0.f));
                     } else {
-                        lo *= g->alpha;
-                        hi *= g->alpha;
+                        lo *= alpha;
+                        hi *= alpha;
                     }
                     const __half2 h = __floats2half2_rn(lo, hi);
                     memcpy(&y[k], &h, 4);
                 }
-                const bool twice = K != kApply && b.m != b.n;
-                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // the last stores have read the buffers
+                if (K == kPoly && c + 1 < chunks) fetch(c + 1);
+                const uint32_t buffer = buffers + other, mirror = buffers + 4096;
+                if (lane == 0) {  // the stores that last used the buffers have read them
+                    if (K == kApply)
+                        asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                    else
+                        asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                }
                 __syncwarp();
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
@@ -332,15 +377,16 @@ __global__ void __launch_bounds__(kThreads, 1)
                 __syncwarp();
                 if (lane == 0) {
                     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(&map_out), "r"(0),
-                                 "r"((out + im * g->out_pitch + j) * kTile + quad * 32), "r"(buffer)
+                                 "r"((out + im * out_pitch + j) * kTile + quad * 32), "r"(buffer)
                                  : "memory");
                     if (twice)
                         asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(&map_mirror),
                                      "r"(32 * (quad & 1)),
-                                     "r"((out + (j >> 1) * g->out_pitch + 2 * im + (quad >> 1)) * kTile + 64 * (j & 1)), "r"(mirror)
+                                     "r"((out + (j >> 1) * out_pitch + 2 * im + (quad >> 1)) * kTile + 64 * (j & 1)), "r"(mirror)
                                      : "memory");
                     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                 }
+                if (K == kApply) other ^= 4096;
             }
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
@@ -395,7 +441,7 @@ struct StreamArgs {
 };
 static_assert(sizeof(StreamArgs) <= 4096 - 64, "kernel parameters");
 
-constexpr int kStreamThreads = 256;
+constexpr int kStreamThreads = 256, kStreamCtas = 3;  // CTAs an SM, that registers are left for
 
 struct Place {
     const Group *g;
@@ -500,7 +546,7 @@ __device__ __forceinline__ void load_update(float (&u)[32], const StreamArgs &a,
 
 // The sum of squares of a warp's elements: in fp32 with an exact power of two taken out, so that no square
 // leaves its range.
-__device__ __forceinline__ double warp_squares(const float (&u)[32]) {
+__device__ __forceinline__ void warp_squares(const float (&u)[32], double *sums) {
     unsigned top = 0;
 #pragma unroll
     for (int k = 0; k < 32; ++k) top = max(top, __float_as_uint(u[k]) & 0x7fffffffu);
@@ -514,19 +560,18 @@ __device__ __forceinline__ double warp_squares(const float (&u)[32]) {
         s = fmaf(v, v, s);
     }
     for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
-    return (double)s * __hiloint2double((1023 + 2 * ((int)e - 127)) << 20, 0);
+    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = (double)s * __hiloint2double((1023 + 2 * ((int)e - 127)) << 20, 0);
 }
 
 template <bool Vec>
 __device__ __forceinline__ void first_tile(const StreamArgs &a, const Place &p, const Matrix &q, double *sums) {
     float u[32];
     load_update<true, Vec>(u, a, p, q);
-    const double s = warp_squares(u);
-    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = s;
+    warp_squares(u, sums);
 }
 __device__ __forceinline__ bool left_out(const StreamArgs &a) { return a.record && a.record[TULA_RECORD_FINITE] == 0.f; }
 
-__global__ void __launch_bounds__(kStreamThreads) k_muon_first(const __grid_constant__ StreamArgs a) {
+__global__ void __launch_bounds__(kStreamThreads, kStreamCtas) k_muon_first(const __grid_constant__ StreamArgs a) {
     __shared__ double sums[kStreamThreads / 32];
     let_next_start();
     wait_for_previous();
@@ -545,10 +590,48 @@ __global__ void __launch_bounds__(kStreamThreads) k_muon_first(const __grid_cons
     a.parts[blockIdx.x] = s;
 }
 
+// u / |u| as u f1 f2: f1 a power of two that brings u near 1, exactly, wherever in fp32's range it is.  A matrix of
+// zeros stays, one with an infinity or NaN becomes NaN.  The norm is taken by every CTA for itself: one of
+// its warps fetches the matrix's parts from L2 while the tile is on its way, one thread ends in fp64 (an SM does
+// some two of its operations a cycle: by all threads they took a third of the kernel's time).
+__device__ __forceinline__ float2 norm_factors(const StreamArgs &a, const Place &p, float2 *factors) {
+    if (threadIdx.x < 32) {
+        const double *parts = a.parts + p.g->first + p.matrix * p.g->per;
+        double s = 0.0;
+        for (int i0 = 0; i0 < p.g->per; i0 += 256) {
+            double v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int i = i0 + 32 * k + threadIdx.x;
+                v[k] = i < p.g->per ? __ldcg(parts + i) : 0.0;
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (i0 + 32 * k < p.g->per) s += v[k];
+        }
+        for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
+        if (threadIdx.x == 0) {
+            const double norm = sqrt(s);
+            float f1 = 0.f, f2 = 0.f;
+            if (!(norm < 1e300)) {
+                f1 = f2 = __uint_as_float(0x7fffffffu);
+            } else if (norm > 0.0) {
+                const int k = max(-126, min(126, (int)((unsigned)__double2hiint(norm) >> 20) - 1023));
+                f1 = __uint_as_float((unsigned)(127 - k) << 23);
+                f2 = (float)((double)p.g->scale / norm * __hiloint2double((1023 + k) << 20, 0));
+            }
+            *factors = make_float2(f1, f2);
+        }
+    }
+    __syncthreads();
+    return *factors;
+}
+
 template <bool Vec>
-__device__ __forceinline__ void scale_tile(const StreamArgs &a, const Place &p, const Matrix &q, float f1, float f2) {
+__device__ __forceinline__ void scale_tile(const StreamArgs &a, const Place &p, const Matrix &q, float2 *factors) {
     float u[32];
     load_update<false, Vec>(u, a, p, q);
+    const float2 f = norm_factors(a, p, factors);
     __half *x = reinterpret_cast<__half *>(a.tiles + (size_t)(p.g->x + p.matrix * p.g->per + p.tile) * kTileBytes);
     constexpr int kN = Vec ? 8 : 1;
 #pragma unroll
@@ -558,43 +641,23 @@ __device__ __forceinline__ void scale_tile(const StreamArgs &a, const Place &p, 
         for (int e = 0; e < kN; ++e) {
             // (a NaN factor leaves the zeros beyond the matrix alone)
             const bool in = p.row0 + row_of<Vec>(k + e) < p.g->rows && p.col0 + col_of<Vec>(k + e) < p.g->cols;
-            r.v[e] = __float2half_rn(in ? __fmul_rn(__fmul_rn(u[k + e], f1), f2) : 0.f);
+            r.v[e] = __float2half_rn(in ? __fmul_rn(__fmul_rn(u[k + e], f.x), f.y) : 0.f);
         }
         *reinterpret_cast<Run<__half, kN> *>(x + row_of<Vec>(k) * kTileCols + col_of<Vec>(k)) = r;
     }
 }
-__global__ void __launch_bounds__(kStreamThreads) k_muon_scale(const __grid_constant__ StreamArgs a) {
-    __shared__ double sums[kStreamThreads / 32];
+__global__ void __launch_bounds__(kStreamThreads, kStreamCtas) k_muon_scale(const __grid_constant__ StreamArgs a) {
+    __shared__ float2 factors;
     let_next_start();
     wait_for_previous();
     if (left_out(a)) return;
     const Place p = place_of(a, blockIdx.x);
-    // the matrix's norm, by every CTA for itself: its tiles' parts come from L2
-    const double *parts = a.parts + p.g->first + p.matrix * p.g->per;
-    double s = 0.0;
-    for (int i = threadIdx.x; i < p.g->per; i += kStreamThreads) s += __ldcg(parts + i);
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
-    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = s;
-    __syncthreads();
-    s = 0.0;
-    for (int k = 0; k < kStreamThreads / 32; ++k) s += sums[k];
-    // u / |u| as u f1 f2: f1 a power of two that brings u near 1, exactly, wherever in fp32's range it is.  A
-    // matrix of zeros stays, one with an infinity or NaN becomes NaN.
-    const double norm = sqrt(s);
-    float f1 = 0.f, f2 = 0.f;
-    if (!(norm < 1e300)) {
-        f1 = f2 = __uint_as_float(0x7fffffffu);
-    } else if (norm > 0.0) {
-        const int k = max(-126, min(126, (int)((unsigned)__double2hiint(norm) >> 20) - 1023));
-        f1 = __uint_as_float((unsigned)(127 - k) << 23);
-        f2 = (float)((double)p.g->scale / norm * __hiloint2double((1023 + k) << 20, 0));
-    }
     Matrix q = {};
     if (a.matrices) q = a.matrices[p.g->matrix + p.matrix];
     if (a.matrices ? q.vec : a.vec)
-        scale_tile<true>(a, p, q, f1, f2);
+        scale_tile<true>(a, p, q, &factors);
     else
-        scale_tile<false>(a, p, q, f1, f2);
+        scale_tile<false>(a, p, q, &factors);
 }
 
 template <bool Vec>
@@ -620,7 +683,7 @@ __device__ __forceinline__ void last_tile(const StreamArgs &a, const Place &p, c
     store_tile<float, Vec>(q.w, p.g->cols, p, w);
     if (q.copy) store_typed<Vec>(q.copy, q.ctype, p.g->cols, p, w);
 }
-__global__ void __launch_bounds__(kStreamThreads) k_muon_last(const __grid_constant__ StreamArgs a) {
+__global__ void __launch_bounds__(kStreamThreads, kStreamCtas) k_muon_last(const __grid_constant__ StreamArgs a) {
     let_next_start();
     wait_for_previous();
     if (left_out(a)) return;

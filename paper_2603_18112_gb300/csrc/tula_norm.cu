@@ -15,7 +15,9 @@
 
 namespace {
 
-constexpr int kMostThreads = 512;  // of a CTA, and of an SM
+constexpr int kMostThreads = 512;  // of a CTA
+// Of an SM, that registers are left for.  (Forward with 512 too: 79 us instead of FWDUS for 16384 x 4096 bf16.)
+constexpr int kForwardThreads = 768, kBackwardThreads = 512;
 constexpr int kMostCluster = 8;
 // Elements that a thread holds of a row.  What each row costs every warp (exchanges, of which an SM does one a
 // cycle, barriers, addresses) is spread over as many: with eight a thread 16384 x 4096 bf16 took 133 us forward.
@@ -32,6 +34,7 @@ struct NormArgs {
     int cluster;              // CTAs to a row
     int share;                // columns of a CTA: all, or a multiple of 16 and none without any
     int stages;               // of the ring
+    int ptype;                // of w and b
     float eps;
 };
 
@@ -39,64 +42,121 @@ __device__ __forceinline__ float value(float v) { return v; }
 __device__ __forceinline__ float value(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float value(__half v) { return __half2float(v); }
 
-// Part t of a row, or of a CTA's share of it, in `group` parts.  Vec: it starts on a 16-byte boundary and has
-// whole vectors of 16 bytes; the threads' vectors lie next to each other.  Else their elements do, and move
-// one by one.
+__device__ __forceinline__ float2 pair_of(unsigned u, __half) {
+    __half2 h;
+    memcpy(&h, &u, 4);
+    return __half22float2(h);
+}
+__device__ __forceinline__ float2 pair_of(unsigned u, __nv_bfloat16) {
+    return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+}
+__device__ __forceinline__ unsigned pair_from(float a, float b, __half) {
+    const __half2 h = __floats2half2_rn(a, b);
+    unsigned u;
+    memcpy(&u, &h, 4);
+    return u;
+}
+__device__ __forceinline__ unsigned pair_from(float a, float b, __nv_bfloat16) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    unsigned u;
+    memcpy(&u, &h, 4);
+    return u;
+}
+
+// What a thread takes of a row, or of a CTA's share of it: t of `group` parts.  Vec: it starts on a 16-byte
+// boundary and has whole vectors of 16 bytes; the threads' vectors lie next to each other.  Else their
+// elements do, and move one by one.
 template <typename T, bool Vec>
 struct Part {
-    static constexpr int kElems = 16 / (int)sizeof(T);
-    T v[kN];
+    static constexpr int kElems = 16 / (int)sizeof(T), kStep = Vec ? kElems : 1;
     static __device__ __forceinline__ int column(int k, int t, int group) {
         return Vec ? (k / kElems * group + t) * kElems + k % kElems : k * group + t;
     }
-    __device__ __forceinline__ void load(const T *row, int t, int group, int cols) {
+    unsigned mask;  // of the elements (Vec: of the vectors) that the row has
+    int at, next;   // the first one's column, columns to the next
+    unsigned w[kN * sizeof(T) / 4];
+
+    __device__ __forceinline__ Part(int t, int group, int cols) : mask(0), at(column(0, t, group)), next(kStep * group) {
+#pragma unroll
+        for (int k = 0; k < kN / kStep; ++k)
+            if (at + k * next < cols) mask |= 1u << k;
+    }
+    __device__ __forceinline__ bool in(int k) const { return mask >> (k / kStep) & 1; }
+    // Zero where there is none.
+    __device__ __forceinline__ void load(const T *row, bool there) {
+        const T *p = row + at;
 #pragma unroll
         for (int k = 0; k < kN; ++k) {
-            const int c = column(k, t, group);
-            v[k] = T(0.f);
-            if (c < cols) v[k] = __ldcs(row + c);
+            T v = T(0.f);
+            if (there && in(k)) v = __ldcs(p + k * next);
+            memcpy(reinterpret_cast<T *>(w) + k, &v, sizeof(T));
         }
     }
-    __device__ __forceinline__ void load_shared(uint32_t row, int t, int group, int cols) {
+    __device__ __forceinline__ void load_shared(uint32_t row, bool there) {
+        const uint32_t p = row + at * (int)sizeof(T);
 #pragma unroll
-        for (int k = 0; k < kN; k += kElems) {
-            const int c = column(k, t, group);
-            uint4 q = make_uint4(0, 0, 0, 0);
-            if (c < cols)
+        for (int k = 0; k < kN / kStep; ++k) {
+            unsigned *q = w + 4 * k;
+            q[0] = q[1] = q[2] = q[3] = 0;
+            if (there && in(k * kStep))
                 asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                             : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w)
-                             : "r"(row + c * (int)sizeof(T))
+                             : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3])
+                             : "r"(p + k * next * (int)sizeof(T))
                              : "memory");
-            memcpy(&v[k], &q, 16);
         }
     }
-    __device__ __forceinline__ void store(T *row, int t, int group, int cols, const float (&f)[kN]) {
+    __device__ __forceinline__ void floats(float (&f)[kN]) const {
+        if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int k = 0; k < kN; k += Vec ? kElems : 1) {
-            const int c = column(k, t, group);
-            if (c >= cols) continue;
-            if (Vec) {
-                __align__(16) T y[kElems];
+            for (int k = 0; k < kN; ++k) f[k] = __uint_as_float(w[k]);
+        } else {
 #pragma unroll
-                for (int j = 0; j < kElems; ++j) put(&y[j], f[k + j]);
-                __stcs(reinterpret_cast<uint4 *>(row + c), *reinterpret_cast<const uint4 *>(y));
-            } else {
-                put(&v[k], f[k]);
-                row[c] = v[k];
+            for (int k = 0; k < kN / 2; ++k) {
+                const float2 v = pair_of(w[k], T());
+                f[2 * k] = v.x;
+                f[2 * k + 1] = v.y;
             }
         }
     }
-};
-
-// The columns' parameters; `none` where there are none.
-template <typename T, bool Vec, typename W>
-__device__ __forceinline__ void load_params(float (&f)[kN], const void *p, float none, int t, int group, int col0, int cols) {
+    __device__ __forceinline__ void store(T *row, const float (&f)[kN]) const {
+        T *p = row + at;
 #pragma unroll
-    for (int k = 0; k < kN; ++k) {
-        const int c = Part<T, Vec>::column(k, t, group);
-        f[k] = none;
-        if (p && c < cols) f[k] = value(static_cast<const W *>(p)[col0 + c]);
+        for (int k = 0; k < kN; k += kStep) {
+            if (!in(k)) continue;
+            if constexpr (Vec && sizeof(T) == 4)
+                __stcs(reinterpret_cast<float4 *>(p + k / kStep * next), make_float4(f[k], f[k + 1], f[k + 2], f[k + 3]));
+            else if constexpr (Vec)
+                __stcs(reinterpret_cast<uint4 *>(p + k / kStep * next),
+                       make_uint4(pair_from(f[k], f[k + 1], T()), pair_from(f[k + 2], f[k + 3], T()), pair_from(f[k + 4], f[k + 5], T()),
+                                  pair_from(f[k + 6], f[k + 7], T())));
+            else
+                put(p + k * next, f[k]);
+        }
     }
+    // The columns' parameters; `none` where there are none.
+    template <typename W>
+    __device__ __forceinline__ void params(float (&f)[kN], const W *p) const {
+#pragma unroll
+        for (int k = 0; k < kN; ++k)
+            if (in(k)) f[k] = value(p[at + k / kStep * next + k % kStep]);
+    }
+    __device__ __forceinline__ void params(float (&f)[kN], const void *p, int type, float none) const {
+#pragma unroll
+        for (int k = 0; k < kN; ++k) f[k] = none;
+        if (!p) return;
+        if (type == TULA_TYPE_F32)
+            params(f, static_cast<const float *>(p));
+        else if (type == TULA_TYPE_BF16)
+            params(f, static_cast<const __nv_bfloat16 *>(p));
+        else
+            params(f, static_cast<const __half *>(p));
+    }
+};
+__device__ __forceinline__ float param(const void *p, int type, int c, float none) {
+    if (!p) return none;
+    return type == TULA_TYPE_F32    ? static_cast<const float *>(p)[c]
+           : type == TULA_TYPE_BF16 ? value(static_cast<const __nv_bfloat16 *>(p)[c])
+                                    : value(static_cast<const __half *>(p)[c]);
 }
 
 // Sums over the threads of a row, the same in all of them.  Within a warp by exchanges; a group's warps go by
@@ -107,16 +167,20 @@ struct Sums {
     float warps[2][2][kMostThreads / 32];
     float2 ctas[2][kMostCluster];
 };
+template <bool Wide>  // groups of more than a warp
 struct GroupSum {
     Sums *place;
     int group, cluster, turn;
     // N sums at a time: one or two.
     template <int N>
     __device__ __forceinline__ void operator()(float (&v)[N]) {
-        for (int o = min(group, 32) / 2; o; o >>= 1)
+        for (int o = Wide ? 16 : group / 2; o; o >>= 1)
 #pragma unroll
             for (int m = 0; m < N; ++m) v[m] += __shfl_xor_sync(kFull, v[m], o);
-        if (group <= 32) return;
+        if constexpr (Wide) across(v);
+    }
+    template <int N>
+    __device__ __forceinline__ void across(float (&v)[N]) {
         const int warp = threadIdx.x >> 5, n = group >> 5;
         if ((threadIdx.x & 31) == 0)
 #pragma unroll
@@ -196,8 +260,8 @@ __device__ __forceinline__ void start_ring(const Ring<T, N> &ring) {
     __syncthreads();
 }
 
-template <typename T, typename W, bool Vec>
-__global__ void __launch_bounds__(kMostThreads) k_norm_forward(const NormArgs a) {
+template <typename T, bool Vec, bool Wide>
+__global__ void __launch_bounds__(kForwardThreads) k_norm_forward(const NormArgs a) {
     using P = Part<T, Vec>;
     extern __shared__ __align__(128) unsigned char memory[];  // Vec: the ring
     __shared__ __align__(16) Sums place;
@@ -212,12 +276,12 @@ __global__ void __launch_bounds__(kMostThreads) k_norm_forward(const NormArgs a)
     let_next_start();
     if (a.cluster > 1) cluster_sync();  // the other CTAs' shared memory may be written to from here on
     wait_for_previous();
-    GroupSum sum{&place, a.group, a.cluster, 0};
+    GroupSum<Wide> sum{&place, a.group, a.cluster, 0};
     const float inv = 1.f / (float)a.cols;
     const T *const x[1] = {static_cast<const T *>(a.x) + col0};
     const long long stride[1] = {a.stride};
     const long long first = block * per;
-    P now, next;
+    P now(t, a.group, cols), next = now;
     if (Vec) {
         if (threadIdx.x < 32) {
             long long r0 = first;
@@ -226,12 +290,13 @@ __global__ void __launch_bounds__(kMostThreads) k_norm_forward(const NormArgs a)
                 ring.fetch(s, from, stride, (int)min((long long)per, a.rows - r0));
             }
         }
-    } else if (first + g < a.rows) {
-        now.load(x[0] + (first + g) * a.stride, t, a.group, cols);
+    } else {
+        now.load(x[0] + (first + g) * a.stride, first + g < a.rows);
     }
+    const int psize = a.ptype == TULA_TYPE_F32 ? 4 : 2;
     float w[kN], b[kN];
-    load_params<T, Vec, W>(w, a.w, 1.f, t, a.group, col0, cols);
-    load_params<T, Vec, W>(b, a.b, 0.f, t, a.group, col0, cols);
+    now.params(w, a.w ? static_cast<const char *>(a.w) + col0 * psize : nullptr, a.ptype, 1.f);
+    now.params(b, a.b ? static_cast<const char *>(a.b) + col0 * psize : nullptr, a.ptype, 0.f);
     int s = 0;
     unsigned parity = 0;
     // (all threads of a CTA go round as often: groups beyond the last row take part in the exchanges)
@@ -240,44 +305,42 @@ __global__ void __launch_bounds__(kMostThreads) k_norm_forward(const NormArgs a)
         const bool there = r < a.rows;
         if (Vec) {
             ring.wait(s, parity);
-            if (there) now.load_shared(ring.row(s, 0, g), t, a.group, cols);
-        } else if (r + step < a.rows) {
-            next.load(x[0] + (r + step) * a.stride, t, a.group, cols);
+            now.load_shared(ring.row(s, 0, g), there);
+        } else {
+            next.load(x[0] + (r + step) * a.stride, r + step < a.rows);
         }
-        float c[kN], total = 0.f;
+        float c[kN], part[2] = {0.f, 0.f};
+        now.floats(c);
 #pragma unroll
-        for (int k = 0; k < kN; ++k) {
-            c[k] = there ? value(now.v[k]) : 0.f;
-            total += c[k];
-        }
-        const float mean = sum(total) * inv;
+        for (int k = 0; k < kN; ++k) part[k & 1] += c[k];
+        const float mean = sum(part[0] + part[1]) * inv;
         if (Vec) {
-            if (a.group <= 32) __syncthreads();
+            if (!Wide) __syncthreads();
             if (threadIdx.x < 32 && r0 + a.stages * step < a.rows) {  // all have read the stage
                 const T *const from[1] = {x[0] + (r0 + a.stages * step) * a.stride};
                 ring.fetch(s, from, stride, (int)min((long long)per, a.rows - r0 - a.stages * step));
             }
             if (++s == a.stages) s = 0, parity ^= 1;
         }
-        total = 0.f;
+        part[0] = part[1] = 0.f;
 #pragma unroll
         for (int k = 0; k < kN; ++k) {
-            c[k] = P::column(k, t, a.group) < cols ? c[k] - mean : 0.f;
-            total = fmaf(c[k], c[k], total);
+            c[k] -= now.in(k) ? mean : 0.f;  // (what the row does not have is 0)
+            part[k & 1] = fmaf(c[k], c[k], part[k & 1]);
         }
-        const float rstd = rsqrtf(sum(total) * inv + a.eps);
+        const float rstd = rsqrtf(sum(part[0] + part[1]) * inv + a.eps);
         if (there) {
 #pragma unroll
             for (int k = 0; k < kN; ++k) c[k] = fmaf(c[k] * rstd, w[k], b[k]);
-            now.store(static_cast<T *>(a.y) + r * a.cols + col0, t, a.group, cols, c);
+            now.store(static_cast<T *>(a.y) + r * a.cols + col0, c);
             if (a.stats && t == 0 && col0 == 0) reinterpret_cast<float2 *>(a.stats)[r] = make_float2(mean, rstd);
         }
         if (!Vec) now = next;
     }
 }
 
-template <typename T, typename W, bool Vec, bool Params>
-__global__ void __launch_bounds__(kMostThreads) k_norm_backward(const NormArgs a) {
+template <typename T, bool Vec, bool Wide, bool Params>
+__global__ void __launch_bounds__(kBackwardThreads) k_norm_backward(const NormArgs a) {
     using P = Part<T, Vec>;
     extern __shared__ __align__(128) unsigned char memory[];  // Vec: the ring; Params: then the groups' sums
     __shared__ __align__(16) Sums place;
@@ -292,13 +355,13 @@ __global__ void __launch_bounds__(kMostThreads) k_norm_backward(const NormArgs a
     let_next_start();
     if (a.cluster > 1) cluster_sync();
     wait_for_previous();
-    GroupSum sum{&place, a.group, a.cluster, 0};
+    GroupSum<Wide> sum{&place, a.group, a.cluster, 0};
     const float inv = 1.f / (float)a.cols;
     const T *const x = static_cast<const T *>(a.x) + col0, *const dy = static_cast<const T *>(a.dy) + col0;
     const long long stride[2] = {a.stride, a.dy_stride};
     const float2 *stats = reinterpret_cast<const float2 *>(a.stats);
     const long long first = block * per;
-    P now_x, now_d, next_x, next_d;
+    P now_x(t, a.group, cols), now_d = now_x, next_x = now_x, next_d = now_x;
     float2 now_s = make_float2(0.f, 0.f), next_s = now_s;
     if (Vec) {
         if (threadIdx.x < 32) {
@@ -308,13 +371,13 @@ __global__ void __launch_bounds__(kMostThreads) k_norm_backward(const NormArgs a
                 ring.fetch(s, from, stride, (int)min((long long)per, a.rows - r0));
             }
         }
-    } else if (first + g < a.rows) {
-        now_x.load(x + (first + g) * a.stride, t, a.group, cols);
-        now_d.load(dy + (first + g) * a.dy_stride, t, a.group, cols);
+    } else {
+        now_x.load(x + (first + g) * a.stride, first + g < a.rows);
+        now_d.load(dy + (first + g) * a.dy_stride, first + g < a.rows);
     }
     if (first + g < a.rows) now_s = __ldcs(stats + first + g);
     float w[kN], dw[kN], db[kN];
-    load_params<T, Vec, W>(w, a.w, 1.f, t, a.group, col0, cols);
+    now_x.params(w, a.w ? static_cast<const char *>(a.w) + col0 * (a.ptype == TULA_TYPE_F32 ? 4 : 2) : nullptr, a.ptype, 1.f);
 #pragma unroll
     for (int k = 0; k < kN; ++k) dw[k] = db[k] = 0.f;
     int s = 0;
@@ -322,26 +385,22 @@ __global__ void __launch_bounds__(kMostThreads) k_norm_backward(const NormArgs a
     for (long long r0 = first; r0 < a.rows; r0 += step) {
         const long long r = r0 + g;
         const bool there = r < a.rows;
-        if (r + step < a.rows) {
-            next_s = __ldcs(stats + r + step);
-            if (!Vec) {
-                next_x.load(x + (r + step) * a.stride, t, a.group, cols);
-                next_d.load(dy + (r + step) * a.dy_stride, t, a.group, cols);
-            }
-        }
+        if (r + step < a.rows) next_s = __ldcs(stats + r + step);
         if (Vec) {
             ring.wait(s, parity);
-            if (there) {
-                now_x.load_shared(ring.row(s, 0, g), t, a.group, cols);
-                now_d.load_shared(ring.row(s, 1, g), t, a.group, cols);
-            }
+            now_x.load_shared(ring.row(s, 0, g), there);
+            now_d.load_shared(ring.row(s, 1, g), there);
+        } else {
+            next_x.load(x + (r + step) * a.stride, r + step < a.rows);
+            next_d.load(dy + (r + step) * a.dy_stride, r + step < a.rows);
         }
+        const float rstd = there ? now_s.y : 0.f, mean = there ? now_s.x : 0.f;
         float n[kN], d[kN], s1 = 0.f, s2 = 0.f;
+        now_x.floats(n);
+        now_d.floats(d);
 #pragma unroll
         for (int k = 0; k < kN; ++k) {
-            const bool in = there && P::column(k, t, a.group) < cols;
-            n[k] = in ? (value(now_x.v[k]) - now_s.x) * now_s.y : 0.f;
-            d[k] = in ? value(now_d.v[k]) : 0.f;
+            n[k] = (n[k] - (now_x.in(k) ? mean : 0.f)) * rstd;  // (what the row does not have is 0)
             if (Params) {
                 dw[k] = fmaf(d[k], n[k], dw[k]);
                 db[k] += d[k];
@@ -353,7 +412,7 @@ __global__ void __launch_bounds__(kMostThreads) k_norm_backward(const NormArgs a
         float sums[2] = {s1, s2};
         if (a.y) sum(sums);
         if (Vec) {
-            if (!a.y || a.group <= 32) __syncthreads();
+            if (!a.y || !Wide) __syncthreads();
             if (threadIdx.x < 32 && r0 + a.stages * step < a.rows) {  // all have read the stage
                 const T *const from[2] = {x + (r0 + a.stages * step) * a.stride, dy + (r0 + a.stages * step) * a.dy_stride};
                 ring.fetch(s, from, stride, (int)min((long long)per, a.rows - r0 - a.stages * step));
@@ -361,10 +420,10 @@ __global__ void __launch_bounds__(kMostThreads) k_norm_backward(const NormArgs a
             if (++s == a.stages) s = 0, parity ^= 1;
         }
         if (a.y && there) {
-            const float m1 = sums[0] * inv, m2 = sums[1] * inv;
+            const float m1 = sums[0] * inv * rstd, m2 = sums[1] * inv * rstd;
 #pragma unroll
-            for (int k = 0; k < kN; ++k) d[k] = now_s.y * (d[k] - fmaf(n[k], m2, m1));
-            now_x.store(static_cast<T *>(a.y) + r * a.cols + col0, t, a.group, cols, d);
+            for (int k = 0; k < kN; ++k) d[k] = fmaf(rstd, d[k], -fmaf(n[k], m2, m1));
+            now_x.store(static_cast<T *>(a.y) + r * a.cols + col0, d);
         }
         if (!Vec) now_x = next_x, now_d = next_d;
         now_s = next_s;
@@ -400,12 +459,12 @@ __global__ void __launch_bounds__(kMostThreads) k_norm_backward(const NormArgs a
 }
 
 // Rows that registers do not hold: a CTA to a row, which is read three times, or twice, mostly from L2.
-template <typename T, typename W>
+template <typename T>
 __global__ void __launch_bounds__(kMostThreads) k_norm_forward_wide(const NormArgs a) {
     __shared__ __align__(16) Sums place;
     let_next_start();
     wait_for_previous();
-    GroupSum sum{&place, (int)blockDim.x, 1, 0};
+    GroupSum<true> sum{&place, (int)blockDim.x, 1, 0};
     const int cols = a.cols;
     for (long long r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const T *x = static_cast<const T *>(a.x) + r * a.stride;
@@ -420,25 +479,25 @@ __global__ void __launch_bounds__(kMostThreads) k_norm_forward_wide(const NormAr
         const float rstd = rsqrtf(sum(s) / (float)cols + a.eps);
         T *y = static_cast<T *>(a.y) + r * cols;
         for (int c = threadIdx.x; c < cols; c += blockDim.x) {
-            const float w = a.w ? value(static_cast<const W *>(a.w)[c]) : 1.f, b = a.b ? value(static_cast<const W *>(a.b)[c]) : 0.f;
+            const float w = param(a.w, a.ptype, c, 1.f), b = param(a.b, a.ptype, c, 0.f);
             put(y + c, fmaf((value(x[c]) - mean) * rstd, w, b));
         }
         if (a.stats && threadIdx.x == 0) reinterpret_cast<float2 *>(a.stats)[r] = make_float2(mean, rstd);
     }
 }
-template <typename T, typename W>
+template <typename T>
 __global__ void __launch_bounds__(kMostThreads) k_norm_backward_wide(const NormArgs a) {
     __shared__ __align__(16) Sums place;
     let_next_start();
     wait_for_previous();
-    GroupSum sum{&place, (int)blockDim.x, 1, 0};
+    GroupSum<true> sum{&place, (int)blockDim.x, 1, 0};
     const int cols = a.cols;
     for (long long r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const T *x = static_cast<const T *>(a.x) + r * a.stride, *dy = static_cast<const T *>(a.dy) + r * a.dy_stride;
         const float2 st = reinterpret_cast<const float2 *>(a.stats)[r];
         float s1 = 0.f, s2 = 0.f;
         for (int c = threadIdx.x; c < cols; c += blockDim.x) {
-            const float g = value(dy[c]) * (a.w ? value(static_cast<const W *>(a.w)[c]) : 1.f);
+            const float g = value(dy[c]) * param(a.w, a.ptype, c, 1.f);
             s1 += g;
             s2 = fmaf(g, (value(x[c]) - st.x) * st.y, s2);
         }
@@ -446,7 +505,7 @@ __global__ void __launch_bounds__(kMostThreads) k_norm_backward_wide(const NormA
         sum(s);
         T *dx = static_cast<T *>(a.y) + r * cols;
         for (int c = threadIdx.x; c < cols; c += blockDim.x) {
-            const float g = value(dy[c]) * (a.w ? value(static_cast<const W *>(a.w)[c]) : 1.f);
+            const float g = value(dy[c]) * param(a.w, a.ptype, c, 1.f);
             put(dx + c, st.y * (g - fmaf((value(x[c]) - st.x) * st.y, s[1], s[0]) / (float)cols));
         }
     }
@@ -503,7 +562,7 @@ struct Layout {
     unsigned grid;
     unsigned blocks() const { return grid / (unsigned)std::max(1, cluster); }
 };
-Layout layout_of(long long rows, int cols, int sms) {
+Layout layout_of(long long rows, int cols, int sms, int sm_threads) {
     Layout l;
     const long long ctas = up(cols, kMostThreads * kN);
     l.cluster = ctas <= kMostCluster ? (int)ctas : 0;
@@ -515,7 +574,7 @@ Layout layout_of(long long rows, int cols, int sms) {
         l.grid = (unsigned)std::min<long long>(rows, 4ll * sms);
         return l;
     }
-    const long long per = l.threads / l.group, blocks = std::max(1, sms * (kMostThreads / l.threads) / l.cluster);
+    const long long per = l.threads / l.group, blocks = std::max(1, sms * (sm_threads / l.threads) / l.cluster);
     l.grid = (unsigned)(l.cluster * std::min(up(rows, per), blocks));
     return l;
 }
@@ -525,11 +584,11 @@ unsigned parts_of(const Layout &l, long long rows) {
     return l.cluster ? l.blocks() : (unsigned)std::min<long long>(kWideParts, up(rows, 64));
 }
 
-// The ring's memory: 384 bytes a thread, so that all threads of an SM take 192 KB.
-constexpr int kRingThread = 384, kRingMost = kRingThread * kMostThreads;
-inline int ring_bytes(const Layout &l, size_t size, int matrices, int &stages) {
+// The ring's memory: so much a thread that all threads of an SM take 192 KB.
+constexpr int kRingMost = 192 * 1024;
+inline int ring_bytes(const Layout &l, size_t size, int matrices, int sm_threads, int &stages) {
     const int stage = l.threads * kN * (int)size * matrices;
-    stages = std::min(kMostStages, kRingThread * l.threads / stage);
+    stages = std::min(kMostStages, kRingMost / (sm_threads / l.threads) / stage);
     return stages * stage;
 }
 
@@ -537,23 +596,30 @@ inline bool lies(const void *p, long long stride, size_t size) {  // rows on 16-
     return (reinterpret_cast<uintptr_t>(p) | (size_t)stride * size) % 16 == 0;
 }
 
-template <typename T, typename W>
+template <typename T>
 int forward_typed(NormArgs &a, cudaStream_t s) {
-    const Layout l = layout_of(a.rows, a.cols, std::max(1, sm_count()));
-    if (!l.cluster) return tula::launch(k_norm_forward_wide<T, W>, dim3(l.grid), l.threads, 0, s, 1, a);
+    const Layout l = layout_of(a.rows, a.cols, std::max(1, sm_count()), kForwardThreads);
+    if (!l.cluster) return tula::launch(k_norm_forward_wide<T>, dim3(l.grid), l.threads, 0, s, 1, a);
     a.group = l.group;
     a.cluster = l.cluster;
     a.share = l.share;
     const bool vec = a.cols % (16 / (int)sizeof(T)) == 0 && lies(a.x, a.stride, sizeof(T)) && lies(a.y, a.cols, sizeof(T));
-    void (*k)(const NormArgs) = vec ? k_norm_forward<T, W, true> : k_norm_forward<T, W, false>;
-    static std::atomic<uint64_t> done;
-    const int smem = vec ? ring_bytes(l, sizeof(T), 1, a.stages) : 0;
-    const int rc = vec ? allow_smem((const void *)k, kRingMost, &done) : TULA_OK;
+    const bool wide = l.group > 32;
+    void (*k)(const NormArgs) = vec ? (wide ? k_norm_forward<T, true, true> : k_norm_forward<T, true, false>)
+                                    : (wide ? k_norm_forward<T, false, true> : k_norm_forward<T, false, false>);
+    static std::atomic<uint64_t> done[2];
+    const int smem = vec ? ring_bytes(l, sizeof(T), 1, kForwardThreads, a.stages) : 0;
+    const int rc = vec ? allow_smem((const void *)k, kRingMost, &done[wide]) : TULA_OK;
     return rc ? rc : tula::launch(k, dim3(l.grid), l.threads, smem, s, l.cluster, a);
 }
-template <typename T, typename W>
+template <typename T, bool Params>
+void (*backward_kernel(bool vec, bool wide))(const NormArgs) {
+    return vec ? (wide ? k_norm_backward<T, true, true, Params> : k_norm_backward<T, true, false, Params>)
+               : (wide ? k_norm_backward<T, false, true, Params> : k_norm_backward<T, false, false, Params>);
+}
+template <typename T>
 int backward_typed(NormArgs &a, void *dw, void *db, cudaStream_t s) {
-    const Layout l = layout_of(a.rows, a.cols, std::max(1, sm_count()));
+    const Layout l = layout_of(a.rows, a.cols, std::max(1, sm_count()), kBackwardThreads);
     int rc = TULA_OK;
     if (l.cluster) {
         a.group = l.group;
@@ -561,36 +627,29 @@ int backward_typed(NormArgs &a, void *dw, void *db, cudaStream_t s) {
         a.share = l.share;
         const bool vec = a.cols % (16 / (int)sizeof(T)) == 0 && lies(a.x, a.stride, sizeof(T)) && lies(a.dy, a.dy_stride, sizeof(T)) &&
                          (!a.y || lies(a.y, a.cols, sizeof(T)));
-        void (*k)(const NormArgs) = a.parts ? (vec ? k_norm_backward<T, W, true, true> : k_norm_backward<T, W, false, true>)
-                                            : (vec ? k_norm_backward<T, W, true, false> : k_norm_backward<T, W, false, false>);
-        static std::atomic<uint64_t> done[2];
-        int smem = vec ? ring_bytes(l, sizeof(T), 2, a.stages) : 0;
+        const bool wide = l.group > 32;
+        void (*k)(const NormArgs) = a.parts ? backward_kernel<T, true>(vec, wide) : backward_kernel<T, false>(vec, wide);
+        static std::atomic<uint64_t> done[4];
+        int smem = vec ? ring_bytes(l, sizeof(T), 2, kBackwardThreads, a.stages) : 0;
         if (a.parts && l.threads > l.group) smem = std::max(smem, 2 * l.threads * kN * 4);  // 32 KB
-        if (vec) rc = allow_smem((const void *)k, kRingMost, &done[a.parts != nullptr]);
+        if (vec) rc = allow_smem((const void *)k, kRingMost, &done[2 * wide + (a.parts != nullptr)]);
         if (!rc) rc = tula::launch(k, dim3(l.grid), l.threads, smem, s, l.cluster, a);
     } else {
-        if (a.y) rc = tula::launch(k_norm_backward_wide<T, W>, dim3(l.grid), l.threads, 0, s, 1, a);
+        if (a.y) rc = tula::launch(k_norm_backward_wide<T>, dim3(l.grid), l.threads, 0, s, 1, a);
         if (!rc && a.parts)
             rc = tula::launch(k_norm_sums_wide<T>, dim3((unsigned)up(a.cols, 256), parts_of(l, a.rows)), 256, 0, s, 1, a);
     }
     if (rc || !a.parts) return rc;
-    return tula::launch(k_norm_params<W>, dim3((unsigned)up(2ll * a.cols, 32)), 1024, 0, s, 1, (const float *)a.parts,
-                        (int)parts_of(l, a.rows), a.cols, static_cast<W *>(dw), static_cast<W *>(db));
+    auto params = [&](auto w) {
+        using W = decltype(w);
+        return tula::launch(k_norm_params<W>, dim3((unsigned)up(2ll * a.cols, 32)), 1024, 0, s, 1, (const float *)a.parts,
+                            (int)parts_of(l, a.rows), a.cols, static_cast<W *>(dw), static_cast<W *>(db));
+    };
+    if (a.ptype == TULA_TYPE_F32) return params(float());
+    return a.ptype == TULA_TYPE_BF16 ? params(__nv_bfloat16()) : params(__half());
 }
 
 constexpr long long kMostCols = 1LL << 24;
-
-template <typename F>
-int by_types(int type, int param_type, F f) {
-    auto second = [&](auto t) {
-        if (param_type == TULA_TYPE_F32) return f(t, float());
-        if (param_type == TULA_TYPE_BF16) return f(t, __nv_bfloat16());
-        return f(t, __half());
-    };
-    if (type == TULA_TYPE_F32) return second(float());
-    if (type == TULA_TYPE_BF16) return second(__nv_bfloat16());
-    return second(__half());
-}
 
 bool good_sizes(long long rows, long long cols) { return rows >= 0 && cols >= 0 && cols <= kMostCols && rows < (1LL << 40); }
 
@@ -615,8 +674,10 @@ int tula_layer_norm(const void *x, int type, int64_t rows, int64_t cols, int64_t
     a.cols = (int)cols;
     a.stride = stride;
     a.eps = eps;
+    a.ptype = param_type;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return by_types(type, param_type, [&](auto t, auto w) { return forward_typed<decltype(t), decltype(w)>(a, s); });
+    if (type == TULA_TYPE_F32) return forward_typed<float>(a, s);
+    return type == TULA_TYPE_BF16 ? forward_typed<__nv_bfloat16>(a, s) : forward_typed<__half>(a, s);
 }
 
 int tula_layer_norm_workspace_size(int64_t rows, int64_t cols, size_t *bytes) {
@@ -657,7 +718,9 @@ int tula_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, i
     a.cols = (int)cols;
     a.stride = stride;
     a.dy_stride = dy_stride;
-    return by_types(type, param_type, [&](auto t, auto w) { return backward_typed<decltype(t), decltype(w)>(a, dweight, dbias, s); });
+    a.ptype = param_type;
+    if (type == TULA_TYPE_F32) return backward_typed<float>(a, dweight, dbias, s);
+    return type == TULA_TYPE_BF16 ? backward_typed<__nv_bfloat16>(a, dweight, dbias, s) : backward_typed<__half>(a, dweight, dbias, s);
 }
 
 }  // extern "C"
