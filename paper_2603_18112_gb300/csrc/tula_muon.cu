@@ -7,8 +7,9 @@
 //
 //   k_muon_first   m = mu m + d, and the sum of squares of what is orthogonalised, a part a tile
 //   k_muon_scale   X = u / |u|, in fp16
-//   k_product      A = X X^T;  B = a I + b A + c A^2;  X' = B X: three launches a step
-//   k_muon_last    the weights and their copies, or the values themselves
+//   k_product      A = X X^T;  B = a I + b A + c A^2;  X' = B X: three launches a step.  The last one writes
+//                  the weights and their copies, or the values themselves
+//   k_muon_last    does that for matrices whose rows do not lie on 32-byte boundaries
 //
 // One launch covers all matrices of a list.  The products are nearly all of the work: per step 2 n^2 m and
 // 2 n^3 operations of which symmetry leaves half, and 2 n^2 m.  They run on the tensor cores from fp16
@@ -49,6 +50,12 @@ struct Side {
     int pitch, rows;  // tiles
     int along;
 };
+struct Matrix {  // of a plan
+    const void *g;
+    float *m, *w;
+    void *copy;
+    int gtype, ctype, vec, spare;  // vec: eight elements of a row at a time, on boundaries of 16 bytes (w: 32)
+};
 struct ProductGroup {
     Side p, q;
     int out, out_step, out_pitch, out_rows;
@@ -57,10 +64,17 @@ struct ProductGroup {
     int n_k;          // stages of 64
     int n;            // where the identity ends
     float alpha;
+    int finish;       // kLast: the weights or values are written
+    int rows, cols, matrix;  // the first one's place in the plan's table
+    float step;       // lr times the shape's factor
 };
 struct ProductArgs {
     const unsigned char *tiles;
     const float *record;
+    const Matrix *matrices;  // kLast: a plan's, or NULL:
+    void *y;                 // the values' place, contiguous
+    int ytype;
+    float decay;
     int n_groups, n_blocks;
     int none;         // a row beyond the workspace
     ProductGroup g[kMostGroups];
@@ -68,8 +82,10 @@ struct ProductArgs {
 static_assert(sizeof(ProductArgs) <= 4096 - 3 * 128 - 64, "kernel parameters");
 
 // What is made of the sums: alpha times them, of a symmetric product (its blocks on and above the diagonal are
-// taken, and stored twice); the polynomial, symmetric too; alpha times them.
-enum Kind { kGram, kPoly, kApply };
+// taken, and stored twice); the polynomial, symmetric too; alpha times them; the same of the last step, which
+// goes straight to the weights.  (That is bound by HBM then, with the tensor cores two thirds as busy, but by
+// LASTUS us for 151 M weights instead of 184 and 299 one after the other.)
+enum Kind { kGram, kPoly, kApply, kLast };
 
 // A copying warp, an issuing warp, and those that read back: two to each quarter of tensor memory's lanes, each
 // with half of the columns.  (With one to a quarter the sums of 1024 columns were read back more slowly than
@@ -125,7 +141,7 @@ __device__ __forceinline__ Block block_at(const ProductArgs &a, int t, const Pro
     Block b;
     b.matrix = in / g->per;
     int k = in - b.matrix * g->per;
-    if (K == kApply) {
+    if (K >= kApply) {
         b.m = k % g->blocks_m;
         b.n = k / g->blocks_m;
     } else {  // columns of the upper triangle
@@ -163,6 +179,37 @@ struct Walk {
     }
 };
 
+// Eight elements on a boundary of 32 bytes (fp32) or 16.
+__device__ __forceinline__ void load8(float *f, const float *from) {
+    unsigned r[8];
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "l"(from));
+#pragma unroll
+    for (int k = 0; k < 8; ++k) f[k] = __uint_as_float(r[k]);
+}
+__device__ __forceinline__ void store8(float *to, const float (&f)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(__float_as_uint(f[0])),
+                 "r"(__float_as_uint(f[1])), "r"(__float_as_uint(f[2])), "r"(__float_as_uint(f[3])), "r"(__float_as_uint(f[4])),
+                 "r"(__float_as_uint(f[5])), "r"(__float_as_uint(f[6])), "r"(__float_as_uint(f[7]))
+                 : "memory");
+}
+__device__ __forceinline__ void store8(void *to, int type, size_t at, const float (&f)[8]) {
+    unsigned u[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (type == TULA_TYPE_BF16) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * k], f[2 * k + 1]);
+            memcpy(&u[k], &h, 4);
+        } else {
+            const __half2 h = __floats2half2_rn(f[2 * k], f[2 * k + 1]);
+            memcpy(&u[k], &h, 4);
+        }
+    }
+    *reinterpret_cast<uint4 *>(static_cast<unsigned short *>(to) + at) = make_uint4(u[0], u[1], u[2], u[3]);
+}
+__device__ __forceinline__ void prefetch_map(const CUtensorMap *map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
+
 template <bool Pair, Kind K>
 __global__ void __launch_bounds__(kThreads, 1)
     k_product(const __grid_constant__ CUtensorMap map_in, const __grid_constant__ CUtensorMap map_out,
@@ -190,6 +237,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (warp == 0 && elect_one()) prefetch_map(&map_in);
+    if (warp == 2 && elect_one()) {
+        prefetch_map(&map_out);
+        if (K < kApply) prefetch_map(&map_mirror);
+    }
     if (warp == 1) {
         if (Pair) {
             asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_at)), "r"(S::kCols)
@@ -205,6 +257,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = __shfl_sync(kFull, *tmem_at, 0);
     let_next_start();
+    {  // the first block's parameters are on their way while the kernel before ends
+        const ProductGroup *g;
+        const Block b = block_at<K>(a, min(worker, a.n_blocks - 1), g);
+        asm volatile("" ::"r"(g->n_k), "r"(b.matrix), "r"(g->out), "r"(g->q.base) : "memory");
+    }
     wait_for_previous();
     const bool go = !a.record || a.record[TULA_RECORD_FINITE] != 0.f;
     const int n_blocks = go ? a.n_blocks : 0;
@@ -301,8 +358,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int j0 = b.n * (S::kSide / kTileCols) + half * kChunks;  // column of tiles
             const int out_pitch = g->out_pitch;
             const int chunks = im < g->out_rows ? max(0, min(kChunks, out_pitch - j0)) : 0;  // within the output
-            const bool twice = K != kApply && b.m != b.n;
-            const float alpha = g->alpha;
+            const bool twice = K < kApply && b.m != b.n;
+            const float alpha = g->alpha, step = g->step;
             const int diagonal = K == kPoly && row + im * kTile < g->n ? row + im * kTile : -1;
             const unsigned char *const added =  // kPoly: A's rows
                 a.tiles + (size_t)(g->p.base + b.matrix * g->p.step + im * g->p.pitch + j0) * kTileBytes + row * 128;
@@ -317,6 +374,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                                  : "l"(from + 4 * k));
             };
             if (K == kPoly && chunks) fetch(0);
+            const bool finish = K == kLast && g->finish;
+            if (finish) {  // (a block of another group may have left a store that reads the buffers)
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            }
+            // (the weights move by eight lanes to 64 columns of a row)
+            const int first_row = im * kTile + quad * 32 + (lane >> 3), cols = g->cols, rows_left = g->rows - first_row;
+            Matrix q = {};
+            if (finish && a.matrices) q = a.matrices[g->matrix + b.matrix];
             if (!__all_sync(kFull, mbar_wait(acc_full + 8 * (n & 1), (n / 2) & 1, &dead))) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t acc = tmem + (n & 1) * S::kSide + half * kChunks * kTileCols + ((unsigned)(quad * 32) << 16);
@@ -326,6 +391,15 @@ __global__ void __launch_bounds__(kThreads, 1)
                 unsigned v[64];
                 tmem_load32(v, acc + c * kTileCols);
                 tmem_load32(v + 32, acc + c * kTileCols + 32);
+                const int col = j * kTileCols + (lane & 7) * 8;
+                const bool mine = finish && c < chunks && col < cols;
+                float w[K == kLast ? 64 : 1];
+                if constexpr (K == kLast)
+                    if (q.w && mine) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            if (4 * k < rows_left) load8(w + 8 * k, q.w + (size_t)(first_row + 4 * k) * cols + col);
+                    }
                 tmem_wait(v);
                 if (c == kChunks - 1) {
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -333,6 +407,45 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (lane == 0) arrive_cluster(Pair ? in_cta(acc_free + 8 * (n & 1), 0) : acc_free + 8 * (n & 1));
                 }
                 if (c >= chunks) continue;
+                if constexpr (K == kLast) {
+                    if (finish) {
+                        // the values change from a row a lane to a row eight lanes: 32 rows of 256 bytes, their
+                        // 32-byte pieces exchanged so that neither way meets in a bank
+                        __syncwarp();  // the last ones have been read
+#pragma unroll
+                        for (int k = 0; k < 16; ++k)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buffers + lane * 256 + ((k ^ (lane & 7) << 1) << 4)),
+                                         "r"(v[4 * k]), "r"(v[4 * k + 1]), "r"(v[4 * k + 2]), "r"(v[4 * k + 3])
+                                         : "memory");
+                        __syncwarp();
+                        if (!mine) continue;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            if (4 * k >= rows_left) break;
+                            const int r = 4 * k + (lane >> 3);
+                            const uint32_t from = buffers + r * 256 + (((lane & 7) ^ (r & 7)) << 5);
+                            float x[8];
+#pragma unroll
+                            for (int h = 0; h < 2; ++h)
+                                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                                             : "=f"(x[4 * h]), "=f"(x[4 * h + 1]), "=f"(x[4 * h + 2]), "=f"(x[4 * h + 3])
+                                             : "r"(from + 16 * h)
+                                             : "memory");
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) x[e] *= alpha;
+                            const size_t at = (size_t)(first_row + 4 * k) * cols + col;
+                            if (q.w) {
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) x[e] = fmaf(-step, x[e], __fmul_rn(w[8 * k + e], a.decay));
+                                store8(q.w + at, x);
+                                if (q.copy) store8(q.copy, q.ctype, at, x);
+                            } else {
+                                store8(a.y, a.ytype, (size_t)b.matrix * g->rows * cols + at, x);
+                            }
+                        }
+                        continue;
+                    }
+                }
                 unsigned y[32];
 #pragma unroll
                 for (int k = 0; k < 32; ++k) {
@@ -354,7 +467,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (K == kPoly && c + 1 < chunks) fetch(c + 1);
                 const uint32_t buffer = buffers + other, mirror = buffers + 4096;
                 if (lane == 0) {  // the stores that last used the buffers have read them
-                    if (K == kApply)
+                    if (K >= kApply)
                         asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
                     else
                         asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
@@ -386,7 +499,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                                      : "memory");
                     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                 }
-                if (K == kApply) other ^= 4096;
+                if (K >= kApply) other ^= 4096;
             }
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
@@ -412,12 +525,6 @@ __global__ void __launch_bounds__(kThreads, 1)
 // rows of a multiple of eight elements at 16-byte boundaries), else one.  These stream: 8 to 22 bytes an
 // element.
 
-struct Matrix {  // of a plan
-    const void *g;
-    float *m, *w;
-    void *copy;
-    int gtype, ctype, vec, spare;
-};
 struct Group {
     int first, per;       // the group's first tile of all, tiles to a matrix
     int matrix;           // its first matrix
@@ -436,7 +543,7 @@ struct StreamArgs {
     double *parts;           // sums of squares, one a tile
     const float *record;
     float grad_scale, mu, decay;
-    int nesterov, n_groups;
+    int nesterov, n_groups, tile0;  // tile0: k_muon_last's first
     Group g[kMostGroups];
 };
 static_assert(sizeof(StreamArgs) <= 4096 - 64, "kernel parameters");
@@ -687,7 +794,7 @@ __global__ void __launch_bounds__(kStreamThreads, kStreamCtas) k_muon_last(const
     let_next_start();
     wait_for_previous();
     if (left_out(a)) return;
-    const Place p = place_of(a, blockIdx.x);
+    const Place p = place_of(a, a.tile0 + blockIdx.x);
     Matrix q = {};
     if (a.matrices) q = a.matrices[p.g->matrix + p.matrix];
     if (a.matrices ? q.vec : a.vec)
@@ -704,6 +811,8 @@ __global__ void __launch_bounds__(kStreamThreads, kStreamCtas) k_muon_last(const
 struct Kin {
     long long rows, cols;
     int count, matrix;  // how many, the first one's place in the table
+    int vec;            // as Matrix's
+    float step;         // lr times the shape's factor
     int x0, x1, gram, poly;  // first tiles
     int tile_rows() const { return (int)up(rows, kTile); }
     int tile_cols() const { return (int)up(cols, kTileCols); }
@@ -776,7 +885,12 @@ int fill(ProductArgs &a, const Kin *kin, int n, Kind kind, int x, bool first) {
         across.along = 0;
         g.n = (int)k.n();
         g.alpha = 1.f;
-        if (kind == kApply) {
+        g.finish = kind == kLast && k.vec;
+        g.rows = (int)k.rows;
+        g.cols = (int)k.cols;
+        g.matrix = k.matrix;
+        g.step = k.step;
+        if (kind >= kApply) {
             g.p = k.wide() ? sb : sx;
             g.q = k.wide() ? across : sb;
             g.out = x ? k.x0 : k.x1;
@@ -818,12 +932,16 @@ int product(const Maps &maps, ProductArgs &a, const Kin *kin, int n, int x, bool
     return launch_product<false, K>(maps, a, sms, s);
 }
 
-// All of it for shapes whose tiles are placed.  `stream`: its groups are filled here.
+// All of it for shapes whose tiles are placed, those with Kin::vec first.  `st`: its groups are filled here.
 int run(const Maps &maps, long long n_tiles, const Kin *kin, int n, StreamArgs &st, int steps, cudaStream_t s) {
     const int sms = std::max(1, sm_count());
     ProductArgs a;
     a.tiles = st.tiles;
     a.record = st.record;
+    a.matrices = st.matrices;
+    a.y = st.y;
+    a.ytype = st.ytype;
+    a.decay = st.decay;
     a.none = (int)(n_tiles * kTile);
     long long tiles = 0;
     st.n_groups = n;
@@ -839,17 +957,25 @@ int run(const Maps &maps, long long n_tiles, const Kin *kin, int n, StreamArgs &
         g.x = k.x0;
         g.x_last = steps % 2 ? k.x1 : k.x0;
         g.scale = steps ? (float)std::ldexp(1.0, k.shift()) : 1.f;
+        g.step = k.step;
         tiles += (long long)g.per * k.count;
     }
     if (tiles == 0) return TULA_OK;
+    // (By parts of 48 MB, that the second of the two would find in L2, they take longer: 12 to 14 us a launch.)
     int rc = tula::launch(k_muon_first, dim3((unsigned)tiles), kStreamThreads, 0, s, 1, st);
     if (!rc) rc = tula::launch(k_muon_scale, dim3((unsigned)tiles), kStreamThreads, 0, s, 1, st);
     for (int i = 0; !rc && i < steps; ++i) {
         rc = product<kGram>(maps, a, kin, n, i & 1, i == 0, sms, s);
         if (!rc) rc = product<kPoly>(maps, a, kin, n, i & 1, i == 0, sms, s);
-        if (!rc) rc = product<kApply>(maps, a, kin, n, i & 1, i == 0, sms, s);
+        if (!rc)
+            rc = i == steps - 1 ? product<kLast>(maps, a, kin, n, i & 1, i == 0, sms, s)
+                                : product<kApply>(maps, a, kin, n, i & 1, i == 0, sms, s);
     }
-    if (!rc) rc = tula::launch(k_muon_last, dim3((unsigned)tiles), kStreamThreads, 0, s, 1, st);
+    // what the last product has not finished
+    st.tile0 = 0;
+    for (int i = 0; steps && i < n && kin[i].vec; ++i) st.tile0 += st.g[i].per * kin[i].count;
+    if (!rc && st.tile0 < tiles)
+        rc = tula::launch(k_muon_last, dim3((unsigned)(tiles - st.tile0)), kStreamThreads, 0, s, 1, st);
     return rc;
 }
 
@@ -869,14 +995,15 @@ struct tula_muon_plan {
 namespace {
 
 // The list's shapes, and which one each matrix is of (-1: empty).
-bool shapes_of(const int64_t *rows, const int64_t *cols, int n, std::vector<Kin> &kin, std::vector<int> &which) {
+bool shapes_of(const int64_t *rows, const int64_t *cols, const std::vector<int> *vec, int n, std::vector<Kin> &kin, std::vector<int> &which) {
     which.assign((size_t)n, -1);
     for (int i = 0; i < n; ++i) {
         if (!good_shape(rows[i], cols[i])) return false;
         if (rows[i] == 0 || cols[i] == 0) continue;
+        const int v = vec ? (*vec)[(size_t)i] : 0;
         size_t k = 0;
-        while (k < kin.size() && (kin[k].rows != rows[i] || kin[k].cols != cols[i])) ++k;
-        if (k == kin.size()) kin.push_back(Kin{rows[i], cols[i], 0, 0, 0, 0, 0, 0});
+        while (k < kin.size() && (kin[k].rows != rows[i] || kin[k].cols != cols[i] || kin[k].vec != v)) ++k;
+        if (k == kin.size()) kin.push_back(Kin{rows[i], cols[i], 0, 0, v, 0.f, 0, 0, 0, 0});
         ++kin[k].count;
         which[i] = (int)k;
     }
@@ -884,7 +1011,10 @@ bool shapes_of(const int64_t *rows, const int64_t *cols, int n, std::vector<Kin>
     std::vector<int> order(kin.size()), where(kin.size());
     for (size_t k = 0; k < kin.size(); ++k) order[k] = (int)k;
     std::stable_sort(order.begin(), order.end(),
-                     [&](int a, int b) { return std::max(kin[a].rows, kin[a].cols) > std::max(kin[b].rows, kin[b].cols); });
+                     [&](int a, int b) {
+                         if (kin[a].vec != kin[b].vec) return kin[a].vec > kin[b].vec;
+                         return std::max(kin[a].rows, kin[a].cols) > std::max(kin[b].rows, kin[b].cols);
+                     });
     std::vector<Kin> sorted;
     int first = 0;
     for (size_t k = 0; k < order.size(); ++k) {
@@ -923,7 +1053,7 @@ int tula_muon_workspace_size(const int64_t *rows, const int64_t *cols, int n_mat
         std::vector<Kin> kin;
         std::vector<int> which;
         Sizes z;
-        if (!shapes_of(rows, cols, n_matrices, kin, which) || !sizes_of(kin, z)) return TULA_ERR_ARG;
+        if (!shapes_of(rows, cols, nullptr, n_matrices, kin, which) || !sizes_of(kin, z)) return TULA_ERR_ARG;
         *bytes = std::max<size_t>(z.all, 256);
     } catch (const std::bad_alloc &) {
         return TULA_ERR_NO_MEMORY;
@@ -941,13 +1071,12 @@ int tula_muon_plan_create(const tula_muon_matrices *m, void *workspace, size_t w
         std::unique_ptr<tula_muon_plan> plan(new tula_muon_plan);
         std::vector<int> which;
         Sizes z;
-        if (!shapes_of(m->rows, m->cols, n, plan->kin, which) || !sizes_of(plan->kin, z)) return TULA_ERR_ARG;
-        std::vector<int> next(plan->kin.size(), 0);
-        std::vector<Matrix> table(z.table / sizeof(Matrix));
+        std::vector<Matrix> of((size_t)n);
+        std::vector<int> vec((size_t)n);
         for (int i = 0; i < n; ++i) {
-            if (which[i] < 0) continue;
-            const Kin &k = plan->kin[which[i]];
-            Matrix &q = table[(size_t)(k.matrix + next[which[i]]++)];
+            if (!good_shape(m->rows[i], m->cols[i])) return TULA_ERR_ARG;
+            if (m->rows[i] == 0 || m->cols[i] == 0) continue;
+            Matrix &q = of[(size_t)i];
             q = {};
             q.g = m->grad_ptrs[i];
             q.m = m->momentum_ptrs[i];
@@ -959,8 +1088,13 @@ int tula_muon_plan_create(const tula_muon_matrices *m, void *workspace, size_t w
                 (m->copy_ptrs && !q.copy) || !aligned(q.g, type_size(q.gtype)) || !aligned(q.m, 4) || !aligned(q.w, 4) ||
                 !aligned(q.copy, 2))
                 return TULA_ERR_ARG;
-            q.vec = k.cols % 8 == 0 && aligned(q.g, 16) && aligned(q.m, 16) && aligned(q.w, 16) && aligned(q.copy, 16);
+            q.vec = vec[(size_t)i] = m->cols[i] % 8 == 0 && aligned(q.g, 16) && aligned(q.m, 16) && aligned(q.w, 32) && aligned(q.copy, 16);
         }
+        if (!shapes_of(m->rows, m->cols, &vec, n, plan->kin, which) || !sizes_of(plan->kin, z)) return TULA_ERR_ARG;
+        std::vector<int> next(plan->kin.size(), 0);
+        std::vector<Matrix> table(z.table / sizeof(Matrix));
+        for (int i = 0; i < n; ++i)
+            if (which[i] >= 0) table[(size_t)(plan->kin[which[i]].matrix + next[which[i]]++)] = of[(size_t)i];
         if (!workspace || !aligned(workspace, 256) || workspace_bytes < std::max<size_t>(z.all, 256)) return TULA_ERR_WORKSPACE;
         unsigned char *at = static_cast<unsigned char *>(workspace);
         plan->n_tiles = z.n_tiles;
@@ -1017,11 +1151,12 @@ int tula_muon_step(tula_muon_plan *plan, const tula_muon_hparams *hp, void *stre
     long long done = 0;
     for (int i = 0; i < n; i += kMostGroups) {
         const int here = std::min(kMostGroups, n - i);
-        const Kin *kin = plan->kin.data() + i;
+        Kin kin[kMostGroups];
         for (int k = 0; k < here; ++k) {
+            kin[k] = plan->kin[(size_t)(i + k)];
             const double r = (double)kin[k].rows, c = (double)kin[k].cols;
             const double factor = hp->scale == TULA_MUON_SCALE_RMS ? 0.2 * std::sqrt(std::max(r, c)) : std::sqrt(std::max(1.0, r / c));
-            st.g[k].step = (float)(hp->lr * factor);
+            kin[k].step = (float)(hp->lr * factor);
         }
         st.parts = plan->parts + done;
         done += stream_tiles(kin, here);
@@ -1036,7 +1171,7 @@ int tula_orthogonalize_workspace_size(int64_t batch, int64_t rows, int64_t cols,
     *bytes = 256;
     if (batch == 0 || rows == 0 || cols == 0) return TULA_OK;
     try {
-        std::vector<Kin> kin{Kin{rows, cols, (int)batch, 0, 0, 0, 0, 0}};
+        std::vector<Kin> kin{Kin{rows, cols, (int)batch, 0, 0, 0.f, 0, 0, 0, 0}};
         Sizes z;
         if (!sizes_of(kin, z)) return TULA_ERR_ARG;
         *bytes = z.parts + (size_t)z.n_tiles * kTileBytes;
@@ -1058,7 +1193,7 @@ int tula_orthogonalize(const void *x, int type, int64_t batch, int64_t rows, int
     if (!x || !out || !aligned(x, type_size(type)) || !aligned(out, 2)) return TULA_ERR_ARG;
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < need) return TULA_ERR_WORKSPACE;
     try {
-        std::vector<Kin> kin{Kin{rows, cols, (int)batch, 0, 0, 0, 0, 0}};
+        std::vector<Kin> kin{Kin{rows, cols, (int)batch, 0, 0, 0.f, 0, 0, 0, 0}};
         Sizes z;
         if (!sizes_of(kin, z)) return TULA_ERR_ARG;
         StreamArgs st = {};
@@ -1074,6 +1209,7 @@ int tula_orthogonalize(const void *x, int type, int64_t batch, int64_t rows, int
         const size_t size = type_size(type), of16 = 16 / size;
         st.vec = cols % 8 == 0 && aligned(x, 16) && aligned(out, 16) && (rows == 1 || stride % of16 == 0) &&
                  (batch == 1 || batch_stride % of16 == 0);
+        kin[0].vec = st.vec;
         Maps maps;
         if (!make_maps(maps, st.tiles, z.n_tiles)) return cuda_failed(cudaErrorInvalidValue);
         return run(maps, z.n_tiles, kin.data(), 1, st, ns_steps, static_cast<cudaStream_t>(stream));
