@@ -10,6 +10,7 @@
 //   k_product      A = X X^T;  B = a I + b A + c A^2;  X' = B X: three launches a step.  The last one writes
 //                  the weights and their copies, or the values themselves
 //   k_muon_last    does that for matrices whose rows do not lie on 32-byte boundaries
+//   k_muon_small   all of it for matrices that a CTA's shared memory holds
 //
 // One launch covers all matrices of a list.  The products are nearly all of the work: per step 2 n^2 m and
 // 2 n^3 operations of which symmetry leaves half, and 2 n^2 m.  They run on the tensor cores from fp16
@@ -107,9 +108,9 @@ struct Shape {
 };
 // Shared-memory matrix descriptors of an operand (bit 46: their version; the 128-byte swizzle).  Along: rows of
 // 64 elements of the sum, groups of eight 1024 bytes apart.  Else: rows of 64 of the side, one for each element
-// of the sum, groups of eight 1024 bytes apart, the next 64 of the side 8192 bytes on.
-__device__ __forceinline__ uint64_t operand_desc(uint32_t addr, bool along) {
-    return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(along ? 1 : 8192 >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
+// of the sum, groups of eight 1024 bytes apart, the next 64 of the side `next` bytes on.
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr, bool along, unsigned next = 8192) {
+    return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(along ? 1 : next >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
            (uint64_t)2 << 61;
 }
 // fp16 operands, fp32 sums.
@@ -701,6 +702,13 @@ __global__ void __launch_bounds__(kStreamThreads, kStreamCtas) k_muon_first(cons
 // zeros stays, one with an infinity or NaN becomes NaN.  The norm is taken by every CTA for itself: one of
 // its warps fetches the matrix's parts from L2 while the tile is on its way, one thread ends in fp64 (an SM does
 // some two of its operations a cycle: by all threads they took a third of the kernel's time).
+__device__ __forceinline__ float2 factors_of(double squares, float scale) {
+    const double norm = sqrt(squares);
+    if (!(norm < 1e300)) return make_float2(__uint_as_float(0x7fffffffu), __uint_as_float(0x7fffffffu));
+    if (!(norm > 0.0)) return make_float2(0.f, 0.f);
+    const int k = max(-126, min(126, (int)((unsigned)__double2hiint(norm) >> 20) - 1023));
+    return make_float2(__uint_as_float((unsigned)(127 - k) << 23), (float)((double)scale / norm * __hiloint2double((1023 + k) << 20, 0)));
+}
 __device__ __forceinline__ float2 norm_factors(const StreamArgs &a, const Place &p, float2 *factors) {
     if (threadIdx.x < 32) {
         const double *parts = a.parts + p.g->first + p.matrix * p.g->per;
@@ -718,22 +726,25 @@ __device__ __forceinline__ float2 norm_factors(const StreamArgs &a, const Place 
         }
         for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
         if (threadIdx.x == 0) {
-            const double norm = sqrt(s);
-            float f1 = 0.f, f2 = 0.f;
-            if (!(norm < 1e300)) {
-                f1 = f2 = __uint_as_float(0x7fffffffu);
-            } else if (norm > 0.0) {
-                const int k = max(-126, min(126, (int)((unsigned)__double2hiint(norm) >> 20) - 1023));
-                f1 = __uint_as_float((unsigned)(127 - k) << 23);
-                f2 = (float)((double)p.g->scale / norm * __hiloint2double((1023 + k) << 20, 0));
-            }
-            *factors = make_float2(f1, f2);
+            *factors = factors_of(s, p.g->scale);
         }
     }
     __syncthreads();
     return *factors;
 }
 
+// Elements of X from k on.
+template <bool Vec>
+__device__ __forceinline__ Run<__half, Vec ? 8 : 1> scaled_run(const float (&u)[32], int k, const Place &p, float2 f) {
+    Run<__half, Vec ? 8 : 1> r;
+#pragma unroll
+    for (int e = 0; e < (Vec ? 8 : 1); ++e) {
+        // (a NaN factor leaves the zeros beyond the matrix alone)
+        const bool in = p.row0 + row_of<Vec>(k + e) < p.g->rows && p.col0 + col_of<Vec>(k + e) < p.g->cols;
+        r.v[e] = __float2half_rn(in ? __fmul_rn(__fmul_rn(u[k + e], f.x), f.y) : 0.f);
+    }
+    return r;
+}
 template <bool Vec>
 __device__ __forceinline__ void scale_tile(const StreamArgs &a, const Place &p, const Matrix &q, float2 *factors) {
     float u[32];
@@ -742,16 +753,8 @@ __device__ __forceinline__ void scale_tile(const StreamArgs &a, const Place &p, 
     __half *x = reinterpret_cast<__half *>(a.tiles + (size_t)(p.g->x + p.matrix * p.g->per + p.tile) * kTileBytes);
     constexpr int kN = Vec ? 8 : 1;
 #pragma unroll
-    for (int k = 0; k < 32; k += kN) {
-        Run<__half, kN> r;
-#pragma unroll
-        for (int e = 0; e < kN; ++e) {
-            // (a NaN factor leaves the zeros beyond the matrix alone)
-            const bool in = p.row0 + row_of<Vec>(k + e) < p.g->rows && p.col0 + col_of<Vec>(k + e) < p.g->cols;
-            r.v[e] = __float2half_rn(in ? __fmul_rn(__fmul_rn(u[k + e], f.x), f.y) : 0.f);
-        }
-        *reinterpret_cast<Run<__half, kN> *>(x + row_of<Vec>(k) * kTileCols + col_of<Vec>(k)) = r;
-    }
+    for (int k = 0; k < 32; k += kN)
+        *reinterpret_cast<Run<__half, kN> *>(x + row_of<Vec>(k) * kTileCols + col_of<Vec>(k)) = scaled_run<Vec>(u, k, p, f);
 }
 __global__ void __launch_bounds__(kStreamThreads, kStreamCtas) k_muon_scale(const __grid_constant__ StreamArgs a) {
     __shared__ float2 factors;
@@ -767,17 +770,9 @@ __global__ void __launch_bounds__(kStreamThreads, kStreamCtas) k_muon_scale(cons
         scale_tile<false>(a, p, q, &factors);
 }
 
+// A tile of O(u) to the weights and their copies, or as it is.
 template <bool Vec>
-__device__ __forceinline__ void last_tile(const StreamArgs &a, const Place &p, const Matrix &q) {
-    float x[32];
-    const __half *from = reinterpret_cast<const __half *>(a.tiles + (size_t)(p.g->x_last + p.matrix * p.g->per + p.tile) * kTileBytes);
-    constexpr int kN = Vec ? 8 : 1;
-#pragma unroll
-    for (int k = 0; k < 32; k += kN) {
-        const Run<__half, kN> r = *reinterpret_cast<const Run<__half, kN> *>(from + row_of<Vec>(k) * kTileCols + col_of<Vec>(k));
-#pragma unroll
-        for (int e = 0; e < kN; ++e) x[k + e] = __half2float(r.v[e]);
-    }
+__device__ __forceinline__ void finish_tile(const StreamArgs &a, const Place &p, const Matrix &q, const float (&x)[32]) {
     if (!a.matrices) {
         const size_t at = (size_t)p.matrix * p.g->rows * p.g->cols * 2;
         store_typed<Vec>(static_cast<unsigned char *>(a.y) + at, a.ytype, p.g->cols, p, x);
@@ -790,6 +785,19 @@ __device__ __forceinline__ void last_tile(const StreamArgs &a, const Place &p, c
     store_tile<float, Vec>(q.w, p.g->cols, p, w);
     if (q.copy) store_typed<Vec>(q.copy, q.ctype, p.g->cols, p, w);
 }
+template <bool Vec>
+__device__ __forceinline__ void last_tile(const StreamArgs &a, const Place &p, const Matrix &q) {
+    float x[32];
+    const __half *from = reinterpret_cast<const __half *>(a.tiles + (size_t)(p.g->x_last + p.matrix * p.g->per + p.tile) * kTileBytes);
+    constexpr int kN = Vec ? 8 : 1;
+#pragma unroll
+    for (int k = 0; k < 32; k += kN) {
+        const Run<__half, kN> r = *reinterpret_cast<const Run<__half, kN> *>(from + row_of<Vec>(k) * kTileCols + col_of<Vec>(k));
+#pragma unroll
+        for (int e = 0; e < kN; ++e) x[k + e] = __half2float(r.v[e]);
+    }
+    finish_tile<Vec>(a, p, q, x);
+}
 __global__ void __launch_bounds__(kStreamThreads, kStreamCtas) k_muon_last(const __grid_constant__ StreamArgs a) {
     let_next_start();
     wait_for_previous();
@@ -801,6 +809,271 @@ __global__ void __launch_bounds__(kStreamThreads, kStreamCtas) k_muon_last(const
         last_tile<true>(a, p, q);
     else
         last_tile<false>(a, p, q);
+}
+
+// ----------------------------------------------------------------------------
+// Small matrices
+// ----------------------------------------------------------------------------
+//
+// One CTA a matrix whose smaller side is at most 128 and whose tiles, at most twelve, shared memory holds beside
+// those of A, which B takes the place of.  Nothing leaves the SM between the first reading and the last
+// writing: one launch and some 4 us a step instead of three launches and 18 (64 x 576: SMALLUS us in all, 105 by
+// the products above).  The tiles have the image that the copies give them there.  One thread issues a
+// product, all eight warps read it back.
+
+constexpr int kSmallTiles = 12;
+constexpr int kSmallSmem = (kSmallTiles + 2) * kTileBytes + 1024;
+constexpr int kSmallSums = 512;  // columns of sums at a time: all of tensor memory
+
+// Where element (row, col) of a tile in shared memory lies, in bytes.
+__device__ __forceinline__ uint32_t small_place(int row, int col) { return row * 128 + (((col >> 3) ^ (row & 7)) << 4) + (col & 7) * 2; }
+
+struct Small {
+    uint32_t x, gram, bar;
+    volatile int *dead;
+    uint32_t tmem;
+    unsigned parity;
+
+    // What the threads have written to shared memory, and read of tensor memory, comes before the next product.
+    __device__ __forceinline__ void before() {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncthreads();
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    }
+    // (a wait that runs out leaves the sums as they are: the others end at once then)
+    __device__ __forceinline__ void after() {
+        mbar_wait(bar, parity, dead);
+        parity ^= 1;
+        __syncwarp();
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    }
+};
+
+template <bool Vec>
+__device__ __forceinline__ void small_load(const StreamArgs &a, Place p, const Matrix &q, int tiles, unsigned char *x, double *sums,
+                                           float2 *factors) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, pitch = p.g->pitch;
+    double total = 0.0;  // lane 0 of a warp
+    for (int t = 0; t < tiles; ++t) {
+        p.row0 = t / pitch * kTile, p.col0 = t % pitch * kTileCols;
+        float u[32];
+        load_update<true, Vec>(u, a, p, q);
+        warp_squares(u, sums);
+        if (lane == 0) total += sums[warp];
+    }
+    if (lane == 0) sums[warp] = total;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double s = 0.0;
+        for (int k = 0; k < kStreamThreads / 32; ++k) s += sums[k];
+        *factors = factors_of(s, p.g->scale);
+    }
+    __syncthreads();
+    const float2 f = *factors;
+    constexpr int kN = Vec ? 8 : 1;
+    for (int t = 0; t < tiles; ++t) {
+        p.row0 = t / pitch * kTile, p.col0 = t % pitch * kTileCols;
+        float u[32];
+        load_update<false, Vec>(u, a, p, q);
+#pragma unroll
+        for (int k = 0; k < 32; k += kN) {
+            const Run<__half, kN> r = scaled_run<Vec>(u, k, p, f);
+            *reinterpret_cast<Run<__half, kN> *>(x + t * kTileBytes + small_place(row_of<Vec>(k), col_of<Vec>(k))) = r;
+        }
+    }
+}
+template <bool Vec>
+__device__ __forceinline__ void small_store(const StreamArgs &a, Place p, const Matrix &q, int tiles, const unsigned char *x) {
+    const int pitch = p.g->pitch;
+    for (int t = 0; t < tiles; ++t) {
+        p.row0 = t / pitch * kTile, p.col0 = t % pitch * kTileCols;
+        float f[32];
+        constexpr int kN = Vec ? 8 : 1;
+#pragma unroll
+        for (int k = 0; k < 32; k += kN) {
+            const Run<__half, kN> r =
+                *reinterpret_cast<const Run<__half, kN> *>(x + t * kTileBytes + small_place(row_of<Vec>(k), col_of<Vec>(k)));
+#pragma unroll
+            for (int e = 0; e < kN; ++e) f[k + e] = __half2float(r.v[e]);
+        }
+        finish_tile<Vec>(a, p, q, f);
+    }
+}
+
+// 64 columns of sums of a warp's 32 rows.
+__device__ __forceinline__ void small_sums(float (&f)[64], uint32_t tmem) {
+    unsigned v[64];
+    tmem_load32(v, tmem);
+    tmem_load32(v + 32, tmem + 32);
+    tmem_wait(v);
+#pragma unroll
+    for (int k = 0; k < 64; ++k) f[k] = __uint_as_float(v[k]);
+}
+// A row of a tile, as fp16.
+__device__ __forceinline__ void small_put(uint32_t tile, int row, const float (&f)[64]) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        unsigned y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const __half2 h = __floats2half2_rn(f[8 * k + 2 * e], f[8 * k + 2 * e + 1]);
+            memcpy(&y[e], &h, 4);
+        }
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(tile + small_place(row, 8 * k)), "r"(y[0]), "r"(y[1]), "r"(y[2]),
+                     "r"(y[3])
+                     : "memory");
+    }
+}
+
+__global__ void __launch_bounds__(kStreamThreads, 1) k_muon_small(const __grid_constant__ StreamArgs a, int steps) {
+    extern __shared__ __align__(16) unsigned char raw[];
+    __shared__ __align__(8) unsigned long long bar;
+    __shared__ double sums[kStreamThreads / 32];
+    __shared__ float2 factors;
+    __shared__ uint32_t tmem_at;
+    __shared__ volatile int dead;
+    unsigned char *x = raw + (-smem_addr(raw) & 1023u);
+    const int lane = threadIdx.x & 31, warp = __shfl_sync(kFull, threadIdx.x >> 5, 0);
+    if (threadIdx.x == 0) {
+        mbar_init(smem_addr(&bar), 1);
+        dead = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) tmem_alloc(smem_addr(&tmem_at), kSmallSums);
+    let_next_start();
+    wait_for_previous();
+    const Place p = place_of(a, blockIdx.x);  // (a group's tiles are its matrices here)
+    const int rows = p.g->rows, cols = p.g->cols, n = min(rows, cols), pitch = p.g->pitch;
+    const int tile_rows = (rows + kTile - 1) / kTile, tiles = tile_rows * pitch;
+    const bool wide = rows <= cols, go = !left_out(a);
+    Matrix q = {};
+    if (a.matrices) q = a.matrices[p.g->matrix + p.matrix];
+    const bool vec = a.matrices ? q.vec : a.vec;
+    Small m{smem_addr(x), smem_addr(x) + kSmallTiles * kTileBytes, smem_addr(&bar), &dead, 0, 0};
+    if (go) {
+        if (vec)
+            small_load<true>(a, p, q, tiles, x, sums, &factors);
+        else
+            small_load<false>(a, p, q, tiles, x, sums, &factors);
+    }
+    m.before();  // (and tensor memory is there)
+    m.tmem = __shfl_sync(kFull, tmem_at, 0);
+    const int quad = warp & 3, half = warp >> 2, row = quad * 32 + lane;
+    const uint32_t lanes = m.tmem + ((unsigned)(quad * 32) << 16);
+    const int sides = n > 64 ? 2 : 1;        // tiles to a row of A's
+    const int parts = (n + 15) / 16;         // of a sum over the smaller side, an instruction each
+    float scale = p.g->scale;
+    for (int step = 0; go && step < steps; ++step) {
+        // A = X X^T along X's tiles, or X^T X along their rows.  (There a tile beyond the last column may be read
+        // as the rows beyond A's: they are not kept.)
+        if (warp == 0) {
+            if (elect_one()) {
+                const uint32_t idesc = product_desc(128, 64 * sides, wide, wide);
+                if (wide) {
+                    for (int t = 0; t < pitch; ++t)
+                        for (int j = 0; j < 4; ++j) {
+                            const uint64_t d = operand_desc(m.x + t * kTileBytes, true) + 2 * j;
+                            mma16<false>(m.tmem, d, d, idesc, t > 0 || j > 0);
+                        }
+                } else {
+                    for (int t = 0; t < tile_rows; ++t)
+                        for (int j = 0; j < 8; ++j) {
+                            const uint64_t d = operand_desc(m.x + t * pitch * kTileBytes, false, kTileBytes) + 128 * j;
+                            mma16<false>(m.tmem, d, d, idesc, t > 0 || j > 0);
+                        }
+                }
+                commit(m.bar);
+            }
+            __syncwarp();
+        }
+        m.after();
+        float f[64];
+        if (half < sides) {
+            const float alpha = 1.f / (scale * scale);
+            small_sums(f, lanes + 64 * half);
+#pragma unroll
+            for (int k = 0; k < 64; ++k) f[k] = row < n && 64 * half + k < n ? f[k] * alpha : 0.f;
+            small_put(m.gram + half * kTileBytes, row, f);
+        }
+        m.before();
+        // B = a I + b A + c A^2, in A's place
+        if (warp == 0) {
+            if (elect_one()) {
+                const uint32_t idesc = product_desc(128, 64 * sides, true, true);
+                for (int j = 0; j < parts; ++j) {
+                    const uint64_t d = operand_desc(m.gram + (j >> 2) * kTileBytes, true) + 2 * (j & 3);
+                    mma16<false>(m.tmem, d, d, idesc, j > 0);
+                }
+                commit(m.bar);
+            }
+            __syncwarp();
+        }
+        m.after();
+        if (half < sides) {
+            small_sums(f, lanes + 64 * half);
+            const int diagonal = row < n ? row - 64 * half : -1;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                unsigned y[4];
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                             : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3])
+                             : "r"(m.gram + half * kTileBytes + small_place(row, 8 * k))
+                             : "memory");
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    __half2 h;
+                    memcpy(&h, &y[e >> 1], 4);
+                    const float g = __half2float(e & 1 ? __high2half(h) : __low2half(h));
+                    f[8 * k + e] = fmaf((float)kC, f[8 * k + e], fmaf((float)kB, g, diagonal == 8 * k + e ? (float)kA : 0.f));
+                }
+            }
+            small_put(m.gram + half * kTileBytes, row, f);
+        }
+        // X' = B X by columns of tiles, or X B by rows of them, in X's place
+        const int at_once = kSmallSums / 64;
+        for (int t0 = 0; t0 < tiles; t0 += at_once) {
+            const int t1 = min(tiles, t0 + at_once);
+            m.before();
+            if (warp == 0) {
+                if (elect_one()) {
+                    if (wide) {
+                        for (int t = t0; t < t1; t += 4) {
+                            const uint32_t idesc = product_desc(128, 64 * min(4, t1 - t), true, false);
+                            for (int j = 0; j < parts; ++j)
+                                mma16<false>(m.tmem + (t - t0) * 64, operand_desc(m.gram + (j >> 2) * kTileBytes, true) + 2 * (j & 3),
+                                             operand_desc(m.x + t * kTileBytes, false, kTileBytes) + 128 * j, idesc, j > 0);
+                        }
+                    } else {
+                        const uint32_t idesc = product_desc(128, 64 * sides, true, true);
+                        for (int t = t0; t < t1; t += sides)
+                            for (int j = 0; j < parts; ++j)
+                                mma16<false>(m.tmem + (t - t0) * 64, operand_desc(m.x + (t + (j >> 2)) * kTileBytes, true) + 2 * (j & 3),
+                                             operand_desc(m.gram + (j >> 2) * kTileBytes, true) + 2 * (j & 3), idesc, j > 0);
+                    }
+                    commit(m.bar);
+                }
+                __syncwarp();
+            }
+            m.after();
+            const float alpha = 1.f / scale;
+            for (int t = t0 + half; t < t1; t += 2) {
+                small_sums(f, lanes + 64 * (t - t0));
+#pragma unroll
+                for (int k = 0; k < 64; ++k) f[k] *= alpha;
+                small_put(m.x + t * kTileBytes, row, f);
+            }
+        }
+        scale = 1.f;
+        m.before();
+    }
+    if (go) {
+        if (vec)
+            small_store<true>(a, p, q, tiles, x);
+        else
+            small_store<false>(a, p, q, tiles, x);
+    }
+    if (warp == 0) tmem_free(m.tmem, kSmallSums);
 }
 
 // ----------------------------------------------------------------------------
@@ -817,6 +1090,7 @@ struct Kin {
     int tile_rows() const { return (int)up(rows, kTile); }
     int tile_cols() const { return (int)up(cols, kTileCols); }
     int tiles() const { return tile_rows() * tile_cols(); }
+    bool small() const { return std::min(rows, cols) <= 128 && up(rows, kTile) * up(cols, kTileCols) <= kSmallTiles; }
     bool wide() const { return rows <= cols; }
     long long n() const { return std::min(rows, cols); }
     int gram_rows() const { return (int)up(n(), kTile); }
@@ -832,6 +1106,7 @@ bool good_shape(long long rows, long long cols) { return rows >= 0 && cols >= 0 
 long long place(std::vector<Kin> &kin) {
     long long at = 0;
     for (Kin &k : kin) {
+        if (k.small()) continue;
         const long long x = (long long)k.tile_rows() * k.tile_cols() * k.count, a = (long long)k.gram_rows() * k.gram_cols() * k.count;
         if (at + 2 * x + 2 * a >= kMostTiles) return -1;
         k.x0 = (int)at;
@@ -844,7 +1119,8 @@ long long place(std::vector<Kin> &kin) {
 }
 long long stream_tiles(const Kin *kin, int n) {
     long long t = 0;
-    for (int i = 0; i < n; ++i) t += (long long)kin[i].tiles() * kin[i].count;
+    for (int i = 0; i < n; ++i)
+        if (!kin[i].small()) t += (long long)kin[i].tiles() * kin[i].count;
     return t;
 }
 
@@ -932,8 +1208,40 @@ int product(const Maps &maps, ProductArgs &a, const Kin *kin, int n, int x, bool
     return launch_product<false, K>(maps, a, sms, s);
 }
 
-// All of it for shapes whose tiles are placed, those with Kin::vec first.  `st`: its groups are filled here.
+// Small matrices.
+int run_small(const Kin *kin, int n, StreamArgs &st, int steps, cudaStream_t s) {
+    long long count = 0;
+    st.n_groups = n;
+    for (int i = 0; i < n; ++i) {
+        const Kin &k = kin[i];
+        Group &g = st.g[i];
+        g = {};
+        g.first = (int)count;
+        g.per = 1;
+        g.matrix = k.matrix;
+        g.rows = (int)k.rows;
+        g.cols = (int)k.cols;
+        g.pitch = k.tile_cols();
+        g.scale = steps ? (float)std::ldexp(1.0, k.shift()) : 1.f;
+        g.step = k.step;
+        count += k.count;
+    }
+    static std::atomic<uint64_t> done;
+    const int rc = allow_smem((const void *)k_muon_small, kSmallSmem, &done);
+    if (rc) return rc;
+    return tula::launch(k_muon_small, dim3((unsigned)count), kStreamThreads, kSmallSmem, s, 1, st, steps);
+}
+
+// All of it for shapes whose tiles are placed, those with Kin::vec first and small ones last.  `st`: its groups are
+// filled here.
 int run(const Maps &maps, long long n_tiles, const Kin *kin, int n, StreamArgs &st, int steps, cudaStream_t s) {
+    int large = 0;
+    while (large < n && !kin[large].small()) ++large;
+    if (large < n) {
+        const int rc = run_small(kin + large, n - large, st, steps, s);
+        if (rc) return rc;
+        n = large;
+    }
     const int sms = std::max(1, sm_count());
     ProductArgs a;
     a.tiles = st.tiles;
@@ -1007,11 +1315,12 @@ bool shapes_of(const int64_t *rows, const int64_t *cols, const std::vector<int> 
         ++kin[k].count;
         which[i] = (int)k;
     }
-    // the longest sums first, so that the last blocks to be taken are short ones
+    // small ones last, and the longest sums first, so that the last blocks to be taken are short ones
     std::vector<int> order(kin.size()), where(kin.size());
     for (size_t k = 0; k < kin.size(); ++k) order[k] = (int)k;
     std::stable_sort(order.begin(), order.end(),
                      [&](int a, int b) {
+                         if (kin[a].small() != kin[b].small()) return kin[b].small();
                          if (kin[a].vec != kin[b].vec) return kin[a].vec > kin[b].vec;
                          return std::max(kin[a].rows, kin[a].cols) > std::max(kin[b].rows, kin[b].cols);
                      });
@@ -1102,12 +1411,12 @@ int tula_muon_plan_create(const tula_muon_matrices *m, void *workspace, size_t w
         plan->parts = reinterpret_cast<double *>(at + z.table);
         plan->tiles = at + z.table + z.parts;
         std::memset(&plan->maps, 0, sizeof(plan->maps));
-        if (z.n_tiles) {
+        if (z.table) {
             cudaStream_t s = static_cast<cudaStream_t>(stream);
             cudaError_t e = cudaMemcpyAsync(at, table.data(), table.size() * sizeof(Matrix), cudaMemcpyHostToDevice, s);
             if (e == cudaSuccess) e = cudaStreamSynchronize(s);
             if (e != cudaSuccess) return cuda_failed(e);
-            if (!make_maps(plan->maps, plan->tiles, z.n_tiles)) return cuda_failed(cudaErrorInvalidValue);
+            if (z.n_tiles && !make_maps(plan->maps, plan->tiles, z.n_tiles)) return cuda_failed(cudaErrorInvalidValue);
         }
         *plan_out = plan.release();
     } catch (const std::bad_alloc &) {
@@ -1174,7 +1483,7 @@ int tula_orthogonalize_workspace_size(int64_t batch, int64_t rows, int64_t cols,
         std::vector<Kin> kin{Kin{rows, cols, (int)batch, 0, 0, 0.f, 0, 0, 0, 0}};
         Sizes z;
         if (!sizes_of(kin, z)) return TULA_ERR_ARG;
-        *bytes = z.parts + (size_t)z.n_tiles * kTileBytes;
+        *bytes = std::max<size_t>(z.parts + (size_t)z.n_tiles * kTileBytes, 256);
     } catch (const std::bad_alloc &) {
         return TULA_ERR_NO_MEMORY;
     }
@@ -1211,7 +1520,8 @@ int tula_orthogonalize(const void *x, int type, int64_t batch, int64_t rows, int
                  (batch == 1 || batch_stride % of16 == 0);
         kin[0].vec = st.vec;
         Maps maps;
-        if (!make_maps(maps, st.tiles, z.n_tiles)) return cuda_failed(cudaErrorInvalidValue);
+        std::memset(&maps, 0, sizeof(maps));
+        if (z.n_tiles && !make_maps(maps, st.tiles, z.n_tiles)) return cuda_failed(cudaErrorInvalidValue);
         return run(maps, z.n_tiles, kin.data(), 1, st, ns_steps, static_cast<cudaStream_t>(stream));
     } catch (const std::bad_alloc &) {
         return TULA_ERR_NO_MEMORY;

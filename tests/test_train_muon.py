@@ -74,10 +74,12 @@ def _size(rows, cols):
 
 
 def test_workspace_sizes():
-    # tiles of 128 x 64 elements, twice each of X and of the two products of its smaller side; parts of
-    # a norm and rows of a table by whole 256 bytes
+    # tiles of 128 x 64 elements, twice each of X and of the two products of its smaller side (none of what a
+    # CTA holds); parts of a norm and rows of a table by whole 256 bytes
     def of(r, c):
         n = min(r, c)
+        if n <= 128 and -(-r // 128) * -(-c // 64) <= 12:
+            return 0, 0
         x, a = -(-r // 128) * -(-c // 64), -(-n // 128) * -(-n // 64)
         return x, 2 * (x + a) * 16384
 
@@ -85,7 +87,7 @@ def test_workspace_sizes():
         full = [s for s in shapes if s[0]]
         tiles = sum(of(*s)[0] for s in full)
         want = -(-48 * len(full) // 256) * 256 + -(-8 * tiles // 256) * 256 + sum(of(*s)[1] for s in full)
-        assert _size(*zip(*shapes)) == (0, want)
+        assert _size(*zip(*shapes)) == (0, max(want, 256))
     assert _size([0], [7])[0] == 0 and _size([-1], [7])[0] == -1 and _size([1 << 21], [1])[0] == -1
     assert _size([1 << 20], [1 << 20])[0] == -1  # beyond 256 GB
 
@@ -99,7 +101,8 @@ def test_refusals_of_the_library():
     for bad in ({"kind": 3}, {"okind": 0}, {"okind": 3}, {"batch": -1}, {"rows": -1}, {"cols": 1 << 21}, {"stride": 7}, {"apart": -1},
                 {"steps": -1}, {"steps": 101}, {"x": n}, {"out": n}, {"x": ctypes.c_void_p(258)}, {"out": ctypes.c_void_p(257)}):
         assert orth(**bad) == -1, bad
-    assert orth(space=n) == orth(size=1000) == orth(space=ctypes.c_void_p(128)) == -2
+    assert orth(space=n) == orth(size=255) == orth(space=ctypes.c_void_p(128)) == -2
+    assert orth(rows=300, cols=300, stride=300, size=1000) == -2
     assert orth(batch=0, x=n) == orth(rows=0, x=n) == 0
     assert L.tula_orthogonalize_workspace_size(1, 4, 4, n) == -1
 
@@ -123,7 +126,7 @@ def test_refusals_of_the_library():
     for bad in ({"rows": -1}, {"cols": 1 << 21}, {"g": 0}, {"w": 0}, {"m": 0}, {"c": 0}, {"gt": 3}, {"ct": 0}, {"g": 258}, {"w": 258},
                 {"m": 258}, {"c": 257}):
         assert create(**bad) == -1, bad
-    assert create(size=1000) == create(space=n) == create(space=ctypes.c_void_p(128)) == -2
+    assert create(size=255) == create(rows=300, cols=300, size=1000) == create(space=n) == create(space=ctypes.c_void_p(128)) == -2
     assert not plan and L.tula_muon_plan_destroy(n) == 0 and L.tula_muon_error(n, n) == -1
     # an empty list wants no GPU: its plan refuses hyperparameters that are out of range
     assert create(rows=0) == 0 and plan
@@ -157,7 +160,8 @@ def test_refusals_of_the_binding():
 
 SHAPES = [(1, 1, 1), (1, 1, 40), (2, 50, 1), (3, 2, 3), (1, 64, 64), (2, 65, 63), (1, 64, 576), (1, 576, 64), (3, 127, 129), (2, 128, 128),
           (1, 128, 256), (2, 129, 130), (5, 200, 333), (2, 333, 200), (1, 257, 640), (1, 1000, 257), (1, 1025, 1030), (2, 700, 2051),
-          (1, 2051, 300), (9, 512, 512)]
+          (1, 2051, 300), (9, 512, 512), (2, 128, 768), (2, 128, 769), (1, 65, 700), (1, 64, 512), (2, 1536, 64), (1, 1537, 64),
+          (2, 768, 128), (1, 769, 128), (3, 1100, 50), (400, 90, 200), (300, 200, 30)]
 
 
 @pytest.mark.gpu
