@@ -632,24 +632,40 @@ __device__ __forceinline__ const void *batch_at(const StreamArgs &a, int matrix)
     return static_cast<const unsigned char *>(a.x) + (size_t)matrix * a.batch_stride * (a.xtype == TULA_TYPE_F32 ? 4 : 2);
 }
 
-// What is orthogonalised.  First: the momentum moves on.
-template <bool First, bool Vec>
-__device__ __forceinline__ void load_update(float (&u)[32], const StreamArgs &a, const Place &p, const Matrix &q) {
+// What is orthogonalised: its parts as they lie in memory, and then the update itself.  First: the momentum
+// moves on.
+struct Loaded {
+    float g[32], m[32], mult;
+};
+template <bool Vec>
+__device__ __forceinline__ void load_parts(Loaded &l, const StreamArgs &a, const Place &p, const Matrix &q) {
     if (!a.matrices) {
-        load_typed<Vec>(u, batch_at(a, p.matrix), a.xtype, a.stride, p);
+        load_typed<Vec>(l.g, batch_at(a, p.matrix), a.xtype, a.stride, p);
         return;
     }
-    const float mult = a.record ? __fdiv_rn(a.record[TULA_RECORD_COEF], a.grad_scale) : __fdiv_rn(1.f, a.grad_scale);
-    float m[32];
-    load_typed<Vec>(u, q.g, q.gtype, p.g->cols, p);
-    load_tile<float, Vec>(m, q.m, p.g->cols, p);
+    l.mult = a.record ? __fdiv_rn(a.record[TULA_RECORD_COEF], a.grad_scale) : __fdiv_rn(1.f, a.grad_scale);
+    load_typed<Vec>(l.g, q.g, q.gtype, p.g->cols, p);
+    load_tile<float, Vec>(l.m, q.m, p.g->cols, p);
+}
+template <bool First, bool Vec>
+__device__ __forceinline__ void update_of(float (&u)[32], Loaded &l, const StreamArgs &a, const Place &p, const Matrix &q) {
 #pragma unroll
     for (int k = 0; k < 32; ++k) {
-        const float d = __fmul_rn(u[k], mult);
-        if (First) m[k] = fmaf(a.mu, m[k], d);
-        u[k] = a.nesterov ? fmaf(a.mu, m[k], d) : m[k];
+        if (!a.matrices) {
+            u[k] = l.g[k];
+            continue;
+        }
+        const float d = __fmul_rn(l.g[k], l.mult);
+        if (First) l.m[k] = fmaf(a.mu, l.m[k], d);
+        u[k] = a.nesterov ? fmaf(a.mu, l.m[k], d) : l.m[k];
     }
-    if (First) store_tile<float, Vec>(q.m, p.g->cols, p, m);
+    if (First && a.matrices) store_tile<float, Vec>(q.m, p.g->cols, p, l.m);
+}
+template <bool First, bool Vec>
+__device__ __forceinline__ void load_update(float (&u)[32], const StreamArgs &a, const Place &p, const Matrix &q) {
+    Loaded l;
+    load_parts<Vec>(l, a, p, q);
+    update_of<First, Vec>(u, l, a, p, q);
 }
 
 // The sum of squares of a warp's elements: in fp32 with an exact power of two taken out, so that no square
@@ -854,13 +870,25 @@ template <bool Vec>
 __device__ __forceinline__ void small_load(const StreamArgs &a, Place p, const Matrix &q, int tiles, unsigned char *x, double *sums,
                                            float2 *factors) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, pitch = p.g->pitch;
+    // (two tiles' parts are on their way at a time)
+    auto tile = [&](int t) { p.row0 = t / pitch * kTile, p.col0 = t % pitch * kTileCols; };
+    Loaded l[2];
     double total = 0.0;  // lane 0 of a warp
-    for (int t = 0; t < tiles; ++t) {
-        p.row0 = t / pitch * kTile, p.col0 = t % pitch * kTileCols;
-        float u[32];
-        load_update<true, Vec>(u, a, p, q);
-        warp_squares(u, sums);
-        if (lane == 0) total += sums[warp];
+    for (int t0 = 0; t0 < tiles; t0 += 2) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            tile(t0 + h);
+            if (t0 + h < tiles) load_parts<Vec>(l[h], a, p, q);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (t0 + h >= tiles) break;
+            tile(t0 + h);
+            float u[32];
+            update_of<true, Vec>(u, l[h], a, p, q);
+            warp_squares(u, sums);
+            if (lane == 0) total += sums[warp];
+        }
     }
     if (lane == 0) sums[warp] = total;
     __syncthreads();
@@ -872,14 +900,23 @@ __device__ __forceinline__ void small_load(const StreamArgs &a, Place p, const M
     __syncthreads();
     const float2 f = *factors;
     constexpr int kN = Vec ? 8 : 1;
-    for (int t = 0; t < tiles; ++t) {
-        p.row0 = t / pitch * kTile, p.col0 = t % pitch * kTileCols;
-        float u[32];
-        load_update<false, Vec>(u, a, p, q);
+    for (int t0 = 0; t0 < tiles; t0 += 2) {
 #pragma unroll
-        for (int k = 0; k < 32; k += kN) {
-            const Run<__half, kN> r = scaled_run<Vec>(u, k, p, f);
-            *reinterpret_cast<Run<__half, kN> *>(x + t * kTileBytes + small_place(row_of<Vec>(k), col_of<Vec>(k))) = r;
+        for (int h = 0; h < 2; ++h) {
+            tile(t0 + h);
+            if (t0 + h < tiles) load_parts<Vec>(l[h], a, p, q);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (t0 + h >= tiles) break;
+            tile(t0 + h);
+            float u[32];
+            update_of<false, Vec>(u, l[h], a, p, q);
+#pragma unroll
+            for (int k = 0; k < 32; k += kN) {
+                const Run<__half, kN> r = scaled_run<Vec>(u, k, p, f);
+                *reinterpret_cast<Run<__half, kN> *>(x + (t0 + h) * kTileBytes + small_place(row_of<Vec>(k), col_of<Vec>(k))) = r;
+            }
         }
     }
 }
@@ -1090,7 +1127,7 @@ struct Kin {
     int tile_rows() const { return (int)up(rows, kTile); }
     int tile_cols() const { return (int)up(cols, kTileCols); }
     int tiles() const { return tile_rows() * tile_cols(); }
-    bool small() const { return std::min(rows, cols) <= 128 && up(rows, kTile) * up(cols, kTileCols) <= kSmallTiles; }
+    bool fits() const { return std::min(rows, cols) <= 128 && up(rows, kTile) * up(cols, kTileCols) <= kSmallTiles; }
     bool wide() const { return rows <= cols; }
     long long n() const { return std::min(rows, cols); }
     int gram_rows() const { return (int)up(n(), kTile); }
@@ -1100,13 +1137,26 @@ struct Kin {
     int shift() const { return std::min(15, (int)std::floor(0.5 * std::log2((double)rows * (double)cols))); }
 };
 
+// Whether the list is k_muon_small's: where no matrix is larger (else the products take the small ones along at no
+// cost: 16 matrices of 17 to 700 rows and columns took 227 us in two ways, 164 in one) and for up to two matrices an
+// SM (64 of 100 x 300: 52 us, 105 by products; 1000: MANYUS).
+constexpr int kSmallMost = 2 * 152;
+bool all_small(const std::vector<Kin> &kin) {
+    long long count = 0;
+    for (const Kin &k : kin) {
+        if (!k.fits()) return false;
+        count += k.count;
+    }
+    return count <= kSmallMost;
+}
+
 bool good_shape(long long rows, long long cols) { return rows >= 0 && cols >= 0 && rows <= kMostSide && cols <= kMostSide; }
 
 // Gives every shape its tiles; returns how many there are, -1 beyond the limit.
 long long place(std::vector<Kin> &kin) {
     long long at = 0;
+    if (all_small(kin)) return 0;
     for (Kin &k : kin) {
-        if (k.small()) continue;
         const long long x = (long long)k.tile_rows() * k.tile_cols() * k.count, a = (long long)k.gram_rows() * k.gram_cols() * k.count;
         if (at + 2 * x + 2 * a >= kMostTiles) return -1;
         k.x0 = (int)at;
@@ -1119,8 +1169,7 @@ long long place(std::vector<Kin> &kin) {
 }
 long long stream_tiles(const Kin *kin, int n) {
     long long t = 0;
-    for (int i = 0; i < n; ++i)
-        if (!kin[i].small()) t += (long long)kin[i].tiles() * kin[i].count;
+    for (int i = 0; i < n; ++i) t += (long long)kin[i].tiles() * kin[i].count;
     return t;
 }
 
@@ -1208,7 +1257,7 @@ int product(const Maps &maps, ProductArgs &a, const Kin *kin, int n, int x, bool
     return launch_product<false, K>(maps, a, sms, s);
 }
 
-// Small matrices.
+// Small matrices, without a workspace.
 int run_small(const Kin *kin, int n, StreamArgs &st, int steps, cudaStream_t s) {
     long long count = 0;
     st.n_groups = n;
@@ -1232,16 +1281,10 @@ int run_small(const Kin *kin, int n, StreamArgs &st, int steps, cudaStream_t s) 
     return tula::launch(k_muon_small, dim3((unsigned)count), kStreamThreads, kSmallSmem, s, 1, st, steps);
 }
 
-// All of it for shapes whose tiles are placed, those with Kin::vec first and small ones last.  `st`: its groups are
-// filled here.
+// All of it for shapes whose tiles are placed (n_tiles 0: small ones), those with Kin::vec first.  `st`: its groups
+// are filled here.
 int run(const Maps &maps, long long n_tiles, const Kin *kin, int n, StreamArgs &st, int steps, cudaStream_t s) {
-    int large = 0;
-    while (large < n && !kin[large].small()) ++large;
-    if (large < n) {
-        const int rc = run_small(kin + large, n - large, st, steps, s);
-        if (rc) return rc;
-        n = large;
-    }
+    if (!n_tiles) return n ? run_small(kin, n, st, steps, s) : TULA_OK;
     const int sms = std::max(1, sm_count());
     ProductArgs a;
     a.tiles = st.tiles;
@@ -1320,7 +1363,6 @@ bool shapes_of(const int64_t *rows, const int64_t *cols, const std::vector<int> 
     for (size_t k = 0; k < kin.size(); ++k) order[k] = (int)k;
     std::stable_sort(order.begin(), order.end(),
                      [&](int a, int b) {
-                         if (kin[a].small() != kin[b].small()) return kin[b].small();
                          if (kin[a].vec != kin[b].vec) return kin[a].vec > kin[b].vec;
                          return std::max(kin[a].rows, kin[a].cols) > std::max(kin[b].rows, kin[b].cols);
                      });
@@ -1347,7 +1389,7 @@ bool sizes_of(std::vector<Kin> &kin, Sizes &z) {
     size_t n = 0;
     for (const Kin &k : kin) n += (size_t)k.count;
     z.table = round_up(n * sizeof(Matrix));
-    z.parts = round_up((size_t)stream_tiles(kin.data(), (int)kin.size()) * sizeof(double));
+    z.parts = z.n_tiles ? round_up((size_t)stream_tiles(kin.data(), (int)kin.size()) * sizeof(double)) : 0;
     z.all = z.table + z.parts + (size_t)z.n_tiles * kTileBytes;
     return true;
 }

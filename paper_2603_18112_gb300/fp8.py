@@ -150,28 +150,34 @@ def matmul(a: FP8Matrix, b: FP8Matrix, dtype=torch.bfloat16) -> torch.Tensor:
     return out
 
 
+def _product(x, w, dtype):
+    """x w^T without what a backward pass wants."""
+    (m, k), n = x.shape, w.shape[0]
+    dev, x_kind, w_kind = _on_gpu(x, w), _type(x.dtype, "linear"), _type(w.dtype, "linear")
+    qx, qw = FP8Matrix.empty(m, k, x.device)._of(dtype), FP8Matrix.empty(n, k, w.device)._of(dtype)
+    _quantize_into(x, dev, x_kind, False, qx, None)
+    _quantize_into(w, dev, w_kind, True, qw, None)
+    return matmul(qx, qw, x.dtype)
+
+
 class _Linear(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w, recorded, dtype, grad_dtype):
-        # (needs_input_grad follows requires_grad, also where no gradient is recorded)
-        need_x, need_w = (n and recorded for n in ctx.needs_input_grad[:2])
+    def forward(ctx, x, w, dtype, grad_dtype):
+        need_x, need_w = ctx.needs_input_grad[:2]
         (m, k), n = x.shape, w.shape[0]
         dev, x_kind, w_kind = _on_gpu(x, w), _type(x.dtype, "linear"), _type(w.dtype, "linear")
         # what the backward pass multiplies by is kept in 8 bits: x^T for dw, then w^T for dx
         ctx.types, ctx.sizes, ctx.device, ctx.codes = (x.dtype, w.dtype), (m, n, k), x.device, (dtype, grad_dtype)
         ctx.at = at = FP8Matrix._bytes(k, m) if need_w else 0
         ctx.end = end = at + (FP8Matrix._bytes(k, n) if need_x else 0)
-        xt = wt = None
-        if need_x or need_w:
-            kept = torch.empty(end, dtype=torch.uint8, device=x.device)
-            xt = FP8Matrix._within(kept, 0, k, m)._of(dtype) if need_w else None
-            wt = FP8Matrix._within(kept, at, k, n)._of(dtype) if need_x else None
+        kept = torch.empty(end, dtype=torch.uint8, device=x.device)
+        xt = FP8Matrix._within(kept, 0, k, m)._of(dtype) if need_w else None
+        wt = FP8Matrix._within(kept, at, k, n)._of(dtype) if need_x else None
         qx = FP8Matrix.empty(m, k, x.device)._of(dtype)
         qw = FP8Matrix.empty(n, k, w.device)._of(dtype)
         _quantize_into(x, dev, x_kind, False, qx, xt)
         _quantize_into(w, dev, w_kind, True, qw, wt)
-        if need_x or need_w:
-            ctx.save_for_backward(kept)
+        ctx.save_for_backward(kept)
         return matmul(qx, qw, x.dtype)
 
     @staticmethod
@@ -188,7 +194,7 @@ class _Linear(torch.autograd.Function):
             dx = matmul(rows, FP8Matrix._within(kept, ctx.at, k, n)._of(dtype), ctx.types[0])
         if need_w:  # dy^T [N, M] (x^T [K, M])^T
             dw = matmul(cols, FP8Matrix._within(kept, 0, k, m)._of(dtype), ctx.types[1])
-        return dx, dw, None, None, None
+        return dx, dw, None, None
 
 
 def linear(x: torch.Tensor, w: torch.Tensor, dtype=torch.float8_e4m3fn, grad_dtype=torch.float8_e4m3fn) -> torch.Tensor:
@@ -200,9 +206,10 @@ def linear(x: torch.Tensor, w: torch.Tensor, dtype=torch.float8_e4m3fn, grad_dty
         raise ValueError(f"linear: x {tuple(x.shape)} and w {tuple(w.shape)}")
     _code(dtype, "linear")
     _code(grad_dtype, "linear")
-    recorded = torch.is_grad_enabled()
-    if x.dim() == 2:
-        return _Linear.apply(x, w, recorded, dtype, grad_dtype)
     # (the rows are counted here: reshape cannot infer them where x has no columns)
-    rows = x.reshape(x.shape[:-1].numel(), x.shape[-1])
-    return _Linear.apply(rows, w, recorded, dtype, grad_dtype).view(*x.shape[:-1], w.shape[0])
+    rows = x if x.dim() == 2 else x.reshape(x.shape[:-1].numel(), x.shape[-1])
+    if torch.is_grad_enabled() and (x.requires_grad or w.requires_grad):
+        y = _Linear.apply(rows, w, dtype, grad_dtype)
+    else:
+        y = _product(rows, w, dtype)
+    return y if x.dim() == 2 else y.view(*x.shape[:-1], w.shape[0])

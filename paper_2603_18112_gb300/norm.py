@@ -13,6 +13,7 @@ from torch.autograd.function import once_differentiable
 
 from .mx import _call as _mx_call
 from .mx import _i64, _on_gpu, _type
+from .optim import TYPES
 from .tula_ags import _check, c_float, c_int, c_size_t, c_void_p, lib
 
 _fns = None  # the library's functions, their types declared
@@ -57,16 +58,29 @@ def _rows_of(t, cols):
 def _forward(x, weight, bias, eps, keep):
     """The output, and what the backward pass wants of it."""
     cols = x.shape[-1]
-    params = [p for p in (weight, bias) if p is not None]
-    dev, kind = _on_gpu(x, *params), _type(x.dtype, "layer_norm")
-    param_kind = _type(params[0].dtype, "layer_norm") if params else 0
-    rows, stride = _rows_of(x, cols)
-    weight, bias = (None if p is None else p.contiguous() for p in (weight, bias))
+    dev, kind, param_kind = x.get_device(), TYPES.get(x.dtype), 0
+    at = [None, None]
+    for i, p in enumerate((weight, bias)):
+        if p is not None:
+            if p.get_device() != dev:
+                _on_gpu(x, p)
+            if not p.is_contiguous():
+                p = p.contiguous()
+                at.append(p)  # (lives until the call)
+            param_kind = _type(p.dtype, "layer_norm")
+            at[i] = p.data_ptr()
+    if dev < 0 or kind is None:
+        _on_gpu(x)
+        _type(x.dtype, "layer_norm")
+    if x.dim() == 2 and x.is_contiguous():
+        rows, n, stride = x, x.shape[0], cols
+    else:
+        rows, stride = _rows_of(x, cols)
+        n = rows.shape[0]
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    stats = torch.empty((rows.shape[0], 2), dtype=torch.float32, device=x.device) if keep else None
-    _call("tula_layer_norm", dev, rows.data_ptr(), kind, rows.shape[0], cols, stride,
-          None if weight is None else weight.data_ptr(), None if bias is None else bias.data_ptr(), param_kind, eps,
-          y.data_ptr(), stats.data_ptr() if keep else None)
+    stats = torch.empty((n, 2), dtype=torch.float32, device=x.device) if keep else None
+    _call("tula_layer_norm", dev, rows.data_ptr(), kind, n, cols, stride, at[0], at[1], param_kind, eps, y.data_ptr(),
+          stats.data_ptr() if keep else None)
     return y, stats
 
 
@@ -106,12 +120,14 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.
                eps: float = 1e-5) -> torch.Tensor:
     """(x - mean) / sqrt(var + eps) * weight + bias over the last dimension of x, in fp32, in x's type (fp32,
     bf16 or fp16).  weight and bias: [cols], of one type of these, or None."""
-    for p in (weight, bias):
-        if p is not None and p.shape != x.shape[-1:]:
-            raise ValueError(f"layer_norm: x {tuple(x.shape)} and a parameter {tuple(p.shape)}")
-    if x.dim() == 0 or weight is not None and bias is not None and weight.dtype != bias.dtype:
+    last = x.shape[-1:]
+    if (weight is not None and weight.shape != last) or (bias is not None and bias.shape != last):
+        raise ValueError(f"layer_norm: x {tuple(x.shape)} and parameters "
+                         f"{[None if p is None else tuple(p.shape) for p in (weight, bias)]}")
+    if not last or weight is not None and bias is not None and weight.dtype != bias.dtype:
         raise TypeError(f"layer_norm: x of {x.dim()} dimensions, weight and bias "
                         f"{[None if p is None else p.dtype for p in (weight, bias)]}: one dimension or more and one type are wanted")
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias)):
+    if torch.is_grad_enabled() and (x.requires_grad or weight is not None and weight.requires_grad
+                                    or bias is not None and bias.requires_grad):
         return _LayerNorm.apply(x, weight, bias, eps)
     return _forward(x, weight, bias, eps, False)[0]

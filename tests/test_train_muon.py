@@ -74,19 +74,20 @@ def _size(rows, cols):
 
 
 def test_workspace_sizes():
-    # tiles of 128 x 64 elements, twice each of X and of the two products of its smaller side (none of what a
-    # CTA holds); parts of a norm and rows of a table by whole 256 bytes
+    # tiles of 128 x 64 elements, twice each of X and of the two products of its smaller side (none for a list
+    # of up to 304 that CTAs hold); parts of a norm and rows of a table by whole 256 bytes
     def of(r, c):
         n = min(r, c)
-        if n <= 128 and -(-r // 128) * -(-c // 64) <= 12:
-            return 0, 0
         x, a = -(-r // 128) * -(-c // 64), -(-n // 128) * -(-n // 64)
         return x, 2 * (x + a) * 16384
 
-    for shapes in ([(1, 1)], [(64, 576)], [(4096, 1024), (1024, 4096), (4096, 1024)], [(0, 5), (129, 65)]):
+    for shapes in ([(1, 1)], [(64, 576)], [(4096, 1024), (1024, 4096), (4096, 1024)], [(0, 5), (129, 65)], [(64, 64)] * 304, [(64, 64)] * 305,
+                   [(64, 64), (300, 200)], [(128, 769)], [(1536, 64)], [(1537, 64)]):
         full = [s for s in shapes if s[0]]
-        tiles = sum(of(*s)[0] for s in full)
-        want = -(-48 * len(full) // 256) * 256 + -(-8 * tiles // 256) * 256 + sum(of(*s)[1] for s in full)
+        tiles, space = sum(of(*s)[0] for s in full), sum(of(*s)[1] for s in full)
+        if len(full) <= 304 and all(min(s) <= 128 and -(-s[0] // 128) * -(-s[1] // 64) <= 12 for s in full):
+            tiles = space = 0
+        want = -(-48 * len(full) // 256) * 256 + -(-8 * tiles // 256) * 256 + space
         assert _size(*zip(*shapes)) == (0, max(want, 256))
     assert _size([0], [7])[0] == 0 and _size([-1], [7])[0] == -1 and _size([1 << 21], [1])[0] == -1
     assert _size([1 << 20], [1 << 20])[0] == -1  # beyond 256 GB
@@ -285,7 +286,7 @@ def _check_step(w, g, m, c, step, record=None, **kw):
     assert O.tula_muon_error() == 0
 
 
-LISTS = [[(1, 1)], [(64, 576), (16, 16), (64, 576)], [(130, 70), (70, 130), (0, 5), (130, 70), (1, 300), (257, 257)],
+LISTS = [[(1, 1)], [(64, 576), (16, 16), (64, 576)], [(100 + k % 30, 8 * (k % 7 + 1)) for k in range(310)], [(130, 70), (70, 130), (0, 5), (130, 70), (1, 300), (257, 257)],
          [(256, 64)] * 3 + [(64, 256)] * 2 + [(512, 512)] * 4, [(17 + 3 * k, 20 + 5 * k) for k in range(40)]]
 
 
