@@ -97,10 +97,10 @@ constexpr int kThreads = 64 + 32 * kReaders;
 template <bool Pair>
 struct Shape {
     static constexpr int kSide = Pair ? 256 : 128;  // of a block of the output
-    static constexpr int kStages = 5;
+    static constexpr int kStages = 6;  // (what is on its way bounds the rate: with five, 4096 x 4096 took SLOW us, FAST so)
     static constexpr int kOperand = 128 * 128;      // bytes of a stage, a CTA
     static constexpr int kStage = 2 * kOperand;
-    static constexpr int kOuts = kReaders * 2 * 4096;  // two buffers a warp
+    static constexpr int kOuts = kReaders * 4096;   // a buffer a warp
     static constexpr int kBars = 2 * kStages + 4;
     static constexpr int kSmem = kStages * kStage + kOuts + 8 * kBars + 16 + 1024;
     static constexpr int kCols = 2 * kSide;         // two accumulators
@@ -348,8 +348,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else {
         const int quad = warp & 3, row = quad * 32 + lane, half = (warp - 2) >> 2;
         constexpr int kChunks = S::kSide / kTileCols / 2;  // of 64 columns, a warp
-        const uint32_t buffers = outs + (warp - 2) * 8192;
-        uint32_t other = 0;  // kApply: the two buffers in turn; else one is for the block's mirror
+        const uint32_t buffer = outs + (warp - 2) * 4096;
+        auto buffer_free = [&] {  // the store that last used it has read it
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            __syncwarp();
+        };
         int n = 0;
         for (int t = worker; t < n_blocks; t += workers, ++n) {
             const ProductGroup *g;
@@ -376,11 +379,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             };
             if (K == kPoly && chunks) fetch(0);
             const bool finish = K == kLast && g->finish;
-            if (finish) {  // (a block of another group may have left a store that reads the buffers)
-                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-            }
-            // (the weights move by eight lanes to 64 columns of a row)
-            const int first_row = im * kTile + quad * 32 + (lane >> 3), cols = g->cols, rows_left = g->rows - first_row;
+            if (finish) buffer_free();  // (of a block of another group)
+            // (the weights move by four lanes to 32 columns of a row)
+            const int first_row = im * kTile + quad * 32 + (lane >> 2), cols = g->cols, rows_left = g->rows - first_row;
             Matrix q = {};
             if (finish && a.matrices) q = a.matrices[g->matrix + b.matrix];
             if (!__all_sync(kFull, mbar_wait(acc_full + 8 * (n & 1), (n / 2) & 1, &dead))) break;
@@ -392,14 +393,15 @@ __global__ void __launch_bounds__(kThreads, 1)
                 unsigned v[64];
                 tmem_load32(v, acc + c * kTileCols);
                 tmem_load32(v + 32, acc + c * kTileCols + 32);
-                const int col = j * kTileCols + (lane & 7) * 8;
-                const bool mine = finish && c < chunks && col < cols;
+                const int col = j * kTileCols + (lane & 3) * 8;  // and 32 further on
+                const bool mine = finish && c < chunks;
                 float w[K == kLast ? 64 : 1];
                 if constexpr (K == kLast)
                     if (q.w && mine) {
 #pragma unroll
                         for (int k = 0; k < 8; ++k)
-                            if (4 * k < rows_left) load8(w + 8 * k, q.w + (size_t)(first_row + 4 * k) * cols + col);
+                            if (8 * (k & 3) < rows_left && col + 8 * (k & 4) < cols)
+                                load8(w + 8 * k, q.w + (size_t)(first_row + 8 * (k & 3)) * cols + col + 8 * (k & 4));
                     }
                 tmem_wait(v);
                 if (c == kChunks - 1) {
@@ -410,38 +412,46 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (c >= chunks) continue;
                 if constexpr (K == kLast) {
                     if (finish) {
-                        // the values change from a row a lane to a row eight lanes: 32 rows of 256 bytes, their
-                        // 32-byte pieces exchanged so that neither way meets in a bank
-                        __syncwarp();  // the last ones have been read
+                        // the values change from a row a lane to a row four lanes, 32 rows of 32 columns at a
+                        // time, their 32-byte pieces exchanged so that neither way meets in a bank
 #pragma unroll
-                        for (int k = 0; k < 16; ++k)
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buffers + lane * 256 + ((k ^ (lane & 7) << 1) << 4)),
-                                         "r"(v[4 * k]), "r"(v[4 * k + 1]), "r"(v[4 * k + 2]), "r"(v[4 * k + 3])
-                                         : "memory");
-                        __syncwarp();
-                        if (!mine) continue;
+                        for (int half_at = 0; half_at < 2; ++half_at) {
+                            __syncwarp();  // the last ones have been read
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            if (4 * k >= rows_left) break;
-                            const int r = 4 * k + (lane >> 3);
-                            const uint32_t from = buffers + r * 256 + (((lane & 7) ^ (r & 7)) << 5);
-                            float x[8];
-#pragma unroll
-                            for (int h = 0; h < 2; ++h)
-                                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
-                                             : "=f"(x[4 * h]), "=f"(x[4 * h + 1]), "=f"(x[4 * h + 2]), "=f"(x[4 * h + 3])
-                                             : "r"(from + 16 * h)
+                            for (int k = 0; k < 8; ++k)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
+                                                 buffer + lane * 128 + ((k ^ (lane & 3) << 1) << 4)),
+                                             "r"(v[32 * half_at + 4 * k]), "r"(v[32 * half_at + 4 * k + 1]),
+                                             "r"(v[32 * half_at + 4 * k + 2]), "r"(v[32 * half_at + 4 * k + 3])
                                              : "memory");
+                            __syncwarp();
+                            const int c0 = col + 32 * half_at;
+                            if (c0 < cols) {
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) x[e] *= alpha;
-                            const size_t at = (size_t)(first_row + 4 * k) * cols + col;
-                            if (q.w) {
+                                for (int k = 0; k < 4; ++k) {
+                                    if (8 * k >= rows_left) break;
+                                    const int r = 8 * k + (lane >> 2);
+                                    const uint32_t from = buffer + r * 128 + (((lane & 3) ^ (r & 3)) << 5);
+                                    float x[8];
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) x[e] = fmaf(-step, x[e], __fmul_rn(w[8 * k + e], a.decay));
-                                store8(q.w + at, x);
-                                if (q.copy) store8(q.copy, q.ctype, at, x);
-                            } else {
-                                store8(a.y, a.ytype, (size_t)b.matrix * g->rows * cols + at, x);
+                                    for (int h = 0; h < 2; ++h)
+                                        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                                                     : "=f"(x[4 * h]), "=f"(x[4 * h + 1]), "=f"(x[4 * h + 2]), "=f"(x[4 * h + 3])
+                                                     : "r"(from + 16 * h)
+                                                     : "memory");
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e) x[e] *= alpha;
+                                    const size_t at = (size_t)(first_row + 8 * k) * cols + c0;
+                                    if (q.w) {
+#pragma unroll
+                                        for (int e = 0; e < 8; ++e)
+                                            x[e] = fmaf(-step, x[e], __fmul_rn(w[32 * half_at + 8 * k + e], a.decay));
+                                        store8(q.w + at, x);
+                                        if (q.copy) store8(q.copy, q.ctype, at, x);
+                                    } else {
+                                        store8(a.y, a.ytype, (size_t)b.matrix * g->rows * cols + at, x);
+                                    }
+                                }
                             }
                         }
                         continue;
@@ -466,41 +476,35 @@ __global__ void __launch_bounds__(kThreads, 1)
                     memcpy(&y[k], &h, 4);
                 }
                 if (K == kPoly && c + 1 < chunks) fetch(c + 1);
-                const uint32_t buffer = buffers + other, mirror = buffers + 4096;
-                if (lane == 0) {  // the stores that last used the buffers have read them
-                    if (K >= kApply)
-                        asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-                    else
-                        asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                }
-                __syncwarp();
+                buffer_free();
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buffer + lane * 128 + ((k ^ (lane & 7)) << 4)),
                                  "r"(y[4 * k]), "r"(y[4 * k + 1]), "r"(y[4 * k + 2]), "r"(y[4 * k + 3])
                                  : "memory");
-                if (twice) {
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0)
+                    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];\n"
+                                 "cp.async.bulk.commit_group;" ::"l"(&map_out),
+                                 "r"(0), "r"((out + im * out_pitch + j) * kTile + quad * 32), "r"(buffer)
+                                 : "memory");
+                if (!twice) continue;
+                buffer_free();
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) {
-                        asm volatile("st.shared.b16 [%0], %1;" ::"r"(mirror + 128 * k + 2 * lane), "h"((unsigned short)y[k]) : "memory");
-                        asm volatile("st.shared.b16 [%0], %1;" ::"r"(mirror + 128 * k + 64 + 2 * lane), "h"((unsigned short)(y[k] >> 16))
-                                     : "memory");
-                    }
+                for (int k = 0; k < 32; ++k) {
+                    asm volatile("st.shared.b16 [%0], %1;" ::"r"(buffer + 128 * k + 2 * lane), "h"((unsigned short)y[k]) : "memory");
+                    asm volatile("st.shared.b16 [%0], %1;" ::"r"(buffer + 128 * k + 64 + 2 * lane), "h"((unsigned short)(y[k] >> 16))
+                                 : "memory");
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) {
-                    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(&map_out), "r"(0),
-                                 "r"((out + im * out_pitch + j) * kTile + quad * 32), "r"(buffer)
+                if (lane == 0)
+                    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];\n"
+                                 "cp.async.bulk.commit_group;" ::"l"(&map_mirror),
+                                 "r"(32 * (quad & 1)), "r"((out + (j >> 1) * out_pitch + 2 * im + (quad >> 1)) * kTile + 64 * (j & 1)),
+                                 "r"(buffer)
                                  : "memory");
-                    if (twice)
-                        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(&map_mirror),
-                                     "r"(32 * (quad & 1)),
-                                     "r"((out + (j >> 1) * out_pitch + 2 * im + (quad >> 1)) * kTile + 64 * (j & 1)), "r"(mirror)
-                                     : "memory");
-                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                }
-                if (K >= kApply) other ^= 4096;
             }
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
