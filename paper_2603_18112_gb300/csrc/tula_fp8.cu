@@ -41,9 +41,12 @@ __device__ __forceinline__ unsigned codes4(float a, float b, float c, float d) {
 //
 // One CTA per 128 x 128 tile of x, which holds 128 blocks of its rows and of its columns, or is one block
 // (Square).  A thread takes 32 bytes of a row at a time; the lanes that share a row find its largest
-// magnitude together.  The transpose reads the tile again from shared memory, a thread per 32 rows of one
-// column (fp32) or of two; four of them share a column's block.  HBM bounds it: 2 or 4 bytes in and one
-// out per element and form.
+// magnitude together.  The transpose reads the tile again from shared memory, four lanes to a word's columns
+// (one column of fp32, two of others), 32 rows each: they find the columns' largest magnitudes by two
+// exchanges and write 128 bytes of codes to each column, so that one barrier is enough.  (With the tops and
+// codes of columns by way of shared memory and two barriers more, 8192 x 4096 bf16 took 30 us in both forms
+// instead of BOTHUS.)  fp32 rows off 32-byte boundaries come word by word, a warp to a row, and through
+// shared memory too.  HBM bounds it: 2 or 4 bytes in and one out per element and form.
 
 struct QuantArgs {
     const void *x;
@@ -61,17 +64,13 @@ struct Shape {
     static constexpr int kRows = kThreads / kLanes;        // at a time: 32
     static constexpr int kSide = kTile * (int)sizeof(T) / 4;  // words of a tile's row
     static constexpr int kCols = 4 / (int)sizeof(T);       // columns of a word
-    static constexpr int kOutPitch = kTile + 16;           // bytes of a column's codes, and some to spread the banks
-    static constexpr int kSmem = kTile * kTile * (int)sizeof(T) + kTile * kOutPitch;
+    static constexpr int kSmem = kTile * kTile * (int)sizeof(T);
     static_assert(kThreads == kSide * 4 && kRows == 32, "a column block is one thread's");
 };
 
 // Where 16-byte chunk `chunk` of a row of the tile lies in shared memory: so that neither the stores of
-// parts nor the column reads (a word a lane, all of one row) meet in a bank.
-template <typename T>
-__device__ __forceinline__ int chunk_place(int row, int chunk) {
-    return sizeof(T) == 4 ? chunk ^ (chunk >> 3 & 3) ^ (row & 1) << 2 : chunk ^ (chunk >> 3) ^ (row & 1) << 1;
-}
+// parts nor the column reads (eight words of each of four rows, 32 rows apart) meet in a bank.
+__device__ __forceinline__ int chunk_place(int row, int chunk) { return chunk ^ (chunk >> 3 & 1) ^ (row >> 5) << 1; }
 
 // The largest magnitude of a word's elements so far, as fp32 bits (16-bit types: of both halves).
 template <typename T>
@@ -91,8 +90,8 @@ __device__ __forceinline__ void put_scale(unsigned char *scales, int row, long l
 template <typename T, bool E5, bool Aligned, bool Square, bool Rows, bool Cols>
 __global__ void __launch_bounds__(Shape<T>::kThreads, Shape<T>::kCtas) k_quantize8(const QuantArgs a) {
     using S = Shape<T>;
-    extern __shared__ __align__(16) unsigned tile[];  // Cols
-    __shared__ unsigned tops[4 * kTile];
+    extern __shared__ __align__(16) unsigned tile[];  // Cols, or fp32 word by word
+    __shared__ unsigned tops[S::kThreads / 32];
     let_next_start();
     wait_for_previous();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -101,41 +100,75 @@ __global__ void __launch_bounds__(Shape<T>::kThreads, Shape<T>::kCtas) k_quantiz
     const int sub = tid % S::kLanes, row0 = tid / S::kLanes;
     const unsigned long long begin = reinterpret_cast<unsigned long long>(a.x);
     const unsigned long long end = begin + ((unsigned long long)(a.rows - 1) * a.stride + a.cols) * sizeof(T);
-    unsigned w[4][8];
-    const T *p0 = static_cast<const T *>(a.x) + (r0 + row0) * a.stride + c0 + S::kElems * sub;
+    constexpr bool kByWord = sizeof(T) == 4 && !Aligned, kStaged = Cols || kByWord;
+    unsigned w[4][8], top_all = 0;
     const bool inner = c0 + kTile <= a.cols && (Aligned ? r0 + kTile <= a.rows : tr > 0 && r0 + kTile < a.rows);
-    if (inner) {
+    if constexpr (kByWord) {
+        // words lane + 32 k of rows warp + 16 i
+        const unsigned *p = static_cast<const unsigned *>(a.x) + (r0 + warp) * a.stride + c0 + lane;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            load_part<T, S::kElems, Aligned>(w[i], p0 + i * 32 * a.stride, true, S::kElems, begin, end);
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                unsigned &v = w[i >> 1][4 * (i & 1) + k];
+                v = 0;
+                if (inner || (r0 + warp + 16 * i < a.rows && c0 + lane + 32 * k < a.cols)) v = __ldcs(p + 16 * i * a.stride + 32 * k);
+            }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int r = warp + 16 * i, c = lane + 32 * k;
+                const unsigned v = w[i >> 1][4 * (i & 1) + k];
+                if (Square) top_all = larger<T>(top_all, v);
+                tile[r * S::kSide + 4 * chunk_place(r, c >> 2) + (c & 3)] = v;
+            }
     } else {
+        const T *p0 = static_cast<const T *>(a.x) + (r0 + row0) * a.stride + c0 + S::kElems * sub;
+        if (inner) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            load_part<T, S::kElems, Aligned>(w[i], p0 + i * 32 * a.stride, false,
-                                             r0 + row0 + 32 * i < a.rows ? a.cols - c0 - S::kElems * sub : 0, begin, end);
+            for (int i = 0; i < 4; ++i)
+                load_part<T, S::kElems, Aligned>(w[i], p0 + i * 32 * a.stride, true, S::kElems, begin, end);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                load_part<T, S::kElems, Aligned>(w[i], p0 + i * 32 * a.stride, false,
+                                                 r0 + row0 + 32 * i < a.rows ? a.cols - c0 - S::kElems * sub : 0, begin, end);
+        }
+        if (Square)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) top_all = larger<T>(top_all, w[i][k]);
+        if (Cols)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    *reinterpret_cast<uint4 *>(&tile[(row0 + 32 * i) * S::kSide + 4 * chunk_place(row0 + 32 * i, sub * 2 + k)]) =
+                        make_uint4(w[i][4 * k], w[i][4 * k + 1], w[i][4 * k + 2], w[i][4 * k + 3]);
     }
+    if (Square) {
+        top_all = __reduce_max_sync(kFull, whole_top<T>(top_all));
+        if (lane == 0) tops[warp] = top_all;
+    }
+    if (Square || kStaged) __syncthreads();
     unsigned s_all = 0;
     if (Square) {
-        unsigned top = 0;
+        top_all = tops[0];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) top = larger<T>(top, w[i][k]);
-        top = __reduce_max_sync(kFull, whole_top<T>(top));
-        if (lane == 0) tops[warp] = top;
-        __syncthreads();
-        top = tops[0];
-#pragma unroll
-        for (int k = 1; k < S::kThreads / 32; ++k) top = max(top, tops[k]);
-        s_all = scale_byte<E5>(top);
+        for (int k = 1; k < S::kThreads / 32; ++k) top_all = max(top_all, tops[k]);
+        s_all = scale_byte<E5>(top_all);
     }
-    if (Cols) {
+    if (Rows && kByWord) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
-                *reinterpret_cast<uint4 *>(&tile[(row0 + 32 * i) * S::kSide + 4 * chunk_place<T>(row0 + 32 * i, sub * 2 + k)]) =
-                    make_uint4(w[i][4 * k], w[i][4 * k + 1], w[i][4 * k + 2], w[i][4 * k + 3]);
+            for (int k = 0; k < 2; ++k) {
+                const uint4 q = *reinterpret_cast<const uint4 *>(
+                    &tile[(row0 + 32 * i) * S::kSide + 4 * chunk_place(row0 + 32 * i, sub * 2 + k)]);
+                w[i][4 * k] = q.x, w[i][4 * k + 1] = q.y, w[i][4 * k + 2] = q.z, w[i][4 * k + 3] = q.w;
+            }
     }
     if (Rows) {
 #pragma unroll
@@ -177,29 +210,25 @@ __global__ void __launch_bounds__(Shape<T>::kThreads, Shape<T>::kCtas) k_quantiz
         }
     }
     if (!Cols) return;
-    __syncthreads();
-    unsigned char *out = reinterpret_cast<unsigned char *>(tile + kTile * S::kSide);
-    const int c = tid % S::kSide, rb = tid / S::kSide;  // word c of 32 rows
-    const int at[2] = {4 * chunk_place<T>(0, c >> 2) + (c & 3), 4 * chunk_place<T>(1, c >> 2) + (c & 3)};
+    const int c = tid >> 2, rb = tid & 3;  // word c of 32 rows
+    const int at = 4 * chunk_place(32 * rb, c >> 2) + (c & 3);
     unsigned v[32], top = 0;
 #pragma unroll
     for (int k = 0; k < 32; ++k) {
-        v[k] = tile[(32 * rb + k) * S::kSide + at[k & 1]];
+        v[k] = tile[(32 * rb + k) * S::kSide + at];
         if (!Square) top = larger<T>(top, v[k]);
     }
-    if (!Square) {
-        top &= sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu;
-#pragma unroll
-        for (int h = 0; h < S::kCols; ++h)
-            tops[rb * kTile + S::kCols * c + h] = sizeof(T) == 4 ? top : top_bits<T>(h ? top >> 16 : top & 0xffffu);
-        __syncthreads();
-    }
+    top &= sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu;
 #pragma unroll
     for (int h = 0; h < S::kCols; ++h) {
         const int col = S::kCols * c + h;
         unsigned s = s_all;
-        if (!Square)
-            s = scale_byte<E5>(max(max(tops[col], tops[kTile + col]), max(tops[2 * kTile + col], tops[3 * kTile + col])));
+        if (!Square) {
+            unsigned t = sizeof(T) == 4 ? top : top_bits<T>(h ? top >> 16 : top & 0xffffu);
+            t = max(t, __shfl_xor_sync(kFull, t, 1));
+            t = max(t, __shfl_xor_sync(kFull, t, 2));
+            s = scale_byte<E5>(t);
+        }
         const float f = inverse_scale(s);
         unsigned q[8];
 #pragma unroll
@@ -217,19 +246,13 @@ __global__ void __launch_bounds__(Shape<T>::kThreads, Shape<T>::kCtas) k_quantiz
             }
             q[k] = s == 255u ? 0u : codes4<E5>(x[0], x[1], x[2], x[3]);
         }
-        uint4 *to = reinterpret_cast<uint4 *>(out + col * S::kOutPitch + 32 * rb);
-        to[0] = make_uint4(q[0], q[1], q[2], q[3]);
-        to[1] = make_uint4(q[4], q[5], q[6], q[7]);
-        if (rb == 0) put_scale(a.scales_t, col, tc, tr, a.tiles_r, c0 + col < a.cols ? s : 0u);
-    }
-    __syncthreads();
-    const size_t pitch_t = (size_t)a.tiles_r * kTile;
-#pragma unroll
-    for (int k = 0; k < 8 * kTile / S::kThreads; ++k) {
-        const int col = (k * S::kThreads + tid) >> 3, part = tid & 7;
-        if (c0 + col < a.cols)
-            *reinterpret_cast<uint4 *>(a.codes_t + (size_t)(c0 + col) * pitch_t + r0 + 16 * part) =
-                *reinterpret_cast<const uint4 *>(out + col * S::kOutPitch + 16 * part);
+        const bool there = c0 + col < a.cols;
+        if (rb == 0) put_scale(a.scales_t, col, tc, tr, a.tiles_r, there ? s : 0u);
+        if (there) {
+            uint4 *to = reinterpret_cast<uint4 *>(a.codes_t + (size_t)(c0 + col) * a.tiles_r * kTile + r0 + 32 * rb);
+            to[0] = make_uint4(q[0], q[1], q[2], q[3]);
+            to[1] = make_uint4(q[4], q[5], q[6], q[7]);
+        }
     }
 }
 
@@ -296,7 +319,7 @@ int launch_quantize(const QuantArgs &a, unsigned grid, cudaStream_t s) {
     void (*k)(const QuantArgs) = which == 0   ? k_quantize8<T, E5, Aligned, Square, true, true>
                                  : which == 1 ? k_quantize8<T, E5, Aligned, Square, true, false>
                                               : k_quantize8<T, E5, Aligned, Square, false, true>;
-    const int smem = a.codes_t ? Shape<T>::kSmem : 0;
+    const int smem = a.codes_t || (sizeof(T) == 4 && !Aligned) ? Shape<T>::kSmem : 0;
     const int rc = allow_smem((const void *)k, smem, &done[which]);
     if (rc) return rc;
     return tula::launch(k, dim3(grid), Shape<T>::kThreads, smem, s, 1, a);
