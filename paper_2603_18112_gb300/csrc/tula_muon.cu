@@ -77,6 +77,7 @@ struct ProductArgs {
     int ytype;
     float decay;
     int n_groups, n_blocks;
+    int n_first, skip;  // see block_of
     int none;         // a row beyond the workspace
     ProductGroup g[kMostGroups];
 };
@@ -127,6 +128,20 @@ __device__ __forceinline__ void mma16(uint32_t d, uint64_t a, uint64_t b, uint32
         asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
                      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((unsigned)add)
                      : "memory");
+}
+
+// The blocks in the order of their groups, those with the longest sums first, go round the workers; those that
+// the first groups, of equal sums, leave with one more than the others are passed over for a.skip rounds of what follows, about
+// as long as that one takes.  (72 matrices, sums of 4096 and of 1024: A in GRAM1US us, GRAM0US without.)
+__device__ __forceinline__ int block_of(const ProductArgs &a, int worker, int workers, int i) {
+    const int full = a.n_first / workers, more = a.n_first - full * workers;
+    if (i < full) return i * workers + worker;
+    if (!a.skip) return i * workers + worker;
+    i -= full;
+    const bool heavy = worker < more;
+    if (heavy && i == 0) return full * workers + worker;
+    if (!heavy && i < a.skip) return a.n_first + i * (workers - more) + worker - more;
+    return a.n_first + a.skip * (workers - more) + (i - (heavy ? 1 : a.skip)) * workers + worker;
 }
 
 // A block of work: its group, matrix and place.
@@ -270,7 +285,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (warp == 0) {
         int i = 0;  // stages filled
         bool ok = true;
-        for (int t = worker; ok && t < n_blocks; t += workers) {
+        for (int at = 0, t; ok && (t = block_of(a, worker, workers, at)) < n_blocks; ++at) {
             const ProductGroup *g;
             const Block b = block_at<K>(a, t, g);
             const int n_k = g->n_k;
@@ -311,7 +326,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (rank == 0) {
             int i = 0, n = 0;
             bool ok = true;
-            for (int t = worker; ok && t < n_blocks; t += workers, ++n) {
+            for (int t; ok && (t = block_of(a, worker, workers, n)) < n_blocks; ++n) {
                 const ProductGroup *g;
                 block_at<K>(a, t, g);
                 const bool pa = g->p.along, qa = g->q.along;
@@ -354,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             __syncwarp();
         };
         int n = 0;
-        for (int t = worker; t < n_blocks; t += workers, ++n) {
+        for (int t; (t = block_of(a, worker, workers, n)) < n_blocks; ++n) {
             const ProductGroup *g;
             const Block b = block_at<K>(a, t, g);
             const int im = Pair ? 2 * b.m + rank : b.m;
@@ -638,38 +653,46 @@ __device__ __forceinline__ const void *batch_at(const StreamArgs &a, int matrix)
 
 // What is orthogonalised: its parts as they lie in memory, and then the update itself.  First: the momentum
 // moves on.
+template <bool Plan>
 struct Loaded {
-    float g[32], m[32], mult;
+    float g[32], m[Plan ? 32 : 1], mult;
 };
-template <bool Vec>
-__device__ __forceinline__ void load_parts(Loaded &l, const StreamArgs &a, const Place &p, const Matrix &q) {
-    if (!a.matrices) {
+template <bool Plan, bool Vec>
+__device__ __forceinline__ void load_parts(Loaded<Plan> &l, const StreamArgs &a, const Place &p, const Matrix &q) {
+    if constexpr (Plan) {
+        l.mult = a.record ? __fdiv_rn(a.record[TULA_RECORD_COEF], a.grad_scale) : __fdiv_rn(1.f, a.grad_scale);
+        load_typed<Vec>(l.g, q.g, q.gtype, p.g->cols, p);
+        load_tile<float, Vec>(l.m, q.m, p.g->cols, p);
+    } else {
         load_typed<Vec>(l.g, batch_at(a, p.matrix), a.xtype, a.stride, p);
-        return;
     }
-    l.mult = a.record ? __fdiv_rn(a.record[TULA_RECORD_COEF], a.grad_scale) : __fdiv_rn(1.f, a.grad_scale);
-    load_typed<Vec>(l.g, q.g, q.gtype, p.g->cols, p);
-    load_tile<float, Vec>(l.m, q.m, p.g->cols, p);
 }
-template <bool First, bool Vec>
-__device__ __forceinline__ void update_of(float (&u)[32], Loaded &l, const StreamArgs &a, const Place &p, const Matrix &q) {
+template <bool First, bool Plan, bool Vec>
+__device__ __forceinline__ void update_of(float (&u)[32], Loaded<Plan> &l, const StreamArgs &a, const Place &p, const Matrix &q) {
+    if constexpr (Plan) {
 #pragma unroll
-    for (int k = 0; k < 32; ++k) {
-        if (!a.matrices) {
-            u[k] = l.g[k];
-            continue;
+        for (int k = 0; k < 32; ++k) {
+            const float d = __fmul_rn(l.g[k], l.mult);
+            if (First) l.m[k] = fmaf(a.mu, l.m[k], d);
+            u[k] = a.nesterov ? fmaf(a.mu, l.m[k], d) : l.m[k];
         }
-        const float d = __fmul_rn(l.g[k], l.mult);
-        if (First) l.m[k] = fmaf(a.mu, l.m[k], d);
-        u[k] = a.nesterov ? fmaf(a.mu, l.m[k], d) : l.m[k];
+        if (First) store_tile<float, Vec>(q.m, p.g->cols, p, l.m);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 32; ++k) u[k] = l.g[k];
     }
-    if (First && a.matrices) store_tile<float, Vec>(q.m, p.g->cols, p, l.m);
 }
 template <bool First, bool Vec>
 __device__ __forceinline__ void load_update(float (&u)[32], const StreamArgs &a, const Place &p, const Matrix &q) {
-    Loaded l;
-    load_parts<Vec>(l, a, p, q);
-    update_of<First, Vec>(u, l, a, p, q);
+    if (a.matrices) {
+        Loaded<true> l;
+        load_parts<true, Vec>(l, a, p, q);
+        update_of<First, true, Vec>(u, l, a, p, q);
+    } else {
+        Loaded<false> l;
+        load_parts<false, Vec>(l, a, p, q);
+        update_of<First, false, Vec>(u, l, a, p, q);
+    }
 }
 
 // The sum of squares of a warp's elements: in fp32 with an exact power of two taken out, so that no square
@@ -870,26 +893,27 @@ struct Small {
     }
 };
 
-template <bool Vec>
+template <bool Plan, bool Vec>
 __device__ __forceinline__ void small_load(const StreamArgs &a, Place p, const Matrix &q, int tiles, unsigned char *x, double *sums,
                                            float2 *factors) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, pitch = p.g->pitch;
-    // (two tiles' parts are on their way at a time)
+    // (several tiles' parts are on their way at a time)
+    constexpr int kAhead = Plan ? 2 : 4;
     auto tile = [&](int t) { p.row0 = t / pitch * kTile, p.col0 = t % pitch * kTileCols; };
-    Loaded l[2];
+    Loaded<Plan> l[kAhead];
     double total = 0.0;  // lane 0 of a warp
-    for (int t0 = 0; t0 < tiles; t0 += 2) {
+    for (int t0 = 0; t0 < tiles; t0 += kAhead) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < kAhead; ++h) {
             tile(t0 + h);
-            if (t0 + h < tiles) load_parts<Vec>(l[h], a, p, q);
+            if (t0 + h < tiles) load_parts<Plan, Vec>(l[h], a, p, q);
         }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < kAhead; ++h) {
             if (t0 + h >= tiles) break;
             tile(t0 + h);
             float u[32];
-            update_of<true, Vec>(u, l[h], a, p, q);
+            update_of<true, Plan, Vec>(u, l[h], a, p, q);
             warp_squares(u, sums);
             if (lane == 0) total += sums[warp];
         }
@@ -904,18 +928,18 @@ __device__ __forceinline__ void small_load(const StreamArgs &a, Place p, const M
     __syncthreads();
     const float2 f = *factors;
     constexpr int kN = Vec ? 8 : 1;
-    for (int t0 = 0; t0 < tiles; t0 += 2) {
+    for (int t0 = 0; t0 < tiles; t0 += kAhead) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < kAhead; ++h) {
             tile(t0 + h);
-            if (t0 + h < tiles) load_parts<Vec>(l[h], a, p, q);
+            if (t0 + h < tiles) load_parts<Plan, Vec>(l[h], a, p, q);
         }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < kAhead; ++h) {
             if (t0 + h >= tiles) break;
             tile(t0 + h);
             float u[32];
-            update_of<false, Vec>(u, l[h], a, p, q);
+            update_of<false, Plan, Vec>(u, l[h], a, p, q);
 #pragma unroll
             for (int k = 0; k < 32; k += kN) {
                 const Run<__half, kN> r = scaled_run<Vec>(u, k, p, f);
@@ -993,10 +1017,14 @@ __global__ void __launch_bounds__(kStreamThreads, 1) k_muon_small(const __grid_c
     const bool vec = a.matrices ? q.vec : a.vec;
     Small m{smem_addr(x), smem_addr(x) + kSmallTiles * kTileBytes, smem_addr(&bar), &dead, 0, 0};
     if (go) {
-        if (vec)
-            small_load<true>(a, p, q, tiles, x, sums, &factors);
+        if (a.matrices && vec)
+            small_load<true, true>(a, p, q, tiles, x, sums, &factors);
+        else if (a.matrices)
+            small_load<true, false>(a, p, q, tiles, x, sums, &factors);
+        else if (vec)
+            small_load<false, true>(a, p, q, tiles, x, sums, &factors);
         else
-            small_load<false>(a, p, q, tiles, x, sums, &factors);
+            small_load<false, false>(a, p, q, tiles, x, sums, &factors);
     }
     m.before();  // (and tensor memory is there)
     m.tmem = __shfl_sync(kFull, tmem_at, 0);
@@ -1188,12 +1216,21 @@ bool make_maps(Maps &m, const void *tiles, long long n) {
 }
 
 template <bool Pair, Kind K>
-int launch_product(const Maps &maps, const ProductArgs &a, int sms, cudaStream_t s) {
+int launch_product(const Maps &maps, ProductArgs &a, int sms, cudaStream_t s) {
     using S = Shape<Pair>;
     static std::atomic<uint64_t> done;
     const int rc = allow_smem((const void *)k_product<Pair, K>, S::kSmem, &done);
     if (rc) return rc;
     const int workers = std::min(a.n_blocks, Pair ? std::max(1, sms / 2) : sms);
+    int next = 1;  // the first group with other sums
+    while (next < a.n_groups && a.g[next].n_k == a.g[0].n_k) ++next;
+    a.n_first = next < a.n_groups ? a.g[next].first : a.n_blocks;
+    a.skip = 0;
+    const int more = a.n_first % workers, rest = a.n_blocks - a.n_first;
+    if (more && rest > 0) {
+        const int rounds = (a.g[0].n_k + a.g[next].n_k / 2) / a.g[next].n_k;
+        a.skip = std::min(rounds, rest / (workers - more));  // whole rounds of those that are left
+    }
     return tula::launch(k_product<Pair, K>, dim3((unsigned)(workers * (Pair ? 2 : 1))), kThreads, S::kSmem, s, Pair ? 2 : 1, maps.in,
                         maps.out, maps.mirror, a);
 }
