@@ -220,6 +220,33 @@ int tula_fp8_matmul(const void *a_codes, const void *a_scales, int a_code, const
                     const void *b_scales, int b_code, int64_t M, int64_t N, int64_t K, void *out,
                     int out_type, void *stream);
 
+/*
+ * A layer's forward pass, y = x w^T, in one call: x (M x K, blocks of 1 x 128) and w (N x K, blocks of
+ * 128 x 128) quantised to `code`, and their product in x's type into y, device [M][N].  What the
+ * backward pass multiplies by is left in `kept`: with need_dw x^T (K x M, blocks along the rows of x),
+ * then with need_dx w^T (K x N), each its scales and then its codes (sizes of tula_fp8_size).  temp
+ * holds x and w quantised, laid out so, and may be used again by what is enqueued after.  Both
+ * 16-byte aligned, NULL where they would be empty (TULA_ERR_WORKSPACE otherwise).
+ */
+typedef struct tula_fp8_operand {
+    const void *data;  /* device; row r, column c at r * stride + c, or with transposed c * stride + r */
+    int64_t stride;    /* in elements, at least the length of what is contiguous */
+    int type;          /* TULA_TYPE_* */
+    int transposed;
+} tula_fp8_operand;
+int tula_fp8_linear(const tula_fp8_operand *x, const tula_fp8_operand *w, int64_t M, int64_t N,
+                    int64_t K, int code, int need_dx, int need_dw, void *kept, void *temp, void *y,
+                    void *stream);
+
+/*
+ * Its backward pass: dy (M x N) quantised to grad_code along the dimension that each product sums over,
+ * dx = dy w (need_dx) into dx, device [M][K], and dw = dy^T x (need_dw) into dw, device [N][K].  `code`,
+ * `kept` and what is needed are the forward pass's; temp holds dy (need_dx), then dy^T (need_dw).
+ */
+int tula_fp8_linear_backward(const tula_fp8_operand *dy, int64_t M, int64_t N, int64_t K, int code,
+                             int grad_code, const void *kept, void *temp, void *dx, int dx_type,
+                             void *dw, int dw_type, int need_dx, int need_dw, void *stream);
+
 /* The error word of the 8-bit products, as tula_mx_error. */
 int tula_fp8_error(void *stream, int *error_out);
 

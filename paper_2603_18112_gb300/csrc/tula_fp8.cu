@@ -333,6 +333,30 @@ int quantize_typed(const QuantArgs &a, unsigned grid, bool square, cudaStream_t 
 
 inline bool good_code(int code) { return code == TULA_FP8_E4M3 || code == TULA_FP8_E5M2; }
 
+// A matrix in memory of the caller's: scales, then codes.
+struct Held {
+    unsigned char *scales = nullptr, *codes = nullptr;
+};
+// The next one of a run of them; false beyond what one may have.
+bool take(unsigned char *&at, long long rows, long long cols, bool wanted, Held &h) {
+    size_t codes = 0, scales = 0;
+    if (!wanted) return true;
+    if (tula_fp8_size(rows, cols, &codes, &scales) != TULA_OK) return false;
+    if (rows && cols) h.scales = at, h.codes = at + scales;
+    at += scales + codes;
+    return true;
+}
+int quantize(const tula_fp8_operand &x, long long rows, long long cols, int code, int square, const Held &h, const Held &t, void *stream) {
+    if (!h.codes && !t.codes) return TULA_OK;  // not wanted, or empty
+    if (x.transposed)
+        return tula_fp8_quantize(x.data, x.type, cols, rows, x.stride, code, square, t.codes, t.scales, h.codes, h.scales, stream);
+    return tula_fp8_quantize(x.data, x.type, rows, cols, x.stride, code, square, h.codes, h.scales, t.codes, t.scales, stream);
+}
+bool good_operand(const tula_fp8_operand *x, long long rows, long long cols) {
+    return x && good_type(x->type) && x->stride >= (x->transposed ? rows : cols) &&
+           (!rows || !cols || (x->data && aligned(x->data, type_size(x->type))));
+}
+
 }  // namespace
 
 extern "C" {
@@ -385,6 +409,41 @@ int tula_fp8_matmul(const void *a_codes, const void *a_scales, int a_code, const
     if (!good_code(a_code) || !good_code(b_code)) return TULA_ERR_ARG;
     return matmul<Codes8>({a_codes, a_scales, a_code}, {b_codes, b_scales, b_code}, M, N, K, out, out_type,
                           static_cast<cudaStream_t>(stream));
+}
+
+int tula_fp8_linear(const tula_fp8_operand *x, const tula_fp8_operand *w, int64_t M, int64_t N, int64_t K, int code, int need_dx,
+                    int need_dw, void *kept, void *temp, void *y, void *stream) {
+    if (!good_operand(x, M, K) || !good_operand(w, N, K) || !good_code(code) || tiles_of(M, K) < 0 || tiles_of(N, K) < 0 ||
+        tiles_of(M, N) < 0 || !aligned(kept, 16) || !aligned(temp, 16) || (M && N && (!y || !aligned(y, type_size(x->type)))))
+        return TULA_ERR_ARG;
+    unsigned char *k = static_cast<unsigned char *>(kept), *t = static_cast<unsigned char *>(temp);
+    Held xt, wt, qx, qw;
+    if (!take(k, K, M, need_dw, xt) || !take(k, K, N, need_dx, wt) || !take(t, M, K, true, qx) || !take(t, N, K, true, qw)) return TULA_ERR_ARG;
+    if ((k > static_cast<unsigned char *>(kept) && !kept) || (t > static_cast<unsigned char *>(temp) && !temp)) return TULA_ERR_WORKSPACE;
+    int rc = quantize(*x, M, K, code, 0, qx, xt, stream);
+    if (!rc) rc = quantize(*w, N, K, code, 1, qw, wt, stream);
+    if (!rc) rc = tula_fp8_matmul(qx.codes, qx.scales, code, qw.codes, qw.scales, code, M, N, K, y, x->type, stream);
+    return rc;
+}
+
+int tula_fp8_linear_backward(const tula_fp8_operand *dy, int64_t M, int64_t N, int64_t K, int code, int grad_code, const void *kept,
+                             void *temp, void *dx, int dx_type, void *dw, int dw_type, int need_dx, int need_dw, void *stream) {
+    if (!good_operand(dy, M, N) || !good_code(code) || !good_code(grad_code) || !good_type(dx_type) || !good_type(dw_type) ||
+        tiles_of(M, K) < 0 || tiles_of(N, K) < 0 || tiles_of(M, N) < 0 || !aligned(kept, 16) || !aligned(temp, 16) ||
+        (need_dx && M && K && (!dx || !aligned(dx, type_size(dx_type)))) || (need_dw && N && K && (!dw || !aligned(dw, type_size(dw_type)))))
+        return TULA_ERR_ARG;
+    unsigned char *k = static_cast<unsigned char *>(const_cast<void *>(kept)), *t = static_cast<unsigned char *>(temp);
+    Held xt, wt, rows, cols;
+    if (!take(k, K, M, need_dw, xt) || !take(k, K, N, need_dx, wt) || !take(t, M, N, need_dx, rows) || !take(t, N, M, need_dw, cols))
+        return TULA_ERR_ARG;
+    if ((k > static_cast<unsigned char *>(const_cast<void *>(kept)) && !kept) || (t > static_cast<unsigned char *>(temp) && !temp))
+        return TULA_ERR_WORKSPACE;
+    int rc = quantize(*dy, M, N, grad_code, 0, rows, cols, stream);
+    if (!rc && need_dx)  // dy [M, N] (w^T [K, N])^T
+        rc = tula_fp8_matmul(rows.codes, rows.scales, grad_code, wt.codes, wt.scales, code, M, K, N, dx, dx_type, stream);
+    if (!rc && need_dw)  // dy^T [N, M] (x^T [K, M])^T
+        rc = tula_fp8_matmul(cols.codes, cols.scales, grad_code, xt.codes, xt.scales, code, N, K, M, dw, dw_type, stream);
+    return rc;
 }
 
 int tula_fp8_error(void *stream, int *error_out) { return read_error(stream, error_out); }

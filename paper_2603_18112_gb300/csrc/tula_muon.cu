@@ -362,7 +362,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
     } else {
         const int quad = warp & 3, row = quad * 32 + lane, half = (warp - 2) >> 2;
-        constexpr int kChunks = S::kSide / kTileCols / 2;  // of 64 columns, a warp
+        constexpr int kChunks = S::kSide / kTileCols / (kReaders / 4);  // of 64 columns, a warp
         const uint32_t buffer = outs + (warp - 2) * 4096;
         auto buffer_free = [&] {  // the store that last used it has read it
             if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");

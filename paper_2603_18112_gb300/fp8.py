@@ -32,6 +32,10 @@ def _lib():
         L.tula_fp8_quantize.argtypes = [c_void_p, c_int, _i64, _i64, _i64, c_int, c_int] + [c_void_p] * 5
         L.tula_fp8_dequantize.argtypes = [c_void_p, c_void_p, _i64, _i64, c_int, c_void_p, c_int, c_void_p]
         L.tula_fp8_matmul.argtypes = [c_void_p, c_void_p, c_int] * 2 + [_i64] * 3 + [c_void_p, c_int, c_void_p]
+        operand = ctypes.POINTER(tula_fp8_operand)
+        L.tula_fp8_linear.argtypes = [operand, operand, _i64, _i64, _i64, c_int, c_int, c_int] + [c_void_p] * 4
+        L.tula_fp8_linear_backward.argtypes = [operand, _i64, _i64, _i64, c_int, c_int, c_void_p, c_void_p, c_void_p, c_int,
+                                               c_void_p, c_int, c_int, c_int, c_void_p]
         L.tula_fp8_error.argtypes = [c_void_p, ctypes.POINTER(c_int)]
         _fns = L
     return _fns
@@ -150,50 +154,66 @@ def matmul(a: FP8Matrix, b: FP8Matrix, dtype=torch.bfloat16) -> torch.Tensor:
     return out
 
 
-def _product(x, w, dtype):
-    """x w^T without what a backward pass wants."""
-    (m, k), n = x.shape, w.shape[0]
-    dev, x_kind, w_kind = _on_gpu(x, w), _type(x.dtype, "linear"), _type(w.dtype, "linear")
-    qx, qw = FP8Matrix.empty(m, k, x.device)._of(dtype), FP8Matrix.empty(n, k, w.device)._of(dtype)
-    _quantize_into(x, dev, x_kind, False, qx, None)
-    _quantize_into(w, dev, w_kind, True, qw, None)
-    return matmul(qx, qw, x.dtype)
+class tula_fp8_operand(ctypes.Structure):
+    """Mirror of the C struct tula_fp8_operand."""
+    _fields_ = [("data", c_void_p), ("stride", _i64), ("type", c_int), ("transposed", c_int)]
+
+
+def _operand(x, what):
+    """A matrix as the library takes it, and what has to live until the call."""
+    kind = _type(x.dtype, what)
+    (r, c), (stride, step) = x.shape, x.stride()
+    if step != 1 and stride == 1 and r > 1 and step >= r:  # it lies in memory as its transpose does
+        return tula_fp8_operand(x.data_ptr(), step, kind, 1), x
+    # a row of one element, or the only row, may have any stride
+    if c > 1 and step != 1 or r > 1 and stride < c:
+        x = x.contiguous()
+        stride = c
+    return tula_fp8_operand(x.data_ptr(), stride if r > 1 else c, kind, 0), x
+
+
+_bytes = FP8Matrix._bytes
+
+
+def _forward(x, w, dtype, need_x, need_w):
+    """x w^T, and what the backward pass multiplies by: x^T for dw, then w^T for dx, in 8 bits."""
+    (m, k), n, dev = x.shape, w.shape[0], _on_gpu(x, w)
+    (ox, x), (ow, w) = _operand(x, "linear"), _operand(w, "linear")
+    device = x.device
+    end = (_bytes(k, m) if need_w else 0) + (_bytes(k, n) if need_x else 0)
+    kept = torch.empty(end, dtype=torch.uint8, device=device)
+    temp = torch.empty(_bytes(m, k) + _bytes(n, k), dtype=torch.uint8, device=device)
+    y = torch.empty((m, n), dtype=x.dtype, device=device)
+    _call("tula_fp8_linear", dev, ox, ow, m, n, k, CODES[dtype], need_x, need_w, kept.data_ptr(), temp.data_ptr(), y.data_ptr())
+    return y, kept
 
 
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, dtype, grad_dtype):
         need_x, need_w = ctx.needs_input_grad[:2]
-        (m, k), n = x.shape, w.shape[0]
-        dev, x_kind, w_kind = _on_gpu(x, w), _type(x.dtype, "linear"), _type(w.dtype, "linear")
-        # what the backward pass multiplies by is kept in 8 bits: x^T for dw, then w^T for dx
-        ctx.types, ctx.sizes, ctx.device, ctx.codes = (x.dtype, w.dtype), (m, n, k), x.device, (dtype, grad_dtype)
-        ctx.at = at = FP8Matrix._bytes(k, m) if need_w else 0
-        ctx.end = end = at + (FP8Matrix._bytes(k, n) if need_x else 0)
-        kept = torch.empty(end, dtype=torch.uint8, device=x.device)
-        xt = FP8Matrix._within(kept, 0, k, m)._of(dtype) if need_w else None
-        wt = FP8Matrix._within(kept, at, k, n)._of(dtype) if need_x else None
-        qx = FP8Matrix.empty(m, k, x.device)._of(dtype)
-        qw = FP8Matrix.empty(n, k, w.device)._of(dtype)
-        _quantize_into(x, dev, x_kind, False, qx, xt)
-        _quantize_into(w, dev, w_kind, True, qw, wt)
+        y, kept = _forward(x, w, dtype, need_x, need_w)
+        ctx.types, ctx.sizes, ctx.codes = (x.dtype, w.dtype), (x.shape[0], *w.shape), (CODES[dtype], CODES[grad_dtype])
+        ctx.end, ctx.device = kept.numel(), x.device
         ctx.save_for_backward(kept)
-        return matmul(qx, qw, x.dtype)
+        return y
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
         kept, = ctx.saved_tensors
-        if kept.dtype != torch.uint8 or kept.numel() != ctx.end or kept.device != ctx.device or not kept.is_contiguous():
+        device = ctx.device
+        if kept.dtype != torch.uint8 or kept.numel() != ctx.end or kept.device != device or not kept.is_contiguous():
             raise RuntimeError("linear: a hook on saved tensors gave back another tensor than it was given")
-        (m, n, k), (need_x, need_w), (dtype, grad_dtype) = ctx.sizes, ctx.needs_input_grad[:2], ctx.codes
-        dx = dw = None
-        q = quantize(dy, rows=need_x, cols=need_w, dtype=grad_dtype)
-        rows, cols = q if need_x and need_w else (q, q)
-        if need_x:  # dy [M, N] (w^T [K, N])^T
-            dx = matmul(rows, FP8Matrix._within(kept, ctx.at, k, n)._of(dtype), ctx.types[0])
-        if need_w:  # dy^T [N, M] (x^T [K, M])^T
-            dw = matmul(cols, FP8Matrix._within(kept, 0, k, m)._of(dtype), ctx.types[1])
+        (m, n, k), (need_x, need_w), (x_type, w_type) = ctx.sizes, ctx.needs_input_grad[:2], ctx.types
+        dev = _on_gpu(dy, kept)
+        od, dy = _operand(dy, "linear")
+        temp = torch.empty((_bytes(m, n) if need_x else 0) + (_bytes(n, m) if need_w else 0), dtype=torch.uint8, device=device)
+        dx = torch.empty((m, k), dtype=x_type, device=device) if need_x else None
+        dw = torch.empty((n, k), dtype=w_type, device=device) if need_w else None
+        _call("tula_fp8_linear_backward", dev, od, m, n, k, *ctx.codes, kept.data_ptr(), temp.data_ptr(),
+              dx.data_ptr() if need_x else None, _type(x_type, "linear"), dw.data_ptr() if need_w else None,
+              _type(w_type, "linear"), need_x, need_w)
         return dx, dw, None, None
 
 
@@ -211,5 +231,5 @@ def linear(x: torch.Tensor, w: torch.Tensor, dtype=torch.float8_e4m3fn, grad_dty
     if torch.is_grad_enabled() and (x.requires_grad or w.requires_grad):
         y = _Linear.apply(rows, w, dtype, grad_dtype)
     else:
-        y = _product(rows, w, dtype)
+        y = _forward(rows, w, dtype, False, False)[0]
     return y if x.dim() == 2 else y.view(*x.shape[:-1], w.shape[0])

@@ -101,6 +101,24 @@ def test_refusals_of_the_library():
         assert product(**bad) == -1, bad
     assert L.tula_fp8_dequantize(p, p, 4, 4, 2, p, 0, n) == -1 and L.tula_fp8_dequantize(n, p, 4, 4, 0, p, 0, n) == -1
     assert L.tula_fp8_error(n, n) == -1
+
+    def layer(data=256, stride=128, kind=0, transposed=0, m=4, k=128, code=0, kept=p, temp=p, y=p):
+        x = fp8.tula_fp8_operand(data, stride, kind, transposed)
+        return L.tula_fp8_linear(x, fp8.tula_fp8_operand(256, 128, 0, 0), m, 4, k, code, 1, 1, kept, temp, y, n)
+
+    def back(data=256, stride=8, kind=0, transposed=0, code=0, grad_code=1, kept=p, temp=p, dx=p, dxt=0, dw=p, dwt=0):
+        dy = fp8.tula_fp8_operand(data, stride, kind, transposed)
+        return L.tula_fp8_linear_backward(dy, 4, 8, 128, code, grad_code, kept, temp, dx, dxt, dw, dwt, 1, 1, n)
+
+    for bad in ({"data": None}, {"data": 258}, {"stride": 127}, {"kind": 3}, {"transposed": 1, "stride": 3}, {"m": -1}, {"k": big}, {"code": 2}, {"y": n},
+                {"kept": ctypes.c_void_p(8)}, {"temp": ctypes.c_void_p(8)}, {"y": ctypes.c_void_p(258)}):
+        assert layer(**bad) == -1, bad
+    for bad in ({"data": None}, {"stride": 7}, {"kind": -1}, {"transposed": 1, "stride": 3}, {"code": -1}, {"grad_code": 2}, {"dx": n}, {"dw": n},
+                {"dxt": 3}, {"dwt": -1}, {"dw": ctypes.c_void_p(258)}, {"temp": ctypes.c_void_p(8)}):
+        assert back(**bad) == -1, bad
+    w = fp8.tula_fp8_operand(258, 128, 0, 0)  # (found before anything is enqueued)
+    assert L.tula_fp8_linear(fp8.tula_fp8_operand(256, 128, 0, 0), w, 4, 4, 128, 0, 1, 1, p, p, p, n) == -1
+    assert layer(kept=n) == layer(temp=n) == back(kept=n) == back(temp=n) == -2
     with pytest.raises(TulaError):
         fp8.tula_fp8_size(-1, 4)
 
@@ -318,6 +336,32 @@ def test_linear_forms():
     with pytest.raises(RuntimeError):  # no second derivative
         g, = torch.autograd.grad(fp8.linear(x, w).sum(), (x,), create_graph=True)
         g.sum().backward()
+
+
+@pytest.mark.gpu
+def test_linear_of_views():
+    """Operands that lie transposed or apart, gradients of strides 0, another than the current device's order."""
+    x = torch.randn(260, 150, device="cuda", dtype=torch.bfloat16)
+    w = torch.randn(300, 150, device="cuda")
+    dy = torch.randn(260, 300, device="cuda", dtype=torch.bfloat16)
+
+    def run(x, w, dy):
+        x, w = x.detach().requires_grad_(), w.detach().requires_grad_()
+        y = fp8.linear(x, w)
+        return (y.detach(), *torch.autograd.grad(y, (x, w), dy))
+
+    want = run(x, w, dy)
+    wide = torch.randn(260, 190, device="cuda", dtype=torch.bfloat16)
+    wide[:, 11:161] = x
+    for forms in ((x.t().contiguous().t(), w.t().contiguous().t(), dy.t().contiguous().t()), (wide[:, 11:161], w, dy),
+                  (x.repeat_interleave(2, 1)[:, ::2], w, dy)):
+        assert all(torch.equal(a, b) for a, b in zip(run(*forms), want))
+    ones = torch.ones(260, 300, device="cuda", dtype=torch.bfloat16)
+    assert all(torch.equal(a, b) for a, b in zip(run(x, w, torch.ones((), device="cuda", dtype=torch.bfloat16).expand(260, 300)), run(x, w, ones)))
+    col = run(x[:, :1], w[:, :1], dy)  # of one column, one row, one output
+    assert torch.equal(col[0], run(x[:, :1].contiguous(), w[:, :1].contiguous(), dy)[0])
+    assert torch.equal(run(x[:1], w, dy[:1])[0], fp8.linear(x[:1].contiguous(), w))
+    assert run(x, w[:1], dy[:, :1])[2].shape == (1, 150)
 
 
 @pytest.mark.gpu
