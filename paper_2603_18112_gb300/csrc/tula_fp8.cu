@@ -44,8 +44,8 @@ __device__ __forceinline__ unsigned codes4(float a, float b, float c, float d) {
 // magnitude together.  The transpose reads the tile again from shared memory, four lanes to a word's columns
 // (one column of fp32, two of others), 32 rows each: they find the columns' largest magnitudes by two
 // exchanges and write 128 bytes of codes to each column, so that one barrier is enough.  (With the tops and
-// codes of columns by way of shared memory and two barriers more, 8192 x 4096 bf16 took 30 us in both forms
-// instead of BOTHUS.)  fp32 rows off 32-byte boundaries come word by word, a warp to a row, and through
+// codes of columns by way of shared memory and two barriers more, 8192 x 4096 bf16 took 29 us in both forms
+// instead of 23.)  fp32 rows off 32-byte boundaries come word by word, a warp to a row, and through
 // shared memory too.  HBM bounds it: 2 or 4 bytes in and one out per element and form.
 
 struct QuantArgs {

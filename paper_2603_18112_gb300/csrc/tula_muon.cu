@@ -85,20 +85,20 @@ static_assert(sizeof(ProductArgs) <= 4096 - 3 * 128 - 64, "kernel parameters");
 
 // What is made of the sums: alpha times them, of a symmetric product (its blocks on and above the diagonal are
 // taken, and stored twice); the polynomial, symmetric too; alpha times them; the same of the last step, which
-// goes straight to the weights.  (That is bound by HBM then, with the tensor cores two thirds as busy, but by
-// LASTUS us for 151 M weights instead of 184 and 299 one after the other.)
+// goes straight to the weights.  (HBM bounds that: 359 us for 151 M weights in place of 176 and 299 one after the
+// other.)
 enum Kind { kGram, kPoly, kApply, kLast };
 
 // A copying warp, an issuing warp, and those that read back: two to each quarter of tensor memory's lanes, each
-// with half of the columns.  (With one to a quarter the sums of 1024 columns were read back more slowly than
-// they were made: 72 matrices, three products of n = 1024 each, took 2.19 ms instead of PRODMS.)
+// with half of the columns (72 matrices of 151 M elements, most sums of 1024: 2.66 to 2.71 ms, 2.72 to 2.78 with one
+// to a quarter).
 constexpr int kReaders = 8;
 constexpr int kThreads = 64 + 32 * kReaders;
 
 template <bool Pair>
 struct Shape {
     static constexpr int kSide = Pair ? 256 : 128;  // of a block of the output
-    static constexpr int kStages = 6;  // (what is on its way bounds the rate: with five, 4096 x 4096 took SLOW us, FAST so)
+    static constexpr int kStages = 6;  // (what is on its way bounds the rate: X' of 151 M in 176 us, 184 with five)
     static constexpr int kOperand = 128 * 128;      // bytes of a stage, a CTA
     static constexpr int kStage = 2 * kOperand;
     static constexpr int kOuts = kReaders * 4096;   // a buffer a warp
@@ -132,7 +132,7 @@ __device__ __forceinline__ void mma16(uint32_t d, uint64_t a, uint64_t b, uint32
 
 // The blocks in the order of their groups, those with the longest sums first, go round the workers; those that
 // the first groups, of equal sums, leave with one more than the others are passed over for a.skip rounds of what follows, about
-// as long as that one takes.  (72 matrices, sums of 4096 and of 1024: A in GRAM1US us, GRAM0US without.)
+// as long as that one takes.  (72 matrices, sums of 4096 and of 1024: A in 108 us, 119 without.)
 __device__ __forceinline__ int block_of(const ProductArgs &a, int worker, int workers, int i) {
     const int full = a.n_first / workers, more = a.n_first - full * workers;
     if (i < full) return i * workers + worker;
@@ -860,7 +860,7 @@ __global__ void __launch_bounds__(kStreamThreads, kStreamCtas) k_muon_last(const
 //
 // One CTA a matrix whose smaller side is at most 128 and whose tiles, at most twelve, shared memory holds beside
 // those of A, which B takes the place of.  Nothing leaves the SM between the first reading and the last
-// writing: one launch and some 4 us a step instead of three launches and 18 (64 x 576: SMALLUS us in all, 105 by
+// writing: one launch and some 4 us a step instead of three launches and 19 (64 x 576: 38 us in all, 102 by
 // the products above).  The tiles have the image that the copies give them there.  One thread issues a
 // product, all eight warps read it back.
 
@@ -1169,17 +1169,13 @@ struct Kin {
     int shift() const { return std::min(15, (int)std::floor(0.5 * std::log2((double)rows * (double)cols))); }
 };
 
-// Whether the list is k_muon_small's: where no matrix is larger (else the products take the small ones along at no
-// cost: 16 matrices of 17 to 700 rows and columns took 227 us in two ways, 164 in one) and for up to two matrices an
-// SM (64 of 100 x 300: 52 us, 105 by products; 1000: MANYUS).
-constexpr int kSmallMost = 2 * 152;
+// Whether the list is k_muon_small's: where no matrix is larger (304 of 100 x 300 in 118 us, by products 225; 304 of
+// 128 x 768 in 154, 374).  Else the products take the small ones along: 16 matrices of 17 to 700 rows and
+// columns took 227 us by both, 160 by products alone.
 bool all_small(const std::vector<Kin> &kin) {
-    long long count = 0;
-    for (const Kin &k : kin) {
+    for (const Kin &k : kin)
         if (!k.fits()) return false;
-        count += k.count;
-    }
-    return count <= kSmallMost;
+    return true;
 }
 
 bool good_shape(long long rows, long long cols) { return rows >= 0 && cols >= 0 && rows <= kMostSide && cols <= kMostSide; }
