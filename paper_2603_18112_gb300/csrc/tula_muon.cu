@@ -44,12 +44,22 @@ constexpr long long kMostTiles = 1LL << 24;  // of a workspace: rows of 128 byte
 // Products
 // ----------------------------------------------------------------------------
 
-// An operand of 128 (or 256, by pairs) rows of the product's side: in tiles of `pitch` to a row of them.
-// along: the sum runs along the tiles' columns (K-major); else along their rows.
+// An operand of 128 (or 256, by pairs) rows of the product's side: in tiles of `pitch` to a row of them.  The sum
+// runs along the tiles' columns (K-major) or along their rows; of a symmetric matrix, of which the blocks on
+// and above the diagonal are there, along rows up to the diagonal and along columns from there on.  (With the
+// blocks below it written too, transposed by way of shared memory, A of 72 matrices took 108 us instead of MIRA,
+// 256 x 256 MIRB us instead of MIRC.)
+enum Way { kAcross, kAlong, kSymmetric };
 struct Side {
     int base, step;   // the first matrix's first tile, tiles from matrix to matrix
     int pitch, rows;  // tiles
-    int along;
+    int way;
+    // The first stage that runs along the columns, of the operand of block `block` of kSide.  (Symmetric ones are
+    // there by blocks of 256, whatever kSide made them.)
+    template <int kSide>
+    __device__ __forceinline__ int turn(int block) const {
+        return way == kAlong ? 0 : way == kAcross ? 1 << 30 : block * kSide / 256 * 4;
+    }
 };
 struct Matrix {  // of a plan
     const void *g;
@@ -81,10 +91,10 @@ struct ProductArgs {
     int none;         // a row beyond the workspace
     ProductGroup g[kMostGroups];
 };
-static_assert(sizeof(ProductArgs) <= 4096 - 3 * 128 - 64, "kernel parameters");
+static_assert(sizeof(ProductArgs) <= 4096 - 2 * 128 - 64, "kernel parameters");
 
 // What is made of the sums: alpha times them, of a symmetric product (its blocks on and above the diagonal are
-// taken, and stored twice); the polynomial, symmetric too; alpha times them; the same of the last step, which
+// taken); the polynomial, symmetric too; alpha times them; the same of the last step, which
 // goes straight to the weights.  (HBM bounds that: 359 us for 151 M weights in place of 176 and 299 one after the
 // other.)
 enum Kind { kGram, kPoly, kApply, kLast };
@@ -148,7 +158,12 @@ __device__ __forceinline__ int block_of(const ProductArgs &a, int worker, int wo
 struct Block {
     int matrix, m, n;
 };
-template <Kind K>
+// A symmetric product's blocks in column n: those on and above the diagonal, by 256.
+template <int kSide>
+__host__ __device__ constexpr int column_blocks(int n, int blocks) {
+    return kSide == 256 ? n + 1 : (n | 1) + 1 < blocks ? (n | 1) + 1 : blocks;
+}
+template <Kind K, int kSide>
 __device__ __forceinline__ Block block_at(const ProductArgs &a, int t, const ProductGroup *&g) {
     int i = 0;
     while (i + 1 < a.n_groups && t >= a.g[i + 1].first) ++i;
@@ -160,9 +175,9 @@ __device__ __forceinline__ Block block_at(const ProductArgs &a, int t, const Pro
     if (K >= kApply) {
         b.m = k % g->blocks_m;
         b.n = k / g->blocks_m;
-    } else {  // columns of the upper triangle
+    } else {
         b.n = 0;
-        while (k > b.n) k -= ++b.n;
+        while (k >= column_blocks<kSide>(b.n, g->blocks_n)) k -= column_blocks<kSide>(b.n++, g->blocks_n);
         b.m = k;
     }
     return b;
@@ -172,26 +187,31 @@ __device__ __forceinline__ Block block_at(const ProductArgs &a, int t, const Pro
 // the compiler may not move loads across, and with the group's fields read again for each stage the copying
 // warp took some 800 cycles to one.
 struct Walk {
-    unsigned row0, row1;  // of the two halves of stage 0; none where there are none
-    unsigned odd, even;   // rows from an even stage to the odd one after it, and from there to the next
-    __device__ __forceinline__ Walk(const Side &s, int matrix, int i, unsigned none) {
+    unsigned row0, row1;      // of the two halves of a stage; none where there are none
+    unsigned odd, even;       // rows from an even stage to the odd one after it, and from there to the next
+    unsigned along0, along1;  // of stage `turn`
+    int turn;
+    __device__ __forceinline__ Walk(const Side &s, int matrix, int i, int first_along, unsigned none) : turn(first_along) {
         const int first = s.base + matrix * s.step;
-        if (s.along) {
-            row0 = i < s.rows ? (first + i * s.pitch) * kTile : none;
-            row1 = row0 == none ? none : row0 + 64;
-            odd = even = kTile;
-        } else {
-            row0 = 2 * i < s.pitch ? (first + 2 * i) * kTile : none;
-            row1 = 2 * i + 1 < s.pitch ? (first + 2 * i + 1) * kTile : none;
-            odd = 64;
-            even = s.pitch * kTile - 64;
-        }
+        along0 = i < s.rows ? (first + i * s.pitch + (turn < s.pitch ? turn : 0)) * kTile : none;
+        along1 = along0 == none ? none : along0 + 64;
+        row0 = 2 * i < s.pitch ? (first + 2 * i) * kTile : none;
+        row1 = 2 * i + 1 < s.pitch ? (first + 2 * i + 1) * kTile : none;
+        odd = 64;
+        even = s.pitch * kTile - 64;
+        if (turn == 0) columns();
         // (none and what comes after it lie beyond the workspace, also as negative coordinates)
+    }
+    __device__ __forceinline__ void columns() {
+        row0 = along0;
+        row1 = along1;
+        odd = even = kTile;
     }
     __device__ __forceinline__ void next(int k) {
         const unsigned by = k & 1 ? even : odd;
         row0 += by;
         row1 += by;
+        if (k + 1 == turn) columns();
     }
 };
 
@@ -229,7 +249,7 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap *map) { asm volat
 template <bool Pair, Kind K>
 __global__ void __launch_bounds__(kThreads, 1)
     k_product(const __grid_constant__ CUtensorMap map_in, const __grid_constant__ CUtensorMap map_out,
-              const __grid_constant__ CUtensorMap map_mirror, const __grid_constant__ ProductArgs a) {
+              const __grid_constant__ ProductArgs a) {
     using S = Shape<Pair>;
     extern __shared__ __align__(16) unsigned char raw[];
     unsigned char *all = raw + (-smem_addr(raw) & 1023u);
@@ -254,10 +274,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0 && elect_one()) prefetch_map(&map_in);
-    if (warp == 2 && elect_one()) {
-        prefetch_map(&map_out);
-        if (K < kApply) prefetch_map(&map_mirror);
-    }
+    if (warp == 2 && elect_one()) prefetch_map(&map_out);
     if (warp == 1) {
         if (Pair) {
             asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_at)), "r"(S::kCols)
@@ -275,7 +292,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     let_next_start();
     {  // the first block's parameters are on their way while the kernel before ends
         const ProductGroup *g;
-        const Block b = block_at<K>(a, min(worker, a.n_blocks - 1), g);
+        const Block b = block_at<K, S::kSide>(a, min(worker, a.n_blocks - 1), g);
         asm volatile("" ::"r"(g->n_k), "r"(b.matrix), "r"(g->out), "r"(g->q.base) : "memory");
     }
     wait_for_previous();
@@ -287,9 +304,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         bool ok = true;
         for (int at = 0, t; ok && (t = block_of(a, worker, workers, at)) < n_blocks; ++at) {
             const ProductGroup *g;
-            const Block b = block_at<K>(a, t, g);
+            const Block b = block_at<K, S::kSide>(a, t, g);
             const int n_k = g->n_k;
-            Walk p(g->p, b.matrix, Pair ? 2 * b.m + rank : b.m, a.none), q(g->q, b.matrix, Pair ? 2 * b.n + rank : b.n, a.none);
+            Walk p(g->p, b.matrix, Pair ? 2 * b.m + rank : b.m, g->p.turn<S::kSide>(b.m), a.none);
+            Walk q(g->q, b.matrix, Pair ? 2 * b.n + rank : b.n, g->q.turn<S::kSide>(b.n), a.none);
             for (int k = 0; k < n_k; ++k, ++i) {
                 const int s = i % S::kStages;
                 if (i >= S::kStages) ok = __all_sync(kFull, mbar_wait(empty + 8 * s, (i / S::kStages - 1) & 1, &dead));
@@ -328,12 +346,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             bool ok = true;
             for (int t; ok && (t = block_of(a, worker, workers, n)) < n_blocks; ++n) {
                 const ProductGroup *g;
-                block_at<K>(a, t, g);
-                const bool pa = g->p.along, qa = g->q.along;
-                const int n_k = g->n_k;
-                const uint32_t idesc = product_desc(S::kSide, S::kSide, pa, qa);
-                // from one instruction's 16 of the sum to the next: 32 bytes of a row, or 16 rows
-                const uint32_t p_next = pa ? 2 : 128, q_next = qa ? 2 : 128;
+                const Block b = block_at<K, S::kSide>(a, t, g);
+                const int n_k = g->n_k, p_turn = g->p.turn<S::kSide>(b.m), q_turn = g->q.turn<S::kSide>(b.n);
                 if (n > 1) ok = __all_sync(kFull, mbar_wait(acc_free + 8 * (n & 1), (n / 2 - 1) & 1, &dead));
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t acc = tmem + (n & 1) * S::kSide;
@@ -343,6 +357,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint32_t at = stages + s * S::kStage;
+                    const bool pa = k >= p_turn, qa = k >= q_turn;
+                    const uint32_t idesc = product_desc(S::kSide, S::kSide, pa, qa);
+                    // from one instruction's 16 of the sum to the next: 32 bytes of a row, or 16 rows
+                    const uint32_t p_next = pa ? 2 : 128, q_next = qa ? 2 : 128;
                     const uint64_t dp = operand_desc(at, pa), dq = operand_desc(at + S::kOperand, qa);
                     if (elect_one()) {
 #pragma unroll
@@ -371,62 +389,53 @@ __global__ void __launch_bounds__(kThreads, 1)
         int n = 0;
         for (int t; (t = block_of(a, worker, workers, n)) < n_blocks; ++n) {
             const ProductGroup *g;
-            const Block b = block_at<K>(a, t, g);
+            const Block b = block_at<K, S::kSide>(a, t, g);
             const int im = Pair ? 2 * b.m + rank : b.m;
             const int out = g->out + b.matrix * g->out_step;
             const int j0 = b.n * (S::kSide / kTileCols) + half * kChunks;  // column of tiles
             const int out_pitch = g->out_pitch;
             const int chunks = im < g->out_rows ? max(0, min(kChunks, out_pitch - j0)) : 0;  // within the output
-            const bool twice = K < kApply && b.m != b.n;
             const float alpha = g->alpha, step = g->step;
-            const int diagonal = K == kPoly && row + im * kTile < g->n ? row + im * kTile : -1;
-            const unsigned char *const added =  // kPoly: A's rows
+            // kPoly: A's rows come to the buffer, each lane's own, and B takes their place there
+            const unsigned char *const added =
                 a.tiles + (size_t)(g->p.base + b.matrix * g->p.step + im * g->p.pitch + j0) * kTileBytes + row * 128;
-            unsigned add[32];
             auto fetch = [&](int c) {
-                const unsigned char *from = added + (size_t)c * kTileBytes;
+                buffer_free();
 #pragma unroll
-                for (int k = 0; k < 32; k += 8)
-                    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                                 : "=r"(add[k]), "=r"(add[k + 1]), "=r"(add[k + 2]), "=r"(add[k + 3]), "=r"(add[k + 4]),
-                                   "=r"(add[k + 5]), "=r"(add[k + 6]), "=r"(add[k + 7])
-                                 : "l"(from + 4 * k));
+                for (int k = 0; k < 8; ++k)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(buffer + lane * 128 + ((k ^ (lane & 7)) << 4)),
+                                 "l"(added + (size_t)c * kTileBytes + 16 * k)
+                                 : "memory");
             };
             if (K == kPoly && chunks) fetch(0);
             const bool finish = K == kLast && g->finish;
-            if (finish) buffer_free();  // (of a block of another group)
-            // (the weights move by four lanes to 32 columns of a row)
-            const int first_row = im * kTile + quad * 32 + (lane >> 2), cols = g->cols, rows_left = g->rows - first_row;
-            Matrix q = {};
-            if (finish && a.matrices) q = a.matrices[g->matrix + b.matrix];
-            if (!__all_sync(kFull, mbar_wait(acc_full + 8 * (n & 1), (n / 2) & 1, &dead))) break;
+            if (!__all_sync(kFull, mbar_wait(acc_full + 8 * (n & 1), (n / 2) & 1, &dead))) {
+                if (K == kPoly) asm volatile("cp.async.wait_all;" ::: "memory");
+                break;
+            }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t acc = tmem + (n & 1) * S::kSide + half * kChunks * kTileCols + ((unsigned)(quad * 32) << 16);
+            if constexpr (K == kLast) {
+                if (finish) {
+                    // the weights move by four lanes to 32 columns of a row
+                    const int first_row = im * kTile + quad * 32 + (lane >> 2), cols = g->cols, rows_left = g->rows - first_row;
+                    Matrix q = {};
+                    if (a.matrices) q = a.matrices[g->matrix + b.matrix];
+                    buffer_free();  // (of a block of another group)
 #pragma unroll 1
-            for (int c = 0; c < kChunks; ++c) {
-                const int j = j0 + c;
-                unsigned v[64];
-                tmem_load32(v, acc + c * kTileCols);
-                tmem_load32(v + 32, acc + c * kTileCols + 32);
-                const int col = j * kTileCols + (lane & 3) * 8;  // and 32 further on
-                const bool mine = finish && c < chunks;
-                float w[K == kLast ? 64 : 1];
-                if constexpr (K == kLast)
-                    if (q.w && mine) {
+                    for (int c = 0; c < chunks; ++c) {
+                        const int col = (j0 + c) * kTileCols + (lane & 3) * 8;  // and 32 further on
+                        unsigned v[64];
+                        tmem_load32(v, acc + c * kTileCols);
+                        tmem_load32(v + 32, acc + c * kTileCols + 32);
+                        float w[64];
+                        if (q.w) {
 #pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            if (8 * (k & 3) < rows_left && col + 8 * (k & 4) < cols)
-                                load8(w + 8 * k, q.w + (size_t)(first_row + 8 * (k & 3)) * cols + col + 8 * (k & 4));
-                    }
-                tmem_wait(v);
-                if (c == kChunks - 1) {
-                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) arrive_cluster(Pair ? in_cta(acc_free + 8 * (n & 1), 0) : acc_free + 8 * (n & 1));
-                }
-                if (c >= chunks) continue;
-                if constexpr (K == kLast) {
-                    if (finish) {
+                            for (int k = 0; k < 8; ++k)
+                                if (8 * (k & 3) < rows_left && col + 8 * (k & 4) < cols)
+                                    load8(w + 8 * k, q.w + (size_t)(first_row + 8 * (k & 3)) * cols + col + 8 * (k & 4));
+                        }
+                        tmem_wait(v);
                         // the values change from a row a lane to a row four lanes, 32 rows of 32 columns at a
                         // time, their 32-byte pieces exchanged so that neither way meets in a bank
 #pragma unroll
@@ -469,58 +478,65 @@ __global__ void __launch_bounds__(kThreads, 1)
                                 }
                             }
                         }
-                        continue;
                     }
                 }
-                unsigned y[32];
-#pragma unroll
-                for (int k = 0; k < 32; ++k) {
-                    float lo = __uint_as_float(v[2 * k]), hi = __uint_as_float(v[2 * k + 1]);
+            }
+            // (rolled: unrolled over 64 columns, the instructions of a launch's only block came from L2 for some 3 us)
+#pragma unroll 1
+            for (int c = 0; c < chunks && !finish; ++c) {
+                if (K != kPoly)
+                    buffer_free();
+                else if (c)
+                    fetch(c);
+                const int diagonal = im * kTile + row < g->n ? im * kTile + row - (j0 + c) * kTileCols : -1;
+#pragma unroll 1
+                for (int h = 0; h < 4; ++h) {
+                    float f[16];
+                    tmem_load16(f, acc + c * kTileCols + 16 * h);
+                    const uint32_t at0 = buffer + lane * 128 + ((2 * h ^ (lane & 7)) << 4), at1 = buffer + lane * 128 + ((2 * h + 1 ^ (lane & 7)) << 4);
                     if (K == kPoly) {
-                        __half2 h;
-                        memcpy(&h, &add[k], 4);
-                        const float2 f = __half22float2(h);
-                        const int col = diagonal - j * kTileCols;
-                        lo = fmaf((float)kC, lo, fmaf((float)kB, f.x, col == 2 * k ? (float)kA : 0.f));
-                        hi = fmaf((float)kC, hi, fmaf((float)kB, f.y, col == 2 * k + 1 ? (float)kA : 0.f));
-                    } else {
-                        lo *= alpha;
-                        hi *= alpha;
-                    }
-                    const __half2 h = __floats2half2_rn(lo, hi);
-                    memcpy(&y[k], &h, 4);
-                }
-                if (K == kPoly && c + 1 < chunks) fetch(c + 1);
-                buffer_free();
+                        if (h == 0) asm volatile("cp.async.wait_all;" ::: "memory");
+                        unsigned add[8];
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                     : "=r"(add[0]), "=r"(add[1]), "=r"(add[2]), "=r"(add[3])
+                                     : "r"(at0)
+                                     : "memory");
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                     : "=r"(add[4]), "=r"(add[5]), "=r"(add[6]), "=r"(add[7])
+                                     : "r"(at1)
+                                     : "memory");
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buffer + lane * 128 + ((k ^ (lane & 7)) << 4)),
-                                 "r"(y[4 * k]), "r"(y[4 * k + 1]), "r"(y[4 * k + 2]), "r"(y[4 * k + 3])
-                                 : "memory");
+                        for (int k = 0; k < 8; ++k) {
+                            __half2 v;
+                            memcpy(&v, &add[k], 4);
+                            const float2 e = __half22float2(v);
+                            f[2 * k] = fmaf((float)kC, f[2 * k], fmaf((float)kB, e.x, diagonal == 16 * h + 2 * k ? (float)kA : 0.f));
+                            f[2 * k + 1] = fmaf((float)kC, f[2 * k + 1], fmaf((float)kB, e.y, diagonal == 16 * h + 2 * k + 1 ? (float)kA : 0.f));
+                        }
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) f[k] *= alpha;
+                    }
+                    unsigned y[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const __half2 v = __floats2half2_rn(f[2 * k], f[2 * k + 1]);
+                        memcpy(&y[k], &v, 4);
+                    }
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at0), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at1), "r"(y[4]), "r"(y[5]), "r"(y[6]), "r"(y[7]) : "memory");
+                }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0)
                     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];\n"
                                  "cp.async.bulk.commit_group;" ::"l"(&map_out),
-                                 "r"(0), "r"((out + im * out_pitch + j) * kTile + quad * 32), "r"(buffer)
-                                 : "memory");
-                if (!twice) continue;
-                buffer_free();
-#pragma unroll
-                for (int k = 0; k < 32; ++k) {
-                    asm volatile("st.shared.b16 [%0], %1;" ::"r"(buffer + 128 * k + 2 * lane), "h"((unsigned short)y[k]) : "memory");
-                    asm volatile("st.shared.b16 [%0], %1;" ::"r"(buffer + 128 * k + 64 + 2 * lane), "h"((unsigned short)(y[k] >> 16))
-                                 : "memory");
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0)
-                    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];\n"
-                                 "cp.async.bulk.commit_group;" ::"l"(&map_mirror),
-                                 "r"(32 * (quad & 1)), "r"((out + (j >> 1) * out_pitch + 2 * im + (quad >> 1)) * kTile + 64 * (j & 1)),
-                                 "r"(buffer)
+                                 "r"(0), "r"((out + im * out_pitch + j0 + c) * kTile + quad * 32), "r"(buffer)
                                  : "memory");
             }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) arrive_cluster(Pair ? in_cta(acc_free + 8 * (n & 1), 0) : acc_free + 8 * (n & 1));
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         __syncwarp();
@@ -1202,13 +1218,12 @@ long long stream_tiles(const Kin *kin, int n) {
 }
 
 struct Maps {
-    CUtensorMap in, out, mirror;
+    CUtensorMap in, out;
 };
 bool make_maps(Maps &m, const void *tiles, long long n) {
     const CUtensorMapDataType f16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     return make_map(&m.in, f16, tiles, n * kTile, kTileCols, 128, 64, kTileCols, CU_TENSOR_MAP_SWIZZLE_128B) &&
-           make_map(&m.out, f16, tiles, n * kTile, kTileCols, 128, 32, kTileCols, CU_TENSOR_MAP_SWIZZLE_128B) &&
-           make_map(&m.mirror, f16, tiles, n * kTile, kTileCols, 128, 64, 32, CU_TENSOR_MAP_SWIZZLE_NONE);
+           make_map(&m.out, f16, tiles, n * kTile, kTileCols, 128, 32, kTileCols, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 template <bool Pair, Kind K>
@@ -1228,7 +1243,7 @@ int launch_product(const Maps &maps, ProductArgs &a, int sms, cudaStream_t s) {
         a.skip = std::min(rounds, rest / (workers - more));  // whole rounds of those that are left
     }
     return tula::launch(k_product<Pair, K>, dim3((unsigned)(workers * (Pair ? 2 : 1))), kThreads, S::kSmem, s, Pair ? 2 : 1, maps.in,
-                        maps.out, maps.mirror, a);
+                        maps.out, a);
 }
 
 // One product of all shapes.  x: X's first tiles are x0 (0) or x1 (1); first: of the first step.
@@ -1240,11 +1255,11 @@ int fill(ProductArgs &a, const Kin *kin, int n, Kind kind, int x, bool first) {
     for (int i = 0; i < n; ++i) {
         const Kin &k = kin[i];
         ProductGroup &g = a.g[i];
-        const Side sx = {x ? k.x1 : k.x0, k.tiles(), k.tile_cols(), k.tile_rows(), 1};
-        const Side sa = {k.gram, k.gram_tiles(), k.gram_cols(), k.gram_rows(), 1};
-        const Side sb = {k.poly, k.gram_tiles(), k.gram_cols(), k.gram_rows(), 1};
+        const Side sx = {x ? k.x1 : k.x0, k.tiles(), k.tile_cols(), k.tile_rows(), kAlong};
+        const Side sa = {k.gram, k.gram_tiles(), k.gram_cols(), k.gram_rows(), kSymmetric};
+        const Side sb = {k.poly, k.gram_tiles(), k.gram_cols(), k.gram_rows(), kSymmetric};
         Side across = sx;
-        across.along = 0;
+        across.way = kAcross;
         g.n = (int)k.n();
         g.alpha = 1.f;
         g.finish = kind == kLast && k.vec;
@@ -1271,7 +1286,10 @@ int fill(ProductArgs &a, const Kin *kin, int n, Kind kind, int x, bool first) {
             g.out_pitch = k.gram_cols();
             g.out_rows = k.gram_rows();
             g.blocks_m = g.blocks_n = (int)up(k.n(), kSide);
-            g.per = (int)((long long)g.blocks_m * (g.blocks_m + 1) / 2);
+            long long per = 0;
+            for (int c = 0; c < g.blocks_n; ++c) per += column_blocks<kSide>(c, g.blocks_n);
+            if (per >= (1LL << 30)) return -1;
+            g.per = (int)per;
             g.n_k = (int)up(kind == kPoly ? k.n() : std::max(k.rows, k.cols), 64);
             if (first && kind == kGram) g.alpha = (float)std::ldexp(1.0, -2 * k.shift());
         }
