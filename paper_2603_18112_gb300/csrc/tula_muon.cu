@@ -290,30 +290,38 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = __shfl_sync(kFull, *tmem_at, 0);
     let_next_start();
-    {  // the first block's parameters are on their way while the kernel before ends
-        const ProductGroup *g;
-        const Block b = block_at<K, S::kSide>(a, min(worker, a.n_blocks - 1), g);
-        asm volatile("" ::"r"(g->n_k), "r"(b.matrix), "r"(g->out), "r"(g->q.base) : "memory");
-    }
-    wait_for_previous();
-    const bool go = !a.record || a.record[TULA_RECORD_FINITE] != 0.f;
-    const int n_blocks = go ? a.n_blocks : 0;
+    // Each role goes through its loop once before it waits for the kernel ahead, without what the others or memory
+    // would see of it: so its instructions and the first block's parameters are there when the wait ends.  (A
+    // launch's instructions come from L2, some 200 cycles to eight of them: of 6.2 us that a product of 256 x 256
+    // took, reading back took 2 to 4.)
+    auto blocks_after_wait = [&] {
+        wait_for_previous();
+        return !a.record || a.record[TULA_RECORD_FINITE] != 0.f ? a.n_blocks : 0;
+    };
+    int n_blocks = 0;
 
     if (warp == 0) {
         int i = 0;  // stages filled
-        bool ok = true;
-        for (int at = 0, t; ok && (t = block_of(a, worker, workers, at)) < n_blocks; ++at) {
+        bool ok = true, dry = true;
+#pragma unroll 1
+        for (int at_block = 0; ok;) {
+            int t = block_of(a, worker, workers, at_block);
+            if (dry)
+                t = min(t, a.n_blocks - 1);
+            else if (t >= n_blocks)
+                break;
             const ProductGroup *g;
             const Block b = block_at<K, S::kSide>(a, t, g);
-            const int n_k = g->n_k;
+            const int n_k = dry ? 1 : g->n_k;
             Walk p(g->p, b.matrix, Pair ? 2 * b.m + rank : b.m, g->p.turn<S::kSide>(b.m), a.none);
             Walk q(g->q, b.matrix, Pair ? 2 * b.n + rank : b.n, g->q.turn<S::kSide>(b.n), a.none);
-            for (int k = 0; k < n_k; ++k, ++i) {
+#pragma unroll 1
+            for (int k = 0; k < n_k; ++k) {
                 const int s = i % S::kStages;
                 if (i >= S::kStages) ok = __all_sync(kFull, mbar_wait(empty + 8 * s, (i / S::kStages - 1) & 1, &dead));
                 if (!ok) break;
                 const uint32_t at = stages + s * S::kStage, bar = Pair ? in_cta(full + 8 * s, 0) : full + 8 * s;
-                if (elect_one()) {
+                if (elect_one() && !dry) {
                     if (rank == 0) mbar_expect(full + 8 * s, (Pair ? 2 : 1) * S::kStage);  // both CTAs' copies
                     if (Pair) {
                         tma_load_pair(at, &map_in, 0, (int)p.row0, bar);
@@ -330,6 +338,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                 __syncwarp();
                 p.next(k);
                 q.next(k);
+                if (!dry) ++i;
+            }
+            if (dry) {
+                dry = false;
+                n_blocks = blocks_after_wait();
+            } else {
+                ++at_block;
             }
         }
         // The issuing warp's arrivals (of the other CTA too) have all landed before the CTA ends.
@@ -343,17 +358,24 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else if (warp == 1) {
         if (rank == 0) {
             int i = 0, n = 0;
-            bool ok = true;
-            for (int t; ok && (t = block_of(a, worker, workers, n)) < n_blocks; ++n) {
+            bool ok = true, dry = true;
+#pragma unroll 1
+            for (; ok;) {
+                int t = block_of(a, worker, workers, n);
+                if (dry)
+                    t = min(t, a.n_blocks - 1);
+                else if (t >= n_blocks)
+                    break;
                 const ProductGroup *g;
                 const Block b = block_at<K, S::kSide>(a, t, g);
-                const int n_k = g->n_k, p_turn = g->p.turn<S::kSide>(b.m), q_turn = g->q.turn<S::kSide>(b.n);
+                const int n_k = dry ? 1 : g->n_k, p_turn = g->p.turn<S::kSide>(b.m), q_turn = g->q.turn<S::kSide>(b.n);
                 if (n > 1) ok = __all_sync(kFull, mbar_wait(acc_free + 8 * (n & 1), (n / 2 - 1) & 1, &dead));
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t acc = tmem + (n & 1) * S::kSide;
-                for (int k = 0; ok && k < n_k; ++k, ++i) {
+#pragma unroll 1
+                for (int k = 0; ok && k < n_k; ++k) {
                     const int s = i % S::kStages;
-                    ok = __all_sync(kFull, mbar_wait(full + 8 * s, (i / S::kStages) & 1, &dead));
+                    if (!dry) ok = __all_sync(kFull, mbar_wait(full + 8 * s, (i / S::kStages) & 1, &dead));
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint32_t at = stages + s * S::kStage;
@@ -362,7 +384,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     // from one instruction's 16 of the sum to the next: 32 bytes of a row, or 16 rows
                     const uint32_t p_next = pa ? 2 : 128, q_next = qa ? 2 : 128;
                     const uint64_t dp = operand_desc(at, pa), dq = operand_desc(at + S::kOperand, qa);
-                    if (elect_one()) {
+                    if (elect_one() && !dry) {
 #pragma unroll
                         for (int j = 0; j < 4; ++j) mma16<Pair>(acc, dp + j * p_next, dq + j * q_next, idesc, k > 0 || j > 0);
                         if (Pair) {
@@ -374,8 +396,17 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                     }
                     __syncwarp();
+                    if (!dry) ++i;
+                }
+                if (dry) {
+                    dry = false;
+                    n_blocks = blocks_after_wait();
+                } else {
+                    ++n;
                 }
             }
+        } else {
+            wait_for_previous();
         }
         __syncwarp();
     } else {
@@ -387,7 +418,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             __syncwarp();
         };
         int n = 0;
-        for (int t; (t = block_of(a, worker, workers, n)) < n_blocks; ++n) {
+        bool dry = true;
+#pragma unroll 1
+        for (;;) {
+            int t = block_of(a, worker, workers, n);
+            if (dry)
+                t = min(t, a.n_blocks - 1);
+            else if (t >= n_blocks)
+                break;
             const ProductGroup *g;
             const Block b = block_at<K, S::kSide>(a, t, g);
             const int im = Pair ? 2 * b.m + rank : b.m;
@@ -407,9 +445,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                                  "l"(added + (size_t)c * kTileBytes + 16 * k)
                                  : "memory");
             };
-            if (K == kPoly && chunks) fetch(0);
+            if (K == kPoly && chunks && !dry) fetch(0);
             const bool finish = K == kLast && g->finish;
-            if (!__all_sync(kFull, mbar_wait(acc_full + 8 * (n & 1), (n / 2) & 1, &dead))) {
+            if (!dry && !__all_sync(kFull, mbar_wait(acc_full + 8 * (n & 1), (n / 2) & 1, &dead))) {
                 if (K == kPoly) asm volatile("cp.async.wait_all;" ::: "memory");
                 break;
             }
@@ -418,9 +456,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             if constexpr (K == kLast) {
                 if (finish) {
                     // the weights move by four lanes to 32 columns of a row
-                    const int first_row = im * kTile + quad * 32 + (lane >> 2), cols = g->cols, rows_left = g->rows - first_row;
+                    const int first_row = im * kTile + quad * 32 + (lane >> 2), cols = g->cols, rows_left = dry ? 0 : g->rows - first_row;
                     Matrix q = {};
-                    if (a.matrices) q = a.matrices[g->matrix + b.matrix];
+                    if (a.matrices && !dry) q = a.matrices[g->matrix + b.matrix];
                     buffer_free();  // (of a block of another group)
 #pragma unroll 1
                     for (int c = 0; c < chunks; ++c) {
@@ -486,7 +524,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int c = 0; c < chunks && !finish; ++c) {
                 if (K != kPoly)
                     buffer_free();
-                else if (c)
+                else if (c && !dry)
                     fetch(c);
                 const int diagonal = im * kTile + row < g->n ? im * kTile + row - (j0 + c) * kTileCols : -1;
 #pragma unroll 1
@@ -528,7 +566,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0)
+                if (lane == 0 && !dry)
                     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];\n"
                                  "cp.async.bulk.commit_group;" ::"l"(&map_out),
                                  "r"(0), "r"((out + im * out_pitch + j0 + c) * kTile + quad * 32), "r"(buffer)
@@ -536,7 +574,13 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
+            if (dry) {
+                dry = false;
+                n_blocks = blocks_after_wait();
+                continue;
+            }
             if (lane == 0) arrive_cluster(Pair ? in_cta(acc_free + 8 * (n & 1), 0) : acc_free + 8 * (n & 1));
+            ++n;
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         __syncwarp();
