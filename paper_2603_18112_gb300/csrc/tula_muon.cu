@@ -1349,7 +1349,9 @@ int product(const Maps &maps, ProductArgs &a, const Kin *kin, int n, int x, bool
     const int pairs = fill<true>(a, kin, n, K, x, first);
     const int singles = fill<false>(a, kin, n, K, x, first);
     if (pairs < 0 || singles < 0) return TULA_ERR_ARG;
-    if (up(pairs, std::max(1, sms / 2)) <= up(singles, sms)) {
+    // Blocks of 128 where each SM has one at most (RULE); else pairs of CTAs where they need no more rounds, since a
+    // round takes as long.
+    if (singles > sms && up(pairs, std::max(1, sms / 2)) <= up(singles, sms)) {
         fill<true>(a, kin, n, K, x, first);
         return launch_product<true, K>(maps, a, sms, s);
     }
