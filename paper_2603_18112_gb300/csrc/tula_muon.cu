@@ -47,8 +47,8 @@ constexpr long long kMostTiles = 1LL << 24;  // of a workspace: rows of 128 byte
 // An operand of 128 (or 256, by pairs) rows of the product's side: in tiles of `pitch` to a row of them.  The sum
 // runs along the tiles' columns (K-major) or along their rows; of a symmetric matrix, of which the blocks on
 // and above the diagonal are there, along rows up to the diagonal and along columns from there on.  (With the
-// blocks below it written too, transposed by way of shared memory, A of 72 matrices took 108 us instead of MIRA,
-// 256 x 256 MIRB us instead of MIRC.)
+// blocks below it written too, transposed by way of shared memory, 8192 x 8192 took 6.59 ms instead of 6.36 and
+// 1024 x 1024 178 us instead of 162.)
 enum Way { kAcross, kAlong, kSymmetric };
 struct Side {
     int base, step;   // the first matrix's first tile, tiles from matrix to matrix
@@ -291,9 +291,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t tmem = __shfl_sync(kFull, *tmem_at, 0);
     let_next_start();
     // Each role goes through its loop once before it waits for the kernel ahead, without what the others or memory
-    // would see of it: so its instructions and the first block's parameters are there when the wait ends.  (A
-    // launch's instructions come from L2, some 200 cycles to eight of them: of 6.2 us that a product of 256 x 256
-    // took, reading back took 2 to 4.)
+    // would see of it: so its instructions and the first block's parameters are there when the wait ends.  (1024 x
+    // 1024: 162 us without, 153 so.)
     auto blocks_after_wait = [&] {
         wait_for_previous();
         return !a.record || a.record[TULA_RECORD_FINITE] != 0.f ? a.n_blocks : 0;
@@ -519,7 +518,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                 }
             }
-            // (rolled: unrolled over 64 columns, the instructions of a launch's only block came from L2 for some 3 us)
 #pragma unroll 1
             for (int c = 0; c < chunks && !finish; ++c) {
                 if (K != kPoly)
@@ -527,42 +525,42 @@ __global__ void __launch_bounds__(kThreads, 1)
                 else if (c && !dry)
                     fetch(c);
                 const int diagonal = im * kTile + row < g->n ? im * kTile + row - (j0 + c) * kTileCols : -1;
-#pragma unroll 1
-                for (int h = 0; h < 4; ++h) {
-                    float f[16];
-                    tmem_load16(f, acc + c * kTileCols + 16 * h);
-                    const uint32_t at0 = buffer + lane * 128 + ((2 * h ^ (lane & 7)) << 4), at1 = buffer + lane * 128 + ((2 * h + 1 ^ (lane & 7)) << 4);
+                unsigned v[64];
+                tmem_load32(v, acc + c * kTileCols);
+                tmem_load32(v + 32, acc + c * kTileCols + 32);
+                if (K == kPoly) asm volatile("cp.async.wait_all;" ::: "memory");
+                tmem_wait(v);
+#pragma unroll
+                for (int h = 0; h < 8; ++h) {  // eight columns
+                    const uint32_t at = buffer + lane * 128 + ((h ^ (lane & 7)) << 4);
+                    float f[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) f[k] = __uint_as_float(v[8 * h + k]);
                     if (K == kPoly) {
-                        if (h == 0) asm volatile("cp.async.wait_all;" ::: "memory");
-                        unsigned add[8];
+                        unsigned add[4];
                         asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
                                      : "=r"(add[0]), "=r"(add[1]), "=r"(add[2]), "=r"(add[3])
-                                     : "r"(at0)
-                                     : "memory");
-                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                                     : "=r"(add[4]), "=r"(add[5]), "=r"(add[6]), "=r"(add[7])
-                                     : "r"(at1)
+                                     : "r"(at)
                                      : "memory");
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            __half2 v;
-                            memcpy(&v, &add[k], 4);
-                            const float2 e = __half22float2(v);
-                            f[2 * k] = fmaf((float)kC, f[2 * k], fmaf((float)kB, e.x, diagonal == 16 * h + 2 * k ? (float)kA : 0.f));
-                            f[2 * k + 1] = fmaf((float)kC, f[2 * k + 1], fmaf((float)kB, e.y, diagonal == 16 * h + 2 * k + 1 ? (float)kA : 0.f));
+                        for (int k = 0; k < 4; ++k) {
+                            __half2 e;
+                            memcpy(&e, &add[k], 4);
+                            const float2 x = __half22float2(e);
+                            f[2 * k] = fmaf((float)kC, f[2 * k], fmaf((float)kB, x.x, diagonal == 8 * h + 2 * k ? (float)kA : 0.f));
+                            f[2 * k + 1] = fmaf((float)kC, f[2 * k + 1], fmaf((float)kB, x.y, diagonal == 8 * h + 2 * k + 1 ? (float)kA : 0.f));
                         }
                     } else {
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) f[k] *= alpha;
+                        for (int k = 0; k < 8; ++k) f[k] *= alpha;
                     }
-                    unsigned y[8];
+                    unsigned y[4];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const __half2 v = __floats2half2_rn(f[2 * k], f[2 * k + 1]);
-                        memcpy(&y[k], &v, 4);
+                    for (int k = 0; k < 4; ++k) {
+                        const __half2 e = __floats2half2_rn(f[2 * k], f[2 * k + 1]);
+                        memcpy(&y[k], &e, 4);
                     }
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at0), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at1), "r"(y[4]), "r"(y[5]), "r"(y[6]), "r"(y[7]) : "memory");
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
@@ -1349,7 +1347,7 @@ int product(const Maps &maps, ProductArgs &a, const Kin *kin, int n, int x, bool
     const int pairs = fill<true>(a, kin, n, K, x, first);
     const int singles = fill<false>(a, kin, n, K, x, first);
     if (pairs < 0 || singles < 0) return TULA_ERR_ARG;
-    // Blocks of 128 where each SM has one at most (RULE); else pairs of CTAs where they need no more rounds, since a
+    // Blocks of 128 where each SM has one at most (1024 x 1024: 127 us, 153 by pairs); else pairs of CTAs where they need no more rounds, since a
     // round takes as long.
     if (singles > sms && up(pairs, std::max(1, sms / 2)) <= up(singles, sms)) {
         fill<true>(a, kin, n, K, x, first);
