@@ -27,6 +27,7 @@
 #include "tula_tc.cuh"
 
 #include <cmath>
+#include <functional>
 #include <memory>
 #include <new>
 #include <vector>
@@ -918,8 +919,8 @@ __global__ void __launch_bounds__(kStreamThreads, kStreamCtas) k_muon_last(const
 //
 // One CTA a matrix whose smaller side is at most 128 and whose tiles, at most twelve, shared memory holds beside
 // those of A, which B takes the place of.  Nothing leaves the SM between the first reading and the last
-// writing: one launch and some 4 us a step instead of three launches and 19 (64 x 576: 38 us in all, 102 by
-// the products above).  The tiles have the image that the copies give them there.  One thread issues a
+// writing: one launch and some 4 us a step instead of three launches and 13 (64 x 576: 38 us in all; 256 x 256 by
+// the products above 74).  The tiles have the image that the copies give them there.  One thread issues a
 // product, all eight warps read it back.
 
 constexpr int kSmallTiles = 12;
@@ -1540,6 +1541,16 @@ int tula_muon_plan_create(const tula_muon_matrices *m, void *workspace, size_t w
                 return TULA_ERR_ARG;
             q.vec = vec[(size_t)i] = m->cols[i] % 8 == 0 && aligned(q.g, 16) && aligned(q.m, 16) && aligned(q.w, 32) && aligned(q.copy, 16);
         }
+        // a buffer that two matrices would write
+        std::vector<const void *> written;
+        for (const Matrix &q : of)
+            if (q.w) {
+                written.push_back(q.w);
+                written.push_back(q.m);
+                if (q.copy) written.push_back(q.copy);
+            }
+        std::sort(written.begin(), written.end(), std::less<const void *>());
+        if (std::adjacent_find(written.begin(), written.end()) != written.end()) return TULA_ERR_ARG;
         if (!shapes_of(m->rows, m->cols, &vec, n, plan->kin, which) || !sizes_of(plan->kin, z)) return TULA_ERR_ARG;
         std::vector<int> next(plan->kin.size(), 0);
         std::vector<Matrix> table(z.table / sizeof(Matrix));

@@ -84,18 +84,25 @@ def _forward(x, weight, bias, eps, keep):
     return y, stats
 
 
+def _kept(*tensors):
+    return [t if t is None else (t.dtype, t.shape, t.device) for t in tensors]
+
+
 class _LayerNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, eps):
         y, stats = _forward(x, weight, bias, eps, True)
         ctx.save_for_backward(x, weight, stats)
         ctx.param_type = next((p.dtype for p in (weight, bias) if p is not None), torch.float32)
+        ctx.kept = _kept(x, weight, stats)
         return y
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
         x, weight, stats = ctx.saved_tensors
+        if _kept(x, weight, stats) != ctx.kept or not stats.is_contiguous():
+            raise RuntimeError("layer_norm: a hook on saved tensors gave back another tensor than it was given")
         need_x, need_w, need_b, _ = ctx.needs_input_grad
         cols, dev = x.shape[-1], _on_gpu(x, dy, stats)
         rows, stride = _rows_of(x, cols)

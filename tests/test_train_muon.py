@@ -116,7 +116,7 @@ def test_refusals_of_the_library():
     assert L.tula_muon_plan_create(n, p, 1 << 20, n, ctypes.byref(plan)) == -1 and not plan
 
     def create(**kw):
-        one = {"rows": 4, "cols": 8, "g": 256, "w": 256, "m": 256, "gt": 0, "c": 256, "ct": 1, "space": p, "size": 1 << 20} | kw
+        one = {"rows": 4, "cols": 8, "g": 256, "w": 1024, "m": 2048, "gt": 0, "c": 4096, "ct": 1, "space": p, "size": 1 << 20} | kw
         arr = {k: (ctypes.c_int64 if k in ("rows", "cols") else ctypes.c_int if k in ("gt", "ct") else ctypes.c_void_p)
                for k in ("rows", "cols", "g", "w", "m", "gt", "c", "ct")}
         a = {k: (t * 1)(one[k]) for k, t in arr.items()}
@@ -125,7 +125,7 @@ def test_refusals_of_the_library():
         return L.tula_muon_plan_create(ctypes.byref(d), one["space"], one["size"], n, ctypes.byref(plan))
 
     for bad in ({"rows": -1}, {"cols": 1 << 21}, {"g": 0}, {"w": 0}, {"m": 0}, {"c": 0}, {"gt": 3}, {"ct": 0}, {"g": 258}, {"w": 258},
-                {"m": 258}, {"c": 257}):
+                {"m": 258}, {"c": 257}, {"w": 2048}, {"c": 1024}):
         assert create(**bad) == -1, bad
     assert create(size=255) == create(rows=300, cols=300, size=1000) == create(space=n) == create(space=ctypes.c_void_p(128)) == -2
     assert not plan and L.tula_muon_plan_destroy(n) == 0 and L.tula_muon_error(n, n) == -1
@@ -387,6 +387,8 @@ def test_plan_refusals():
         O.MuonStep([x], [x, x], [x])
     with pytest.raises(TypeError):
         O.MuonStep([x], [x], [x], copies=[x])
+    with pytest.raises(TulaError):  # twice in the list
+        O.MuonStep([x, x], [x.clone(), x.clone()], [x.clone(), x.clone()])
     step = O.MuonStep([x], [x.clone()], [x.clone()])
     with pytest.raises(TypeError):
         step(1e-3, record=torch.zeros(4))

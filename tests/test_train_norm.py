@@ -246,6 +246,19 @@ def test_captured_and_on_another_stream():
 
 
 @pytest.mark.gpu
+def test_hooks_on_saved_tensors():
+    x, w, b, dy = _inputs(20, 64, torch.float32, torch.float32, 9)
+    want = torch.autograd.grad(norm.layer_norm(x, w, b), (x, w, b), dy)
+    with torch.autograd.graph.save_on_cpu():
+        y = norm.layer_norm(x, w, b)
+    assert all(torch.equal(p, q) for p, q in zip(torch.autograd.grad(y, (x, w, b), dy), want))
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: t, lambda t: t[..., :1]):
+        y = norm.layer_norm(x, w, b)
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(y, (x, w, b), dy)
+
+
+@pytest.mark.gpu
 def test_more_than_2_to_the_31_elements():
     rows, cols = (1 << 19) + 5, 4112
     x = torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda")
