@@ -8,16 +8,18 @@
 // HBM bounds all of it: some ten operations an element of 2 or 4 bytes read and written once.  A group of
 // threads holds a row in registers, so that the mean, the variance about it and the output come from one
 // reading, and keeps its columns' weights, and in the backward pass their sums, in registers from row to row.
-// Rows on 16-byte boundaries come by bulk copies into a ring of shared memory, several rows ahead (with one row
-// ahead in registers instead, 16384 x 4096 bf16 took 254 us forward and backward); others into
-// registers, one row ahead.
+// Rows come by bulk copies into a ring of shared memory, several ahead (with one row ahead in registers
+// instead, 16384 x 4096 bf16 took 254 us forward and backward where it takes 174 now, and 50000 x 1001 fp32 316
+// instead of 203).
 #include "tula_tc.cuh"
 
 namespace {
 
 constexpr int kMostThreads = 512;  // of a CTA
-// Of an SM, that registers are left for.  (Forward with 512 too: 79 us instead of 71 for 16384 x 4096 bf16.)
+// Of an SM, that registers are left for.  (Forward with 512 too: 79 us instead of 71 for 16384 x
+// 4096 bf16; rows off 16-byte boundaries take 78 us with 512, 160 with 768, for 50000 x 1001.)
 constexpr int kForwardThreads = 768, kBackwardThreads = 512;
+constexpr int forward_threads(bool vec) { return vec ? kForwardThreads : kBackwardThreads; }
 constexpr int kMostCluster = 8;
 // Elements that a thread holds of a row.  What each row costs every warp (exchanges, of which an SM does one a
 // cycle, barriers, addresses) is spread over as many: with eight a thread 16384 x 4096 bf16 took 133 us forward.
@@ -94,15 +96,29 @@ struct Part {
     }
     __device__ __forceinline__ void load_shared(uint32_t row, bool there) {
         const uint32_t p = row + at * (int)sizeof(T);
+        if constexpr (!Vec) {
 #pragma unroll
-        for (int k = 0; k < kN / kStep; ++k) {
-            unsigned *q = w + 4 * k;
-            q[0] = q[1] = q[2] = q[3] = 0;
-            if (there && in(k * kStep))
-                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                             : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3])
-                             : "r"(p + k * next * (int)sizeof(T))
-                             : "memory");
+            for (int k = 0; k < kN; ++k) {
+                if constexpr (sizeof(T) == 4) {
+                    w[k] = 0;
+                    if (there && in(k)) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[k]) : "r"(p + 4 * k * next) : "memory");
+                } else {
+                    unsigned short v = 0;
+                    if (there && in(k)) asm volatile("ld.shared.b16 %0, [%1];" : "=h"(v) : "r"(p + 2 * k * next) : "memory");
+                    w[k / 2] = k & 1 ? w[k / 2] | (unsigned)v << 16 : v;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kN / kStep; ++k) {
+                unsigned *q = w + 4 * k;
+                q[0] = q[1] = q[2] = q[3] = 0;
+                if (there && in(k * kStep))
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                 : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3])
+                                 : "r"(p + k * next * (int)sizeof(T))
+                                 : "memory");
+            }
         }
     }
     __device__ __forceinline__ void floats(float (&f)[kN]) const {
@@ -223,35 +239,66 @@ struct GroupSum {
     }
 };
 
-// The ring: stage s holds the rows of one round of the CTA's groups, of each of N matrices.  A wait that runs
-// out leaves what is there: the others end at once then, and the error word says so.
-template <typename T, int N>
+// The ring: stage s holds the rows of one round of the CTA's groups, of each of N matrices.  Rows off 16-byte
+// boundaries come with what shares their first and last 16 bytes; a round that has the matrix's first or last
+// row, beside which there may be nothing, is read directly.  A wait that runs out leaves what is there: the
+// others end at once then, and the error word says so.
+template <typename T, int N, bool Vec>
 struct Ring {
     uint32_t at, bars;  // shared addresses
     volatile int *dead;
-    int stages, per, bytes, pitch;  // rows to a round; bytes of a row here, and from row to row
+    int stages, per, bytes;  // rows to a round; bytes of a row
+    long long rows;
 
-    __device__ __forceinline__ uint32_t row(int s, int m, int g) const { return at + ((s * N + m) * per + g) * pitch; }
-    // Of rows r0 to r0 + n; by one warp.
-    __device__ __forceinline__ void fetch(int s, const T *const (&from)[N], const long long (&stride)[N], int n) {
+    __device__ __forceinline__ int pitch() const { return Vec ? bytes : (bytes + 15) / 16 * 16 + 16; }
+    __device__ __forceinline__ uint32_t place(int s, int m) const { return at + (s * N + m) * per * pitch(); }
+    __device__ __forceinline__ bool direct(long long r0) const { return !Vec && (r0 == 0 || r0 + per >= rows); }
+    __device__ __forceinline__ bool joined(long long stride) const { return stride * (long long)sizeof(T) == bytes; }
+    static __device__ __forceinline__ unsigned off(const T *p) { return Vec ? 0u : (unsigned)reinterpret_cast<unsigned long long>(p) & 15u; }
+    // Where row g of the round that starts with `from` lies.
+    __device__ __forceinline__ uint32_t row(int s, int m, int g, const T *from, long long stride) const {
+        if constexpr (Vec) return place(s, m) + g * bytes;
+        return joined(stride) ? place(s, m) + off(from) + g * bytes : place(s, m) + g * pitch() + off(from + g * stride);
+    }
+    // Of rows r0 to r0 + n, the first ones at `from`; by one warp.
+    __device__ __forceinline__ void fetch(int s, long long r0, const T *const (&from)[N], const long long (&stride)[N], int n) {
         const int lane = threadIdx.x & 31;
         const uint32_t bar = bars + 8 * s;
-        if (lane == 0) mbar_expect(bar, (unsigned)(N * n * bytes));
+        if (direct(r0)) {
+            if (lane == 0) mbar_expect(bar, 0);
+            return;
+        }
+        unsigned total = 0;
+#pragma unroll
+        for (int m = 0; m < N; ++m) {
+            if (joined(stride[m]))
+                total += lane == 0 ? (off(from[m]) + n * bytes + 15) / 16 * 16 : 0u;
+            else
+                for (int g = lane; g < n; g += 32) total += (off(from[m] + g * stride[m]) + bytes + 15) / 16 * 16;
+        }
+        total = __reduce_add_sync(kFull, total);
+        if (lane == 0) mbar_expect(bar, total);
         __syncwarp();
 #pragma unroll
         for (int m = 0; m < N; ++m) {
-            if (stride[m] * (long long)sizeof(T) == bytes && pitch == bytes) {
-                if (lane == 0) bulk_load(row(s, m, 0), from[m], (unsigned)(n * bytes), bar);
+            if (joined(stride[m])) {
+                const unsigned o = off(from[m]);
+                if (lane == 0)
+                    bulk_load(place(s, m), reinterpret_cast<const unsigned char *>(from[m]) - o, (o + n * bytes + 15) / 16 * 16, bar);
             } else {
-                for (int g = lane; g < n; g += 32) bulk_load(row(s, m, g), from[m] + g * stride[m], (unsigned)bytes, bar);
+                for (int g = lane; g < n; g += 32) {
+                    const T *p = from[m] + g * stride[m];
+                    const unsigned o = off(p);
+                    bulk_load(place(s, m) + g * pitch(), reinterpret_cast<const unsigned char *>(p) - o, (o + bytes + 15) / 16 * 16, bar);
+                }
             }
         }
     }
     __device__ __forceinline__ void wait(int s, unsigned parity) { mbar_wait(bars + 8 * s, parity, dead); }
 };
 
-template <typename T, int N>
-__device__ __forceinline__ void start_ring(const Ring<T, N> &ring) {
+template <typename T, int N, bool Vec>
+__device__ __forceinline__ void start_ring(const Ring<T, N, Vec> &ring) {
     if (threadIdx.x == 0) {
         for (int s = 0; s < ring.stages; ++s) mbar_init(ring.bars + 8 * s, 1);
         *ring.dead = 0;
@@ -261,9 +308,9 @@ __device__ __forceinline__ void start_ring(const Ring<T, N> &ring) {
 }
 
 template <typename T, bool Vec, bool Wide>
-__global__ void __launch_bounds__(kForwardThreads) k_norm_forward(const NormArgs a) {
+__global__ void __launch_bounds__(forward_threads(Vec)) k_norm_forward(const NormArgs a) {
     using P = Part<T, Vec>;
-    extern __shared__ __align__(128) unsigned char memory[];  // Vec: the ring
+    extern __shared__ __align__(128) unsigned char memory[];  // the ring
     __shared__ __align__(16) Sums place;
     __shared__ __align__(8) unsigned long long bars[kMostStages];
     __shared__ volatile int dead;
@@ -271,8 +318,8 @@ __global__ void __launch_bounds__(kForwardThreads) k_norm_forward(const NormArgs
     const int col0 = blockIdx.x % a.cluster * a.share, cols = min(a.cols - col0, a.share);  // the CTA's share
     const long long block = blockIdx.x / a.cluster, step = (long long)(gridDim.x / a.cluster) * per;
     const int bytes = cols * (int)sizeof(T);
-    Ring<T, 1> ring{smem_addr(memory), smem_addr(bars), &dead, a.stages, per, bytes, bytes};
-    if (Vec) start_ring(ring);
+    Ring<T, 1, Vec> ring{smem_addr(memory), smem_addr(bars), &dead, a.stages, per, bytes, a.rows};
+    start_ring(ring);
     let_next_start();
     if (a.cluster > 1) cluster_sync();  // the other CTAs' shared memory may be written to from here on
     wait_for_previous();
@@ -281,17 +328,13 @@ __global__ void __launch_bounds__(kForwardThreads) k_norm_forward(const NormArgs
     const T *const x[1] = {static_cast<const T *>(a.x) + col0};
     const long long stride[1] = {a.stride};
     const long long first = block * per;
-    P now(t, a.group, cols), next = now;
-    if (Vec) {
-        if (threadIdx.x < 32) {
-            long long r0 = first;
-            for (int s = 0; s < a.stages && r0 < a.rows; ++s, r0 += step) {
-                const T *const from[1] = {x[0] + r0 * a.stride};
-                ring.fetch(s, from, stride, (int)min((long long)per, a.rows - r0));
-            }
+    P now(t, a.group, cols);
+    if (threadIdx.x < 32) {
+        long long r0 = first;
+        for (int s = 0; s < a.stages && r0 < a.rows; ++s, r0 += step) {
+            const T *const from[1] = {x[0] + r0 * a.stride};
+            ring.fetch(s, r0, from, stride, (int)min((long long)per, a.rows - r0));
         }
-    } else {
-        now.load(x[0] + (first + g) * a.stride, first + g < a.rows);
     }
     const int psize = a.ptype == TULA_TYPE_F32 ? 4 : 2;
     float w[kN], b[kN];
@@ -303,25 +346,23 @@ __global__ void __launch_bounds__(kForwardThreads) k_norm_forward(const NormArgs
     for (long long r0 = first; r0 < a.rows; r0 += step) {
         const long long r = r0 + g;
         const bool there = r < a.rows;
-        if (Vec) {
-            ring.wait(s, parity);
-            now.load_shared(ring.row(s, 0, g), there);
-        } else {
-            next.load(x[0] + (r + step) * a.stride, r + step < a.rows);
-        }
+        ring.wait(s, parity);
+        if (ring.direct(r0))
+            now.load(x[0] + r * a.stride, there);
+        else
+            now.load_shared(ring.row(s, 0, g, x[0] + r0 * a.stride, a.stride), there);
         float c[kN], part[2] = {0.f, 0.f};
         now.floats(c);
 #pragma unroll
         for (int k = 0; k < kN; ++k) part[k & 1] += c[k];
         const float mean = sum(part[0] + part[1]) * inv;
-        if (Vec) {
-            if (!Wide) __syncthreads();
-            if (threadIdx.x < 32 && r0 + a.stages * step < a.rows) {  // all have read the stage
-                const T *const from[1] = {x[0] + (r0 + a.stages * step) * a.stride};
-                ring.fetch(s, from, stride, (int)min((long long)per, a.rows - r0 - a.stages * step));
-            }
-            if (++s == a.stages) s = 0, parity ^= 1;
+        if (!Wide) __syncthreads();
+        if (threadIdx.x < 32 && r0 + a.stages * step < a.rows) {  // all have read the stage
+            const long long r1 = r0 + a.stages * step;
+            const T *const from[1] = {x[0] + r1 * a.stride};
+            ring.fetch(s, r1, from, stride, (int)min((long long)per, a.rows - r1));
         }
+        if (++s == a.stages) s = 0, parity ^= 1;
         part[0] = part[1] = 0.f;
 #pragma unroll
         for (int k = 0; k < kN; ++k) {
@@ -335,14 +376,13 @@ __global__ void __launch_bounds__(kForwardThreads) k_norm_forward(const NormArgs
             now.store(static_cast<T *>(a.y) + r * a.cols + col0, c);
             if (a.stats && t == 0 && col0 == 0) reinterpret_cast<float2 *>(a.stats)[r] = make_float2(mean, rstd);
         }
-        if (!Vec) now = next;
     }
 }
 
 template <typename T, bool Vec, bool Wide, bool Params>
 __global__ void __launch_bounds__(kBackwardThreads) k_norm_backward(const NormArgs a) {
     using P = Part<T, Vec>;
-    extern __shared__ __align__(128) unsigned char memory[];  // Vec: the ring; Params: then the groups' sums
+    extern __shared__ __align__(128) unsigned char memory[];  // the ring; Params: then the groups' sums
     __shared__ __align__(16) Sums place;
     __shared__ __align__(8) unsigned long long bars[kMostStages];
     __shared__ volatile int dead;
@@ -350,8 +390,8 @@ __global__ void __launch_bounds__(kBackwardThreads) k_norm_backward(const NormAr
     const int col0 = blockIdx.x % a.cluster * a.share, cols = min(a.cols - col0, a.share);  // the CTA's share
     const long long block = blockIdx.x / a.cluster, step = (long long)(gridDim.x / a.cluster) * per;
     const int bytes = cols * (int)sizeof(T);
-    Ring<T, 2> ring{smem_addr(memory), smem_addr(bars), &dead, a.stages, per, bytes, bytes};
-    if (Vec) start_ring(ring);
+    Ring<T, 2, Vec> ring{smem_addr(memory), smem_addr(bars), &dead, a.stages, per, bytes, a.rows};
+    start_ring(ring);
     let_next_start();
     if (a.cluster > 1) cluster_sync();
     wait_for_previous();
@@ -361,19 +401,14 @@ __global__ void __launch_bounds__(kBackwardThreads) k_norm_backward(const NormAr
     const long long stride[2] = {a.stride, a.dy_stride};
     const float2 *stats = reinterpret_cast<const float2 *>(a.stats);
     const long long first = block * per;
-    P now_x(t, a.group, cols), now_d = now_x, next_x = now_x, next_d = now_x;
+    P now_x(t, a.group, cols), now_d = now_x;
     float2 now_s = make_float2(0.f, 0.f), next_s = now_s;
-    if (Vec) {
-        if (threadIdx.x < 32) {
-            long long r0 = first;
-            for (int s = 0; s < a.stages && r0 < a.rows; ++s, r0 += step) {
-                const T *const from[2] = {x + r0 * a.stride, dy + r0 * a.dy_stride};
-                ring.fetch(s, from, stride, (int)min((long long)per, a.rows - r0));
-            }
+    if (threadIdx.x < 32) {
+        long long r0 = first;
+        for (int s = 0; s < a.stages && r0 < a.rows; ++s, r0 += step) {
+            const T *const from[2] = {x + r0 * a.stride, dy + r0 * a.dy_stride};
+            ring.fetch(s, r0, from, stride, (int)min((long long)per, a.rows - r0));
         }
-    } else {
-        now_x.load(x + (first + g) * a.stride, first + g < a.rows);
-        now_d.load(dy + (first + g) * a.dy_stride, first + g < a.rows);
     }
     if (first + g < a.rows) now_s = __ldcs(stats + first + g);
     float w[kN], dw[kN], db[kN];
@@ -386,13 +421,13 @@ __global__ void __launch_bounds__(kBackwardThreads) k_norm_backward(const NormAr
         const long long r = r0 + g;
         const bool there = r < a.rows;
         if (r + step < a.rows) next_s = __ldcs(stats + r + step);
-        if (Vec) {
-            ring.wait(s, parity);
-            now_x.load_shared(ring.row(s, 0, g), there);
-            now_d.load_shared(ring.row(s, 1, g), there);
+        ring.wait(s, parity);
+        if (ring.direct(r0)) {
+            now_x.load(x + r * a.stride, there);
+            now_d.load(dy + r * a.dy_stride, there);
         } else {
-            next_x.load(x + (r + step) * a.stride, r + step < a.rows);
-            next_d.load(dy + (r + step) * a.dy_stride, r + step < a.rows);
+            now_x.load_shared(ring.row(s, 0, g, x + r0 * a.stride, a.stride), there);
+            now_d.load_shared(ring.row(s, 1, g, dy + r0 * a.dy_stride, a.dy_stride), there);
         }
         const float rstd = there ? now_s.y : 0.f, mean = there ? now_s.x : 0.f;
         float n[kN], d[kN], s1 = 0.f, s2 = 0.f;
@@ -411,21 +446,19 @@ __global__ void __launch_bounds__(kBackwardThreads) k_norm_backward(const NormAr
         }
         float sums[2] = {s1, s2};
         if (a.y) sum(sums);
-        if (Vec) {
-            if (!a.y || !Wide) __syncthreads();
-            if (threadIdx.x < 32 && r0 + a.stages * step < a.rows) {  // all have read the stage
-                const T *const from[2] = {x + (r0 + a.stages * step) * a.stride, dy + (r0 + a.stages * step) * a.dy_stride};
-                ring.fetch(s, from, stride, (int)min((long long)per, a.rows - r0 - a.stages * step));
-            }
-            if (++s == a.stages) s = 0, parity ^= 1;
+        if (!a.y || !Wide) __syncthreads();
+        if (threadIdx.x < 32 && r0 + a.stages * step < a.rows) {  // all have read the stage
+            const long long r1 = r0 + a.stages * step;
+            const T *const from[2] = {x + r1 * a.stride, dy + r1 * a.dy_stride};
+            ring.fetch(s, r1, from, stride, (int)min((long long)per, a.rows - r1));
         }
+        if (++s == a.stages) s = 0, parity ^= 1;
         if (a.y && there) {
             const float m1 = sums[0] * inv * rstd, m2 = sums[1] * inv * rstd;
 #pragma unroll
             for (int k = 0; k < kN; ++k) d[k] = fmaf(rstd, d[k], -fmaf(n[k], m2, m1));
             now_x.store(static_cast<T *>(a.y) + r * a.cols + col0, d);
         }
-        if (!Vec) now_x = next_x, now_d = next_d;
         now_s = next_s;
     }
     if (!Params) return;
@@ -586,9 +619,10 @@ unsigned parts_of(const Layout &l, long long rows) {
 
 // The ring's memory: so much a thread that all threads of an SM take 192 KB.
 constexpr int kRingMost = 192 * 1024;
-inline int ring_bytes(const Layout &l, size_t size, int matrices, int sm_threads, int &stages) {
-    const int stage = l.threads * kN * (int)size * matrices;
-    stages = std::min(kMostStages, kRingMost / (sm_threads / l.threads) / stage);
+inline int ring_bytes(const Layout &l, bool vec, size_t size, int matrices, int sm_threads, int &stages) {
+    const int bytes = l.share * (int)size, pitch = vec ? bytes : (bytes + 15) / 16 * 16 + 16;  // as Ring's
+    const int stage = l.threads / l.group * pitch * matrices;
+    stages = std::max(1, std::min(kMostStages, kRingMost / (sm_threads / l.threads) / stage));
     return stages * stage;
 }
 
@@ -598,18 +632,18 @@ inline bool lies(const void *p, long long stride, size_t size) {  // rows on 16-
 
 template <typename T>
 int forward_typed(NormArgs &a, cudaStream_t s) {
-    const Layout l = layout_of(a.rows, a.cols, std::max(1, sm_count()), kForwardThreads);
+    const bool vec = a.cols % (16 / (int)sizeof(T)) == 0 && lies(a.x, a.stride, sizeof(T)) && lies(a.y, a.cols, sizeof(T));
+    const Layout l = layout_of(a.rows, a.cols, std::max(1, sm_count()), forward_threads(vec));
     if (!l.cluster) return tula::launch(k_norm_forward_wide<T>, dim3(l.grid), l.threads, 0, s, 1, a);
     a.group = l.group;
     a.cluster = l.cluster;
     a.share = l.share;
-    const bool vec = a.cols % (16 / (int)sizeof(T)) == 0 && lies(a.x, a.stride, sizeof(T)) && lies(a.y, a.cols, sizeof(T));
     const bool wide = l.group > 32;
     void (*k)(const NormArgs) = vec ? (wide ? k_norm_forward<T, true, true> : k_norm_forward<T, true, false>)
                                     : (wide ? k_norm_forward<T, false, true> : k_norm_forward<T, false, false>);
-    static std::atomic<uint64_t> done[2];
-    const int smem = vec ? ring_bytes(l, sizeof(T), 1, kForwardThreads, a.stages) : 0;
-    const int rc = vec ? allow_smem((const void *)k, kRingMost, &done[wide]) : TULA_OK;
+    static std::atomic<uint64_t> done[4];
+    const int smem = ring_bytes(l, vec, sizeof(T), 1, forward_threads(vec), a.stages);
+    const int rc = allow_smem((const void *)k, kRingMost, &done[2 * vec + wide]);
     return rc ? rc : tula::launch(k, dim3(l.grid), l.threads, smem, s, l.cluster, a);
 }
 template <typename T, bool Params>
@@ -629,10 +663,10 @@ int backward_typed(NormArgs &a, void *dw, void *db, cudaStream_t s) {
                          (!a.y || lies(a.y, a.cols, sizeof(T)));
         const bool wide = l.group > 32;
         void (*k)(const NormArgs) = a.parts ? backward_kernel<T, true>(vec, wide) : backward_kernel<T, false>(vec, wide);
-        static std::atomic<uint64_t> done[4];
-        int smem = vec ? ring_bytes(l, sizeof(T), 2, kBackwardThreads, a.stages) : 0;
+        static std::atomic<uint64_t> done[8];
+        int smem = ring_bytes(l, vec, sizeof(T), 2, kBackwardThreads, a.stages);
         if (a.parts && l.threads > l.group) smem = std::max(smem, 2 * l.threads * kN * 4);  // 32 KB
-        if (vec) rc = allow_smem((const void *)k, kRingMost, &done[2 * wide + (a.parts != nullptr)]);
+        rc = allow_smem((const void *)k, kRingMost, &done[4 * vec + 2 * wide + (a.parts != nullptr)]);
         if (!rc) rc = tula::launch(k, dim3(l.grid), l.threads, smem, s, l.cluster, a);
     } else {
         if (a.y) rc = tula::launch(k_norm_backward_wide<T>, dim3(l.grid), l.threads, 0, s, 1, a);
