@@ -281,6 +281,9 @@ int tula_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, i
                              const float *stats, void *dx, void *dweight, void *dbias,
                              void *workspace, size_t workspace_bytes, void *stream);
 
+/* The error word of these kernels, as tula_mx_error. */
+int tula_layer_norm_error(void *stream, int *error_out);
+
 /* ---------------------------------------------------------------------------------------------
  * Orthogonalised updates (Muon)
  * ------------------------------------------------------------------------------------------ */

@@ -14,7 +14,7 @@ from torch.autograd.function import once_differentiable
 from .mx import _call as _mx_call
 from .mx import _i64, _on_gpu, _type
 from .optim import TYPES
-from .tula_ags import _check, c_float, c_int, c_size_t, c_void_p, lib
+from .tula_ags import _check, _stream_ptr, c_float, c_int, c_size_t, c_void_p, lib
 
 _fns = None  # the library's functions, their types declared
 
@@ -28,6 +28,7 @@ def _lib():
         L.tula_layer_norm_workspace_size.argtypes = [_i64, _i64, ctypes.POINTER(c_size_t)]
         L.tula_layer_norm_backward.argtypes = [c_void_p, _i64, c_void_p, _i64, c_int, _i64, _i64, c_void_p, c_int,
                                                c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+        L.tula_layer_norm_error.argtypes = [c_void_p, ctypes.POINTER(c_int)]
         _fns = L
     return _fns
 
@@ -41,6 +42,14 @@ def _call(name, dev, *args):
 def tula_layer_norm_workspace_size(rows: int, cols: int) -> int:
     out = c_size_t(0)
     _check(_lib().tula_layer_norm_workspace_size(rows, cols, ctypes.byref(out)), "tula_layer_norm_workspace_size")
+    return out.value
+
+
+def tula_layer_norm_error(stream=None) -> int:
+    """Reads and clears the kernels' error word after the work on `stream` (synchronous): 0 = every wait
+    inside them completed."""
+    out = c_int(0)
+    _check(_lib().tula_layer_norm_error(_stream_ptr(stream), ctypes.byref(out)), "tula_layer_norm_error")
     return out.value
 
 

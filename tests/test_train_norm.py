@@ -37,6 +37,7 @@ def test_refusals_of_the_library():
     need = norm.tula_layer_norm_workspace_size(4, 8)
     short = L.tula_layer_norm_backward(p, 8, p, 8, 0, 4, 8, p, 0, p, p, p, n, p, need - 1, n)
     assert short == backward(dw=p) == -2
+    assert L.tula_layer_norm_error(n, n) == -1
     with pytest.raises(TulaError):
         norm.tula_layer_norm_workspace_size(-1, 8)
 
@@ -124,6 +125,7 @@ def test_layer_norm(rows, cols, dtype):
         first = _check(*_inputs(rows, cols, dtype, wtype, rows + cols))
         again = _check(*_inputs(rows, cols, dtype, wtype, rows + cols))
         assert all(torch.equal(a, b) for a, b in zip(first, again))
+    assert norm.tula_layer_norm_error() == 0
 
 
 @pytest.mark.gpu
