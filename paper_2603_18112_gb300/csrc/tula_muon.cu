@@ -802,14 +802,16 @@ __global__ void __launch_bounds__(kStreamThreads, kStreamCtas) k_muon_first(cons
 
 // u / |u| as u f1 f2: f1 a power of two that brings u near 1, exactly, wherever in fp32's range it is.  A matrix of
 // zeros stays, one with an infinity or NaN becomes NaN.  The norm is taken by every CTA for itself: one of
-// its warps fetches the matrix's parts from L2 while the tile is on its way, one thread ends in fp64 (an SM does
-// some two of its operations a cycle: by all threads they took a third of the kernel's time).
+// its warps fetches the matrix's parts from L2 while the tile is on its way, one thread ends (an SM does
+// some two fp64 operations a cycle: by all threads they took a third of the kernel's time).
 __device__ __forceinline__ float2 factors_of(double squares, float scale) {
-    const double norm = sqrt(squares);
-    if (!(norm < 1e300)) return make_float2(__uint_as_float(0x7fffffffu), __uint_as_float(0x7fffffffu));
-    if (!(norm > 0.0)) return make_float2(0.f, 0.f);
-    const int k = max(-126, min(126, (int)((unsigned)__double2hiint(norm) >> 20) - 1023));
-    return make_float2(__uint_as_float((unsigned)(127 - k) << 23), (float)((double)scale / norm * __hiloint2double((1023 + k) << 20, 0)));
+    if (!(squares < 1e300)) return make_float2(__uint_as_float(0x7fffffffu), __uint_as_float(0x7fffffffu));
+    if (!(squares > 0.0)) return make_float2(0.f, 0.f);
+    // |u| = root 2^k, 1 <= root < 2, in fp32 from here on
+    const int k = ((int)((unsigned)__double2hiint(squares) >> 20) - 1023) >> 1;
+    const float root = sqrtf((float)(squares * __hiloint2double((1023 - 2 * k) << 20, 0)));
+    const int c = max(-126, min(126, k));
+    return make_float2(__uint_as_float((unsigned)(127 - c) << 23), __fdiv_rn(scale, root) * __uint_as_float((unsigned)(127 + c - k) << 23));
 }
 __device__ __forceinline__ float2 norm_factors(const StreamArgs &a, const Place &p, float2 *factors) {
     if (threadIdx.x < 32) {
@@ -822,9 +824,7 @@ __device__ __forceinline__ float2 norm_factors(const StreamArgs &a, const Place 
                 const int i = i0 + 32 * k + threadIdx.x;
                 v[k] = i < p.g->per ? __ldcg(parts + i) : 0.0;
             }
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (i0 + 32 * k < p.g->per) s += v[k];
+            s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
         }
         for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
         if (threadIdx.x == 0) {
