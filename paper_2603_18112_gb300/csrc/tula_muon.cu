@@ -66,7 +66,7 @@ struct Matrix {  // of a plan
     const void *g;
     float *m, *w;
     void *copy;
-    int gtype, ctype, vec, spare;  // vec: eight elements of a row at a time, on boundaries of 16 bytes (w: 32)
+    int gtype, ctype, vec, spare;  // vec: elements of a row at a time, see load_tile
 };
 struct ProductGroup {
     Side p, q;
@@ -600,8 +600,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 // Before and after the products
 // ----------------------------------------------------------------------------
 //
-// One CTA a tile of 128 x 64, 32 elements a thread: eight of a row at a time where all buffers allow it (Vec:
-// rows of a multiple of eight elements at 16-byte boundaries), else one.  These stream: 8 to 22 bytes an
+// One CTA a tile of 128 x 64, 32 elements a thread, V of a row at a time: eight where all buffers' rows have a
+// multiple of eight at boundaries of 16 bytes, two where they have an even number at boundaries of two (6 of
+// 4099 x 1502 bf16: 110 us for the three kernels, 149 one by one and three CTAs an SM), else one.  These stream: 8 to 22 bytes an
 // element.
 
 struct Group {
@@ -627,7 +628,11 @@ struct StreamArgs {
 };
 static_assert(sizeof(StreamArgs) <= 4096 - 64, "kernel parameters");
 
-constexpr int kStreamThreads = 256, kStreamCtas = 3;  // CTAs an SM, that registers are left for
+constexpr int kStreamThreads = 256;
+// CTAs an SM, that registers are left for: of a plan's matrices, which have a momentum or weights to hold too, and
+// of others (with three for both, 145 us for those; k_muon_scale has four, at five it spills).
+template <bool Plan>
+constexpr int kStreamCtas = Plan ? 3 : 5;
 
 struct Place {
     const Group *g;
@@ -646,10 +651,10 @@ __device__ __forceinline__ Place place_of(const StreamArgs &a, int t) {
     return p;
 }
 // Element k of a thread's 32, within the tile.
-template <bool Vec>
-__device__ __forceinline__ int row_of(int k) { return Vec ? (k >> 3) * 32 + (threadIdx.x >> 3) : k * 4 + (threadIdx.x >> 6); }
-template <bool Vec>
-__device__ __forceinline__ int col_of(int k) { return Vec ? (threadIdx.x & 7) * 8 + (k & 7) : threadIdx.x & 63; }
+template <int V>
+__device__ __forceinline__ int row_of(int k) { return k / V * (4 * V) + threadIdx.x / (kTileCols / V); }
+template <int V>
+__device__ __forceinline__ int col_of(int k) { return threadIdx.x % (kTileCols / V) * V + k % V; }
 
 __device__ __forceinline__ float value(float v) { return v; }
 __device__ __forceinline__ float value(__nv_bfloat16 v) { return __bfloat162float(v); }
@@ -660,13 +665,13 @@ struct alignas(sizeof(T) * N < 16 ? sizeof(T) * N : 16) Run {
     T v[N];
 };
 // A thread's elements of a matrix whose rows lie `stride` apart; zero beyond it.
-template <typename T, bool Vec>
+template <typename T, int V>
 __device__ __forceinline__ void load_tile(float (&f)[32], const T *base, long long stride, const Place &p) {
-    constexpr int kN = Vec ? 8 : 1;
+    constexpr int kN = V;
     Run<T, kN> r[32 / kN];
 #pragma unroll
     for (int k = 0; k < 32; k += kN) {
-        const int i = p.row0 + row_of<Vec>(k), j = p.col0 + col_of<Vec>(k);
+        const int i = p.row0 + row_of<V>(k), j = p.col0 + col_of<V>(k);
         if (i < p.g->rows && j < p.g->cols)
             r[k / kN] = *reinterpret_cast<const Run<T, kN> *>(base + i * stride + j);
         else
@@ -676,12 +681,12 @@ __device__ __forceinline__ void load_tile(float (&f)[32], const T *base, long lo
 #pragma unroll
     for (int k = 0; k < 32; ++k) f[k] = value(r[k / kN].v[k % kN]);
 }
-template <typename T, bool Vec>
+template <typename T, int V>
 __device__ __forceinline__ void store_tile(T *base, long long stride, const Place &p, const float (&f)[32]) {
-    constexpr int kN = Vec ? 8 : 1;
+    constexpr int kN = V;
 #pragma unroll
     for (int k = 0; k < 32; k += kN) {
-        const int i = p.row0 + row_of<Vec>(k), j = p.col0 + col_of<Vec>(k);
+        const int i = p.row0 + row_of<V>(k), j = p.col0 + col_of<V>(k);
         if (i >= p.g->rows || j >= p.g->cols) continue;
         Run<T, kN> r;
 #pragma unroll
@@ -689,21 +694,21 @@ __device__ __forceinline__ void store_tile(T *base, long long stride, const Plac
         *reinterpret_cast<Run<T, kN> *>(base + i * stride + j) = r;
     }
 }
-template <bool Vec>
+template <int V>
 __device__ __forceinline__ void load_typed(float (&f)[32], const void *base, int type, long long stride, const Place &p) {
     if (type == TULA_TYPE_F32)
-        load_tile<float, Vec>(f, static_cast<const float *>(base), stride, p);
+        load_tile<float, V>(f, static_cast<const float *>(base), stride, p);
     else if (type == TULA_TYPE_BF16)
-        load_tile<__nv_bfloat16, Vec>(f, static_cast<const __nv_bfloat16 *>(base), stride, p);
+        load_tile<__nv_bfloat16, V>(f, static_cast<const __nv_bfloat16 *>(base), stride, p);
     else
-        load_tile<__half, Vec>(f, static_cast<const __half *>(base), stride, p);
+        load_tile<__half, V>(f, static_cast<const __half *>(base), stride, p);
 }
-template <bool Vec>
+template <int V>
 __device__ __forceinline__ void store_typed(void *base, int type, long long stride, const Place &p, const float (&f)[32]) {
     if (type == TULA_TYPE_BF16)
-        store_tile<__nv_bfloat16, Vec>(static_cast<__nv_bfloat16 *>(base), stride, p, f);
+        store_tile<__nv_bfloat16, V>(static_cast<__nv_bfloat16 *>(base), stride, p, f);
     else
-        store_tile<__half, Vec>(static_cast<__half *>(base), stride, p, f);
+        store_tile<__half, V>(static_cast<__half *>(base), stride, p, f);
 }
 // A plan's element type starts at the matrix; another's matrices lie batch_stride apart.
 __device__ __forceinline__ const void *batch_at(const StreamArgs &a, int matrix) {
@@ -716,17 +721,17 @@ template <bool Plan>
 struct Loaded {
     float g[32], m[Plan ? 32 : 1], mult;
 };
-template <bool Plan, bool Vec>
+template <bool Plan, int V>
 __device__ __forceinline__ void load_parts(Loaded<Plan> &l, const StreamArgs &a, const Place &p, const Matrix &q) {
     if constexpr (Plan) {
         l.mult = a.record ? __fdiv_rn(a.record[TULA_RECORD_COEF], a.grad_scale) : __fdiv_rn(1.f, a.grad_scale);
-        load_typed<Vec>(l.g, q.g, q.gtype, p.g->cols, p);
-        load_tile<float, Vec>(l.m, q.m, p.g->cols, p);
+        load_typed<V>(l.g, q.g, q.gtype, p.g->cols, p);
+        load_tile<float, V>(l.m, q.m, p.g->cols, p);
     } else {
-        load_typed<Vec>(l.g, batch_at(a, p.matrix), a.xtype, a.stride, p);
+        load_typed<V>(l.g, batch_at(a, p.matrix), a.xtype, a.stride, p);
     }
 }
-template <bool First, bool Plan, bool Vec>
+template <bool First, bool Plan, int V>
 __device__ __forceinline__ void update_of(float (&u)[32], Loaded<Plan> &l, const StreamArgs &a, const Place &p, const Matrix &q) {
     if constexpr (Plan) {
 #pragma unroll
@@ -735,23 +740,17 @@ __device__ __forceinline__ void update_of(float (&u)[32], Loaded<Plan> &l, const
             if (First) l.m[k] = fmaf(a.mu, l.m[k], d);
             u[k] = a.nesterov ? fmaf(a.mu, l.m[k], d) : l.m[k];
         }
-        if (First) store_tile<float, Vec>(q.m, p.g->cols, p, l.m);
+        if (First) store_tile<float, V>(q.m, p.g->cols, p, l.m);
     } else {
 #pragma unroll
         for (int k = 0; k < 32; ++k) u[k] = l.g[k];
     }
 }
-template <bool First, bool Vec>
+template <bool First, bool Plan, int V>
 __device__ __forceinline__ void load_update(float (&u)[32], const StreamArgs &a, const Place &p, const Matrix &q) {
-    if (a.matrices) {
-        Loaded<true> l;
-        load_parts<true, Vec>(l, a, p, q);
-        update_of<First, true, Vec>(u, l, a, p, q);
-    } else {
-        Loaded<false> l;
-        load_parts<false, Vec>(l, a, p, q);
-        update_of<First, false, Vec>(u, l, a, p, q);
-    }
+    Loaded<Plan> l;
+    load_parts<Plan, V>(l, a, p, q);
+    update_of<First, Plan, V>(u, l, a, p, q);
 }
 
 // The sum of squares of a warp's elements: in fp32 with an exact power of two taken out, so that no square
@@ -773,26 +772,28 @@ __device__ __forceinline__ void warp_squares(const float (&u)[32], double *sums)
     if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = (double)s * __hiloint2double((1023 + 2 * ((int)e - 127)) << 20, 0);
 }
 
-template <bool Vec>
+template <bool Plan, int V>
 __device__ __forceinline__ void first_tile(const StreamArgs &a, const Place &p, const Matrix &q, double *sums) {
     float u[32];
-    load_update<true, Vec>(u, a, p, q);
+    load_update<true, Plan, V>(u, a, p, q);
     warp_squares(u, sums);
 }
 __device__ __forceinline__ bool left_out(const StreamArgs &a) { return a.record && a.record[TULA_RECORD_FINITE] == 0.f; }
 
-__global__ void __launch_bounds__(kStreamThreads, kStreamCtas) k_muon_first(const __grid_constant__ StreamArgs a) {
+template <bool Plan>
+__global__ void __launch_bounds__(kStreamThreads, kStreamCtas<Plan>) k_muon_first(const __grid_constant__ StreamArgs a) {
     __shared__ double sums[kStreamThreads / 32];
     let_next_start();
     wait_for_previous();
     if (left_out(a)) return;
     const Place p = place_of(a, blockIdx.x);
     Matrix q = {};
-    if (a.matrices) q = a.matrices[p.g->matrix + p.matrix];
-    if (a.matrices ? q.vec : a.vec)
-        first_tile<true>(a, p, q, sums);
-    else
-        first_tile<false>(a, p, q, sums);
+    if (Plan) q = a.matrices[p.g->matrix + p.matrix];
+    switch (Plan ? q.vec : a.vec) {
+        case 8: first_tile<Plan, 8>(a, p, q, sums); break;
+        case 2: first_tile<Plan, 2>(a, p, q, sums); break;
+        default: first_tile<Plan, 1>(a, p, q, sums);
+    }
     __syncthreads();
     if (threadIdx.x) return;
     double s = 0.0;
@@ -836,81 +837,85 @@ __device__ __forceinline__ float2 norm_factors(const StreamArgs &a, const Place 
 }
 
 // Elements of X from k on.
-template <bool Vec>
-__device__ __forceinline__ Run<__half, Vec ? 8 : 1> scaled_run(const float (&u)[32], int k, const Place &p, float2 f) {
-    Run<__half, Vec ? 8 : 1> r;
+template <int V>
+__device__ __forceinline__ Run<__half, V> scaled_run(const float (&u)[32], int k, const Place &p, float2 f) {
+    Run<__half, V> r;
 #pragma unroll
-    for (int e = 0; e < (Vec ? 8 : 1); ++e) {
+    for (int e = 0; e < V; ++e) {
         // (a NaN factor leaves the zeros beyond the matrix alone)
-        const bool in = p.row0 + row_of<Vec>(k + e) < p.g->rows && p.col0 + col_of<Vec>(k + e) < p.g->cols;
+        const bool in = p.row0 + row_of<V>(k + e) < p.g->rows && p.col0 + col_of<V>(k + e) < p.g->cols;
         r.v[e] = __float2half_rn(in ? __fmul_rn(__fmul_rn(u[k + e], f.x), f.y) : 0.f);
     }
     return r;
 }
-template <bool Vec>
+template <bool Plan, int V>
 __device__ __forceinline__ void scale_tile(const StreamArgs &a, const Place &p, const Matrix &q, float2 *factors) {
     float u[32];
-    load_update<false, Vec>(u, a, p, q);
+    load_update<false, Plan, V>(u, a, p, q);
     const float2 f = norm_factors(a, p, factors);
     __half *x = reinterpret_cast<__half *>(a.tiles + (size_t)(p.g->x + p.matrix * p.g->per + p.tile) * kTileBytes);
-    constexpr int kN = Vec ? 8 : 1;
+    constexpr int kN = V;
 #pragma unroll
     for (int k = 0; k < 32; k += kN)
-        *reinterpret_cast<Run<__half, kN> *>(x + row_of<Vec>(k) * kTileCols + col_of<Vec>(k)) = scaled_run<Vec>(u, k, p, f);
+        *reinterpret_cast<Run<__half, kN> *>(x + row_of<V>(k) * kTileCols + col_of<V>(k)) = scaled_run<V>(u, k, p, f);
 }
-__global__ void __launch_bounds__(kStreamThreads, kStreamCtas) k_muon_scale(const __grid_constant__ StreamArgs a) {
+template <bool Plan>
+__global__ void __launch_bounds__(kStreamThreads, Plan ? 3 : 4) k_muon_scale(const __grid_constant__ StreamArgs a) {
     __shared__ float2 factors;
     let_next_start();
     wait_for_previous();
     if (left_out(a)) return;
     const Place p = place_of(a, blockIdx.x);
     Matrix q = {};
-    if (a.matrices) q = a.matrices[p.g->matrix + p.matrix];
-    if (a.matrices ? q.vec : a.vec)
-        scale_tile<true>(a, p, q, &factors);
-    else
-        scale_tile<false>(a, p, q, &factors);
+    if (Plan) q = a.matrices[p.g->matrix + p.matrix];
+    switch (Plan ? q.vec : a.vec) {
+        case 8: scale_tile<Plan, 8>(a, p, q, &factors); break;
+        case 2: scale_tile<Plan, 2>(a, p, q, &factors); break;
+        default: scale_tile<Plan, 1>(a, p, q, &factors);
+    }
 }
 
 // A tile of O(u) to the weights and their copies, or as it is.
-template <bool Vec>
+template <bool Plan, int V>
 __device__ __forceinline__ void finish_tile(const StreamArgs &a, const Place &p, const Matrix &q, const float (&x)[32]) {
-    if (!a.matrices) {
+    if constexpr (!Plan) {
         const size_t at = (size_t)p.matrix * p.g->rows * p.g->cols * 2;
-        store_typed<Vec>(static_cast<unsigned char *>(a.y) + at, a.ytype, p.g->cols, p, x);
-        return;
-    }
-    float w[32];
-    load_tile<float, Vec>(w, q.w, p.g->cols, p);
+        store_typed<V>(static_cast<unsigned char *>(a.y) + at, a.ytype, p.g->cols, p, x);
+    } else {
+        float w[32];
+        load_tile<float, V>(w, q.w, p.g->cols, p);
 #pragma unroll
-    for (int k = 0; k < 32; ++k) w[k] = fmaf(-p.g->step, x[k], __fmul_rn(w[k], a.decay));
-    store_tile<float, Vec>(q.w, p.g->cols, p, w);
-    if (q.copy) store_typed<Vec>(q.copy, q.ctype, p.g->cols, p, w);
+        for (int k = 0; k < 32; ++k) w[k] = fmaf(-p.g->step, x[k], __fmul_rn(w[k], a.decay));
+        store_tile<float, V>(q.w, p.g->cols, p, w);
+        if (q.copy) store_typed<V>(q.copy, q.ctype, p.g->cols, p, w);
+    }
 }
-template <bool Vec>
+template <bool Plan, int V>
 __device__ __forceinline__ void last_tile(const StreamArgs &a, const Place &p, const Matrix &q) {
     float x[32];
     const __half *from = reinterpret_cast<const __half *>(a.tiles + (size_t)(p.g->x_last + p.matrix * p.g->per + p.tile) * kTileBytes);
-    constexpr int kN = Vec ? 8 : 1;
+    constexpr int kN = V;
 #pragma unroll
     for (int k = 0; k < 32; k += kN) {
-        const Run<__half, kN> r = *reinterpret_cast<const Run<__half, kN> *>(from + row_of<Vec>(k) * kTileCols + col_of<Vec>(k));
+        const Run<__half, kN> r = *reinterpret_cast<const Run<__half, kN> *>(from + row_of<V>(k) * kTileCols + col_of<V>(k));
 #pragma unroll
         for (int e = 0; e < kN; ++e) x[k + e] = __half2float(r.v[e]);
     }
-    finish_tile<Vec>(a, p, q, x);
+    finish_tile<Plan, V>(a, p, q, x);
 }
-__global__ void __launch_bounds__(kStreamThreads, kStreamCtas) k_muon_last(const __grid_constant__ StreamArgs a) {
+template <bool Plan>
+__global__ void __launch_bounds__(kStreamThreads, kStreamCtas<Plan>) k_muon_last(const __grid_constant__ StreamArgs a) {
     let_next_start();
     wait_for_previous();
     if (left_out(a)) return;
     const Place p = place_of(a, a.tile0 + blockIdx.x);
     Matrix q = {};
-    if (a.matrices) q = a.matrices[p.g->matrix + p.matrix];
-    if (a.matrices ? q.vec : a.vec)
-        last_tile<true>(a, p, q);
-    else
-        last_tile<false>(a, p, q);
+    if (Plan) q = a.matrices[p.g->matrix + p.matrix];
+    switch (Plan ? q.vec : a.vec) {
+        case 8: last_tile<Plan, 8>(a, p, q); break;
+        case 2: last_tile<Plan, 2>(a, p, q); break;
+        default: last_tile<Plan, 1>(a, p, q);
+    }
 }
 
 // ----------------------------------------------------------------------------
@@ -952,7 +957,7 @@ struct Small {
     }
 };
 
-template <bool Plan, bool Vec>
+template <bool Plan, int V>
 __device__ __forceinline__ void small_load(const StreamArgs &a, Place p, const Matrix &q, int tiles, unsigned char *x, double *sums,
                                            float2 *factors) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, pitch = p.g->pitch;
@@ -965,14 +970,14 @@ __device__ __forceinline__ void small_load(const StreamArgs &a, Place p, const M
 #pragma unroll
         for (int h = 0; h < kAhead; ++h) {
             tile(t0 + h);
-            if (t0 + h < tiles) load_parts<Plan, Vec>(l[h], a, p, q);
+            if (t0 + h < tiles) load_parts<Plan, V>(l[h], a, p, q);
         }
 #pragma unroll
         for (int h = 0; h < kAhead; ++h) {
             if (t0 + h >= tiles) break;
             tile(t0 + h);
             float u[32];
-            update_of<true, Plan, Vec>(u, l[h], a, p, q);
+            update_of<true, Plan, V>(u, l[h], a, p, q);
             warp_squares(u, sums);
             if (lane == 0) total += sums[warp];
         }
@@ -986,42 +991,45 @@ __device__ __forceinline__ void small_load(const StreamArgs &a, Place p, const M
     }
     __syncthreads();
     const float2 f = *factors;
-    constexpr int kN = Vec ? 8 : 1;
+    constexpr int kN = V;
     for (int t0 = 0; t0 < tiles; t0 += kAhead) {
 #pragma unroll
         for (int h = 0; h < kAhead; ++h) {
             tile(t0 + h);
-            if (t0 + h < tiles) load_parts<Plan, Vec>(l[h], a, p, q);
+            if (t0 + h < tiles) load_parts<Plan, V>(l[h], a, p, q);
         }
 #pragma unroll
         for (int h = 0; h < kAhead; ++h) {
             if (t0 + h >= tiles) break;
             tile(t0 + h);
             float u[32];
-            update_of<false, Plan, Vec>(u, l[h], a, p, q);
+            update_of<false, Plan, V>(u, l[h], a, p, q);
 #pragma unroll
             for (int k = 0; k < 32; k += kN) {
-                const Run<__half, kN> r = scaled_run<Vec>(u, k, p, f);
-                *reinterpret_cast<Run<__half, kN> *>(x + (t0 + h) * kTileBytes + small_place(row_of<Vec>(k), col_of<Vec>(k))) = r;
+                const Run<__half, kN> r = scaled_run<V>(u, k, p, f);
+                *reinterpret_cast<Run<__half, kN> *>(x + (t0 + h) * kTileBytes + small_place(row_of<V>(k), col_of<V>(k))) = r;
             }
         }
     }
 }
-template <bool Vec>
+template <int V>
 __device__ __forceinline__ void small_store(const StreamArgs &a, Place p, const Matrix &q, int tiles, const unsigned char *x) {
     const int pitch = p.g->pitch;
     for (int t = 0; t < tiles; ++t) {
         p.row0 = t / pitch * kTile, p.col0 = t % pitch * kTileCols;
         float f[32];
-        constexpr int kN = Vec ? 8 : 1;
+        constexpr int kN = V;
 #pragma unroll
         for (int k = 0; k < 32; k += kN) {
             const Run<__half, kN> r =
-                *reinterpret_cast<const Run<__half, kN> *>(x + t * kTileBytes + small_place(row_of<Vec>(k), col_of<Vec>(k)));
+                *reinterpret_cast<const Run<__half, kN> *>(x + t * kTileBytes + small_place(row_of<V>(k), col_of<V>(k)));
 #pragma unroll
             for (int e = 0; e < kN; ++e) f[k + e] = __half2float(r.v[e]);
         }
-        finish_tile<Vec>(a, p, q, f);
+        if (a.matrices)
+            finish_tile<true, V>(a, p, q, f);
+        else
+            finish_tile<false, V>(a, p, q, f);
     }
 }
 
@@ -1073,17 +1081,22 @@ __global__ void __launch_bounds__(kStreamThreads, 1) k_muon_small(const __grid_c
     const bool wide = rows <= cols, go = !left_out(a);
     Matrix q = {};
     if (a.matrices) q = a.matrices[p.g->matrix + p.matrix];
-    const bool vec = a.matrices ? q.vec : a.vec;
+    const int vec = a.matrices ? q.vec : a.vec;
     Small m{smem_addr(x), smem_addr(x) + kSmallTiles * kTileBytes, smem_addr(&bar), &dead, 0, 0};
     if (go) {
-        if (a.matrices && vec)
-            small_load<true, true>(a, p, q, tiles, x, sums, &factors);
-        else if (a.matrices)
-            small_load<true, false>(a, p, q, tiles, x, sums, &factors);
-        else if (vec)
-            small_load<false, true>(a, p, q, tiles, x, sums, &factors);
-        else
-            small_load<false, false>(a, p, q, tiles, x, sums, &factors);
+        if (a.matrices) {
+            switch (vec) {
+                case 8: small_load<true, 8>(a, p, q, tiles, x, sums, &factors); break;
+                case 2: small_load<true, 2>(a, p, q, tiles, x, sums, &factors); break;
+                default: small_load<true, 1>(a, p, q, tiles, x, sums, &factors);
+            }
+        } else {
+            switch (vec) {
+                case 8: small_load<false, 8>(a, p, q, tiles, x, sums, &factors); break;
+                case 2: small_load<false, 2>(a, p, q, tiles, x, sums, &factors); break;
+                default: small_load<false, 1>(a, p, q, tiles, x, sums, &factors);
+            }
+        }
     }
     m.before();  // (and tensor memory is there)
     m.tmem = __shfl_sync(kFull, tmem_at, 0);
@@ -1196,10 +1209,11 @@ __global__ void __launch_bounds__(kStreamThreads, 1) k_muon_small(const __grid_c
         m.before();
     }
     if (go) {
-        if (vec)
-            small_store<true>(a, p, q, tiles, x);
-        else
-            small_store<false>(a, p, q, tiles, x);
+        switch (vec) {
+            case 8: small_store<8>(a, p, q, tiles, x); break;
+            case 2: small_store<2>(a, p, q, tiles, x); break;
+            default: small_store<1>(a, p, q, tiles, x);
+        }
     }
     if (warp == 0) tmem_free(m.tmem, kSmallSums);
 }
@@ -1305,7 +1319,7 @@ int fill(ProductArgs &a, const Kin *kin, int n, Kind kind, int x, bool first) {
         across.way = kAcross;
         g.n = (int)k.n();
         g.alpha = 1.f;
-        g.finish = kind == kLast && k.vec;
+        g.finish = kind == kLast && k.vec == 8;
         g.rows = (int)k.rows;
         g.cols = (int)k.cols;
         g.matrix = k.matrix;
@@ -1413,8 +1427,9 @@ int run(const Maps &maps, long long n_tiles, const Kin *kin, int n, StreamArgs &
     }
     if (tiles == 0) return TULA_OK;
     // (By parts of 48 MB, that the second of the two would find in L2, they take longer: 12 to 14 us a launch.)
-    int rc = tula::launch(k_muon_first, dim3((unsigned)tiles), kStreamThreads, 0, s, 1, st);
-    if (!rc) rc = tula::launch(k_muon_scale, dim3((unsigned)tiles), kStreamThreads, 0, s, 1, st);
+    const bool plan = st.matrices != nullptr;
+    int rc = tula::launch(plan ? k_muon_first<true> : k_muon_first<false>, dim3((unsigned)tiles), kStreamThreads, 0, s, 1, st);
+    if (!rc) rc = tula::launch(plan ? k_muon_scale<true> : k_muon_scale<false>, dim3((unsigned)tiles), kStreamThreads, 0, s, 1, st);
     for (int i = 0; !rc && i < steps; ++i) {
         rc = product<kGram>(maps, a, kin, n, i & 1, i == 0, sms, s);
         if (!rc) rc = product<kPoly>(maps, a, kin, n, i & 1, i == 0, sms, s);
@@ -1424,9 +1439,9 @@ int run(const Maps &maps, long long n_tiles, const Kin *kin, int n, StreamArgs &
     }
     // what the last product has not finished
     st.tile0 = 0;
-    for (int i = 0; steps && i < n && kin[i].vec; ++i) st.tile0 += st.g[i].per * kin[i].count;
+    for (int i = 0; steps && i < n && kin[i].vec == 8; ++i) st.tile0 += st.g[i].per * kin[i].count;
     if (!rc && st.tile0 < tiles)
-        rc = tula::launch(k_muon_last, dim3((unsigned)(tiles - st.tile0)), kStreamThreads, 0, s, 1, st);
+        rc = tula::launch(plan ? k_muon_last<true> : k_muon_last<false>, dim3((unsigned)(tiles - st.tile0)), kStreamThreads, 0, s, 1, st);
     return rc;
 }
 
@@ -1539,7 +1554,12 @@ int tula_muon_plan_create(const tula_muon_matrices *m, void *workspace, size_t w
                 (m->copy_ptrs && !q.copy) || !aligned(q.g, type_size(q.gtype)) || !aligned(q.m, 4) || !aligned(q.w, 4) ||
                 !aligned(q.copy, 2))
                 return TULA_ERR_ARG;
-            q.vec = vec[(size_t)i] = m->cols[i] % 8 == 0 && aligned(q.g, 16) && aligned(q.m, 16) && aligned(q.w, 32) && aligned(q.copy, 16);
+            const unsigned two = 2 * type_size(q.gtype);
+            if (m->cols[i] % 8 == 0 && aligned(q.g, 16) && aligned(q.m, 16) && aligned(q.w, 32) && aligned(q.copy, 16))
+                q.vec = 8;
+            else
+                q.vec = m->cols[i] % 2 == 0 && aligned(q.g, two) && aligned(q.m, 8) && aligned(q.w, 8) && aligned(q.copy, 4) ? 2 : 1;
+            vec[(size_t)i] = q.vec;
         }
         // a buffer that two matrices would write
         std::vector<const void *> written;
@@ -1667,9 +1687,13 @@ int tula_orthogonalize(const void *x, int type, int64_t batch, int64_t rows, int
         st.parts = static_cast<double *>(workspace);
         st.tiles = static_cast<unsigned char *>(workspace) + z.parts;
         st.grad_scale = 1.f;
-        const size_t size = type_size(type), of16 = 16 / size;
-        st.vec = cols % 8 == 0 && aligned(x, 16) && aligned(out, 16) && (rows == 1 || stride % of16 == 0) &&
-                 (batch == 1 || batch_stride % of16 == 0);
+        const size_t size = type_size(type);
+        auto lies = [&](unsigned n, unsigned bytes) {  // runs of n elements at boundaries of n, or of so many bytes
+            const unsigned at = std::min<unsigned>(n, 16 / (unsigned)size);
+            return cols % n == 0 && aligned(x, at * (unsigned)size) && aligned(out, bytes) && (rows == 1 || stride % at == 0) &&
+                   (batch == 1 || batch_stride % at == 0);
+        };
+        st.vec = lies(8, 16) ? 8 : lies(2, 4) ? 2 : 1;
         kin[0].vec = st.vec;
         Maps maps;
         std::memset(&maps, 0, sizeof(maps));
