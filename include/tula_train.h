@@ -293,15 +293,15 @@ int tula_layer_norm_error(void *stream, int *error_out);
  *   X <- a X + b A X + c A^2 X,  A = X X^T,  (a, b, c) = (3.4445, -4.7750, 2.0315)
  * which bring the singular values near 1 (to 0.7 to 1.2 in five steps) and leave the singular vectors.
  * Operands are held in fp16 and summed in fp32, so that values are within about 2e-3 of the formula's
- * relative to the matrix's norm (more where singular values lie far below the largest one: a rounding of
- * 2^-12 of that grows with them).  A matrix with an infinity or NaN gives NaN.
+ * relative to the matrix's norm (up to 5e-3 where the smaller side is a few; more where singular values lie
+ * far below the largest one: a rounding of 2^-12 of that grows with them).  A matrix with an infinity or NaN gives NaN.
  */
 
 /*
  * O of each of `batch` matrices x, device [rows][stride] of `type`, batch_stride elements apart
  * (stride >= cols, batch_stride >= 0), into out, device [batch][rows][cols] of out_type, bf16 or fp16.
  * ns_steps in [0, 100], rows and cols up to 2^20 (TULA_ERR_ARG).  The workspace (256-byte aligned, any
- * contents; some 6 to 8 bytes an element, TULA_ERR_ARG beyond 256 GB) may be used again by what is
+ * contents; some 4 to 8 bytes an element, of tiles of 128 x 64, TULA_ERR_ARG beyond 256 GB) may be used again by what is
  * enqueued after; calls that share one must be ordered.  Sums depend on sizes and alignments only.
  */
 int tula_orthogonalize_workspace_size(int64_t batch, int64_t rows, int64_t cols, size_t *bytes);
@@ -323,7 +323,8 @@ typedef struct tula_muon_matrices {
     const int *copy_types;             /* TULA_TYPE_BF16 or TULA_TYPE_F16; NULL: all bf16 */
 } tula_muon_matrices;
 
-/* Bytes of device workspace a plan over these sizes needs (host only): some 6 to 8 an element.
+/* Bytes of device workspace a plan over these sizes needs (host only): some 4 to 8 an element, of tiles of
+ * 128 x 64; a few for a list of matrices that an SM's shared memory holds (smaller sides up to 128).
  * TULA_ERR_ARG for sizes beyond the limits and for more than 256 GB. */
 int tula_muon_workspace_size(const int64_t *rows, const int64_t *cols, int n_matrices, size_t *bytes);
 

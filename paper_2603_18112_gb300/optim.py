@@ -341,7 +341,8 @@ class MuonStep:
 
 def orthogonalize(x: torch.Tensor, steps: int = 5, dtype=torch.bfloat16) -> torch.Tensor:
     """The matrix x, or each matrix of a batch [..., rows, cols] (fp32, bf16 or fp16), with its singular
-    values brought near 1 by Muon's Newton-Schulz steps, as bf16 or fp16, on the current stream."""
+    values brought near 1 by Muon's Newton-Schulz steps, as bf16 or fp16, on the current stream.  No
+    gradient is recorded."""
     if x.dim() < 2:
         raise ValueError(f"orthogonalize: a matrix or a batch of them is wanted, got {tuple(x.shape)}")
     if x.dtype not in TYPES or dtype not in (torch.bfloat16, torch.float16) or not x.is_cuda:
