@@ -16,8 +16,8 @@
 namespace {
 
 constexpr int kMostThreads = 512;  // of a CTA
-// Of an SM, that registers are left for.  (Forward with 512 too: 79 us instead of 71 for 16384 x
-// 4096 bf16; rows off 16-byte boundaries take 78 us with 512, 160 with 768, for 50000 x 1001.)
+// Of an SM, that registers are left for.  (Forward with 512 too, of an earlier form: 79 us instead of 71 for 16384 x
+// 4096 bf16; rows off 16-byte boundaries took 78 us with 512, 160 with 768, for 50000 x 1001.)
 constexpr int kForwardThreads = 768, kBackwardThreads = 512;
 constexpr int forward_threads(bool vec) { return vec ? kForwardThreads : kBackwardThreads; }
 constexpr int kMostCluster = 8;
@@ -193,14 +193,35 @@ struct GroupSum {
         for (int o = Wide ? 16 : group / 2; o; o >>= 1)
 #pragma unroll
             for (int m = 0; m < N; ++m) v[m] += __shfl_xor_sync(kFull, v[m], o);
-        if constexpr (Wide) across(v);
+        if constexpr (Wide) {
+            if ((threadIdx.x & 31) == 0)
+#pragma unroll
+                for (int m = 0; m < N; ++m) place->warps[turn][m][threadIdx.x >> 5] = v[m];
+            across(v);
+        }
+    }
+    // The same of two, in a warp's five exchanges instead of ten: the halves go on with one each after the first.
+    // (16384 x 4096 bf16 forward 76 us, 87 with ten.  The gradients of parameters leave no registers for it: 105 us
+    // for 102.)
+    __device__ __forceinline__ void two(float (&v)[2]) {
+        const int half = Wide ? 16 : group / 2;
+        if (!Wide && !half) return;  // a thread has its row
+        const bool upper = threadIdx.x & half;
+        float mine = upper ? v[1] : v[0];
+        mine += __shfl_xor_sync(kFull, upper ? v[0] : v[1], half);
+        for (int o = half / 2; o; o >>= 1) mine += __shfl_xor_sync(kFull, mine, o);
+        if constexpr (Wide) {
+            if ((threadIdx.x & 15) == 0) place->warps[turn][upper][threadIdx.x >> 5] = mine;
+            across(v);
+        } else {
+            const float other = __shfl_xor_sync(kFull, mine, half);
+            v[0] = upper ? other : mine;
+            v[1] = upper ? mine : other;
+        }
     }
     template <int N>
     __device__ __forceinline__ void across(float (&v)[N]) {
         const int warp = threadIdx.x >> 5, n = group >> 5;
-        if ((threadIdx.x & 31) == 0)
-#pragma unroll
-            for (int m = 0; m < N; ++m) place->warps[turn][m][warp] = v[m];
         __syncthreads();
 #pragma unroll
         for (int m = 0; m < N; ++m) {
@@ -307,6 +328,16 @@ __device__ __forceinline__ void start_ring(const Ring<T, N, Vec> &ring) {
     __syncthreads();
 }
 
+// The mean comes in two parts: `near` is off by the roundings of its sum, each of them one of the row's size, and
+// what the differences to it add up to, the rest of the mean, is that but for roundings of the differences' size.
+// So a row of equal values gives b, and a row's offset costs no digits.  (From `near` alone 1000 columns of 1000.0
+// had a mean of 1000.00006 and outputs of -0.019 w + b.)  The variance about near + rest from the mean of the
+// squares about near; a NaN stays.
+__device__ __forceinline__ float variance(float squares, float rest) {
+    const float v = fmaf(-rest, rest, squares);
+    return v < 0.f ? 0.f : v;
+}
+
 template <typename T, bool Vec, bool Wide>
 __global__ void __launch_bounds__(forward_threads(Vec)) k_norm_forward(const NormArgs a) {
     using P = Part<T, Vec>;
@@ -355,7 +386,7 @@ __global__ void __launch_bounds__(forward_threads(Vec)) k_norm_forward(const Nor
         now.floats(c);
 #pragma unroll
         for (int k = 0; k < kN; ++k) part[k & 1] += c[k];
-        const float mean = sum(part[0] + part[1]) * inv;
+        const float near = sum(part[0] + part[1]) * inv;
         if (!Wide) __syncthreads();
         if (threadIdx.x < 32 && r0 + a.stages * step < a.rows) {  // all have read the stage
             const long long r1 = r0 + a.stages * step;
@@ -363,18 +394,24 @@ __global__ void __launch_bounds__(forward_threads(Vec)) k_norm_forward(const Nor
             ring.fetch(s, r1, from, stride, (int)min((long long)per, a.rows - r1));
         }
         if (++s == a.stages) s = 0, parity ^= 1;
-        part[0] = part[1] = 0.f;
+        // Chains of additions to either sum (16384 x 4096: bf16 76 us with two, 86 with one; fp32, which has no
+        // registers left, 102 and 95).
+        constexpr int kChains = sizeof(T) == 4 ? 1 : 2;
+        float rests[2] = {0.f, 0.f}, squares[2] = {0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < kN; ++k) {
-            c[k] -= now.in(k) ? mean : 0.f;  // (what the row does not have is 0)
-            part[k & 1] = fmaf(c[k], c[k], part[k & 1]);
+            c[k] -= now.in(k) ? near : 0.f;  // (what the row does not have is 0)
+            rests[k % kChains] += c[k];
+            squares[k % kChains] = fmaf(c[k], c[k], squares[k % kChains]);
         }
-        const float rstd = rsqrtf(sum(part[0] + part[1]) * inv + a.eps);
+        float both[2] = {rests[0] + rests[1], squares[0] + squares[1]};
+        sum.two(both);
+        const float rest = both[0] * inv, rstd = rsqrtf(variance(both[1] * inv, rest) + a.eps), off = -rest * rstd;
         if (there) {
 #pragma unroll
-            for (int k = 0; k < kN; ++k) c[k] = fmaf(c[k] * rstd, w[k], b[k]);
+            for (int k = 0; k < kN; ++k) c[k] = fmaf(fmaf(c[k], rstd, off), w[k], b[k]);
             now.store(static_cast<T *>(a.y) + r * a.cols + col0, c);
-            if (a.stats && t == 0 && col0 == 0) reinterpret_cast<float2 *>(a.stats)[r] = make_float2(mean, rstd);
+            if (a.stats && t == 0 && col0 == 0) reinterpret_cast<float2 *>(a.stats)[r] = make_float2(near + rest, rstd);
         }
     }
 }
@@ -503,19 +540,21 @@ __global__ void __launch_bounds__(kMostThreads) k_norm_forward_wide(const NormAr
         const T *x = static_cast<const T *>(a.x) + r * a.stride;
         float s = 0.f;
         for (int c = threadIdx.x; c < cols; c += blockDim.x) s += value(x[c]);
-        const float mean = sum(s) / (float)cols;
-        s = 0.f;
+        const float near = sum(s) / (float)cols;
+        float both[2] = {0.f, 0.f};
         for (int c = threadIdx.x; c < cols; c += blockDim.x) {
-            const float d = value(x[c]) - mean;
-            s = fmaf(d, d, s);
+            const float d = value(x[c]) - near;
+            both[0] += d;
+            both[1] = fmaf(d, d, both[1]);
         }
-        const float rstd = rsqrtf(sum(s) / (float)cols + a.eps);
+        sum(both);
+        const float rest = both[0] / (float)cols, rstd = rsqrtf(variance(both[1] / (float)cols, rest) + a.eps);
         T *y = static_cast<T *>(a.y) + r * cols;
         for (int c = threadIdx.x; c < cols; c += blockDim.x) {
             const float w = param(a.w, a.ptype, c, 1.f), b = param(a.b, a.ptype, c, 0.f);
-            put(y + c, fmaf((value(x[c]) - mean) * rstd, w, b));
+            put(y + c, fmaf((value(x[c]) - near - rest) * rstd, w, b));
         }
-        if (a.stats && threadIdx.x == 0) reinterpret_cast<float2 *>(a.stats)[r] = make_float2(mean, rstd);
+        if (a.stats && threadIdx.x == 0) reinterpret_cast<float2 *>(a.stats)[r] = make_float2(near + rest, rstd);
     }
 }
 template <typename T>

@@ -1,0 +1,75 @@
+"""Layer norm where its sums and copies can go wrong: rows far from zero, and what follows below."""
+import pytest
+import torch
+
+from paper_2603_18112_gb300 import norm
+
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+ROUND = {t: torch.finfo(t).eps / 2 for t in TYPES}  # a rounding is off by at most half a step
+TINY = {torch.float32: 2.0 ** -149, torch.bfloat16: 2.0 ** -133, torch.float16: 2.0 ** -24}
+U = 2.0 ** -24  # fp32's rounding
+
+# --------------------------------------------------------------------------------------------
+# Rows far from zero
+# --------------------------------------------------------------------------------------------
+
+# one to some warps to a row, several CTAs, and rows that registers do not hold
+WIDTHS = [24, 1000, 1001, 4099, 7168, 12000, 65540]
+
+
+def _depth(cols):
+    """Additions one after the other in a row's sum: of a thread's 16 elements, 5 exchanges, 6 of a CTA's warps and
+    8 of a cluster's CTAs; of wide rows cols / 512 and those of the warp and the CTA."""
+    return 36 if cols <= 65536 else cols // 512 + 14
+
+
+def _forward_exact(x, w, b, eps):
+    """The output in 64 bits and how far it may be off before its last rounding, without a term of the row's
+    size: the mean is near + rest, near off by `depth` roundings of the row's mean magnitude and known exactly
+    from then on, the differences c to it by a rounding each, the rest by depth + 2 roundings of their mean
+    magnitude; the variance by depth + 6 of the mean square of c."""
+    x, w, b = x.double(), w.double(), b.double()
+    cols = x.shape[1]
+    depth = _depth(cols)
+    mean = x.mean(1, keepdim=True)
+    var = (x - mean).square().mean(1, keepdim=True)
+    r = 1 / (var + eps).sqrt()
+    n = (x - mean) * r
+    shift = depth * U * x.abs().mean(1, keepdim=True)  # of near
+    c = (x - mean).abs() + shift
+    off_n = r * U * ((depth + 2) * c.mean(1, keepdim=True) + 2 * c)
+    off_n = off_n + n.abs() * U * ((depth + 6) * (1 + shift.square() * r.square()) + 8)
+    return n * w + b, off_n * w.abs() + 2 * U * (n * w).abs() + 2 * U * b.abs()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", WIDTHS)
+def test_rows_far_from_zero(cols, dtype):
+    """Equal values, and values about a large offset, through all kernels and with rows off 16-byte boundaries."""
+    gen = torch.Generator().manual_seed(cols)
+    offsets = torch.tensor([0.0, 1.0, 1000.0, 3000.0, -1000.0, 0.1, 60000.0, 1e-3]).repeat(8)[:, None]
+    spread = torch.tensor([0.0, 1.0, 1e-2, 30.0]).repeat_interleave(16)[:, None]
+    x = (offsets + spread * torch.randn(64, cols, generator=gen)).clamp(-65504, 65504).to(dtype).cuda()
+    w, b = (1 + 0.3 * torch.randn(cols, generator=gen)).cuda(), (0.2 * torch.randn(cols, generator=gen)).cuda()
+    apart = torch.zeros(64, cols + 3, dtype=dtype, device="cuda")
+    apart[:, 1:cols + 1] = x
+    want, off = _forward_exact(x, w, b, 1e-5)
+    tol = off + 1.01 * ROUND[dtype] * want.abs() + TINY[dtype]
+    for rows in (x, apart[:, 1:cols + 1]):
+        y = norm.layer_norm(rows, w, b)
+        bad = (y.double() - want).abs() - tol
+        assert bool((bad <= 0).all()), [(i, float(v)) for i, v in enumerate(bad.max(1).values) if v > 0][:8]
+    assert norm.tula_layer_norm_error() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cols", WIDTHS)
+def test_mean_of_rows_of_equal_values(cols):
+    """What the backward pass is given: the mean of whole numbers is the number itself."""
+    x = torch.tensor([1000.0, 3000.0, -7.0, 60000.0, 5.0, 333.0], device="cuda")[:, None].expand(6, cols).contiguous()
+    y, stats = norm._forward(x, None, None, 1e-5, True)
+    assert torch.equal(stats[:, 0], x[:, 0])
+    # near is off by depth roundings of the value, the rest that is taken out by depth + 4 of that
+    depth = _depth(cols)
+    assert bool((y.double().abs().amax(1) <= (depth + 4) * U * depth * U * x[:, 0].double().abs() * 1e-5 ** -0.5).all())
