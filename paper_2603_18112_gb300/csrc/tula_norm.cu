@@ -263,7 +263,8 @@ struct GroupSum {
 // The ring: stage s holds the rows of one round of the CTA's groups, of each of N matrices.  Rows off 16-byte
 // boundaries come with what shares their first and last 16 bytes; a round that has the matrix's first or last
 // row, beside which there may be nothing, is read directly.  A wait that runs out leaves what is there: the
-// others end at once then, and the error word says so.
+// others end at once then, nothing more is fetched (a barrier whose phase is not over may not be armed again, nor
+// may a copy be issued over another), and the error word says so.
 template <typename T, int N, bool Vec>
 struct Ring {
     uint32_t at, bars;  // shared addresses
@@ -285,6 +286,7 @@ struct Ring {
     __device__ __forceinline__ void fetch(int s, long long r0, const T *const (&from)[N], const long long (&stride)[N], int n) {
         const int lane = threadIdx.x & 31;
         const uint32_t bar = bars + 8 * s;
+        if (__any_sync(kFull, *dead)) return;  // (*dead: also if this warp's own wait for the stage ran out)
         if (direct(r0)) {
             if (lane == 0) mbar_expect(bar, 0);
             return;
@@ -316,6 +318,12 @@ struct Ring {
         }
     }
     __device__ __forceinline__ void wait(int s, unsigned parity) { mbar_wait(bars + 8 * s, parity, dead); }
+    // No copy may be in flight when the CTA ends.  Nothing was fetched after the wait that ran out had begun: every
+    // copy has had its whole limit, and here a millisecond more.
+    __device__ __forceinline__ void leave() const {
+        if (*dead)
+            for (int w = 0; w < 1000; ++w) __nanosleep(1000);
+    }
 };
 
 template <typename T, int N, bool Vec>
@@ -414,6 +422,7 @@ __global__ void __launch_bounds__(forward_threads(Vec)) k_norm_forward(const Nor
             if (a.stats && t == 0 && col0 == 0) reinterpret_cast<float2 *>(a.stats)[r] = make_float2(near + rest, rstd);
         }
     }
+    ring.leave();
 }
 
 template <typename T, bool Vec, bool Wide, bool Params>
@@ -498,6 +507,7 @@ __global__ void __launch_bounds__(kBackwardThreads) k_norm_backward(const NormAr
         }
         now_s = next_s;
     }
+    ring.leave();
     if (!Params) return;
     float *to = a.parts + (size_t)block * 2 * a.cols + col0;
     const int group = a.group;
