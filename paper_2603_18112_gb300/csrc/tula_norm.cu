@@ -11,6 +11,7 @@
 // Rows come by bulk copies into a ring of shared memory, several ahead (with one row ahead in registers
 // instead, 16384 x 4096 bf16 took 254 us forward and backward where it takes 174 now, and 50000 x 1001 fp32 316
 // instead of 203).
+#include "tula_ring.h"
 #include "tula_tc.cuh"
 
 namespace {
@@ -36,6 +37,7 @@ struct NormArgs {
     int cluster;              // CTAs to a row
     int share;                // columns of a CTA: all, or a multiple of 16 and none without any
     int stages;               // of the ring
+    long long last_copied;    // rows off 16-byte boundaries: the last row that a round which is copied begins with
     int ptype;                // of w and b
     float eps;
 };
@@ -261,8 +263,8 @@ struct GroupSum {
 };
 
 // The ring: stage s holds the rows of one round of the CTA's groups, of each of N matrices.  Rows off 16-byte
-// boundaries come with what shares their first and last 16 bytes; a round that has the matrix's first or last
-// row, beside which there may be nothing, is read directly.  A wait that runs out leaves what is there: the
+// boundaries come with what shares their first and last 16 bytes; a round beside which the matrix may not go on so
+// far is read directly.  A wait that runs out leaves what is there: the
 // others end at once then, nothing more is fetched (a barrier whose phase is not over may not be armed again, nor
 // may a copy be issued over another), and the error word says so.
 template <typename T, int N, bool Vec>
@@ -270,11 +272,11 @@ struct Ring {
     uint32_t at, bars;  // shared addresses
     volatile int *dead;
     int stages, per, bytes;  // rows to a round; bytes of a row
-    long long rows;
+    long long last;          // row that a round which is copied begins with
 
     __device__ __forceinline__ int pitch() const { return Vec ? bytes : (bytes + 15) / 16 * 16 + 16; }
     __device__ __forceinline__ uint32_t place(int s, int m) const { return at + (s * N + m) * per * pitch(); }
-    __device__ __forceinline__ bool direct(long long r0) const { return !Vec && (r0 == 0 || r0 + per >= rows); }
+    __device__ __forceinline__ bool direct(long long r0) const { return !Vec && (r0 == 0 || r0 > last); }
     __device__ __forceinline__ bool joined(long long stride) const { return stride * (long long)sizeof(T) == bytes; }
     static __device__ __forceinline__ unsigned off(const T *p) { return Vec ? 0u : (unsigned)reinterpret_cast<unsigned long long>(p) & 15u; }
     // Where row g of the round that starts with `from` lies.
@@ -295,9 +297,9 @@ struct Ring {
 #pragma unroll
         for (int m = 0; m < N; ++m) {
             if (joined(stride[m]))
-                total += lane == 0 ? (off(from[m]) + n * bytes + 15) / 16 * 16 : 0u;
+                total += lane == 0 ? tula::bytes_copied(off(from[m]), n * bytes) : 0u;
             else
-                for (int g = lane; g < n; g += 32) total += (off(from[m] + g * stride[m]) + bytes + 15) / 16 * 16;
+                for (int g = lane; g < n; g += 32) total += tula::bytes_copied(off(from[m] + g * stride[m]), bytes);
         }
         total = __reduce_add_sync(kFull, total);
         if (lane == 0) mbar_expect(bar, total);
@@ -307,12 +309,12 @@ struct Ring {
             if (joined(stride[m])) {
                 const unsigned o = off(from[m]);
                 if (lane == 0)
-                    bulk_load(place(s, m), reinterpret_cast<const unsigned char *>(from[m]) - o, (o + n * bytes + 15) / 16 * 16, bar);
+                    bulk_load(place(s, m), reinterpret_cast<const unsigned char *>(from[m]) - o, tula::bytes_copied(o, n * bytes), bar);
             } else {
                 for (int g = lane; g < n; g += 32) {
                     const T *p = from[m] + g * stride[m];
                     const unsigned o = off(p);
-                    bulk_load(place(s, m) + g * pitch(), reinterpret_cast<const unsigned char *>(p) - o, (o + bytes + 15) / 16 * 16, bar);
+                    bulk_load(place(s, m) + g * pitch(), reinterpret_cast<const unsigned char *>(p) - o, tula::bytes_copied(o, bytes), bar);
                 }
             }
         }
@@ -357,7 +359,7 @@ __global__ void __launch_bounds__(forward_threads(Vec)) k_norm_forward(const Nor
     const int col0 = blockIdx.x % a.cluster * a.share, cols = min(a.cols - col0, a.share);  // the CTA's share
     const long long block = blockIdx.x / a.cluster, step = (long long)(gridDim.x / a.cluster) * per;
     const int bytes = cols * (int)sizeof(T);
-    Ring<T, 1, Vec> ring{smem_addr(memory), smem_addr(bars), &dead, a.stages, per, bytes, a.rows};
+    Ring<T, 1, Vec> ring{smem_addr(memory), smem_addr(bars), &dead, a.stages, per, bytes, a.last_copied};
     start_ring(ring);
     let_next_start();
     if (a.cluster > 1) cluster_sync();  // the other CTAs' shared memory may be written to from here on
@@ -436,7 +438,7 @@ __global__ void __launch_bounds__(kBackwardThreads) k_norm_backward(const NormAr
     const int col0 = blockIdx.x % a.cluster * a.share, cols = min(a.cols - col0, a.share);  // the CTA's share
     const long long block = blockIdx.x / a.cluster, step = (long long)(gridDim.x / a.cluster) * per;
     const int bytes = cols * (int)sizeof(T);
-    Ring<T, 2, Vec> ring{smem_addr(memory), smem_addr(bars), &dead, a.stages, per, bytes, a.rows};
+    Ring<T, 2, Vec> ring{smem_addr(memory), smem_addr(bars), &dead, a.stages, per, bytes, a.last_copied};
     start_ring(ring);
     let_next_start();
     if (a.cluster > 1) cluster_sync();
@@ -675,6 +677,11 @@ inline int ring_bytes(const Layout &l, bool vec, size_t size, int matrices, int 
     return stages * stage;
 }
 
+// (of a cluster the first CTA's share, at least; all are of some thousand columns)
+inline long long last_copied(const Layout &l, long long rows, size_t size) {
+    return tula::last_round_copied(rows, l.threads / l.group, l.share * (int)size);
+}
+
 inline bool lies(const void *p, long long stride, size_t size) {  // rows on 16-byte boundaries
     return (reinterpret_cast<uintptr_t>(p) | (size_t)stride * size) % 16 == 0;
 }
@@ -692,6 +699,7 @@ int forward_typed(NormArgs &a, cudaStream_t s) {
                                     : (wide ? k_norm_forward<T, false, true> : k_norm_forward<T, false, false>);
     static std::atomic<uint64_t> done[4];
     const int smem = ring_bytes(l, vec, sizeof(T), 1, forward_threads(vec), a.stages);
+    a.last_copied = last_copied(l, a.rows, sizeof(T));
     const int rc = allow_smem((const void *)k, kRingMost, &done[2 * vec + wide]);
     return rc ? rc : tula::launch(k, dim3(l.grid), l.threads, smem, s, l.cluster, a);
 }
@@ -714,6 +722,7 @@ int backward_typed(NormArgs &a, void *dw, void *db, cudaStream_t s) {
         void (*k)(const NormArgs) = a.parts ? backward_kernel<T, true>(vec, wide) : backward_kernel<T, false>(vec, wide);
         static std::atomic<uint64_t> done[8];
         int smem = ring_bytes(l, vec, sizeof(T), 2, kBackwardThreads, a.stages);
+        a.last_copied = last_copied(l, a.rows, sizeof(T));
         if (a.parts && l.threads > l.group) smem = std::max(smem, 2 * l.threads * kN * 4);  // 32 KB
         rc = allow_smem((const void *)k, kRingMost, &done[4 * vec + 2 * wide + (a.parts != nullptr)]);
         if (!rc) rc = tula::launch(k, dim3(l.grid), l.threads, smem, s, l.cluster, a);

@@ -73,3 +73,43 @@ def test_mean_of_rows_of_equal_values(cols):
     # near is off by depth roundings of the value, the rest that is taken out by depth + 4 of that
     depth = _depth(cols)
     assert bool((y.double().abs().amax(1) <= (depth + 4) * U * depth * U * x[:, 0].double().abs() * 1e-5 ** -0.5).all())
+
+
+# --------------------------------------------------------------------------------------------
+# Narrow rows off 16-byte boundaries
+# --------------------------------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows", [1, 255, 256, 257, 513, 769])
+def test_narrow_rows(rows, dtype):
+    """Rows of a few bytes, the matrix and its gradient anywhere within 16 bytes and ending where their memory does."""
+    gen = torch.Generator().manual_seed(rows)
+    for cols in range(1, 8):
+        for start, dstart, more in ((0, 0, 0), (1, 3, 0), (7, 2, 0), (5, 5, 3)):
+            stride = cols + more
+            size = (rows - 1) * stride + cols
+
+            def made(first):
+                flat = torch.randn(first + size, generator=gen).to(dtype).cuda()
+                return flat.as_strided((rows, cols), (stride, 1), first)
+
+            x, dy = made(start), made(dstart)
+            w, b = torch.randn(cols, generator=gen).cuda(), torch.randn(cols, generator=gen).cuda()
+            leaves = [t.requires_grad_() for t in (x.detach(), w, b)]
+            y = norm.layer_norm(leaves[0], w, b, 0.5)
+            grads = torch.autograd.grad(y, leaves, dy)
+            x64, w64, g64 = x.double(), w.detach().double(), dy.double()
+            mean = x64.mean(1, keepdim=True)
+            r = 1 / ((x64 - mean).square().mean(1, keepdim=True) + 0.5).sqrt()
+            n, g = (x64 - mean) * r, g64 * w64
+            dx = r * (g - g.mean(1, keepdim=True) - n * (g * n).mean(1, keepdim=True))
+            want = (n * w64 + b.detach().double(), dx, (g64 * n).sum(0), g64.sum(0))
+            # r is below 1.5 and n below 3 (sqrt(7)): some 10 roundings of what is added up, of columns `rows` of it
+            sizes = ((n * w64).abs() + b.detach().abs() + w64.abs(), r * (g.abs() + g.abs().mean(1, keepdim=True) * (1 + 3 * n.abs())),
+                     (g64.abs() * (n.abs() + 1)).sum(0), g64.abs().sum(0))
+            chain = 30 + min(rows, 16 + 256)
+            for got, ref, size_of, c in zip((y, *grads), want, sizes, (20, 20, chain, chain)):
+                tol = c * U * size_of + 1.01 * ROUND[got.dtype] * ref.abs() + TINY[got.dtype]
+                assert bool(((got.detach().double() - ref).abs() <= tol).all()), (cols, start)
+    assert norm.tula_layer_norm_error() == 0

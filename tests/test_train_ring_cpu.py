@@ -1,6 +1,14 @@
-"""Layer norm's ring of copies when a wait runs out, as a model on the CPU: who arms a barrier and issues copies
-when, with copies that land late or never."""
+"""Layer norm's ring of copies on the CPU.  When a wait runs out, as a model: who arms a barrier and issues copies
+when, with copies that land late or never; and what the copies reach."""
+import os
 import random
+import shutil
+import subprocess
+from pathlib import Path
+
+import pytest
+
+ROOT = Path(__file__).resolve().parent.parent
 
 
 class Cta:
@@ -82,3 +90,15 @@ def test_a_wait_that_runs_out():
     # the model tells: going on, the first warp arms barriers twice, and leaves copies that it has just issued
     died, armed_again, least = _all(False)
     assert died > 500 and armed_again > 0 and least < 0
+
+
+def test_copies_of_rows_off_16_byte_boundaries_stay_within_the_matrix(tmp_path):
+    """By the kernels' own arithmetic (csrc/tula_ring.h), compiled for the host."""
+    cxx = os.environ.get("CXX") or shutil.which("g++") or shutil.which("c++")
+    if not cxx:
+        pytest.skip("no C++ compiler")
+    out = tmp_path / "ranges"
+    subprocess.run([cxx, "-std=c++17", "-O1", "-Wall", "-Wextra", "-Werror", "-I", str(ROOT / "paper_2603_18112_gb300" / "csrc"),
+                    str(ROOT / "tests" / "ring_ranges.cpp"), "-o", str(out)], check=True)
+    copies, outside = map(int, subprocess.run([str(out)], check=True, capture_output=True, text=True, timeout=120).stdout.split())
+    assert copies > 100000 and outside == 0
