@@ -540,6 +540,24 @@ __global__ void __launch_bounds__(kBackwardThreads) k_norm_backward(const NormAr
     }
 }
 
+// Additions one after the other, at most, before a sum is added to the next one's: a sum of n of a sign is off by n
+// roundings in the worst case.
+constexpr int kMostChain = 128;
+
+// N sums over a row's columns, a thread's by itself: add(column, sums).
+template <int N, class Add>
+__device__ __forceinline__ void over_columns(float (&v)[N], int cols, Add add) {
+#pragma unroll
+    for (int m = 0; m < N; ++m) v[m] = 0.f;
+    for (int c0 = threadIdx.x; c0 < cols; c0 += kMostChain * blockDim.x) {
+        float part[N] = {};
+        const int end = min(cols, c0 + kMostChain * (int)blockDim.x);
+        for (int c = c0; c < end; c += blockDim.x) add(c, part);
+#pragma unroll
+        for (int m = 0; m < N; ++m) v[m] += part[m];
+    }
+}
+
 // Rows that registers do not hold: a CTA to a row, which is read three times, or twice, mostly from L2.
 template <typename T>
 __global__ void __launch_bounds__(kMostThreads) k_norm_forward_wide(const NormArgs a) {
@@ -550,15 +568,14 @@ __global__ void __launch_bounds__(kMostThreads) k_norm_forward_wide(const NormAr
     const int cols = a.cols;
     for (long long r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const T *x = static_cast<const T *>(a.x) + r * a.stride;
-        float s = 0.f;
-        for (int c = threadIdx.x; c < cols; c += blockDim.x) s += value(x[c]);
-        const float near = sum(s) / (float)cols;
-        float both[2] = {0.f, 0.f};
-        for (int c = threadIdx.x; c < cols; c += blockDim.x) {
+        float all[1], both[2];
+        over_columns(all, cols, [&](int c, float (&v)[1]) { v[0] += value(x[c]); });
+        const float near = sum(all[0]) / (float)cols;
+        over_columns(both, cols, [&](int c, float (&v)[2]) {
             const float d = value(x[c]) - near;
-            both[0] += d;
-            both[1] = fmaf(d, d, both[1]);
-        }
+            v[0] += d;
+            v[1] = fmaf(d, d, v[1]);
+        });
         sum(both);
         const float rest = both[0] / (float)cols, rstd = rsqrtf(variance(both[1] / (float)cols, rest) + a.eps);
         T *y = static_cast<T *>(a.y) + r * cols;
@@ -579,13 +596,12 @@ __global__ void __launch_bounds__(kMostThreads) k_norm_backward_wide(const NormA
     for (long long r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const T *x = static_cast<const T *>(a.x) + r * a.stride, *dy = static_cast<const T *>(a.dy) + r * a.dy_stride;
         const float2 st = reinterpret_cast<const float2 *>(a.stats)[r];
-        float s1 = 0.f, s2 = 0.f;
-        for (int c = threadIdx.x; c < cols; c += blockDim.x) {
+        float s[2];
+        over_columns(s, cols, [&](int c, float (&v)[2]) {
             const float g = value(dy[c]) * param(a.w, a.ptype, c, 1.f);
-            s1 += g;
-            s2 = fmaf(g, (value(x[c]) - st.x) * st.y, s2);
-        }
-        float s[2] = {s1, s2};
+            v[0] += g;
+            v[1] = fmaf(g, (value(x[c]) - st.x) * st.y, v[1]);
+        });
         sum(s);
         T *dx = static_cast<T *>(a.y) + r * cols;
         for (int c = threadIdx.x; c < cols; c += blockDim.x) {
@@ -624,8 +640,13 @@ __global__ void __launch_bounds__(1024) k_norm_params(const float *parts, int n,
     const long long c = (long long)blockIdx.x * 32 + lane;  // of both gradients
     float v = 0.f;
     if (c < 2ll * cols)
+        for (int i0 = turn; i0 < n; i0 += 32 * kMostChain) {
+            const int end = min(n, i0 + 32 * kMostChain);
+            float part = 0.f;
 #pragma unroll 4
-        for (int i = turn; i < n; i += 32) v += __ldcg(parts + (size_t)i * 2 * cols + c);
+            for (int i = i0; i < end; i += 32) part += __ldcg(parts + (size_t)i * 2 * cols + c);
+            v += part;
+        }
     sums[turn][lane] = v;
     __syncthreads();
     v = sums[lane][turn];  // part `lane` of column `turn`
@@ -640,13 +661,22 @@ __global__ void __launch_bounds__(1024) k_norm_params(const float *parts, int n,
 // Host side
 // ----------------------------------------------------------------------------
 
+// Parts that the sums over so many rows (or rounds of rows) are taken in, at least, so that no chain is longer than
+// kMostChain: a matrix of more rows than that for each CTA has some 4 / kMostChain of it in bf16 more to write and
+// read.  (The limit of their number is far beyond what memory holds.)
+inline long long least_parts(long long rows) { return std::min(up(rows, kMostChain), 1ll << 24); }
+constexpr int kWideParts = 64;  // of wide rows, before those
+inline long long wide_parts(long long rows) {
+    return std::min(std::max(std::min<long long>(kWideParts, up(rows, 64)), least_parts(rows)), 65535ll);
+}
+
 // How rows of so many columns are shared out: the threads of a CTA to a row, the CTAs to one.
 struct Layout {
     int group, threads, cluster, share;  // cluster 0: rows that registers do not hold
     unsigned grid;
     unsigned blocks() const { return grid / (unsigned)std::max(1, cluster); }
 };
-Layout layout_of(long long rows, int cols, int sms, int sm_threads) {
+Layout layout_of(long long rows, int cols, int sms, int sm_threads, bool sums = false) {
     Layout l;
     const long long ctas = up(cols, kMostThreads * kN);
     l.cluster = ctas <= kMostCluster ? (int)ctas : 0;
@@ -658,14 +688,9 @@ Layout layout_of(long long rows, int cols, int sms, int sm_threads) {
         l.grid = (unsigned)std::min<long long>(rows, 4ll * sms);
         return l;
     }
-    const long long per = l.threads / l.group, blocks = std::max(1, sms * (sm_threads / l.threads) / l.cluster);
-    l.grid = (unsigned)(l.cluster * std::min(up(rows, per), blocks));
+    const long long rounds = up(rows, l.threads / l.group), resident = std::max(1, sms * (sm_threads / l.threads) / l.cluster);
+    l.grid = (unsigned)(l.cluster * std::max(std::min(rounds, resident), sums ? least_parts(rounds) : 1));
     return l;
-}
-constexpr int kWideParts = 64;  // of the rows, whose sums are taken apart (wide rows)
-
-unsigned parts_of(const Layout &l, long long rows) {
-    return l.cluster ? l.blocks() : (unsigned)std::min<long long>(kWideParts, up(rows, 64));
 }
 
 // The ring's memory: so much a thread that all threads of an SM take 192 KB.
@@ -710,7 +735,8 @@ void (*backward_kernel(bool vec, bool wide))(const NormArgs) {
 }
 template <typename T>
 int backward_typed(NormArgs &a, void *dw, void *db, cudaStream_t s) {
-    const Layout l = layout_of(a.rows, a.cols, std::max(1, sm_count()), kBackwardThreads);
+    const Layout l = layout_of(a.rows, a.cols, std::max(1, sm_count()), kBackwardThreads, a.parts != nullptr);
+    const long long parts = l.cluster ? (long long)l.blocks() : wide_parts(a.rows);
     int rc = TULA_OK;
     if (l.cluster) {
         a.group = l.group;
@@ -729,13 +755,13 @@ int backward_typed(NormArgs &a, void *dw, void *db, cudaStream_t s) {
     } else {
         if (a.y) rc = tula::launch(k_norm_backward_wide<T>, dim3(l.grid), l.threads, 0, s, 1, a);
         if (!rc && a.parts)
-            rc = tula::launch(k_norm_sums_wide<T>, dim3((unsigned)up(a.cols, 256), parts_of(l, a.rows)), 256, 0, s, 1, a);
+            rc = tula::launch(k_norm_sums_wide<T>, dim3((unsigned)up(a.cols, 256), (unsigned)parts), 256, 0, s, 1, a);
     }
     if (rc || !a.parts) return rc;
     auto params = [&](auto w) {
         using W = decltype(w);
         return tula::launch(k_norm_params<W>, dim3((unsigned)up(2ll * a.cols, 32)), 1024, 0, s, 1, (const float *)a.parts,
-                            (int)parts_of(l, a.rows), a.cols, static_cast<W *>(dw), static_cast<W *>(db));
+                            (int)parts, a.cols, static_cast<W *>(dw), static_cast<W *>(db));
     };
     if (a.ptype == TULA_TYPE_F32) return params(float());
     return a.ptype == TULA_TYPE_BF16 ? params(__nv_bfloat16()) : params(__half());
@@ -774,8 +800,12 @@ int tula_layer_norm(const void *x, int type, int64_t rows, int64_t cols, int64_t
 
 int tula_layer_norm_workspace_size(int64_t rows, int64_t cols, size_t *bytes) {
     if (!bytes || !good_sizes(rows, cols)) return TULA_ERR_ARG;
-    // as many parts as a GPU of up to 256 SMs has CTAs (of 256 threads, two an SM)
-    const long long parts = std::min<long long>(std::max<long long>(rows, 1), 2 * 256);
+    *bytes = 0;
+    if (cols == 0) return TULA_OK;
+    // as many parts as a GPU of up to 256 SMs has CTAs (of 256 threads, two an SM), or more of long sums
+    const Layout l = layout_of(rows, (int)cols, 256, kBackwardThreads);
+    const long long most = std::min<long long>(std::max<long long>(rows, 1), 2 * 256);
+    const long long parts = l.cluster ? std::max(most, least_parts(up(rows, l.threads / l.group))) : wide_parts(std::max<long long>(rows, 1));
     *bytes = (size_t)parts * 2 * (size_t)cols * 4;
     return TULA_OK;
 }

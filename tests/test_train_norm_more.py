@@ -113,3 +113,54 @@ def test_narrow_rows(rows, dtype):
                 tol = c * U * size_of + 1.01 * ROUND[got.dtype] * ref.abs() + TINY[got.dtype]
                 assert bool(((got.detach().double() - ref).abs() <= tol).all()), (cols, start)
     assert norm.tula_layer_norm_error() == 0
+
+
+# --------------------------------------------------------------------------------------------
+# Long sums
+# --------------------------------------------------------------------------------------------
+
+def _backward_sums(t, cols, stats, dw, db):
+    """dweight and dbias alone, of dy = x = t."""
+    rows = t.shape[0]
+    n = norm.tula_layer_norm_workspace_size(rows, cols)
+    space = torch.empty(n, dtype=torch.uint8, device="cuda")
+    norm._call("tula_layer_norm_backward", 0, t.data_ptr(), cols, t.data_ptr(), cols, 0, rows, cols, None, 0, stats.data_ptr(), None,
+               dw.data_ptr(), db.data_ptr(), space.data_ptr(), n)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols", [(1 << 18, 4112), (1 << 16, 65540), ((1 << 22) + 3, 200)])
+def test_gradients_of_parameters_over_many_rows(rows, cols):
+    """Equal rows of 1 + 2^-14 or so: a single chain of additions rounds the same way again and again once its sum
+    is large.  A part takes 128 rows (or rounds of rows), its threads' sums are added up, then the parts, by 32."""
+    value = 1.0 + 0.49 * 2.0 ** (-13 if cols == 4112 else -14)
+    t = torch.full((rows, cols), value, device="cuda")
+    stats = torch.tensor([0.0, 0.75], device="cuda").repeat(rows, 1)  # n = 0.75 t
+    dw, db = torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+    _backward_sums(t, cols, stats, dw, db)
+    v = float(t[0, 0])
+    per = max(1, 256 * 16 // cols)
+    parts = max(512, rows // per // 128)
+    chain = 128 + per + min(128, parts // 32) + parts // 4096 + 10
+    assert bool((db.double() / (rows * v) - 1).abs().max() <= chain * U)
+    assert bool((dw.double() / (rows * v * (0.75 * v)) - 1).abs().max() <= (chain + 2) * U)
+    assert norm.tula_layer_norm_error() == 0
+
+
+@pytest.mark.gpu
+def test_rows_of_2_to_the_24_columns():
+    """The squares' sums of values that each round the same way."""
+    cols = 1 << 24
+    x = torch.full((2, cols), (1.0 + 0.49 * 2.0 ** -9) ** 0.5, device="cuda")
+    x[:, ::2] *= -1
+    dy = x.abs()
+    leaf = x.requires_grad_()
+    y = norm.layer_norm(leaf, None, None)
+    dx, = torch.autograd.grad(y, leaf, dy)
+    v = float(dy[0, 0])
+    r = (v * v + 1e-5) ** -0.5
+    chain = 128 + 256 + 10  # of a thread's 32768 columns by 128, and the CTA's threads
+    tol = (chain + 8) * U
+    assert bool((y.detach().double() / (x.detach().double() * r) - 1).abs().max() <= tol)
+    # dy is constant: dx = r (dy - mean(dy) - n mean(dy n)), both of its terms sums that cancel; each off by that
+    assert float(dx.double().abs().max()) <= 3 * tol * r * v
