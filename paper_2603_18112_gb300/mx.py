@@ -13,6 +13,7 @@ from __future__ import annotations
 import ctypes
 
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
 from .optim import TYPES
@@ -244,6 +245,13 @@ def _on_gpu(*tensors):
         if t.get_device() != dev or dev < 0:
             raise TypeError(f"tensors on one GPU are wanted, got {[str(t.device) for t in tensors]}")
     return dev
+
+
+def _forward_gradient(*tensors):
+    """Whether any of them (or None) is a dual tensor of forward-mode differentiation, whose tangent no call here
+    would carry on.  (Outside of a level that is told by the level alone.)"""
+    return getattr(forward_ad, "_current_level", 0) >= 0 and any(
+        t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors)
 
 
 def _call(name, dev, *args):

@@ -12,7 +12,7 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from .mx import _call as _mx_call
-from .mx import _i64, _on_gpu, _type
+from .mx import _forward_gradient, _i64, _on_gpu, _type
 from .optim import TYPES
 from .tula_ags import _check, _stream_ptr, c_float, c_int, c_size_t, c_void_p, lib
 
@@ -110,6 +110,8 @@ class _LayerNorm(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dy):
         x, weight, stats = ctx.saved_tensors
+        if _forward_gradient(dy):
+            raise NotImplementedError("layer_norm: no forward-mode derivative of the gradients")
         if _kept(x, weight, stats) != ctx.kept or not stats.is_contiguous():
             raise RuntimeError("layer_norm: a hook on saved tensors gave back another tensor than it was given")
         need_x, need_w, need_b, _ = ctx.needs_input_grad
@@ -146,4 +148,6 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.
     if torch.is_grad_enabled() and (x.requires_grad or weight is not None and weight.requires_grad
                                     or bias is not None and bias.requires_grad):
         return _LayerNorm.apply(x, weight, bias, eps)
+    if _forward_gradient(x, weight, bias):
+        raise NotImplementedError("layer_norm: no forward-mode derivative")
     return _forward(x, weight, bias, eps, False)[0]

@@ -1,0 +1,34 @@
+"""Forward-mode differentiation: refused, never an output without its tangent.  On the CPU, the library's calls left
+out."""
+import pytest
+import torch
+from torch.autograd import forward_ad
+
+from paper_2603_18112_gb300 import norm
+
+
+def _dual(t):
+    return forward_ad.make_dual(t, torch.ones_like(t))
+
+
+@pytest.fixture
+def no_library(monkeypatch):
+    for module in (norm,):
+        monkeypatch.setattr(module, "_call", lambda *args: None)
+        monkeypatch.setattr(module, "_on_gpu", lambda *tensors: 0)
+
+
+@pytest.mark.parametrize("recorded", [False, True])
+def test_layer_norm(no_library, recorded):
+    x, w, b = torch.randn(5, 8), torch.ones(8), torch.zeros(8)
+    with forward_ad.dual_level():
+        for args in ((_dual(x), w, b), (x, _dual(w), b), (x, w, _dual(b)), (_dual(x), None, None), (x, w.clone().requires_grad_(), _dual(b))):
+            with torch.set_grad_enabled(recorded), pytest.raises(NotImplementedError):
+                norm.layer_norm(*args)
+        assert norm.layer_norm(x, w, b).shape == x.shape  # a level alone is no reason
+        leaf = x.clone().requires_grad_()
+        y = norm.layer_norm(leaf, w, b)
+        with pytest.raises(NotImplementedError):
+            torch.autograd.grad(y, leaf, _dual(torch.ones_like(y)), retain_graph=True)
+        torch.autograd.grad(y, leaf, torch.ones_like(y))
+    norm.layer_norm(x, w, b)
