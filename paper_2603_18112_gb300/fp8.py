@@ -16,7 +16,7 @@ import ctypes
 import torch
 from torch.autograd.function import once_differentiable
 
-from .mx import _i64, _on_gpu, _Quantised, _type
+from .mx import _forward_gradient, _i64, _on_gpu, _Quantised, _type
 from .mx import _call as _mx_call
 from .tula_ags import _check, _stream_ptr, c_int, c_size_t, c_void_p, lib
 
@@ -203,6 +203,8 @@ class _Linear(torch.autograd.Function):
     def backward(ctx, dy):
         kept, = ctx.saved_tensors
         device = ctx.device
+        if _forward_gradient(dy):
+            raise NotImplementedError("linear: no forward-mode derivative of the gradients")
         if kept.dtype != torch.uint8 or kept.numel() != ctx.end or kept.device != device or not kept.is_contiguous():
             raise RuntimeError("linear: a hook on saved tensors gave back another tensor than it was given")
         (m, n, k), (need_x, need_w), (x_type, w_type) = ctx.sizes, ctx.needs_input_grad[:2], ctx.types
@@ -230,6 +232,8 @@ def linear(x: torch.Tensor, w: torch.Tensor, dtype=torch.float8_e4m3fn, grad_dty
     rows = x if x.dim() == 2 else x.reshape(x.shape[:-1].numel(), x.shape[-1])
     if torch.is_grad_enabled() and (x.requires_grad or w.requires_grad):
         y = _Linear.apply(rows, w, dtype, grad_dtype)
+    elif _forward_gradient(rows, w):
+        raise NotImplementedError("linear: no forward-mode derivative")
     else:
         y = _forward(rows, w, dtype, False, False)[0]
     return y if x.dim() == 2 else y.view(*x.shape[:-1], w.shape[0])

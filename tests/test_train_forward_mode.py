@@ -4,7 +4,7 @@ import pytest
 import torch
 from torch.autograd import forward_ad
 
-from paper_2603_18112_gb300 import norm
+from paper_2603_18112_gb300 import fp8, norm
 
 
 def _dual(t):
@@ -13,7 +13,7 @@ def _dual(t):
 
 @pytest.fixture
 def no_library(monkeypatch):
-    for module in (norm,):
+    for module in (fp8, norm):
         monkeypatch.setattr(module, "_call", lambda *args: None)
         monkeypatch.setattr(module, "_on_gpu", lambda *tensors: 0)
 
@@ -32,3 +32,19 @@ def test_layer_norm(no_library, recorded):
             torch.autograd.grad(y, leaf, _dual(torch.ones_like(y)), retain_graph=True)
         torch.autograd.grad(y, leaf, torch.ones_like(y))
     norm.layer_norm(x, w, b)
+
+
+@pytest.mark.parametrize("recorded", [False, True])
+def test_8_bit_layer(no_library, recorded):
+    x, w = torch.randn(3, 5, 8), torch.ones(4, 8)
+    with forward_ad.dual_level():
+        for args in ((_dual(x), w), (x, _dual(w)), (_dual(x[0]), w), (x, _dual(w.clone().requires_grad_()))):
+            with torch.set_grad_enabled(recorded), pytest.raises(NotImplementedError):
+                fp8.linear(*args)
+        assert fp8.linear(x, w).shape == (3, 5, 4)
+        leaf = w.clone().requires_grad_()
+        y = fp8.linear(x, leaf)
+        with pytest.raises(NotImplementedError):
+            torch.autograd.grad(y, leaf, _dual(torch.ones_like(y)), retain_graph=True)
+        torch.autograd.grad(y, leaf, torch.ones_like(y))
+    fp8.linear(x, w)
