@@ -377,6 +377,8 @@ class _Linear(torch.autograd.Function):
         kept, = ctx.saved_tensors
         if kept.dtype != torch.uint8 or kept.numel() != ctx.end or kept.device != ctx.device or not kept.is_contiguous():
             raise RuntimeError("linear: a hook on saved tensors gave back another tensor than it was given")
+        if _forward_gradient(dy):
+            raise NotImplementedError("linear: no forward-mode derivative of the gradients")
         (m, n, k), (need_x, need_w, _) = ctx.sizes, ctx.needs_input_grad
         dx = dw = None
         q = quantize(dy, rows=need_x, cols=need_w)

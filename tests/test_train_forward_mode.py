@@ -4,7 +4,7 @@ import pytest
 import torch
 from torch.autograd import forward_ad
 
-from paper_2603_18112_gb300 import fp8, norm
+from paper_2603_18112_gb300 import fp8, mx, norm
 
 
 def _dual(t):
@@ -48,3 +48,18 @@ def test_8_bit_layer(no_library, recorded):
             torch.autograd.grad(y, leaf, _dual(torch.ones_like(y)), retain_graph=True)
         torch.autograd.grad(y, leaf, torch.ones_like(y))
     fp8.linear(x, w)
+
+
+def test_gradients_of_the_mxfp4_layer():
+    """(Its output goes through torch's function always, which refuses dual tensors.)"""
+    dy = torch.ones(5, 4)
+
+    class Context:
+        saved_tensors, end, device = (torch.zeros(0, dtype=torch.uint8),), 0, torch.device("cpu")
+        sizes, needs_input_grad = (5, 4, 8), (True, True, False)
+
+    with forward_ad.dual_level():
+        with pytest.raises(NotImplementedError):
+            mx._Linear.backward(Context(), _dual(dy))
+        with pytest.raises(TypeError, match="GPU"):  # goes on
+            mx._Linear.backward(Context(), dy)
