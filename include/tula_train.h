@@ -359,7 +359,7 @@ void tula_muon_default_hparams(tula_muon_hparams *hp);
  *   w = w (1 - lr weight_decay) - lr s O(u)
  * in fp32 but for O, and the copies w rounded to their type.  Gradients are read only.  0 <= momentum < 1;
  * TULA_ERR_ARG for other values, for NaN, for grad_scale outside [2^-100, 2^100], for lr or weight_decay
- * outside [0, 1e30], and for an unknown scale.
+ * outside [0, 1e30], for an unknown scale, and when the current device is not the plan's.
  */
 int tula_muon_step(tula_muon_plan *plan, const tula_muon_hparams *hp, void *stream);
 

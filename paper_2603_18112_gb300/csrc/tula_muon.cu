@@ -1451,6 +1451,7 @@ inline size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
 
 struct tula_muon_plan {
     std::vector<Kin> kin;
+    int dev;  // that it was made on
     Maps maps;
     long long n_tiles;
     const Matrix *matrices;
@@ -1585,7 +1586,8 @@ int tula_muon_plan_create(const tula_muon_matrices *m, void *workspace, size_t w
         std::memset(&plan->maps, 0, sizeof(plan->maps));
         if (z.table) {
             cudaStream_t s = static_cast<cudaStream_t>(stream);
-            cudaError_t e = cudaMemcpyAsync(at, table.data(), table.size() * sizeof(Matrix), cudaMemcpyHostToDevice, s);
+            cudaError_t e = cudaGetDevice(&plan->dev);
+            if (e == cudaSuccess) e = cudaMemcpyAsync(at, table.data(), table.size() * sizeof(Matrix), cudaMemcpyHostToDevice, s);
             if (e == cudaSuccess) e = cudaStreamSynchronize(s);
             if (e != cudaSuccess) return cuda_failed(e);
             if (z.n_tiles && !make_maps(plan->maps, plan->tiles, z.n_tiles)) return cuda_failed(cudaErrorInvalidValue);
@@ -1620,6 +1622,12 @@ int tula_muon_step(tula_muon_plan *plan, const tula_muon_hparams *hp, void *stre
                       hp->ns_steps <= kMostSteps && (hp->scale == TULA_MUON_SCALE_RMS || hp->scale == TULA_MUON_SCALE_ASPECT) &&
                       aligned(hp->record, 4);
     if (!good) return TULA_ERR_ARG;
+    const int n = (int)plan->kin.size();
+    if (!n) return TULA_OK;
+    int dev = 0;
+    const cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return cuda_failed(e);
+    if (dev != plan->dev) return TULA_ERR_ARG;
     StreamArgs st = {};
     st.matrices = plan->matrices;
     st.tiles = plan->tiles;
@@ -1628,7 +1636,6 @@ int tula_muon_step(tula_muon_plan *plan, const tula_muon_hparams *hp, void *stre
     st.mu = (float)hp->momentum;
     st.decay = (float)(1.0 - hp->lr * hp->weight_decay);
     st.nesterov = hp->nesterov != 0;
-    const int n = (int)plan->kin.size();
     long long done = 0;
     for (int i = 0; i < n; i += kMostGroups) {
         const int here = std::min(kMostGroups, n - i);

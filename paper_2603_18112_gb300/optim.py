@@ -117,8 +117,25 @@ def _ptrs(tensors, allowed, numels, index, what):
     return _host_array(c_void_p, "Q", map(_data_ptr, tensors))
 
 
+_get_device = torch._C._cuda_getDevice
+
+
 class _Planned:
     """What plans over fixed tensors have in common: a handle, and memory of their own."""
+
+    def call(self, name, stream, *args):
+        """The library's `name` for this plan and these arguments, on `stream` or the current one of the plan's GPU,
+        which is made current for the call where it is not."""
+        index = self.device.index
+        if isinstance(stream, torch.cuda.Stream) and stream.device.index != index:
+            raise ValueError(f"{name}: tensors on GPU {index}, a stream of {stream.device}")
+        if index != _get_device():
+            with torch.cuda.device(index):
+                return self.call(name, stream, *args)
+        s = _stream_ptr(stream)
+        _check(getattr(_lib(), name)(self.handle, *args, s), name)
+        if s.value != self.last:
+            self.ran_on(s)
 
     def ran_on(self, stream):
         """A call went to this stream, not the one of the call before.  Kernels read the tiles' rows from the
@@ -196,19 +213,13 @@ class GradClipper:
     def norm(self, grad_scale=1.0, max_norm=0.0, stream=None) -> torch.Tensor:
         """|G| / grad_scale, and the coefficient that max_norm would ask for; gradients are read
         only.  Returns the record."""
-        s, plan = _stream_ptr(stream), self._plan
-        _check(_lib().tula_grad_norm(plan.handle, grad_scale, max_norm, self._record, s), "tula_grad_norm")
-        if s.value != plan.last:
-            plan.ran_on(s)
+        self._plan.call("tula_grad_norm", stream, grad_scale, max_norm, self._record)
         return self.record
 
     def clip_(self, max_norm, stream=None) -> torch.Tensor:
         """Scales the gradients in place to a norm of at most max_norm.  Returns the record, whose
         norm is that before clipping."""
-        s, plan = _stream_ptr(stream), self._plan
-        _check(_lib().tula_grad_clip(plan.handle, max_norm, self._record, s), "tula_grad_clip")
-        if s.value != plan.last:
-            plan.ran_on(s)
+        self._plan.call("tula_grad_clip", stream, max_norm, self._record)
         return self.record
 
 
@@ -245,10 +256,7 @@ class AdamWStep:
         hp = self.hp
         hp.lr, hp.eps, hp.weight_decay, hp.grad_scale = lr, eps, weight_decay, grad_scale
         hp.beta1, hp.beta2 = betas
-        s, plan = _stream_ptr(stream), self._plan
-        _check(_lib().tula_adamw_step(plan.handle, self._hp, s), "tula_adamw_step")
-        if s.value != plan.last:
-            plan.ran_on(s)
+        self._plan.call("tula_adamw_step", stream, self._hp)
 
     __call__ = step
 
@@ -331,10 +339,7 @@ class MuonStep:
                     or not record.is_contiguous()):
                 raise TypeError(f"record: {TULA_RECORD_LEN} float32 on {plan.device} are wanted")
             hp.record = record.data_ptr()
-        s = _stream_ptr(stream)
-        _check(_lib().tula_muon_step(plan.handle, self._hp, s), "tula_muon_step")
-        if s.value != plan.last:
-            plan.ran_on(s)
+        plan.call("tula_muon_step", stream, self._hp)
 
     __call__ = step
 
