@@ -247,8 +247,9 @@ int tula_fp8_linear_backward(const tula_fp8_operand *dy, int64_t M, int64_t N, i
                              int grad_code, const void *kept, void *temp, void *dx, int dx_type,
                              void *dw, int dw_type, int need_dx, int need_dw, void *stream);
 
-/* The error word of the 8-bit products, as tula_mx_error. */
+/* The error word of the 8-bit products and its check, as tula_mx_error and tula_mx_check_wait_timeout. */
 int tula_fp8_error(void *stream, int *error_out);
+int tula_fp8_check_wait_timeout(void *stream);
 
 /* ---------------------------------------------------------------------------------------------
  * Layer norm
@@ -281,8 +282,9 @@ int tula_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, i
                              const float *stats, void *dx, void *dweight, void *dbias,
                              void *workspace, size_t workspace_bytes, void *stream);
 
-/* The error word of these kernels, as tula_mx_error. */
+/* The error word of these kernels and its check, as tula_mx_error and tula_mx_check_wait_timeout. */
 int tula_layer_norm_error(void *stream, int *error_out);
+int tula_layer_norm_check_wait_timeout(void *stream);
 
 /* ---------------------------------------------------------------------------------------------
  * Orthogonalised updates (Muon)
@@ -363,8 +365,9 @@ void tula_muon_default_hparams(tula_muon_hparams *hp);
  */
 int tula_muon_step(tula_muon_plan *plan, const tula_muon_hparams *hp, void *stream);
 
-/* The error word of these products, as tula_mx_error. */
+/* The error word of these products and its check, as tula_mx_error and tula_mx_check_wait_timeout. */
 int tula_muon_error(void *stream, int *error_out);
+int tula_muon_check_wait_timeout(void *stream);
 
 #ifdef __cplusplus
 }

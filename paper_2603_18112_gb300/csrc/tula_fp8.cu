@@ -446,6 +446,8 @@ int tula_fp8_linear_backward(const tula_fp8_operand *dy, int64_t M, int64_t N, i
     return rc;
 }
 
+int tula_fp8_check_wait_timeout(void *stream) { return check_wait_timeout(stream); }
+
 int tula_fp8_error(void *stream, int *error_out) { return read_error(stream, error_out); }
 
 }  // extern "C"

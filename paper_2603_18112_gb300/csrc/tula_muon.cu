@@ -1711,6 +1711,8 @@ int tula_orthogonalize(const void *x, int type, int64_t batch, int64_t rows, int
     }
 }
 
+int tula_muon_check_wait_timeout(void *stream) { return check_wait_timeout(stream); }
+
 int tula_muon_error(void *stream, int *error_out) { return read_error(stream, error_out); }
 
 }  // extern "C"

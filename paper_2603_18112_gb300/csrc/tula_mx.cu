@@ -519,9 +519,7 @@ int tula_mx_matmul(const void *a_codes, const void *a_scales, const void *b_code
     return matmul<Codes4>({a_codes, a_scales, 0}, {b_codes, b_scales, 0}, M, N, K, out, out_type, static_cast<cudaStream_t>(stream));
 }
 
-int tula_mx_check_wait_timeout(void *stream) {
-    return tula::launch(k_wait_check, dim3(1), 32, 0, static_cast<cudaStream_t>(stream), 1);
-}
+int tula_mx_check_wait_timeout(void *stream) { return check_wait_timeout(stream); }
 
 int tula_mx_error(void *stream, int *error_out) { return read_error(stream, error_out); }
 

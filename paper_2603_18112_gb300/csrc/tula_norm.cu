@@ -845,6 +845,8 @@ int tula_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, i
     return type == TULA_TYPE_BF16 ? backward_typed<__nv_bfloat16>(a, dweight, dbias, s) : backward_typed<__half>(a, dweight, dbias, s);
 }
 
+int tula_layer_norm_check_wait_timeout(void *stream) { return check_wait_timeout(stream); }
+
 int tula_layer_norm_error(void *stream, int *error_out) { return read_error(stream, error_out); }
 
 }  // extern "C"

@@ -252,6 +252,8 @@ inline int sm_count() {
     return n;
 }
 
+inline int check_wait_timeout(void *stream) { return tula::launch(k_wait_check, dim3(1), 32, 0, static_cast<cudaStream_t>(stream), 1); }
+
 // Reads and clears this translation unit's error word after the work on the stream.
 inline int read_error(void *stream, int *error_out) {
     if (!error_out) return TULA_ERR_ARG;

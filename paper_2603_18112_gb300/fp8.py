@@ -37,6 +37,7 @@ def _lib():
         L.tula_fp8_linear_backward.argtypes = [operand, _i64, _i64, _i64, c_int, c_int, c_void_p, c_void_p, c_void_p, c_int,
                                                c_void_p, c_int, c_int, c_int, c_void_p]
         L.tula_fp8_error.argtypes = [c_void_p, ctypes.POINTER(c_int)]
+        L.tula_fp8_check_wait_timeout.argtypes = [c_void_p]
         _fns = L
     return _fns
 
@@ -85,6 +86,12 @@ def tula_fp8_size(rows: int, cols: int) -> tuple[int, int]:
     a, b = c_size_t(0), c_size_t(0)
     _check(_lib().tula_fp8_size(rows, cols, ctypes.byref(a), ctypes.byref(b)), "tula_fp8_size")
     return a.value, b.value
+
+
+def tula_fp8_check_wait_timeout(stream=None) -> None:
+    """Makes a bounded wait of these kernels run out (about two seconds on the GPU): afterwards
+    tula_fp8_error reports bit 0."""
+    _check(_lib().tula_fp8_check_wait_timeout(_stream_ptr(stream)), "tula_fp8_check_wait_timeout")
 
 
 def tula_fp8_error(stream=None) -> int:

@@ -29,6 +29,7 @@ def _lib():
         L.tula_layer_norm_backward.argtypes = [c_void_p, _i64, c_void_p, _i64, c_int, _i64, _i64, c_void_p, c_int,
                                                c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
         L.tula_layer_norm_error.argtypes = [c_void_p, ctypes.POINTER(c_int)]
+        L.tula_layer_norm_check_wait_timeout.argtypes = [c_void_p]
         _fns = L
     return _fns
 
@@ -43,6 +44,12 @@ def tula_layer_norm_workspace_size(rows: int, cols: int) -> int:
     out = c_size_t(0)
     _check(_lib().tula_layer_norm_workspace_size(rows, cols, ctypes.byref(out)), "tula_layer_norm_workspace_size")
     return out.value
+
+
+def tula_layer_norm_check_wait_timeout(stream=None) -> None:
+    """Makes a bounded wait of these kernels run out (about two seconds on the GPU): afterwards
+    tula_layer_norm_error reports bit 0."""
+    _check(_lib().tula_layer_norm_check_wait_timeout(_stream_ptr(stream)), "tula_layer_norm_check_wait_timeout")
 
 
 def tula_layer_norm_error(stream=None) -> int:

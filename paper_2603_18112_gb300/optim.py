@@ -84,6 +84,7 @@ def _lib():
         L.tula_muon_default_hparams.restype = None
         L.tula_muon_step.argtypes = [c_void_p, ctypes.POINTER(tula_muon_hparams), c_void_p]
         L.tula_muon_error.argtypes = [c_void_p, ctypes.POINTER(c_int)]
+        L.tula_muon_check_wait_timeout.argtypes = [c_void_p]
         i64 = ctypes.c_int64
         L.tula_orthogonalize_workspace_size.argtypes = [i64, i64, i64, ctypes.POINTER(c_size_t)]
         L.tula_orthogonalize.argtypes = [c_void_p, c_int, i64, i64, i64, i64, i64, c_int, c_void_p, c_int,
@@ -373,6 +374,12 @@ def orthogonalize(x: torch.Tensor, steps: int = 5, dtype=torch.bfloat16) -> torc
                                          apart, steps, out.data_ptr(), TYPES[dtype], space.data_ptr(), need.value,
                                          _stream_ptr(None)), "tula_orthogonalize")
     return out
+
+
+def tula_muon_check_wait_timeout(stream=None) -> None:
+    """Makes a bounded wait of these kernels run out (about two seconds on the GPU): afterwards
+    tula_muon_error reports bit 0."""
+    _check(_lib().tula_muon_check_wait_timeout(_stream_ptr(stream)), "tula_muon_check_wait_timeout")
 
 
 def tula_muon_error(stream=None) -> int:
