@@ -331,7 +331,8 @@ typedef struct tula_muon_matrices {
 int tula_muon_workspace_size(const int64_t *rows, const int64_t *cols, int n_matrices, size_t *bytes);
 
 /* A plan, as tula_train_plan_create's: the same contract, errors and lifetime.  A buffer of weights,
- * momentum or copies that the list has twice is TULA_ERR_ARG. */
+ * momentum or copies that shares memory with another of the list is TULA_ERR_ARG (gradients may with each other, and
+ * lie within their own matrix's weights or copy, which then overwrite them). */
 typedef struct tula_muon_plan tula_muon_plan;
 int tula_muon_plan_create(const tula_muon_matrices *matrices, void *workspace, size_t workspace_bytes,
                           void *stream, tula_muon_plan **plan_out);

@@ -27,7 +27,6 @@
 #include "tula_tc.cuh"
 
 #include <cmath>
-#include <functional>
 #include <memory>
 #include <new>
 #include <vector>
@@ -1495,6 +1494,37 @@ bool shapes_of(const int64_t *rows, const int64_t *cols, const std::vector<int> 
     kin.swap(sorted);
     return true;
 }
+// Whether a buffer that is written shares memory with another.  Gradients may with each other, and with their own
+// matrix's weights or copy, which are written after the last reading of them.
+bool overlapping(const std::vector<Matrix> &of, const int64_t *rows, const int64_t *cols) {
+    struct Range {
+        uintptr_t begin, end;
+        bool written;
+        bool holds(const Range &r) const { return begin <= r.begin && r.end <= end; }
+    };
+    std::vector<Range> all;
+    for (size_t i = 0; i < of.size(); ++i) {
+        const Matrix &q = of[i];
+        if (!q.w) continue;
+        auto range = [&](const void *p, int size, bool written) {
+            const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+            return Range{at, at + (uintptr_t)rows[i] * (uintptr_t)cols[i] * (uintptr_t)size, written};
+        };
+        const Range g = range(q.g, type_size(q.gtype), false), w = range(q.w, 4, true), copy = range(q.copy, 2, true);
+        all.push_back(w);
+        all.push_back(range(q.m, 4, true));
+        if (q.copy) all.push_back(copy);
+        if (!w.holds(g) && !(q.copy && copy.holds(g))) all.push_back(g);
+    }
+    std::sort(all.begin(), all.end(), [](const Range &a, const Range &b) { return a.begin < b.begin; });
+    uintptr_t end = 0, end_written = 0;  // of those before
+    for (const Range &r : all) {
+        if (r.begin < (r.written ? end : end_written)) return true;
+        end = std::max(end, r.end);
+        if (r.written) end_written = std::max(end_written, r.end);
+    }
+    return false;
+}
 struct Sizes {
     size_t table, parts, all;
     long long n_tiles;
@@ -1562,22 +1592,13 @@ int tula_muon_plan_create(const tula_muon_matrices *m, void *workspace, size_t w
                 q.vec = m->cols[i] % 2 == 0 && aligned(q.g, two) && aligned(q.m, 8) && aligned(q.w, 8) && aligned(q.copy, 4) ? 2 : 1;
             vec[(size_t)i] = q.vec;
         }
-        // a buffer that two matrices would write
-        std::vector<const void *> written;
-        for (const Matrix &q : of)
-            if (q.w) {
-                written.push_back(q.w);
-                written.push_back(q.m);
-                if (q.copy) written.push_back(q.copy);
-            }
-        std::sort(written.begin(), written.end(), std::less<const void *>());
-        if (std::adjacent_find(written.begin(), written.end()) != written.end()) return TULA_ERR_ARG;
         if (!shapes_of(m->rows, m->cols, &vec, n, plan->kin, which) || !sizes_of(plan->kin, z)) return TULA_ERR_ARG;
         std::vector<int> next(plan->kin.size(), 0);
         std::vector<Matrix> table(z.table / sizeof(Matrix));
         for (int i = 0; i < n; ++i)
             if (which[i] >= 0) table[(size_t)(plan->kin[which[i]].matrix + next[which[i]]++)] = of[(size_t)i];
         if (!workspace || !aligned(workspace, 256) || workspace_bytes < std::max<size_t>(z.all, 256)) return TULA_ERR_WORKSPACE;
+        if (overlapping(of, m->rows, m->cols)) return TULA_ERR_ARG;
         unsigned char *at = static_cast<unsigned char *>(workspace);
         plan->n_tiles = z.n_tiles;
         plan->matrices = reinterpret_cast<const Matrix *>(at);
