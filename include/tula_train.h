@@ -260,7 +260,8 @@ int tula_fp8_check_wait_timeout(void *stream);
  * elements), mean and var (the mean of (x - mean)^2) over its cols elements, r = 1 / sqrt(var + eps);
  * y device [rows][cols] of `type`.  weight and bias: device [cols] of param_type, or NULL (1 and 0).
  * stats: device fp32 [rows][2], mean and r for the backward pass, or NULL.  In fp32, rounded once (the
- * squares of x - mean have to lie in its range).  A row with an infinity or NaN gives NaN.  rows below
+ * sum of x and those of x - mean and its square have to lie in its range); errors are of the size of x - mean, not
+ * of x, but for the mean in stats, which is one fp32 number.  A row with an infinity or NaN gives NaN.  rows below
  * 2^40, cols up to 2^24, eps >= 0 (TULA_ERR_ARG).
  */
 int tula_layer_norm(const void *x, int type, int64_t rows, int64_t cols, int64_t stride,
@@ -312,8 +313,9 @@ int tula_orthogonalize(const void *x, int type, int64_t batch, int64_t rows, int
                        void *workspace, size_t workspace_bytes, void *stream);
 
 /* A list of matrices.  HOST arrays of n_matrices entries, read by tula_muon_plan_create only; what
- * they point to is device memory, contiguous [rows][cols], aligned to its element (matrices whose
- * columns are a multiple of eight and whose buffers all start at 16 bytes move eight at a time). */
+ * they point to is device memory, contiguous [rows][cols], aligned to its element (matrices whose columns are a
+ * multiple of eight, whose weights start at 32 bytes and whose other buffers start at 16 move eight at a time, and
+ * the last product writes their weights). */
 typedef struct tula_muon_matrices {
     int n_matrices;
     const int64_t *rows, *cols;        /* >= 0 (0: skipped), up to 2^20 */

@@ -1473,7 +1473,8 @@ bool shapes_of(const int64_t *rows, const int64_t *cols, const std::vector<int> 
         ++kin[k].count;
         which[i] = (int)k;
     }
-    // small ones last, and the longest sums first, so that the last blocks to be taken are short ones
+    // those that the last product finishes first (see run), and the longest sums first, so that the last blocks to be
+    // taken are short ones
     std::vector<int> order(kin.size()), where(kin.size());
     for (size_t k = 0; k < kin.size(); ++k) order[k] = (int)k;
     std::stable_sort(order.begin(), order.end(),
