@@ -10,6 +10,7 @@
 //   k_product      A = X X^T;  B = a I + b A + c A^2;  X' = B X: three launches a step.  The last one writes
 //                  the weights and their copies, or the values themselves
 //   k_muon_last    does that for matrices whose rows do not lie on 32-byte boundaries
+//   k_gram_sum     A of matrices with a side beyond 65536, whose sums are taken in parts
 //   k_muon_small   all of it for matrices that a CTA's shared memory holds
 //
 // One launch covers all matrices of a list.  The products are nearly all of the work: per step 2 n^2 m and
@@ -39,6 +40,10 @@ constexpr int kMostGroups = 32;    // shapes of one launch
 constexpr int kMostSteps = 100;
 constexpr long long kMostSide = 1LL << 20;
 constexpr long long kMostTiles = 1LL << 24;  // of a workspace: rows of 128 bytes fit an int
+// Elements that A's sums run over at a time.  The tensor cores cut their fp32 sums off, 16 products at a time, so that
+// a sum of squares loses up to 2^-23 of itself with each: O of 2^20 x 1 was 5e-3 off with one sum, three times what
+// fp16 operands leave.  Parts are rounded to fp16 and added in fp32, which costs less than the sum's own rounding.
+constexpr int kMostSum = 65536;
 
 // ----------------------------------------------------------------------------
 // Products
@@ -902,6 +907,37 @@ __device__ __forceinline__ void last_tile(const StreamArgs &a, const Place &p, c
     }
     finish_tile<Plan, V>(a, p, q, x);
 }
+// A tile of A from its parts, in the first one's place; matrices `step` tiles apart.
+__global__ void __launch_bounds__(kStreamThreads) k_gram_sum(unsigned char *tiles, const float *record, int base, int step, int gram_tiles,
+                                                             int parts) {
+    let_next_start();
+    wait_for_previous();
+    if (record && record[TULA_RECORD_FINITE] == 0.f) return;
+    const int matrix = blockIdx.x / gram_tiles, tile = blockIdx.x - matrix * gram_tiles;
+    unsigned char *const first = tiles + (size_t)(base + matrix * step + tile) * kTileBytes + threadIdx.x * 16;
+#pragma unroll
+    for (int at = 0; at < kTileBytes; at += kStreamThreads * 16) {
+        float f[8] = {};
+        for (int p = 0; p < parts; ++p) {
+            const uint4 q = __ldcg(reinterpret_cast<const uint4 *>(first + (size_t)p * gram_tiles * kTileBytes + at));
+            __half2 h[4];
+            memcpy(h, &q, 16);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float2 v = __half22float2(h[k]);
+                f[2 * k] += v.x;
+                f[2 * k + 1] += v.y;
+            }
+        }
+        __half2 h[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) h[k] = __floats2half2_rn(f[2 * k], f[2 * k + 1]);
+        uint4 q;
+        memcpy(&q, h, 16);
+        *reinterpret_cast<uint4 *>(first + at) = q;
+    }
+}
+
 template <bool Plan>
 __global__ void __launch_bounds__(kStreamThreads, kStreamCtas<Plan>) k_muon_last(const __grid_constant__ StreamArgs a) {
     let_next_start();
@@ -1237,6 +1273,10 @@ struct Kin {
     int gram_rows() const { return (int)up(n(), kTile); }
     int gram_cols() const { return (int)up(n(), kTileCols); }
     int gram_tiles() const { return gram_rows() * gram_cols(); }
+    // parts of A's sums, tiles of X from one to the next, and a part's stages
+    int parts() const { return (int)up(std::max(rows, cols), kMostSum); }
+    int part_step() const { return wide() ? kMostSum / kTileCols : kMostSum / kTile * tile_cols(); }
+    int part_stages(int p) const { return (int)up(std::min<long long>(std::max(rows, cols) - (long long)p * kMostSum, kMostSum), 64); }
     // 2^s, s the whole part of log2(sqrt(rows cols)), at most 15: no element of X, 1 at most, leaves fp16's range
     int shift() const { return std::min(15, (int)std::floor(0.5 * std::log2((double)rows * (double)cols))); }
 };
@@ -1258,12 +1298,13 @@ long long place(std::vector<Kin> &kin) {
     if (all_small(kin)) return 0;
     for (Kin &k : kin) {
         const long long x = (long long)k.tile_rows() * k.tile_cols() * k.count, a = (long long)k.gram_rows() * k.gram_cols() * k.count;
-        if (at + 2 * x + 2 * a >= kMostTiles) return -1;
+        const long long all = 2 * x + a * (k.parts() + 1);
+        if (at + all >= kMostTiles) return -1;
         k.x0 = (int)at;
         k.x1 = (int)(at + x);
         k.gram = (int)(at + 2 * x);
-        k.poly = (int)(at + 2 * x + a);
-        at += 2 * x + 2 * a;
+        k.poly = (int)(at + 2 * x + a * k.parts());
+        at += all;
     }
     return at;
 }
@@ -1302,17 +1343,19 @@ int launch_product(const Maps &maps, ProductArgs &a, int sms, cudaStream_t s) {
                         maps.out, a);
 }
 
-// One product of all shapes.  x: X's first tiles are x0 (0) or x1 (1); first: of the first step.
+// One product of all shapes (of A the sums' first part), or, part0 > 0, of one shape's A the parts from there on.  x:
+// X's first tiles are x0 (0) or x1 (1); first: of the first step.
 template <bool Pair>
-int fill(ProductArgs &a, const Kin *kin, int n, Kind kind, int x, bool first) {
+int fill(ProductArgs &a, const Kin *kin, int n, Kind kind, int x, bool first, int part0) {
     constexpr int kSide = Shape<Pair>::kSide;
     long long blocks = 0;
-    a.n_groups = n;
-    for (int i = 0; i < n; ++i) {
-        const Kin &k = kin[i];
+    a.n_groups = part0 ? kin->parts() - part0 : n;
+    for (int i = 0; i < a.n_groups; ++i) {
+        const Kin &k = kin[part0 ? 0 : i];
+        const int part = part0 ? part0 + i : 0;
         ProductGroup &g = a.g[i];
-        const Side sx = {x ? k.x1 : k.x0, k.tiles(), k.tile_cols(), k.tile_rows(), kAlong};
-        const Side sa = {k.gram, k.gram_tiles(), k.gram_cols(), k.gram_rows(), kSymmetric};
+        const Side sx = {(x ? k.x1 : k.x0) + part * k.part_step(), k.tiles(), k.tile_cols(), k.tile_rows(), kAlong};
+        const Side sa = {k.gram, k.gram_tiles() * k.parts(), k.gram_cols(), k.gram_rows(), kSymmetric};
         const Side sb = {k.poly, k.gram_tiles(), k.gram_cols(), k.gram_rows(), kSymmetric};
         Side across = sx;
         across.way = kAcross;
@@ -1337,8 +1380,8 @@ int fill(ProductArgs &a, const Kin *kin, int n, Kind kind, int x, bool first) {
             if (first) g.alpha = (float)std::ldexp(1.0, -k.shift());
         } else {
             g.p = g.q = kind == kPoly ? sa : k.wide() ? sx : across;
-            g.out = kind == kPoly ? k.poly : k.gram;
-            g.out_step = k.gram_tiles();
+            g.out = kind == kPoly ? k.poly : k.gram + part * k.gram_tiles();
+            g.out_step = kind == kPoly ? k.gram_tiles() : k.gram_tiles() * k.parts();
             g.out_pitch = k.gram_cols();
             g.out_rows = k.gram_rows();
             g.blocks_m = g.blocks_n = (int)up(k.n(), kSide);
@@ -1346,7 +1389,7 @@ int fill(ProductArgs &a, const Kin *kin, int n, Kind kind, int x, bool first) {
             for (int c = 0; c < g.blocks_n; ++c) per += column_blocks<kSide>(c, g.blocks_n);
             if (per >= (1LL << 30)) return -1;
             g.per = (int)per;
-            g.n_k = (int)up(kind == kPoly ? k.n() : std::max(k.rows, k.cols), 64);
+            g.n_k = kind == kPoly ? (int)up(k.n(), 64) : k.part_stages(part);
             if (first && kind == kGram) g.alpha = (float)std::ldexp(1.0, -2 * k.shift());
         }
         g.first = (int)blocks;
@@ -1357,17 +1400,30 @@ int fill(ProductArgs &a, const Kin *kin, int n, Kind kind, int x, bool first) {
     return (int)blocks;
 }
 template <Kind K>
-int product(const Maps &maps, ProductArgs &a, const Kin *kin, int n, int x, bool first, int sms, cudaStream_t s) {
-    const int pairs = fill<true>(a, kin, n, K, x, first);
-    const int singles = fill<false>(a, kin, n, K, x, first);
+int product(const Maps &maps, ProductArgs &a, const Kin *kin, int n, int x, bool first, int sms, cudaStream_t s, int part0 = 0) {
+    const int pairs = fill<true>(a, kin, n, K, x, first, part0);
+    const int singles = fill<false>(a, kin, n, K, x, first, part0);
     if (pairs < 0 || singles < 0) return TULA_ERR_ARG;
     // Blocks of 128 where each SM has one at most (1024 x 1024: 127 us, 153 by pairs); else pairs of CTAs where they need no more rounds, since a
     // round takes as long.
     if (singles > sms && up(pairs, std::max(1, sms / 2)) <= up(singles, sms)) {
-        fill<true>(a, kin, n, K, x, first);
+        fill<true>(a, kin, n, K, x, first, part0);
         return launch_product<true, K>(maps, a, sms, s);
     }
     return launch_product<false, K>(maps, a, sms, s);
+}
+// A: its sums' first parts, those of long sides, and their sums.
+int gram(const Maps &maps, ProductArgs &a, const Kin *kin, int n, int x, bool first, unsigned char *tiles, int sms, cudaStream_t s) {
+    int rc = product<kGram>(maps, a, kin, n, x, first, sms, s);
+    for (int i = 0; !rc && i < n; ++i) {
+        const Kin &k = kin[i];
+        if (k.parts() == 1) continue;
+        rc = product<kGram>(maps, a, &k, 1, x, first, sms, s, 1);
+        if (!rc)
+            rc = tula::launch(k_gram_sum, dim3((unsigned)(k.gram_tiles() * k.count)), kStreamThreads, 0, s, 1, tiles, a.record, k.gram,
+                              k.gram_tiles() * k.parts(), k.gram_tiles(), k.parts());
+    }
+    return rc;
 }
 
 // Small matrices, without a workspace.
@@ -1430,7 +1486,7 @@ int run(const Maps &maps, long long n_tiles, const Kin *kin, int n, StreamArgs &
     int rc = tula::launch(plan ? k_muon_first<true> : k_muon_first<false>, dim3((unsigned)tiles), kStreamThreads, 0, s, 1, st);
     if (!rc) rc = tula::launch(plan ? k_muon_scale<true> : k_muon_scale<false>, dim3((unsigned)tiles), kStreamThreads, 0, s, 1, st);
     for (int i = 0; !rc && i < steps; ++i) {
-        rc = product<kGram>(maps, a, kin, n, i & 1, i == 0, sms, s);
+        rc = gram(maps, a, kin, n, i & 1, i == 0, st.tiles, sms, s);
         if (!rc) rc = product<kPoly>(maps, a, kin, n, i & 1, i == 0, sms, s);
         if (!rc)
             rc = i == steps - 1 ? product<kLast>(maps, a, kin, n, i & 1, i == 0, sms, s)
