@@ -295,9 +295,14 @@ int tula_layer_norm_check_wait_timeout(void *stream);
  * O(u): u / |u| (the Frobenius norm; a matrix of zeros stays) and then ns_steps of
  *   X <- a X + b A X + c A^2 X,  A = X X^T,  (a, b, c) = (3.4445, -4.7750, 2.0315)
  * which bring the singular values near 1 (to 0.7 to 1.2 in five steps) and leave the singular vectors.
- * Operands are held in fp16 and summed in fp32, so that values are within about 2e-3 of the formula's
- * relative to the matrix's norm (up to 5e-3 where the smaller side is a few; more where singular values lie
- * far below the largest one: a rounding of 2^-12 of that grows with them).  A matrix with an infinity or NaN gives NaN.
+ * Operands are held in fp16 and summed in fp32: X, A and B are rounded in each step.  Relative to its norm O is
+ * then off by
+ *   0.5 to 2e-3   where most singular values are within 20 of the largest one,
+ *   up to 1e-2    where the smaller side is 2 to 7 (a few values, whose roundings do not average),
+ *   more          the more of them lie far below the largest ones, whose roundings grow with the small ones: 3e-3 for
+ *                 1, 1/2, 1/3, ..., 2e-2 for their squares, 2 to 5e-2 with four 1000 times the others;
+ * but for narrow matrices always by about as much as rounding the matrix to bf16 moves O, or less (a seventh of it in
+ * the last two).  A matrix with an infinity or NaN gives NaN.
  */
 
 /*

@@ -16,8 +16,10 @@
 // One launch covers all matrices of a list.  The products are nearly all of the work: per step 2 n^2 m and
 // 2 n^3 operations of which symmetry leaves half, and 2 n^2 m.  They run on the tensor cores from fp16
 // operands with fp32 sums.  Why fp16: all values are bounded (singular values of at most about 1.2, so
-// elements too), and its 11 bits leave the result 1 to 2e-3 off, where bf16's 8 leave it 1e-2 off; the first
-// step's X, whose elements are about 1 / sqrt(n m), is kept larger by a power of two.  B takes in a I before
+// elements too), and its 11 bits leave the result 1 to 2e-3 off, where bf16's 8 leave it 1e-2 off, for singular values
+// within 20 of the largest (a rounding of 2^-12 of that falls on the others and grows with them by up to 3.4445 a step:
+// 2e-2 for values that fall off like 1 / k^2, where rounding the matrix itself to bf16 moves the result by 0.15); the
+// first step's X, whose elements are about 1 / sqrt(n m), is kept larger by a power of two.  B takes in a I before
 // it is rounded: then its diagonal is near 0.7 instead of -2.7, and X need not be added afterwards.
 //
 // Matrices lie in the workspace as tiles of 128 rows by 64 columns, 16 KB each, zero beyond the matrix, and
