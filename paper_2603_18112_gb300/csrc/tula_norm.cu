@@ -661,13 +661,15 @@ __global__ void __launch_bounds__(1024) k_norm_params(const float *parts, int n,
 // Host side
 // ----------------------------------------------------------------------------
 
-// Parts that the sums over so many rows (or rounds of rows) are taken in, at least, so that no chain is longer than
-// kMostChain: a matrix of more rows than that for each CTA has some 4 / kMostChain of it in bf16 more to write and
-// read.  (The limit of their number is far beyond what memory holds.)
-inline long long least_parts(long long rows) { return std::min(up(rows, kMostChain), 1ll << 24); }
-constexpr int kWideParts = 64;  // of wide rows, before those
+// Parts that the sums over so many rounds of rows are taken in, at least: none is of more than kMostRounds, so that a
+// matrix of more than that for each CTA has more CTAs than there is room for at a time.  (2^17 x 4096 bf16 backward:
+// 711 us as one chain, 732 with 256, 753 with 128; the threads' sums held in memory from time to time instead, 786,
+// and fewer registers for all.  The limit of their number is far beyond what memory holds.)
+constexpr int kMostRounds = 2 * kMostChain;
+inline long long least_parts(long long rounds) { return std::min(up(rounds, kMostRounds), 1ll << 24); }
+// Those of wide rows, of kMostChain at most.
 inline long long wide_parts(long long rows) {
-    return std::min(std::max(std::min<long long>(kWideParts, up(rows, 64)), least_parts(rows)), 65535ll);
+    return std::min(std::max(std::min(64ll, up(rows, 64)), up(rows, kMostChain)), 65535ll);
 }
 
 // How rows of so many columns are shared out: the threads of a CTA to a row, the CTAs to one.
@@ -689,7 +691,10 @@ Layout layout_of(long long rows, int cols, int sms, int sm_threads, bool sums = 
         return l;
     }
     const long long rounds = up(rows, l.threads / l.group), resident = std::max(1, sms * (sm_threads / l.threads) / l.cluster);
-    l.grid = (unsigned)(l.cluster * std::max(std::min(rounds, resident), sums ? least_parts(rounds) : 1));
+    long long blocks = std::min(rounds, resident);
+    // (whole waves: 2^18 x 4112 bf16 by 2048 CTAs 2.95 ms, by 14 for each SM 2.91)
+    if (sums && least_parts(rounds) > resident) blocks = up(least_parts(rounds), resident) * resident;
+    l.grid = (unsigned)(l.cluster * blocks);
     return l;
 }
 
@@ -804,8 +809,10 @@ int tula_layer_norm_workspace_size(int64_t rows, int64_t cols, size_t *bytes) {
     if (cols == 0) return TULA_OK;
     // as many parts as a GPU of up to 256 SMs has CTAs (of 256 threads, two an SM), or more of long sums
     const Layout l = layout_of(rows, (int)cols, 256, kBackwardThreads);
-    const long long most = std::min<long long>(std::max<long long>(rows, 1), 2 * 256);
-    const long long parts = l.cluster ? std::max(most, least_parts(up(rows, l.threads / l.group))) : wide_parts(std::max<long long>(rows, 1));
+    const long long resident = 2 * 256, least = l.cluster ? least_parts(up(rows, l.threads / l.group)) : 0;
+    long long parts = std::min(std::max<long long>(rows, 1), resident);
+    if (least > 1) parts = std::max(parts, least + resident);
+    if (!l.cluster) parts = wide_parts(std::max<long long>(rows, 1));
     *bytes = (size_t)parts * 2 * (size_t)cols * 4;
     return TULA_OK;
 }
