@@ -151,7 +151,8 @@ int tula_mx_dequantize(const void *codes, const void *scales, int64_t rows, int6
 /*
  * out = A B^T, A an M x K and B an N x K matrix in MXFP4; out device [M][N] of `out_type`.
  * Products of codes and scales are exact and added in fp32 by the tensor cores in an order that
- * depends on M, N and K only; the sum is rounded once.  A row with a NaN scale gives NaN.
+ * depends on M, N and K only; the sum is rounded once.  (They cut their sums off, with every 64 columns: a sum of
+ * one sign may lose K 2^-29 of itself.)  A row with a NaN scale gives NaN.
  * M, N, K >= 0 (K = 0 gives zeros).
  */
 int tula_mx_matmul(const void *a_codes, const void *a_scales, const void *b_codes,
@@ -214,7 +215,8 @@ int tula_fp8_dequantize(const void *codes, const void *scales, int64_t rows, int
 /*
  * out = A B^T, A an M x K and B an N x K matrix of 8-bit codes (each of its own kind of code); out
  * device [M][N] of `out_type`.  As tula_mx_matmul: products of codes and scales are exact and added in
- * fp32 by the tensor cores in an order that depends on M, N and K only; the sum is rounded once.
+ * fp32 by the tensor cores in an order that depends on M, N and K only; the sum is rounded once.  (Here sums are
+ * cut off with every 32 columns: K 2^-28.)
  */
 int tula_fp8_matmul(const void *a_codes, const void *a_scales, int a_code, const void *b_codes,
                     const void *b_scales, int b_code, int64_t M, int64_t N, int64_t K, void *out,

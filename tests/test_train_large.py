@@ -3,7 +3,7 @@ the far end against the same by itself."""
 import pytest
 import torch
 
-from paper_2603_18112_gb300 import fp8
+from paper_2603_18112_gb300 import fp8, mx
 from paper_2603_18112_gb300 import optim as O
 from test_train_fp8 import E4, E5
 from test_train_muon import U, _near, _off, _updates
@@ -120,3 +120,23 @@ def test_products_of_many_outputs():
     for rows in (slice(0, 200), slice(35000, 35100), slice(69800, 70001)):
         assert torch.equal(y[rows], (x64[rows] @ w64.t()).bfloat16())
     assert fp8.tula_fp8_error() == 0
+
+
+@pytest.mark.parametrize("m,n", [(1, 64), (64, 64), (2048, 4096)])
+@pytest.mark.parametrize("module,lost", [(fp8, 2.0 ** -28), (mx, 2.0 ** -29)])
+def test_sums_of_one_sign_over_2_to_the_19_columns(module, lost, m, n):
+    """What the tensor cores cut off: a unit in fp32's last place, 2^-23, with every instruction of 32 columns (4
+    bits: 64); and the last rounding."""
+    k = 1 << 19
+    gen = torch.Generator(device="cuda").manual_seed(11)
+
+    def made(rows):
+        x = torch.rand(rows, k, generator=gen, device="cuda") + 0.5
+        x *= torch.exp2(torch.randint(-3, 4, (1, k // 128), generator=gen, device="cuda").float()).repeat_interleave(128, 1)
+        return module.quantize(x)
+
+    a, b = made(m), made(n)
+    got = module.matmul(a, b, torch.float32).double()
+    x, w = module.dequantize(a, torch.float32), module.dequantize(b, torch.float32)
+    want = sum(x[:, c:c + 8192].double() @ w[:, c:c + 8192].double().t() for c in range(0, k, 8192))
+    assert float((got / want - 1).abs().max()) <= k * lost + U
