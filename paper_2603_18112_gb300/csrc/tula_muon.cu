@@ -1252,6 +1252,11 @@ __global__ void __launch_bounds__(kStreamThreads, 1) k_muon_small(const __grid_c
             default: small_store<1>(a, p, q, tiles, x);
         }
     }
+    // No product may be under way when tensor memory is given back.  Where a wait has run out the others did not wait:
+    // a millisecond is far more than they take.
+    if (dead)
+        for (int w = 0; w < 1000; ++w) __nanosleep(1000);
+    __syncwarp();
     if (warp == 0) tmem_free(m.tmem, kSmallSums);
 }
 
