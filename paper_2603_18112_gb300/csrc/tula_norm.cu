@@ -264,9 +264,9 @@ struct GroupSum {
 
 // The ring: stage s holds the rows of one round of the CTA's groups, of each of N matrices.  Rows off 16-byte
 // boundaries come with what shares their first and last 16 bytes; a round beside which the matrix may not go on so
-// far is read directly.  A wait that runs out leaves what is there: the
-// others end at once then, nothing more is fetched (a barrier whose phase is not over may not be armed again, nor
-// may a copy be issued over another), and the error word says so.
+// far is read directly.  A wait that runs out leaves what is there: the others end at once then, nothing more is
+// fetched (a barrier whose phase is not over may not be armed again, nor may a copy be issued over another), and
+// the error word says so.
 template <typename T, int N, bool Vec>
 struct Ring {
     uint32_t at, bars;  // shared addresses
@@ -340,7 +340,7 @@ __device__ __forceinline__ void start_ring(const Ring<T, N, Vec> &ring) {
 
 // The mean comes in two parts: `near` is off by the roundings of its sum, each of them one of the row's size, and
 // what the differences to it add up to, the rest of the mean, is that but for roundings of the differences' size.
-// So a row of equal values gives b, and a row's offset costs no digits.  (From `near` alone 1000 columns of 1000.0
+// So a row of equal values gives b (but for 1e-9), and a row's offset costs no digits.  (From `near` alone 1000 columns of 1000.0
 // had a mean of 1000.00006 and outputs of -0.019 w + b.)  The variance about near + rest from the mean of the
 // squares about near; a NaN stays.
 __device__ __forceinline__ float variance(float squares, float rest) {
